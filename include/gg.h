@@ -549,6 +549,62 @@ int gg_sage_forward(const gg_wsample_t* smp, int64_t num_nodes, int32_t W, int32
                     const gg_sage_layer_t* layers_h, float* out_d, int64_t out_rows_cap,
                     int32_t* status_d, void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators of models that learn rows and train on the consumer's answers:
+ * embedding rows and their gradient, RMS norm with 8-bit rows, and the
+ * distillation loss of a teacher's top logits.
+ * ------------------------------------------------------------------------- */
+
+#define GG_BF16 2
+#define GG_E4M3 3             /* 8-bit floating point (4 exponent, 3 mantissa bits, no infinities) */
+#define GG_MIN_GROUP 16       /* elements that share a scale of 8-bit rows: a power of two */
+#define GG_MAX_GROUP 256
+
+/* A matrix of rows on the device: row r's elements lie back to back at
+ * data + r * stride (bytes; any multiple of the element's size, 0 for an input
+ * whose rows are all the same one).  8-bit rows (GG_E4M3) stand for code *
+ * scale; row r's fp32 scales lie at scales + r * scales_stride, one per
+ * `group` elements (the last group may be shorter), or one per row (group 0).
+ * Codes and scales may share rows, the scales behind the codes at the next
+ * multiple of 4: opaque rows that the fetch path moves whole. */
+typedef struct gg_rows {
+  void* data;
+  int64_t stride;
+  int32_t dtype;          /* GG_F32, GG_F16, GG_BF16 or GG_E4M3 */
+  int32_t group;          /* GG_E4M3 only */
+  void* scales;           /* GG_E4M3 only */
+  int64_t scales_stride;
+} gg_rows_t;
+
+#define GG_EMBED_MAX_DIM 32768
+#define GG_EMBED_ADD 1    /* gg_embed_backward adds to the rows instead of writing them */
+
+/* Embedding lookup: out[i] = scale * table[ids[i]], i < n, rounded once to
+ * out's type.  ids_d: int32 or int64 (id_bits), or NULL for the rows 0 .. n-1
+ * in order (8-bit rows that the fetch path gathered, back to fp32).  An id of
+ * -1 (the padding of neighbour lists) gives a row of zeros, any other id
+ * outside [0, num_rows) too, and sets GG_DEV_BAD_ID.  table: any type; out:
+ * GG_F32, GG_F16 or GG_BF16, and no memory of the table's. */
+int gg_embed_forward(const gg_rows_t* table, int64_t num_rows, int32_t dim, const void* ids_d,
+                     int32_t id_bits, int64_t n, float scale, const gg_rows_t* out,
+                     int32_t* status_d, hipStream_t stream);
+
+size_t gg_ws_embed(int64_t n, int64_t num_rows, int32_t dim);
+
+/* Its gradient: grad[v] = scale * (sum of dy[i] over the i with ids[i] = v), for
+ * every row v < num_rows (zeros where no id is v), rounded once to grad's
+ * type.  With GG_EMBED_ADD the sum is added to what grad[v] holds, and only
+ * rows that occur among the ids are read and written: gradients of a tied
+ * table, or, with scale = -rate, a gradient step on the table itself.  Ids of -1
+ * and ids out of range (GG_DEV_BAD_ID) add nothing.  The ids are sorted and
+ * every row's terms are added in fp32 in an order that depends on the ids
+ * alone, so results are reproducible bit for bit.  n and num_rows are at most
+ * 2^31 - 2. */
+int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t id_bits, int64_t n,
+                      int64_t num_rows, int32_t dim, float scale, const gg_rows_t* grad,
+                      int32_t flags, int32_t* status_d, void* ws, size_t ws_bytes,
+                      hipStream_t stream);
+
 /* Helpers. */
 
 /* Reads the sticky device status word once the work queued so far on

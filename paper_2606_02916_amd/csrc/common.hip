@@ -2,6 +2,7 @@
 #include <string.h>
 
 #include "gg_host.hpp"
+#include "rows.hpp"
 
 namespace gg {
 
@@ -122,6 +123,38 @@ int resolve_tuning(const gg_tuning_t* t, Tune* out) {
   out->mark_min_slots = t->mark_min_slots == 0 ? (int64_t)out->mark_slice_chunks * 2048
                         : t->mark_min_slots < 0 ? 0
                                                 : t->mark_min_slots;
+  return GG_OK;
+}
+
+int pack_rows(const gg_rows_t* r, const char* name, int64_t n, int64_t dim, uint32_t types,
+              bool written, KRows* out) {
+  GG_REQUIRE(r != nullptr, "%s: no rows given", name);
+  GG_REQUIRE(r->dtype >= 0 && r->dtype < 32 && ((types >> r->dtype) & 1u), "%s: dtype %d unsupported",
+             name, r->dtype);
+  const int64_t esz = elem_bytes(r->dtype);
+  GG_REQUIRE(n == 0 || r->data != nullptr, "%s: data is NULL", name);
+  GG_REQUIRE((uintptr_t)r->data % esz == 0 && r->stride % esz == 0,
+             "%s: not aligned to its %lld-byte elements", name, (long long)esz);
+  GG_REQUIRE(n <= 1 || (r->stride >= 0 && (!written || r->stride >= dim * esz)),
+             "%s: stride %lld invalid for rows of %lld bytes", name, (long long)r->stride,
+             (long long)(dim * esz));
+  if (r->dtype == GG_E4M3) {
+    const int32_t g = r->group;
+    GG_REQUIRE(g == 0 || (g >= GG_MIN_GROUP && g <= GG_MAX_GROUP && (g & (g - 1)) == 0),
+               "%s: group %d is neither 0 nor a power of two from %d to %d", name, g, GG_MIN_GROUP,
+               GG_MAX_GROUP);
+    const int64_t sb = 4 * (g ? cdiv(dim, g) : 1);
+    GG_REQUIRE(n == 0 || r->scales != nullptr, "%s: 8-bit rows without scales", name);
+    GG_REQUIRE((uintptr_t)r->scales % 4 == 0 && r->scales_stride % 4 == 0,
+               "%s: scales are not 4-byte aligned", name);
+    GG_REQUIRE(n <= 1 || (r->scales_stride >= 0 && (!written || r->scales_stride >= sb)),
+               "%s: scales' stride %lld invalid", name, (long long)r->scales_stride);
+  }
+  out->p = (char*)r->data;
+  out->stride = r->stride;
+  out->scales = (char*)r->scales;
+  out->sstride = r->scales_stride;
+  out->group = r->dtype == GG_E4M3 ? r->group : 0;
   return GG_OK;
 }
 

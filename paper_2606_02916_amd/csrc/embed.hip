@@ -1,0 +1,796 @@
+// Embedding lookup with scaling, and its gradient by sorted ids.
+#include "rows.hpp"
+
+namespace gg {
+namespace {
+
+__device__ __forceinline__ int64_t id_at(const void* ids, int32_t bits, int64_t i) {
+  return bits == 64 ? ((const int64_t*)ids)[i] : (int64_t)((const int32_t*)ids)[i];
+}
+
+// ---------------------------------------------------------------------------
+// Lookup: out[i] = scale * table[ids[i]].
+//
+// Nothing is used twice, so the call is bound by memory: the rows read and the
+// rows written.  The output is one run of n * pieces pieces of 16 bytes (of
+// the wider type), dealt to the lanes in order: every store covers a
+// contiguous run, rows of any width fill the waves, and one wide row spreads
+// over as many waves as it has.  A lane has U pieces in flight.
+// ---------------------------------------------------------------------------
+struct LookupArgs {
+  KRows table, out;
+  const void* ids;
+  int32_t id_bits;
+  int32_t dim;
+  int64_t rows, n;
+  float scale;
+  uint32_t pieces, pmagic;
+  int32_t glog;       // log2 of the elements per scale; 31: one scale per row
+  int32_t* status;
+};
+
+template <typename TI, typename TO, int V, int U>
+__global__ void __launch_bounds__(kBlock) k_embed_rows(LookupArgs a) {
+  // The block's first row and piece (the same for all lanes).
+  const uint64_t base = (uint64_t)blockIdx.x * (kBlock * U);
+  uint64_t row0;
+  if (base >> 32)
+    row0 = base / a.pieces;
+  else
+    row0 = (uint32_t)base / a.pieces;
+  const uint32_t rem = (uint32_t)(base - row0 * a.pieces);
+  typename Raw<TI, V>::vec raw[U];
+  float mul[U], mul2[U];
+  uint64_t row[U];
+  int32_t e[U];
+  bool ok[U];
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    const uint32_t o = rem + (uint32_t)(j * kBlock + threadIdx.x);
+    const uint32_t r = chunk_row(o, a.pmagic);
+    int32_t skip;
+    e[j] = piece_start<V>((int32_t)(o - r * a.pieces), a.dim, &skip);
+    row[j] = row0 + r;
+    ok[j] = row[j] < (uint64_t)a.n;
+    raw[j] = {};
+    mul[j] = mul2[j] = 0.0f;
+    if (ok[j]) {
+      const int64_t id = a.ids ? id_at(a.ids, a.id_bits, (int64_t)row[j]) : (int64_t)row[j];
+      if ((uint64_t)id < (uint64_t)a.rows) {
+        raw[j] = raw_load<TI, V>(a.table.p + id * a.table.stride + e[j] * (int64_t)sizeof(TI));
+        mul[j] = a.scale;
+        if constexpr (sizeof(TI) == 1) {
+          // The row's last piece may lie in two groups (never in more).
+          const float* sc = (const float*)(a.table.scales + id * a.table.sstride);
+          mul2[j] = mul[j] * sc[(e[j] + V - 1) >> a.glog];
+          mul[j] *= sc[e[j] >> a.glog];
+        }
+      } else {
+        bad |= id != -1;
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
+    if (!ok[j]) continue;
+    float v[V];
+    to_f32<TI, V>(raw[j], v);
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      v[k] *= sizeof(TI) == 1 && ((e[j] ^ (e[j] + k)) >> a.glog) ? mul2[j] : mul[j];
+    row_store<TO, V>(a.out.p + (int64_t)row[j] * a.out.stride + e[j] * (int64_t)sizeof(TO), v);
+  }
+  if (bad) set_status(a.status, GG_DEV_BAD_ID);
+}
+
+// ---------------------------------------------------------------------------
+// Sorting the ids: pairs (key, position) by key, positions ascending within a
+// key.  A key is its id, or num_rows for an id that adds nothing; the radix
+// passes take the low digit first and keep the order of equal digits, so the
+// result depends on the ids alone.
+//
+// A tile of kTile pairs belongs to a block; wave w of it holds the pairs
+// [w * kTileWave, (w + 1) * kTileWave) of the tile, 64 neighbouring ones at a
+// time.  Lanes whose digits agree find each other by one ballot per digit bit,
+// so equal digits are counted and ranked without atomics.
+// ---------------------------------------------------------------------------
+constexpr int kSortBlock = 1024;
+constexpr int kSortWaves = kSortBlock / kWave;
+constexpr int kSortKeys = 8;                      // pairs per lane
+constexpr int kTileWave = kWave * kSortKeys;
+constexpr int kTile = kSortBlock * kSortKeys;
+constexpr int kMaxDigit = 11;                     // bits; 2,048 counters per wave
+constexpr int kWideTiles = 32;                    // at most this many tiles: digits of 11 bits
+
+struct Keys {
+  const void* ids;       // first pass: the ids; later passes: key and pos
+  int32_t id_bits;
+  const uint32_t* key;
+  const uint32_t* pos;
+  int64_t n;
+  uint32_t rows;         // num_rows
+  int32_t shift, bits;   // the pass's digit
+  int32_t* status;
+};
+
+__device__ __forceinline__ uint32_t key_of(const Keys& a, int64_t i, bool* bad) {
+  if (!a.ids) return a.key[i];
+  const int64_t id = id_at(a.ids, a.id_bits, i);
+  if ((uint64_t)id < (uint64_t)a.rows) return (uint32_t)id;
+  *bad |= id != -1;
+  return a.rows;
+}
+
+// Lanes with this lane's digit, among the valid ones.
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, bool valid) {
+  uint64_t m = __ballot(valid);
+  for (int b = 0; b < bits; ++b) {
+    const uint64_t one = __ballot((d >> b) & 1u);
+    m &= ((d >> b) & 1u) ? one : ~one;
+  }
+  return m;
+}
+
+// Ranks a tile's pairs: cnt[w][d] ends as the number of the wave's pairs with
+// digit d, rank[j] as the number of earlier ones in the wave.
+__device__ __forceinline__ void rank_tile(const uint32_t (&key)[kSortKeys], int shift, int bits,
+                                          int left, uint16_t* cnt, uint16_t (&rank)[kSortKeys]) {
+  const uint32_t mask = (1u << bits) - 1u;
+  const int lane = lane_id();
+#pragma unroll
+  for (int j = 0; j < kSortKeys; ++j) {
+    const uint32_t d = (key[j] >> shift) & mask;
+    const bool valid = j * kWave + lane < left;
+    const uint64_t m = same_digit(d, bits, valid);
+    // A wave's LDS accesses run in order: all its lanes read before one writes.
+    const uint32_t before = valid ? ((volatile uint16_t*)cnt)[d] : 0u;
+    const int below = lanes_below(m);
+    rank[j] = (uint16_t)(before + below);
+    if (valid && below == 0) ((volatile uint16_t*)cnt)[d] = (uint16_t)(before + __popcll(m));
+  }
+}
+
+// Digit counts of each tile: hist[tile][digit].
+__global__ void __launch_bounds__(kSortBlock) k_sort_count(Keys a, int32_t* hist) {
+  __shared__ uint16_t cnt[kSortWaves << kMaxDigit];
+  const int digits = 1 << a.bits, w = threadIdx.x / kWave;
+  for (int i = threadIdx.x; i < kSortWaves * digits; i += kSortBlock) cnt[i] = 0;
+  const int64_t first = (int64_t)blockIdx.x * kTile + w * kTileWave;
+  const int left = (int)min((int64_t)kTileWave, max((int64_t)0, a.n - first));
+  uint32_t key[kSortKeys];
+  uint16_t rank[kSortKeys];
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < kSortKeys; ++j) {
+    const int o = j * kWave + lane_id();
+    key[j] = o < left ? key_of(a, first + o, &bad) : 0u;
+  }
+  if (bad) set_status(a.status, GG_DEV_BAD_ID);
+  __syncthreads();
+  rank_tile(key, a.shift, a.bits, left, cnt + w * digits, rank);
+  __syncthreads();
+  for (int d = threadIdx.x; d < digits; d += kSortBlock) {
+    int32_t s = 0;
+#pragma unroll
+    for (int v = 0; v < kSortWaves; ++v) s += cnt[v * digits + d];
+    hist[(int64_t)blockIdx.x * digits + d] = s;
+  }
+}
+
+// First output place of each digit of this block's tile -> base[d] (LDS), from
+// the counts of all tiles: smaller digits first, then earlier tiles.
+__device__ void tile_bases(const int32_t* hist, int tiles, int digits, int32_t* base) {
+  const int tid = threadIdx.x;
+  const int cols = digits < kSortBlock ? digits : kSortBlock;
+  const int groups = kSortBlock / cols;
+  const int per = (tiles + groups - 1) / groups;
+  int32_t run = 0;
+  __shared__ int32_t s_scan[kSortWaves];
+  __shared__ int32_t s_mine[kSortBlock], s_all[kSortBlock];
+  for (int d0 = 0; d0 < digits; d0 += cols) {
+    const int d = d0 + tid % cols, g = tid / cols;
+    int32_t mine = 0, all = 0;
+    const int t1 = min(tiles, (g + 1) * per);
+#pragma unroll 8
+    for (int t = g * per; t < t1; ++t) {
+      const int32_t c = hist[(int64_t)t * digits + d];
+      all += c;
+      mine += t < (int)blockIdx.x ? c : 0;
+    }
+    s_mine[tid] = mine;
+    s_all[tid] = all;
+    __syncthreads();
+    int32_t total = 0;
+    mine = all = 0;
+    if (tid < cols)
+      for (int x = 0; x < groups; ++x) {
+        mine += s_mine[x * cols + tid];
+        all += s_all[x * cols + tid];
+      }
+    const int32_t before = block_excl_scan<kSortBlock>(all, s_scan, &total);
+    if (tid < cols) base[d0 + tid] = run + before + mine;
+    run += total;
+    __syncthreads();
+  }
+}
+
+__global__ void __launch_bounds__(kSortBlock) k_sort_scatter(Keys a, const int32_t* hist, int tiles,
+                                                             uint32_t* key_out,
+                                                             uint32_t* pos_out) {
+  __shared__ uint16_t cnt[kSortWaves << kMaxDigit];
+  __shared__ int32_t base[1 << kMaxDigit];
+  const int digits = 1 << a.bits, w = threadIdx.x / kWave;
+  for (int i = threadIdx.x; i < kSortWaves * digits; i += kSortBlock) cnt[i] = 0;
+  const int64_t first = (int64_t)blockIdx.x * kTile + w * kTileWave;
+  const int left = (int)min((int64_t)kTileWave, max((int64_t)0, a.n - first));
+  uint32_t key[kSortKeys], pos[kSortKeys];
+  uint16_t rank[kSortKeys];
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < kSortKeys; ++j) {
+    const int o = j * kWave + lane_id();
+    key[j] = o < left ? key_of(a, first + o, &bad) : 0u;
+    pos[j] = o < left ? (a.ids ? (uint32_t)(first + o) : a.pos[first + o]) : 0u;
+  }
+  tile_bases(hist, tiles, digits, base);
+  rank_tile(key, a.shift, a.bits, left, cnt + w * digits, rank);
+  __syncthreads();
+  // Counts of earlier waves, in place.
+  for (int d = threadIdx.x; d < digits; d += kSortBlock) {
+    uint16_t s = 0;
+#pragma unroll
+    for (int v = 0; v < kSortWaves; ++v) {
+      const uint16_t c = cnt[v * digits + d];
+      cnt[v * digits + d] = s;
+      s += c;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < kSortKeys; ++j) {
+    if (j * kWave + lane_id() >= left) continue;
+    const uint32_t d = (key[j] >> a.shift) & (digits - 1);
+    const uint32_t to = (uint32_t)base[d] + cnt[w * digits + d] + rank[j];
+    key_out[to] = key[j];
+    pos_out[to] = pos[j];
+  }
+}
+
+// One tile: every pass in one launch, the pairs in LDS between passes.
+__global__ void __launch_bounds__(kSortBlock) k_sort_tile(Keys a, int key_bits, int digit_bits,
+                                                          uint32_t* key_out, uint32_t* pos_out) {
+  __shared__ uint32_t s_key[kTile];
+  __shared__ uint16_t s_pos[kTile];
+  __shared__ uint16_t cnt[kSortWaves << 8];
+  __shared__ int32_t s_scan[kSortWaves];
+  __shared__ int32_t base[1 << 8];
+  const int w = threadIdx.x / kWave, n = (int)a.n;
+  const int first = w * kTileWave, left = min(kTileWave, max(0, n - first));
+  uint32_t key[kSortKeys];
+  uint16_t pos[kSortKeys], rank[kSortKeys];
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < kSortKeys; ++j) {
+    const int o = j * kWave + lane_id();
+    key[j] = o < left ? key_of(a, first + o, &bad) : 0u;
+    pos[j] = (uint16_t)(first + o);
+  }
+  if (bad) set_status(a.status, GG_DEV_BAD_ID);
+  for (int shift = 0; shift < key_bits; shift += digit_bits) {
+    const int bits = min(digit_bits, key_bits - shift), digits = 1 << bits;
+    if (shift) {
+#pragma unroll
+      for (int j = 0; j < kSortKeys; ++j) {
+        const int o = j * kWave + lane_id();
+        if (o < left) {
+          key[j] = s_key[first + o];
+          pos[j] = s_pos[first + o];
+        }
+      }
+    }
+    for (int i = threadIdx.x; i < kSortWaves * digits; i += kSortBlock) cnt[i] = 0;
+    __syncthreads();
+    rank_tile(key, shift, bits, left, cnt + w * digits, rank);
+    __syncthreads();
+    int32_t s = 0, total;
+    if ((int)threadIdx.x < digits)
+#pragma unroll
+      for (int v = 0; v < kSortWaves; ++v) {
+        const uint16_t c = cnt[v * digits + threadIdx.x];
+        cnt[v * digits + threadIdx.x] = (uint16_t)s;
+        s += c;
+      }
+    const int32_t before = block_excl_scan<kSortBlock>(s, s_scan, &total);
+    if ((int)threadIdx.x < digits) base[threadIdx.x] = before;
+    __syncthreads();
+    const bool last = shift + bits >= key_bits;
+#pragma unroll
+    for (int j = 0; j < kSortKeys; ++j) {
+      if (j * kWave + lane_id() >= left) continue;
+      const uint32_t d = (key[j] >> shift) & (digits - 1);
+      const uint32_t to = (uint32_t)base[d] + cnt[w * digits + d] + rank[j];
+      if (last) {
+        key_out[to] = key[j];
+        pos_out[to] = pos[j];
+      } else {
+        s_key[to] = key[j];
+        s_pos[to] = pos[j];
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Sums of the sorted rows.
+//
+// A run is the positions of one id.  k_grad_rows gives a block `per` rows of
+// the gradient (or, when rows are added to, the runs that start in `per` sorted
+// positions), so that every row is written once, zeros included, and the
+// gradient needs no pass that clears it.  Short runs are summed by a group of
+// `lanes` lanes each, longer ones by the block's groups together.  Runs of
+// more than `chunk` positions are cut at multiples of it: k_grad_parts sums
+// their parts first, a block per chunk, so that an id that fills the whole
+// call still spreads over the chip.
+// ---------------------------------------------------------------------------
+constexpr int kGradRows = 256;       // most entries of a block
+constexpr int kGroupRun = 32;        // longest run that one group sums
+constexpr int kGradUnroll = 4;
+
+struct GradArgs {
+  const uint32_t* key;     // sorted
+  const uint32_t* pos;
+  uint32_t n, rows;
+  int32_t dim;
+  int32_t pieces;          // column pieces of a row
+  int32_t lanes_log;       // lanes of a group (a power of two up to 64)
+  int32_t tiles;           // column tiles of a group
+  uint32_t per;            // rows (or positions) of a block
+  uint32_t chunk;
+  int32_t add;
+  float scale;
+  KRows dy, grad;
+  float* part;             // [chunk][2][dim]: a run from before the chunk, one into the next
+};
+
+// First i in [lo, hi) with k[i] >= v, or hi.  All lanes of a wave together: 64
+// probes a step.
+__device__ uint32_t wave_lower_bound(const uint32_t* k, uint32_t lo, uint32_t hi, uint32_t v) {
+  const uint32_t lane = lane_id();
+  while (hi - lo > kWave) {
+    const uint32_t step = (hi - lo + kWave - 1) / kWave;
+    const uint64_t i = (uint64_t)lo + (uint64_t)(lane + 1) * step - 1;
+    const uint32_t c = (uint32_t)__popcll(__ballot(i < hi && k[i] < v));
+    lo += c * step;
+    hi = min(hi, lo + step);
+  }
+  return lo + (uint32_t)__popcll(__ballot(lo + lane < hi && k[lo + lane] < v));
+}
+
+// Adds the rows dy[pos[p]], p = p0, p0 + step, .. < p1, to acc.
+template <typename TD, int V>
+__device__ __forceinline__ void add_rows(const GradArgs& a, uint32_t p0, uint32_t p1, uint32_t step,
+                                         int32_t e, float (&acc)[V]) {
+  const char* base = a.dy.p + e * (int64_t)sizeof(TD);
+  for (uint64_t p = p0; p < p1; p += (uint64_t)step * kGradUnroll) {
+    typename Raw<TD, V>::vec raw[kGradUnroll];
+    uint32_t at[kGradUnroll];
+#pragma unroll
+    for (int u = 0; u < kGradUnroll; ++u) {
+      const uint64_t q = p + (uint64_t)u * step;
+      at[u] = a.pos[q < p1 ? q : p];
+    }
+#pragma unroll
+    for (int u = 0; u < kGradUnroll; ++u)
+      raw[u] = raw_load<TD, V>(base + (int64_t)at[u] * a.dy.stride);
+#pragma unroll
+    for (int u = 0; u < kGradUnroll; ++u) {
+      if (p + (uint64_t)u * step >= p1) break;
+      float v[V];
+      to_f32<TD, V>(raw[u], v);
+#pragma unroll
+      for (int k = 0; k < V; ++k) acc[k] += v[k];
+    }
+  }
+}
+
+// As add_rows, over the parts of run [beg, end) that k_grad_parts left.
+template <int V>
+__device__ __forceinline__ void add_parts(const GradArgs& a, uint32_t beg, uint32_t end,
+                                          uint32_t first, uint32_t step, int32_t e,
+                                          float (&acc)[V]) {
+  const uint32_t c0 = beg / a.chunk, c1 = (end - 1) / a.chunk;
+#pragma unroll 4
+  for (uint32_t c = c0 + first; c <= c1; c += step) {
+    // the chunk where the run starts holds a part that leads into the next one
+    const float* p = a.part + ((int64_t)c * 2 + (c == c0 ? 1 : 0)) * a.dim + e;
+    float v[V];
+    row_load<float, V>((const char*)p, v);
+#pragma unroll
+    for (int k = 0; k < V; ++k) acc[k] += v[k];
+  }
+}
+
+// Sums the groups' accumulators into group 0's, in the order of the groups.
+template <int V>
+__device__ __forceinline__ void join_groups(float (&acc)[V], float* lds, int lanes, int groups) {
+  const int tid = threadIdx.x;
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < V; ++k) lds[k * kBlock + tid] = acc[k];
+  __syncthreads();
+  if (tid < lanes)
+    for (int g = 1; g < groups; ++g)
+#pragma unroll
+      for (int k = 0; k < V; ++k) acc[k] += lds[k * kBlock + g * lanes + tid];
+}
+
+template <typename TD, int V>
+__global__ void __launch_bounds__(kBlock) k_grad_parts(GradArgs a) {
+  __shared__ float lds[V * kBlock];
+  __shared__ uint32_t s_run[2][2];
+  const uint32_t c = blockIdx.x, c0 = c * a.chunk;
+  const uint32_t c1 = (uint32_t)min((uint64_t)a.n, (uint64_t)c0 + a.chunk);
+  const uint32_t kb = a.key[c0], ke = a.key[c1 - 1];
+  const bool from = c0 > 0 && a.key[c0 - 1] == kb && kb < a.rows;
+  const bool into = c1 < a.n && a.key[c1] == ke && ke < a.rows && !(from && ke == kb);
+  if (!from && !into) return;
+  const int w = threadIdx.x / kWave;
+  if (w < 2) {
+    const uint32_t k = w == 0 ? kb : ke;
+    if (w == 0 ? from : into) {
+      const uint32_t lo = wave_lower_bound(a.key, 0, a.n, k);
+      const uint32_t hi = wave_lower_bound(a.key, 0, a.n, k + 1);
+      if (lane_id() == 0) {
+        s_run[w][0] = max(lo, c0);
+        s_run[w][1] = hi - lo > a.chunk ? min(hi, c1) : 0u;
+      }
+    } else if (lane_id() == 0) {
+      s_run[w][0] = s_run[w][1] = 0u;
+    }
+  }
+  __syncthreads();
+  const int lanes = 1 << a.lanes_log, groups = kBlock >> a.lanes_log;
+  const int g = threadIdx.x >> a.lanes_log, l = threadIdx.x & (lanes - 1);
+  const int32_t piece = (int32_t)blockIdx.y * lanes + l;
+  int32_t skip;
+  const int32_t e = piece_start<V>(min(piece, a.pieces - 1), a.dim, &skip);
+  for (int s = 0; s < 2; ++s) {
+    const uint32_t p0 = s_run[s][0], p1 = s_run[s][1];
+    if (p0 >= p1) continue;
+    float acc[V] = {};
+    add_rows<TD, V>(a, p0 + g, p1, groups, e, acc);
+    join_groups<V>(acc, lds, lanes, groups);
+    if (g == 0 && piece < a.pieces)
+      row_store<float, V>((char*)(a.part + ((int64_t)c * 2 + s) * a.dim + e), acc);
+  }
+}
+
+template <typename TG, int V>
+__device__ __forceinline__ void put_row(const GradArgs& a, uint32_t row, int32_t e,
+                                        float (&acc)[V]) {
+  char* p = a.grad.p + (int64_t)row * a.grad.stride + e * (int64_t)sizeof(TG);
+#pragma unroll
+  for (int k = 0; k < V; ++k) acc[k] *= a.scale;
+  if (a.add) {
+    float old[V];
+    row_load<TG, V>(p, old);
+#pragma unroll
+    for (int k = 0; k < V; ++k) acc[k] += old[k];
+  }
+  row_store<TG, V>(p, acc);
+}
+
+template <typename TD, typename TG, int V>
+__global__ void __launch_bounds__(kBlock) k_grad_rows(GradArgs a) {
+  __shared__ float lds[V * kBlock];
+  __shared__ uint32_t s_row[kGradRows], s_beg[kGradRows], s_end[kGradRows];
+  __shared__ uint32_t s_range[2], s_many;
+  __shared__ int32_t s_heads[kBlock / kWave];
+  const uint32_t tid = threadIdx.x, w = tid / kWave;
+  uint32_t entries;
+  if (tid == 0) s_many = 0;
+  if (!a.add) {
+    // Rows [v0, v0 + entries) and their runs.
+    const uint32_t v0 = blockIdx.x * a.per;
+    entries = min(a.per, a.rows - v0);
+    if (w < 2) {
+      const uint32_t r = wave_lower_bound(a.key, 0, a.n, w == 0 ? v0 : v0 + entries);
+      if (lane_id() == 0) s_range[w] = r;
+    }
+    if (tid < entries) {
+      s_row[tid] = v0 + tid;
+      s_beg[tid] = s_end[tid] = 0u;
+    }
+    __syncthreads();
+    const uint32_t p0 = s_range[0], p1 = s_range[1];
+    if (p1 - p0 <= 4 * kBlock) {
+      for (uint32_t p = p0 + tid; p < p1; p += kBlock) {
+        const uint32_t k = a.key[p];
+        if (p == p0 || a.key[p - 1] != k) s_beg[k - v0] = p;
+        if (p + 1 == p1 || a.key[p + 1] != k) s_end[k - v0] = p + 1;
+      }
+    } else if (tid < entries) {
+      uint32_t at[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        uint32_t lo = p0, hi = p1;
+        while (lo < hi) {
+          const uint32_t mid = lo + (hi - lo) / 2;
+          if (a.key[mid] < v0 + tid + x) lo = mid + 1;
+          else hi = mid;
+        }
+        at[x] = lo;
+      }
+      s_beg[tid] = at[0];
+      s_end[tid] = at[1];
+    }
+  } else {
+    // Runs that start at positions [p0, p0 + per).
+    const uint32_t p = blockIdx.x * a.per + tid;
+    const uint32_t last = min(a.n, blockIdx.x * a.per + a.per);
+    const uint32_t k = p < last ? a.key[p] : a.rows;
+    const bool head = k < a.rows && (p == 0 || a.key[p - 1] != k);
+    const uint64_t m = __ballot(head);
+    if (lane_id() == 0) s_heads[w] = __popcll(m);
+    __syncthreads();
+    uint32_t i = lanes_below(m);
+    entries = 0;
+    for (uint32_t x = 0; x < kBlock / kWave; ++x) {
+      i += x < w ? s_heads[x] : 0;
+      entries += s_heads[x];
+    }
+    if (entries == 0) return;
+    if (head) {
+      s_row[i] = k;
+      s_beg[i] = p;
+    }
+    __syncthreads();
+    if (tid + 1 < entries) s_end[tid] = s_beg[tid + 1];
+    if (w == 0) {
+      const uint32_t beg = s_beg[entries - 1];
+      const uint32_t end = wave_lower_bound(a.key, beg, a.n, s_row[entries - 1] + 1);
+      if (lane_id() == 0) s_end[entries - 1] = end;
+    }
+  }
+  __syncthreads();
+
+  const int lanes = 1 << a.lanes_log, groups = kBlock >> a.lanes_log;
+  const int g = tid >> a.lanes_log, l = tid & (lanes - 1);
+  int32_t skip;
+  const uint32_t items = entries * (uint32_t)a.tiles;
+  for (uint32_t item = g; item < items; item += groups) {
+    const uint32_t x = a.tiles == 1 ? item : item / a.tiles;
+    const int32_t piece = (int32_t)(item - x * a.tiles) * lanes + l;
+    const uint32_t beg = s_beg[x], end = s_end[x];
+    if (end - beg > kGroupRun) {
+      s_many = 1;
+      continue;
+    }
+    if (piece >= a.pieces) continue;
+    const int32_t e = piece_start<V>(piece, a.dim, &skip);
+    float acc[V] = {};
+    add_rows<TD, V>(a, beg, end, 1, e, acc);
+    put_row<TG, V>(a, s_row[x], e, acc);
+  }
+  __syncthreads();
+  if (!s_many) return;
+  for (uint32_t x = 0; x < entries; ++x) {
+    const uint32_t beg = s_beg[x], end = s_end[x];
+    if (end - beg <= kGroupRun) continue;
+    for (int32_t t = 0; t < a.tiles; ++t) {
+      const int32_t piece = t * lanes + l;
+      const int32_t e = piece_start<V>(min(piece, a.pieces - 1), a.dim, &skip);
+      float acc[V] = {};
+      if (end - beg > a.chunk)
+        add_parts<V>(a, beg, end, g, groups, e, acc);
+      else
+        add_rows<TD, V>(a, beg + g, end, groups, e, acc);
+      join_groups<V>(acc, lds, lanes, groups);
+      if (g == 0 && piece < a.pieces) put_row<TG, V>(a, s_row[x], e, acc);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------
+uint32_t grad_chunk(int64_t n) {
+  uint32_t c = 128;
+  while (c < 1024 && (int64_t)c * 1024 < n) c *= 2;
+  return c;
+}
+
+struct EmbedWs {
+  uint32_t *key[2], *pos[2];
+  int32_t* hist;
+  float* part;
+};
+
+size_t embed_ws_layout(int64_t n, int32_t dim, char* base, EmbedWs* out) {
+  Carve c{base, 0, 0};
+  EmbedWs w;
+  const int64_t tiles = cdiv(n, kTile);
+  for (int i = 0; i < 2; ++i) {
+    w.key[i] = c.take<uint32_t>((size_t)n);
+    w.pos[i] = c.take<uint32_t>((size_t)n);
+  }
+  w.hist = c.take<int32_t>((size_t)tiles << (tiles <= kWideTiles ? kMaxDigit : 8));
+  w.part = c.take<float>((size_t)cdiv(n, grad_chunk(n)) * 2 * dim);
+  if (out) *out = w;
+  return align_up(c.used, 256);
+}
+
+struct Lanes {
+  int32_t pieces, lanes_log, tiles;
+};
+
+Lanes lanes_of(int32_t dim, int vec) {
+  Lanes r;
+  r.pieces = (int32_t)cdiv(dim, vec);
+  r.lanes_log = 0;
+  while (r.lanes_log < 6 && (1 << r.lanes_log) < r.pieces) ++r.lanes_log;
+  r.tiles = (int32_t)cdiv(r.pieces, 1 << r.lanes_log);
+  return r;
+}
+
+template <typename TI, typename TO>
+int launch_lookup(LookupArgs& a, hipStream_t stream) {
+  // The wider type's pieces are 16 bytes.
+  constexpr int V = sizeof(TI) > sizeof(TO) ? kVec<TI> : kVec<TO>;
+  const bool wide = a.dim >= V;
+  a.pieces = (uint32_t)cdiv(a.dim, wide ? V : 1);
+  a.pmagic = div_magic(a.pieces);
+  const uint64_t total = (uint64_t)a.n * a.pieces;
+  GG_REQUIRE(total <= 1ULL << 33, "%lld rows of %d elements are too many for one call",
+             (long long)a.n, a.dim);
+  // One piece per lane while that leaves lanes idle, four in flight after.
+  const int u = total < 256 * 1024 ? 1 : 4;
+  const dim3 grid((unsigned)((total + kBlock * u - 1) / (kBlock * u)));
+  if (!wide)
+    hipLaunchKernelGGL((k_embed_rows<TI, TO, 1, 4>),
+                       dim3((unsigned)((total + kBlock * 4 - 1) / (kBlock * 4))), dim3(kBlock), 0,
+                       stream, a);
+  else if (u == 1)
+    hipLaunchKernelGGL((k_embed_rows<TI, TO, V, 1>), grid, dim3(kBlock), 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_embed_rows<TI, TO, V, 4>), grid, dim3(kBlock), 0, stream, a);
+  GG_LAUNCH_CHECK("k_embed_rows");
+  return GG_OK;
+}
+
+template <typename TD, typename TG, int V>
+int launch_grad(const GradArgs& a, hipStream_t stream) {
+  const unsigned chunks = (unsigned)cdiv(a.n, a.chunk);
+  if (chunks > 1) {
+    hipLaunchKernelGGL((k_grad_parts<TD, V>), dim3(chunks, (unsigned)a.tiles), dim3(kBlock), 0,
+                       stream, a);
+    GG_LAUNCH_CHECK("k_grad_parts");
+  }
+  const unsigned blocks = (unsigned)cdiv(a.add ? a.n : a.rows, a.per);
+  if (blocks > 0) {
+    hipLaunchKernelGGL((k_grad_rows<TD, TG, V>), dim3(blocks), dim3(kBlock), 0, stream, a);
+    GG_LAUNCH_CHECK("k_grad_rows");
+  }
+  return GG_OK;
+}
+
+}  // namespace
+}  // namespace gg
+
+using namespace gg;
+
+extern "C" int gg_embed_forward(const gg_rows_t* table, int64_t num_rows, int32_t dim,
+                                const void* ids_d, int32_t id_bits, int64_t n, float scale,
+                                const gg_rows_t* out, int32_t* status_d, hipStream_t stream) {
+  GG_REQUIRE(status_d, "status is NULL");
+  GG_REQUIRE(dim >= 1 && dim <= GG_EMBED_MAX_DIM, "dim %d outside 1..%d", dim, GG_EMBED_MAX_DIM);
+  GG_REQUIRE(num_rows >= 0 && n >= 0 && n <= 1LL << 33, "num_rows %lld or n %lld invalid",
+             (long long)num_rows, (long long)n);
+  GG_REQUIRE(id_bits == 32 || id_bits == 64, "ids of %d bits", id_bits);
+  GG_REQUIRE((uintptr_t)ids_d % (id_bits / 8) == 0, "ids are not aligned");
+  LookupArgs a = {};
+  int rc = pack_rows(table, "table", num_rows, dim, kBitFloats | kBitE4M3, false, &a.table);
+  if (rc == GG_OK) rc = pack_rows(out, "out", n, dim, kBitFloats, true, &a.out);
+  if (rc != GG_OK || n == 0) return rc;
+  a.ids = ids_d;
+  a.id_bits = id_bits;
+  a.dim = dim;
+  a.rows = num_rows;
+  a.n = n;
+  a.scale = scale;
+  a.glog = a.table.group ? __builtin_ctz((unsigned)a.table.group) : 31;
+  a.status = status_d;
+  GG_FOR_FLOAT(out->dtype, TO, {
+    if (table->dtype == GG_E4M3) return launch_lookup<e4m3, TO>(a, stream);
+    GG_FOR_FLOAT(table->dtype, TI, { return launch_lookup<TI, TO>(a, stream); });
+  });
+}
+
+extern "C" size_t gg_ws_embed(int64_t n, int64_t num_rows, int32_t dim) {
+  if (n < 0 || n > INT32_MAX - 1 || num_rows < 0 || num_rows > INT32_MAX - 1 || dim < 1 ||
+      dim > GG_EMBED_MAX_DIM)
+    return 0;
+  return embed_ws_layout(n, dim, nullptr, nullptr);
+}
+
+extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t id_bits, int64_t n,
+                                 int64_t num_rows, int32_t dim, float scale, const gg_rows_t* grad,
+                                 int32_t flags, int32_t* status_d, void* ws, size_t ws_bytes,
+                                 hipStream_t stream) {
+  GG_REQUIRE(status_d, "status is NULL");
+  GG_REQUIRE(dim >= 1 && dim <= GG_EMBED_MAX_DIM, "dim %d outside 1..%d", dim, GG_EMBED_MAX_DIM);
+  GG_REQUIRE(n >= 0 && n <= INT32_MAX - 1, "n = %lld unsupported", (long long)n);
+  GG_REQUIRE(num_rows >= 0 && num_rows <= INT32_MAX - 1, "num_rows %lld unsupported",
+             (long long)num_rows);
+  GG_REQUIRE(id_bits == 32 || id_bits == 64, "ids of %d bits", id_bits);
+  GG_REQUIRE(n == 0 || ids_d, "ids are NULL");
+  GG_REQUIRE((uintptr_t)ids_d % (id_bits / 8) == 0, "ids are not aligned");
+  GG_REQUIRE((flags & ~GG_EMBED_ADD) == 0, "unknown flags %d", flags);
+  GradArgs a = {};
+  int rc = pack_rows(dy, "dy", n, dim, kBitFloats, false, &a.dy);
+  if (rc == GG_OK) rc = pack_rows(grad, "grad", num_rows, dim, kBitFloats, true, &a.grad);
+  if (rc != GG_OK) return rc;
+  const size_t need = embed_ws_layout(n, dim, nullptr, nullptr);
+  GG_REQUIRE(n == 0 || (ws && ws_bytes >= need), "workspace of %zu bytes < %zu", ws_bytes, need);
+  a.add = flags & GG_EMBED_ADD;
+  if (a.add ? n == 0 : num_rows == 0) return GG_OK;
+  EmbedWs w = {};
+  if (n > 0) embed_ws_layout(n, dim, (char*)ws, &w);
+
+  // The sort, of as many passes as the ids' width needs.
+  Keys k = {};
+  k.ids = ids_d;
+  k.id_bits = id_bits;
+  k.n = n;
+  k.rows = (uint32_t)num_rows;
+  k.status = status_d;
+  const int key_bits = 32 - __builtin_clz((unsigned)std::max<int64_t>(num_rows, 1));
+  const int tiles = (int)cdiv(n, kTile);
+  const int most = tiles > 1 && tiles <= kWideTiles ? kMaxDigit : 8;
+  const int passes = (int)cdiv(key_bits, most), digit = (int)cdiv(key_bits, passes);
+  int at = 0;
+  if (tiles == 1) {
+    hipLaunchKernelGGL(k_sort_tile, dim3(1), dim3(kSortBlock), 0, stream, k, key_bits, digit,
+                       w.key[0], w.pos[0]);
+    GG_LAUNCH_CHECK("k_sort_tile");
+  } else if (tiles > 1) {
+    for (int p = 0; p < passes; ++p) {
+      k.shift = p * digit;
+      k.bits = std::min(digit, key_bits - k.shift);
+      at = p & 1;
+      hipLaunchKernelGGL(k_sort_count, dim3((unsigned)tiles), dim3(kSortBlock), 0, stream, k,
+                         w.hist);
+      GG_LAUNCH_CHECK("k_sort_count");
+      hipLaunchKernelGGL(k_sort_scatter, dim3((unsigned)tiles), dim3(kSortBlock), 0, stream, k,
+                         w.hist, tiles, w.key[at], w.pos[at]);
+      GG_LAUNCH_CHECK("k_sort_scatter");
+      k.ids = nullptr;
+      k.key = w.key[at];
+      k.pos = w.pos[at];
+    }
+  }
+
+  a.key = w.key[at];
+  a.pos = w.pos[at];
+  a.n = (uint32_t)n;
+  a.rows = (uint32_t)num_rows;
+  a.dim = dim;
+  a.scale = scale;
+  a.part = w.part;
+  a.chunk = grad_chunk(n);
+  // Rows of a block: as many as leave the chip 2,048 blocks.
+  a.per = 1;
+  while (a.per < kGradRows && (int64_t)a.per * 4096 <= (a.add ? n : num_rows)) a.per *= 2;
+  GG_FOR_FLOAT(dy->dtype, TD, {
+    constexpr int V = kVec<TD>;
+    const Lanes l = lanes_of(dim, dim >= V ? V : 1);
+    a.pieces = l.pieces;
+    a.lanes_log = l.lanes_log;
+    a.tiles = l.tiles;
+    GG_FOR_FLOAT(grad->dtype, TG, {
+      return dim >= V ? launch_grad<TD, TG, V>(a, stream) : launch_grad<TD, TG, 1>(a, stream);
+    });
+  });
+}

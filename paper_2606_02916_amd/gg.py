@@ -111,7 +111,13 @@ class gg_sage_layer_t(C.Structure):
                 ("w_self", C.c_void_p), ("w_neigh", C.c_void_p), ("bias", C.c_void_p)]
 
 
-GG_F32, GG_F16 = 0, 1
+class gg_rows_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("dtype", C.c_int32),
+                ("group", C.c_int32), ("scales", C.c_void_p), ("scales_stride", C.c_int64)]
+
+
+GG_F32, GG_F16, GG_BF16, GG_E4M3 = 0, 1, 2, 3
+GG_EMBED_ADD = 1
 STAGE_STATS_BYTES = C.sizeof(gg_stage_stats_t)
 GATHER_STATS_BYTES = C.sizeof(gg_gather_stats_t)
 SIM_ACC_BYTES = C.sizeof(gg_sim_acc_t)
@@ -146,6 +152,10 @@ SIGNATURES = {
     "gg_ws_sage": (_SZ, [_I64, _I32, _I64, _I32, _P]),
     "gg_sage_forward": (C.c_int, [_P, _I64, _I32, _I32, _P, _P, _I32, _I64, _I64, _P, _P, _I64, _P,
                                   _P, _SZ, _P]),
+    "gg_embed_forward": (C.c_int, [_P, _I64, _I32, _P, _I32, _I64, C.c_float, _P, _P, _P]),
+    "gg_ws_embed": (_SZ, [_I64, _I64, _I32]),
+    "gg_embed_backward": (C.c_int, [_P, _P, _I32, _I64, _I64, _I32, C.c_float, _P, _I32, _P, _P,
+                                    _SZ, _P]),
     "gg_read_status": (C.c_int, [_P, _P, _P]),
     "gg_status_string": (C.c_char_p, [_I32]),
     "gg_last_error": (C.c_char_p, []),
@@ -449,6 +459,73 @@ def gg_sage_forward(wsample, num_nodes, W, fanout, x, x_dtype, x_stride, rows_ca
                                      x_dtype, x_stride, rows_cap, layers_arr, _ptr(out),
                                      out_rows_cap, _ptr(status), _ptr(ws), ws.numel(),
                                      _stream(stream)), "gg_sage_forward")
+
+
+_DTYPES = {torch.float32: GG_F32, torch.float16: GG_F16, torch.bfloat16: GG_BF16,
+           torch.float8_e4m3fn: GG_E4M3}
+
+
+def make_rows(t, scales=None, group=0):
+    """The rows of a 2-d tensor whose rows are contiguous (any stride between
+    them), with the fp32 scales [rows, groups] (or [rows]) of 8-bit rows, one per
+    `group` elements or, with group 0, one per row.  The description keeps its
+    tensors alive."""
+    if t.dtype not in _DTYPES:
+        raise GGError(f"rows of {t.dtype} are not supported")
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise GGError("rows must be a 2-d tensor with contiguous rows")
+    r = gg_rows_t()
+    r.data, r.dtype = t.data_ptr(), _DTYPES[t.dtype]
+    r.stride = t.stride(0) * t.element_size()
+    if r.dtype == GG_E4M3:
+        groups = -(-t.shape[1] // group) if group else 1
+        if scales is None or scales.dtype != torch.float32:
+            raise GGError("8-bit rows need fp32 scales")
+        if scales.numel() != t.shape[0] * groups or scales.dim() not in (1, 2) or \
+                scales.shape[0] != t.shape[0] or (groups > 1 and scales.stride(1) != 1):
+            raise GGError(f"scales of shape {tuple(scales.shape)} for {t.shape[0]} rows of "
+                          f"{groups} groups")
+        r.group, r.scales, r.scales_stride = group, scales.data_ptr(), scales.stride(0) * 4
+    elif scales is not None or group:
+        raise GGError(f"scales for rows of {t.dtype}")
+    r.keep = (t, scales)
+    return r
+
+
+def _rows(r):
+    return None if r is None else C.byref(r)
+
+
+_ID_BITS = {torch.int32: 32, torch.int64: 64}
+
+
+def _ids(ids, n, what):
+    """Address and bits of at least n contiguous ids."""
+    if ids is None:
+        return None, 32
+    if ids.dtype not in _ID_BITS or not ids.is_contiguous() or ids.numel() < n:
+        raise GGError(f"{what}: ids must be at least {n} contiguous int32 or int64 values")
+    return ids.data_ptr(), _ID_BITS[ids.dtype]
+
+
+def gg_embed_forward(table, num_rows, dim, ids, n, scale, out, status, stream=None):
+    """table and out: make_rows of a [num_rows, dim] and an [n, dim] tensor.
+    ids: int32 or int64, or None for the rows 0 .. n-1."""
+    ptr, bits = _ids(ids, n, "gg_embed_forward")
+    return check(lib.gg_embed_forward(_rows(table), num_rows, dim, ptr, bits, n, scale, _rows(out),
+                                      _ptr(status), _stream(stream)), "gg_embed_forward")
+
+
+def gg_ws_embed(n, num_rows, dim):
+    return int(lib.gg_ws_embed(n, num_rows, dim))
+
+
+def gg_embed_backward(dy, ids, n, num_rows, dim, scale, grad, flags, status, ws, stream=None):
+    """dy and grad: make_rows of an [n, dim] and a [num_rows, dim] tensor."""
+    ptr, bits = _ids(ids, n, "gg_embed_backward")
+    return check(lib.gg_embed_backward(_rows(dy), ptr, bits, n, num_rows, dim, scale, _rows(grad),
+                                       flags, _ptr(status), _ptr(ws), ws.numel(),
+                                       _stream(stream)), "gg_embed_backward")
 
 
 def gg_read_status(status, stream=None):

@@ -1,0 +1,293 @@
+"""Embedding lookup and its gradient against their formulas in 64 bits."""
+import itertools
+import zlib
+
+import pytest
+import torch
+
+from tests.op_util import BF16, E4M3, F16, F32, FLOOR, U, UNIT, like, rows, untouched, within
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def lib():
+    from paper_2606_02916_amd import gg
+    return gg
+
+
+def status_word():
+    return torch.zeros(1, dtype=torch.int32, device=DEV)
+
+
+def gen(*key):
+    return torch.Generator().manual_seed(zlib.crc32(repr(key).encode()))
+
+
+def make_ids(kind, n, v, g, dtype=torch.int64):
+    if kind == "same":
+        ids = torch.full((n,), v // 2)
+    elif kind == "padding":
+        ids = torch.full((n,), -1)
+    elif kind == "distinct":
+        ids = torch.randperm(max(v, n), generator=g)[:n] % v
+    elif kind == "frequent":          # a few ids many times, some once, some padding
+        ids = ((v + 1) ** torch.rand(n, generator=g, dtype=torch.float64) - 1).long().clamp(0, v - 1)
+        ids[torch.rand(n, generator=g) < 0.05] = -1
+    else:
+        ids = torch.randint(0, v, (n,), generator=g)
+    return ids.to(dtype)
+
+
+@pytest.mark.parametrize("dim,n,v", [(1, 5, 3), (3, 70, 9), (7, 257, 40), (8, 1, 1), (100, 1000, 333),
+                                     (601, 301, 1000), (602, 65, 70), (4096, 3, 50),
+                                     (2049, 1031, 64), (4, 0, 7)])
+@pytest.mark.parametrize("tin,tout", list(itertools.product((F32, F16, BF16), repeat=2)))
+def test_lookup(dim, n, v, tin, tout):
+    print(f"lookup of {n} from {v} x {dim}, {tin} to {tout}", flush=True)
+    gg, g = lib(), gen(dim, n, v)
+    table = rows(torch.randn(v, dim, generator=g), tin, DEV, lead=3, pad=dim % 5)
+    ids = make_ids("frequent", n, v, g, torch.int32 if dim % 2 else torch.int64)
+    out, flat, own = like(n, dim, tout, DEV, lead=1, pad=dim % 3)
+    st = status_word()
+    gg.gg_embed_forward(gg.make_rows(table), v, dim, ids.to(DEV), n, 1.7, gg.make_rows(out), st)
+    scale = torch.tensor(1.7, dtype=F32).double()
+    want = torch.where(ids[:, None] >= 0, table.cpu().double()[ids.long().clamp(0)] * scale, 0.0)
+    assert within(out, want, want.abs() * (U + 1.01 * UNIT[tout]) + FLOOR[tout]) <= 0
+    assert untouched(flat, own) and int(st) == 0
+
+
+@pytest.mark.parametrize("dim,group", [(5, 0), (17, 16), (100, 0), (100, 32), (129, 128), (602, 64),
+                                       (1030, 256), (256, 16)])
+@pytest.mark.parametrize("tout", [F32, F16, BF16])
+def test_lookup_of_8bit_rows_with_their_scales_behind_the_codes(dim, group, tout):
+    """Rows as the fetch path moves them: codes, then the scales."""
+    gg, g = lib(), gen(dim, group)
+    v, n = 77, 203
+    k = -(-dim // group) if group else 1
+    at = (dim + 3) // 4 * 4
+    buf = torch.zeros(v, at + 4 * k + 8, dtype=torch.uint8)
+    # every code but the two NaNs
+    codes = torch.randint(0, 254, (v, dim), generator=g, dtype=torch.int64)
+    codes = (codes + (codes >= 127)).to(torch.uint8)
+    scales = torch.rand(v, k, generator=g) + 0.1
+    buf[:, :dim] = codes
+    buf[:, at:at + 4 * k] = scales.view(torch.uint8).view(v, 4 * k)
+    buf = buf.to(DEV)
+    q = buf[:, :dim].view(E4M3)
+    sc = buf[:, at:at + 4 * k].view(F32)
+    out, flat, own = like(n, dim, tout, DEV, lead=2, pad=1)
+    ids, st = make_ids("frequent", n, v, g), status_word()
+    gg.gg_embed_forward(gg.make_rows(q, scales=sc, group=group), v, dim, ids.to(DEV), n, 0.3,
+                        gg.make_rows(out), st)
+    col = torch.arange(dim) // (group or dim)
+    value = codes.view(E4M3).double() * scales.double()[:, col]
+    want = torch.where(ids[:, None] >= 0,
+                       value[ids.clamp(0)] * torch.tensor(0.3, dtype=F32).double(), 0.0)
+    assert within(out, want, want.abs() * (2 * U + 1.01 * UNIT[tout]) + FLOOR[tout]) <= 0
+    assert untouched(flat, own) and int(st) == 0
+
+
+def test_lookup_without_ids_takes_the_rows_in_order():
+    gg, g = lib(), gen(4)
+    table = rows(torch.randn(50, 33, generator=g), BF16, DEV)
+    out, flat, own = like(40, 33, F32, DEV)
+    st = status_word()
+    gg.gg_embed_forward(gg.make_rows(table), 50, 33, None, 40, 1.0, gg.make_rows(out), st)
+    assert torch.equal(out.cpu(), table[:40].cpu().float()) and untouched(flat, own)
+    # more rows than the table has: zeros, and the status word
+    out, _, _ = like(60, 33, F32, DEV)
+    gg.gg_embed_forward(gg.make_rows(table), 50, 33, None, 60, 1.0, gg.make_rows(out), st)
+    assert torch.equal(out[:50].cpu(), table.cpu().float()) and not out[50:].cpu().any()
+    assert int(st) == gg.DEV_BAD_ID
+
+
+@pytest.mark.parametrize("dtype", [torch.int32, torch.int64])
+def test_ids_out_of_range_are_zeros_add_nothing_and_are_reported(dtype):
+    gg = lib()
+    v, dim = 20, 9
+    ids = torch.tensor([0, 19, 20, -1, -2, 2 ** 31 - 1, -2 ** 31, 5], dtype=dtype)
+    if dtype == torch.int64:
+        ids[2], ids[5] = 2 ** 32, 2 ** 40 + 5       # their low words are in range
+    fine = torch.tensor([1, 1, 0, 0, 0, 0, 0, 1], dtype=torch.bool)
+    table = torch.randn(v, dim, generator=gen(5)).to(DEV)
+    out, _, _ = like(8, dim, F32, DEV)
+    st = status_word()
+    gg.gg_embed_forward(gg.make_rows(table), v, dim, ids.to(DEV), 8, 1.0, gg.make_rows(out), st)
+    want = torch.where(fine[:, None], table.cpu()[ids.long().clamp(0, v - 1)], 0.0)
+    assert torch.equal(out.cpu(), want) and int(st) == gg.DEV_BAD_ID
+    st = status_word()
+    grad, _, _ = like(v, dim, F32, DEV)
+    dy = torch.randn(8, dim, generator=gen(6)).to(DEV)
+    ws = torch.empty(gg.gg_ws_embed(8, v, dim), dtype=torch.uint8, device=DEV)
+    gg.gg_embed_backward(gg.make_rows(dy), ids.to(DEV), 8, v, dim, 1.0, gg.make_rows(grad), 0, st, ws)
+    want = torch.zeros(v, dim).index_add_(0, ids[fine].long(), dy.cpu()[fine])
+    assert torch.equal(grad.cpu(), want) and int(st) == gg.DEV_BAD_ID
+
+
+def grad_case(kind, n, v, dim, tdy, tgrad, add=False, idt=torch.int64, lead=1, pad=0, scale=1.3):
+    gg, g = lib(), gen(kind, n, v, dim)
+    print(f"gradient of {n} rows of {dim} ({tdy}) to {v} ({tgrad}), ids {kind}, add {add}",
+          flush=True)
+    dy = rows(torch.randn(n, dim, generator=g), tdy, DEV, lead=lead, pad=pad)
+    ids = make_ids(kind, n, v, g, idt)
+    grad, flat, own = like(v, dim, tgrad, DEV, lead=lead, pad=pad)
+    old = torch.zeros(v, dim, dtype=torch.float64)
+    if add:
+        grad.copy_(torch.randn(v, dim, generator=g).to(tgrad))
+        old = grad.cpu().double()
+    st = status_word()
+    ws = torch.full((gg.gg_ws_embed(n, v, dim),), 0xFF, dtype=torch.uint8, device=DEV)
+    flags = gg.GG_EMBED_ADD if add else 0
+    gg.gg_embed_backward(gg.make_rows(dy), ids.to(DEV), n, v, dim, scale, gg.make_rows(grad), flags,
+                         st, ws)
+    here = ids >= 0
+    x, i = dy.cpu().double()[here], ids[here].long()
+    s64 = torch.tensor(scale, dtype=F32).double()
+    total = torch.zeros(v, dim, dtype=torch.float64).index_add_(0, i, x) * s64
+    mags = torch.zeros(v, dim, dtype=torch.float64).index_add_(0, i, x.abs()) * s64
+    m = torch.bincount(i, minlength=v)[:, None].double()
+    want = old + total
+    bound = (m + 3) * U * (mags + old.abs()) + 1.01 * UNIT[tgrad] * want.abs() + FLOOR[tgrad]
+    assert within(grad, want, bound) <= 0
+    if add:                            # rows that do not occur stay as they are
+        away = (m == 0)[:, 0]
+        assert torch.equal(grad.cpu().double()[away], old[away])
+    assert untouched(flat, own) and int(st) == 0
+    return dy, ids, grad
+
+
+@pytest.mark.parametrize("kind", ["same", "padding", "distinct", "frequent", "random"])
+@pytest.mark.parametrize("n,v,dim", [(1, 1, 1), (3, 2, 5), (64, 300, 8), (1000, 257, 33),
+                                     (5000, 3, 12), (2500, 4000, 100), (700, 65, 1030)])
+@pytest.mark.parametrize("add", [False, True])
+def test_gradient(kind, n, v, dim, add):
+    grad_case(kind, n, v, dim, F32, F32, add, torch.int32 if n % 2 else torch.int64, pad=n % 3)
+
+
+@pytest.mark.parametrize("tdy,tgrad", [p for p in itertools.product((F32, F16, BF16), repeat=2)
+                                       if p != (F32, F32)])
+@pytest.mark.parametrize("n,v,dim", [(900, 300, 7), (900, 300, 602)])
+@pytest.mark.parametrize("add", [False, True])
+def test_gradient_types(tdy, tgrad, n, v, dim, add):
+    grad_case("frequent", n, v, dim, tdy, tgrad, add, pad=1)
+
+
+# More than one tile of the sort (8,192 ids), up to 32 tiles and beyond; runs
+# that cross many chunks; the largest key of one, two and three digits.
+@pytest.mark.parametrize("kind,n,v,dim", [
+    ("frequent", 8193, 2047, 4), ("random", 20_000, 2048, 4), ("frequent", 30_000, 128_000, 16),
+    ("same", 40_001, 70_000, 20), ("frequent", 300_001, 70_000, 4), ("same", 300_001, 5, 8),
+    ("distinct", 262_145, 300_000, 3), ("random", 262_144, 255, 4), ("random", 270_000, 256, 2),
+    ("frequent", 9000, 1_100_000, 1), ("frequent", 270_000, 17_000_000, 1)])
+@pytest.mark.parametrize("add", [False, True])
+def test_gradient_of_many_ids(kind, n, v, dim, add):
+    grad_case(kind, n, v, dim, F32, F32, add)
+
+
+def test_gradient_without_ids_clears_the_rows():
+    gg = lib()
+    grad, flat, own = like(1000, 33, BF16, DEV, lead=1, pad=2)
+    dy = torch.empty(0, 33, device=DEV)
+    st, ws = status_word(), torch.empty(0, dtype=torch.uint8, device=DEV)
+    ids = torch.empty(0, dtype=torch.int64, device=DEV)
+    gg.gg_embed_backward(gg.make_rows(dy), ids, 0, 1000, 33, 1.0, gg.make_rows(grad), 0, st, ws)
+    assert not grad.cpu().any() and untouched(flat, own)
+
+
+def test_gradient_of_one_broadcast_row():
+    """dy of stride 0: every id gets the same row."""
+    gg, n, v, dim = lib(), 500, 40, 19
+    dy = torch.randn(1, dim, generator=gen(8)).to(DEV).expand(n, dim)
+    ids = make_ids("random", n, v, gen(9))
+    grad, _, _ = like(v, dim, F32, DEV)
+    ws = torch.empty(gg.gg_ws_embed(n, v, dim), dtype=torch.uint8, device=DEV)
+    gg.gg_embed_backward(gg.make_rows(dy), ids.to(DEV), n, v, dim, 1.0, gg.make_rows(grad), 0,
+                         status_word(), ws)
+    m = torch.bincount(ids, minlength=v)[:, None].double()
+    want = m * dy[0].cpu().double()
+    assert within(grad, want, (m + 1) * U * want.abs() + FLOOR[F32]) <= 0
+
+
+def test_gradient_is_the_same_each_time_and_on_another_stream():
+    gg = lib()
+    dy, ids, grad = grad_case("frequent", 50_000, 3000, 37, F32, F32)
+    first = grad.clone()
+    side = torch.cuda.Stream()
+    ws = torch.empty(gg.gg_ws_embed(50_000, 3000, 37), dtype=torch.uint8, device=DEV)
+    at, st = ids.to(DEV), status_word()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        grad.zero_()
+        side.wait_stream(torch.cuda.current_stream())
+        gg.gg_embed_backward(gg.make_rows(dy), at, 50_000, 3000, 37, 1.3, gg.make_rows(grad), 0, st,
+                             ws, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(grad, first)
+
+
+def test_gradient_against_differences():
+    """The lookup is linear in the table: its change over a step is the
+    gradient's product with the step, up to the fp32 roundings of both."""
+    gg, g = lib(), gen(11)
+    n, v, dim, scale = 400, 60, 24, 1.5
+    ids = make_ids("frequent", n, v, g)
+    # multiples of 2^-8: table, step and products are exact in fp32
+    table = (torch.randn(v, dim, generator=g) * 256).round() / 256
+    step = (torch.randn(v, dim, generator=g) * 256).round() / 256
+    c = torch.randn(n, dim, generator=g)
+    outs = []
+    for t in (table, table + step):
+        out, _, _ = like(n, dim, F32, DEV)
+        gg.gg_embed_forward(gg.make_rows(t.to(DEV)), v, dim, ids.to(DEV), n, scale,
+                            gg.make_rows(out), status_word())
+        outs.append(out.cpu().double())
+    grad, _, _ = like(v, dim, F32, DEV)
+    ws = torch.empty(gg.gg_ws_embed(n, v, dim), dtype=torch.uint8, device=DEV)
+    gg.gg_embed_backward(gg.make_rows(c.to(DEV)), ids.to(DEV), n, v, dim, scale, gg.make_rows(grad),
+                         0, status_word(), ws)
+    changed = float((c.double() * (outs[1] - outs[0])).sum())
+    product = float((grad.cpu().double() * step.double()).sum())
+    size = float((c.double().abs() * (outs[1] - outs[0]).abs()).sum())
+    assert abs(changed - product) <= (n + 3) * U * size
+
+
+def test_a_gradient_step_on_the_table_itself():
+    """GG_EMBED_ADD with a negative scale on the table's own rows."""
+    gg, g = lib(), gen(12)
+    n, v, dim = 300, 1000, 50
+    table = torch.randn(v, dim, generator=g)
+    dy, ids = torch.randn(n, dim, generator=g), make_ids("frequent", n, v, g)
+    t = table.to(DEV)
+    ws = torch.empty(gg.gg_ws_embed(n, v, dim), dtype=torch.uint8, device=DEV)
+    gg.gg_embed_backward(gg.make_rows(dy.to(DEV)), ids.to(DEV), n, v, dim, -0.125, gg.make_rows(t),
+                         gg.GG_EMBED_ADD, status_word(), ws)
+    here = ids >= 0
+    add = torch.zeros(v, dim, dtype=torch.float64).index_add_(0, ids[here], dy.double()[here])
+    mag = torch.zeros(v, dim, dtype=torch.float64).index_add_(0, ids[here], dy.double()[here].abs())
+    m = torch.bincount(ids[here], minlength=v)[:, None].double()
+    want = table.double() - 0.125 * add
+    assert within(t, want, (m + 2) * U * (0.125 * mag + table.double().abs())) <= 0
+
+
+def test_rows_beyond_four_gigabytes():
+    """Offsets of the last rows pass 32 bits, in bytes and in elements."""
+    gg = lib()
+    dim, v = 2048, 2_200_000            # 4.5e9 elements of 2 bytes
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB of device memory")
+    table = torch.zeros(v, dim, dtype=BF16, device=DEV)
+    ids = torch.tensor([0, v - 1, v // 2, v - 1])
+    table[ids] = torch.randn(4, dim, generator=gen(13)).to(BF16).to(DEV)
+    out, _, _ = like(4, dim, BF16, DEV)
+    st = status_word()
+    gg.gg_embed_forward(gg.make_rows(table), v, dim, ids.to(DEV), 4, 1.0, gg.make_rows(out), st)
+    assert torch.equal(out, table[ids.to(DEV)])
+    ws = torch.empty(gg.gg_ws_embed(4, v, dim), dtype=torch.uint8, device=DEV)
+    table.fill_(float("nan"))
+    gg.gg_embed_backward(gg.make_rows(out), ids.to(DEV), 4, v, dim, 1.0, gg.make_rows(table), 0, st,
+                         ws)
+    rest = table[1:v // 2].any() | table[v // 2 + 1:v - 1].any()
+    assert not bool(rest) and int(st) == 0
+    twice = (out[1].cpu().float() + out[3].cpu().float()).to(BF16)
+    assert torch.equal(table[v - 1].cpu(), twice) and torch.equal(table[0], out[0])

@@ -1,0 +1,122 @@
+"""Host-side argument checks of the operator calls: a bad call is refused with
+a message before anything is enqueued, so no GPU is needed.  Addresses here
+are numbers that nothing reads."""
+import ctypes as C
+import os
+import subprocess
+import tempfile
+
+import pytest
+import torch
+
+from paper_2606_02916_amd import gg
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P = 1 << 20
+
+
+def rows(dtype=gg.GG_F32, data=P, stride=400, group=0, scales=P, scales_stride=64):
+    r = gg.gg_rows_t()
+    r.data, r.stride, r.dtype, r.group, r.scales, r.scales_stride = (data, stride, dtype, group,
+                                                                     scales, scales_stride)
+    return r
+
+
+def refused(call, args, change, word):
+    args = {**args, **change}
+    ref = [C.byref(v) if isinstance(v, C.Structure) else v for v in args.values()]
+    assert call(*ref) == gg.GG_ERR_ARG, change
+    assert word in gg.gg_last_error(), (change, gg.gg_last_error())
+
+
+def test_rows_layout_matches_the_header():
+    src = r"""
+#include <stddef.h>
+#include <stdio.h>
+#include "gg.h"
+int main() {
+  printf("%zu %zu %zu %zu %zu %zu %zu\n", sizeof(gg_rows_t), offsetof(gg_rows_t, stride),
+         offsetof(gg_rows_t, dtype), offsetof(gg_rows_t, group), offsetof(gg_rows_t, scales),
+         offsetof(gg_rows_t, scales_stride), offsetof(gg_rows_t, data));
+  printf("%d %d %d %d %d\n", GG_F32, GG_F16, GG_BF16, GG_E4M3, GG_EMBED_ADD);
+}
+"""
+    d = tempfile.mkdtemp(prefix="ggrows_")
+    with open(os.path.join(d, "p.cpp"), "w") as f:
+        f.write(src)
+    subprocess.run(["g++", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
+                    "-I" + os.path.join(ROOT, "include"), os.path.join(d, "p.cpp"), "-o",
+                    os.path.join(d, "p")], check=True)
+    a, b = subprocess.run([os.path.join(d, "p")], capture_output=True,
+                          text=True).stdout.split("\n")[:2]
+    R = gg.gg_rows_t
+    assert [int(x) for x in a.split()] == [C.sizeof(R), R.stride.offset, R.dtype.offset,
+                                           R.group.offset, R.scales.offset, R.scales_stride.offset,
+                                           R.data.offset]
+    assert [int(x) for x in b.split()] == [gg.GG_F32, gg.GG_F16, gg.GG_BF16, gg.GG_E4M3,
+                                           gg.GG_EMBED_ADD]
+
+
+def test_make_rows_refuses_what_it_cannot_describe():
+    x = torch.zeros(6, 40)
+    assert gg.make_rows(x[:, 3:9]).stride == 160
+    assert gg.make_rows(x[:1].expand(9, 40)).stride == 0
+    q = torch.zeros(6, 40, dtype=torch.float8_e4m3fn)
+    assert gg.make_rows(q, scales=torch.zeros(6, 3), group=16).group == 16
+    assert gg.make_rows(q, scales=torch.zeros(6)).scales_stride == 4
+    for bad in (lambda: gg.make_rows(x.t()), lambda: gg.make_rows(x[0]),
+                lambda: gg.make_rows(x.double()), lambda: gg.make_rows(x[:, ::2]),
+                lambda: gg.make_rows(q), lambda: gg.make_rows(q, scales=torch.zeros(6, 2), group=16),
+                lambda: gg.make_rows(q, scales=torch.zeros(6).double()),
+                lambda: gg.make_rows(q, scales=torch.zeros(3, 6).t(), group=16),
+                lambda: gg.make_rows(x, scales=torch.zeros(6))):
+        with pytest.raises(gg.GGError):
+            bad()
+
+
+LOOKUP = dict(table=rows(), num_rows=50, dim=100, ids=P, bits=64, n=7, scale=1.0, out=rows(),
+              status=P, stream=None)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(status=None), "status"), (dict(dim=0), "dim"), (dict(dim=32769), "dim"),
+    (dict(n=-1), "n -1"), (dict(num_rows=-1), "num_rows"), (dict(bits=16), "16 bits"),
+    (dict(ids=P + 4), "aligned"), (dict(table=None), "table"), (dict(out=None), "out"),
+    (dict(table=rows(data=None)), "table: data"), (dict(table=rows(data=P + 2)), "table: not aligned"),
+    (dict(out=rows(stride=396)), "out: stride"), (dict(out=rows(gg.GG_E4M3)), "out: dtype"),
+    (dict(table=rows(7)), "table: dtype"), (dict(table=rows(stride=-400)), "table: stride"),
+    (dict(table=rows(gg.GG_E4M3, group=8)), "group"), (dict(table=rows(gg.GG_E4M3, group=48)), "group"),
+    (dict(table=rows(gg.GG_E4M3, scales=None)), "scales"),
+    (dict(table=rows(gg.GG_E4M3, scales=P + 2)), "scales"), (dict(n=1 << 33), "too many")])
+def test_lookup_refuses(change, word):
+    refused(gg.lib.gg_embed_forward, LOOKUP, change, word)
+
+
+GRAD = dict(dy=rows(), ids=P, bits=64, n=7, num_rows=50, dim=100, scale=1.0, grad=rows(), flags=0,
+            status=P, ws=P, ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(status=None), "status"), (dict(dim=0), "dim"), (dict(n=-1), "n = -1"),
+    (dict(n=(1 << 31) - 1), "n = "), (dict(num_rows=(1 << 31) - 1), "num_rows"),
+    (dict(bits=8), "8 bits"), (dict(ids=None), "ids are NULL"), (dict(ids=P + 2), "aligned"),
+    (dict(flags=2), "flags"), (dict(dy=None), "dy"), (dict(dy=rows(gg.GG_E4M3)), "dy: dtype"),
+    (dict(grad=rows(stride=0)), "grad: stride"), (dict(grad=rows(data=P + 1)), "grad: not aligned"),
+    (dict(ws=None), "workspace"), (dict(ws_bytes=64), "workspace")])
+def test_gradient_refuses(change, word):
+    refused(gg.lib.gg_embed_backward, GRAD, change, word)
+
+
+def test_workspace_sizes():
+    assert gg.gg_ws_embed(0, 10, 4) == 0 or gg.gg_ws_embed(0, 10, 4) % 256 == 0
+    assert gg.gg_ws_embed(1000, 10, 4) >= 4 * 4 * 1000
+    assert gg.gg_ws_embed(-1, 10, 4) == gg.gg_ws_embed(1 << 31, 10, 4) == gg.gg_ws_embed(9, 9, 0) == 0
+
+
+def test_bindings_check_the_ids():
+    with pytest.raises(gg.GGError, match="ids"):
+        gg._ids(torch.zeros(3), 3, "x")
+    with pytest.raises(gg.GGError, match="ids"):
+        gg._ids(torch.zeros(3, dtype=torch.int32), 4, "x")
+    with pytest.raises(gg.GGError, match="ids"):
+        gg._ids(torch.zeros(8, dtype=torch.int64)[::2], 4, "x")
