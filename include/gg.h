@@ -605,6 +605,36 @@ int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t id_bits, i
                       int32_t flags, int32_t* status_d, void* ws, size_t ws_bytes,
                       hipStream_t stream);
 
+#define GG_NORM_MAX_DIM 16384
+#define GG_NORM_MAX_ROWS (1LL << 27)
+
+/* Root-mean-square norm of n rows: s = x + res (res NULL: s = x),
+ * rstd = (mean(s^2) + eps)^-1/2, y = s * rstd * w (w_d NULL: ones), in fp32
+ * from the unrounded s.  Outputs, each NULL where it is not wanted: sum (s),
+ * y, q (y in 8 bits) and rstd_d [n].  q's scale is max(|y|) of its group or
+ * row / 448, at least 2^-126, and its code y / scale rounded to nearest even; a
+ * group that holds a NaN or an infinity has that scale.  x and y have one type
+ * of GG_F32, GG_F16 and GG_BF16; res and sum have that type or both GG_F32;
+ * weights [dim] too (w_dtype).  sum and y may be the memory of res or x. */
+int gg_rmsnorm_forward(const gg_rows_t* x, const gg_rows_t* res, int64_t n, int32_t dim,
+                       const void* w_d, int32_t w_dtype, float eps, const gg_rows_t* sum,
+                       const gg_rows_t* y, const gg_rows_t* q, float* rstd_d, hipStream_t stream);
+
+size_t gg_ws_rmsnorm(int64_t n, int32_t dim);
+
+/* Its gradient.  dy: the gradient of y (straight through the rounding to 8
+ * bits); dsum: the gradient that reaches s by other ways, or NULL; s and rstd_d
+ * as the forward call gave them.  dx = dsum + rstd * (dy w - s rstd^2
+ * mean(dy w s)) is the gradient of x and of res alike; dw_d [dim] (fp32, or
+ * NULL: not wanted) = sum over the rows of dy s rstd, in an order that depends
+ * on n and dim alone.  dy has the type of y, and s, dsum and dx one type: that
+ * one or GG_F32.  dx may be the memory of dsum, dy or s.  ws: for dw_d only,
+ * 16-byte aligned. */
+int gg_rmsnorm_backward(const gg_rows_t* dy, const gg_rows_t* dsum, const gg_rows_t* s,
+                        const float* rstd_d, int64_t n, int32_t dim, const void* w_d,
+                        int32_t w_dtype, const gg_rows_t* dx, float* dw_d, void* ws,
+                        size_t ws_bytes, hipStream_t stream);
+
 /* Helpers. */
 
 /* Reads the sticky device status word once the work queued so far on

@@ -1,0 +1,479 @@
+// Root-mean-square norm with the residual's addition and 8-bit rows with
+// scales, forward and backward.
+#include "rows.hpp"
+
+namespace gg {
+namespace {
+
+constexpr float kE4M3Max = 448.0f;
+constexpr float kScaleMin = 1.17549435e-38f;   // 2^-126
+
+// A row's pieces are dealt to a group of lanes: piece p = step * lanes + lane.
+// A group is 2^lanes_log lanes of a wave (several rows per wave for narrow
+// rows), or the whole block for wide ones.
+struct NormArgs {
+  KRows x, res, sum, y, q;     // p == nullptr: absent
+  const char* w;               // nullptr: ones
+  int32_t w_f32;
+  float eps;
+  float* rstd;
+  int64_t n;
+  int32_t dim, pieces, lanes_log;
+  int32_t group_lanes_log;     // lanes that share a scale; -1: the row
+  int32_t group_log;
+};
+
+template <bool BLK>
+__device__ __forceinline__ float group_sum(float v, int lanes, float* lds) {
+  if constexpr (BLK) {
+    v = wave_sum(v);
+    __syncthreads();
+    if (lane_id() == 0) lds[threadIdx.x / kWave] = v;
+    __syncthreads();
+    const int waves = lanes / kWave;
+    float t = 0.0f;
+    for (int i = 0; i < waves; ++i) t += lds[i];
+    return t;
+  } else {
+    for (int o = lanes / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, kWave);
+    return v;
+  }
+}
+
+// Maximum of magnitudes as bits: a NaN is more than every number.
+__device__ __forceinline__ uint32_t lanes_max(uint32_t m, int lanes) {
+  for (int o = lanes / 2; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, kWave));
+  return m;
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void load_weight(const char* w, int32_t w_f32, int32_t e,
+                                            float (&v)[V]) {
+  if (!w) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = 1.0f;
+  } else if (sizeof(T) == 4 || w_f32) {
+    row_load<float, V>(w + e * 4LL, v);
+  } else {
+    row_load<T, V>(w + e * (int64_t)sizeof(T), v);
+  }
+}
+
+// s = x + r; y = s * rstd * w; scale = max(amax|y| / 448, 2^-126) per group,
+// code = y / scale rounded to e4m3.
+//
+// Bound by memory: each input is read once, the row stays in registers
+// between the sum of squares and the outputs.  Nothing is stored before the
+// row is read whole, so outputs may lie on the inputs.
+template <typename T, typename R, int V, int STEPS, bool BLK>
+__global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
+  __shared__ float lds[BLK ? 1024 / kWave : 1];
+  const int lanes = BLK ? (int)blockDim.x : 1 << a.lanes_log;
+  const int64_t row = BLK ? block_index() : (block_index() * kBlock + threadIdx.x) >> a.lanes_log;
+  if (row >= a.n) return;
+  const int l = BLK ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1);
+  float s[STEPS][V];
+  float w[STEPS][V];
+  float sq = 0.0f;
+#pragma unroll
+  for (int t = 0; t < STEPS; ++t) {
+    const int p = t * lanes + l;
+#pragma unroll
+    for (int k = 0; k < V; ++k) s[t][k] = w[t][k] = 0.0f;
+    if (p < a.pieces) {
+      int32_t skip;
+      const int32_t e = piece_start<V>(p, a.dim, &skip);
+      row_load<T, V>(a.x.p + row * a.x.stride + e * (int64_t)sizeof(T), s[t]);
+      if (a.res.p) {
+        float r[V];
+        row_load<R, V>(a.res.p + row * a.res.stride + e * (int64_t)sizeof(R), r);
+#pragma unroll
+        for (int k = 0; k < V; ++k) s[t][k] += r[k];
+      }
+      load_weight<T, V>(a.w, a.w_f32, e, w[t]);
+#pragma unroll
+      for (int k = 0; k < V; ++k) sq += k >= skip ? s[t][k] * s[t][k] : 0.0f;
+    }
+  }
+  sq = group_sum<BLK>(sq, lanes, lds);
+  const float rstd = 1.0f / sqrtf(sq / (float)a.dim + a.eps);
+  if (a.rstd && l == 0) a.rstd[row] = rstd;
+
+#pragma unroll
+  for (int t = 0; t < STEPS; ++t) {
+    const int p = t * lanes + l;
+    if (p < a.pieces) {
+      int32_t skip;
+      const int32_t e = piece_start<V>(p, a.dim, &skip);
+      if (a.sum.p) row_store<R, V>(a.sum.p + row * a.sum.stride + e * (int64_t)sizeof(R), s[t]);
+#pragma unroll
+      for (int k = 0; k < V; ++k) s[t][k] = s[t][k] * rstd * w[t][k];
+      if (a.y.p) row_store<T, V>(a.y.p + row * a.y.stride + e * (int64_t)sizeof(T), s[t]);
+    }
+  }
+  if (!a.q.p) return;
+
+  // Largest magnitudes, each piece's own elements only.
+  uint32_t top[STEPS], all = 0;
+#pragma unroll
+  for (int t = 0; t < STEPS; ++t) {
+    const int32_t skip = max(0, (t * lanes + l) * V - (a.dim - V));
+    top[t] = 0;
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+      top[t] = max(top[t], k >= skip ? __float_as_uint(s[t][k]) & 0x7fffffffu : 0u);
+    all = max(all, top[t]);
+  }
+  const bool per_row = a.group_lanes_log < 0;
+  if (per_row) {
+    all = lanes_max(all, min(lanes, kWave));
+    if constexpr (BLK) {
+      __syncthreads();
+      if (lane_id() == 0) ((uint32_t*)lds)[threadIdx.x / kWave] = all;
+      __syncthreads();
+      for (int i = 0; i < lanes / kWave; ++i) all = max(all, ((uint32_t*)lds)[i]);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < STEPS; ++t) {
+    const int p = t * lanes + l;
+    const uint32_t m = per_row ? all : lanes_max(top[t], 1 << a.group_lanes_log);
+    if (p >= a.pieces) continue;
+    float scale = __uint_as_float(m) / kE4M3Max;
+    scale = scale < kScaleMin ? kScaleMin : scale;   // a NaN stays
+    const float inv = 1.0f / scale;
+    const bool first = per_row ? p == 0 : (p & ((1 << a.group_lanes_log) - 1)) == 0;
+    if (first)
+      ((float*)(a.q.scales + row * a.q.sstride))[per_row ? 0 : (p * V) >> a.group_log] = scale;
+    int32_t skip;
+    const int32_t e = piece_start<V>(p, a.dim, &skip);
+    float c[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) c[k] = s[t][k] * inv;
+    char* to = a.q.p + row * a.q.stride + e;
+    if (skip == 0) {
+      row_store<e4m3, V>(to, c);
+    } else {
+      // the skipped elements have their own piece's scale
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const float one[1] = {c[k]};
+        if (k >= skip) row_store<e4m3, 1>(to + k, one);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Backward.  With g = dy * w and rho = rstd:
+//   dx = dsum + rho * (g - s * rho^2 * mean(g * s)),  dw = sum_rows dy * s * rho.
+// Blocks stay for many rows and keep their share of dw in registers; the
+// shares of all blocks are added in a second launch, in the order of the
+// blocks.
+// ---------------------------------------------------------------------------
+struct NormBackArgs {
+  KRows dy, dsum, s, dx;
+  const char* w;
+  int32_t w_f32;
+  const float* rstd;
+  int64_t n;
+  int32_t dim, pieces, lanes_log;
+  float* part;                 // [blocks][dim], or nullptr: no dw
+};
+
+template <typename T, typename R, int V, int STEPS, bool BLK>
+__global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm_back(NormBackArgs a) {
+  __shared__ float lds[BLK ? 1024 / kWave : kBlock * V];
+  const int lanes = BLK ? (int)blockDim.x : 1 << a.lanes_log;
+  const int groups = BLK ? 1 : kBlock >> a.lanes_log;
+  const int g = BLK ? 0 : (int)threadIdx.x >> a.lanes_log;
+  const int l = BLK ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1);
+  float w[STEPS][V], acc[STEPS][V];
+#pragma unroll
+  for (int t = 0; t < STEPS; ++t) {
+    const int p = t * lanes + l;
+    int32_t skip;
+#pragma unroll
+    for (int k = 0; k < V; ++k) acc[t][k] = w[t][k] = 0.0f;
+    if (p < a.pieces) load_weight<T, V>(a.w, a.w_f32, piece_start<V>(p, a.dim, &skip), w[t]);
+  }
+  for (int64_t row = (int64_t)blockIdx.x * groups + g; row < a.n;
+       row += (int64_t)gridDim.x * groups) {
+    const float rho = a.rstd[row];
+    float s[STEPS][V], d[STEPS][V], ds[STEPS][V];
+    float dot = 0.0f;
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t) {
+      const int p = t * lanes + l;
+#pragma unroll
+      for (int k = 0; k < V; ++k) s[t][k] = d[t][k] = ds[t][k] = 0.0f;
+      if (p < a.pieces) {
+        int32_t skip;
+        const int32_t e = piece_start<V>(p, a.dim, &skip);
+        row_load<T, V>(a.dy.p + row * a.dy.stride + e * (int64_t)sizeof(T), d[t]);
+        row_load<R, V>(a.s.p + row * a.s.stride + e * (int64_t)sizeof(R), s[t]);
+        if (a.dsum.p)
+          row_load<R, V>(a.dsum.p + row * a.dsum.stride + e * (int64_t)sizeof(R), ds[t]);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+          s[t][k] *= rho;
+          acc[t][k] += d[t][k] * s[t][k];
+          d[t][k] *= w[t][k];
+          dot += k >= skip ? d[t][k] * s[t][k] : 0.0f;
+        }
+      }
+    }
+    dot = group_sum<BLK>(dot, lanes, lds);
+    const float mean = dot / (float)a.dim;
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t) {
+      const int p = t * lanes + l;
+      if (p < a.pieces) {
+        int32_t skip;
+        const int32_t e = piece_start<V>(p, a.dim, &skip);
+#pragma unroll
+        for (int k = 0; k < V; ++k) d[t][k] = ds[t][k] + rho * (d[t][k] - s[t][k] * mean);
+        row_store<R, V>(a.dx.p + row * a.dx.stride + e * (int64_t)sizeof(R), d[t]);
+      }
+    }
+  }
+  if (!a.part) return;
+  float* part = a.part + (int64_t)blockIdx.x * a.dim;
+#pragma unroll
+  for (int t = 0; t < STEPS; ++t) {
+    if constexpr (!BLK) {
+      // the block's groups, in order
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < V; ++k) lds[k * kBlock + threadIdx.x] = acc[t][k];
+      __syncthreads();
+      if (g == 0)
+        for (int x = 1; x < groups; ++x)
+#pragma unroll
+          for (int k = 0; k < V; ++k) acc[t][k] += lds[k * kBlock + x * lanes + l];
+    }
+    const int p = t * lanes + l;
+    if (g == 0 && p < a.pieces) {
+      int32_t skip;
+      const int32_t e = piece_start<V>(p, a.dim, &skip);
+      row_store<float, V>((char*)(part + e), acc[t]);
+    }
+  }
+}
+
+// dw[j] = sum of the blocks' shares: 64 columns a block, its waves take the
+// shares in turn.
+constexpr int kSumWaves = 16;
+
+__global__ void __launch_bounds__(kSumWaves * kWave) k_norm_dw(const float* part, int32_t blocks,
+                                                              int32_t dim, float* dw) {
+  __shared__ float lds[kSumWaves][kWave];
+  const int w = threadIdx.x / kWave, l = lane_id();
+  const int32_t j = (int32_t)blockIdx.x * kWave + l;
+  float v = 0.0f;
+  if (j < dim)
+#pragma unroll 8
+    for (int32_t b = w; b < blocks; b += kSumWaves) v += part[(int64_t)b * dim + j];
+  lds[w][l] = v;
+  __syncthreads();
+  if (w == 0 && j < dim) {
+#pragma unroll
+    for (int x = 1; x < kSumWaves; ++x) v += lds[x][l];
+    dw[j] = v;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------
+struct Shape {
+  bool blk;
+  int32_t pieces, lanes_log, steps;   // steps: 1, 2 or 4
+  int threads;
+};
+
+// A wave (or part of one) per row up to `wave_steps` pieces per lane, a block
+// per row beyond, of threads with about `blk_steps` pieces each.
+Shape shape_of(int32_t dim, int vec, int wave_steps, int blk_steps) {
+  Shape s;
+  s.pieces = (int32_t)cdiv(dim, vec);
+  s.lanes_log = 0;
+  while (s.lanes_log < 6 && (1 << s.lanes_log) < s.pieces) ++s.lanes_log;
+  s.blk = s.pieces > kWave * wave_steps;
+  s.threads = kBlock;
+  int lanes = 1 << s.lanes_log;
+  if (s.blk) {
+    s.threads = 128;
+    while (s.threads < 1024 && s.threads * blk_steps < s.pieces) s.threads *= 2;
+    lanes = s.threads;
+  }
+  s.steps = 1;
+  while (s.steps * lanes < s.pieces) s.steps *= 2;
+  return s;
+}
+
+// Instantiations: a block per row takes 2 pieces per lane, or 4 of fp32 rows
+// (16,384 elements, 1,024 lanes); a wave per row up to MW.
+#define GG_NORM_LAUNCH(K, T, R, V, MW, S)                                                       \
+  do {                                                                                          \
+    const dim3 threads((unsigned)(S).threads);                                                  \
+    if ((S).blk) {                                                                              \
+      if ((S).steps == 1)                                                                       \
+        hipLaunchKernelGGL((K<T, R, V, 1, true>), grid, threads, 0, stream, a);                 \
+      else if (V > 4 || (S).steps == 2)                                                         \
+        hipLaunchKernelGGL((K<T, R, V, 2, true>), grid, threads, 0, stream, a);                 \
+      else                                                                                      \
+        hipLaunchKernelGGL((K<T, R, V, (V > 4 ? 2 : 4), true>), grid, threads, 0, stream, a);   \
+    } else {                                                                                    \
+      if ((S).steps == 1)                                                                       \
+        hipLaunchKernelGGL((K<T, R, V, 1, false>), grid, threads, 0, stream, a);                \
+      else if (MW == 2 || (S).steps == 2)                                                       \
+        hipLaunchKernelGGL((K<T, R, V, 2, false>), grid, threads, 0, stream, a);                \
+      else                                                                                      \
+        hipLaunchKernelGGL((K<T, R, V, (MW > 2 ? MW : 2), false>), grid, threads, 0, stream, a); \
+    }                                                                                           \
+  } while (0)
+
+constexpr int kWaveSteps = 4, kBackWaveSteps = 2;
+
+template <typename T, typename R>
+int launch_norm(NormArgs& a, hipStream_t stream) {
+  constexpr int V = kVec<T>;
+  const bool wide = a.dim >= V;
+  const int vec = wide ? V : 1;
+  const Shape s = shape_of(a.dim, vec, kWaveSteps, a.n < 256 ? 1 : 2);
+  a.pieces = s.pieces;
+  a.lanes_log = s.lanes_log;
+  a.group_lanes_log = -1;
+  if (a.q.p && a.q.group && a.q.group < a.dim) {
+    a.group_log = __builtin_ctz((unsigned)a.q.group);
+    a.group_lanes_log = a.group_log - __builtin_ctz((unsigned)vec);
+  }
+  const dim3 grid = grid_of(s.blk ? a.n : cdiv(a.n << s.lanes_log, kBlock));
+  if (!wide)
+    hipLaunchKernelGGL((k_norm<T, R, 1, 1, false>), grid, dim3(kBlock), 0, stream, a);
+  else
+    GG_NORM_LAUNCH(k_norm, T, R, V, kWaveSteps, s);
+  GG_LAUNCH_CHECK("k_norm");
+  return GG_OK;
+}
+
+// Blocks of the backward pass.
+int back_blocks(int64_t n, const Shape& s) {
+  const int64_t rows = s.blk ? 1 : kBlock >> s.lanes_log;   // at a time in a block
+  return (int)std::min<int64_t>(cdiv(n, rows), s.threads <= 256 ? 1024 : 512);
+}
+
+template <typename T, typename R>
+int launch_back(NormBackArgs& a, float* dw, hipStream_t stream) {
+  constexpr int V = kVec<T>;
+  const bool wide = a.dim >= V;
+  const Shape s = shape_of(a.dim, wide ? V : 1, kBackWaveSteps, 2);
+  a.pieces = s.pieces;
+  a.lanes_log = s.lanes_log;
+  const int blocks = back_blocks(a.n, s);
+  const dim3 grid((unsigned)blocks);
+  if (blocks > 0) {
+    if (!wide)
+      hipLaunchKernelGGL((k_norm_back<T, R, 1, 1, false>), grid, dim3(kBlock), 0, stream, a);
+    else
+      GG_NORM_LAUNCH(k_norm_back, T, R, V, kBackWaveSteps, s);
+    GG_LAUNCH_CHECK("k_norm_back");
+  }
+  if (dw) {
+    hipLaunchKernelGGL(k_norm_dw, dim3((unsigned)cdiv(a.dim, kWave)), dim3(kSumWaves * kWave), 0,
+                       stream, a.part, blocks, a.dim, dw);
+    GG_LAUNCH_CHECK("k_norm_dw");
+  }
+  return GG_OK;
+}
+
+// Optional rows: absent (p stays NULL) or checked.
+int pack_optional(const gg_rows_t* r, const char* name, int64_t n, int64_t dim, uint32_t types,
+                  bool written, KRows* out) {
+  if (!r) return GG_OK;
+  return pack_rows(r, name, n, dim, types, written, out);
+}
+
+}  // namespace
+}  // namespace gg
+
+using namespace gg;
+
+extern "C" int gg_rmsnorm_forward(const gg_rows_t* x, const gg_rows_t* res, int64_t n, int32_t dim,
+                                  const void* w_d, int32_t w_dtype, float eps,
+                                  const gg_rows_t* sum, const gg_rows_t* y, const gg_rows_t* q,
+                                  float* rstd_d, hipStream_t stream) {
+  GG_REQUIRE(dim >= 1 && dim <= GG_NORM_MAX_DIM, "dim %d outside 1..%d", dim, GG_NORM_MAX_DIM);
+  GG_REQUIRE(n >= 0 && n <= GG_NORM_MAX_ROWS, "n = %lld unsupported", (long long)n);
+  GG_REQUIRE(eps >= 0.0f, "eps must not be negative");
+  GG_REQUIRE(sum || y || q || rstd_d, "no output asked for");
+  NormArgs a = {};
+  int rc = pack_rows(x, "x", n, dim, kBitFloats, false, &a.x);
+  if (rc != GG_OK) return rc;
+  const int32_t t = x->dtype;
+  GG_REQUIRE(!w_d || w_dtype == t || w_dtype == GG_F32, "weights of dtype %d for x of dtype %d",
+             w_dtype, t);
+  GG_REQUIRE(!w_d || (uintptr_t)w_d % elem_bytes(w_dtype) == 0, "weights are not aligned");
+  GG_REQUIRE((uintptr_t)rstd_d % 4 == 0, "rstd is not aligned");
+  const uint32_t stream_types = (1u << t) | kBitF32;
+  rc = pack_optional(res, "res", n, dim, stream_types, false, &a.res);
+  if (rc == GG_OK) rc = pack_optional(sum, "sum", n, dim, stream_types, true, &a.sum);
+  if (rc == GG_OK) rc = pack_optional(y, "y", n, dim, 1u << t, true, &a.y);
+  if (rc == GG_OK) rc = pack_optional(q, "q", n, dim, kBitE4M3, true, &a.q);
+  if (rc != GG_OK) return rc;
+  GG_REQUIRE(!res || !sum || res->dtype == sum->dtype, "res and sum differ in dtype");
+  if (n == 0) return GG_OK;
+  const int32_t r = res ? res->dtype : sum ? sum->dtype : t;
+  a.w = (const char*)w_d;
+  a.w_f32 = w_dtype == GG_F32;
+  a.eps = eps;
+  a.rstd = rstd_d;
+  a.n = n;
+  a.dim = dim;
+  GG_FOR_FLOAT(t, T, {
+    if (r == t) return launch_norm<T, T>(a, stream);
+    return launch_norm<T, float>(a, stream);
+  });
+}
+
+extern "C" size_t gg_ws_rmsnorm(int64_t n, int32_t dim) {
+  if (n < 0 || n > GG_NORM_MAX_ROWS || dim < 1 || dim > GG_NORM_MAX_DIM) return 0;
+  return align_up((size_t)std::min<int64_t>(n, 1024) * dim * sizeof(float), 256);
+}
+
+extern "C" int gg_rmsnorm_backward(const gg_rows_t* dy, const gg_rows_t* dsum, const gg_rows_t* s,
+                                   const float* rstd_d, int64_t n, int32_t dim, const void* w_d,
+                                   int32_t w_dtype, const gg_rows_t* dx, float* dw_d, void* ws,
+                                   size_t ws_bytes, hipStream_t stream) {
+  GG_REQUIRE(dim >= 1 && dim <= GG_NORM_MAX_DIM, "dim %d outside 1..%d", dim, GG_NORM_MAX_DIM);
+  GG_REQUIRE(n >= 0 && n <= GG_NORM_MAX_ROWS, "n = %lld unsupported", (long long)n);
+  NormBackArgs a = {};
+  int rc = pack_rows(dy, "dy", n, dim, kBitFloats, false, &a.dy);
+  if (rc != GG_OK) return rc;
+  const int32_t t = dy->dtype;
+  rc = pack_rows(s, "s", n, dim, (1u << t) | kBitF32, false, &a.s);
+  if (rc != GG_OK) return rc;
+  const int32_t r = s->dtype;
+  rc = pack_rows(dx, "dx", n, dim, 1u << r, true, &a.dx);
+  if (rc == GG_OK) rc = pack_optional(dsum, "dsum", n, dim, 1u << r, false, &a.dsum);
+  if (rc != GG_OK) return rc;
+  GG_REQUIRE(n == 0 || rstd_d, "rstd is NULL");
+  GG_REQUIRE((uintptr_t)rstd_d % 4 == 0 && (uintptr_t)dw_d % 4 == 0, "rstd or dw is not aligned");
+  GG_REQUIRE(!w_d || w_dtype == t || w_dtype == GG_F32, "weights of dtype %d for dy of dtype %d",
+             w_dtype, t);
+  GG_REQUIRE(!w_d || (uintptr_t)w_d % elem_bytes(w_dtype) == 0, "weights are not aligned");
+  const size_t need = gg_ws_rmsnorm(n, dim);
+  GG_REQUIRE(!dw_d || need == 0 || (ws && (uintptr_t)ws % 16 == 0 && ws_bytes >= need),
+             "workspace of %zu bytes < %zu, or not aligned", ws_bytes, need);
+  a.w = (const char*)w_d;
+  a.w_f32 = w_dtype == GG_F32;
+  a.rstd = rstd_d;
+  a.n = n;
+  a.dim = dim;
+  a.part = dw_d ? (float*)ws : nullptr;
+  GG_FOR_FLOAT(t, T, {
+    if (r == t) return launch_back<T, T>(a, dw_d, stream);
+    return launch_back<T, float>(a, dw_d, stream);
+  });
+}

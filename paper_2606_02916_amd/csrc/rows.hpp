@@ -145,7 +145,18 @@ __device__ __forceinline__ int32_t piece_start(int32_t p, int32_t dim, int32_t* 
   return e;
 }
 
-// Runs f with a value of the dtype's element type.
+// A launch of `blocks` blocks: one dimension holds fewer than 2^32 lanes.
+constexpr int64_t kGridX = 1 << 21;
+
+inline dim3 grid_of(int64_t blocks) {
+  return dim3((unsigned)std::min(blocks, kGridX), (unsigned)cdiv(blocks, kGridX));
+}
+
+__device__ __forceinline__ int64_t block_index() {
+  return (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+}
+
+// Runs the statements with T as the dtype's element type.
 #define GG_FOR_FLOAT(dtype, T, ...)      \
   do {                                   \
     if ((dtype) == GG_F32) {             \

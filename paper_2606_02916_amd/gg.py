@@ -156,6 +156,9 @@ SIGNATURES = {
     "gg_ws_embed": (_SZ, [_I64, _I64, _I32]),
     "gg_embed_backward": (C.c_int, [_P, _P, _I32, _I64, _I64, _I32, C.c_float, _P, _I32, _P, _P,
                                     _SZ, _P]),
+    "gg_rmsnorm_forward": (C.c_int, [_P, _P, _I64, _I32, _P, _I32, C.c_float, _P, _P, _P, _P, _P]),
+    "gg_ws_rmsnorm": (_SZ, [_I64, _I32]),
+    "gg_rmsnorm_backward": (C.c_int, [_P, _P, _P, _P, _I64, _I32, _P, _I32, _P, _P, _P, _SZ, _P]),
     "gg_read_status": (C.c_int, [_P, _P, _P]),
     "gg_status_string": (C.c_char_p, [_I32]),
     "gg_last_error": (C.c_char_p, []),
@@ -526,6 +529,45 @@ def gg_embed_backward(dy, ids, n, num_rows, dim, scale, grad, flags, status, ws,
     return check(lib.gg_embed_backward(_rows(dy), ptr, bits, n, num_rows, dim, scale, _rows(grad),
                                        flags, _ptr(status), _ptr(ws), ws.numel(),
                                        _stream(stream)), "gg_embed_backward")
+
+
+def _weight(w, dim, what):
+    """Address and dtype of dim contiguous weights."""
+    if w is None:
+        return None, GG_F32
+    if w.dtype not in _DTYPES or not w.is_contiguous() or w.numel() != dim:
+        raise GGError(f"{what}: weights must be {dim} contiguous values")
+    return w.data_ptr(), _DTYPES[w.dtype]
+
+
+def _fp32(t, n, what):
+    """Address of at least n contiguous fp32 values."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or not t.is_contiguous() or t.numel() < n:
+        raise GGError(f"{what}: at least {n} contiguous fp32 values are needed")
+    return t.data_ptr()
+
+
+def gg_rmsnorm_forward(x, res, n, dim, w, eps, sum, y, q, rstd, stream=None):
+    """x, res, sum, y, q: make_rows, or None (all but x)."""
+    ptr, wt = _weight(w, dim, "gg_rmsnorm_forward")
+    return check(lib.gg_rmsnorm_forward(_rows(x), _rows(res), n, dim, ptr, wt, eps, _rows(sum),
+                                        _rows(y), _rows(q), _fp32(rstd, n, "rstd"),
+                                        _stream(stream)), "gg_rmsnorm_forward")
+
+
+def gg_ws_rmsnorm(n, dim):
+    return int(lib.gg_ws_rmsnorm(n, dim))
+
+
+def gg_rmsnorm_backward(dy, dsum, s, rstd, n, dim, w, dx, dw, ws, stream=None):
+    """dy, dsum, s, dx: make_rows (dsum may be None); dw and ws may be None."""
+    ptr, wt = _weight(w, dim, "gg_rmsnorm_backward")
+    return check(lib.gg_rmsnorm_backward(_rows(dy), _rows(dsum), _rows(s), _fp32(rstd, n, "rstd"),
+                                         n, dim, ptr, wt, _rows(dx), _fp32(dw, dim, "dw"),
+                                         _ptr(ws), 0 if ws is None else ws.numel(),
+                                         _stream(stream)), "gg_rmsnorm_backward")
 
 
 def gg_read_status(status, stream=None):

@@ -120,3 +120,35 @@ def test_bindings_check_the_ids():
         gg._ids(torch.zeros(3, dtype=torch.int32), 4, "x")
     with pytest.raises(gg.GGError, match="ids"):
         gg._ids(torch.zeros(8, dtype=torch.int64)[::2], 4, "x")
+
+
+NORM = dict(x=rows(), res=None, n=7, dim=100, w=P, w_dtype=gg.GG_F32, eps=1e-6, sum=None, y=rows(),
+            q=None, rstd=P, stream=None)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(dim=0), "dim"), (dict(dim=16385), "dim"), (dict(n=-1), "n = -1"), (dict(n=1 << 28), "n = "),
+    (dict(eps=-1.0), "eps"), (dict(eps=float("nan")), "eps"), (dict(y=None, rstd=None), "output"),
+    (dict(x=None), "x: "), (dict(x=rows(gg.GG_E4M3)), "x: dtype"), (dict(w_dtype=gg.GG_F16), "weights"),
+    (dict(w=P + 2), "weights"), (dict(rstd=P + 2), "rstd"), (dict(y=rows(gg.GG_BF16)), "y: dtype"),
+    (dict(y=rows(stride=200)), "y: stride"), (dict(res=rows(gg.GG_F16)), "res: dtype"),
+    (dict(q=rows()), "q: dtype"), (dict(q=rows(gg.GG_E4M3, group=512)), "q: group"),
+    (dict(q=rows(gg.GG_E4M3, group=16, scales_stride=24)), "q: scales"),
+    (dict(q=rows(gg.GG_E4M3, stride=99)), "q: stride"),
+    (dict(x=rows(gg.GG_BF16), y=rows(gg.GG_BF16), res=rows(gg.GG_BF16), sum=rows()), "differ")])
+def test_norm_refuses(change, word):
+    refused(gg.lib.gg_rmsnorm_forward, NORM, change, word)
+
+
+NORM_BACK = dict(dy=rows(), dsum=None, s=rows(), rstd=P, n=7, dim=100, w=P, w_dtype=gg.GG_F32,
+                 dx=rows(), dw=P, ws=P, ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(dim=0), "dim"), (dict(n=-1), "n = -1"), (dict(dy=None), "dy"), (dict(s=None), "s: "),
+    (dict(s=rows(gg.GG_F16)), "s: dtype"), (dict(dx=rows(gg.GG_F16)), "dx: dtype"),
+    (dict(dsum=rows(gg.GG_BF16)), "dsum: dtype"), (dict(rstd=None), "rstd"), (dict(dw=P + 1), "dw"),
+    (dict(w_dtype=gg.GG_BF16), "weights"), (dict(w=P + 1), "weights"), (dict(ws=None), "workspace"),
+    (dict(ws=P + 8), "workspace"), (dict(ws_bytes=16), "workspace"), (dict(dx=rows(stride=4)), "dx: stride")])
+def test_norm_gradient_refuses(change, word):
+    refused(gg.lib.gg_rmsnorm_backward, NORM_BACK, change, word)
