@@ -635,6 +635,39 @@ int gg_rmsnorm_backward(const gg_rows_t* dy, const gg_rows_t* dsum, const gg_row
                         int32_t w_dtype, const gg_rows_t* dx, float* dw_d, void* ws,
                         size_t ws_bytes, hipStream_t stream);
 
+#define GG_DISTILL_MAX_ROWS (1LL << 27)
+#define GG_DISTILL_MAX_VOCAB (1 << 24)
+#define GG_DISTILL_MAX_K 256
+
+size_t gg_ws_distill(int64_t n, int64_t vocab);
+
+/* Distillation loss of n rows of logits z [n][vocab] against a teacher's top
+ * logits: row i has k entries, ids (int32 or int64, row i's at top_ids_d + i *
+ * ids_stride bytes; -1: no entry) and logits top [n][k].  With T the
+ * temperature, p = softmax(top / T) over the row's entries, q = softmax(z / T)
+ * over the vocabulary and a = weight * row_w_d[i] (NULL: ones):
+ *   loss_d[i] = a T^2 sum_k p_k (log p_k - log q[id_k])
+ *   lse_d[i]  = log sum_j exp(z_j / T)                       (NULL: not wanted)
+ *   dz[i][j]  = a T (q_j - sum of the p_k with id_k = j)     (NULL: not wanted)
+ * An id that recurs in a row counts each time.  A logit of -infinity has q = 0
+ * (the loss is infinite where its p is not).  A row without an entry, without a
+ * weight (a = 0) or with no logit above -infinity has loss 0 and a gradient of
+ * zeros.  Ids outside -1 .. vocab - 1 are no entries and set GG_DEV_BAD_ID.  z,
+ * top: GG_F32, GG_F16 or GG_BF16; dz has z's type and may be its memory.  The
+ * gradient is rounded once from fp32.  ws: 8-byte aligned. */
+int gg_distill_forward(const gg_rows_t* z, int64_t n, int64_t vocab, const void* top_ids_d,
+                       int32_t id_bits, int64_t ids_stride, const gg_rows_t* top, int32_t k,
+                       float temperature, float weight, const float* row_w_d, float* loss_d,
+                       float* lse_d, const gg_rows_t* dz, int32_t* status_d, void* ws,
+                       size_t ws_bytes, hipStream_t stream);
+
+/* The gradient alone, from the lse_d of the forward call; row_w_d may now hold
+ * the gradient that reaches each row's loss. */
+int gg_distill_backward(const gg_rows_t* z, int64_t n, int64_t vocab, const void* top_ids_d,
+                        int32_t id_bits, int64_t ids_stride, const gg_rows_t* top, int32_t k,
+                        float temperature, float weight, const float* row_w_d, const float* lse_d,
+                        const gg_rows_t* dz, int32_t* status_d, hipStream_t stream);
+
 /* Helpers. */
 
 /* Reads the sticky device status word once the work queued so far on

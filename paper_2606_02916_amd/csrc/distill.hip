@@ -1,0 +1,572 @@
+// Distillation from a teacher's top logits, forward and backward.
+//
+// With T the temperature, p = softmax(t / T) over a row's entries and
+// q = softmax(z / T) over the vocabulary:
+//   loss = a T^2 sum_k p_k (log p_k - log q[id_k]),  a = weight * row_w
+//   dz_j = a T (q_j - sum of p_k over the entries with id_k = j).
+#include "rows.hpp"
+
+namespace gg {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLn2 = 0.69314718055994531f;
+
+struct DistillArgs {
+  KRows z, top, dz;
+  const char* ids;             // row r's at ids + r * ids_stride
+  int64_t ids_stride;
+  int32_t ids64, k;
+  int32_t top_dtype;
+  int32_t vocab;
+  int64_t n;
+  float temp, inv_temp;        // T, 1 / T
+  float c2;                    // log2(e) / T
+  float weight;
+  const float* row_w;          // nullptr: ones
+  float* loss;
+  float* lse;
+  const float* lse_in;         // backward: as the forward call wrote it
+  int32_t lanes_log;
+  int32_t splits;              // blocks of a row
+  int32_t chunk;               // pieces of a split
+  float2* part;                // [n][splits]: maximum of z, sum of exp((z - maximum) / T)
+  float* lesson;               // [n]: sum p (log p - z / T)
+  int32_t* status;
+};
+
+// exp((z - m) / T).  The difference comes first: it is exact or small where the
+// result counts, also for logits of the type's lowest value.
+__device__ __forceinline__ float exp_of(float z, float m, float c2) {
+  return __builtin_amdgcn_exp2f((z - m) * c2);
+}
+// A maximum to subtract: 0 for one of -infinity, so that masked logits give 0.
+__device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
+
+struct MaxSum {
+  float m, s;
+};
+
+__device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float c2) {
+  // a sum beside a maximum of -infinity is 0 (or NaN, which stays)
+  const float m = fmaxf(a.m, b.m), f = finite_max(m);
+  return {m, a.s * exp_of(a.m, f, c2) + b.s * exp_of(b.m, f, c2)};
+}
+
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+  for (int o = lanes / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, kWave);
+  return v;
+}
+__device__ __forceinline__ float lanes_maxf(float v, int lanes) {
+  for (int o = lanes / 2; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));
+  return v;
+}
+
+// The row's entries: id (-1: none), p, log2 p and z[id], in LDS.
+constexpr int kEntryBytes = 16;
+
+struct Entries {
+  int32_t* id;
+  float *p, *lp, *z;
+};
+
+__device__ __forceinline__ Entries entries_at(char* lds, int group, int k) {
+  char* at = lds + (size_t)group * k * kEntryBytes;
+  return {(int32_t*)at, (float*)(at + 4 * k), (float*)(at + 8 * k), (float*)(at + 12 * k)};
+}
+
+// Fills the entries, by `lanes` lanes of one wave; whether the row has a lesson
+// (an entry with a finite logit, and a weight).
+template <typename T>
+__device__ __forceinline__ bool read_entries(const DistillArgs& a, int64_t row, int l, int lanes,
+                                             const Entries& en) {
+  const char* ids = a.ids + row * a.ids_stride;
+  const char* tp = a.top.p + row * a.top.stride;
+  const char* zp = a.z.p + row * a.z.stride;
+  float tm = -INFINITY;
+  bool bad = false;
+  for (int j = l; j < a.k; j += lanes) {
+    const int64_t id = a.ids64 ? ((const int64_t*)ids)[j] : (int64_t)((const int32_t*)ids)[j];
+    const bool in = (uint64_t)id < (uint64_t)a.vocab;
+    bad |= !in && id != -1;
+    float t[1];
+    GG_FOR_FLOAT(a.top_dtype, TT, { row_load<TT, 1>(tp + j * (int64_t)sizeof(TT), t); });
+    float z[1] = {0.0f};
+    if (in) row_load<T, 1>(zp + id * (int64_t)sizeof(T), z);
+    t[0] = in ? t[0] : -INFINITY;
+    en.id[j] = in ? (int32_t)id : -1;
+    en.lp[j] = t[0];
+    en.z[j] = z[0];
+    tm = fmaxf(tm, t[0]);
+  }
+  if (bad) set_status(a.status, GG_DEV_BAD_ID);
+  tm = lanes_maxf(tm, lanes);
+  const float f = finite_max(tm);
+  float total = 0.0f;
+  for (int j = l; j < a.k; j += lanes) total += exp_of(en.lp[j], f, a.c2);
+  total = lanes_sum(total, lanes);
+  const float log_total = __builtin_amdgcn_logf(total);
+  for (int j = l; j < a.k; j += lanes) {
+    const float lp = (en.lp[j] - f) * a.c2 - log_total;
+    en.lp[j] = lp;
+    en.p[j] = __builtin_amdgcn_exp2f(lp);
+  }
+  return tm != -INFINITY && (a.row_w ? a.row_w[row] : 1.0f) * a.weight != 0.0f;
+}
+
+// sum_k p_k (log p_k - z_k / T + lse), by the same lanes.
+__device__ __forceinline__ float lesson_of(const DistillArgs& a, int l, int lanes,
+                                           const Entries& en, float lse) {
+  float v = 0.0f;
+  for (int j = l; j < a.k; j += lanes) {
+    const float p = en.p[j];
+    if (p != 0.0f) v += p * (kLn2 * en.lp[j] - (en.z[j] * a.inv_temp - lse));
+  }
+  return lanes_sum(v, lanes);
+}
+
+// The gradient at the entries' own places, after the rest of the row is
+// stored: q from `q_of`, less the p of all entries with that id.
+template <typename T, typename F>
+__device__ __forceinline__ void store_entries(const DistillArgs& a, int64_t row, int l, int lanes,
+                                              const Entries& en, float c, int32_t lo, int32_t hi,
+                                              F q_of) {
+  for (int j = l; j < a.k; j += lanes) {
+    const int32_t id = en.id[j];
+    if (id < lo || id >= hi) continue;
+    float p = 0.0f;
+    for (int x = 0; x < a.k; ++x) p += en.id[x] == id ? en.p[x] : 0.0f;
+    const float v[1] = {c * (q_of(en.z[j]) - p)};
+    row_store<T, 1>(a.dz.p + row * a.dz.stride + id * (int64_t)sizeof(T), v);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// A row in registers: read once, written once.  The row's whole pieces are
+// dealt to a group of lanes (part of a wave, or a block); its last elements,
+// fewer than a piece, go to the first lanes, one each.
+// ---------------------------------------------------------------------------
+enum { kLossOnly = 0, kFused = 1, kBackward = 2 };
+
+template <typename T, int V, int STEPS, bool BLK, int MODE>
+__global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArgs a) {
+  extern __shared__ char lds[];
+  __shared__ float2 s_part[1024 / kWave];
+  __shared__ int32_t s_has;
+  const int lanes = BLK ? (int)blockDim.x : 1 << a.lanes_log;
+  const int64_t row = BLK ? block_index() : (block_index() * kBlock + threadIdx.x) >> a.lanes_log;
+  if (row >= a.n) return;
+  const int l = BLK ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1);
+  const int pieces = a.vocab / V, rest = a.vocab - pieces * V;
+  const char* zp = a.z.p + row * a.z.stride;
+
+  typename Raw<T, V>::vec raw[STEPS];
+#pragma unroll
+  for (int t = 0; t < STEPS; ++t)
+    if (t * lanes + l < pieces) raw[t] = raw_load<T, V>(zp + (int64_t)(t * lanes + l) * 16);
+  float last[1] = {-INFINITY};
+  if (l < rest) row_load<T, 1>(zp + (pieces * V + l) * (int64_t)sizeof(T), last);
+
+  const int el = BLK ? min(lanes, kWave) : lanes;     // lanes that read the entries
+  const Entries en = entries_at(lds, BLK ? 0 : (int)threadIdx.x >> a.lanes_log, a.k);
+  bool has = false;
+  if (l < el) {
+    has = read_entries<T>(a, row, l, el, en);
+    if (BLK && l == 0) s_has = has;
+  }
+
+  // Softmax statistics.
+  float top = 0.0f, inv = 0.0f, lse = 0.0f;      // q_j = inv * exp((z_j - top) / T)
+  bool empty = false;
+  if constexpr (MODE != kBackward) {
+    float m = last[0];
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t)
+      if (t * lanes + l < pieces) {
+        float v[V];
+        to_f32<T, V>(raw[t], v);
+#pragma unroll
+        for (int k = 0; k < V; ++k) m = fmaxf(m, v[k]);
+      }
+    m = lanes_maxf(m, min(lanes, kWave));
+    top = finite_max(m);
+    float s = exp_of(last[0], top, a.c2);
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t)
+      if (t * lanes + l < pieces) {
+        float v[V];
+        to_f32<T, V>(raw[t], v);
+#pragma unroll
+        for (int k = 0; k < V; ++k) s += exp_of(v[k], top, a.c2);
+      }
+    s = lanes_sum(s, min(lanes, kWave));
+    MaxSum all = {m, s};
+    if constexpr (BLK) {
+      if (lane_id() == 0) s_part[threadIdx.x / kWave] = make_float2(m, s);
+      __syncthreads();
+      all = {s_part[0].x, s_part[0].y};
+      for (int w = 1; w < lanes / kWave; ++w) all = join(all, {s_part[w].x, s_part[w].y}, a.c2);
+      top = finite_max(all.m);
+    }
+    // Sums are at least 1, but for a row of which every logit is -infinity.
+    empty = all.s == 0.0f;
+    inv = empty ? 0.0f : 1.0f / all.s;
+    lse = all.m * a.inv_temp + (empty ? 0.0f : kLn2 * __builtin_amdgcn_logf(all.s));
+  } else {
+    lse = a.lse_in[row];
+    empty = lse == -INFINITY;
+    top = empty ? 0.0f : lse * a.temp;
+    inv = 1.0f;
+    if (BLK) __syncthreads();
+  }
+  if (BLK) has = s_has;
+  has = has && !empty;
+  const float weight = a.weight * (a.row_w ? a.row_w[row] : 1.0f);
+  if constexpr (MODE != kBackward) {
+    if (l < el) {
+      const float v = has ? lesson_of(a, l, el, en, lse) : 0.0f;
+      if (l == 0) {
+        a.loss[row] = has ? weight * a.temp * a.temp * v : 0.0f;
+        if (a.lse) a.lse[row] = lse;
+      }
+    }
+  }
+  if constexpr (MODE == kLossOnly) return;
+
+  // The gradient: a row without a lesson gets zeros.
+  const float c = has ? weight * a.temp : 0.0f;
+  const float ci = c * inv;
+  char* dp = a.dz.p + row * a.dz.stride;
+#pragma unroll
+  for (int t = 0; t < STEPS; ++t)
+    if (t * lanes + l < pieces) {
+      float v[V];
+      to_f32<T, V>(raw[t], v);
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[k] = has ? ci * exp_of(v[k], top, a.c2) : 0.0f;
+      row_store<T, V>(dp + (int64_t)(t * lanes + l) * 16, v);
+    }
+  if (l < rest) {
+    const float v[1] = {has ? ci * exp_of(last[0], top, a.c2) : 0.0f};
+    row_store<T, 1>(dp + (pieces * V + l) * (int64_t)sizeof(T), v);
+  }
+  if (!has) return;      // the same for the whole row
+  if constexpr (BLK)
+    __syncthreads();
+  else
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (l < el)
+    store_entries<T>(a, row, l, el, en, c, 0, a.vocab,
+                     [&](float z) { return inv * exp_of(z, top, a.c2); });
+}
+
+// ---------------------------------------------------------------------------
+// Rows that do not fit the registers of a block, and few long rows: several
+// blocks per row, the statistics joined by the blocks of a second launch.
+// ---------------------------------------------------------------------------
+constexpr int kSplitUnroll = 4;
+
+template <typename T, int V>
+__global__ void __launch_bounds__(kBlock) k_distill_stats(DistillArgs a) {
+  extern __shared__ char lds[];
+  __shared__ float2 s_part[kBlock / kWave];
+  const int64_t row = block_index() / a.splits;
+  const int c = (int)(block_index() - row * a.splits);
+  if (row >= a.n) return;
+  const int pieces = a.vocab / V, rest = a.vocab - pieces * V;
+  const int p0 = c * a.chunk, p1 = min(pieces, p0 + a.chunk);
+  const char* zp = a.z.p + row * a.z.stride;
+  const int tid = threadIdx.x;
+  MaxSum st = {-INFINITY, 0.0f};
+  for (int p = p0 + tid; p < p1; p += kBlock * kSplitUnroll) {
+    typename Raw<T, V>::vec raw[kSplitUnroll];
+#pragma unroll
+    for (int u = 0; u < kSplitUnroll; ++u) {
+      const int q = p + u * kBlock;
+      raw[u] = raw_load<T, V>(zp + (int64_t)(q < p1 ? q : p) * 16);
+    }
+#pragma unroll
+    for (int u = 0; u < kSplitUnroll; ++u) {
+      if (p + u * kBlock >= p1) break;
+      float v[V], m = st.m;
+      to_f32<T, V>(raw[u], v);
+#pragma unroll
+      for (int k = 0; k < V; ++k) m = fmaxf(m, v[k]);
+      const float top = finite_max(m);
+      st.s *= exp_of(st.m, top, a.c2);
+      st.m = m;
+#pragma unroll
+      for (int k = 0; k < V; ++k) st.s += exp_of(v[k], top, a.c2);
+    }
+  }
+  if (c == a.splits - 1 && tid < rest) {
+    float v[1];
+    row_load<T, 1>(zp + (pieces * V + tid) * (int64_t)sizeof(T), v);
+    st = join(st, {v[0], v[0] == -INFINITY ? 0.0f : v[0] - v[0] + 1.0f}, a.c2);
+  }
+  for (int o = kWave / 2; o >= 1; o >>= 1)
+    st = join(st, {__shfl_xor(st.m, o, kWave), __shfl_xor(st.s, o, kWave)}, a.c2);
+  if (lane_id() == 0) s_part[tid / kWave] = make_float2(st.m, st.s);
+  // The lesson's part that needs no statistics, while z is still whole (the
+  // gradient may take its place).
+  if (c == 0 && tid < kWave) {
+    const Entries en = entries_at(lds, 0, a.k);
+    const bool has = read_entries<T>(a, row, tid, kWave, en);
+    const float v = lesson_of(a, tid, kWave, en, 0.0f);
+    if (tid == 0) a.lesson[row] = has ? v : 0.0f;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    st = {s_part[0].x, s_part[0].y};
+    for (int w = 1; w < kBlock / kWave; ++w) st = join(st, {s_part[w].x, s_part[w].y}, a.c2);
+    a.part[row * a.splits + c] = make_float2(st.m, st.s);
+  }
+}
+
+template <typename T, int V, int MODE>
+__global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
+  extern __shared__ char lds[];
+  __shared__ int32_t s_has;
+  const int64_t row = block_index() / a.splits;
+  const int c = (int)(block_index() - row * a.splits);
+  if (row >= a.n || (MODE == kLossOnly && c > 0)) return;
+  const int tid = threadIdx.x;
+  float top, inv, lse;      // q_j = inv * exp((z_j - top) / T)
+  bool empty;
+  if constexpr (MODE != kBackward) {
+    // Every wave joins all parts of the row.
+    MaxSum st = {-INFINITY, 0.0f};
+    for (int x = lane_id(); x < a.splits; x += kWave) {
+      const float2 v = a.part[row * a.splits + x];
+      st = join(st, {v.x, v.y}, a.c2);
+    }
+    for (int o = kWave / 2; o >= 1; o >>= 1)
+      st = join(st, {__shfl_xor(st.m, o, kWave), __shfl_xor(st.s, o, kWave)}, a.c2);
+    empty = st.s == 0.0f;
+    top = finite_max(st.m);
+    inv = empty ? 0.0f : 1.0f / st.s;
+    lse = st.m * a.inv_temp + (empty ? 0.0f : kLn2 * __builtin_amdgcn_logf(st.s));
+  } else {
+    lse = a.lse_in[row];
+    empty = lse == -INFINITY;
+    top = empty ? 0.0f : lse * a.temp;
+    inv = 1.0f;
+  }
+  const Entries en = entries_at(lds, 0, a.k);
+  if (tid < kWave) {
+    const bool has = read_entries<T>(a, row, tid, kWave, en);
+    if (tid == 0) s_has = has;
+  }
+  __syncthreads();
+  const bool has = s_has && !empty;
+  const float weight = a.weight * (a.row_w ? a.row_w[row] : 1.0f);
+  if (MODE != kBackward && c == 0 && tid == 0) {
+    a.loss[row] = has ? weight * a.temp * a.temp * (a.lesson[row] + lse) : 0.0f;
+    if (a.lse) a.lse[row] = lse;
+  }
+  if constexpr (MODE == kLossOnly) return;
+
+  const int pieces = a.vocab / V, rest = a.vocab - pieces * V;
+  const int p0 = c * a.chunk, p1 = min(pieces, p0 + a.chunk);
+  const char* zp = a.z.p + row * a.z.stride;
+  char* dp = a.dz.p + row * a.dz.stride;
+  const float scale = has ? weight * a.temp : 0.0f;
+  const float ci = scale * inv;
+  for (int p = p0 + tid; p < p1; p += kBlock * kSplitUnroll) {
+    typename Raw<T, V>::vec raw[kSplitUnroll];
+#pragma unroll
+    for (int u = 0; u < kSplitUnroll; ++u) {
+      const int q = p + u * kBlock;
+      raw[u] = raw_load<T, V>(zp + (int64_t)(q < p1 ? q : p) * 16);
+    }
+#pragma unroll
+    for (int u = 0; u < kSplitUnroll; ++u) {
+      if (p + u * kBlock >= p1) break;
+      float v[V];
+      to_f32<T, V>(raw[u], v);
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[k] = has ? ci * exp_of(v[k], top, a.c2) : 0.0f;
+      row_store<T, V>(dp + (int64_t)(p + u * kBlock) * 16, v);
+    }
+  }
+  const bool end = c == a.splits - 1;
+  if (end && tid < rest) {
+    float v[1];
+    row_load<T, 1>(zp + (pieces * V + tid) * (int64_t)sizeof(T), v);
+    v[0] = has ? ci * exp_of(v[0], top, a.c2) : 0.0f;
+    row_store<T, 1>(dp + (pieces * V + tid) * (int64_t)sizeof(T), v);
+  }
+  if (!has) return;
+  __syncthreads();
+  if (tid < kWave)
+    store_entries<T>(a, row, tid, kWave, en, scale, p0 * V, end ? a.vocab : p1 * V,
+                     [&](float z) { return inv * exp_of(z, top, a.c2); });
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+// ---------------------------------------------------------------------------
+constexpr int kMaxSplits = 64;
+constexpr int kMaxSteps = 16;         // pieces per lane of a block
+constexpr int kWaveSteps = 4;
+constexpr int64_t kFewRows = 256;     // below: rows of kSplitPieces pieces and more are split
+constexpr int kSplitPieces = 2048;
+
+int split_count(int64_t n) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>(kMaxSplits, 1024 / std::max<int64_t>(n, 1)));
+}
+
+struct DistillWs {
+  float2* part;
+  float* lesson;
+};
+
+size_t distill_ws_layout(int64_t n, char* base, DistillWs* out) {
+  Carve c{base, 0, 0};
+  DistillWs w;
+  w.part = c.take<float2>((size_t)n * split_count(n));
+  w.lesson = c.take<float>((size_t)n);
+  if (out) *out = w;
+  return align_up(c.used, 256);
+}
+
+template <typename T, int MODE>
+int launch_rows(DistillArgs& a, hipStream_t stream) {
+  constexpr int V = kVec<T>;
+  const int pieces = a.vocab / V;
+  const bool split = pieces > 1024 * kMaxSteps || (a.n < kFewRows && pieces >= kSplitPieces);
+  if (split) {
+    a.splits = split_count(a.n);
+    a.chunk = (int)cdiv(pieces, a.splits);
+    const size_t lds = (size_t)a.k * kEntryBytes;
+    const dim3 grid = grid_of(a.n * a.splits);
+    if (MODE != kBackward) {
+      hipLaunchKernelGGL((k_distill_stats<T, V>), grid, dim3(kBlock), lds, stream, a);
+      GG_LAUNCH_CHECK("k_distill_stats");
+    }
+    hipLaunchKernelGGL((k_distill_finish<T, V, MODE>), grid, dim3(kBlock), lds, stream, a);
+    GG_LAUNCH_CHECK("k_distill_finish");
+    return GG_OK;
+  }
+  if (pieces <= kWave * kWaveSteps) {
+    a.lanes_log = 4;
+    // (at most 32 KB of entries per block)
+    while (a.lanes_log < 6 && ((1 << a.lanes_log) < pieces ||
+                               (kBlock >> a.lanes_log) * a.k * kEntryBytes > 32768))
+      ++a.lanes_log;
+    const int steps = (int)cdiv(pieces, 1 << a.lanes_log);
+    const dim3 grid = grid_of(cdiv(a.n << a.lanes_log, kBlock));
+    const size_t lds = (size_t)(kBlock >> a.lanes_log) * a.k * kEntryBytes;
+    if (steps <= 1)
+      hipLaunchKernelGGL((k_distill_rows<T, V, 1, false, MODE>), grid, dim3(kBlock), lds, stream, a);
+    else if (steps == 2)
+      hipLaunchKernelGGL((k_distill_rows<T, V, 2, false, MODE>), grid, dim3(kBlock), lds, stream, a);
+    else
+      hipLaunchKernelGGL((k_distill_rows<T, V, 4, false, MODE>), grid, dim3(kBlock), lds, stream, a);
+  } else {
+    int threads = 256;
+    while (threads < 1024 && threads * kMaxSteps < pieces) threads *= 2;
+    const int steps = (int)cdiv(pieces, threads);
+    const dim3 grid = grid_of(a.n);
+    const size_t lds = (size_t)a.k * kEntryBytes;
+    if (steps <= 2)
+      hipLaunchKernelGGL((k_distill_rows<T, V, 2, true, MODE>), grid, dim3(threads), lds, stream, a);
+    else if (steps <= 4)
+      hipLaunchKernelGGL((k_distill_rows<T, V, 4, true, MODE>), grid, dim3(threads), lds, stream, a);
+    else if (steps <= 8)
+      hipLaunchKernelGGL((k_distill_rows<T, V, 8, true, MODE>), grid, dim3(threads), lds, stream, a);
+    else
+      hipLaunchKernelGGL((k_distill_rows<T, V, 16, true, MODE>), grid, dim3(threads), lds, stream, a);
+  }
+  GG_LAUNCH_CHECK("k_distill_rows");
+  return GG_OK;
+}
+
+int pack_args(const gg_rows_t* z, int64_t n, int64_t vocab, const void* top_ids_d, int32_t id_bits,
+              int64_t ids_stride, const gg_rows_t* top, int32_t k, float temperature, float weight,
+              const float* row_w_d, const gg_rows_t* dz, int32_t* status_d, DistillArgs* a) {
+  GG_REQUIRE(status_d, "status is NULL");
+  GG_REQUIRE(n >= 0 && n <= GG_DISTILL_MAX_ROWS, "n = %lld unsupported", (long long)n);
+  GG_REQUIRE(vocab >= 1 && vocab <= GG_DISTILL_MAX_VOCAB, "vocab %lld outside 1..%d",
+             (long long)vocab, GG_DISTILL_MAX_VOCAB);
+  GG_REQUIRE(k >= 1 && k <= GG_DISTILL_MAX_K, "k = %d outside 1..%d", k, GG_DISTILL_MAX_K);
+  GG_REQUIRE(temperature > 0.0f && temperature <= 3.0e38f, "temperature must be positive and finite");
+  int rc = pack_rows(z, "z", n, vocab, kBitFloats, false, &a->z);
+  if (rc == GG_OK) rc = pack_rows(top, "top", n, k, kBitFloats, false, &a->top);
+  if (rc == GG_OK && dz) rc = pack_rows(dz, "dz", n, vocab, 1u << z->dtype, true, &a->dz);
+  if (rc != GG_OK) return rc;
+  GG_REQUIRE(id_bits == 32 || id_bits == 64, "ids of %d bits", id_bits);
+  GG_REQUIRE(n == 0 || top_ids_d, "ids are NULL");
+  GG_REQUIRE((uintptr_t)top_ids_d % (id_bits / 8) == 0 && ids_stride % (id_bits / 8) == 0 &&
+                 ids_stride >= 0,
+             "ids are not aligned");
+  GG_REQUIRE((uintptr_t)row_w_d % 4 == 0, "row_w is not aligned");
+  a->ids = (const char*)top_ids_d;
+  a->ids_stride = ids_stride;
+  a->ids64 = id_bits == 64;
+  a->k = k;
+  a->top_dtype = top->dtype;
+  a->n = n;
+  a->vocab = (int32_t)vocab;
+  a->temp = temperature;
+  a->inv_temp = 1.0f / temperature;
+  a->c2 = kLog2e / temperature;
+  a->weight = weight;
+  a->row_w = row_w_d;
+  a->status = status_d;
+  return GG_OK;
+}
+
+}  // namespace
+}  // namespace gg
+
+using namespace gg;
+
+extern "C" size_t gg_ws_distill(int64_t n, int64_t vocab) {
+  if (n < 0 || n > GG_DISTILL_MAX_ROWS || vocab < 1 || vocab > GG_DISTILL_MAX_VOCAB) return 0;
+  return distill_ws_layout(n, nullptr, nullptr);
+}
+
+extern "C" int gg_distill_forward(const gg_rows_t* z, int64_t n, int64_t vocab,
+                                  const void* top_ids_d, int32_t id_bits, int64_t ids_stride,
+                                  const gg_rows_t* top, int32_t k, float temperature, float weight,
+                                  const float* row_w_d, float* loss_d, float* lse_d,
+                                  const gg_rows_t* dz, int32_t* status_d, void* ws,
+                                  size_t ws_bytes, hipStream_t stream) {
+  DistillArgs a = {};
+  const int rc = pack_args(z, n, vocab, top_ids_d, id_bits, ids_stride, top, k, temperature, weight,
+                           row_w_d, dz, status_d, &a);
+  if (rc != GG_OK) return rc;
+  GG_REQUIRE(n == 0 || loss_d, "loss is NULL");
+  GG_REQUIRE((uintptr_t)loss_d % 4 == 0 && (uintptr_t)lse_d % 4 == 0, "loss or lse is not aligned");
+  const size_t need = gg_ws_distill(n, vocab);
+  GG_REQUIRE(n == 0 || (ws && (uintptr_t)ws % 8 == 0 && ws_bytes >= need),
+             "workspace of %zu bytes < %zu, or not aligned", ws_bytes, need);
+  if (n == 0) return GG_OK;
+  DistillWs w;
+  distill_ws_layout(n, (char*)ws, &w);
+  a.part = w.part;
+  a.lesson = w.lesson;
+  a.loss = loss_d;
+  a.lse = lse_d;
+  GG_FOR_FLOAT(z->dtype, T, {
+    return dz ? launch_rows<T, kFused>(a, stream) : launch_rows<T, kLossOnly>(a, stream);
+  });
+}
+
+extern "C" int gg_distill_backward(const gg_rows_t* z, int64_t n, int64_t vocab,
+                                   const void* top_ids_d, int32_t id_bits, int64_t ids_stride,
+                                   const gg_rows_t* top, int32_t k, float temperature,
+                                   float weight, const float* row_w_d, const float* lse_d,
+                                   const gg_rows_t* dz, int32_t* status_d, hipStream_t stream) {
+  GG_REQUIRE(dz, "dz: no rows given");
+  DistillArgs a = {};
+  const int rc = pack_args(z, n, vocab, top_ids_d, id_bits, ids_stride, top, k, temperature, weight,
+                           row_w_d, dz, status_d, &a);
+  if (rc != GG_OK) return rc;
+  GG_REQUIRE(n == 0 || lse_d, "lse is NULL");
+  GG_REQUIRE((uintptr_t)lse_d % 4 == 0, "lse is not aligned");
+  if (n == 0) return GG_OK;
+  a.lse_in = lse_d;
+  GG_FOR_FLOAT(z->dtype, T, { return launch_rows<T, kBackward>(a, stream); });
+}

@@ -159,6 +159,11 @@ SIGNATURES = {
     "gg_rmsnorm_forward": (C.c_int, [_P, _P, _I64, _I32, _P, _I32, C.c_float, _P, _P, _P, _P, _P]),
     "gg_ws_rmsnorm": (_SZ, [_I64, _I32]),
     "gg_rmsnorm_backward": (C.c_int, [_P, _P, _P, _P, _I64, _I32, _P, _I32, _P, _P, _P, _SZ, _P]),
+    "gg_ws_distill": (_SZ, [_I64, _I64]),
+    "gg_distill_forward": (C.c_int, [_P, _I64, _I64, _P, _I32, _I64, _P, _I32, C.c_float, C.c_float,
+                                     _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "gg_distill_backward": (C.c_int, [_P, _I64, _I64, _P, _I32, _I64, _P, _I32, C.c_float,
+                                      C.c_float, _P, _P, _P, _P, _P]),
     "gg_read_status": (C.c_int, [_P, _P, _P]),
     "gg_status_string": (C.c_char_p, [_I32]),
     "gg_last_error": (C.c_char_p, []),
@@ -568,6 +573,40 @@ def gg_rmsnorm_backward(dy, dsum, s, rstd, n, dim, w, dx, dw, ws, stream=None):
                                          n, dim, ptr, wt, _rows(dx), _fp32(dw, dim, "dw"),
                                          _ptr(ws), 0 if ws is None else ws.numel(),
                                          _stream(stream)), "gg_rmsnorm_backward")
+
+
+def gg_ws_distill(n, vocab):
+    return int(lib.gg_ws_distill(n, vocab))
+
+
+def _top_ids(ids, n, k):
+    """Address, bits and row stride (bytes) of the ids of n rows of k entries."""
+    if ids.dtype not in _ID_BITS or ids.dim() != 2 or tuple(ids.shape) != (n, k) or \
+            (k > 1 and ids.stride(1) != 1):
+        raise GGError(f"top ids must be int32 or int64 values of shape ({n}, {k})")
+    return ids.data_ptr(), _ID_BITS[ids.dtype], ids.stride(0) * ids.element_size()
+
+
+def gg_distill_forward(z, n, vocab, top_ids, top, k, temperature, weight, row_w, loss, lse, dz,
+                       status, ws, stream=None):
+    """z, top and dz: make_rows (dz may be None); top_ids: an [n, k] tensor;
+    row_w and lse may be None."""
+    ptr, bits, stride = _top_ids(top_ids, n, k)
+    return check(lib.gg_distill_forward(_rows(z), n, vocab, ptr, bits, stride, _rows(top), k,
+                                        temperature, weight, _fp32(row_w, n, "row_w"),
+                                        _fp32(loss, n, "loss"), _fp32(lse, n, "lse"), _rows(dz),
+                                        _ptr(status), _ptr(ws), ws.numel(), _stream(stream)),
+                 "gg_distill_forward")
+
+
+def gg_distill_backward(z, n, vocab, top_ids, top, k, temperature, weight, row_w, lse, dz, status,
+                        stream=None):
+    """The gradient alone, from the forward call's lse."""
+    ptr, bits, stride = _top_ids(top_ids, n, k)
+    return check(lib.gg_distill_backward(_rows(z), n, vocab, ptr, bits, stride, _rows(top), k,
+                                         temperature, weight, _fp32(row_w, n, "row_w"),
+                                         _fp32(lse, n, "lse"), _rows(dz), _ptr(status),
+                                         _stream(stream)), "gg_distill_backward")
 
 
 def gg_read_status(status, stream=None):

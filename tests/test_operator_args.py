@@ -152,3 +152,42 @@ NORM_BACK = dict(dy=rows(), dsum=None, s=rows(), rstd=P, n=7, dim=100, w=P, w_dt
     (dict(ws=P + 8), "workspace"), (dict(ws_bytes=16), "workspace"), (dict(dx=rows(stride=4)), "dx: stride")])
 def test_norm_gradient_refuses(change, word):
     refused(gg.lib.gg_rmsnorm_backward, NORM_BACK, change, word)
+
+
+DISTILL = dict(z=rows(), n=7, vocab=100, ids=P, bits=64, ids_stride=64, top=rows(), k=8,
+               temperature=2.0, weight=1.0, row_w=None, loss=P, lse=P, dz=rows(), status=P, ws=P,
+               ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(status=None), "status"), (dict(n=-1), "n = -1"), (dict(n=1 << 28), "n = "),
+    (dict(vocab=0), "vocab"), (dict(vocab=(1 << 24) + 1), "vocab"), (dict(k=0), "k = 0"),
+    (dict(k=257), "k = 257"), (dict(temperature=0.0), "temperature"),
+    (dict(temperature=-1.0), "temperature"), (dict(temperature=float("inf")), "temperature"),
+    (dict(temperature=float("nan")), "temperature"), (dict(z=None), "z: "), (dict(top=None), "top: "),
+    (dict(z=rows(gg.GG_E4M3)), "z: dtype"), (dict(dz=rows(gg.GG_F16)), "dz: dtype"),
+    (dict(dz=rows(stride=0)), "dz: stride"), (dict(bits=31), "31 bits"), (dict(ids=None), "ids are NULL"),
+    (dict(ids=P + 4), "aligned"), (dict(ids_stride=4), "aligned"), (dict(ids_stride=-64), "aligned"),
+    (dict(row_w=P + 2), "row_w"), (dict(loss=None), "loss"), (dict(lse=P + 2), "lse"),
+    (dict(ws=None), "workspace"), (dict(ws_bytes=8), "workspace")])
+def test_distill_refuses(change, word):
+    refused(gg.lib.gg_distill_forward, DISTILL, change, word)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(dz=None), "dz"), (dict(lse=None), "lse"), (dict(lse=P + 1), "lse"), (dict(n=-1), "n = -1"),
+    (dict(status=None), "status"), (dict(k=0), "k = 0")])
+def test_distill_gradient_refuses(change, word):
+    args = {k: v for k, v in DISTILL.items() if k not in ("loss", "ws", "ws_bytes")}
+    refused(gg.lib.gg_distill_backward, args, change, word)
+
+
+def test_bindings_check_shapes_of_lists_and_vectors():
+    ids = torch.zeros(5, 8, dtype=torch.int64)
+    assert gg._top_ids(ids[:, :4], 5, 4)[1:] == (64, 64)
+    for bad in (lambda: gg._top_ids(ids, 5, 7), lambda: gg._top_ids(ids.float(), 5, 8),
+                lambda: gg._top_ids(ids.t(), 8, 5), lambda: gg._fp32(torch.zeros(4), 5, "x"),
+                lambda: gg._fp32(torch.zeros(8)[::2], 4, "x"),
+                lambda: gg._weight(torch.zeros(4), 5, "x"), lambda: gg._weight(ids[0], 8, "x")):
+        with pytest.raises(gg.GGError):
+            bad()
