@@ -95,13 +95,15 @@ __global__ void __launch_bounds__(kBlock) k_embed_rows(LookupArgs a) {
 // time.  Lanes whose digits agree find each other by one ballot per digit bit,
 // so equal digits are counted and ranked without atomics.
 // ---------------------------------------------------------------------------
-constexpr int kSortBlock = 1024;
-constexpr int kSortWaves = kSortBlock / kWave;
 constexpr int kSortKeys = 8;                      // pairs per lane
 constexpr int kTileWave = kWave * kSortKeys;
-constexpr int kTile = kSortBlock * kSortKeys;
-constexpr int kMaxDigit = 11;                     // bits; 2,048 counters per wave
-constexpr int kWideTiles = 32;                    // at most this many tiles: digits of 11 bits
+constexpr int kTileBlock = 1024;                  // lanes of the one-tile sort
+constexpr int kTile = kTileBlock * kSortKeys;
+constexpr int kMaxDigit = 9;                      // bits of a digit; 8 beyond kWideTiles tiles
+constexpr int kWideTiles = 64;
+// A tile's work is instructions, which a block of 4 waves spreads over more of
+// the chip; blocks of 16 waves keep the counters of many tiles few.
+constexpr int kSmallSortTiles = 256;              // most tiles of 4-wave blocks
 
 struct Keys {
   const void* ids;       // first pass: the ids; later passes: key and pos
@@ -122,24 +124,29 @@ __device__ __forceinline__ uint32_t key_of(const Keys& a, int64_t i, bool* bad) 
   return a.rows;
 }
 
-// Lanes with this lane's digit, among the valid ones.
+// Lanes with this lane's digit, among the valid ones: six instructions a bit.
 __device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, bool valid) {
   uint64_t m = __ballot(valid);
+  uint32_t lo = (uint32_t)m, hi = (uint32_t)(m >> 32);
   for (int b = 0; b < bits; ++b) {
-    const uint64_t one = __ballot((d >> b) & 1u);
-    m &= ((d >> b) & 1u) ? one : ~one;
+    const uint32_t t = (uint32_t)__builtin_amdgcn_sbfe((int)d, (uint32_t)b, 1u);   // 0 or ~0
+    const uint64_t one = __ballot(t != 0);
+    lo &= ~((uint32_t)one ^ t);
+    hi &= ~((uint32_t)(one >> 32) ^ t);
   }
-  return m;
+  return (uint64_t)hi << 32 | lo;
 }
 
-// Ranks a tile's pairs: cnt[w][d] ends as the number of the wave's pairs with
-// digit d, rank[j] as the number of earlier ones in the wave.
+// Ranks a wave's pairs, `steps` of them per lane: cnt[d] ends as their number
+// with digit d, rank[j] as the number of earlier ones.
 __device__ __forceinline__ void rank_tile(const uint32_t (&key)[kSortKeys], int shift, int bits,
-                                          int left, uint16_t* cnt, uint16_t (&rank)[kSortKeys]) {
+                                          int left, int steps, uint16_t* cnt,
+                                          uint16_t (&rank)[kSortKeys]) {
   const uint32_t mask = (1u << bits) - 1u;
   const int lane = lane_id();
 #pragma unroll
   for (int j = 0; j < kSortKeys; ++j) {
+    if (j >= steps) break;
     const uint32_t d = (key[j] >> shift) & mask;
     const bool valid = j * kWave + lane < left;
     const uint64_t m = same_digit(d, bits, valid);
@@ -151,9 +158,14 @@ __device__ __forceinline__ void rank_tile(const uint32_t (&key)[kSortKeys], int 
   }
 }
 
+// Digit bits of a block of nt lanes at most.
+constexpr int digit_limit(int nt) { return nt == kBlock ? kMaxDigit : 8; }
+
 // Digit counts of each tile: hist[tile][digit].
-__global__ void __launch_bounds__(kSortBlock) k_sort_count(Keys a, int32_t* hist) {
-  __shared__ uint16_t cnt[kSortWaves << kMaxDigit];
+template <int NT>
+__global__ void __launch_bounds__(NT) k_sort_count(Keys a, int32_t* hist) {
+  constexpr int kSortBlock = NT, kSortWaves = NT / kWave, kTile = NT * kSortKeys;
+  __shared__ uint16_t cnt[kSortWaves << digit_limit(NT)];
   const int digits = 1 << a.bits, w = threadIdx.x / kWave;
   for (int i = threadIdx.x; i < kSortWaves * digits; i += kSortBlock) cnt[i] = 0;
   const int64_t first = (int64_t)blockIdx.x * kTile + w * kTileWave;
@@ -168,7 +180,7 @@ __global__ void __launch_bounds__(kSortBlock) k_sort_count(Keys a, int32_t* hist
   }
   if (bad) set_status(a.status, GG_DEV_BAD_ID);
   __syncthreads();
-  rank_tile(key, a.shift, a.bits, left, cnt + w * digits, rank);
+  rank_tile(key, a.shift, a.bits, left, kSortKeys, cnt + w * digits, rank);
   __syncthreads();
   for (int d = threadIdx.x; d < digits; d += kSortBlock) {
     int32_t s = 0;
@@ -178,50 +190,21 @@ __global__ void __launch_bounds__(kSortBlock) k_sort_count(Keys a, int32_t* hist
   }
 }
 
-// First output place of each digit of this block's tile -> base[d] (LDS), from
-// the counts of all tiles: smaller digits first, then earlier tiles.
-__device__ void tile_bases(const int32_t* hist, int tiles, int digits, int32_t* base) {
-  const int tid = threadIdx.x;
-  const int cols = digits < kSortBlock ? digits : kSortBlock;
-  const int groups = kSortBlock / cols;
-  const int per = (tiles + groups - 1) / groups;
-  int32_t run = 0;
-  __shared__ int32_t s_scan[kSortWaves];
-  __shared__ int32_t s_mine[kSortBlock], s_all[kSortBlock];
-  for (int d0 = 0; d0 < digits; d0 += cols) {
-    const int d = d0 + tid % cols, g = tid / cols;
-    int32_t mine = 0, all = 0;
-    const int t1 = min(tiles, (g + 1) * per);
-#pragma unroll 8
-    for (int t = g * per; t < t1; ++t) {
-      const int32_t c = hist[(int64_t)t * digits + d];
-      all += c;
-      mine += t < (int)blockIdx.x ? c : 0;
-    }
-    s_mine[tid] = mine;
-    s_all[tid] = all;
-    __syncthreads();
-    int32_t total = 0;
-    mine = all = 0;
-    if (tid < cols)
-      for (int x = 0; x < groups; ++x) {
-        mine += s_mine[x * cols + tid];
-        all += s_all[x * cols + tid];
-      }
-    const int32_t before = block_excl_scan<kSortBlock>(all, s_scan, &total);
-    if (tid < cols) base[d0 + tid] = run + before + mine;
-    run += total;
-    __syncthreads();
-  }
-}
-
-__global__ void __launch_bounds__(kSortBlock) k_sort_scatter(Keys a, const int32_t* hist, int tiles,
-                                                             uint32_t* key_out,
-                                                             uint32_t* pos_out) {
-  __shared__ uint16_t cnt[kSortWaves << kMaxDigit];
-  __shared__ int32_t base[1 << kMaxDigit];
-  const int digits = 1 << a.bits, w = threadIdx.x / kWave;
-  for (int i = threadIdx.x; i < kSortWaves * digits; i += kSortBlock) cnt[i] = 0;
+// Moves a tile's pairs to their places: those of smaller digits come first,
+// then those of earlier tiles with the same digit, as the counts of all tiles
+// (hist) tell.
+template <int NT>
+__global__ void __launch_bounds__(NT) k_sort_scatter(Keys a, const int32_t* hist, int tiles,
+                                                     uint32_t* key_out, uint32_t* pos_out) {
+  constexpr int kSortWaves = NT / kWave, kTile = NT * kSortKeys;
+  __shared__ uint16_t cnt[kSortWaves << digit_limit(NT)];
+  __shared__ int32_t base[1 << digit_limit(NT)];
+  __shared__ uint16_t local[1 << digit_limit(NT)];     // first place of a digit in the tile
+  __shared__ uint32_t s_key[kTile], s_pos[kTile];
+  __shared__ int2 s_mine[NT], s_all[NT];
+  __shared__ uint64_t s_scan[kSortWaves];
+  const int tid = threadIdx.x, digits = 1 << a.bits, w = tid / kWave;
+  for (int i = tid; i < kSortWaves * digits; i += NT) cnt[i] = 0;
   const int64_t first = (int64_t)blockIdx.x * kTile + w * kTileWave;
   const int left = (int)min((int64_t)kTileWave, max((int64_t)0, a.n - first));
   uint32_t key[kSortKeys], pos[kSortKeys];
@@ -233,40 +216,88 @@ __global__ void __launch_bounds__(kSortBlock) k_sort_scatter(Keys a, const int32
     key[j] = o < left ? key_of(a, first + o, &bad) : 0u;
     pos[j] = o < left ? (a.ids ? (uint32_t)(first + o) : a.pos[first + o]) : 0u;
   }
-  tile_bases(hist, tiles, digits, base);
-  rank_tile(key, a.shift, a.bits, left, cnt + w * digits, rank);
+  // A lane adds up two neighbouring digits over a share of the tiles.
+  const int cols = digits / 2, groups = NT / cols, c = tid & (cols - 1), g = tid / cols;
+  const int per = (tiles + groups - 1) / groups, t1 = min(tiles, (g + 1) * per);
+  int2 mine = {0, 0}, all = {0, 0};
+#pragma unroll 16
+  for (int t = g * per; t < t1; ++t) {
+    const int2 v = ((const int2*)hist)[(int64_t)t * cols + c];
+    const bool before = t < (int)blockIdx.x;
+    all.x += v.x;
+    all.y += v.y;
+    mine.x += before ? v.x : 0;
+    mine.y += before ? v.y : 0;
+  }
+  s_mine[tid] = mine;
+  s_all[tid] = all;
   __syncthreads();
-  // Counts of earlier waves, in place.
-  for (int d = threadIdx.x; d < digits; d += kSortBlock) {
-    uint16_t s = 0;
-#pragma unroll
-    for (int v = 0; v < kSortWaves; ++v) {
-      const uint16_t c = cnt[v * digits + d];
-      cnt[v * digits + d] = s;
-      s += c;
+  rank_tile(key, a.shift, a.bits, left, kSortKeys, cnt + w * digits, rank);
+  __syncthreads();
+  // The digits' totals over all tiles and in this one, scanned together.
+  mine = all = {0, 0};
+  int32_t in[2] = {0, 0};
+  if (tid < cols) {
+    for (int x = 0; x < groups; ++x) {
+      mine.x += s_mine[x * cols + tid].x;
+      mine.y += s_mine[x * cols + tid].y;
+      all.x += s_all[x * cols + tid].x;
+      all.y += s_all[x * cols + tid].y;
     }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int v = 0; v < kSortWaves; ++v) {
+        const uint16_t n = cnt[v * digits + 2 * tid + h];
+        cnt[v * digits + 2 * tid + h] = (uint16_t)in[h];     // of earlier waves
+        in[h] += n;
+      }
+  }
+  uint64_t total;
+  const uint64_t before = block_excl_scan<NT>(
+      (uint64_t)(uint32_t)(all.x + all.y) << 32 | (uint32_t)(in[0] + in[1]), s_scan, &total);
+  if (tid < cols) {
+    const int32_t b = (int32_t)(before >> 32), l = (int32_t)(before & 0xffffffffu);
+    base[2 * tid] = b + mine.x;
+    base[2 * tid + 1] = b + all.x + mine.y;
+    local[2 * tid] = (uint16_t)l;
+    local[2 * tid + 1] = (uint16_t)(l + in[0]);
   }
   __syncthreads();
+  // The tile in order in LDS, so that a digit's pairs leave in one run.
 #pragma unroll
   for (int j = 0; j < kSortKeys; ++j) {
     if (j * kWave + lane_id() >= left) continue;
     const uint32_t d = (key[j] >> a.shift) & (digits - 1);
-    const uint32_t to = (uint32_t)base[d] + cnt[w * digits + d] + rank[j];
-    key_out[to] = key[j];
-    pos_out[to] = pos[j];
+    const uint32_t to = (uint32_t)local[d] + cnt[w * digits + d] + rank[j];
+    s_key[to] = key[j];
+    s_pos[to] = pos[j];
+  }
+  __syncthreads();
+  const int size = (int)min((int64_t)kTile, a.n - (int64_t)blockIdx.x * kTile);
+#pragma unroll
+  for (int j = 0; j < kSortKeys; ++j) {
+    const int i = j * NT + tid;
+    if (i >= size) continue;
+    const uint32_t k = s_key[i], d = (k >> a.shift) & (digits - 1);
+    const uint32_t to = (uint32_t)base[d] + (uint32_t)(i - (int)local[d]);
+    key_out[to] = k;
+    pos_out[to] = s_pos[i];
   }
 }
 
 // One tile: every pass in one launch, the pairs in LDS between passes.
-__global__ void __launch_bounds__(kSortBlock) k_sort_tile(Keys a, int key_bits, int digit_bits,
+__global__ void __launch_bounds__(kTileBlock) k_sort_tile(Keys a, int key_bits, int digit_bits,
                                                           uint32_t* key_out, uint32_t* pos_out) {
+  constexpr int kSortBlock = kTileBlock, kSortWaves = kTileBlock / kWave;
   __shared__ uint32_t s_key[kTile];
   __shared__ uint16_t s_pos[kTile];
   __shared__ uint16_t cnt[kSortWaves << 8];
   __shared__ int32_t s_scan[kSortWaves];
   __shared__ int32_t base[1 << 8];
   const int w = threadIdx.x / kWave, n = (int)a.n;
-  const int first = w * kTileWave, left = min(kTileWave, max(0, n - first));
+  const int steps = (n + kSortBlock - 1) / kSortBlock;     // few ids: fewer per lane
+  const int first = w * steps * kWave, left = min(steps * kWave, max(0, n - first));
   uint32_t key[kSortKeys];
   uint16_t pos[kSortKeys], rank[kSortKeys];
   bool bad = false;
@@ -291,7 +322,7 @@ __global__ void __launch_bounds__(kSortBlock) k_sort_tile(Keys a, int key_bits, 
     }
     for (int i = threadIdx.x; i < kSortWaves * digits; i += kSortBlock) cnt[i] = 0;
     __syncthreads();
-    rank_tile(key, shift, bits, left, cnt + w * digits, rank);
+    rank_tile(key, shift, bits, left, steps, cnt + w * digits, rank);
     __syncthreads();
     int32_t s = 0, total;
     if ((int)threadIdx.x < digits)
@@ -336,7 +367,10 @@ __global__ void __launch_bounds__(kSortBlock) k_sort_tile(Keys a, int key_bits, 
 // ---------------------------------------------------------------------------
 constexpr int kGradRows = 256;       // most entries of a block
 constexpr int kGroupRun = 32;        // longest run that one group sums
-constexpr int kGradUnroll = 4;
+constexpr int kPosCache = 1024;
+constexpr int kLongUnroll = 8;       // rows in flight in a longer run
+template <int V>
+constexpr int kItems = 16 / V < 4 ? 16 / V : 4;     // short runs in flight
 
 struct GradArgs {
   const uint32_t* key;     // sorted
@@ -346,6 +380,7 @@ struct GradArgs {
   int32_t pieces;          // column pieces of a row
   int32_t lanes_log;       // lanes of a group (a power of two up to 64)
   int32_t tiles;           // column tiles of a group
+  uint32_t tmagic;         // div_magic(tiles)
   uint32_t per;            // rows (or positions) of a block
   uint32_t chunk;
   int32_t add;
@@ -369,28 +404,29 @@ __device__ uint32_t wave_lower_bound(const uint32_t* k, uint32_t lo, uint32_t hi
 }
 
 // Adds the rows dy[pos[p]], p = p0, p0 + step, .. < p1, to acc.
-template <typename TD, int V>
+template <typename TD, int V, int U>
 __device__ __forceinline__ void add_rows(const GradArgs& a, uint32_t p0, uint32_t p1, uint32_t step,
                                          int32_t e, float (&acc)[V]) {
   const char* base = a.dy.p + e * (int64_t)sizeof(TD);
-  for (uint64_t p = p0; p < p1; p += (uint64_t)step * kGradUnroll) {
-    typename Raw<TD, V>::vec raw[kGradUnroll];
-    uint32_t at[kGradUnroll];
+  for (uint64_t p = p0; p < p1; p += (uint64_t)step * U) {
+    // U rows in flight; places past the end repeat the first row and add 0.
+    typename Raw<TD, V>::vec raw[U];
+    uint32_t at[U];
 #pragma unroll
-    for (int u = 0; u < kGradUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
       const uint64_t q = p + (uint64_t)u * step;
       at[u] = a.pos[q < p1 ? q : p];
     }
 #pragma unroll
-    for (int u = 0; u < kGradUnroll; ++u)
+    for (int u = 0; u < U; ++u)
       raw[u] = raw_load<TD, V>(base + (int64_t)at[u] * a.dy.stride);
 #pragma unroll
-    for (int u = 0; u < kGradUnroll; ++u) {
-      if (p + (uint64_t)u * step >= p1) break;
+    for (int u = 0; u < U; ++u) {
+      const bool in = p + (uint64_t)u * step < p1;
       float v[V];
       to_f32<TD, V>(raw[u], v);
 #pragma unroll
-      for (int k = 0; k < V; ++k) acc[k] += v[k];
+      for (int k = 0; k < V; ++k) acc[k] += in ? v[k] : 0.0f;
     }
   }
 }
@@ -437,17 +473,23 @@ __global__ void __launch_bounds__(kBlock) k_grad_parts(GradArgs a) {
   const bool into = c1 < a.n && a.key[c1] == ke && ke < a.rows && !(from && ke == kb);
   if (!from && !into) return;
   const int w = threadIdx.x / kWave;
-  if (w < 2) {
-    const uint32_t k = w == 0 ? kb : ke;
-    if (w == 0 ? from : into) {
-      const uint32_t lo = wave_lower_bound(a.key, 0, a.n, k);
-      const uint32_t hi = wave_lower_bound(a.key, 0, a.n, k + 1);
-      if (lane_id() == 0) {
-        s_run[w][0] = max(lo, c0);
-        s_run[w][1] = hi - lo > a.chunk ? min(hi, c1) : 0u;
-      }
-    } else if (lane_id() == 0) {
-      s_run[w][0] = s_run[w][1] = 0u;
+  // Each run's positions in this chunk, none if the run is not a long one: a run
+  // that ends at h began more than a chunk earlier if the position a chunk
+  // before its last holds it too.
+  if (w == 0) {
+    const uint32_t h = from ? wave_lower_bound(a.key, c0, c1, kb + 1) : c0;
+    const bool is_long = from && ((h == c1 && c1 < a.n && a.key[c1] == kb) ||
+                                  (h > a.chunk && a.key[h - 1 - a.chunk] == kb));
+    if (lane_id() == 0) {
+      s_run[0][0] = c0;
+      s_run[0][1] = is_long ? h : c0;
+    }
+  } else if (w == 1) {
+    const uint32_t b = into ? wave_lower_bound(a.key, c0, c1, ke) : c1;
+    const bool is_long = into && (uint64_t)b + a.chunk < a.n && a.key[b + a.chunk] == ke;
+    if (lane_id() == 0) {
+      s_run[1][0] = is_long ? b : c1;
+      s_run[1][1] = c1;
     }
   }
   __syncthreads();
@@ -460,7 +502,7 @@ __global__ void __launch_bounds__(kBlock) k_grad_parts(GradArgs a) {
     const uint32_t p0 = s_run[s][0], p1 = s_run[s][1];
     if (p0 >= p1) continue;
     float acc[V] = {};
-    add_rows<TD, V>(a, p0 + g, p1, groups, e, acc);
+    add_rows<TD, V, kLongUnroll>(a, p0 + g, p1, groups, e, acc);
     join_groups<V>(acc, lds, lanes, groups);
     if (g == 0 && piece < a.pieces)
       row_store<float, V>((char*)(a.part + ((int64_t)c * 2 + s) * a.dim + e), acc);
@@ -482,14 +524,91 @@ __device__ __forceinline__ void put_row(const GradArgs& a, uint32_t row, int32_t
   row_store<TG, V>(p, acc);
 }
 
+// The runs of up to kGroupRun positions.  Items are (entry, column tile); a
+// group sums kItems of them at a time, two terms of each in flight, so that a
+// run of one or two rows, as most are, costs one wait.  CACHED: the positions
+// are in LDS.
+template <typename TD, typename TG, int V, bool CACHED>
+__device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entries,
+                                               const uint32_t* s_row, const uint32_t* s_beg,
+                                               const uint32_t* s_end, const uint32_t* s_pos,
+                                               uint32_t p0, uint32_t* many) {
+  const int lanes = 1 << a.lanes_log, groups = kBlock >> a.lanes_log;
+  const int g = threadIdx.x >> a.lanes_log, l = threadIdx.x & (lanes - 1);
+  const uint32_t items = entries * (uint32_t)a.tiles;
+  for (uint32_t i0 = 0; i0 < items; i0 += groups * kItems<V>) {
+    uint32_t x[kItems<V>], cnt[kItems<V>], most = 0;
+    int32_t e[kItems<V>];
+    typename Raw<TG, V>::vec old[kItems<V>];
+    float acc[kItems<V>][V];
+#pragma unroll
+    for (int u = 0; u < kItems<V>; ++u) {
+      const uint32_t item = i0 + u * groups + g;
+      x[u] = item < items ? chunk_row(item, a.tmagic) : 0u;
+      const int32_t piece = (int32_t)(item - x[u] * a.tiles) * lanes + l;
+      const bool mine = item < items && piece < a.pieces;
+      int32_t skip;
+      e[u] = mine ? piece_start<V>(piece, a.dim, &skip) : -1;
+      cnt[u] = s_end[x[u]] - s_beg[x[u]];
+      if (cnt[u] > kGroupRun) {
+        *many = 1;
+        e[u] = -1;
+      }
+      if (e[u] < 0) cnt[u] = 0;
+      most = max(most, cnt[u]);
+      old[u] = {};
+      if (a.add && e[u] >= 0)
+        old[u] = raw_load<TG, V>(a.grad.p + (int64_t)s_row[x[u]] * a.grad.stride +
+                                 e[u] * (int64_t)sizeof(TG));
+#pragma unroll
+      for (int k = 0; k < V; ++k) acc[u][k] = 0.0f;
+    }
+    for (uint32_t r = 0; r < most; r += 2) {
+      typename Raw<TD, V>::vec raw[kItems<V>][2];
+#pragma unroll
+      for (int u = 0; u < kItems<V>; ++u)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          raw[u][t] = {};
+          if (r + t < cnt[u]) {
+            const uint32_t p = s_beg[x[u]] + r + t;
+            const uint32_t at = CACHED ? s_pos[p - p0] : a.pos[p];
+            raw[u][t] = raw_load<TD, V>(a.dy.p + (int64_t)at * a.dy.stride +
+                                        e[u] * (int64_t)sizeof(TD));
+          }
+        }
+#pragma unroll
+      for (int u = 0; u < kItems<V>; ++u)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          float v[V];
+          to_f32<TD, V>(raw[u][t], v);
+#pragma unroll
+          for (int k = 0; k < V; ++k) acc[u][k] += v[k];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kItems<V>; ++u) {
+      if (e[u] < 0) continue;
+      float was[V];
+      to_f32<TG, V>(old[u], was);
+#pragma unroll
+      for (int k = 0; k < V; ++k) acc[u][k] = acc[u][k] * a.scale + was[k];
+      row_store<TG, V>(a.grad.p + (int64_t)s_row[x[u]] * a.grad.stride +
+                           e[u] * (int64_t)sizeof(TG), acc[u]);
+    }
+  }
+}
+
 template <typename TD, typename TG, int V>
 __global__ void __launch_bounds__(kBlock) k_grad_rows(GradArgs a) {
   __shared__ float lds[V * kBlock];
   __shared__ uint32_t s_row[kGradRows], s_beg[kGradRows], s_end[kGradRows];
+  __shared__ uint32_t s_pos[kPosCache];      // pos of the block's positions [p0, p0 + cached)
   __shared__ uint32_t s_range[2], s_many;
   __shared__ int32_t s_heads[kBlock / kWave];
   const uint32_t tid = threadIdx.x, w = tid / kWave;
-  uint32_t entries;
+  uint32_t entries, p0, cached;
   if (tid == 0) s_many = 0;
   if (!a.add) {
     // Rows [v0, v0 + entries) and their runs.
@@ -504,14 +623,17 @@ __global__ void __launch_bounds__(kBlock) k_grad_rows(GradArgs a) {
       s_beg[tid] = s_end[tid] = 0u;
     }
     __syncthreads();
-    const uint32_t p0 = s_range[0], p1 = s_range[1];
-    if (p1 - p0 <= 4 * kBlock) {
+    const uint32_t p1 = s_range[1];
+    p0 = s_range[0];
+    cached = p1 - p0 <= kPosCache ? p1 - p0 : 0u;
+    if (cached) {
       for (uint32_t p = p0 + tid; p < p1; p += kBlock) {
         const uint32_t k = a.key[p];
+        s_pos[p - p0] = a.pos[p];
         if (p == p0 || a.key[p - 1] != k) s_beg[k - v0] = p;
         if (p + 1 == p1 || a.key[p + 1] != k) s_end[k - v0] = p + 1;
       }
-    } else if (tid < entries) {
+    } else if (p1 > p0 && tid < entries) {
       uint32_t at[2];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
@@ -528,8 +650,11 @@ __global__ void __launch_bounds__(kBlock) k_grad_rows(GradArgs a) {
     }
   } else {
     // Runs that start at positions [p0, p0 + per).
-    const uint32_t p = blockIdx.x * a.per + tid;
-    const uint32_t last = min(a.n, blockIdx.x * a.per + a.per);
+    // (a run may end up to kGroupRun positions behind them)
+    p0 = blockIdx.x * a.per;
+    const uint32_t p = p0 + tid, last = min(a.n, p0 + a.per);
+    cached = min(a.n, p0 + a.per + kGroupRun) - p0;
+    for (uint32_t i = tid; i < cached; i += kBlock) s_pos[i] = a.pos[p0 + i];
     const uint32_t k = p < last ? a.key[p] : a.rows;
     const bool head = k < a.rows && (p == 0 || a.key[p - 1] != k);
     const uint64_t m = __ballot(head);
@@ -558,24 +683,13 @@ __global__ void __launch_bounds__(kBlock) k_grad_rows(GradArgs a) {
 
   const int lanes = 1 << a.lanes_log, groups = kBlock >> a.lanes_log;
   const int g = tid >> a.lanes_log, l = tid & (lanes - 1);
-  int32_t skip;
-  const uint32_t items = entries * (uint32_t)a.tiles;
-  for (uint32_t item = g; item < items; item += groups) {
-    const uint32_t x = a.tiles == 1 ? item : item / a.tiles;
-    const int32_t piece = (int32_t)(item - x * a.tiles) * lanes + l;
-    const uint32_t beg = s_beg[x], end = s_end[x];
-    if (end - beg > kGroupRun) {
-      s_many = 1;
-      continue;
-    }
-    if (piece >= a.pieces) continue;
-    const int32_t e = piece_start<V>(piece, a.dim, &skip);
-    float acc[V] = {};
-    add_rows<TD, V>(a, beg, end, 1, e, acc);
-    put_row<TG, V>(a, s_row[x], e, acc);
-  }
+  if (cached || entries == 0)
+    sum_short_runs<TD, TG, V, true>(a, entries, s_row, s_beg, s_end, s_pos, p0, &s_many);
+  else
+    sum_short_runs<TD, TG, V, false>(a, entries, s_row, s_beg, s_end, s_pos, p0, &s_many);
   __syncthreads();
   if (!s_many) return;
+  int32_t skip;
   for (uint32_t x = 0; x < entries; ++x) {
     const uint32_t beg = s_beg[x], end = s_end[x];
     if (end - beg <= kGroupRun) continue;
@@ -586,7 +700,7 @@ __global__ void __launch_bounds__(kBlock) k_grad_rows(GradArgs a) {
       if (end - beg > a.chunk)
         add_parts<V>(a, beg, end, g, groups, e, acc);
       else
-        add_rows<TD, V>(a, beg + g, end, groups, e, acc);
+        add_rows<TD, V, kLongUnroll>(a, beg + g, end, groups, e, acc);
       join_groups<V>(acc, lds, lanes, groups);
       if (g == 0 && piece < a.pieces) put_row<TG, V>(a, s_row[x], e, acc);
     }
@@ -597,9 +711,21 @@ __global__ void __launch_bounds__(kBlock) k_grad_rows(GradArgs a) {
 // Host side.
 // ---------------------------------------------------------------------------
 uint32_t grad_chunk(int64_t n) {
-  uint32_t c = 128;
+  uint32_t c = 64;
   while (c < 1024 && (int64_t)c * 1024 < n) c *= 2;
   return c;
+}
+
+// The sort of n ids: one tile in one launch, or tiles of a block each.
+struct SortShape {
+  int tiles, threads, digit;   // digit: most bits of one
+};
+
+SortShape sort_shape(int64_t n) {
+  if (n <= kTile) return {n > 0 ? 1 : 0, kTileBlock, 8};
+  const int64_t small = cdiv(n, kBlock * kSortKeys);
+  if (small <= kSmallSortTiles) return {(int)small, kBlock, small <= kWideTiles ? kMaxDigit : 8};
+  return {(int)cdiv(n, kTile), 1024, 8};
 }
 
 struct EmbedWs {
@@ -611,12 +737,12 @@ struct EmbedWs {
 size_t embed_ws_layout(int64_t n, int32_t dim, char* base, EmbedWs* out) {
   Carve c{base, 0, 0};
   EmbedWs w;
-  const int64_t tiles = cdiv(n, kTile);
+  const SortShape sh = sort_shape(n);
   for (int i = 0; i < 2; ++i) {
     w.key[i] = c.take<uint32_t>((size_t)n);
     w.pos[i] = c.take<uint32_t>((size_t)n);
   }
-  w.hist = c.take<int32_t>((size_t)tiles << (tiles <= kWideTiles ? kMaxDigit : 8));
+  w.hist = c.take<int32_t>((size_t)sh.tiles << sh.digit);
   w.part = c.take<float>((size_t)cdiv(n, grad_chunk(n)) * 2 * dim);
   if (out) *out = w;
   return align_up(c.used, 256);
@@ -747,12 +873,12 @@ extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t
   k.rows = (uint32_t)num_rows;
   k.status = status_d;
   const int key_bits = 32 - __builtin_clz((unsigned)std::max<int64_t>(num_rows, 1));
-  const int tiles = (int)cdiv(n, kTile);
-  const int most = tiles > 1 && tiles <= kWideTiles ? kMaxDigit : 8;
+  const SortShape sh = sort_shape(n);
+  const int tiles = sh.tiles, most = sh.digit;
   const int passes = (int)cdiv(key_bits, most), digit = (int)cdiv(key_bits, passes);
   int at = 0;
   if (tiles == 1) {
-    hipLaunchKernelGGL(k_sort_tile, dim3(1), dim3(kSortBlock), 0, stream, k, key_bits, digit,
+    hipLaunchKernelGGL(k_sort_tile, dim3(1), dim3(kTileBlock), 0, stream, k, key_bits, digit,
                        w.key[0], w.pos[0]);
     GG_LAUNCH_CHECK("k_sort_tile");
   } else if (tiles > 1) {
@@ -760,11 +886,19 @@ extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t
       k.shift = p * digit;
       k.bits = std::min(digit, key_bits - k.shift);
       at = p & 1;
-      hipLaunchKernelGGL(k_sort_count, dim3((unsigned)tiles), dim3(kSortBlock), 0, stream, k,
-                         w.hist);
+      if (sh.threads == kBlock)
+        hipLaunchKernelGGL(k_sort_count<kBlock>, dim3((unsigned)tiles), dim3(kBlock), 0, stream, k,
+                           w.hist);
+      else
+        hipLaunchKernelGGL(k_sort_count<1024>, dim3((unsigned)tiles), dim3(1024), 0, stream, k,
+                           w.hist);
       GG_LAUNCH_CHECK("k_sort_count");
-      hipLaunchKernelGGL(k_sort_scatter, dim3((unsigned)tiles), dim3(kSortBlock), 0, stream, k,
-                         w.hist, tiles, w.key[at], w.pos[at]);
+      if (sh.threads == kBlock)
+        hipLaunchKernelGGL(k_sort_scatter<kBlock>, dim3((unsigned)tiles), dim3(kBlock), 0, stream,
+                           k, w.hist, tiles, w.key[at], w.pos[at]);
+      else
+        hipLaunchKernelGGL(k_sort_scatter<1024>, dim3((unsigned)tiles), dim3(1024), 0, stream, k,
+                           w.hist, tiles, w.key[at], w.pos[at]);
       GG_LAUNCH_CHECK("k_sort_scatter");
       k.ids = nullptr;
       k.key = w.key[at];
@@ -780,15 +914,16 @@ extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t
   a.scale = scale;
   a.part = w.part;
   a.chunk = grad_chunk(n);
-  // Rows of a block: as many as leave the chip 2,048 blocks.
+  // Rows of a block: as many as leave the chip 8,192 blocks.
   a.per = 1;
-  while (a.per < kGradRows && (int64_t)a.per * 4096 <= (a.add ? n : num_rows)) a.per *= 2;
+  while (a.per < kGradRows && (int64_t)a.per * 8192 <= (a.add ? n : num_rows)) a.per *= 2;
   GG_FOR_FLOAT(dy->dtype, TD, {
     constexpr int V = kVec<TD>;
     const Lanes l = lanes_of(dim, dim >= V ? V : 1);
     a.pieces = l.pieces;
     a.lanes_log = l.lanes_log;
     a.tiles = l.tiles;
+    a.tmagic = div_magic((uint32_t)l.tiles);
     GG_FOR_FLOAT(grad->dtype, TG, {
       return dim >= V ? launch_grad<TD, TG, V>(a, stream) : launch_grad<TD, TG, 1>(a, stream);
     });
