@@ -105,6 +105,30 @@ constexpr int kWideTiles = 64;
 // the chip; blocks of 16 waves keep the counters of many tiles few.
 constexpr int kSmallSortTiles = 256;              // most tiles of 4-wave blocks
 
+// Rows to be cleared by the sort's launches, in blocks behind its own: the sort
+// waits for memory more than it uses it.
+struct FillArgs {
+  char* p;
+  int64_t stride;
+  int64_t r0, r1;          // rows of this launch
+  int32_t row_bytes, pieces, lanes_log;
+};
+
+template <int NT>
+__device__ void fill_rows_with_zeros(const FillArgs& f, uint32_t block, uint32_t blocks) {
+  const int groups = NT >> f.lanes_log, lanes = 1 << f.lanes_log;
+  const int g = threadIdx.x >> f.lanes_log, l = threadIdx.x & (lanes - 1);
+  for (int64_t r = f.r0 + (int64_t)block * groups + g; r < f.r1; r += (int64_t)blocks * groups) {
+    char* p = f.p + r * f.stride;
+    for (int32_t c = l; c < f.pieces; c += lanes) {
+      if (f.row_bytes >= 16)
+        *(GG_GLOBAL Raw<f16, 8>::mem*)(p + min(c * 16, f.row_bytes - 16)) = Raw<f16, 8>::vec{};
+      else
+        *(GG_GLOBAL uint16_t*)(p + 2 * c) = 0;
+    }
+  }
+}
+
 struct Keys {
   const void* ids;       // first pass: the ids; later passes: key and pos
   int32_t id_bits;
@@ -163,7 +187,10 @@ constexpr int digit_limit(int nt) { return nt == kBlock ? kMaxDigit : 8; }
 
 // Digit counts of each tile: hist[tile][digit].
 template <int NT>
-__global__ void __launch_bounds__(NT) k_sort_count(Keys a, int32_t* hist) {
+__global__ void __launch_bounds__(NT) k_sort_count(Keys a, int32_t* hist, int tiles,
+                                                   FillArgs f) {
+  if ((int)blockIdx.x >= tiles)
+    return fill_rows_with_zeros<NT>(f, blockIdx.x - tiles, gridDim.x - tiles);
   constexpr int kSortBlock = NT, kSortWaves = NT / kWave, kTile = NT * kSortKeys;
   __shared__ uint16_t cnt[kSortWaves << digit_limit(NT)];
   const int digits = 1 << a.bits, w = threadIdx.x / kWave;
@@ -195,7 +222,10 @@ __global__ void __launch_bounds__(NT) k_sort_count(Keys a, int32_t* hist) {
 // (hist) tell.
 template <int NT>
 __global__ void __launch_bounds__(NT) k_sort_scatter(Keys a, const int32_t* hist, int tiles,
-                                                     uint32_t* key_out, uint32_t* pos_out) {
+                                                     uint32_t* key_out, uint32_t* pos_out,
+                                                     FillArgs f) {
+  if ((int)blockIdx.x >= tiles)
+    return fill_rows_with_zeros<NT>(f, blockIdx.x - tiles, gridDim.x - tiles);
   constexpr int kSortWaves = NT / kWave, kTile = NT * kSortKeys;
   __shared__ uint16_t cnt[kSortWaves << digit_limit(NT)];
   __shared__ int32_t base[1 << digit_limit(NT)];
@@ -288,7 +318,10 @@ __global__ void __launch_bounds__(NT) k_sort_scatter(Keys a, const int32_t* hist
 
 // One tile: every pass in one launch, the pairs in LDS between passes.
 __global__ void __launch_bounds__(kTileBlock) k_sort_tile(Keys a, int key_bits, int digit_bits,
-                                                          uint32_t* key_out, uint32_t* pos_out) {
+                                                          uint32_t* key_out, uint32_t* pos_out,
+                                                          FillArgs f) {
+  if (blockIdx.x > 0)
+    return fill_rows_with_zeros<kTileBlock>(f, blockIdx.x - 1, gridDim.x - 1);
   constexpr int kSortBlock = kTileBlock, kSortWaves = kTileBlock / kWave;
   __shared__ uint32_t s_key[kTile];
   __shared__ uint16_t s_pos[kTile];
@@ -384,6 +417,8 @@ struct GradArgs {
   uint32_t per;            // rows (or positions) of a block
   uint32_t chunk;
   int32_t add;
+  int32_t by_position;     // blocks have positions, not rows: rows are added to, or were cleared
+  uint32_t part_blocks;
   float scale;
   KRows dy, grad;
   float* part;             // [chunk][2][dim]: a run from before the chunk, one into the next
@@ -404,24 +439,24 @@ __device__ uint32_t wave_lower_bound(const uint32_t* k, uint32_t lo, uint32_t hi
 }
 
 // Adds the rows dy[pos[p]], p = p0, p0 + step, .. < p1, to acc.
-template <typename TD, int V, int U>
+template <typename TD, int V>
 __device__ __forceinline__ void add_rows(const GradArgs& a, uint32_t p0, uint32_t p1, uint32_t step,
                                          int32_t e, float (&acc)[V]) {
   const char* base = a.dy.p + e * (int64_t)sizeof(TD);
-  for (uint64_t p = p0; p < p1; p += (uint64_t)step * U) {
-    // U rows in flight; places past the end repeat the first row and add 0.
-    typename Raw<TD, V>::vec raw[U];
-    uint32_t at[U];
+  for (uint64_t p = p0; p < p1; p += (uint64_t)step * kLongUnroll) {
+    // Several rows in flight; places past the end repeat the first row and add 0.
+    typename Raw<TD, V>::vec raw[kLongUnroll];
+    uint32_t at[kLongUnroll];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < kLongUnroll; ++u) {
       const uint64_t q = p + (uint64_t)u * step;
       at[u] = a.pos[q < p1 ? q : p];
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < kLongUnroll; ++u)
       raw[u] = raw_load<TD, V>(base + (int64_t)at[u] * a.dy.stride);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < kLongUnroll; ++u) {
       const bool in = p + (uint64_t)u * step < p1;
       float v[V];
       to_f32<TD, V>(raw[u], v);
@@ -462,11 +497,11 @@ __device__ __forceinline__ void join_groups(float (&acc)[V], float* lds, int lan
       for (int k = 0; k < V; ++k) acc[k] += lds[k * kBlock + g * lanes + tid];
 }
 
+// One column tile of a chunk's parts of long runs.
 template <typename TD, int V>
-__global__ void __launch_bounds__(kBlock) k_grad_parts(GradArgs a) {
-  __shared__ float lds[V * kBlock];
-  __shared__ uint32_t s_run[2][2];
-  const uint32_t c = blockIdx.x, c0 = c * a.chunk;
+__device__ __forceinline__ void sum_parts(const GradArgs& a, uint32_t c, int32_t tile, float* lds,
+                                          uint32_t (*s_run)[2]) {
+  const uint32_t c0 = c * a.chunk;
   const uint32_t c1 = (uint32_t)min((uint64_t)a.n, (uint64_t)c0 + a.chunk);
   const uint32_t kb = a.key[c0], ke = a.key[c1 - 1];
   const bool from = c0 > 0 && a.key[c0 - 1] == kb && kb < a.rows;
@@ -495,14 +530,14 @@ __global__ void __launch_bounds__(kBlock) k_grad_parts(GradArgs a) {
   __syncthreads();
   const int lanes = 1 << a.lanes_log, groups = kBlock >> a.lanes_log;
   const int g = threadIdx.x >> a.lanes_log, l = threadIdx.x & (lanes - 1);
-  const int32_t piece = (int32_t)blockIdx.y * lanes + l;
+  const int32_t piece = tile * lanes + l;
   int32_t skip;
   const int32_t e = piece_start<V>(min(piece, a.pieces - 1), a.dim, &skip);
   for (int s = 0; s < 2; ++s) {
     const uint32_t p0 = s_run[s][0], p1 = s_run[s][1];
     if (p0 >= p1) continue;
     float acc[V] = {};
-    add_rows<TD, V, kLongUnroll>(a, p0 + g, p1, groups, e, acc);
+    add_rows<TD, V>(a, p0 + g, p1, groups, e, acc);
     join_groups<V>(acc, lds, lanes, groups);
     if (g == 0 && piece < a.pieces)
       row_store<float, V>((char*)(a.part + ((int64_t)c * 2 + s) * a.dim + e), acc);
@@ -525,9 +560,10 @@ __device__ __forceinline__ void put_row(const GradArgs& a, uint32_t row, int32_t
 }
 
 // The runs of up to kGroupRun positions.  Items are (entry, column tile); a
-// group sums kItems of them at a time, two terms of each in flight, so that a
-// run of one or two rows, as most are, costs one wait.  CACHED: the positions
-// are in LDS.
+// group sums kItems of them at a time, two rows of each in flight, so that runs
+// of one or two rows, as most are, cost one wait (eight rows of one item at a
+// time instead, after the first two, need more registers: 1.5M rows of 100 fp32
+// into 2.45M 478 us, this way 441).  CACHED: the positions are in LDS.
 template <typename TD, typename TG, int V, bool CACHED>
 __device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entries,
                                                const uint32_t* s_row, const uint32_t* s_beg,
@@ -568,7 +604,7 @@ __device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entri
 #pragma unroll
       for (int u = 0; u < kItems<V>; ++u)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (uint32_t t = 0; t < 2; ++t) {
           raw[u][t] = {};
           if (r + t < cnt[u]) {
             const uint32_t p = s_beg[x[u]] + r + t;
@@ -600,9 +636,18 @@ __device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entri
   }
 }
 
+// The first blocks sum the chunks' parts of long runs, a column tile each; the
+// others have rows of the gradient.
 template <typename TD, typename TG, int V>
 __global__ void __launch_bounds__(kBlock) k_grad_rows(GradArgs a) {
   __shared__ float lds[V * kBlock];
+  __shared__ uint32_t s_run[2][2];
+  if (blockIdx.x < a.part_blocks) {
+    const uint32_t c = blockIdx.x / (uint32_t)a.tiles;
+    sum_parts<TD, V>(a, c, (int32_t)(blockIdx.x - c * a.tiles), lds, s_run);
+    return;
+  }
+  const uint32_t block = blockIdx.x - a.part_blocks;
   __shared__ uint32_t s_row[kGradRows], s_beg[kGradRows], s_end[kGradRows];
   __shared__ uint32_t s_pos[kPosCache];      // pos of the block's positions [p0, p0 + cached)
   __shared__ uint32_t s_range[2], s_many;
@@ -610,9 +655,9 @@ __global__ void __launch_bounds__(kBlock) k_grad_rows(GradArgs a) {
   const uint32_t tid = threadIdx.x, w = tid / kWave;
   uint32_t entries, p0, cached;
   if (tid == 0) s_many = 0;
-  if (!a.add) {
+  if (!a.by_position) {
     // Rows [v0, v0 + entries) and their runs.
-    const uint32_t v0 = blockIdx.x * a.per;
+    const uint32_t v0 = block * a.per;
     entries = min(a.per, a.rows - v0);
     if (w < 2) {
       const uint32_t r = wave_lower_bound(a.key, 0, a.n, w == 0 ? v0 : v0 + entries);
@@ -651,7 +696,7 @@ __global__ void __launch_bounds__(kBlock) k_grad_rows(GradArgs a) {
   } else {
     // Runs that start at positions [p0, p0 + per).
     // (a run may end up to kGroupRun positions behind them)
-    p0 = blockIdx.x * a.per;
+    p0 = block * a.per;
     const uint32_t p = p0 + tid, last = min(a.n, p0 + a.per);
     cached = min(a.n, p0 + a.per + kGroupRun) - p0;
     for (uint32_t i = tid; i < cached; i += kBlock) s_pos[i] = a.pos[p0 + i];
@@ -692,19 +737,39 @@ __global__ void __launch_bounds__(kBlock) k_grad_rows(GradArgs a) {
   int32_t skip;
   for (uint32_t x = 0; x < entries; ++x) {
     const uint32_t beg = s_beg[x], end = s_end[x];
-    if (end - beg <= kGroupRun) continue;
+    if (end - beg <= kGroupRun || end - beg > a.chunk) continue;
     for (int32_t t = 0; t < a.tiles; ++t) {
       const int32_t piece = t * lanes + l;
       const int32_t e = piece_start<V>(min(piece, a.pieces - 1), a.dim, &skip);
       float acc[V] = {};
-      if (end - beg > a.chunk)
-        add_parts<V>(a, beg, end, g, groups, e, acc);
-      else
-        add_rows<TD, V, kLongUnroll>(a, beg + g, end, groups, e, acc);
+      add_rows<TD, V>(a, beg + g, end, groups, e, acc);
       join_groups<V>(acc, lds, lanes, groups);
       if (g == 0 && piece < a.pieces) put_row<TG, V>(a, s_row[x], e, acc);
     }
   }
+}
+
+// The long runs that start in chunk blockIdx.x, which is at most one: its
+// parts are added up in the order of the chunks.
+template <typename TG, int V>
+__global__ void __launch_bounds__(kBlock) k_grad_long(GradArgs a) {
+  __shared__ float lds[V * kBlock];
+  const uint32_t c = blockIdx.x, c0 = c * a.chunk, c1 = c0 + a.chunk;   // c1 < n
+  const uint32_t k = a.key[c1 - 1];
+  if (k >= a.rows || a.key[c1] != k) return;
+  const uint32_t beg = wave_lower_bound(a.key, c0, c1, k);
+  if (beg == c0 && c0 > 0 && a.key[c0 - 1] == k) return;        // started earlier
+  if ((uint64_t)beg + a.chunk >= a.n || a.key[beg + a.chunk] != k) return;
+  const uint32_t end = wave_lower_bound(a.key, c1, a.n, k + 1);
+  const int lanes = 1 << a.lanes_log, groups = kBlock >> a.lanes_log;
+  const int g = threadIdx.x >> a.lanes_log, l = threadIdx.x & (lanes - 1);
+  const int32_t piece = (int32_t)blockIdx.y * lanes + l;
+  int32_t skip;
+  const int32_t e = piece_start<V>(min(piece, a.pieces - 1), a.dim, &skip);
+  float acc[V] = {};
+  add_parts<V>(a, beg, end, g, groups, e, acc);
+  join_groups<V>(acc, lds, lanes, groups);
+  if (g == 0 && piece < a.pieces) put_row<TG, V>(a, k, e, acc);
 }
 
 // ---------------------------------------------------------------------------
@@ -748,6 +813,8 @@ size_t embed_ws_layout(int64_t n, int32_t dim, char* base, EmbedWs* out) {
   return align_up(c.used, 256);
 }
 
+constexpr int kFillLanes = 256 * 1024;      // most lanes that clear rows in a launch
+
 struct Lanes {
   int32_t pieces, lanes_log, tiles;
 };
@@ -787,17 +854,18 @@ int launch_lookup(LookupArgs& a, hipStream_t stream) {
 }
 
 template <typename TD, typename TG, int V>
-int launch_grad(const GradArgs& a, hipStream_t stream) {
-  const unsigned chunks = (unsigned)cdiv(a.n, a.chunk);
-  if (chunks > 1) {
-    hipLaunchKernelGGL((k_grad_parts<TD, V>), dim3(chunks, (unsigned)a.tiles), dim3(kBlock), 0,
-                       stream, a);
-    GG_LAUNCH_CHECK("k_grad_parts");
-  }
-  const unsigned blocks = (unsigned)cdiv(a.add ? a.n : a.rows, a.per);
+int launch_grad(GradArgs& a, hipStream_t stream) {
+  const int64_t chunks = cdiv(a.n, a.chunk);
+  a.part_blocks = chunks > 1 ? (uint32_t)(chunks * a.tiles) : 0u;
+  const int64_t blocks = a.part_blocks + cdiv(a.by_position ? a.n : a.rows, a.per);
   if (blocks > 0) {
-    hipLaunchKernelGGL((k_grad_rows<TD, TG, V>), dim3(blocks), dim3(kBlock), 0, stream, a);
+    hipLaunchKernelGGL((k_grad_rows<TD, TG, V>), dim3((unsigned)blocks), dim3(kBlock), 0, stream, a);
     GG_LAUNCH_CHECK("k_grad_rows");
+  }
+  if (chunks > 1) {
+    hipLaunchKernelGGL((k_grad_long<TG, V>), dim3((unsigned)chunks - 1, (unsigned)a.tiles),
+                       dim3(kBlock), 0, stream, a);
+    GG_LAUNCH_CHECK("k_grad_long");
   }
   return GG_OK;
 }
@@ -876,29 +944,55 @@ extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t
   const SortShape sh = sort_shape(n);
   const int tiles = sh.tiles, most = sh.digit;
   const int passes = (int)cdiv(key_bits, most), digit = (int)cdiv(key_bits, passes);
+  // Where ids reach few of the rows, the sort's launches clear all rows beside
+  // their own work and only rows that occur are written after it.  (The rows'
+  // first stores count twice then: from one id per two rows on, the pass over
+  // all rows is faster.)
+  a.by_position = a.add || (n > 0 && n * 2 <= num_rows);
+  const bool clear = a.by_position && !a.add;
+  FillArgs f = {};
+  f.p = a.grad.p;
+  f.stride = a.grad.stride;
+  f.row_bytes = dim * (int32_t)elem_bytes(grad->dtype);
+  const Lanes fl = lanes_of(f.row_bytes, f.row_bytes >= 16 ? 16 : 2);
+  f.pieces = fl.pieces;
+  f.lanes_log = fl.lanes_log;
+  const int launches = tiles == 1 ? 1 : 2 * passes;
+  int launched = 0;
+  // Blocks that clear the next launch's share of the rows.
+  const auto fill_blocks = [&](int threads) {
+    f.r0 = num_rows * launched / launches;
+    f.r1 = num_rows * (launched + 1) / launches;
+    ++launched;
+    if (!clear) return 0;
+    const int64_t want = cdiv((f.r1 - f.r0) << f.lanes_log, threads);
+    return (int)std::min<int64_t>(want, kFillLanes / threads);
+  };
   int at = 0;
   if (tiles == 1) {
-    hipLaunchKernelGGL(k_sort_tile, dim3(1), dim3(kTileBlock), 0, stream, k, key_bits, digit,
-                       w.key[0], w.pos[0]);
+    const int fb = fill_blocks(kTileBlock);
+    hipLaunchKernelGGL(k_sort_tile, dim3(1 + fb), dim3(kTileBlock), 0, stream, k, key_bits, digit,
+                       w.key[0], w.pos[0], f);
     GG_LAUNCH_CHECK("k_sort_tile");
   } else if (tiles > 1) {
     for (int p = 0; p < passes; ++p) {
       k.shift = p * digit;
       k.bits = std::min(digit, key_bits - k.shift);
       at = p & 1;
+      const dim3 threads((unsigned)sh.threads);
+      dim3 grid((unsigned)(tiles + fill_blocks(sh.threads)));
       if (sh.threads == kBlock)
-        hipLaunchKernelGGL(k_sort_count<kBlock>, dim3((unsigned)tiles), dim3(kBlock), 0, stream, k,
-                           w.hist);
+        hipLaunchKernelGGL(k_sort_count<kBlock>, grid, threads, 0, stream, k, w.hist, tiles, f);
       else
-        hipLaunchKernelGGL(k_sort_count<1024>, dim3((unsigned)tiles), dim3(1024), 0, stream, k,
-                           w.hist);
+        hipLaunchKernelGGL(k_sort_count<1024>, grid, threads, 0, stream, k, w.hist, tiles, f);
       GG_LAUNCH_CHECK("k_sort_count");
+      grid.x = (unsigned)(tiles + fill_blocks(sh.threads));
       if (sh.threads == kBlock)
-        hipLaunchKernelGGL(k_sort_scatter<kBlock>, dim3((unsigned)tiles), dim3(kBlock), 0, stream,
-                           k, w.hist, tiles, w.key[at], w.pos[at]);
+        hipLaunchKernelGGL(k_sort_scatter<kBlock>, grid, threads, 0, stream, k, w.hist, tiles,
+                           w.key[at], w.pos[at], f);
       else
-        hipLaunchKernelGGL(k_sort_scatter<1024>, dim3((unsigned)tiles), dim3(1024), 0, stream, k,
-                           w.hist, tiles, w.key[at], w.pos[at]);
+        hipLaunchKernelGGL(k_sort_scatter<1024>, grid, threads, 0, stream, k, w.hist, tiles,
+                           w.key[at], w.pos[at], f);
       GG_LAUNCH_CHECK("k_sort_scatter");
       k.ids = nullptr;
       k.key = w.key[at];
@@ -916,7 +1010,7 @@ extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t
   a.chunk = grad_chunk(n);
   // Rows of a block: as many as leave the chip 8,192 blocks.
   a.per = 1;
-  while (a.per < kGradRows && (int64_t)a.per * 8192 <= (a.add ? n : num_rows)) a.per *= 2;
+  while (a.per < kGradRows && (int64_t)a.per * 8192 <= (a.by_position ? n : num_rows)) a.per *= 2;
   GG_FOR_FLOAT(dy->dtype, TD, {
     constexpr int V = kVec<TD>;
     const Lanes l = lanes_of(dim, dim >= V ? V : 1);
