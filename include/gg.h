@@ -644,7 +644,7 @@ size_t gg_ws_distill(int64_t n, int64_t vocab);
 /* Distillation loss of n rows of logits z [n][vocab] against a teacher's top
  * logits: row i has k entries, ids (int32 or int64, row i's at top_ids_d + i *
  * ids_stride bytes; -1: no entry) and logits top [n][k].  With T the
- * temperature, p = softmax(top / T) over the row's entries, q = softmax(z / T)
+ * temperature (1e-30 to 1e30), p = softmax(top / T) over the row's entries, q = softmax(z / T)
  * over the vocabulary and a = weight * row_w_d[i] (NULL: ones):
  *   loss_d[i] = a T^2 sum_k p_k (log p_k - log q[id_k])
  *   lse_d[i]  = log sum_j exp(z_j / T)                       (NULL: not wanted)

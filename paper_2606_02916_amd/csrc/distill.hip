@@ -35,22 +35,50 @@ struct DistillArgs {
   int32_t* status;
 };
 
-// exp((z - m) / T).  The difference comes first: it is exact or small where the
-// result counts, also for logits of the type's lowest value.
-__device__ __forceinline__ float exp_of(float z, float m, float c2) {
-  return __builtin_amdgcn_exp2f((z - m) * c2);
+// exp((z - m) / T) as 2^(z c2 - b), c2 = log2(e) / T and b = m c2: one fused
+// multiply-add, rounded once, and the same b in a sum and in what is divided
+// by it.  A b beyond fp32's range (all logits at the type's lowest value, say) or
+// close to it means that logits which differ at all differ by far too much to
+// count, so c2 becomes a power of two under which m c2 is exact and the least
+// difference is 2^10.
+struct Soft {
+  float m, c2, b;
+  bool coarse;
+};
+
+__device__ __forceinline__ Soft soft_of(float m, float c2) {
+  if (m == -INFINITY) return {m, c2, 0.0f, false};     // masked logits give 0
+  const float b = m * c2;
+  if (fabsf(b) > 0x1p126f && fabsf(m) <= 3.4028235e38f) {
+    const uint32_t e = (__float_as_uint(m) >> 23) & 255u;
+    const float c = __uint_as_float((254u + 34u - e) << 23);
+    return {m, c, m * c, true};
+  }
+  return {m, c2, b, false};
 }
-// A maximum to subtract: 0 for one of -infinity, so that masked logits give 0.
-__device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.0f : m; }
+
+__device__ __forceinline__ float exp_of(float z, const Soft& s) {
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(z, s.c2, -s.b));
+}
+
+// What a sum relative to a counts for relative to the larger maximum of t.
+__device__ __forceinline__ float factor(const Soft& a, const Soft& t) {
+  if (a.m == t.m) return 1.0f;
+  return a.coarse || t.coarse || a.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(a.b - t.b);
+}
 
 struct MaxSum {
-  float m, s;
+  float m, s;     // largest logit; sum of exp((z - m) / T)
 };
 
 __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float c2) {
-  // a sum beside a maximum of -infinity is 0 (or NaN, which stays)
-  const float m = fmaxf(a.m, b.m), f = finite_max(m);
-  return {m, a.s * exp_of(a.m, f, c2) + b.s * exp_of(b.m, f, c2)};
+  const Soft t = soft_of(fmaxf(a.m, b.m), c2);
+  return {t.m, a.s * factor(soft_of(a.m, c2), t) + b.s * factor(soft_of(b.m, c2), t)};
+}
+
+__device__ __forceinline__ float lse_of(const MaxSum& st, const Soft& t, float inv_temp) {
+  const float l2 = __builtin_amdgcn_logf(st.s);       // -infinity for a row of none
+  return t.coarse ? t.m * inv_temp + kLn2 * l2 : kLn2 * (t.b + l2);
 }
 
 __device__ __forceinline__ float lanes_sum(float v, int lanes) {
@@ -62,8 +90,15 @@ __device__ __forceinline__ float lanes_maxf(float v, int lanes) {
   return v;
 }
 
-// The row's entries: id (-1: none), p, log2 p and z[id], in LDS.
+// ---------------------------------------------------------------------------
+// A row's entries, up to kPerLane for each of `lanes` lanes of one wave.  Their
+// loads are issued around the row's own: the ids before it, the logits at the
+// ids behind it.  LDS holds, per entry, its id (-1: none), p summed over the
+// entries with that id, log2 of its own p, and z[id].
+// ---------------------------------------------------------------------------
 constexpr int kEntryBytes = 16;
+constexpr int kPerLane = 4;
+static_assert(kPerLane * kWave >= GG_DISTILL_MAX_K, "a wave holds all entries");
 
 struct Entries {
   int32_t* id;
@@ -75,43 +110,88 @@ __device__ __forceinline__ Entries entries_at(char* lds, int group, int k) {
   return {(int32_t*)at, (float*)(at + 4 * k), (float*)(at + 8 * k), (float*)(at + 12 * k)};
 }
 
-// Fills the entries, by `lanes` lanes of one wave; whether the row has a lesson
-// (an entry with a finite logit, and a weight).
-template <typename T>
-__device__ __forceinline__ bool read_entries(const DistillArgs& a, int64_t row, int l, int lanes,
-                                             const Entries& en) {
+struct Held {
+  int32_t id[kPerLane];
+  float t[kPerLane], z[kPerLane];
+};
+
+__device__ __forceinline__ void load_entries(const DistillArgs& a, int64_t row, int l, int lanes,
+                                             Held& h) {
   const char* ids = a.ids + row * a.ids_stride;
   const char* tp = a.top.p + row * a.top.stride;
-  const char* zp = a.z.p + row * a.z.stride;
-  float tm = -INFINITY;
   bool bad = false;
-  for (int j = l; j < a.k; j += lanes) {
-    const int64_t id = a.ids64 ? ((const int64_t*)ids)[j] : (int64_t)((const int32_t*)ids)[j];
-    const bool in = (uint64_t)id < (uint64_t)a.vocab;
-    bad |= !in && id != -1;
-    float t[1];
-    GG_FOR_FLOAT(a.top_dtype, TT, { row_load<TT, 1>(tp + j * (int64_t)sizeof(TT), t); });
-    float z[1] = {0.0f};
-    if (in) row_load<T, 1>(zp + id * (int64_t)sizeof(T), z);
-    t[0] = in ? t[0] : -INFINITY;
-    en.id[j] = in ? (int32_t)id : -1;
-    en.lp[j] = t[0];
-    en.z[j] = z[0];
-    tm = fmaxf(tm, t[0]);
+#pragma unroll
+  for (int u = 0; u < kPerLane; ++u) {
+    const int j = u * lanes + l;
+    h.id[u] = -1;
+    h.t[u] = -INFINITY;
+    if (j < a.k) {
+      const int64_t id = a.ids64 ? ((const int64_t*)ids)[j] : (int64_t)((const int32_t*)ids)[j];
+      float t[1];
+      GG_FOR_FLOAT(a.top_dtype, TT, { row_load<TT, 1>(tp + j * (int64_t)sizeof(TT), t); });
+      const bool in = (uint64_t)id < (uint64_t)a.vocab;
+      bad |= !in && id != -1;
+      if (in) {
+        h.id[u] = (int32_t)id;
+        h.t[u] = t[0];
+      }
+    }
   }
   if (bad) set_status(a.status, GG_DEV_BAD_ID);
-  tm = lanes_maxf(tm, lanes);
-  const float f = finite_max(tm);
-  float total = 0.0f;
-  for (int j = l; j < a.k; j += lanes) total += exp_of(en.lp[j], f, a.c2);
-  total = lanes_sum(total, lanes);
-  const float log_total = __builtin_amdgcn_logf(total);
-  for (int j = l; j < a.k; j += lanes) {
-    const float lp = (en.lp[j] - f) * a.c2 - log_total;
-    en.lp[j] = lp;
-    en.p[j] = __builtin_amdgcn_exp2f(lp);
+}
+
+template <typename T>
+__device__ __forceinline__ void load_entry_logits(const DistillArgs& a, int64_t row, Held& h) {
+  const char* zp = a.z.p + row * a.z.stride;
+#pragma unroll
+  for (int u = 0; u < kPerLane; ++u) {
+    float z[1] = {0.0f};
+    if (h.id[u] >= 0) row_load<T, 1>(zp + h.id[u] * (int64_t)sizeof(T), z);
+    h.z[u] = z[0];
   }
-  return tm != -INFINITY && (a.row_w ? a.row_w[row] : 1.0f) * a.weight != 0.0f;
+}
+
+// Whether the row has a lesson: an entry with a logit above -infinity, and a weight.
+__device__ __forceinline__ bool share_entries(const DistillArgs& a, int64_t row, int l, int lanes,
+                                              const Held& h, const Entries& en) {
+  float tm = h.t[0];
+#pragma unroll
+  for (int u = 1; u < kPerLane; ++u) tm = fmaxf(tm, h.t[u]);
+  const Soft f = soft_of(lanes_maxf(tm, lanes), a.c2);
+  float total = 0.0f;
+#pragma unroll
+  for (int u = 0; u < kPerLane; ++u) total += exp_of(h.t[u], f);
+  const float log_total = __builtin_amdgcn_logf(lanes_sum(total, lanes));
+#pragma unroll
+  for (int u = 0; u < kPerLane; ++u) {
+    const int j = u * lanes + l;
+    if (j < a.k) {
+      const float lp = __builtin_fmaf(h.t[u], f.c2, -f.b) - log_total;
+      en.id[j] = h.id[u];
+      en.lp[j] = lp;
+      en.p[j] = __builtin_amdgcn_exp2f(lp);
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  float p[kPerLane] = {};
+  for (int x = 0; x < a.k; ++x) {
+    const int32_t id = en.id[x];
+    const float px = en.p[x];
+#pragma unroll
+    for (int u = 0; u < kPerLane; ++u) p[u] += h.id[u] == id ? px : 0.0f;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+  for (int u = 0; u < kPerLane; ++u)
+    if (u * lanes + l < a.k) en.p[u * lanes + l] = p[u];
+  return f.m != -INFINITY && (a.row_w ? a.row_w[row] : 1.0f) * a.weight != 0.0f;
+}
+
+__device__ __forceinline__ void share_logits(const DistillArgs& a, int l, int lanes, const Held& h,
+                                             const Entries& en) {
+#pragma unroll
+  for (int u = 0; u < kPerLane; ++u)
+    if (u * lanes + l < a.k) en.z[u * lanes + l] = h.z[u];
 }
 
 // sum_k p_k (log p_k - z_k / T + lse), by the same lanes.
@@ -119,24 +199,22 @@ __device__ __forceinline__ float lesson_of(const DistillArgs& a, int l, int lane
                                            const Entries& en, float lse) {
   float v = 0.0f;
   for (int j = l; j < a.k; j += lanes) {
-    const float p = en.p[j];
+    const float p = en.id[j] < 0 ? 0.0f : __builtin_amdgcn_exp2f(en.lp[j]);
     if (p != 0.0f) v += p * (kLn2 * en.lp[j] - (en.z[j] * a.inv_temp - lse));
   }
   return lanes_sum(v, lanes);
 }
 
-// The gradient at the entries' own places, after the rest of the row is
-// stored: q from `q_of`, less the p of all entries with that id.
-template <typename T, typename F>
+// The gradient at the entries' own places in [lo, hi), after the rest of the
+// row is stored.
+template <typename T>
 __device__ __forceinline__ void store_entries(const DistillArgs& a, int64_t row, int l, int lanes,
-                                              const Entries& en, float c, int32_t lo, int32_t hi,
-                                              F q_of) {
+                                              const Entries& en, float c, float inv, const Soft& t,
+                                              int32_t lo, int32_t hi) {
   for (int j = l; j < a.k; j += lanes) {
     const int32_t id = en.id[j];
     if (id < lo || id >= hi) continue;
-    float p = 0.0f;
-    for (int x = 0; x < a.k; ++x) p += en.id[x] == id ? en.p[x] : 0.0f;
-    const float v[1] = {c * (q_of(en.z[j]) - p)};
+    const float v[1] = {c * (inv * exp_of(en.z[j], t) - en.p[j])};
     row_store<T, 1>(a.dz.p + row * a.dz.stride + id * (int64_t)sizeof(T), v);
   }
 }
@@ -147,6 +225,18 @@ __device__ __forceinline__ void store_entries(const DistillArgs& a, int64_t row,
 // fewer than a piece, go to the first lanes, one each.
 // ---------------------------------------------------------------------------
 enum { kLossOnly = 0, kFused = 1, kBackward = 2 };
+
+// Keeps the row in its own type between the passes over it: unseen by the
+// compiler, which would hold the converted values, twice as large, as well.
+template <typename R, int N>
+__device__ __forceinline__ void keep_packed(R (&raw)[N]) {
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    auto w = __builtin_bit_cast(u32x4, raw[t]);
+    asm volatile("" : "+v"(w));
+    raw[t] = __builtin_bit_cast(R, w);
+  }
+}
 
 template <typename T, int V, int STEPS, bool BLK, int MODE>
 __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArgs a) {
@@ -160,24 +250,27 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
   const int pieces = a.vocab / V, rest = a.vocab - pieces * V;
   const char* zp = a.z.p + row * a.z.stride;
 
+  const int el = BLK ? min(lanes, kWave) : lanes;     // lanes that read the entries
+  const Entries en = entries_at(lds, BLK ? 0 : (int)threadIdx.x >> a.lanes_log, a.k);
+  Held held;
+  if (l < el) load_entries(a, row, l, el, held);
   typename Raw<T, V>::vec raw[STEPS];
 #pragma unroll
   for (int t = 0; t < STEPS; ++t)
     if (t * lanes + l < pieces) raw[t] = raw_load<T, V>(zp + (int64_t)(t * lanes + l) * 16);
   float last[1] = {-INFINITY};
   if (l < rest) row_load<T, 1>(zp + (pieces * V + l) * (int64_t)sizeof(T), last);
-
-  const int el = BLK ? min(lanes, kWave) : lanes;     // lanes that read the entries
-  const Entries en = entries_at(lds, BLK ? 0 : (int)threadIdx.x >> a.lanes_log, a.k);
   bool has = false;
   if (l < el) {
-    has = read_entries<T>(a, row, l, el, en);
+    load_entry_logits<T>(a, row, held);
+    has = share_entries(a, row, l, el, held, en);
     if (BLK && l == 0) s_has = has;
   }
 
-  // Softmax statistics.
-  float top = 0.0f, inv = 0.0f, lse = 0.0f;      // q_j = inv * exp((z_j - top) / T)
-  bool empty = false;
+  // Softmax statistics: q_j = inv * exp_of(z_j, top).
+  Soft top;
+  float inv = 1.0f, lse;
+  bool empty;
   if constexpr (MODE != kBackward) {
     float m = last[0];
 #pragma unroll
@@ -188,35 +281,36 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
 #pragma unroll
         for (int k = 0; k < V; ++k) m = fmaxf(m, v[k]);
       }
-    m = lanes_maxf(m, min(lanes, kWave));
-    top = finite_max(m);
-    float s = exp_of(last[0], top, a.c2);
+    keep_packed(raw);
+    if (l < el) share_logits(a, l, el, held, en);
+    top = soft_of(lanes_maxf(m, min(lanes, kWave)), a.c2);
+    float s = exp_of(last[0], top);
 #pragma unroll
     for (int t = 0; t < STEPS; ++t)
       if (t * lanes + l < pieces) {
         float v[V];
         to_f32<T, V>(raw[t], v);
 #pragma unroll
-        for (int k = 0; k < V; ++k) s += exp_of(v[k], top, a.c2);
+        for (int k = 0; k < V; ++k) s += exp_of(v[k], top);
       }
-    s = lanes_sum(s, min(lanes, kWave));
-    MaxSum all = {m, s};
+    keep_packed(raw);
+    MaxSum all = {top.m, lanes_sum(s, min(lanes, kWave))};
     if constexpr (BLK) {
-      if (lane_id() == 0) s_part[threadIdx.x / kWave] = make_float2(m, s);
+      if (lane_id() == 0) s_part[threadIdx.x / kWave] = make_float2(all.m, all.s);
       __syncthreads();
       all = {s_part[0].x, s_part[0].y};
       for (int w = 1; w < lanes / kWave; ++w) all = join(all, {s_part[w].x, s_part[w].y}, a.c2);
-      top = finite_max(all.m);
+      top = soft_of(all.m, a.c2);
     }
-    // Sums are at least 1, but for a row of which every logit is -infinity.
+    // Sums are about 1 at least, but for a row of which every logit is -infinity.
     empty = all.s == 0.0f;
-    inv = empty ? 0.0f : 1.0f / all.s;
-    lse = all.m * a.inv_temp + (empty ? 0.0f : kLn2 * __builtin_amdgcn_logf(all.s));
+    inv = 1.0f / all.s;
+    lse = lse_of(all, top, a.inv_temp);
   } else {
+    if (l < el) share_logits(a, l, el, held, en);
     lse = a.lse_in[row];
     empty = lse == -INFINITY;
-    top = empty ? 0.0f : lse * a.temp;
-    inv = 1.0f;
+    top = soft_of(lse * a.temp, a.c2);
     if (BLK) __syncthreads();
   }
   if (BLK) has = s_has;
@@ -233,31 +327,34 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
   }
   if constexpr (MODE == kLossOnly) return;
 
-  // The gradient: a row without a lesson gets zeros.
-  const float c = has ? weight * a.temp : 0.0f;
-  const float ci = c * inv;
   char* dp = a.dz.p + row * a.dz.stride;
+  if (!has) {      // the same for the whole row
+    const float zero[V] = {}, one[1] = {0.0f};
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t)
+      if (t * lanes + l < pieces) row_store<T, V>(dp + (int64_t)(t * lanes + l) * 16, zero);
+    if (l < rest) row_store<T, 1>(dp + (pieces * V + l) * (int64_t)sizeof(T), one);
+    return;
+  }
+  const float c = weight * a.temp, ci = c * inv;
 #pragma unroll
   for (int t = 0; t < STEPS; ++t)
     if (t * lanes + l < pieces) {
       float v[V];
       to_f32<T, V>(raw[t], v);
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[k] = has ? ci * exp_of(v[k], top, a.c2) : 0.0f;
+      for (int k = 0; k < V; ++k) v[k] = ci * exp_of(v[k], top);
       row_store<T, V>(dp + (int64_t)(t * lanes + l) * 16, v);
     }
   if (l < rest) {
-    const float v[1] = {has ? ci * exp_of(last[0], top, a.c2) : 0.0f};
+    const float v[1] = {ci * exp_of(last[0], top)};
     row_store<T, 1>(dp + (pieces * V + l) * (int64_t)sizeof(T), v);
   }
-  if (!has) return;      // the same for the whole row
   if constexpr (BLK)
     __syncthreads();
   else
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  if (l < el)
-    store_entries<T>(a, row, l, el, en, c, 0, a.vocab,
-                     [&](float z) { return inv * exp_of(z, top, a.c2); });
+  if (l < el) store_entries<T>(a, row, l, el, en, c, inv, top, 0, a.vocab);
 }
 
 // ---------------------------------------------------------------------------
@@ -292,11 +389,11 @@ __global__ void __launch_bounds__(kBlock) k_distill_stats(DistillArgs a) {
       to_f32<T, V>(raw[u], v);
 #pragma unroll
       for (int k = 0; k < V; ++k) m = fmaxf(m, v[k]);
-      const float top = finite_max(m);
-      st.s *= exp_of(st.m, top, a.c2);
+      const Soft top = soft_of(m, a.c2);
+      st.s *= factor(soft_of(st.m, a.c2), top);
       st.m = m;
 #pragma unroll
-      for (int k = 0; k < V; ++k) st.s += exp_of(v[k], top, a.c2);
+      for (int k = 0; k < V; ++k) st.s += exp_of(v[k], top);
     }
   }
   if (c == a.splits - 1 && tid < rest) {
@@ -311,7 +408,11 @@ __global__ void __launch_bounds__(kBlock) k_distill_stats(DistillArgs a) {
   // gradient may take its place).
   if (c == 0 && tid < kWave) {
     const Entries en = entries_at(lds, 0, a.k);
-    const bool has = read_entries<T>(a, row, tid, kWave, en);
+    Held held;
+    load_entries(a, row, tid, kWave, held);
+    load_entry_logits<T>(a, row, held);
+    const bool has = share_entries(a, row, tid, kWave, held, en);
+    share_logits(a, tid, kWave, held, en);
     const float v = lesson_of(a, tid, kWave, en, 0.0f);
     if (tid == 0) a.lesson[row] = has ? v : 0.0f;
   }
@@ -331,7 +432,11 @@ __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
   const int c = (int)(block_index() - row * a.splits);
   if (row >= a.n || (MODE == kLossOnly && c > 0)) return;
   const int tid = threadIdx.x;
-  float top, inv, lse;      // q_j = inv * exp((z_j - top) / T)
+  const Entries en = entries_at(lds, 0, a.k);
+  Held held;
+  if (tid < kWave) load_entries(a, row, tid, kWave, held);
+  Soft top;                // q_j = inv * exp_of(z_j, top)
+  float inv = 1.0f, lse;
   bool empty;
   if constexpr (MODE != kBackward) {
     // Every wave joins all parts of the row.
@@ -343,18 +448,18 @@ __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
     for (int o = kWave / 2; o >= 1; o >>= 1)
       st = join(st, {__shfl_xor(st.m, o, kWave), __shfl_xor(st.s, o, kWave)}, a.c2);
     empty = st.s == 0.0f;
-    top = finite_max(st.m);
-    inv = empty ? 0.0f : 1.0f / st.s;
-    lse = st.m * a.inv_temp + (empty ? 0.0f : kLn2 * __builtin_amdgcn_logf(st.s));
+    top = soft_of(st.m, a.c2);
+    inv = 1.0f / st.s;
+    lse = lse_of(st, top, a.inv_temp);
   } else {
     lse = a.lse_in[row];
     empty = lse == -INFINITY;
-    top = empty ? 0.0f : lse * a.temp;
-    inv = 1.0f;
+    top = soft_of(lse * a.temp, a.c2);
   }
-  const Entries en = entries_at(lds, 0, a.k);
   if (tid < kWave) {
-    const bool has = read_entries<T>(a, row, tid, kWave, en);
+    load_entry_logits<T>(a, row, held);
+    const bool has = share_entries(a, row, tid, kWave, held, en);
+    share_logits(a, tid, kWave, held, en);
     if (tid == 0) s_has = has;
   }
   __syncthreads();
@@ -370,8 +475,7 @@ __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
   const int p0 = c * a.chunk, p1 = min(pieces, p0 + a.chunk);
   const char* zp = a.z.p + row * a.z.stride;
   char* dp = a.dz.p + row * a.dz.stride;
-  const float scale = has ? weight * a.temp : 0.0f;
-  const float ci = scale * inv;
+  const float scale = weight * a.temp, ci = scale * inv;
   for (int p = p0 + tid; p < p1; p += kBlock * kSplitUnroll) {
     typename Raw<T, V>::vec raw[kSplitUnroll];
 #pragma unroll
@@ -385,7 +489,7 @@ __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
       float v[V];
       to_f32<T, V>(raw[u], v);
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[k] = has ? ci * exp_of(v[k], top, a.c2) : 0.0f;
+      for (int k = 0; k < V; ++k) v[k] = has ? ci * exp_of(v[k], top) : 0.0f;
       row_store<T, V>(dp + (int64_t)(p + u * kBlock) * 16, v);
     }
   }
@@ -393,14 +497,13 @@ __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
   if (end && tid < rest) {
     float v[1];
     row_load<T, 1>(zp + (pieces * V + tid) * (int64_t)sizeof(T), v);
-    v[0] = has ? ci * exp_of(v[0], top, a.c2) : 0.0f;
+    v[0] = has ? ci * exp_of(v[0], top) : 0.0f;
     row_store<T, 1>(dp + (pieces * V + tid) * (int64_t)sizeof(T), v);
   }
   if (!has) return;
   __syncthreads();
   if (tid < kWave)
-    store_entries<T>(a, row, tid, kWave, en, scale, p0 * V, end ? a.vocab : p1 * V,
-                     [&](float z) { return inv * exp_of(z, top, a.c2); });
+    store_entries<T>(a, row, tid, kWave, en, scale, inv, top, p0 * V, end ? a.vocab : p1 * V);
 }
 
 // ---------------------------------------------------------------------------
@@ -450,9 +553,7 @@ int launch_rows(DistillArgs& a, hipStream_t stream) {
   }
   if (pieces <= kWave * kWaveSteps) {
     a.lanes_log = 4;
-    // (at most 32 KB of entries per block)
-    while (a.lanes_log < 6 && ((1 << a.lanes_log) < pieces ||
-                               (kBlock >> a.lanes_log) * a.k * kEntryBytes > 32768))
+    while (a.lanes_log < 6 && ((1 << a.lanes_log) < pieces || kPerLane << a.lanes_log < a.k))
       ++a.lanes_log;
     const int steps = (int)cdiv(pieces, 1 << a.lanes_log);
     const dim3 grid = grid_of(cdiv(a.n << a.lanes_log, kBlock));
@@ -490,7 +591,7 @@ int pack_args(const gg_rows_t* z, int64_t n, int64_t vocab, const void* top_ids_
   GG_REQUIRE(vocab >= 1 && vocab <= GG_DISTILL_MAX_VOCAB, "vocab %lld outside 1..%d",
              (long long)vocab, GG_DISTILL_MAX_VOCAB);
   GG_REQUIRE(k >= 1 && k <= GG_DISTILL_MAX_K, "k = %d outside 1..%d", k, GG_DISTILL_MAX_K);
-  GG_REQUIRE(temperature > 0.0f && temperature <= 3.0e38f, "temperature must be positive and finite");
+  GG_REQUIRE(temperature >= 1e-30f && temperature <= 1e30f, "temperature outside 1e-30 .. 1e30");
   int rc = pack_rows(z, "z", n, vocab, kBitFloats, false, &a->z);
   if (rc == GG_OK) rc = pack_rows(top, "top", n, k, kBitFloats, false, &a->top);
   if (rc == GG_OK && dz) rc = pack_rows(dz, "dz", n, vocab, 1u << z->dtype, true, &a->dz);
