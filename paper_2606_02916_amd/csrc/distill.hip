@@ -31,7 +31,7 @@ struct DistillArgs {
   int32_t splits;              // blocks of a row
   int32_t chunk;               // pieces of a split
   float2* part;                // [n][splits]: maximum of z, sum of exp((z - maximum) / T)
-  float* lesson;               // [n]: sum p (log p - z / T)
+  float2* lesson;              // [n]: sum p (log p - z / T); whether the row has a lesson
   int32_t* status;
 };
 
@@ -67,6 +67,15 @@ __device__ __forceinline__ float factor(const Soft& a, const Soft& t) {
   return a.coarse || t.coarse || a.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(a.b - t.b);
 }
 
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+  for (int o = lanes / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, kWave);
+  return v;
+}
+__device__ __forceinline__ float lanes_maxf(float v, int lanes) {
+  for (int o = lanes / 2; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));
+  return v;
+}
+
 struct MaxSum {
   float m, s;     // largest logit; sum of exp((z - m) / T)
 };
@@ -76,18 +85,24 @@ __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float c2) {
   return {t.m, a.s * factor(soft_of(a.m, c2), t) + b.s * factor(soft_of(b.m, c2), t)};
 }
 
+// The statistics of `lanes` lanes, or of a block's waves, relative to their
+// common maximum.
+__device__ __forceinline__ MaxSum join_lanes(MaxSum st, int lanes, float c2) {
+  const Soft t = soft_of(lanes_maxf(st.m, lanes), c2);
+  return {t.m, lanes_sum(st.s * factor(soft_of(st.m, c2), t), lanes)};
+}
+
+__device__ __forceinline__ MaxSum join_waves(const float2* part, int waves, float c2) {
+  float m = part[0].x, s = 0.0f;
+  for (int w = 1; w < waves; ++w) m = fmaxf(m, part[w].x);
+  const Soft t = soft_of(m, c2);
+  for (int w = 0; w < waves; ++w) s += part[w].y * factor(soft_of(part[w].x, c2), t);
+  return {m, s};
+}
+
 __device__ __forceinline__ float lse_of(const MaxSum& st, const Soft& t, float inv_temp) {
   const float l2 = __builtin_amdgcn_logf(st.s);       // -infinity for a row of none
   return t.coarse ? t.m * inv_temp + kLn2 * l2 : kLn2 * (t.b + l2);
-}
-
-__device__ __forceinline__ float lanes_sum(float v, int lanes) {
-  for (int o = lanes / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, kWave);
-  return v;
-}
-__device__ __forceinline__ float lanes_maxf(float v, int lanes) {
-  for (int o = lanes / 2; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));
-  return v;
 }
 
 // ---------------------------------------------------------------------------
@@ -151,7 +166,9 @@ __device__ __forceinline__ void load_entry_logits(const DistillArgs& a, int64_t 
   }
 }
 
-// Whether the row has a lesson: an entry with a logit above -infinity, and a weight.
+// Whether the row has a lesson: an entry with a logit above -infinity, and a
+// weight.  SUM: p is summed over equal ids (for the gradient).
+template <bool SUM>
 __device__ __forceinline__ bool share_entries(const DistillArgs& a, int64_t row, int l, int lanes,
                                               const Held& h, const Entries& en) {
   float tm = h.t[0];
@@ -172,18 +189,20 @@ __device__ __forceinline__ bool share_entries(const DistillArgs& a, int64_t row,
       en.p[j] = __builtin_amdgcn_exp2f(lp);
     }
   }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  float p[kPerLane] = {};
-  for (int x = 0; x < a.k; ++x) {
-    const int32_t id = en.id[x];
-    const float px = en.p[x];
+  if constexpr (SUM) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    float p[kPerLane] = {};
+    for (int x = 0; x < a.k; ++x) {
+      const int32_t id = en.id[x];
+      const float px = en.p[x];
 #pragma unroll
-    for (int u = 0; u < kPerLane; ++u) p[u] += h.id[u] == id ? px : 0.0f;
+      for (int u = 0; u < kPerLane; ++u) p[u] += h.id[u] == id ? px : 0.0f;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int u = 0; u < kPerLane; ++u)
+      if (u * lanes + l < a.k) en.p[u * lanes + l] = p[u];
   }
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
-  for (int u = 0; u < kPerLane; ++u)
-    if (u * lanes + l < a.k) en.p[u * lanes + l] = p[u];
   return f.m != -INFINITY && (a.row_w ? a.row_w[row] : 1.0f) * a.weight != 0.0f;
 }
 
@@ -263,7 +282,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
   bool has = false;
   if (l < el) {
     load_entry_logits<T>(a, row, held);
-    has = share_entries(a, row, l, el, held, en);
+    has = share_entries<MODE != kLossOnly>(a, row, l, el, held, en);
     if (BLK && l == 0) s_has = has;
   }
 
@@ -298,8 +317,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
     if constexpr (BLK) {
       if (lane_id() == 0) s_part[threadIdx.x / kWave] = make_float2(all.m, all.s);
       __syncthreads();
-      all = {s_part[0].x, s_part[0].y};
-      for (int w = 1; w < lanes / kWave; ++w) all = join(all, {s_part[w].x, s_part[w].y}, a.c2);
+      all = join_waves(s_part, lanes / kWave, a.c2);
       top = soft_of(all.m, a.c2);
     }
     // Sums are about 1 at least, but for a row of which every logit is -infinity.
@@ -363,37 +381,65 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
 // ---------------------------------------------------------------------------
 constexpr int kSplitUnroll = 4;
 
+// A block's pieces from p on, kSplitUnroll per lane; those past p1 repeat the first.
+template <typename T, int V>
+__device__ __forceinline__ void load_batch(const char* zp, int p, int p1,
+                                           typename Raw<T, V>::vec (&raw)[kSplitUnroll]) {
+#pragma unroll
+  for (int u = 0; u < kSplitUnroll; ++u) {
+    const int q = p + u * kBlock;
+    raw[u] = raw_load<T, V>(zp + (int64_t)(q < p1 ? q : p) * 16);
+  }
+}
+
+// Statistics of one split of a row; the last block of a row has its lesson
+// instead, as far as it needs no statistics and while z is still whole (the
+// gradient may take its place).
 template <typename T, int V>
 __global__ void __launch_bounds__(kBlock) k_distill_stats(DistillArgs a) {
   extern __shared__ char lds[];
   __shared__ float2 s_part[kBlock / kWave];
-  const int64_t row = block_index() / a.splits;
-  const int c = (int)(block_index() - row * a.splits);
+  const int64_t row = block_index() / (a.splits + 1);
+  const int c = (int)(block_index() - row * (a.splits + 1));
   if (row >= a.n) return;
+  const int tid = threadIdx.x;
+  if (c == a.splits) {
+    if (tid >= kWave) return;
+    const Entries en = entries_at(lds, 0, a.k);
+    Held held;
+    load_entries(a, row, tid, kWave, held);
+    load_entry_logits<T>(a, row, held);
+    const bool has = share_entries<false>(a, row, tid, kWave, held, en);
+    share_logits(a, tid, kWave, held, en);
+    const float v = lesson_of(a, tid, kWave, en, 0.0f);
+    if (tid == 0) a.lesson[row] = make_float2(v, has ? 1.0f : 0.0f);
+    return;
+  }
   const int pieces = a.vocab / V, rest = a.vocab - pieces * V;
   const int p0 = c * a.chunk, p1 = min(pieces, p0 + a.chunk);
   const char* zp = a.z.p + row * a.z.stride;
-  const int tid = threadIdx.x;
   MaxSum st = {-INFINITY, 0.0f};
   for (int p = p0 + tid; p < p1; p += kBlock * kSplitUnroll) {
     typename Raw<T, V>::vec raw[kSplitUnroll];
+    load_batch<T, V>(zp, p, p1, raw);
+    // (the repeated pieces do not change the maximum)
+    float v[V], m = st.m;
 #pragma unroll
     for (int u = 0; u < kSplitUnroll; ++u) {
-      const int q = p + u * kBlock;
-      raw[u] = raw_load<T, V>(zp + (int64_t)(q < p1 ? q : p) * 16);
-    }
-#pragma unroll
-    for (int u = 0; u < kSplitUnroll; ++u) {
-      if (p + u * kBlock >= p1) break;
-      float v[V], m = st.m;
       to_f32<T, V>(raw[u], v);
 #pragma unroll
       for (int k = 0; k < V; ++k) m = fmaxf(m, v[k]);
-      const Soft top = soft_of(m, a.c2);
-      st.s *= factor(soft_of(st.m, a.c2), top);
-      st.m = m;
+    }
+    const Soft top = soft_of(m, a.c2);
+    st.s *= factor(soft_of(st.m, a.c2), top);
+    st.m = m;
 #pragma unroll
-      for (int k = 0; k < V; ++k) st.s += exp_of(v[k], top);
+    for (int u = 0; u < kSplitUnroll; ++u) {
+      to_f32<T, V>(raw[u], v);
+      float s = 0.0f;
+#pragma unroll
+      for (int k = 0; k < V; ++k) s += exp_of(v[k], top);
+      st.s += p + u * kBlock < p1 ? s : 0.0f;
     }
   }
   if (c == a.splits - 1 && tid < rest) {
@@ -401,27 +447,41 @@ __global__ void __launch_bounds__(kBlock) k_distill_stats(DistillArgs a) {
     row_load<T, 1>(zp + (pieces * V + tid) * (int64_t)sizeof(T), v);
     st = join(st, {v[0], v[0] == -INFINITY ? 0.0f : v[0] - v[0] + 1.0f}, a.c2);
   }
-  for (int o = kWave / 2; o >= 1; o >>= 1)
-    st = join(st, {__shfl_xor(st.m, o, kWave), __shfl_xor(st.s, o, kWave)}, a.c2);
+  st = join_lanes(st, kWave, a.c2);
   if (lane_id() == 0) s_part[tid / kWave] = make_float2(st.m, st.s);
-  // The lesson's part that needs no statistics, while z is still whole (the
-  // gradient may take its place).
-  if (c == 0 && tid < kWave) {
-    const Entries en = entries_at(lds, 0, a.k);
-    Held held;
-    load_entries(a, row, tid, kWave, held);
-    load_entry_logits<T>(a, row, held);
-    const bool has = share_entries(a, row, tid, kWave, held, en);
-    share_logits(a, tid, kWave, held, en);
-    const float v = lesson_of(a, tid, kWave, en, 0.0f);
-    if (tid == 0) a.lesson[row] = has ? v : 0.0f;
-  }
   __syncthreads();
   if (tid == 0) {
-    st = {s_part[0].x, s_part[0].y};
-    for (int w = 1; w < kBlock / kWave; ++w) st = join(st, {s_part[w].x, s_part[w].y}, a.c2);
+    st = join_waves(s_part, kBlock / kWave, a.c2);
     a.part[row * a.splits + c] = make_float2(st.m, st.s);
   }
+}
+
+// All parts of a row joined, by every wave that calls it.
+__device__ __forceinline__ MaxSum row_stats(const DistillArgs& a, int64_t row) {
+  MaxSum st = {-INFINITY, 0.0f};
+  for (int x = lane_id(); x < a.splits; x += kWave) {
+    const float2 v = a.part[row * a.splits + x];
+    st = join(st, {v.x, v.y}, a.c2);
+  }
+  return join_lanes(st, kWave, a.c2);
+}
+
+__device__ __forceinline__ void store_loss(const DistillArgs& a, int64_t row, float2 lesson,
+                                           bool empty, float lse) {
+  const float weight = a.weight * (a.row_w ? a.row_w[row] : 1.0f);
+  a.loss[row] =
+      lesson.y != 0.0f && !empty ? weight * a.temp * a.temp * (lesson.x + lse) : 0.0f;
+  if (a.lse) a.lse[row] = lse;
+}
+
+// The loss alone: a wave per row.
+__global__ void __launch_bounds__(kWave) k_distill_loss(DistillArgs a) {
+  const int64_t row = block_index();
+  if (row >= a.n) return;
+  const float2 lesson = a.lesson[row];
+  const MaxSum st = row_stats(a, row);
+  if (threadIdx.x == 0)
+    store_loss(a, row, lesson, st.s == 0.0f, lse_of(st, soft_of(st.m, a.c2), a.inv_temp));
 }
 
 template <typename T, int V, int MODE>
@@ -430,68 +490,53 @@ __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
   __shared__ int32_t s_has;
   const int64_t row = block_index() / a.splits;
   const int c = (int)(block_index() - row * a.splits);
-  if (row >= a.n || (MODE == kLossOnly && c > 0)) return;
+  if (row >= a.n) return;
   const int tid = threadIdx.x;
+  const int pieces = a.vocab / V, rest = a.vocab - pieces * V;
+  const int p0 = c * a.chunk, p1 = min(pieces, p0 + a.chunk);
+  const char* zp = a.z.p + row * a.z.stride;
+  char* dp = a.dz.p + row * a.dz.stride;
   const Entries en = entries_at(lds, 0, a.k);
   Held held;
   if (tid < kWave) load_entries(a, row, tid, kWave, held);
+  typename Raw<T, V>::vec raw[kSplitUnroll];
+  int p = p0 + tid;
+  if (p < p1) load_batch<T, V>(zp, p, p1, raw);
   Soft top;                // q_j = inv * exp_of(z_j, top)
-  float inv = 1.0f, lse;
+  float inv = 1.0f;
   bool empty;
-  if constexpr (MODE != kBackward) {
-    // Every wave joins all parts of the row.
-    MaxSum st = {-INFINITY, 0.0f};
-    for (int x = lane_id(); x < a.splits; x += kWave) {
-      const float2 v = a.part[row * a.splits + x];
-      st = join(st, {v.x, v.y}, a.c2);
-    }
-    for (int o = kWave / 2; o >= 1; o >>= 1)
-      st = join(st, {__shfl_xor(st.m, o, kWave), __shfl_xor(st.s, o, kWave)}, a.c2);
+  if constexpr (MODE == kFused) {
+    const MaxSum st = row_stats(a, row);
     empty = st.s == 0.0f;
     top = soft_of(st.m, a.c2);
     inv = 1.0f / st.s;
-    lse = lse_of(st, top, a.inv_temp);
+    if (c == 0 && tid == 0)
+      store_loss(a, row, a.lesson[row], empty, lse_of(st, top, a.inv_temp));
   } else {
-    lse = a.lse_in[row];
+    const float lse = a.lse_in[row];
     empty = lse == -INFINITY;
     top = soft_of(lse * a.temp, a.c2);
   }
   if (tid < kWave) {
     load_entry_logits<T>(a, row, held);
-    const bool has = share_entries(a, row, tid, kWave, held, en);
+    const bool has = share_entries<true>(a, row, tid, kWave, held, en);
     share_logits(a, tid, kWave, held, en);
     if (tid == 0) s_has = has;
   }
-  __syncthreads();
+  __syncthreads();         // and the entries' logits are read before any is overwritten
   const bool has = s_has && !empty;
-  const float weight = a.weight * (a.row_w ? a.row_w[row] : 1.0f);
-  if (MODE != kBackward && c == 0 && tid == 0) {
-    a.loss[row] = has ? weight * a.temp * a.temp * (a.lesson[row] + lse) : 0.0f;
-    if (a.lse) a.lse[row] = lse;
-  }
-  if constexpr (MODE == kLossOnly) return;
-
-  const int pieces = a.vocab / V, rest = a.vocab - pieces * V;
-  const int p0 = c * a.chunk, p1 = min(pieces, p0 + a.chunk);
-  const char* zp = a.z.p + row * a.z.stride;
-  char* dp = a.dz.p + row * a.dz.stride;
-  const float scale = weight * a.temp, ci = scale * inv;
-  for (int p = p0 + tid; p < p1; p += kBlock * kSplitUnroll) {
-    typename Raw<T, V>::vec raw[kSplitUnroll];
+  const float scale = a.weight * (a.row_w ? a.row_w[row] : 1.0f) * a.temp, ci = scale * inv;
+  while (p < p1) {
 #pragma unroll
     for (int u = 0; u < kSplitUnroll; ++u) {
-      const int q = p + u * kBlock;
-      raw[u] = raw_load<T, V>(zp + (int64_t)(q < p1 ? q : p) * 16);
-    }
-#pragma unroll
-    for (int u = 0; u < kSplitUnroll; ++u) {
-      if (p + u * kBlock >= p1) break;
       float v[V];
       to_f32<T, V>(raw[u], v);
 #pragma unroll
       for (int k = 0; k < V; ++k) v[k] = has ? ci * exp_of(v[k], top) : 0.0f;
-      row_store<T, V>(dp + (int64_t)(p + u * kBlock) * 16, v);
+      if (p + u * kBlock < p1) row_store<T, V>(dp + (int64_t)(p + u * kBlock) * 16, v);
     }
+    p += kBlock * kSplitUnroll;
+    if (p < p1) load_batch<T, V>(zp, p, p1, raw);
   }
   const bool end = c == a.splits - 1;
   if (end && tid < rest) {
@@ -521,14 +566,14 @@ int split_count(int64_t n) {
 
 struct DistillWs {
   float2* part;
-  float* lesson;
+  float2* lesson;
 };
 
 size_t distill_ws_layout(int64_t n, char* base, DistillWs* out) {
   Carve c{base, 0, 0};
   DistillWs w;
   w.part = c.take<float2>((size_t)n * split_count(n));
-  w.lesson = c.take<float>((size_t)n);
+  w.lesson = c.take<float2>((size_t)n);
   if (out) *out = w;
   return align_up(c.used, 256);
 }
@@ -542,13 +587,19 @@ int launch_rows(DistillArgs& a, hipStream_t stream) {
     a.splits = split_count(a.n);
     a.chunk = (int)cdiv(pieces, a.splits);
     const size_t lds = (size_t)a.k * kEntryBytes;
-    const dim3 grid = grid_of(a.n * a.splits);
     if (MODE != kBackward) {
-      hipLaunchKernelGGL((k_distill_stats<T, V>), grid, dim3(kBlock), lds, stream, a);
+      hipLaunchKernelGGL((k_distill_stats<T, V>), grid_of(a.n * (a.splits + 1)), dim3(kBlock), lds,
+                         stream, a);
       GG_LAUNCH_CHECK("k_distill_stats");
     }
-    hipLaunchKernelGGL((k_distill_finish<T, V, MODE>), grid, dim3(kBlock), lds, stream, a);
-    GG_LAUNCH_CHECK("k_distill_finish");
+    if constexpr (MODE == kLossOnly) {
+      hipLaunchKernelGGL(k_distill_loss, grid_of(a.n), dim3(kWave), 0, stream, a);
+      GG_LAUNCH_CHECK("k_distill_loss");
+    } else {
+      hipLaunchKernelGGL((k_distill_finish<T, V, MODE>), grid_of(a.n * a.splits), dim3(kBlock), lds,
+                         stream, a);
+      GG_LAUNCH_CHECK("k_distill_finish");
+    }
     return GG_OK;
   }
   if (pieces <= kWave * kWaveSteps) {

@@ -199,9 +199,15 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+# The current stream's handle without a torch.cuda.Stream around it: making
+# one costs as much as a small launch (3 us).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream):
     if stream is None:
-        import torch
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
 
