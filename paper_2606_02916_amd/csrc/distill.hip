@@ -67,15 +67,6 @@ __device__ __forceinline__ float factor(const Soft& a, const Soft& t) {
   return a.coarse || t.coarse || a.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(a.b - t.b);
 }
 
-__device__ __forceinline__ float lanes_sum(float v, int lanes) {
-  for (int o = lanes / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, kWave);
-  return v;
-}
-__device__ __forceinline__ float lanes_maxf(float v, int lanes) {
-  for (int o = lanes / 2; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, kWave));
-  return v;
-}
-
 struct MaxSum {
   float m, s;     // largest logit; sum of exp((z - m) / T)
 };

@@ -26,7 +26,7 @@ struct NormArgs {
 template <bool BLK>
 __device__ __forceinline__ float group_sum(float v, int lanes, float* lds) {
   if constexpr (BLK) {
-    v = wave_sum(v);
+    v = lanes_sum(v, kWave);
     __syncthreads();
     if (lane_id() == 0) lds[threadIdx.x / kWave] = v;
     __syncthreads();
@@ -35,14 +35,35 @@ __device__ __forceinline__ float group_sum(float v, int lanes, float* lds) {
     for (int i = 0; i < waves; ++i) t += lds[i];
     return t;
   } else {
-    for (int o = lanes / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, kWave);
-    return v;
+    return lanes_sum(v, lanes);
   }
 }
 
-// Maximum of magnitudes as bits: a NaN is more than every number.
-__device__ __forceinline__ uint32_t lanes_max(uint32_t m, int lanes) {
-  for (int o = lanes / 2; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, kWave));
+// Sum of squares, and largest magnitude, of a piece's own elements: only a
+// row's last piece has others (skip > 0).
+template <int V>
+__device__ __forceinline__ float squares(const float (&v)[V], int32_t skip) {
+  float s = 0.0f;
+  if (skip == 0) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) s += v[k] * v[k];
+  } else {
+#pragma unroll
+    for (int k = 0; k < V; ++k) s += k >= skip ? v[k] * v[k] : 0.0f;
+  }
+  return s;
+}
+
+template <int V>
+__device__ __forceinline__ uint32_t magnitude(const float (&v)[V], int32_t skip) {
+  uint32_t m = 0;
+  if (skip == 0) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) m = max(m, __float_as_uint(v[k]) & 0x7fffffffu);
+  } else {
+#pragma unroll
+    for (int k = 0; k < V; ++k) m = max(m, k >= skip ? __float_as_uint(v[k]) & 0x7fffffffu : 0u);
+  }
   return m;
 }
 
@@ -91,8 +112,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
         for (int k = 0; k < V; ++k) s[t][k] += r[k];
       }
       load_weight<T, V>(a.w, a.w_f32, e, w[t]);
-#pragma unroll
-      for (int k = 0; k < V; ++k) sq += k >= skip ? s[t][k] * s[t][k] : 0.0f;
+      sq += squares<V>(s[t], skip);
     }
   }
   sq = group_sum<BLK>(sq, lanes, lds);
@@ -117,11 +137,9 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
   uint32_t top[STEPS], all = 0;
 #pragma unroll
   for (int t = 0; t < STEPS; ++t) {
-    const int32_t skip = max(0, (t * lanes + l) * V - (a.dim - V));
     top[t] = 0;
-#pragma unroll
-    for (int k = 0; k < V; ++k)
-      top[t] = max(top[t], k >= skip ? __float_as_uint(s[t][k]) & 0x7fffffffu : 0u);
+    if (t * lanes + l < a.pieces)
+      top[t] = magnitude<V>(s[t], max(0, (t * lanes + l) * V - (a.dim - V)));
     all = max(all, top[t]);
   }
   const bool per_row = a.group_lanes_log < 0;
@@ -139,9 +157,11 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
     const int p = t * lanes + l;
     const uint32_t m = per_row ? all : lanes_max(top[t], 1 << a.group_lanes_log);
     if (p >= a.pieces) continue;
-    float scale = __uint_as_float(m) / kE4M3Max;
+    float scale = __uint_as_float(m) * (1.0f / kE4M3Max);
     scale = scale < kScaleMin ? kScaleMin : scale;   // a NaN stays
-    const float inv = 1.0f / scale;
+    // (one unit off at most: a value that close to two codes' middle may round
+    // either way)
+    const float inv = __builtin_amdgcn_rcpf(scale);
     const bool first = per_row ? p == 0 : (p & ((1 << a.group_lanes_log) - 1)) == 0;
     if (first)
       ((float*)(a.q.scales + row * a.q.sstride))[per_row ? 0 : (p * V) >> a.group_log] = scale;
@@ -288,7 +308,7 @@ __global__ void __launch_bounds__(kSumWaves * kWave) k_norm_dw(const float* part
 // ---------------------------------------------------------------------------
 struct Shape {
   bool blk;
-  int32_t pieces, lanes_log, steps;   // steps: 1, 2 or 4
+  int32_t pieces, lanes_log, steps;   // steps: 1 .. 4
   int threads;
 };
 
@@ -307,8 +327,7 @@ Shape shape_of(int32_t dim, int vec, int wave_steps, int blk_steps) {
     while (s.threads < 1024 && s.threads * blk_steps < s.pieces) s.threads *= 2;
     lanes = s.threads;
   }
-  s.steps = 1;
-  while (s.steps * lanes < s.pieces) s.steps *= 2;
+  s.steps = (int32_t)cdiv(s.pieces, lanes);
   return s;
 }
 
@@ -329,6 +348,8 @@ Shape shape_of(int32_t dim, int vec, int wave_steps, int blk_steps) {
         hipLaunchKernelGGL((K<T, R, V, 1, false>), grid, threads, 0, stream, a);                \
       else if (MW == 2 || (S).steps == 2)                                                       \
         hipLaunchKernelGGL((K<T, R, V, 2, false>), grid, threads, 0, stream, a);                \
+      else if ((S).steps == 3)                                                                  \
+        hipLaunchKernelGGL((K<T, R, V, (MW > 2 ? 3 : 2), false>), grid, threads, 0, stream, a); \
       else                                                                                      \
         hipLaunchKernelGGL((K<T, R, V, (MW > 2 ? MW : 2), false>), grid, threads, 0, stream, a); \
     }                                                                                           \

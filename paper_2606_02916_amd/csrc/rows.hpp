@@ -145,6 +145,41 @@ __device__ __forceinline__ int32_t piece_start(int32_t p, int32_t dim, int32_t* 
   return e;
 }
 
+// Reductions over groups of `lanes` lanes of a wave (a power of two), the
+// result in every lane: neighbours by DPP, which costs an operand, up to 16
+// lanes, shuffles beyond.  Every lane of a group must call it.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(v), CTRL, 0xf, 0xf,
+                                                            true));
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, CTRL, 0xf, 0xf, true);
+}
+
+template <typename T, typename F>
+__device__ __forceinline__ T lanes_reduce(T v, int lanes, F f) {
+  if (lanes >= 2) v = f(v, dpp<0xB1>(v));      // quad_perm 1,0,3,2
+  if (lanes >= 4) v = f(v, dpp<0x4E>(v));      // quad_perm 2,3,0,1
+  if (lanes >= 8) v = f(v, dpp<0x141>(v));     // row_half_mirror: the other quad
+  if (lanes >= 16) v = f(v, dpp<0x140>(v));    // row_mirror: the other eight
+  if (lanes >= 32) v = f(v, __shfl_xor(v, 16, kWave));
+  if (lanes >= 64) v = f(v, __shfl_xor(v, 32, kWave));
+  return v;
+}
+
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+  return lanes_reduce(v, lanes, [](float x, float y) { return x + y; });
+}
+__device__ __forceinline__ float lanes_maxf(float v, int lanes) {
+  return lanes_reduce(v, lanes, [](float x, float y) { return fmaxf(x, y); });
+}
+// Of magnitudes as bits: a NaN is more than every number.
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v, int lanes) {
+  return lanes_reduce(v, lanes, [](uint32_t x, uint32_t y) { return max(x, y); });
+}
+
 // A launch of `blocks` blocks: one dimension holds fewer than 2^32 lanes.
 constexpr int64_t kGridX = 1 << 21;
 
