@@ -27,6 +27,7 @@ struct DistillArgs {
   float* loss;
   float* lse;
   const float* lse_in;         // backward: as the forward call wrote it
+  bool past;                   // the gradient goes past the caches
   int32_t lanes_log;
   int32_t splits;              // blocks of a row
   int32_t chunk;               // pieces of a split
@@ -85,8 +86,10 @@ __device__ __forceinline__ MaxSum join_lanes(MaxSum st, int lanes, float c2) {
 
 __device__ __forceinline__ MaxSum join_waves(const float2* part, int waves, float c2) {
   float m = part[0].x, s = 0.0f;
+#pragma unroll 1
   for (int w = 1; w < waves; ++w) m = fmaxf(m, part[w].x);
   const Soft t = soft_of(m, c2);
+#pragma unroll 1
   for (int w = 0; w < waves; ++w) s += part[w].y * factor(soft_of(part[w].x, c2), t);
   return {m, s};
 }
@@ -298,12 +301,13 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
 #pragma unroll
     for (int t = 0; t < STEPS; ++t)
       if (t * lanes + l < pieces) {
-        float v[V];
+        float v[V], sum = 0.0f;
         to_f32<T, V>(raw[t], v);
 #pragma unroll
-        for (int k = 0; k < V; ++k) s += exp_of(v[k], top);
+        for (int k = 0; k < V; ++k) sum += exp_of(v[k], top);
+        s += sum;
       }
-    keep_packed(raw);
+    if constexpr (MODE == kFused) keep_packed(raw);
     MaxSum all = {top.m, lanes_sum(s, min(lanes, kWave))};
     if constexpr (BLK) {
       if (lane_id() == 0) s_part[threadIdx.x / kWave] = make_float2(all.m, all.s);
@@ -353,7 +357,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
       to_f32<T, V>(raw[t], v);
 #pragma unroll
       for (int k = 0; k < V; ++k) v[k] = ci * exp_of(v[k], top);
-      row_store<T, V>(dp + (int64_t)(t * lanes + l) * 16, v);
+      row_store<T, V>(dp + (int64_t)(t * lanes + l) * 16, v, a.past);
     }
   if (l < rest) {
     const float v[1] = {ci * exp_of(last[0], top)};
@@ -524,7 +528,7 @@ __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
       to_f32<T, V>(raw[u], v);
 #pragma unroll
       for (int k = 0; k < V; ++k) v[k] = has ? ci * exp_of(v[k], top) : 0.0f;
-      if (p + u * kBlock < p1) row_store<T, V>(dp + (int64_t)(p + u * kBlock) * 16, v);
+      if (p + u * kBlock < p1) row_store<T, V>(dp + (int64_t)(p + u * kBlock) * 16, v, a.past);
     }
     p += kBlock * kSplitUnroll;
     if (p < p1) load_batch<T, V>(zp, p, p1, raw);
@@ -573,6 +577,7 @@ template <typename T, int MODE>
 int launch_rows(DistillArgs& a, hipStream_t stream) {
   constexpr int V = kVec<T>;
   const int pieces = a.vocab / V;
+  a.past = (int64_t)sizeof(T) * a.n * a.vocab > kStreamBytes;
   const bool split = pieces > 1024 * kMaxSteps || (a.n < kFewRows && pieces >= kSplitPieces);
   if (split) {
     a.splits = split_count(a.n);
@@ -610,6 +615,9 @@ int launch_rows(DistillArgs& a, hipStream_t stream) {
     int threads = 256;
     while (threads < 1024 && threads * kMaxSteps < pieces) threads *= 2;
     const int steps = (int)cdiv(pieces, threads);
+    // (a block that fills its CU waits for its own stores: 4,096 rows of 128,000
+    // bf16 411 us past the caches, 403 through them; of 32,000 97 and 108)
+    a.past = a.past && threads < 1024;
     const dim3 grid = grid_of(a.n);
     const size_t lds = (size_t)a.k * kEntryBytes;
     if (steps <= 2)

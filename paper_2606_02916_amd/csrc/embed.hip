@@ -25,6 +25,7 @@ struct LookupArgs {
   int64_t rows, n;
   float scale;
   uint32_t pieces, pmagic;
+  bool stream;        // the output goes past the caches
   int32_t glog;       // log2 of the elements per scale; 31: one scale per row
   int32_t* status;
 };
@@ -79,7 +80,8 @@ __global__ void __launch_bounds__(kBlock) k_embed_rows(LookupArgs a) {
 #pragma unroll
     for (int k = 0; k < V; ++k)
       v[k] *= sizeof(TI) == 1 && ((e[j] ^ (e[j] + k)) >> a.glog) ? mul2[j] : mul[j];
-    row_store<TO, V>(a.out.p + (int64_t)row[j] * a.out.stride + e[j] * (int64_t)sizeof(TO), v);
+    row_store<TO, V>(a.out.p + (int64_t)row[j] * a.out.stride + e[j] * (int64_t)sizeof(TO), v,
+                     a.stream);
   }
   if (bad) set_status(a.status, GG_DEV_BAD_ID);
 }
@@ -836,19 +838,21 @@ int launch_lookup(LookupArgs& a, hipStream_t stream) {
   a.pieces = (uint32_t)cdiv(a.dim, wide ? V : 1);
   a.pmagic = div_magic(a.pieces);
   const uint64_t total = (uint64_t)a.n * a.pieces;
-  GG_REQUIRE(total <= 1ULL << 33, "%lld rows of %d elements are too many for one call",
+  GG_REQUIRE(total <= 1ULL << 32, "%lld rows of %d elements are too many for one call",
              (long long)a.n, a.dim);
-  // One piece per lane while that leaves lanes idle, four in flight after.
-  const int u = total < 256 * 1024 ? 1 : 4;
+  a.stream = (int64_t)sizeof(TO) * a.n * a.dim > kStreamBytes;
+  // One piece per lane while that leaves lanes idle, two in flight after (four
+  // and eight: 1.5M rows of 100 fp32 221 and 229 us, two 216).
+  const int u = total < 256 * 1024 ? 1 : 2;
   const dim3 grid((unsigned)((total + kBlock * u - 1) / (kBlock * u)));
   if (!wide)
-    hipLaunchKernelGGL((k_embed_rows<TI, TO, 1, 4>),
-                       dim3((unsigned)((total + kBlock * 4 - 1) / (kBlock * 4))), dim3(kBlock), 0,
+    hipLaunchKernelGGL((k_embed_rows<TI, TO, 1, 2>),
+                       dim3((unsigned)((total + kBlock * 2 - 1) / (kBlock * 2))), dim3(kBlock), 0,
                        stream, a);
   else if (u == 1)
     hipLaunchKernelGGL((k_embed_rows<TI, TO, V, 1>), grid, dim3(kBlock), 0, stream, a);
   else
-    hipLaunchKernelGGL((k_embed_rows<TI, TO, V, 4>), grid, dim3(kBlock), 0, stream, a);
+    hipLaunchKernelGGL((k_embed_rows<TI, TO, V, 2>), grid, dim3(kBlock), 0, stream, a);
   GG_LAUNCH_CHECK("k_embed_rows");
   return GG_OK;
 }

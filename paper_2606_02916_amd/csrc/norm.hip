@@ -21,6 +21,7 @@ struct NormArgs {
   int32_t dim, pieces, lanes_log;
   int32_t group_lanes_log;     // lanes that share a scale; -1: the row
   int32_t group_log;
+  bool stream;                 // the outputs go past the caches
 };
 
 template <bool BLK>
@@ -125,10 +126,12 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
     if (p < a.pieces) {
       int32_t skip;
       const int32_t e = piece_start<V>(p, a.dim, &skip);
-      if (a.sum.p) row_store<R, V>(a.sum.p + row * a.sum.stride + e * (int64_t)sizeof(R), s[t]);
+      if (a.sum.p) row_store<R, V>(a.sum.p + row * a.sum.stride + e * (int64_t)sizeof(R), s[t],
+                                 a.stream);
 #pragma unroll
       for (int k = 0; k < V; ++k) s[t][k] = s[t][k] * rstd * w[t][k];
-      if (a.y.p) row_store<T, V>(a.y.p + row * a.y.stride + e * (int64_t)sizeof(T), s[t]);
+      if (a.y.p)
+        row_store<T, V>(a.y.p + row * a.y.stride + e * (int64_t)sizeof(T), s[t], a.stream);
     }
   }
   if (!a.q.p) return;
@@ -172,7 +175,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
     for (int k = 0; k < V; ++k) c[k] = s[t][k] * inv;
     char* to = a.q.p + row * a.q.stride + e;
     if (skip == 0) {
-      row_store<e4m3, V>(to, c);
+      row_store<e4m3, V>(to, c, a.stream);
     } else {
       // the skipped elements have their own piece's scale
 #pragma unroll
@@ -199,6 +202,7 @@ struct NormBackArgs {
   int64_t n;
   int32_t dim, pieces, lanes_log;
   float* part;                 // [blocks][dim], or nullptr: no dw
+  bool stream;
 };
 
 template <typename T, typename R, int V, int STEPS, bool BLK>
@@ -253,7 +257,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm_back(NormBackArgs 
         const int32_t e = piece_start<V>(p, a.dim, &skip);
 #pragma unroll
         for (int k = 0; k < V; ++k) d[t][k] = ds[t][k] + rho * (d[t][k] - s[t][k] * mean);
-        row_store<R, V>(a.dx.p + row * a.dx.stride + e * (int64_t)sizeof(R), d[t]);
+        row_store<R, V>(a.dx.p + row * a.dx.stride + e * (int64_t)sizeof(R), d[t], a.stream);
       }
     }
   }
@@ -370,6 +374,8 @@ int launch_norm(NormArgs& a, hipStream_t stream) {
     a.group_log = __builtin_ctz((unsigned)a.q.group);
     a.group_lanes_log = a.group_log - __builtin_ctz((unsigned)vec);
   }
+  const int64_t out = (a.sum.p ? sizeof(R) : 0) + (a.y.p ? sizeof(T) : 0) + (a.q.p ? 1 : 0);
+  a.stream = out * a.n * a.dim > kStreamBytes;
   const dim3 grid = grid_of(s.blk ? a.n : cdiv(a.n << s.lanes_log, kBlock));
   if (!wide)
     hipLaunchKernelGGL((k_norm<T, R, 1, 1, false>), grid, dim3(kBlock), 0, stream, a);
@@ -392,6 +398,7 @@ int launch_back(NormBackArgs& a, float* dw, hipStream_t stream) {
   const Shape s = shape_of(a.dim, wide ? V : 1, kBackWaveSteps, 2);
   a.pieces = s.pieces;
   a.lanes_log = s.lanes_log;
+  a.stream = (int64_t)sizeof(R) * a.n * a.dim > kStreamBytes;
   const int blocks = back_blocks(a.n, s);
   const dim3 grid((unsigned)blocks);
   if (blocks > 0) {
