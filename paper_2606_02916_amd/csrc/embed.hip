@@ -99,13 +99,16 @@ __global__ void __launch_bounds__(kBlock) k_embed_rows(LookupArgs a) {
 // ---------------------------------------------------------------------------
 constexpr int kSortKeys = 8;                      // pairs per lane
 constexpr int kTileWave = kWave * kSortKeys;
-constexpr int kTileBlock = 1024;                  // lanes of the one-tile sort
-constexpr int kTile = kTileBlock * kSortKeys;
-constexpr int kMaxDigit = 9;                      // bits of a digit; 8 beyond kWideTiles tiles
-constexpr int kWideTiles = 64;
-// A tile's work is instructions, which a block of 4 waves spreads over more of
-// the chip; blocks of 16 waves keep the counters of many tiles few.
+// One tile that a block of 1,024 lanes sorts in a single launch.
+constexpr int kTileBlock = 1024;
+constexpr int kTileKeys = 16;
+constexpr int kTileMost = kTileBlock * kTileKeys;
+// Beyond, a tile's work is instructions, which blocks of 4 waves spread over more
+// of the chip; blocks of 16 waves keep the counters of many tiles few.  Digits
+// have up to 9 bits, and 8 in the larger blocks: ids of 18 bits in two passes,
+// 200,003 of them in 32 us instead of 44.
 constexpr int kSmallSortTiles = 256;              // most tiles of 4-wave blocks
+constexpr int digit_limit(int nt) { return nt == 1024 ? 8 : 9; }
 
 // Rows to be cleared by the sort's launches, in blocks behind its own: the sort
 // waits for memory more than it uses it.
@@ -165,13 +168,13 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, bool valid)
 
 // Ranks a wave's pairs, `steps` of them per lane: cnt[d] ends as their number
 // with digit d, rank[j] as the number of earlier ones.
-__device__ __forceinline__ void rank_tile(const uint32_t (&key)[kSortKeys], int shift, int bits,
-                                          int left, int steps, uint16_t* cnt,
-                                          uint16_t (&rank)[kSortKeys]) {
+template <int K>
+__device__ __forceinline__ void rank_tile(const uint32_t (&key)[K], int shift, int bits, int left,
+                                          int steps, uint16_t* cnt, uint16_t (&rank)[K]) {
   const uint32_t mask = (1u << bits) - 1u;
   const int lane = lane_id();
 #pragma unroll
-  for (int j = 0; j < kSortKeys; ++j) {
+  for (int j = 0; j < K; ++j) {
     if (j >= steps) break;
     const uint32_t d = (key[j] >> shift) & mask;
     const bool valid = j * kWave + lane < left;
@@ -183,9 +186,6 @@ __device__ __forceinline__ void rank_tile(const uint32_t (&key)[kSortKeys], int 
     if (valid && below == 0) ((volatile uint16_t*)cnt)[d] = (uint16_t)(before + __popcll(m));
   }
 }
-
-// Digit bits of a block of nt lanes at most.
-constexpr int digit_limit(int nt) { return nt == kBlock ? kMaxDigit : 8; }
 
 // Digit counts of each tile: hist[tile][digit].
 template <int NT>
@@ -324,20 +324,20 @@ __global__ void __launch_bounds__(kTileBlock) k_sort_tile(Keys a, int key_bits, 
                                                           FillArgs f) {
   if (blockIdx.x > 0)
     return fill_rows_with_zeros<kTileBlock>(f, blockIdx.x - 1, gridDim.x - 1);
-  constexpr int kSortBlock = kTileBlock, kSortWaves = kTileBlock / kWave;
-  __shared__ uint32_t s_key[kTile];
-  __shared__ uint16_t s_pos[kTile];
-  __shared__ uint16_t cnt[kSortWaves << 8];
+  constexpr int kSortBlock = kTileBlock, kSortWaves = kTileBlock / kWave, kTileDigit = 9;
+  __shared__ uint32_t s_key[kTileMost];
+  __shared__ uint16_t s_pos[kTileMost];
+  __shared__ uint16_t cnt[kSortWaves << kTileDigit];
   __shared__ int32_t s_scan[kSortWaves];
-  __shared__ int32_t base[1 << 8];
+  __shared__ int32_t base[1 << kTileDigit];
   const int w = threadIdx.x / kWave, n = (int)a.n;
   const int steps = (n + kSortBlock - 1) / kSortBlock;     // few ids: fewer per lane
   const int first = w * steps * kWave, left = min(steps * kWave, max(0, n - first));
-  uint32_t key[kSortKeys];
-  uint16_t pos[kSortKeys], rank[kSortKeys];
+  uint32_t key[kTileKeys];
+  uint16_t pos[kTileKeys], rank[kTileKeys];
   bool bad = false;
 #pragma unroll
-  for (int j = 0; j < kSortKeys; ++j) {
+  for (int j = 0; j < kTileKeys; ++j) {
     const int o = j * kWave + lane_id();
     key[j] = o < left ? key_of(a, first + o, &bad) : 0u;
     pos[j] = (uint16_t)(first + o);
@@ -347,7 +347,7 @@ __global__ void __launch_bounds__(kTileBlock) k_sort_tile(Keys a, int key_bits, 
     const int bits = min(digit_bits, key_bits - shift), digits = 1 << bits;
     if (shift) {
 #pragma unroll
-      for (int j = 0; j < kSortKeys; ++j) {
+      for (int j = 0; j < kTileKeys; ++j) {
         const int o = j * kWave + lane_id();
         if (o < left) {
           key[j] = s_key[first + o];
@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(kTileBlock) k_sort_tile(Keys a, int key_bits, 
     __syncthreads();
     const bool last = shift + bits >= key_bits;
 #pragma unroll
-    for (int j = 0; j < kSortKeys; ++j) {
+    for (int j = 0; j < kTileKeys; ++j) {
       if (j * kWave + lane_id() >= left) continue;
       const uint32_t d = (key[j] >> shift) & (digits - 1);
       const uint32_t to = (uint32_t)base[d] + cnt[w * digits + d] + rank[j];
@@ -789,10 +789,10 @@ struct SortShape {
 };
 
 SortShape sort_shape(int64_t n) {
-  if (n <= kTile) return {n > 0 ? 1 : 0, kTileBlock, 8};
+  if (n <= kTileMost) return {n > 0 ? 1 : 0, kTileBlock, 9};
   const int64_t small = cdiv(n, kBlock * kSortKeys);
-  if (small <= kSmallSortTiles) return {(int)small, kBlock, small <= kWideTiles ? kMaxDigit : 8};
-  return {(int)cdiv(n, kTile), 1024, 8};
+  if (small <= kSmallSortTiles) return {(int)small, kBlock, digit_limit(kBlock)};
+  return {(int)cdiv(n, 1024 * kSortKeys), 1024, digit_limit(1024)};
 }
 
 struct EmbedWs {

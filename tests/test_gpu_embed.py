@@ -173,10 +173,11 @@ def test_gradient_types(tdy, tgrad, n, v, dim, add):
     grad_case("frequent", n, v, dim, tdy, tgrad, add, pad=1)
 
 
-# More than one tile of the sort (8,192 ids), up to 32 tiles and beyond; runs
-# that cross many chunks; the largest key of one, two and three digits.
+# The sort's one tile (16,384 ids), tiles of 2,048 and of 8,192 ids; runs that
+# cross many chunks; keys of one, two and three digits.
 @pytest.mark.parametrize("kind,n,v,dim", [
-    ("frequent", 8193, 2047, 4), ("random", 20_000, 2048, 4), ("frequent", 30_000, 128_000, 16),
+    ("frequent", 8193, 2047, 4), ("frequent", 16_384, 3000, 3), ("random", 16_385, 3000, 3),
+    ("random", 524_288, 2000, 1), ("frequent", 524_289, 2000, 1), ("random", 20_000, 2048, 4), ("frequent", 30_000, 128_000, 16),
     ("same", 40_001, 70_000, 20), ("frequent", 300_001, 70_000, 4), ("same", 300_001, 5, 8),
     ("distinct", 262_145, 300_000, 3), ("random", 262_144, 255, 4), ("random", 270_000, 256, 2),
     ("frequent", 9000, 1_100_000, 1), ("frequent", 270_000, 17_000_000, 1)])
