@@ -40,9 +40,10 @@ __global__ void __launch_bounds__(kBlock) k_embed_rows(LookupArgs a) {
   else
     row0 = (uint32_t)base / a.pieces;
   const uint32_t rem = (uint32_t)(base - row0 * a.pieces);
+  // All ids, then all rows: a lane waits twice, whatever U is.
   typename Raw<TI, V>::vec raw[U];
   float mul[U], mul2[U];
-  uint64_t row[U];
+  int64_t row[U], id[U];
   int32_t e[U];
   bool ok[U];
   bool bad = false;
@@ -52,29 +53,40 @@ __global__ void __launch_bounds__(kBlock) k_embed_rows(LookupArgs a) {
     const uint32_t r = chunk_row(o, a.pmagic);
     int32_t skip;
     e[j] = piece_start<V>((int32_t)(o - r * a.pieces), a.dim, &skip);
-    row[j] = row0 + r;
-    ok[j] = row[j] < (uint64_t)a.n;
+    row[j] = (int64_t)(row0 + r);
+    ok[j] = row[j] < a.n;
+    id[j] = min(row[j], a.n - 1);
+  }
+  if (a.ids) {
+#pragma unroll
+    for (int j = 0; j < U; ++j) id[j] = id_at(a.ids, a.id_bits, id[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < U; ++j) {
     raw[j] = {};
     mul[j] = mul2[j] = 0.0f;
     if (ok[j]) {
-      const int64_t id = a.ids ? id_at(a.ids, a.id_bits, (int64_t)row[j]) : (int64_t)row[j];
-      if ((uint64_t)id < (uint64_t)a.rows) {
-        raw[j] = raw_load<TI, V>(a.table.p + id * a.table.stride + e[j] * (int64_t)sizeof(TI));
-        mul[j] = a.scale;
+      if ((uint64_t)id[j] < (uint64_t)a.rows) {
+        raw[j] = raw_load<TI, V>(a.table.p + id[j] * a.table.stride + e[j] * (int64_t)sizeof(TI));
+        mul[j] = mul2[j] = 1.0f;
         if constexpr (sizeof(TI) == 1) {
           // The row's last piece may lie in two groups (never in more).
-          const float* sc = (const float*)(a.table.scales + id * a.table.sstride);
-          mul2[j] = mul[j] * sc[(e[j] + V - 1) >> a.glog];
-          mul[j] *= sc[e[j] >> a.glog];
+          const float* sc = (const float*)(a.table.scales + id[j] * a.table.sstride);
+          mul[j] = sc[e[j] >> a.glog];
+          mul2[j] = sc[(e[j] + V - 1) >> a.glog];
         }
       } else {
-        bad |= id != -1;
+        bad |= id[j] != -1;
       }
     }
   }
 #pragma unroll
   for (int j = 0; j < U; ++j) {
     if (!ok[j]) continue;
+    if ((uint64_t)id[j] < (uint64_t)a.rows) {
+      mul[j] *= a.scale;
+      mul2[j] *= a.scale;
+    }
     float v[V];
     to_f32<TI, V>(raw[j], v);
 #pragma unroll
@@ -145,15 +157,38 @@ struct Keys {
   int32_t* status;
 };
 
-__device__ __forceinline__ uint32_t key_of(const Keys& a, int64_t i, bool* bad) {
-  if (!a.ids) return a.key[i];
-  const int64_t id = id_at(a.ids, a.id_bits, i);
-  if ((uint64_t)id < (uint64_t)a.rows) return (uint32_t)id;
-  *bad |= id != -1;
-  return a.rows;
+// A lane's keys of the pairs first + lane, first + 64 + lane, .. below `left`,
+// all loads in flight together (places past the end repeat the last pair).
+template <int K>
+__device__ __forceinline__ void load_keys(const Keys& a, int64_t first, int left,
+                                          uint32_t (&key)[K]) {
+  int64_t at[K];
+#pragma unroll
+  for (int j = 0; j < K; ++j) at[j] = min(first + j * kWave + lane_id(), a.n - 1);
+  if (!a.ids) {
+#pragma unroll
+    for (int j = 0; j < K; ++j) key[j] = a.key[at[j]];
+    return;
+  }
+  int64_t id[K];
+  if (a.id_bits == 64) {
+#pragma unroll
+    for (int j = 0; j < K; ++j) id[j] = ((const int64_t*)a.ids)[at[j]];
+  } else {
+#pragma unroll
+    for (int j = 0; j < K; ++j) id[j] = ((const int32_t*)a.ids)[at[j]];
+  }
+  bool bad = false;
+#pragma unroll
+  for (int j = 0; j < K; ++j) {
+    const bool in = (uint64_t)id[j] < (uint64_t)a.rows;
+    key[j] = in ? (uint32_t)id[j] : a.rows;
+    bad |= !in && id[j] != -1 && j * kWave + lane_id() < left;
+  }
+  if (bad) set_status(a.status, GG_DEV_BAD_ID);
 }
 
-// Lanes with this lane's digit, among the valid ones: six instructions a bit.
+// Lanes with this lane's digit, among the valid ones: four instructions a bit.
 __device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, bool valid) {
   uint64_t m = __ballot(valid);
   uint32_t lo = (uint32_t)m, hi = (uint32_t)(m >> 32);
@@ -168,22 +203,26 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, bool valid)
 
 // Ranks a wave's pairs, `steps` of them per lane: cnt[d] ends as their number
 // with digit d, rank[j] as the number of earlier ones.
+// (The counters go by LDS addresses: through generic ones, volatile accesses
+// become flat ones, with a wait for global memory at each.)
 template <int K>
 __device__ __forceinline__ void rank_tile(const uint32_t (&key)[K], int shift, int bits, int left,
                                           int steps, uint16_t* cnt, uint16_t (&rank)[K]) {
   const uint32_t mask = (1u << bits) - 1u;
   const int lane = lane_id();
+  auto* c = (__attribute__((address_space(3))) volatile uint16_t*)cnt;
 #pragma unroll
   for (int j = 0; j < K; ++j) {
-    if (j >= steps) break;
-    const uint32_t d = (key[j] >> shift) & mask;
-    const bool valid = j * kWave + lane < left;
-    const uint64_t m = same_digit(d, bits, valid);
-    // A wave's LDS accesses run in order: all its lanes read before one writes.
-    const uint32_t before = valid ? ((volatile uint16_t*)cnt)[d] : 0u;
-    const int below = lanes_below(m);
-    rank[j] = (uint16_t)(before + below);
-    if (valid && below == 0) ((volatile uint16_t*)cnt)[d] = (uint16_t)(before + __popcll(m));
+    if (j < steps) {
+      const uint32_t d = (key[j] >> shift) & mask;
+      const bool valid = j * kWave + lane < left;
+      const uint64_t m = same_digit(d, bits, valid);
+      // A wave's LDS accesses run in order: all its lanes read before one writes.
+      const uint32_t before = c[d];
+      const int below = lanes_below(m);
+      rank[j] = (uint16_t)(before + below);
+      if (valid && below == 0) c[d] = (uint16_t)(before + __popcll(m));
+    }
   }
 }
 
@@ -201,13 +240,7 @@ __global__ void __launch_bounds__(NT) k_sort_count(Keys a, int32_t* hist, int ti
   const int left = (int)min((int64_t)kTileWave, max((int64_t)0, a.n - first));
   uint32_t key[kSortKeys];
   uint16_t rank[kSortKeys];
-  bool bad = false;
-#pragma unroll
-  for (int j = 0; j < kSortKeys; ++j) {
-    const int o = j * kWave + lane_id();
-    key[j] = o < left ? key_of(a, first + o, &bad) : 0u;
-  }
-  if (bad) set_status(a.status, GG_DEV_BAD_ID);
+  load_keys(a, first, left, key);
   __syncthreads();
   rank_tile(key, a.shift, a.bits, left, kSortKeys, cnt + w * digits, rank);
   __syncthreads();
@@ -241,13 +274,13 @@ __global__ void __launch_bounds__(NT) k_sort_scatter(Keys a, const int32_t* hist
   const int left = (int)min((int64_t)kTileWave, max((int64_t)0, a.n - first));
   uint32_t key[kSortKeys], pos[kSortKeys];
   uint16_t rank[kSortKeys];
-  bool bad = false;
 #pragma unroll
-  for (int j = 0; j < kSortKeys; ++j) {
-    const int o = j * kWave + lane_id();
-    key[j] = o < left ? key_of(a, first + o, &bad) : 0u;
-    pos[j] = o < left ? (a.ids ? (uint32_t)(first + o) : a.pos[first + o]) : 0u;
+  for (int j = 0; j < kSortKeys; ++j) pos[j] = (uint32_t)(first + j * kWave + lane_id());
+  if (!a.ids) {
+#pragma unroll
+    for (int j = 0; j < kSortKeys; ++j) pos[j] = a.pos[min((int64_t)pos[j], a.n - 1)];
   }
+  load_keys(a, first, left, key);
   // A lane adds up two neighbouring digits over a share of the tiles.
   const int cols = digits / 2, groups = NT / cols, c = tid & (cols - 1), g = tid / cols;
   const int per = (tiles + groups - 1) / groups, t1 = min(tiles, (g + 1) * per);
@@ -335,14 +368,9 @@ __global__ void __launch_bounds__(kTileBlock) k_sort_tile(Keys a, int key_bits, 
   const int first = w * steps * kWave, left = min(steps * kWave, max(0, n - first));
   uint32_t key[kTileKeys];
   uint16_t pos[kTileKeys], rank[kTileKeys];
-  bool bad = false;
 #pragma unroll
-  for (int j = 0; j < kTileKeys; ++j) {
-    const int o = j * kWave + lane_id();
-    key[j] = o < left ? key_of(a, first + o, &bad) : 0u;
-    pos[j] = (uint16_t)(first + o);
-  }
-  if (bad) set_status(a.status, GG_DEV_BAD_ID);
+  for (int j = 0; j < kTileKeys; ++j) pos[j] = (uint16_t)(first + j * kWave + lane_id());
+  load_keys(a, first, left, key);
   for (int shift = 0; shift < key_bits; shift += digit_bits) {
     const int bits = min(digit_bits, key_bits - shift), digits = 1 << bits;
     if (shift) {
@@ -1012,9 +1040,6 @@ extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t
   a.scale = scale;
   a.part = w.part;
   a.chunk = grad_chunk(n);
-  // Rows of a block: as many as leave the chip 8,192 blocks.
-  a.per = 1;
-  while (a.per < kGradRows && (int64_t)a.per * 8192 <= (a.by_position ? n : num_rows)) a.per *= 2;
   GG_FOR_FLOAT(dy->dtype, TD, {
     constexpr int V = kVec<TD>;
     const Lanes l = lanes_of(dim, dim >= V ? V : 1);
@@ -1022,6 +1047,16 @@ extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t
     a.lanes_log = l.lanes_log;
     a.tiles = l.tiles;
     a.tmagic = div_magic((uint32_t)l.tiles);
+    // Rows of a block: what its groups take at a time, as far as these rows
+    // have no more than 512 positions together, and more while that leaves 8,192
+    // blocks.
+    const int64_t all = a.by_position ? n : num_rows;
+    const int64_t fill = (kBlock >> l.lanes_log) * kItems<V> / l.tiles;
+    a.per = 1;
+    while (a.per < kGradRows &&
+           (a.per * 8192LL <= all ||
+            (a.per * 2LL <= fill && (a.by_position || a.per * 2LL * n <= 512 * num_rows))))
+      a.per *= 2;
     GG_FOR_FLOAT(grad->dtype, TG, {
       return dim >= V ? launch_grad<TD, TG, V>(a, stream) : launch_grad<TD, TG, 1>(a, stream);
     });

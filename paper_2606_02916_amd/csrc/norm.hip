@@ -68,16 +68,20 @@ __device__ __forceinline__ uint32_t magnitude(const float (&v)[V], int32_t skip)
   return m;
 }
 
-template <typename T, int V>
-__device__ __forceinline__ void load_weight(const char* w, int32_t w_f32, int32_t e,
-                                            float (&v)[V]) {
+template <typename T, int V, int STEPS>
+__device__ __forceinline__ void load_weights(const char* w, int32_t w_f32, const int32_t (&e)[STEPS],
+                                             float (&v)[STEPS][V]) {
   if (!w) {
 #pragma unroll
-    for (int k = 0; k < V; ++k) v[k] = 1.0f;
+    for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+      for (int k = 0; k < V; ++k) v[t][k] = 1.0f;
   } else if (sizeof(T) == 4 || w_f32) {
-    row_load<float, V>(w + e * 4LL, v);
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t) row_load<float, V>(w + e[t] * 4LL, v[t]);
   } else {
-    row_load<T, V>(w + e * (int64_t)sizeof(T), v);
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t) row_load<T, V>(w + e[t] * (int64_t)sizeof(T), v[t]);
   }
 }
 
@@ -94,27 +98,34 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
   const int64_t row = BLK ? block_index() : (block_index() * kBlock + threadIdx.x) >> a.lanes_log;
   if (row >= a.n) return;
   const int l = BLK ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1);
-  float s[STEPS][V];
-  float w[STEPS][V];
+  // All loads before any use, so that the row is one wait; lanes behind the
+  // last piece repeat it and count nothing.
+  typename Raw<T, V>::vec rx[STEPS];
+  typename Raw<R, V>::vec rr[STEPS];
+  float s[STEPS][V], w[STEPS][V];
+  int32_t e[STEPS], skip[STEPS];
+#pragma unroll
+  for (int t = 0; t < STEPS; ++t) {
+    e[t] = piece_start<V>(min(t * lanes + l, a.pieces - 1), a.dim, &skip[t]);
+    rx[t] = raw_load<T, V>(a.x.p + row * a.x.stride + e[t] * (int64_t)sizeof(T));
+  }
+  if (a.res.p) {
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t)
+      rr[t] = raw_load<R, V>(a.res.p + row * a.res.stride + e[t] * (int64_t)sizeof(R));
+  }
+  load_weights<T, V, STEPS>(a.w, a.w_f32, e, w);
   float sq = 0.0f;
 #pragma unroll
   for (int t = 0; t < STEPS; ++t) {
-    const int p = t * lanes + l;
+    to_f32<T, V>(rx[t], s[t]);
+    if (a.res.p) {
+      float r[V];
+      to_f32<R, V>(rr[t], r);
 #pragma unroll
-    for (int k = 0; k < V; ++k) s[t][k] = w[t][k] = 0.0f;
-    if (p < a.pieces) {
-      int32_t skip;
-      const int32_t e = piece_start<V>(p, a.dim, &skip);
-      row_load<T, V>(a.x.p + row * a.x.stride + e * (int64_t)sizeof(T), s[t]);
-      if (a.res.p) {
-        float r[V];
-        row_load<R, V>(a.res.p + row * a.res.stride + e * (int64_t)sizeof(R), r);
-#pragma unroll
-        for (int k = 0; k < V; ++k) s[t][k] += r[k];
-      }
-      load_weight<T, V>(a.w, a.w_f32, e, w[t]);
-      sq += squares<V>(s[t], skip);
+      for (int k = 0; k < V; ++k) s[t][k] += r[k];
     }
+    if (t * lanes + l < a.pieces) sq += squares<V>(s[t], skip[t]);
   }
   sq = group_sum<BLK>(sq, lanes, lds);
   const float rstd = 1.0f / sqrtf(sq / (float)a.dim + a.eps);
@@ -124,14 +135,12 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
   for (int t = 0; t < STEPS; ++t) {
     const int p = t * lanes + l;
     if (p < a.pieces) {
-      int32_t skip;
-      const int32_t e = piece_start<V>(p, a.dim, &skip);
-      if (a.sum.p) row_store<R, V>(a.sum.p + row * a.sum.stride + e * (int64_t)sizeof(R), s[t],
+      if (a.sum.p) row_store<R, V>(a.sum.p + row * a.sum.stride + e[t] * (int64_t)sizeof(R), s[t],
                                  a.stream);
 #pragma unroll
       for (int k = 0; k < V; ++k) s[t][k] = s[t][k] * rstd * w[t][k];
       if (a.y.p)
-        row_store<T, V>(a.y.p + row * a.y.stride + e * (int64_t)sizeof(T), s[t], a.stream);
+        row_store<T, V>(a.y.p + row * a.y.stride + e[t] * (int64_t)sizeof(T), s[t], a.stream);
     }
   }
   if (!a.q.p) return;
@@ -142,7 +151,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
   for (int t = 0; t < STEPS; ++t) {
     top[t] = 0;
     if (t * lanes + l < a.pieces)
-      top[t] = magnitude<V>(s[t], max(0, (t * lanes + l) * V - (a.dim - V)));
+      top[t] = magnitude<V>(s[t], skip[t]);
     all = max(all, top[t]);
   }
   const bool per_row = a.group_lanes_log < 0;
@@ -168,20 +177,18 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
     const bool first = per_row ? p == 0 : (p & ((1 << a.group_lanes_log) - 1)) == 0;
     if (first)
       ((float*)(a.q.scales + row * a.q.sstride))[per_row ? 0 : (p * V) >> a.group_log] = scale;
-    int32_t skip;
-    const int32_t e = piece_start<V>(p, a.dim, &skip);
     float c[V];
 #pragma unroll
     for (int k = 0; k < V; ++k) c[k] = s[t][k] * inv;
-    char* to = a.q.p + row * a.q.stride + e;
-    if (skip == 0) {
+    char* to = a.q.p + row * a.q.stride + e[t];
+    if (skip[t] == 0) {
       row_store<e4m3, V>(to, c, a.stream);
     } else {
       // the skipped elements have their own piece's scale
 #pragma unroll
       for (int k = 0; k < V; ++k) {
         const float one[1] = {c[k]};
-        if (k >= skip) row_store<e4m3, 1>(to + k, one);
+        if (k >= skip[t]) row_store<e4m3, 1>(to + k, one);
       }
     }
   }
@@ -213,51 +220,68 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm_back(NormBackArgs 
   const int g = BLK ? 0 : (int)threadIdx.x >> a.lanes_log;
   const int l = BLK ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1);
   float w[STEPS][V], acc[STEPS][V];
+  int32_t e[STEPS], skip[STEPS];
 #pragma unroll
   for (int t = 0; t < STEPS; ++t) {
-    const int p = t * lanes + l;
-    int32_t skip;
+    e[t] = piece_start<V>(min(t * lanes + l, a.pieces - 1), a.dim, &skip[t]);
 #pragma unroll
-    for (int k = 0; k < V; ++k) acc[t][k] = w[t][k] = 0.0f;
-    if (p < a.pieces) load_weight<T, V>(a.w, a.w_f32, piece_start<V>(p, a.dim, &skip), w[t]);
+    for (int k = 0; k < V; ++k) acc[t][k] = 0.0f;
   }
-  for (int64_t row = (int64_t)blockIdx.x * groups + g; row < a.n;
-       row += (int64_t)gridDim.x * groups) {
-    const float rho = a.rstd[row];
+  load_weights<T, V, STEPS>(a.w, a.w_f32, e, w);
+  // A row's loads are issued together (lanes behind the last piece repeat it),
+  // and those of the next row before this one's sum is known, where the
+  // registers hold both.
+  constexpr bool kAhead = STEPS * V < 16;
+  typename Raw<T, V>::vec rd[STEPS];
+  typename Raw<R, V>::vec rs[STEPS], ra[STEPS];
+  float rho_next = 0.0f;
+  const auto load_row = [&](int64_t row) {
+    rho_next = a.rstd[row];
+#pragma unroll
+    for (int t = 0; t < STEPS; ++t) {
+      rd[t] = raw_load<T, V>(a.dy.p + row * a.dy.stride + e[t] * (int64_t)sizeof(T));
+      rs[t] = raw_load<R, V>(a.s.p + row * a.s.stride + e[t] * (int64_t)sizeof(R));
+      ra[t] = {};
+    }
+    if (a.dsum.p) {
+#pragma unroll
+      for (int t = 0; t < STEPS; ++t)
+        ra[t] = raw_load<R, V>(a.dsum.p + row * a.dsum.stride + e[t] * (int64_t)sizeof(R));
+    }
+  };
+  const int64_t step = (int64_t)gridDim.x * groups;
+  int64_t row = (int64_t)blockIdx.x * groups + g;
+  if (kAhead && row < a.n) load_row(row);
+  for (; row < a.n; row += step) {
+    if (!kAhead) load_row(row);
+    const float rho = rho_next;
     float s[STEPS][V], d[STEPS][V], ds[STEPS][V];
     float dot = 0.0f;
 #pragma unroll
     for (int t = 0; t < STEPS; ++t) {
-      const int p = t * lanes + l;
+      to_f32<T, V>(rd[t], d[t]);
+      to_f32<R, V>(rs[t], s[t]);
+      to_f32<R, V>(ra[t], ds[t]);
+      float part = 0.0f;
 #pragma unroll
-      for (int k = 0; k < V; ++k) s[t][k] = d[t][k] = ds[t][k] = 0.0f;
-      if (p < a.pieces) {
-        int32_t skip;
-        const int32_t e = piece_start<V>(p, a.dim, &skip);
-        row_load<T, V>(a.dy.p + row * a.dy.stride + e * (int64_t)sizeof(T), d[t]);
-        row_load<R, V>(a.s.p + row * a.s.stride + e * (int64_t)sizeof(R), s[t]);
-        if (a.dsum.p)
-          row_load<R, V>(a.dsum.p + row * a.dsum.stride + e * (int64_t)sizeof(R), ds[t]);
-#pragma unroll
-        for (int k = 0; k < V; ++k) {
-          s[t][k] *= rho;
-          acc[t][k] += d[t][k] * s[t][k];
-          d[t][k] *= w[t][k];
-          dot += k >= skip ? d[t][k] * s[t][k] : 0.0f;
-        }
+      for (int k = 0; k < V; ++k) {
+        s[t][k] *= rho;
+        acc[t][k] += d[t][k] * s[t][k];
+        d[t][k] *= w[t][k];
+        part += k >= skip[t] ? d[t][k] * s[t][k] : 0.0f;
       }
+      dot += t * lanes + l < a.pieces ? part : 0.0f;
     }
+    if (kAhead && row + step < a.n) load_row(row + step);
     dot = group_sum<BLK>(dot, lanes, lds);
     const float mean = dot / (float)a.dim;
 #pragma unroll
     for (int t = 0; t < STEPS; ++t) {
       const int p = t * lanes + l;
       if (p < a.pieces) {
-        int32_t skip;
-        const int32_t e = piece_start<V>(p, a.dim, &skip);
 #pragma unroll
         for (int k = 0; k < V; ++k) d[t][k] = ds[t][k] + rho * (d[t][k] - s[t][k] * mean);
-        row_store<R, V>(a.dx.p + row * a.dx.stride + e * (int64_t)sizeof(R), d[t], a.stream);
+        row_store<R, V>(a.dx.p + row * a.dx.stride + e[t] * (int64_t)sizeof(R), d[t], a.stream);
       }
     }
   }
@@ -278,9 +302,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm_back(NormBackArgs 
     }
     const int p = t * lanes + l;
     if (g == 0 && p < a.pieces) {
-      int32_t skip;
-      const int32_t e = piece_start<V>(p, a.dim, &skip);
-      row_store<float, V>((char*)(part + e), acc[t]);
+      row_store<float, V>((char*)(part + e[t]), acc[t]);
     }
   }
 }
@@ -385,21 +407,23 @@ int launch_norm(NormArgs& a, hipStream_t stream) {
   return GG_OK;
 }
 
-// Blocks of the backward pass.
-int back_blocks(int64_t n, const Shape& s) {
+// Blocks of the backward pass: three for each of 256 CUs, four where a block's
+// row is below 4 KB (100,000 x 602 fp32: 149 us with 768 blocks, 134 with
+// 1,024; 65,536 x 2,048 bf16: 188 and 215).
+int back_blocks(int64_t n, int64_t row_bytes, const Shape& s) {
   const int64_t rows = s.blk ? 1 : kBlock >> s.lanes_log;   // at a time in a block
-  return (int)std::min<int64_t>(cdiv(n, rows), s.threads <= 256 ? 1024 : 512);
+  return (int)std::min<int64_t>(cdiv(n, rows), s.blk && row_bytes < 4096 ? 1024 : 768);
 }
 
 template <typename T, typename R>
 int launch_back(NormBackArgs& a, float* dw, hipStream_t stream) {
   constexpr int V = kVec<T>;
   const bool wide = a.dim >= V;
-  const Shape s = shape_of(a.dim, wide ? V : 1, kBackWaveSteps, 2);
+  const Shape s = shape_of(a.dim, wide ? V : 1, kBackWaveSteps, 1);
   a.pieces = s.pieces;
   a.lanes_log = s.lanes_log;
   a.stream = (int64_t)sizeof(R) * a.n * a.dim > kStreamBytes;
-  const int blocks = back_blocks(a.n, s);
+  const int blocks = back_blocks(a.n, a.dim * (int64_t)sizeof(T), s);
   const dim3 grid((unsigned)blocks);
   if (blocks > 0) {
     if (!wide)
