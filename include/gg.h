@@ -589,6 +589,8 @@ int gg_embed_forward(const gg_rows_t* table, int64_t num_rows, int32_t dim, cons
                      int32_t id_bits, int64_t n, float scale, const gg_rows_t* out,
                      int32_t* status_d, hipStream_t stream);
 
+/* Workspace bytes of the calls below grow with n: a workspace for n rows serves
+ * calls of fewer. */
 size_t gg_ws_embed(int64_t n, int64_t num_rows, int32_t dim);
 
 /* Its gradient: grad[v] = scale * (sum of dy[i] over the i with ids[i] = v), for

@@ -570,7 +570,8 @@ struct DistillWs {
 size_t distill_ws_layout(int64_t n, char* base, DistillWs* out) {
   Carve c{base, 0, 0};
   DistillWs w;
-  w.part = c.take<float2>((size_t)n * split_count(n));
+  // (the most that any m <= n takes, so that a workspace serves smaller calls)
+  w.part = c.take<float2>((size_t)std::min<int64_t>(kMaxSplits * n, std::max<int64_t>(1024, n)));
   w.lesson = c.take<float2>((size_t)n);
   if (out) *out = w;
   return align_up(c.used, 256);

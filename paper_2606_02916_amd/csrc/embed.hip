@@ -111,10 +111,9 @@ __global__ void __launch_bounds__(kBlock) k_embed_rows(LookupArgs a) {
 // ---------------------------------------------------------------------------
 constexpr int kSortKeys = 8;                      // pairs per lane
 constexpr int kTileWave = kWave * kSortKeys;
-// One tile that a block of 1,024 lanes sorts in a single launch.
-constexpr int kTileBlock = 1024;
-constexpr int kTileKeys = 16;
-constexpr int kTileMost = kTileBlock * kTileKeys;
+// Up to this many pairs find their places by counting, in a single launch.
+constexpr int kRankBlock = 1024;
+constexpr int kRankMost = 16384;
 // Beyond, a tile's work is instructions, which blocks of 4 waves spread over more
 // of the chip; blocks of 16 waves keep the counters of many tiles few.  Digits
 // have up to 9 bits, and 8 in the larger blocks: ids of 18 bits in two passes,
@@ -201,28 +200,26 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits, bool valid)
   return (uint64_t)hi << 32 | lo;
 }
 
-// Ranks a wave's pairs, `steps` of them per lane: cnt[d] ends as their number
-// with digit d, rank[j] as the number of earlier ones.
+// Ranks a wave's pairs: cnt[d] ends as their number with digit d, rank[j] as the
+// number of earlier ones.
 // (The counters go by LDS addresses: through generic ones, volatile accesses
 // become flat ones, with a wait for global memory at each.)
 template <int K>
 __device__ __forceinline__ void rank_tile(const uint32_t (&key)[K], int shift, int bits, int left,
-                                          int steps, uint16_t* cnt, uint16_t (&rank)[K]) {
+                                          uint16_t* cnt, uint16_t (&rank)[K]) {
   const uint32_t mask = (1u << bits) - 1u;
   const int lane = lane_id();
   auto* c = (__attribute__((address_space(3))) volatile uint16_t*)cnt;
 #pragma unroll
   for (int j = 0; j < K; ++j) {
-    if (j < steps) {
-      const uint32_t d = (key[j] >> shift) & mask;
-      const bool valid = j * kWave + lane < left;
-      const uint64_t m = same_digit(d, bits, valid);
-      // A wave's LDS accesses run in order: all its lanes read before one writes.
-      const uint32_t before = c[d];
-      const int below = lanes_below(m);
-      rank[j] = (uint16_t)(before + below);
-      if (valid && below == 0) c[d] = (uint16_t)(before + __popcll(m));
-    }
+    const uint32_t d = (key[j] >> shift) & mask;
+    const bool valid = j * kWave + lane < left;
+    const uint64_t m = same_digit(d, bits, valid);
+    // A wave's LDS accesses run in order: all its lanes read before one writes.
+    const uint32_t before = c[d];
+    const int below = lanes_below(m);
+    rank[j] = (uint16_t)(before + below);
+    if (valid && below == 0) c[d] = (uint16_t)(before + __popcll(m));
   }
 }
 
@@ -242,7 +239,7 @@ __global__ void __launch_bounds__(NT) k_sort_count(Keys a, int32_t* hist, int ti
   uint16_t rank[kSortKeys];
   load_keys(a, first, left, key);
   __syncthreads();
-  rank_tile(key, a.shift, a.bits, left, kSortKeys, cnt + w * digits, rank);
+  rank_tile(key, a.shift, a.bits, left, cnt + w * digits, rank);
   __syncthreads();
   for (int d = threadIdx.x; d < digits; d += kSortBlock) {
     int32_t s = 0;
@@ -297,7 +294,7 @@ __global__ void __launch_bounds__(NT) k_sort_scatter(Keys a, const int32_t* hist
   s_mine[tid] = mine;
   s_all[tid] = all;
   __syncthreads();
-  rank_tile(key, a.shift, a.bits, left, kSortKeys, cnt + w * digits, rank);
+  rank_tile(key, a.shift, a.bits, left, cnt + w * digits, rank);
   __syncthreads();
   // The digits' totals over all tiles and in this one, scanned together.
   mine = all = {0, 0};
@@ -351,68 +348,63 @@ __global__ void __launch_bounds__(NT) k_sort_scatter(Keys a, const int32_t* hist
   }
 }
 
-// One tile: every pass in one launch, the pairs in LDS between passes.
-__global__ void __launch_bounds__(kTileBlock) k_sort_tile(Keys a, int key_bits, int digit_bits,
-                                                          uint32_t* key_out, uint32_t* pos_out,
-                                                          FillArgs f) {
-  if (blockIdx.x > 0)
-    return fill_rows_with_zeros<kTileBlock>(f, blockIdx.x - 1, gridDim.x - 1);
-  constexpr int kSortBlock = kTileBlock, kSortWaves = kTileBlock / kWave, kTileDigit = 9;
-  __shared__ uint32_t s_key[kTileMost];
-  __shared__ uint16_t s_pos[kTileMost];
-  __shared__ uint16_t cnt[kSortWaves << kTileDigit];
-  __shared__ int32_t s_scan[kSortWaves];
-  __shared__ int32_t base[1 << kTileDigit];
-  const int w = threadIdx.x / kWave, n = (int)a.n;
-  const int steps = (n + kSortBlock - 1) / kSortBlock;     // few ids: fewer per lane
-  const int first = w * steps * kWave, left = min(steps * kWave, max(0, n - first));
-  uint32_t key[kTileKeys];
-  uint16_t pos[kTileKeys], rank[kTileKeys];
+// Few pairs: a pair's place is the number of smaller keys, and of equal ones
+// before it.  A block has 64 pairs, one per lane, and its waves compare them
+// with a share of all keys each, which they read from LDS four at a time.  That
+// is n^2 comparisons, but on the whole chip and in one launch: 14,298 ids in
+// 20 us, where two passes over a tile in one block's LDS took 29 and four
+// launches of the other kernels take 27.
+__global__ void __launch_bounds__(kRankBlock) k_sort_rank(Keys a, int blocks, uint32_t* key_out,
+                                                          uint32_t* pos_out, FillArgs f) {
+  if ((int)blockIdx.x >= blocks)
+    return fill_rows_with_zeros<kRankBlock>(f, blockIdx.x - blocks, gridDim.x - blocks);
+  constexpr int kWaves = kRankBlock / kWave;
+  __shared__ uint4 s_key[kWaves][kWave / 4];
+  __shared__ uint32_t s_count[kWaves][kWave];
+  const int n = (int)a.n, w = threadIdx.x / kWave, lane = lane_id();
+  const int i0 = (int)blockIdx.x * kWave;
+  uint32_t own[1];
+  // (the ids out of range are reported once)
+  load_keys(a, i0, w == 0 ? n - i0 : 0, own);
+  const uint32_t k = own[0];
+  const int chunks = (n + kWave - 1) / kWave, per = (chunks + kWaves - 1) / kWaves;
+  const int c1 = min(chunks, (w + 1) * per);
+  uint32_t count = 0;
+  uint32_t next[1];
+  if (w * per < c1) load_keys(a, (int64_t)w * per * kWave, 0, next);
+  for (int c = w * per; c < c1; ++c) {
+    // a place past the end counts for nobody
+    const uint32_t mine = c * kWave + lane < n ? next[0] : ~0u;
+    if (c + 1 < c1) load_keys(a, (int64_t)(c + 1) * kWave, 0, next);
+    ((uint32_t*)s_key[w])[lane] = mine;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (c < (int)blockIdx.x) {
 #pragma unroll
-  for (int j = 0; j < kTileKeys; ++j) pos[j] = (uint16_t)(first + j * kWave + lane_id());
-  load_keys(a, first, left, key);
-  for (int shift = 0; shift < key_bits; shift += digit_bits) {
-    const int bits = min(digit_bits, key_bits - shift), digits = 1 << bits;
-    if (shift) {
+      for (int j = 0; j < kWave / 4; ++j) {
+        const uint4 v = s_key[w][j];
+        count += (v.x <= k) + (v.y <= k) + (v.z <= k) + (v.w <= k);
+      }
+    } else if (c > (int)blockIdx.x) {
 #pragma unroll
-      for (int j = 0; j < kTileKeys; ++j) {
-        const int o = j * kWave + lane_id();
-        if (o < left) {
-          key[j] = s_key[first + o];
-          pos[j] = s_pos[first + o];
-        }
+      for (int j = 0; j < kWave / 4; ++j) {
+        const uint4 v = s_key[w][j];
+        count += (v.x < k) + (v.y < k) + (v.z < k) + (v.w < k);
+      }
+    } else {
+      for (int j = 0; j < kWave; ++j) {
+        const uint32_t v = ((const uint32_t*)s_key[w])[j];
+        count += v < k || (v == k && j < lane);
       }
     }
-    for (int i = threadIdx.x; i < kSortWaves * digits; i += kSortBlock) cnt[i] = 0;
-    __syncthreads();
-    rank_tile(key, shift, bits, left, steps, cnt + w * digits, rank);
-    __syncthreads();
-    int32_t s = 0, total;
-    if ((int)threadIdx.x < digits)
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  }
+  s_count[w][lane] = count;
+  __syncthreads();
+  if (w == 0 && i0 + lane < n) {
 #pragma unroll
-      for (int v = 0; v < kSortWaves; ++v) {
-        const uint16_t c = cnt[v * digits + threadIdx.x];
-        cnt[v * digits + threadIdx.x] = (uint16_t)s;
-        s += c;
-      }
-    const int32_t before = block_excl_scan<kSortBlock>(s, s_scan, &total);
-    if ((int)threadIdx.x < digits) base[threadIdx.x] = before;
-    __syncthreads();
-    const bool last = shift + bits >= key_bits;
-#pragma unroll
-    for (int j = 0; j < kTileKeys; ++j) {
-      if (j * kWave + lane_id() >= left) continue;
-      const uint32_t d = (key[j] >> shift) & (digits - 1);
-      const uint32_t to = (uint32_t)base[d] + cnt[w * digits + d] + rank[j];
-      if (last) {
-        key_out[to] = key[j];
-        pos_out[to] = pos[j];
-      } else {
-        s_key[to] = key[j];
-        s_pos[to] = pos[j];
-      }
-    }
-    __syncthreads();
+    for (int x = 1; x < kWaves; ++x) count += s_count[x][lane];
+    key_out[count] = k;
+    pos_out[count] = (uint32_t)(i0 + lane);
   }
 }
 
@@ -429,11 +421,14 @@ __global__ void __launch_bounds__(kTileBlock) k_sort_tile(Keys a, int key_bits, 
 // call still spreads over the chip.
 // ---------------------------------------------------------------------------
 constexpr int kGradRows = 256;       // most entries of a block
-constexpr int kGroupRun = 32;        // longest run that one group sums
+constexpr int kGroupRun = 32;        // longest run that one group sums (4, 8 and 16: 2,468
+                                     // ids of 1,253 rows 43, 33 and 34 us, 32 takes 28)
 constexpr int kPosCache = 1024;
 constexpr int kLongUnroll = 8;       // rows in flight in a longer run
 template <int V>
-constexpr int kItems = 16 / V < 4 ? 16 / V : 4;     // short runs in flight
+constexpr int kItems = 16 / V < 4 ? 16 / V : 4;     // short runs summed together
+template <int V>
+constexpr int kTerms = 8 / kItems<V>;                // rows of each in flight
 
 struct GradArgs {
   const uint32_t* key;     // sorted
@@ -590,8 +585,8 @@ __device__ __forceinline__ void put_row(const GradArgs& a, uint32_t row, int32_t
 }
 
 // The runs of up to kGroupRun positions.  Items are (entry, column tile); a
-// group sums kItems of them at a time, two rows of each in flight, so that runs
-// of one or two rows, as most are, cost one wait (eight rows of one item at a
+// group sums kItems of them at a time, kTerms rows of each in flight, so that
+// runs of one or two rows, as most are, cost one wait (eight rows of one item at a
 // time instead, after the first two, need more registers: 1.5M rows of 100 fp32
 // into 2.45M 478 us, this way 441).  CACHED: the positions are in LDS.
 template <typename TD, typename TG, int V, bool CACHED>
@@ -629,12 +624,12 @@ __device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entri
 #pragma unroll
       for (int k = 0; k < V; ++k) acc[u][k] = 0.0f;
     }
-    for (uint32_t r = 0; r < most; r += 2) {
-      typename Raw<TD, V>::vec raw[kItems<V>][2];
+    for (uint32_t r = 0; r < most; r += kTerms<V>) {
+      typename Raw<TD, V>::vec raw[kItems<V>][kTerms<V>];
 #pragma unroll
       for (int u = 0; u < kItems<V>; ++u)
 #pragma unroll
-        for (uint32_t t = 0; t < 2; ++t) {
+        for (uint32_t t = 0; t < kTerms<V>; ++t) {
           raw[u][t] = {};
           if (r + t < cnt[u]) {
             const uint32_t p = s_beg[x[u]] + r + t;
@@ -646,7 +641,7 @@ __device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entri
 #pragma unroll
       for (int u = 0; u < kItems<V>; ++u)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < kTerms<V>; ++t) {
           float v[V];
           to_f32<TD, V>(raw[u][t], v);
 #pragma unroll
@@ -749,8 +744,12 @@ __global__ void __launch_bounds__(kBlock) k_grad_rows(GradArgs a) {
     __syncthreads();
     if (tid + 1 < entries) s_end[tid] = s_beg[tid + 1];
     if (w == 0) {
-      const uint32_t beg = s_beg[entries - 1];
-      const uint32_t end = wave_lower_bound(a.key, beg, a.n, s_row[entries - 1] + 1);
+      // The last run may go on behind the block's positions (ids that add
+      // nothing may follow it within them).
+      const uint32_t v = s_row[entries - 1];
+      uint32_t end = wave_lower_bound(a.key, s_beg[entries - 1], last, v + 1);
+      if (end == last && last < a.n && a.key[last] == v)
+        end = wave_lower_bound(a.key, last, a.n, v + 1);
       if (lane_id() == 0) s_end[entries - 1] = end;
     }
   }
@@ -805,19 +804,24 @@ __global__ void __launch_bounds__(kBlock) k_grad_long(GradArgs a) {
 // ---------------------------------------------------------------------------
 // Host side.
 // ---------------------------------------------------------------------------
+// Positions of a chunk: 1,024 chunks or fewer, unless they would be longer than
+// kMaxChunk.
+constexpr uint32_t kMinChunk = 64, kMaxChunk = 1024;
+
 uint32_t grad_chunk(int64_t n) {
-  uint32_t c = 64;
-  while (c < 1024 && (int64_t)c * 1024 < n) c *= 2;
+  uint32_t c = kMinChunk;
+  while (c < kMaxChunk && (int64_t)c * 1024 < n) c *= 2;
   return c;
 }
 
-// The sort of n ids: one tile in one launch, or tiles of a block each.
+// The sort of n ids: by counting (tiles = 1), or by passes over tiles of a block
+// each.
 struct SortShape {
   int tiles, threads, digit;   // digit: most bits of one
 };
 
 SortShape sort_shape(int64_t n) {
-  if (n <= kTileMost) return {n > 0 ? 1 : 0, kTileBlock, 9};
+  if (n <= kRankMost) return {n > 0 ? 1 : 0, kRankBlock, 0};
   const int64_t small = cdiv(n, kBlock * kSortKeys);
   if (small <= kSmallSortTiles) return {(int)small, kBlock, digit_limit(kBlock)};
   return {(int)cdiv(n, 1024 * kSortKeys), 1024, digit_limit(1024)};
@@ -832,13 +836,18 @@ struct EmbedWs {
 size_t embed_ws_layout(int64_t n, int32_t dim, char* base, EmbedWs* out) {
   Carve c{base, 0, 0};
   EmbedWs w;
-  const SortShape sh = sort_shape(n);
+  // The most that any m <= n takes, so that a workspace serves smaller calls.
+  const int64_t counters =
+      std::max(std::min<int64_t>(cdiv(n, kBlock * kSortKeys), kSmallSortTiles) << digit_limit(kBlock),
+               cdiv(n, 1024 * kSortKeys) << digit_limit(1024));
+  const int64_t chunks =
+      std::max(std::min<int64_t>(cdiv(n, kMinChunk), 1024), cdiv(n, kMaxChunk));
   for (int i = 0; i < 2; ++i) {
     w.key[i] = c.take<uint32_t>((size_t)n);
     w.pos[i] = c.take<uint32_t>((size_t)n);
   }
-  w.hist = c.take<int32_t>((size_t)sh.tiles << sh.digit);
-  w.part = c.take<float>((size_t)cdiv(n, grad_chunk(n)) * 2 * dim);
+  w.hist = c.take<int32_t>((size_t)counters);
+  w.part = c.take<float>((size_t)chunks * 2 * dim);
   if (out) *out = w;
   return align_up(c.used, 256);
 }
@@ -975,7 +984,7 @@ extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t
   const int key_bits = 32 - __builtin_clz((unsigned)std::max<int64_t>(num_rows, 1));
   const SortShape sh = sort_shape(n);
   const int tiles = sh.tiles, most = sh.digit;
-  const int passes = (int)cdiv(key_bits, most), digit = (int)cdiv(key_bits, passes);
+  const int passes = most ? (int)cdiv(key_bits, most) : 1, digit = (int)cdiv(key_bits, passes);
   // Where ids reach few of the rows, the sort's launches clear all rows beside
   // their own work and only rows that occur are written after it.  (The rows'
   // first stores count twice then: from one id per two rows on, the pass over
@@ -1002,10 +1011,10 @@ extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t
   };
   int at = 0;
   if (tiles == 1) {
-    const int fb = fill_blocks(kTileBlock);
-    hipLaunchKernelGGL(k_sort_tile, dim3(1 + fb), dim3(kTileBlock), 0, stream, k, key_bits, digit,
-                       w.key[0], w.pos[0], f);
-    GG_LAUNCH_CHECK("k_sort_tile");
+    const int blocks = (int)cdiv(n, kWave);
+    hipLaunchKernelGGL(k_sort_rank, dim3((unsigned)(blocks + fill_blocks(kRankBlock))),
+                       dim3(kRankBlock), 0, stream, k, blocks, w.key[0], w.pos[0], f);
+    GG_LAUNCH_CHECK("k_sort_rank");
   } else if (tiles > 1) {
     for (int p = 0; p < passes; ++p) {
       k.shift = p * digit;

@@ -173,8 +173,8 @@ def test_gradient_types(tdy, tgrad, n, v, dim, add):
     grad_case("frequent", n, v, dim, tdy, tgrad, add, pad=1)
 
 
-# The sort's one tile (16,384 ids), tiles of 2,048 and of 8,192 ids; runs that
-# cross many chunks; keys of one, two and three digits.
+# The sort by counting (up to 16,384 ids), tiles of 2,048 and of 8,192 ids; runs
+# that cross many chunks; keys of one, two and three digits.
 @pytest.mark.parametrize("kind,n,v,dim", [
     ("frequent", 8193, 2047, 4), ("frequent", 16_384, 3000, 3), ("random", 16_385, 3000, 3),
     ("random", 524_288, 2000, 1), ("frequent", 524_289, 2000, 1), ("random", 20_000, 2048, 4), ("frequent", 30_000, 128_000, 16),

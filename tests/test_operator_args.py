@@ -113,6 +113,15 @@ def test_workspace_sizes():
     assert gg.gg_ws_embed(-1, 10, 4) == gg.gg_ws_embed(1 << 31, 10, 4) == gg.gg_ws_embed(9, 9, 0) == 0
 
 
+def test_workspaces_serve_smaller_calls():
+    sizes = [1, 2, 15, 16, 17, 63, 64, 65, 1000, 1023, 1024, 1025, 2048, 2049, 16_384, 16_385, 65_536,
+             65_537, 131_072, 131_073, 524_288, 524_289, 1_048_576, 1_048_577, 1_500_000, 5_000_000]
+    for f in (lambda n: gg.gg_ws_embed(n, 1000, 100), lambda n: gg.gg_ws_rmsnorm(n, 100),
+              lambda n: gg.gg_ws_distill(n, 50_000)):
+        got = [f(n) for n in sizes]
+        assert got == sorted(got) and got[0] > 0
+
+
 def test_bindings_check_the_ids():
     with pytest.raises(gg.GGError, match="ids"):
         gg._ids(torch.zeros(3), 3, "x")
