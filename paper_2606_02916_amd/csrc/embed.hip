@@ -122,7 +122,13 @@ constexpr int kSmallSortTiles = 256;              // most tiles of 4-wave blocks
 constexpr int digit_limit(int nt) { return nt == 1024 ? 8 : 9; }
 
 // Rows to be cleared by the sort's launches, in blocks behind its own: the sort
-// waits for memory more than it uses it.
+// waits for memory more than it uses it.  Rows that lie back to back are one
+// run of 16-byte pieces, which a block clears 8 pieces a lane in one place: past
+// the caches, so that what the sort and the sums read stays there (32,768 ids
+// and 128,000 x 2,048 bf16 rows 140 us, through the caches 164; one piece a lane
+// in one place 151).
+constexpr int kFillRun = 8;
+
 struct FillArgs {
   char* p;
   int64_t stride;
@@ -132,13 +138,29 @@ struct FillArgs {
 
 template <int NT>
 __device__ void fill_rows_with_zeros(const FillArgs& f, uint32_t block, uint32_t blocks) {
+  typedef Raw<f16, 8>::vec vec;
+  typedef Raw<f16, 8>::mem mem;
+  if (f.stride == f.row_bytes) {
+    char* p = f.p + f.r0 * f.stride;
+    const int64_t bytes = (f.r1 - f.r0) * f.stride, n = bytes / 16;
+    constexpr int kRun = NT * kFillRun;      // pieces that a block clears in one place
+    for (int64_t i0 = (int64_t)block * kRun; i0 < n; i0 += (int64_t)blocks * kRun)
+#pragma unroll
+      for (int u = 0; u < kFillRun; ++u) {
+        const int64_t i = i0 + u * NT + threadIdx.x;
+        if (i < n) __builtin_nontemporal_store(vec{}, (GG_GLOBAL mem*)(p + i * 16));
+      }
+    if (block == 0 && threadIdx.x < (bytes - n * 16) / 2)
+      *(GG_GLOBAL uint16_t*)(p + n * 16 + threadIdx.x * 2) = 0;
+    return;
+  }
   const int groups = NT >> f.lanes_log, lanes = 1 << f.lanes_log;
   const int g = threadIdx.x >> f.lanes_log, l = threadIdx.x & (lanes - 1);
   for (int64_t r = f.r0 + (int64_t)block * groups + g; r < f.r1; r += (int64_t)blocks * groups) {
     char* p = f.p + r * f.stride;
     for (int32_t c = l; c < f.pieces; c += lanes) {
       if (f.row_bytes >= 16)
-        *(GG_GLOBAL Raw<f16, 8>::mem*)(p + min(c * 16, f.row_bytes - 16)) = Raw<f16, 8>::vec{};
+        *(GG_GLOBAL mem*)(p + min(c * 16, f.row_bytes - 16)) = vec{};
       else
         *(GG_GLOBAL uint16_t*)(p + 2 * c) = 0;
     }
@@ -852,7 +874,7 @@ size_t embed_ws_layout(int64_t n, int32_t dim, char* base, EmbedWs* out) {
   return align_up(c.used, 256);
 }
 
-constexpr int kFillLanes = 256 * 1024;      // most lanes that clear rows in a launch
+constexpr int kFillLanes = 1024 * 1024;      // most lanes that clear rows in a launch
 
 struct Lanes {
   int32_t pieces, lanes_log, tiles;
