@@ -611,7 +611,7 @@ __device__ __forceinline__ void put_row(const GradArgs& a, uint32_t row, int32_t
 // runs of one or two rows, as most are, cost one wait (eight rows of one item at a
 // time instead, after the first two, need more registers: 1.5M rows of 100 fp32
 // into 2.45M 478 us, this way 441).  CACHED: the positions are in LDS.
-template <typename TD, typename TG, int V, bool CACHED>
+template <typename TD, typename TG, int V, bool CACHED, bool ADD>
 __device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entries,
                                                const uint32_t* s_row, const uint32_t* s_beg,
                                                const uint32_t* s_end, const uint32_t* s_pos,
@@ -639,8 +639,7 @@ __device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entri
       }
       if (e[u] < 0) cnt[u] = 0;
       most = max(most, cnt[u]);
-      old[u] = {};
-      if (a.add && e[u] >= 0)
+      if (ADD && e[u] >= 0)
         old[u] = raw_load<TG, V>(a.grad.p + (int64_t)s_row[x[u]] * a.grad.stride +
                                  e[u] * (int64_t)sizeof(TG));
 #pragma unroll
@@ -673,10 +672,14 @@ __device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entri
 #pragma unroll
     for (int u = 0; u < kItems<V>; ++u) {
       if (e[u] < 0) continue;
-      float was[V];
-      to_f32<TG, V>(old[u], was);
 #pragma unroll
-      for (int k = 0; k < V; ++k) acc[u][k] = acc[u][k] * a.scale + was[k];
+      for (int k = 0; k < V; ++k) acc[u][k] *= a.scale;
+      if constexpr (ADD) {
+        float was[V];
+        to_f32<TG, V>(old[u], was);
+#pragma unroll
+        for (int k = 0; k < V; ++k) acc[u][k] += was[k];
+      }
       row_store<TG, V>(a.grad.p + (int64_t)s_row[x[u]] * a.grad.stride +
                            e[u] * (int64_t)sizeof(TG), acc[u]);
     }
@@ -685,8 +688,12 @@ __device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entri
 
 // The first blocks sum the chunks' parts of long runs, a column tile each; the
 // others have rows of the gradient.
-template <typename TD, typename TG, int V>
-__global__ void __launch_bounds__(kBlock) k_grad_rows(GradArgs a) {
+// ADD: rows are added to.  (A kernel of its own: what the rows hold takes
+// registers, and 96 leave five waves a SIMD; in one kernel for both, 104, 1.5M
+// rows of 100 fp32 into 2.45M took 462 us and now take 420.)
+template <typename TD, typename TG, int V, bool ADD>
+__global__ void __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(5)))
+k_grad_rows(GradArgs a) {
   __shared__ float lds[V * kBlock];
   __shared__ uint32_t s_run[2][2];
   if (blockIdx.x < a.part_blocks) {
@@ -780,9 +787,9 @@ __global__ void __launch_bounds__(kBlock) k_grad_rows(GradArgs a) {
   const int lanes = 1 << a.lanes_log, groups = kBlock >> a.lanes_log;
   const int g = tid >> a.lanes_log, l = tid & (lanes - 1);
   if (cached || entries == 0)
-    sum_short_runs<TD, TG, V, true>(a, entries, s_row, s_beg, s_end, s_pos, p0, &s_many);
+    sum_short_runs<TD, TG, V, true, ADD>(a, entries, s_row, s_beg, s_end, s_pos, p0, &s_many);
   else
-    sum_short_runs<TD, TG, V, false>(a, entries, s_row, s_beg, s_end, s_pos, p0, &s_many);
+    sum_short_runs<TD, TG, V, false, ADD>(a, entries, s_row, s_beg, s_end, s_pos, p0, &s_many);
   __syncthreads();
   if (!s_many) return;
   int32_t skip;
@@ -922,7 +929,12 @@ int launch_grad(GradArgs& a, hipStream_t stream) {
   a.part_blocks = chunks > 1 ? (uint32_t)(chunks * a.tiles) : 0u;
   const int64_t blocks = a.part_blocks + cdiv(a.by_position ? a.n : a.rows, a.per);
   if (blocks > 0) {
-    hipLaunchKernelGGL((k_grad_rows<TD, TG, V>), dim3((unsigned)blocks), dim3(kBlock), 0, stream, a);
+    if (a.add)
+      hipLaunchKernelGGL((k_grad_rows<TD, TG, V, true>), dim3((unsigned)blocks), dim3(kBlock), 0,
+                         stream, a);
+    else
+      hipLaunchKernelGGL((k_grad_rows<TD, TG, V, false>), dim3((unsigned)blocks), dim3(kBlock), 0,
+                         stream, a);
     GG_LAUNCH_CHECK("k_grad_rows");
   }
   if (chunks > 1) {
