@@ -460,6 +460,7 @@ struct GradArgs {
   int32_t pieces;          // column pieces of a row
   int32_t lanes_log;       // lanes of a group (a power of two up to 64)
   int32_t tiles;           // column tiles of a group
+  int32_t shift;           // column tiles start at piece -shift
   uint32_t tmagic;         // div_magic(tiles)
   uint32_t per;            // rows (or positions) of a block
   uint32_t chunk;
@@ -483,6 +484,16 @@ __device__ uint32_t wave_lower_bound(const uint32_t* k, uint32_t lo, uint32_t hi
     hi = min(hi, lo + step);
   }
   return lo + (uint32_t)__popcll(__ballot(lo + lane < hi && k[lo + lane] < v));
+}
+
+// The piece of lane l of a group in a column tile; `in`: it has one (lanes
+// without one get another's).  A row's last piece and the one before it, which it
+// overlaps, are always of one tile (shift, below): a wave reads both before it
+// writes either, so that what is added to is added to once.
+__device__ __forceinline__ int32_t piece_of(const GradArgs& a, int32_t tile, int32_t l, bool* in) {
+  const int32_t p = (tile << a.lanes_log) + l - a.shift;
+  *in = (uint32_t)p < (uint32_t)a.pieces;
+  return min(max(p, 0), a.pieces - 1);
 }
 
 // Adds the rows dy[pos[p]], p = p0, p0 + step, .. < p1, to acc.
@@ -577,16 +588,16 @@ __device__ __forceinline__ void sum_parts(const GradArgs& a, uint32_t c, int32_t
   __syncthreads();
   const int lanes = 1 << a.lanes_log, groups = kBlock >> a.lanes_log;
   const int g = threadIdx.x >> a.lanes_log, l = threadIdx.x & (lanes - 1);
-  const int32_t piece = tile * lanes + l;
   int32_t skip;
-  const int32_t e = piece_start<V>(min(piece, a.pieces - 1), a.dim, &skip);
+  bool in;
+  const int32_t e = piece_start<V>(piece_of(a, tile, l, &in), a.dim, &skip);
   for (int s = 0; s < 2; ++s) {
     const uint32_t p0 = s_run[s][0], p1 = s_run[s][1];
     if (p0 >= p1) continue;
     float acc[V] = {};
     add_rows<TD, V>(a, p0 + g, p1, groups, e, acc);
     join_groups<V>(acc, lds, lanes, groups);
-    if (g == 0 && piece < a.pieces)
+    if (g == 0 && in)
       row_store<float, V>((char*)(a.part + ((int64_t)c * 2 + s) * a.dim + e), acc);
   }
 }
@@ -616,8 +627,8 @@ __device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entri
                                                const uint32_t* s_row, const uint32_t* s_beg,
                                                const uint32_t* s_end, const uint32_t* s_pos,
                                                uint32_t p0, uint32_t* many) {
-  const int lanes = 1 << a.lanes_log, groups = kBlock >> a.lanes_log;
-  const int g = threadIdx.x >> a.lanes_log, l = threadIdx.x & (lanes - 1);
+  const int groups = kBlock >> a.lanes_log;
+  const int g = threadIdx.x >> a.lanes_log, l = threadIdx.x & ((1 << a.lanes_log) - 1);
   const uint32_t items = entries * (uint32_t)a.tiles;
   for (uint32_t i0 = 0; i0 < items; i0 += groups * kItems<V>) {
     uint32_t x[kItems<V>], cnt[kItems<V>], most = 0;
@@ -628,9 +639,9 @@ __device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entri
     for (int u = 0; u < kItems<V>; ++u) {
       const uint32_t item = i0 + u * groups + g;
       x[u] = item < items ? chunk_row(item, a.tmagic) : 0u;
-      const int32_t piece = (int32_t)(item - x[u] * a.tiles) * lanes + l;
-      const bool mine = item < items && piece < a.pieces;
       int32_t skip;
+      const int32_t piece = ((int32_t)(item - x[u] * a.tiles) << a.lanes_log) + l - a.shift;
+      const bool mine = item < items && (uint32_t)piece < (uint32_t)a.pieces;
       e[u] = mine ? piece_start<V>(piece, a.dim, &skip) : -1;
       cnt[u] = s_end[x[u]] - s_beg[x[u]];
       if (cnt[u] > kGroupRun) {
@@ -797,12 +808,12 @@ k_grad_rows(GradArgs a) {
     const uint32_t beg = s_beg[x], end = s_end[x];
     if (end - beg <= kGroupRun || end - beg > a.chunk) continue;
     for (int32_t t = 0; t < a.tiles; ++t) {
-      const int32_t piece = t * lanes + l;
-      const int32_t e = piece_start<V>(min(piece, a.pieces - 1), a.dim, &skip);
+      bool in;
+      const int32_t e = piece_start<V>(piece_of(a, t, l, &in), a.dim, &skip);
       float acc[V] = {};
       add_rows<TD, V>(a, beg + g, end, groups, e, acc);
       join_groups<V>(acc, lds, lanes, groups);
-      if (g == 0 && piece < a.pieces) put_row<TG, V>(a, s_row[x], e, acc);
+      if (g == 0 && in) put_row<TG, V>(a, s_row[x], e, acc);
     }
   }
 }
@@ -821,13 +832,13 @@ __global__ void __launch_bounds__(kBlock) k_grad_long(GradArgs a) {
   const uint32_t end = wave_lower_bound(a.key, c1, a.n, k + 1);
   const int lanes = 1 << a.lanes_log, groups = kBlock >> a.lanes_log;
   const int g = threadIdx.x >> a.lanes_log, l = threadIdx.x & (lanes - 1);
-  const int32_t piece = (int32_t)blockIdx.y * lanes + l;
   int32_t skip;
-  const int32_t e = piece_start<V>(min(piece, a.pieces - 1), a.dim, &skip);
+  bool in;
+  const int32_t e = piece_start<V>(piece_of(a, (int32_t)blockIdx.y, l, &in), a.dim, &skip);
   float acc[V] = {};
   add_parts<V>(a, beg, end, g, groups, e, acc);
   join_groups<V>(acc, lds, lanes, groups);
-  if (g == 0 && piece < a.pieces) put_row<TG, V>(a, k, e, acc);
+  if (g == 0 && in) put_row<TG, V>(a, k, e, acc);
 }
 
 // ---------------------------------------------------------------------------
@@ -1089,6 +1100,9 @@ extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t
     a.pieces = l.pieces;
     a.lanes_log = l.lanes_log;
     a.tiles = l.tiles;
+    // A last piece alone in its tile gets the one before it beside it (there is
+    // room: the tile has all other lanes free).
+    a.shift = l.tiles > 1 && l.pieces % (1 << l.lanes_log) == 1 ? 1 : 0;
     a.tmagic = div_magic((uint32_t)l.tiles);
     // Rows of a block: what its groups take at a time, as far as these rows
     // have no more than 512 positions together, and more while that leaves 8,192

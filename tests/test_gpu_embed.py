@@ -186,6 +186,18 @@ def test_gradient_of_many_ids(kind, n, v, dim, add):
     grad_case(kind, n, v, dim, F32, F32, add)
 
 
+# Rows whose last piece of 16 bytes overlaps the one before it across two column
+# tiles (64 pieces each): what is added to is added to once.  Runs of one id that a
+# group, a block and several blocks sum.
+@pytest.mark.parametrize("kind,n,v", [("distinct", 500, 600), ("same", 20, 5), ("same", 50, 5),
+                                      ("same", 1000, 5), ("random", 3000, 40)])
+@pytest.mark.parametrize("tdy,tgrad,dim", [(F32, F32, 257), (F32, BF16, 258), (F32, F32, 515),
+                                           (BF16, F32, 513), (BF16, BF16, 519), (F16, F16, 1029)])
+@pytest.mark.parametrize("add", [False, True])
+def test_gradient_whose_last_piece_is_alone_in_its_tile(kind, n, v, tdy, tgrad, dim, add):
+    grad_case(kind, n, v, dim, tdy, tgrad, add, pad=1)
+
+
 def test_gradient_without_ids_clears_the_rows():
     gg = lib()
     grad, flat, own = like(1000, 33, BF16, DEV, lead=1, pad=2)
