@@ -104,22 +104,24 @@ __global__ void __launch_bounds__(kBlock) k_embed_rows(LookupArgs a) {
 // passes take the low digit first and keep the order of equal digits, so the
 // result depends on the ids alone.
 //
-// A tile of kTile pairs belongs to a block; wave w of it holds the pairs
+// A tile of pairs belongs to a block; wave w of it holds the pairs
 // [w * kTileWave, (w + 1) * kTileWave) of the tile, 64 neighbouring ones at a
 // time.  Lanes whose digits agree find each other by one ballot per digit bit,
 // so equal digits are counted and ranked without atomics.
 // ---------------------------------------------------------------------------
-constexpr int kSortKeys = 8;                      // pairs per lane
-constexpr int kTileWave = kWave * kSortKeys;
 // Up to this many pairs find their places by counting, in a single launch.
 constexpr int kRankBlock = 1024;
 constexpr int kRankMost = 16384;
-// Beyond, a tile's work is instructions, which blocks of 4 waves spread over more
-// of the chip; blocks of 16 waves keep the counters of many tiles few.  Digits
-// have up to 9 bits, and 8 in the larger blocks: ids of 18 bits in two passes,
-// 200,003 of them in 32 us instead of 44.
-constexpr int kSmallSortTiles = 256;              // most tiles of 4-wave blocks
-constexpr int digit_limit(int nt) { return nt == 1024 ? 8 : 9; }
+// Beyond, tiles of 2,048 pairs spread the instructions over the chip, two pairs a
+// lane, so that a SIMD has several waves to take them from (eight pairs a lane in
+// blocks of 4 waves: 60,000 ids of 64 fp32 60 us instead of 50, 524,000 of 16 66
+// instead of 62; four in 8 waves 52 and 66).  Every tile reads the counters of all,
+// so many ids have tiles of 8,192, with digits of 8 bits instead of 9.
+constexpr int kSmallThreads = 1024, kSmallKeys = 2;     // pairs per lane
+constexpr int kLargeThreads = 1024, kLargeKeys = 8;
+constexpr int kSmallTile = kSmallThreads * kSmallKeys, kLargeTile = kLargeThreads * kLargeKeys;
+constexpr int kSmallSortTiles = 256;                    // most small tiles
+constexpr int digit_limit(int tile) { return tile == kSmallTile ? 9 : 8; }
 
 // Rows to be cleared by the sort's launches, in blocks behind its own: the sort
 // waits for memory more than it uses it.  Rows that lie back to back are one
@@ -246,24 +248,24 @@ __device__ __forceinline__ void rank_tile(const uint32_t (&key)[K], int shift, i
 }
 
 // Digit counts of each tile: hist[tile][digit].
-template <int NT>
+template <int NT, int K>
 __global__ void __launch_bounds__(NT) k_sort_count(Keys a, int32_t* hist, int tiles,
                                                    FillArgs f) {
   if ((int)blockIdx.x >= tiles)
     return fill_rows_with_zeros<NT>(f, blockIdx.x - tiles, gridDim.x - tiles);
-  constexpr int kSortBlock = NT, kSortWaves = NT / kWave, kTile = NT * kSortKeys;
-  __shared__ uint16_t cnt[kSortWaves << digit_limit(NT)];
+  constexpr int kSortWaves = NT / kWave, kTile = NT * K, kTileWave = kWave * K;
+  __shared__ uint16_t cnt[kSortWaves << digit_limit(kTile)];
   const int digits = 1 << a.bits, w = threadIdx.x / kWave;
-  for (int i = threadIdx.x; i < kSortWaves * digits; i += kSortBlock) cnt[i] = 0;
+  for (int i = threadIdx.x; i < kSortWaves * digits; i += NT) cnt[i] = 0;
   const int64_t first = (int64_t)blockIdx.x * kTile + w * kTileWave;
   const int left = (int)min((int64_t)kTileWave, max((int64_t)0, a.n - first));
-  uint32_t key[kSortKeys];
-  uint16_t rank[kSortKeys];
+  uint32_t key[K];
+  uint16_t rank[K];
   load_keys(a, first, left, key);
   __syncthreads();
   rank_tile(key, a.shift, a.bits, left, cnt + w * digits, rank);
   __syncthreads();
-  for (int d = threadIdx.x; d < digits; d += kSortBlock) {
+  for (int d = threadIdx.x; d < digits; d += NT) {
     int32_t s = 0;
 #pragma unroll
     for (int v = 0; v < kSortWaves; ++v) s += cnt[v * digits + d];
@@ -274,16 +276,16 @@ __global__ void __launch_bounds__(NT) k_sort_count(Keys a, int32_t* hist, int ti
 // Moves a tile's pairs to their places: those of smaller digits come first,
 // then those of earlier tiles with the same digit, as the counts of all tiles
 // (hist) tell.
-template <int NT>
+template <int NT, int K>
 __global__ void __launch_bounds__(NT) k_sort_scatter(Keys a, const int32_t* hist, int tiles,
                                                      uint32_t* key_out, uint32_t* pos_out,
                                                      FillArgs f) {
   if ((int)blockIdx.x >= tiles)
     return fill_rows_with_zeros<NT>(f, blockIdx.x - tiles, gridDim.x - tiles);
-  constexpr int kSortWaves = NT / kWave, kTile = NT * kSortKeys;
-  __shared__ uint16_t cnt[kSortWaves << digit_limit(NT)];
-  __shared__ int32_t base[1 << digit_limit(NT)];
-  __shared__ uint16_t local[1 << digit_limit(NT)];     // first place of a digit in the tile
+  constexpr int kSortWaves = NT / kWave, kTile = NT * K, kTileWave = kWave * K;
+  __shared__ uint16_t cnt[kSortWaves << digit_limit(kTile)];
+  __shared__ int32_t base[1 << digit_limit(kTile)];
+  __shared__ uint16_t local[1 << digit_limit(kTile)];     // first place of a digit in the tile
   __shared__ uint32_t s_key[kTile], s_pos[kTile];
   __shared__ int2 s_mine[NT], s_all[NT];
   __shared__ uint64_t s_scan[kSortWaves];
@@ -291,13 +293,13 @@ __global__ void __launch_bounds__(NT) k_sort_scatter(Keys a, const int32_t* hist
   for (int i = tid; i < kSortWaves * digits; i += NT) cnt[i] = 0;
   const int64_t first = (int64_t)blockIdx.x * kTile + w * kTileWave;
   const int left = (int)min((int64_t)kTileWave, max((int64_t)0, a.n - first));
-  uint32_t key[kSortKeys], pos[kSortKeys];
-  uint16_t rank[kSortKeys];
+  uint32_t key[K], pos[K];
+  uint16_t rank[K];
 #pragma unroll
-  for (int j = 0; j < kSortKeys; ++j) pos[j] = (uint32_t)(first + j * kWave + lane_id());
+  for (int j = 0; j < K; ++j) pos[j] = (uint32_t)(first + j * kWave + lane_id());
   if (!a.ids) {
 #pragma unroll
-    for (int j = 0; j < kSortKeys; ++j) pos[j] = a.pos[min((int64_t)pos[j], a.n - 1)];
+    for (int j = 0; j < K; ++j) pos[j] = a.pos[min((int64_t)pos[j], a.n - 1)];
   }
   load_keys(a, first, left, key);
   // A lane adds up two neighbouring digits over a share of the tiles.
@@ -350,7 +352,7 @@ __global__ void __launch_bounds__(NT) k_sort_scatter(Keys a, const int32_t* hist
   __syncthreads();
   // The tile in order in LDS, so that a digit's pairs leave in one run.
 #pragma unroll
-  for (int j = 0; j < kSortKeys; ++j) {
+  for (int j = 0; j < K; ++j) {
     if (j * kWave + lane_id() >= left) continue;
     const uint32_t d = (key[j] >> a.shift) & (digits - 1);
     const uint32_t to = (uint32_t)local[d] + cnt[w * digits + d] + rank[j];
@@ -360,7 +362,7 @@ __global__ void __launch_bounds__(NT) k_sort_scatter(Keys a, const int32_t* hist
   __syncthreads();
   const int size = (int)min((int64_t)kTile, a.n - (int64_t)blockIdx.x * kTile);
 #pragma unroll
-  for (int j = 0; j < kSortKeys; ++j) {
+  for (int j = 0; j < K; ++j) {
     const int i = j * NT + tid;
     if (i >= size) continue;
     const uint32_t k = s_key[i], d = (k >> a.shift) & (digits - 1);
@@ -858,13 +860,15 @@ uint32_t grad_chunk(int64_t n) {
 // each.
 struct SortShape {
   int tiles, threads, digit;   // digit: most bits of one
+  bool small;
 };
 
 SortShape sort_shape(int64_t n) {
-  if (n <= kRankMost) return {n > 0 ? 1 : 0, kRankBlock, 0};
-  const int64_t small = cdiv(n, kBlock * kSortKeys);
-  if (small <= kSmallSortTiles) return {(int)small, kBlock, digit_limit(kBlock)};
-  return {(int)cdiv(n, 1024 * kSortKeys), 1024, digit_limit(1024)};
+  if (n <= kRankMost) return {n > 0 ? 1 : 0, kRankBlock, 0, true};
+  const int64_t small = cdiv(n, kSmallTile);
+  if (small <= kSmallSortTiles)
+    return {(int)small, kSmallThreads, digit_limit(kSmallTile), true};
+  return {(int)cdiv(n, kLargeTile), kLargeThreads, digit_limit(kLargeTile), false};
 }
 
 struct EmbedWs {
@@ -878,8 +882,8 @@ size_t embed_ws_layout(int64_t n, int32_t dim, char* base, EmbedWs* out) {
   EmbedWs w;
   // The most that any m <= n takes, so that a workspace serves smaller calls.
   const int64_t counters =
-      std::max(std::min<int64_t>(cdiv(n, kBlock * kSortKeys), kSmallSortTiles) << digit_limit(kBlock),
-               cdiv(n, 1024 * kSortKeys) << digit_limit(1024));
+      std::max(std::min<int64_t>(cdiv(n, kSmallTile), kSmallSortTiles) << digit_limit(kSmallTile),
+               cdiv(n, kLargeTile) << digit_limit(kLargeTile));
   const int64_t chunks =
       std::max(std::min<int64_t>(cdiv(n, kMinChunk), 1024), cdiv(n, kMaxChunk));
   for (int i = 0; i < 2; ++i) {
@@ -1067,18 +1071,20 @@ extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t
       at = p & 1;
       const dim3 threads((unsigned)sh.threads);
       dim3 grid((unsigned)(tiles + fill_blocks(sh.threads)));
-      if (sh.threads == kBlock)
-        hipLaunchKernelGGL(k_sort_count<kBlock>, grid, threads, 0, stream, k, w.hist, tiles, f);
+      if (sh.small)
+        hipLaunchKernelGGL((k_sort_count<kSmallThreads, kSmallKeys>), grid, threads, 0, stream, k,
+                           w.hist, tiles, f);
       else
-        hipLaunchKernelGGL(k_sort_count<1024>, grid, threads, 0, stream, k, w.hist, tiles, f);
+        hipLaunchKernelGGL((k_sort_count<kLargeThreads, kLargeKeys>), grid, threads, 0, stream, k,
+                           w.hist, tiles, f);
       GG_LAUNCH_CHECK("k_sort_count");
       grid.x = (unsigned)(tiles + fill_blocks(sh.threads));
-      if (sh.threads == kBlock)
-        hipLaunchKernelGGL(k_sort_scatter<kBlock>, grid, threads, 0, stream, k, w.hist, tiles,
-                           w.key[at], w.pos[at], f);
+      if (sh.small)
+        hipLaunchKernelGGL((k_sort_scatter<kSmallThreads, kSmallKeys>), grid, threads, 0, stream, k,
+                           w.hist, tiles, w.key[at], w.pos[at], f);
       else
-        hipLaunchKernelGGL(k_sort_scatter<1024>, grid, threads, 0, stream, k, w.hist, tiles,
-                           w.key[at], w.pos[at], f);
+        hipLaunchKernelGGL((k_sort_scatter<kLargeThreads, kLargeKeys>), grid, threads, 0, stream, k,
+                           w.hist, tiles, w.key[at], w.pos[at], f);
       GG_LAUNCH_CHECK("k_sort_scatter");
       k.ids = nullptr;
       k.key = w.key[at];
