@@ -452,7 +452,7 @@ constexpr int kLongUnroll = 8;       // rows in flight in a longer run
 template <int V>
 constexpr int kItems = 16 / V < 4 ? 16 / V : 4;     // short runs summed together
 template <int V>
-constexpr int kTerms = 8 / kItems<V>;                // rows of each in flight
+constexpr uint32_t kTerms = 8 / kItems<V>;           // rows of each in flight
 
 struct GradArgs {
   const uint32_t* key;     // sorted
@@ -621,9 +621,11 @@ __device__ __forceinline__ void put_row(const GradArgs& a, uint32_t row, int32_t
 
 // The runs of up to kGroupRun positions.  Items are (entry, column tile); a
 // group sums kItems of them at a time, kTerms rows of each in flight, so that
-// runs of one or two rows, as most are, cost one wait (eight rows of one item at a
-// time instead, after the first two, need more registers: 1.5M rows of 100 fp32
-// into 2.45M 478 us, this way 441).  CACHED: the positions are in LDS.
+// runs of one or two rows, as most are, cost one wait.  What is left of longer ones
+// is summed an item at a time, kLongUnroll rows in flight, where kItems are four
+// (200,003 fp32 rows of 256 into 100,000, ids by a power law, 111 us instead of
+// 124); with two, of four rows each, all go on together (32,768 bf16 rows of
+// 1,024 into 64,000 61 us, 64 the other way).  CACHED: the positions are in LDS.
 template <typename TD, typename TG, int V, bool CACHED, bool ADD>
 __device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entries,
                                                const uint32_t* s_row, const uint32_t* s_beg,
@@ -658,7 +660,9 @@ __device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entri
 #pragma unroll
       for (int k = 0; k < V; ++k) acc[u][k] = 0.0f;
     }
-    for (uint32_t r = 0; r < most; r += kTerms<V>) {
+    constexpr bool kOneByOne = kItems<V> == 4;
+    const uint32_t together = kOneByOne ? min(most, kTerms<V>) : most;
+    for (uint32_t r = 0; r < together; r += kTerms<V>) {
       typename Raw<TD, V>::vec raw[kItems<V>][kTerms<V>];
 #pragma unroll
       for (int u = 0; u < kItems<V>; ++u)
@@ -675,11 +679,35 @@ __device__ __forceinline__ void sum_short_runs(const GradArgs& a, uint32_t entri
 #pragma unroll
       for (int u = 0; u < kItems<V>; ++u)
 #pragma unroll
-        for (int t = 0; t < kTerms<V>; ++t) {
+        for (uint32_t t = 0; t < kTerms<V>; ++t) {
           float v[V];
           to_f32<TD, V>(raw[u][t], v);
 #pragma unroll
           for (int k = 0; k < V; ++k) acc[u][k] += v[k];
+        }
+    }
+    if (kOneByOne && most > kTerms<V>) {
+#pragma unroll
+      for (int u = 0; u < kItems<V>; ++u)
+        for (uint32_t r = kTerms<V>; r < cnt[u]; r += kLongUnroll) {
+          typename Raw<TD, V>::vec raw[kLongUnroll];
+#pragma unroll
+          for (uint32_t t = 0; t < kLongUnroll; ++t) {
+            raw[t] = {};
+            if (r + t < cnt[u]) {
+              const uint32_t p = s_beg[x[u]] + r + t;
+              const uint32_t at = CACHED ? s_pos[p - p0] : a.pos[p];
+              raw[t] = raw_load<TD, V>(a.dy.p + (int64_t)at * a.dy.stride +
+                                       e[u] * (int64_t)sizeof(TD));
+            }
+          }
+#pragma unroll
+          for (uint32_t t = 0; t < kLongUnroll; ++t) {
+            float v[V];
+            to_f32<TD, V>(raw[t], v);
+#pragma unroll
+            for (int k = 0; k < V; ++k) acc[u][k] += v[k];
+          }
         }
     }
 #pragma unroll
