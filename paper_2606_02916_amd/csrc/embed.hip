@@ -925,6 +925,7 @@ size_t embed_ws_layout(int64_t n, int32_t dim, char* base, EmbedWs* out) {
 }
 
 constexpr int kFillLanes = 1024 * 1024;      // most lanes that clear rows in a launch
+constexpr int64_t kClearBytes = 320LL << 20;
 
 struct Lanes {
   int32_t pieces, lanes_log, tiles;
@@ -1062,16 +1063,22 @@ extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t
   const SortShape sh = sort_shape(n);
   const int tiles = sh.tiles, most = sh.digit;
   const int passes = most ? (int)cdiv(key_bits, most) : 1, digit = (int)cdiv(key_bits, passes);
-  // Where ids reach few of the rows, the sort's launches clear all rows beside
-  // their own work and only rows that occur are written after it.  (The rows'
-  // first stores count twice then: from one id per two rows on, the pass over
-  // all rows is faster.)
-  a.by_position = a.add || (n > 0 && n * 2 <= num_rows);
+  // Either the sort's launches clear all rows beside their own work and only rows
+  // that occur are written after it, or the pass after it goes over all rows.
+  // Clearing is faster where ids reach few of the rows (from one id per two rows
+  // on their first stores count twice), and where the sort's launches hide
+  // all of it, up to kClearBytes (fp32 rows into 200,000, 200,003 ids of a window:
+  // of 256 115 us, 120 by rows; of 384 161, 162; of 512 207, 199; of 602 294, 262;
+  // ids by a power law of 256 105, 138; one launch hides less: 16,000 bf16 rows
+  // of 2,048 58, 50).  Many ids to a row leave nothing to clear: 1M in 5,000 95, 90.
+  const int32_t row_bytes = dim * (int32_t)elem_bytes(grad->dtype);
+  const bool hidden = tiles > 1 && n <= 8 * num_rows && num_rows * row_bytes <= kClearBytes;
+  a.by_position = a.add || (n > 0 && (n * 2 <= num_rows || hidden));
   const bool clear = a.by_position && !a.add;
   FillArgs f = {};
   f.p = a.grad.p;
   f.stride = a.grad.stride;
-  f.row_bytes = dim * (int32_t)elem_bytes(grad->dtype);
+  f.row_bytes = row_bytes;
   const Lanes fl = lanes_of(f.row_bytes, f.row_bytes >= 16 ? 16 : 2);
   f.pieces = fl.pieces;
   f.lanes_log = fl.lanes_log;
