@@ -17,6 +17,7 @@ struct DistillArgs {
   const char* ids;             // row r's at ids + r * ids_stride
   int64_t ids_stride;
   int32_t ids64, k;
+  int32_t kp;                  // k rounded up to 4: entries in LDS
   int32_t top_dtype;
   int32_t vocab;
   int64_t n;
@@ -66,6 +67,10 @@ __device__ __forceinline__ float exp_of(float z, const Soft& s) {
 __device__ __forceinline__ float factor(const Soft& a, const Soft& t) {
   if (a.m == t.m) return 1.0f;
   return a.coarse || t.coarse || a.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(a.b - t.b);
+}
+
+__device__ __forceinline__ float weight_of(const DistillArgs& a, int64_t row) {
+  return a.row_w ? a.weight * a.row_w[row] : a.weight;
 }
 
 struct MaxSum {
@@ -119,52 +124,71 @@ __device__ __forceinline__ Entries entries_at(char* lds, int group, int k) {
   return {(int32_t*)at, (float*)(at + 4 * k), (float*)(at + 8 * k), (float*)(at + 12 * k)};
 }
 
+template <typename T>
 struct Held {
-  int32_t id[kPerLane];
-  float t[kPerLane], z[kPerLane];
+  uint32_t lo[kPerLane], hi[kPerLane];   // words of the id; the same word of 32 bits
+  uint16_t tl[kPerLane], th[kPerLane];   // halves of the logit; the same one of 16 bits
+  int32_t id[kPerLane];                  // -1: none
+  float t[kPerLane];
+  typename Raw<T, 1>::vec z[kPerLane];   // the row's own logit there
 };
 
+// Issues the loads of ids and logits of any width, without a branch that would
+// wait for them; lanes behind the last entry repeat it.
+template <typename T>
 __device__ __forceinline__ void load_entries(const DistillArgs& a, int64_t row, int l, int lanes,
-                                             Held& h) {
-  const char* ids = a.ids + row * a.ids_stride;
-  const char* tp = a.top.p + row * a.top.stride;
+                                             Held<T>& h) {
+  const auto* ids = (const GG_GLOBAL uint32_t*)(a.ids + row * a.ids_stride);
+  const auto* tp = (const GG_GLOBAL uint16_t*)(a.top.p + row * a.top.stride);
+  const int iw = a.ids64 ? 2 : 1, tw = a.top_dtype == GG_F32 ? 2 : 1;
+#pragma unroll
+  for (int u = 0; u < kPerLane; ++u) {
+    h.lo[u] = h.hi[u] = 0;
+    h.tl[u] = h.th[u] = 0;
+    if (u * lanes < a.k) {
+      const int j = min(u * lanes + l, a.k - 1);
+      h.lo[u] = ids[j * iw];
+      h.hi[u] = ids[j * iw + iw - 1];
+      h.tl[u] = tp[j * tw];
+      h.th[u] = tp[j * tw + tw - 1];
+    }
+  }
+}
+
+// Their values, and the loads of the row's logits at them (of the first where
+// there is no entry).
+template <typename T>
+__device__ __forceinline__ void take_entries(const DistillArgs& a, int64_t row, int l, int lanes,
+                                             Held<T>& h) {
+  const char* zp = a.z.p + row * a.z.stride;
   bool bad = false;
 #pragma unroll
   for (int u = 0; u < kPerLane; ++u) {
-    const int j = u * lanes + l;
     h.id[u] = -1;
     h.t[u] = -INFINITY;
-    if (j < a.k) {
-      const int64_t id = a.ids64 ? ((const int64_t*)ids)[j] : (int64_t)((const int32_t*)ids)[j];
-      float t[1];
-      GG_FOR_FLOAT(a.top_dtype, TT, { row_load<TT, 1>(tp + j * (int64_t)sizeof(TT), t); });
-      const bool in = (uint64_t)id < (uint64_t)a.vocab;
-      bad |= !in && id != -1;
-      if (in) {
-        h.id[u] = (int32_t)id;
-        h.t[u] = t[0];
+    h.z[u] = {};
+    if (u * lanes < a.k) {
+      const bool own = u * lanes + l < a.k;
+      const bool in = h.lo[u] < (uint32_t)a.vocab && (!a.ids64 || h.hi[u] == 0);
+      bad |= own && !in && (h.lo[u] & h.hi[u]) != ~0u;
+      const float wide = __uint_as_float((uint32_t)h.th[u] << 16 |
+                                         (a.top_dtype == GG_F32 ? h.tl[u] : 0u));
+      const float half = (float)__builtin_bit_cast(f16, h.th[u]);
+      if (own && in) {
+        h.id[u] = (int32_t)h.lo[u];
+        h.t[u] = a.top_dtype == GG_F16 ? half : wide;
       }
+      h.z[u] = raw_load<T, 1>(zp + max(h.id[u], 0) * (int64_t)sizeof(T));
     }
   }
   if (bad) set_status(a.status, GG_DEV_BAD_ID);
 }
 
-template <typename T>
-__device__ __forceinline__ void load_entry_logits(const DistillArgs& a, int64_t row, Held& h) {
-  const char* zp = a.z.p + row * a.z.stride;
-#pragma unroll
-  for (int u = 0; u < kPerLane; ++u) {
-    float z[1] = {0.0f};
-    if (h.id[u] >= 0) row_load<T, 1>(zp + h.id[u] * (int64_t)sizeof(T), z);
-    h.z[u] = z[0];
-  }
-}
-
 // Whether the row has a lesson: an entry with a logit above -infinity, and a
 // weight.  SUM: p is summed over equal ids (for the gradient).
-template <bool SUM>
-__device__ __forceinline__ bool share_entries(const DistillArgs& a, int64_t row, int l, int lanes,
-                                              const Held& h, const Entries& en) {
+template <bool SUM, typename T>
+__device__ __forceinline__ bool share_entries(const DistillArgs& a, float weight, int l, int lanes,
+                                              const Held<T>& h, const Entries& en) {
   float tm = h.t[0];
 #pragma unroll
   for (int u = 1; u < kPerLane; ++u) tm = fmaxf(tm, h.t[u]);
@@ -176,7 +200,7 @@ __device__ __forceinline__ bool share_entries(const DistillArgs& a, int64_t row,
 #pragma unroll
   for (int u = 0; u < kPerLane; ++u) {
     const int j = u * lanes + l;
-    if (j < a.k) {
+    if (j < a.kp) {
       const float lp = __builtin_fmaf(h.t[u], f.c2, -f.b) - log_total;
       en.id[j] = h.id[u];
       en.lp[j] = lp;
@@ -186,25 +210,33 @@ __device__ __forceinline__ bool share_entries(const DistillArgs& a, int64_t row,
   if constexpr (SUM) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     float p[kPerLane] = {};
-    for (int x = 0; x < a.k; ++x) {
-      const int32_t id = en.id[x];
-      const float px = en.p[x];
+#pragma unroll 4
+    for (int x = 0; x < a.kp; x += 4) {
+      const int4 id = *(const int4*)(en.id + x);
+      const float4 px = *(const float4*)(en.p + x);
 #pragma unroll
-      for (int u = 0; u < kPerLane; ++u) p[u] += h.id[u] == id ? px : 0.0f;
+      for (int u = 0; u < kPerLane; ++u)
+        if (u * lanes < a.k) {
+          p[u] += h.id[u] == id.x ? px.x : 0.0f;
+          p[u] += h.id[u] == id.y ? px.y : 0.0f;
+          p[u] += h.id[u] == id.z ? px.z : 0.0f;
+          p[u] += h.id[u] == id.w ? px.w : 0.0f;
+        }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
     for (int u = 0; u < kPerLane; ++u)
       if (u * lanes + l < a.k) en.p[u * lanes + l] = p[u];
   }
-  return f.m != -INFINITY && (a.row_w ? a.row_w[row] : 1.0f) * a.weight != 0.0f;
+  return f.m != -INFINITY && weight != 0.0f;
 }
 
-__device__ __forceinline__ void share_logits(const DistillArgs& a, int l, int lanes, const Held& h,
-                                             const Entries& en) {
+template <typename T>
+__device__ __forceinline__ void share_logits(const DistillArgs& a, int l, int lanes,
+                                             const Held<T>& h, const Entries& en) {
 #pragma unroll
   for (int u = 0; u < kPerLane; ++u)
-    if (u * lanes + l < a.k) en.z[u * lanes + l] = h.z[u];
+    if (u * lanes + l < a.k) en.z[u * lanes + l] = h.id[u] < 0 ? 0.0f : (float)h.z[u];
 }
 
 // sum_k p_k (log p_k - z_k / T + lse), by the same lanes.
@@ -244,41 +276,46 @@ enum { kLossOnly = 0, kFused = 1, kBackward = 2 };
 template <typename R, int N>
 __device__ __forceinline__ void keep_packed(R (&raw)[N]) {
 #pragma unroll
-  for (int t = 0; t < N; ++t) {
-    auto w = __builtin_bit_cast(u32x4, raw[t]);
-    asm volatile("" : "+v"(w));
-    raw[t] = __builtin_bit_cast(R, w);
-  }
+  for (int t = 0; t < N; ++t)
+    if constexpr (sizeof(R) == 16) {
+      auto w = __builtin_bit_cast(u32x4, raw[t]);
+      asm volatile("" : "+v"(w));
+      raw[t] = __builtin_bit_cast(R, w);
+    }
 }
 
 template <typename T, int V, int STEPS, bool BLK, int MODE>
 __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArgs a) {
-  extern __shared__ char lds[];
+  extern __shared__ __align__(16) char lds[];
   __shared__ float2 s_part[1024 / kWave];
   __shared__ int32_t s_has;
   const int lanes = BLK ? (int)blockDim.x : 1 << a.lanes_log;
   const int64_t row = BLK ? block_index() : (block_index() * kBlock + threadIdx.x) >> a.lanes_log;
   if (row >= a.n) return;
   const int l = BLK ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1);
+  constexpr int kPiece = V * (int)sizeof(T);
   const int pieces = a.vocab / V, rest = a.vocab - pieces * V;
   const char* zp = a.z.p + row * a.z.stride;
 
   const int el = BLK ? min(lanes, kWave) : lanes;     // lanes that read the entries
-  const Entries en = entries_at(lds, BLK ? 0 : (int)threadIdx.x >> a.lanes_log, a.k);
-  Held held;
+  const Entries en = entries_at(lds, BLK ? 0 : (int)threadIdx.x >> a.lanes_log, a.kp);
+  Held<T> held;
   if (l < el) load_entries(a, row, l, el, held);
+  const float weight = weight_of(a, row);
+  // (lanes behind the last piece repeat it: a load in a branch would be waited for
+  // with the entries)
   typename Raw<T, V>::vec raw[STEPS];
 #pragma unroll
   for (int t = 0; t < STEPS; ++t)
-    if (t * lanes + l < pieces) raw[t] = raw_load<T, V>(zp + (int64_t)(t * lanes + l) * 16);
-  float last[1] = {-INFINITY};
-  if (l < rest) row_load<T, 1>(zp + (pieces * V + l) * (int64_t)sizeof(T), last);
+    raw[t] = raw_load<T, V>(zp + (int64_t)min(t * lanes + l, pieces - 1) * kPiece);
+  const auto raw_last = raw_load<T, 1>(zp + min(pieces * V + l, a.vocab - 1) * (int64_t)sizeof(T));
   bool has = false;
   if (l < el) {
-    load_entry_logits<T>(a, row, held);
-    has = share_entries<MODE != kLossOnly>(a, row, l, el, held, en);
+    take_entries(a, row, l, el, held);
+    has = share_entries<MODE != kLossOnly>(a, weight, l, el, held, en);
     if (BLK && l == 0) s_has = has;
   }
+  const float last[1] = {l < rest ? (float)raw_last : -INFINITY};
 
   // Softmax statistics: q_j = inv * exp_of(z_j, top).
   Soft top;
@@ -328,7 +365,6 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
   }
   if (BLK) has = s_has;
   has = has && !empty;
-  const float weight = a.weight * (a.row_w ? a.row_w[row] : 1.0f);
   if constexpr (MODE != kBackward) {
     if (l < el) {
       const float v = has ? lesson_of(a, l, el, en, lse) : 0.0f;
@@ -345,7 +381,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
     const float zero[V] = {}, one[1] = {0.0f};
 #pragma unroll
     for (int t = 0; t < STEPS; ++t)
-      if (t * lanes + l < pieces) row_store<T, V>(dp + (int64_t)(t * lanes + l) * 16, zero);
+      if (t * lanes + l < pieces) row_store<T, V>(dp + (int64_t)(t * lanes + l) * kPiece, zero);
     if (l < rest) row_store<T, 1>(dp + (pieces * V + l) * (int64_t)sizeof(T), one);
     return;
   }
@@ -357,7 +393,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
       to_f32<T, V>(raw[t], v);
 #pragma unroll
       for (int k = 0; k < V; ++k) v[k] = ci * exp_of(v[k], top);
-      row_store<T, V>(dp + (int64_t)(t * lanes + l) * 16, v, a.past);
+      row_store<T, V>(dp + (int64_t)(t * lanes + l) * kPiece, v);
     }
   if (l < rest) {
     const float v[1] = {ci * exp_of(last[0], top)};
@@ -392,7 +428,7 @@ __device__ __forceinline__ void load_batch(const char* zp, int p, int p1,
 // gradient may take its place).
 template <typename T, int V>
 __global__ void __launch_bounds__(kBlock) k_distill_stats(DistillArgs a) {
-  extern __shared__ char lds[];
+  extern __shared__ __align__(16) char lds[];
   __shared__ float2 s_part[kBlock / kWave];
   const int64_t row = block_index() / (a.splits + 1);
   const int c = (int)(block_index() - row * (a.splits + 1));
@@ -400,11 +436,11 @@ __global__ void __launch_bounds__(kBlock) k_distill_stats(DistillArgs a) {
   const int tid = threadIdx.x;
   if (c == a.splits) {
     if (tid >= kWave) return;
-    const Entries en = entries_at(lds, 0, a.k);
-    Held held;
+    const Entries en = entries_at(lds, 0, a.kp);
+    Held<T> held;
     load_entries(a, row, tid, kWave, held);
-    load_entry_logits<T>(a, row, held);
-    const bool has = share_entries<false>(a, row, tid, kWave, held, en);
+    take_entries(a, row, tid, kWave, held);
+    const bool has = share_entries<false>(a, weight_of(a, row), tid, kWave, held, en);
     share_logits(a, tid, kWave, held, en);
     const float v = lesson_of(a, tid, kWave, en, 0.0f);
     if (tid == 0) a.lesson[row] = make_float2(v, has ? 1.0f : 0.0f);
@@ -463,7 +499,7 @@ __device__ __forceinline__ MaxSum row_stats(const DistillArgs& a, int64_t row) {
 
 __device__ __forceinline__ void store_loss(const DistillArgs& a, int64_t row, float2 lesson,
                                            bool empty, float lse) {
-  const float weight = a.weight * (a.row_w ? a.row_w[row] : 1.0f);
+  const float weight = weight_of(a, row);
   a.loss[row] =
       lesson.y != 0.0f && !empty ? weight * a.temp * a.temp * (lesson.x + lse) : 0.0f;
   if (a.lse) a.lse[row] = lse;
@@ -481,7 +517,7 @@ __global__ void __launch_bounds__(kWave) k_distill_loss(DistillArgs a) {
 
 template <typename T, int V, int MODE>
 __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
-  extern __shared__ char lds[];
+  extern __shared__ __align__(16) char lds[];
   __shared__ int32_t s_has;
   const int64_t row = block_index() / a.splits;
   const int c = (int)(block_index() - row * a.splits);
@@ -491,9 +527,10 @@ __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
   const int p0 = c * a.chunk, p1 = min(pieces, p0 + a.chunk);
   const char* zp = a.z.p + row * a.z.stride;
   char* dp = a.dz.p + row * a.dz.stride;
-  const Entries en = entries_at(lds, 0, a.k);
-  Held held;
+  const Entries en = entries_at(lds, 0, a.kp);
+  Held<T> held;
   if (tid < kWave) load_entries(a, row, tid, kWave, held);
+  const float weight = weight_of(a, row);
   typename Raw<T, V>::vec raw[kSplitUnroll];
   int p = p0 + tid;
   if (p < p1) load_batch<T, V>(zp, p, p1, raw);
@@ -513,14 +550,14 @@ __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
     top = soft_of(lse * a.temp, a.c2);
   }
   if (tid < kWave) {
-    load_entry_logits<T>(a, row, held);
-    const bool has = share_entries<true>(a, row, tid, kWave, held, en);
+    take_entries(a, row, tid, kWave, held);
+    const bool has = share_entries<true>(a, weight, tid, kWave, held, en);
     share_logits(a, tid, kWave, held, en);
     if (tid == 0) s_has = has;
   }
   __syncthreads();         // and the entries' logits are read before any is overwritten
   const bool has = s_has && !empty;
-  const float scale = a.weight * (a.row_w ? a.row_w[row] : 1.0f) * a.temp, ci = scale * inv;
+  const float scale = weight * a.temp, ci = scale * inv;
   while (p < p1) {
 #pragma unroll
     for (int u = 0; u < kSplitUnroll; ++u) {
@@ -551,7 +588,14 @@ __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
 // ---------------------------------------------------------------------------
 constexpr int kMaxSplits = 64;
 constexpr int kMaxSteps = 16;         // pieces per lane of a block
-constexpr int kWaveSteps = 4;
+// A row is dealt to as few lanes as have 4 pieces each, so that a wave works on
+// several rows' entries at once, or to more (a piece a lane at most) while all rows
+// leave lanes of the chip idle: 100,000 rows of 172 fp32 take 26 us with 16 lanes
+// each and 71 with 64, 1M of 9 50 with 4 and 137 with 16.  A wave has rows of up
+// to 8 pieces a lane to itself (50,000 rows of 1,500 fp32 110 us, in blocks of 4
+// waves 190), blocks the longer ones.
+constexpr int kWaveSteps = 8;
+constexpr int64_t kFillLanes = 256 * 1024;
 // Fewer rows than this are split if they have more pieces than that: 8 rows of
 // 65,536 fp32 take 10.6 us in parts and 12.3 whole, 160 of them 27.7 and 19.8, 8 of
 // 20,000 10.4 and 9.4.
@@ -581,12 +625,14 @@ template <typename T, int MODE>
 int launch_rows(DistillArgs& a, hipStream_t stream) {
   constexpr int V = kVec<T>;
   const int pieces = a.vocab / V;
-  a.past = (int64_t)sizeof(T) * a.n * a.vocab > kStreamBytes;
   const bool split = pieces > 1024 * kMaxSteps || (a.n < kFewRows && pieces > kSplitPieces);
   if (split) {
     a.splits = split_count(a.n);
     a.chunk = (int)cdiv(pieces, a.splits);
-    const size_t lds = (size_t)a.k * kEntryBytes;
+    // (rows that stay in registers are faster through the caches: 16,384 rows of
+    // 16,001 fp32 455 and 408 us; 512 of 262,144 bf16 in parts 140 and 171)
+    a.past = (int64_t)sizeof(T) * a.n * a.vocab > kStreamBytes;
+    const size_t lds = (size_t)a.kp * kEntryBytes;
     if (MODE != kBackward) {
       hipLaunchKernelGGL((k_distill_stats<T, V>), grid_of(a.n * (a.splits + 1)), dim3(kBlock), lds,
                          stream, a);
@@ -602,33 +648,39 @@ int launch_rows(DistillArgs& a, hipStream_t stream) {
     }
     return GG_OK;
   }
-  if (pieces <= kWave * kWaveSteps) {
-    a.lanes_log = 4;
-    while (a.lanes_log < 6 && ((1 << a.lanes_log) < pieces || kPerLane << a.lanes_log < a.k))
+  // (a row's last elements, fewer than V, take a lane each)
+  a.lanes_log = V == 8 ? 3 : 2;
+  if (pieces == 0) {       // rows of less than a piece
+    while (kPerLane << a.lanes_log < a.k) ++a.lanes_log;
+    hipLaunchKernelGGL((k_distill_rows<T, 1, 1, false, MODE>),
+                       grid_of(cdiv(a.n << a.lanes_log, kBlock)), dim3(kBlock),
+                       (size_t)(kBlock >> a.lanes_log) * a.kp * kEntryBytes, stream, a);
+  } else if (pieces <= kWave * kWaveSteps) {
+    while (a.lanes_log < 6 &&
+           (kPerLane << a.lanes_log < a.k || 4 << a.lanes_log < pieces ||
+            ((1 << a.lanes_log) < pieces && a.n << a.lanes_log < kFillLanes)))
       ++a.lanes_log;
     const int steps = (int)cdiv(pieces, 1 << a.lanes_log);
     const dim3 grid = grid_of(cdiv(a.n << a.lanes_log, kBlock));
-    const size_t lds = (size_t)(kBlock >> a.lanes_log) * a.k * kEntryBytes;
+    const size_t lds = (size_t)(kBlock >> a.lanes_log) * a.kp * kEntryBytes;
     if (steps <= 1)
       hipLaunchKernelGGL((k_distill_rows<T, V, 1, false, MODE>), grid, dim3(kBlock), lds, stream, a);
     else if (steps == 2)
       hipLaunchKernelGGL((k_distill_rows<T, V, 2, false, MODE>), grid, dim3(kBlock), lds, stream, a);
-    else
+    else if (steps <= 4)
       hipLaunchKernelGGL((k_distill_rows<T, V, 4, false, MODE>), grid, dim3(kBlock), lds, stream, a);
+    else
+      hipLaunchKernelGGL((k_distill_rows<T, V, kWaveSteps, false, MODE>), grid, dim3(kBlock), lds,
+                         stream, a);
   } else {
     // With fewer rows than CUs a row has a whole CU's lanes, but for short ones (3,000
     // fp32: 8.2 us with 1,024 lanes, 7.1 with 256).
     int threads = a.n < 256 && pieces > 2048 ? 1024 : 256;
     while (threads < 1024 && threads * kMaxSteps < pieces) threads *= 2;
     const int steps = (int)cdiv(pieces, threads);
-    // (a block that fills its CU waits for its own stores: 4,096 rows of 128,000
-    // bf16 411 us past the caches, 403 through them; of 32,000 97 and 108)
-    a.past = a.past && threads < 1024;
     const dim3 grid = grid_of(a.n);
-    const size_t lds = (size_t)a.k * kEntryBytes;
-    if (steps <= 2)
-      hipLaunchKernelGGL((k_distill_rows<T, V, 2, true, MODE>), grid, dim3(threads), lds, stream, a);
-    else if (steps <= 4)
+    const size_t lds = (size_t)a.kp * kEntryBytes;
+    if (steps <= 4)             // 3 at least
       hipLaunchKernelGGL((k_distill_rows<T, V, 4, true, MODE>), grid, dim3(threads), lds, stream, a);
     else if (steps <= 8)
       hipLaunchKernelGGL((k_distill_rows<T, V, 8, true, MODE>), grid, dim3(threads), lds, stream, a);
@@ -662,6 +714,7 @@ int pack_args(const gg_rows_t* z, int64_t n, int64_t vocab, const void* top_ids_
   a->ids_stride = ids_stride;
   a->ids64 = id_bits == 64;
   a->k = k;
+  a->kp = (k + 3) / 4 * 4;
   a->top_dtype = top->dtype;
   a->n = n;
   a->vocab = (int32_t)vocab;

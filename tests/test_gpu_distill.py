@@ -126,6 +126,19 @@ def test_many_rows_at_the_largest_that_a_block_holds(n, v, fused):
     check(*make(n, v, 20, BF16), fused=fused)
 
 
+# Rows dealt to 4, 8, 16 and more lanes, of a few pieces each; rows of less than a
+# piece; the longest rows that one wave has, and the next ones.
+@pytest.mark.parametrize("fused", [True, False])
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("n,v,k", [(66_001, 3, 3), (66_001, 7, 16), (70_003, 17, 5), (66_000, 47, 16),
+                                   (33_001, 100, 17), (20_003, 172, 64), (9001, 601, 30),
+                                   (4100, 1025, 3), (300, 2047, 64), (300, 2052, 64),
+                                   (300, 4095, 9), (300, 4104, 256)])
+def test_rows_of_a_part_of_a_wave(n, v, k, t, fused):
+    check(*make(n, v, k, t, idt=torch.int32 if v % 2 else torch.int64, tt=BF16 if k % 2 else F32),
+          fused=fused)
+
+
 @pytest.mark.parametrize("tt", [F32, F16, BF16])
 def test_the_teachers_logits_have_a_type_of_their_own(tt):
     check(*make(20, 300, 12, BF16, tt=tt))
