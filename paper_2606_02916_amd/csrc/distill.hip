@@ -268,6 +268,12 @@ __device__ __forceinline__ void store_entries(const DistillArgs& a, int64_t row,
 // A row in registers: read once, written once.  The row's whole pieces are
 // dealt to a group of lanes (part of a wave, or a block); its last elements,
 // fewer than a piece, go to the first lanes, one each.
+//
+// Bound by memory where rows are long: 4,096 of 128,000 bf16, loss and gradient
+// 400 us, 5.2 TB/s read and written; the loss alone 214, 4.9; of 50,000 x 1,500 fp32
+// 49 us, 6.1.  Short rows are bound by what a row costs beside its logits, its
+// entries' softmax and the reductions: 1M of 9 with 5 entries 50 us.  Rows that do
+// not start at 16 bytes move at 4.0 TB/s (4,096 of 128,001).
 // ---------------------------------------------------------------------------
 enum { kLossOnly = 0, kFused = 1, kBackward = 2 };
 
@@ -425,7 +431,8 @@ __device__ __forceinline__ void load_batch(const char* zp, int p, int p1,
 
 // Statistics of one split of a row; the last block of a row has its lesson
 // instead, as far as it needs no statistics and while z is still whole (the
-// gradient may take its place).
+// gradient may take its place).  12 rows of 64 splits 5.3 us: one pass over a
+// split and the joins; 2,000 rows of 262,144 fp32 4.9 TB/s.
 template <typename T, int V>
 __global__ void __launch_bounds__(kBlock) k_distill_stats(DistillArgs a) {
   extern __shared__ __align__(16) char lds[];
@@ -505,7 +512,7 @@ __device__ __forceinline__ void store_loss(const DistillArgs& a, int64_t row, fl
   if (a.lse) a.lse[row] = lse;
 }
 
-// The loss alone: a wave per row.
+// The loss alone: a wave per row.  3 us for few rows, an empty launch's time.
 __global__ void __launch_bounds__(kWave) k_distill_loss(DistillArgs a) {
   const int64_t row = block_index();
   if (row >= a.n) return;
@@ -515,6 +522,9 @@ __global__ void __launch_bounds__(kWave) k_distill_loss(DistillArgs a) {
     store_loss(a, row, lesson, st.s == 0.0f, lse_of(st, soft_of(st.m, a.c2), a.inv_temp));
 }
 
+// The gradient of one split: reads it again and writes it.  64 rows of 262,144 fp32
+// 25 us with the gradient alone, 5.3 TB/s; 12 of 64 splits 7.6 us, whose first half
+// is the wait for ids, then logits at them, beside the split's own loads.
 template <typename T, int V, int MODE>
 __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
   extern __shared__ __align__(16) char lds[];

@@ -15,7 +15,10 @@ __device__ __forceinline__ int64_t id_at(const void* ids, int32_t bits, int64_t 
 // rows written.  The output is one run of n * pieces pieces of 16 bytes (of
 // the wider type), dealt to the lanes in order: every store covers a
 // contiguous run, rows of any width fill the waves, and one wide row spreads
-// over as many waves as it has.  A lane has U pieces in flight.
+// over as many waves as it has.  A lane has U pieces in flight.  1.5M rows of
+// 100 fp32 take 210 us, 5.0 TB/s if each distinct row counts once, a 1 GiB copy's
+// rate; 400,000 rows of 128 codes to fp16 30 us, 5.1; one row 2.2 us, an empty
+// launch's time.
 // ---------------------------------------------------------------------------
 struct LookupArgs {
   KRows table, out;
@@ -108,6 +111,11 @@ __global__ void __launch_bounds__(kBlock) k_embed_rows(LookupArgs a) {
 // [w * kTileWave, (w + 1) * kTileWave) of the tile, 64 neighbouring ones at a
 // time.  Lanes whose digits agree find each other by one ballot per digit bit,
 // so equal digits are counted and ranked without atomics.
+//
+// Each launch waits more than it works: 200,003 ids take four of 5, 13, 5 and 13
+// us, of which reading and writing the pairs at a copy's rate would be half a
+// microsecond each.  What they cost is the way through one tile: its load, the
+// counters of all tiles, the scan, LDS and the store.
 // ---------------------------------------------------------------------------
 // Up to this many pairs find their places by counting, in a single launch.
 constexpr int kRankBlock = 1024;
@@ -377,7 +385,7 @@ __global__ void __launch_bounds__(NT) k_sort_scatter(Keys a, const int32_t* hist
 // with a share of all keys each, which they read from LDS four at a time.  That
 // is n^2 comparisons, but on the whole chip and in one launch: 14,298 ids in
 // 20 us, where two passes over a tile in one block's LDS took 29 and four
-// launches of the other kernels take 27.
+// launches of the other kernels 27.  Comparisons bound it.
 __global__ void __launch_bounds__(kRankBlock) k_sort_rank(Keys a, int blocks, uint32_t* key_out,
                                                           uint32_t* pos_out, FillArgs f) {
   if ((int)blockIdx.x >= blocks)
@@ -440,9 +448,13 @@ __global__ void __launch_bounds__(kRankBlock) k_sort_rank(Keys a, int blocks, ui
 // positions), so that every row is written once, zeros included, and the
 // gradient needs no pass that clears it.  Short runs are summed by a group of
 // `lanes` lanes each, longer ones by the block's groups together.  Runs of
-// more than `chunk` positions are cut at multiples of it: k_grad_parts sums
-// their parts first, a block per chunk, so that an id that fills the whole
-// call still spreads over the chip.
+// more than `chunk` positions are cut at multiples of it: the launch's first
+// blocks sum their parts, a block per chunk, so that an id that fills the whole
+// call still spreads over the chip, and k_grad_long joins them.
+//
+// Bound by memory: dy's rows are read once in the order of the ids, the
+// gradient's written once.  200,003 x 602 fp32 rows into 233,000 take 222 us, 4.7
+// TB/s; 32,768 x 2,048 bf16 rows, ids by a power law, 49.
 // ---------------------------------------------------------------------------
 constexpr int kGradRows = 256;       // most entries of a block
 constexpr int kGroupRun = 32;        // longest run that one group sums (4, 8 and 16: 2,468
@@ -526,7 +538,7 @@ __device__ __forceinline__ void add_rows(const GradArgs& a, uint32_t p0, uint32_
   }
 }
 
-// As add_rows, over the parts of run [beg, end) that k_grad_parts left.
+// As add_rows, over the parts of run [beg, end) that sum_parts left.
 template <int V>
 __device__ __forceinline__ void add_parts(const GradArgs& a, uint32_t beg, uint32_t end,
                                           uint32_t first, uint32_t step, int32_t e,
@@ -849,7 +861,8 @@ k_grad_rows(GradArgs a) {
 }
 
 // The long runs that start in chunk blockIdx.x, which is at most one: its
-// parts are added up in the order of the chunks.
+// parts are added up in the order of the chunks.  5 to 7 us: an empty launch, a
+// search for the run's ends and, for the longest run, its few hundred parts.
 template <typename TG, int V>
 __global__ void __launch_bounds__(kBlock) k_grad_long(GradArgs a) {
   __shared__ float lds[V * kBlock];

@@ -90,7 +90,11 @@ __device__ __forceinline__ void load_weights(const char* w, int32_t w_f32, const
 //
 // Bound by memory: each input is read once, the row stays in registers
 // between the sum of squares and the outputs.  Nothing is stored before the
-// row is read whole, so outputs may lie on the inputs.
+// row is read whole, so outputs may lie on the inputs.  A wave has a row of up to
+// 256 pieces to itself, several where they are narrow, so that a sum needs no
+// barrier.  32,768 rows of 4,096 bf16 with residual and sum take 182 us, 5.9
+// TB/s; 200,000 of 602 fp32 364 us, 5.3; 2M of 33 fp32 177 us, 6.0; without a
+// residual, 65,536 of 1,000 bf16 39 us, 6.7 (a 1 GiB copy: 5.0).
 template <typename T, typename R, int V, int STEPS, bool BLK>
 __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
   __shared__ float lds[BLK ? 1024 / kWave : 1];
@@ -199,7 +203,8 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
 //   dx = dsum + rho * (g - s * rho^2 * mean(g * s)),  dw = sum_rows dy * s * rho.
 // Blocks stay for many rows and keep their share of dw in registers; the
 // shares of all blocks are added in a second launch, in the order of the
-// blocks.
+// blocks.  Bound by memory: 32,768 rows of 4,096 bf16 209 us, 5.1 TB/s; 200,000 of
+// 602 fp32 376 us, 5.1.
 // ---------------------------------------------------------------------------
 struct NormBackArgs {
   KRows dy, dsum, s, dx;
@@ -308,7 +313,8 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm_back(NormBackArgs 
 }
 
 // dw[j] = sum of the blocks' shares: 64 columns a block, its waves take the
-// shares in turn.
+// shares in turn.  768 shares of 4,096 columns from the caches: 4.8 us, most of it
+// the launch and two waits.
 constexpr int kSumWaves = 16;
 
 __global__ void __launch_bounds__(kSumWaves * kWave) k_norm_dw(const float* part, int32_t blocks,
