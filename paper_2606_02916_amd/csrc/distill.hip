@@ -290,6 +290,25 @@ __device__ __forceinline__ void keep_packed(R (&raw)[N]) {
     }
 }
 
+// How a row is cut: its elements up to the first 16-byte boundary, whole pieces
+// from there, and what is left.  Single elements take a lane each, 14 at most, so
+// rows that share a wave start with a piece, on the boundary or not.
+struct Cut {
+  int head, pieces;
+  // The single element of lane l, where there is one.
+  template <int V>
+  __device__ __forceinline__ int single(int l) const {
+    return l < head ? l : pieces * V + l;
+  }
+};
+
+template <typename T, int V>
+__device__ __forceinline__ Cut cut_of(const char* row, int vocab, int lanes) {
+  const int head = V > 1 && lanes >= 16 && vocab >= 2 * V
+                       ? (int)((0 - (uint32_t)(uintptr_t)row) & 15u) / (int)sizeof(T) : 0;
+  return {head, (vocab - head) / V};
+}
+
 template <typename T, int V, int STEPS, bool BLK, int MODE>
 __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArgs a) {
   extern __shared__ __align__(16) char lds[];
@@ -300,8 +319,10 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
   if (row >= a.n) return;
   const int l = BLK ? (int)threadIdx.x : (int)threadIdx.x & (lanes - 1);
   constexpr int kPiece = V * (int)sizeof(T);
-  const int pieces = a.vocab / V, rest = a.vocab - pieces * V;
   const char* zp = a.z.p + row * a.z.stride;
+  const Cut cut = cut_of<T, V>(zp, a.vocab, lanes);
+  const int pieces = cut.pieces, rest = a.vocab - pieces * V;
+  const int single = cut.single<V>(l);
 
   const int el = BLK ? min(lanes, kWave) : lanes;     // lanes that read the entries
   const Entries en = entries_at(lds, BLK ? 0 : (int)threadIdx.x >> a.lanes_log, a.kp);
@@ -313,8 +334,9 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
   typename Raw<T, V>::vec raw[STEPS];
 #pragma unroll
   for (int t = 0; t < STEPS; ++t)
-    raw[t] = raw_load<T, V>(zp + (int64_t)min(t * lanes + l, pieces - 1) * kPiece);
-  const auto raw_last = raw_load<T, 1>(zp + min(pieces * V + l, a.vocab - 1) * (int64_t)sizeof(T));
+    raw[t] = raw_load<T, V>(zp + cut.head * (int)sizeof(T) +
+                            (int64_t)min(t * lanes + l, pieces - 1) * kPiece);
+  const auto raw_last = raw_load<T, 1>(zp + min(single, a.vocab - 1) * (int64_t)sizeof(T));
   bool has = false;
   if (l < el) {
     take_entries(a, row, l, el, held);
@@ -382,13 +404,14 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
   }
   if constexpr (MODE == kLossOnly) return;
 
-  char* dp = a.dz.p + row * a.dz.stride;
+  char* d0 = a.dz.p + row * a.dz.stride;
+  char* dp = d0 + cut.head * (int)sizeof(T);
   if (!has) {      // the same for the whole row
     const float zero[V] = {}, one[1] = {0.0f};
 #pragma unroll
     for (int t = 0; t < STEPS; ++t)
       if (t * lanes + l < pieces) row_store<T, V>(dp + (int64_t)(t * lanes + l) * kPiece, zero);
-    if (l < rest) row_store<T, 1>(dp + (pieces * V + l) * (int64_t)sizeof(T), one);
+    if (l < rest) row_store<T, 1>(d0 + single * (int64_t)sizeof(T), one);
     return;
   }
   const float c = weight * a.temp, ci = c * inv;
@@ -403,7 +426,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
     }
   if (l < rest) {
     const float v[1] = {ci * exp_of(last[0], top)};
-    row_store<T, 1>(dp + (pieces * V + l) * (int64_t)sizeof(T), v);
+    row_store<T, 1>(d0 + single * (int64_t)sizeof(T), v);
   }
   if constexpr (BLK)
     __syncthreads();
