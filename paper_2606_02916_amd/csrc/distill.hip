@@ -39,10 +39,10 @@ struct DistillArgs {
 
 // exp((z - m) / T) as 2^(z c2 - b), c2 = log2(e) / T and b = m c2: one fused
 // multiply-add, rounded once, and the same b in a sum and in what is divided
-// by it.  A b beyond fp32's range (all logits at the type's lowest value, say) or
-// close to it means that logits which differ at all differ by far too much to
-// count, so c2 becomes a power of two under which m c2 is exact and the least
-// difference is 2^10.
+// by it, so that b's own rounding, up to 2^6 where |b| is 2^31, cancels.  Beyond
+// (all logits at -1e30 or the type's lowest value, say, or a tiny T) logits which
+// differ at all differ by 2^7 at least, far too much to count, so c2 becomes a power
+// of two under which m c2 is exact and the least difference is 2^10.
 struct Soft {
   float m, c2, b;
   bool coarse;
@@ -51,7 +51,7 @@ struct Soft {
 __device__ __forceinline__ Soft soft_of(float m, float c2) {
   if (m == -INFINITY) return {m, c2, 0.0f, false};     // masked logits give 0
   const float b = m * c2;
-  if (fabsf(b) > 0x1p126f && fabsf(m) <= 3.4028235e38f) {
+  if (fabsf(b) > 0x1p31f && fabsf(m) <= 3.4028235e38f) {
     const uint32_t e = (__float_as_uint(m) >> 23) & 255u;
     const float c = __uint_as_float((254u + 34u - e) << 23);
     return {m, c, m * c, true};

@@ -308,3 +308,33 @@ def test_the_same_each_time_and_on_another_stream():
             again = run(z, ids, top, w, 2.0, 1.0, True)
         torch.cuda.current_stream().wait_stream(side)
         assert all(torch.equal(a, b) for a, b in zip(first[:3], again[:3]))
+
+
+# Rows of one value; of a value and two larger ones; and with one largest logit a few
+# units above the rest: beyond |z| / T of 2^31 any difference leaves all to the largest.
+def huge_rows(v, mask, T):
+    z, ids, top, w = make(3, v, 4, F32, seed=11)
+    z[:] = mask
+    z[1, 1] = z[1, 3] = mask * (1.5 if mask > 0 else 0.5)
+    z[2, 2] = mask * (1 - 2.0 ** -22 if mask < 0 else 1 + 2.0 ** -22)
+    ids[:] = torch.arange(4)
+    top[:] = 0.25
+    q = torch.zeros(3, v, dtype=torch.float64)
+    q[0] = 1.0 / v
+    q[1, 1] = q[1, 3] = 0.5
+    q[2, 2] = 1.0
+    want = q.clone()
+    want[:, :4] -= 0.25
+    a = w.cpu().double()[:, None] * T
+    return (z, ids, top, w), want * a, (q + 0.25) * a * 40 * U
+
+
+HUGE = [(-1e30, 1.0), (-1e10, 0.1), (-1e37, 2.0), (3.3, 1e-30), (-1e20, 3.0)]
+
+
+@pytest.mark.parametrize("v", [5, 50, 5000, 30_000, 40_000])
+@pytest.mark.parametrize("mask,T", HUGE)
+def test_the_largest_logit_may_be_a_masks_value(mask, T, v):
+    args, want, bound = huge_rows(v, mask, T)
+    loss, lse, dz, st = run(*args, T, 1.0, True)
+    assert within(dz, want, bound) <= 0 and st == 0
