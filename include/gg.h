@@ -664,7 +664,9 @@ int gg_distill_forward(const gg_rows_t* z, int64_t n, int64_t vocab, const void*
                        size_t ws_bytes, hipStream_t stream);
 
 /* The gradient alone, from the lse_d of the forward call; row_w_d may now hold
- * the gradient that reaches each row's loss. */
+ * the gradient that reaches each row's loss.  q takes the rounding of lse, a few
+ * |lse| 2^-24 of its size; rows with an lse of 4096 or more have theirs computed
+ * again, by one workgroup where rows are split. */
 int gg_distill_backward(const gg_rows_t* z, int64_t n, int64_t vocab, const void* top_ids_d,
                         int32_t id_bits, int64_t ids_stride, const gg_rows_t* top, int32_t k,
                         float temperature, float weight, const float* row_w_d, const float* lse_d,

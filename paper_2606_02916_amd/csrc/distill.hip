@@ -104,6 +104,16 @@ __device__ __forceinline__ float lse_of(const MaxSum& st, const Soft& t, float i
   return t.coarse ? t.m * inv_temp + kLn2 * l2 : kLn2 * (t.b + l2);
 }
 
+// An lse from which the backward call does not take q: q's relative error is a few
+// times |lse| 2^-24, and an lse beside a logit of -1e30 does not hold the number of
+// logits that share it.  The row's statistics are computed again where that
+// matters (2^-10 of q here; the gradient of a 16-bit row has 2^-9 at best).
+constexpr float kFarLse = 4096.0f;
+
+__device__ __forceinline__ bool is_far(float weight, float lse) {
+  return weight != 0.0f && !(fabsf(lse) < kFarLse);
+}
+
 // ---------------------------------------------------------------------------
 // A row's entries, up to kPerLane for each of `lanes` lanes of one wave.  Their
 // loads are issued around the row's own: the ids before it, the logits at the
@@ -347,9 +357,14 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
 
   // Softmax statistics: q_j = inv * exp_of(z_j, top).
   Soft top;
-  float inv = 1.0f, lse;
-  bool empty;
-  if constexpr (MODE != kBackward) {
+  float inv = 1.0f, lse = 0.0f;
+  bool empty, fresh = true;
+  if constexpr (MODE == kBackward) {
+    lse = a.lse_in[row];
+    fresh = is_far(weight, lse);
+    if (l < el) share_logits(a, l, el, held, en);
+  }
+  if (fresh) {
     float m = last[0];
 #pragma unroll
     for (int t = 0; t < STEPS; ++t)
@@ -360,7 +375,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
         for (int k = 0; k < V; ++k) m = fmaxf(m, v[k]);
       }
     keep_packed(raw);
-    if (l < el) share_logits(a, l, el, held, en);
+    if (MODE != kBackward && l < el) share_logits(a, l, el, held, en);
     top = soft_of(lanes_maxf(m, min(lanes, kWave)), a.c2);
     float s = exp_of(last[0], top);
 #pragma unroll
@@ -372,7 +387,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
         for (int k = 0; k < V; ++k) sum += exp_of(v[k], top);
         s += sum;
       }
-    if constexpr (MODE == kFused) keep_packed(raw);
+    if constexpr (MODE != kLossOnly) keep_packed(raw);
     MaxSum all = {top.m, lanes_sum(s, min(lanes, kWave))};
     if constexpr (BLK) {
       if (lane_id() == 0) s_part[threadIdx.x / kWave] = make_float2(all.m, all.s);
@@ -385,8 +400,6 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
     inv = 1.0f / all.s;
     lse = lse_of(all, top, a.inv_temp);
   } else {
-    if (l < el) share_logits(a, l, el, held, en);
-    lse = a.lse_in[row];
     empty = lse == -INFINITY;
     top = soft_of(lse * a.temp, a.c2);
     if (BLK) __syncthreads();
@@ -452,33 +465,12 @@ __device__ __forceinline__ void load_batch(const char* zp, int p, int p1,
   }
 }
 
-// Statistics of one split of a row; the last block of a row has its lesson
-// instead, as far as it needs no statistics and while z is still whole (the
-// gradient may take its place).  12 rows of 64 splits 5.3 us: one pass over a
-// split and the joins; 2,000 rows of 262,144 fp32 4.9 TB/s.
+// Statistics of a lane's share of the pieces [p0, p1) and, with `end`, of the row's
+// last elements.
 template <typename T, int V>
-__global__ void __launch_bounds__(kBlock) k_distill_stats(DistillArgs a) {
-  extern __shared__ __align__(16) char lds[];
-  __shared__ float2 s_part[kBlock / kWave];
-  const int64_t row = block_index() / (a.splits + 1);
-  const int c = (int)(block_index() - row * (a.splits + 1));
-  if (row >= a.n) return;
-  const int tid = threadIdx.x;
-  if (c == a.splits) {
-    if (tid >= kWave) return;
-    const Entries en = entries_at(lds, 0, a.kp);
-    Held<T> held;
-    load_entries(a, row, tid, kWave, held);
-    take_entries(a, row, tid, kWave, held);
-    const bool has = share_entries<false>(a, weight_of(a, row), tid, kWave, held, en);
-    share_logits(a, tid, kWave, held, en);
-    const float v = lesson_of(a, tid, kWave, en, 0.0f);
-    if (tid == 0) a.lesson[row] = make_float2(v, has ? 1.0f : 0.0f);
-    return;
-  }
-  const int pieces = a.vocab / V, rest = a.vocab - pieces * V;
-  const int p0 = c * a.chunk, p1 = min(pieces, p0 + a.chunk);
-  const char* zp = a.z.p + row * a.z.stride;
+__device__ __forceinline__ MaxSum lane_stats(const DistillArgs& a, const char* zp, int p0, int p1,
+                                             bool end) {
+  const int tid = threadIdx.x, pieces = a.vocab / V, rest = a.vocab - pieces * V;
   MaxSum st = {-INFINITY, 0.0f};
   for (int p = p0 + tid; p < p1; p += kBlock * kSplitUnroll) {
     typename Raw<T, V>::vec raw[kSplitUnroll];
@@ -503,11 +495,41 @@ __global__ void __launch_bounds__(kBlock) k_distill_stats(DistillArgs a) {
       st.s += p + u * kBlock < p1 ? s : 0.0f;
     }
   }
-  if (c == a.splits - 1 && tid < rest) {
+  if (end && tid < rest) {
     float v[1];
     row_load<T, 1>(zp + (pieces * V + tid) * (int64_t)sizeof(T), v);
     st = join(st, {v[0], v[0] == -INFINITY ? 0.0f : v[0] - v[0] + 1.0f}, a.c2);
   }
+  return st;
+}
+
+// Statistics of one split of a row; the last block of a row has its lesson
+// instead, as far as it needs no statistics and while z is still whole (the
+// gradient may take its place).  12 rows of 64 splits 5.3 us: one pass over a
+// split and the joins; 2,000 rows of 262,144 fp32 4.9 TB/s.
+template <typename T, int V>
+__global__ void __launch_bounds__(kBlock) k_distill_stats(DistillArgs a) {
+  extern __shared__ __align__(16) char lds[];
+  __shared__ float2 s_part[kBlock / kWave];
+  const int64_t row = block_index() / (a.splits + 1);
+  const int c = (int)(block_index() - row * (a.splits + 1));
+  if (row >= a.n) return;
+  const int tid = threadIdx.x;
+  if (c == a.splits) {
+    if (tid >= kWave) return;
+    const Entries en = entries_at(lds, 0, a.kp);
+    Held<T> held;
+    load_entries(a, row, tid, kWave, held);
+    take_entries(a, row, tid, kWave, held);
+    const bool has = share_entries<false>(a, weight_of(a, row), tid, kWave, held, en);
+    share_logits(a, tid, kWave, held, en);
+    const float v = lesson_of(a, tid, kWave, en, 0.0f);
+    if (tid == 0) a.lesson[row] = make_float2(v, has ? 1.0f : 0.0f);
+    return;
+  }
+  const int p0 = c * a.chunk, p1 = min(a.vocab / V, p0 + a.chunk);
+  const char* zp = a.z.p + row * a.z.stride;
+  MaxSum st = lane_stats<T, V>(a, zp, p0, p1, c == a.splits - 1);
   st = join_lanes(st, kWave, a.c2);
   if (lane_id() == 0) s_part[tid / kWave] = make_float2(st.m, st.s);
   __syncthreads();
@@ -552,12 +574,15 @@ template <typename T, int V, int MODE>
 __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
   extern __shared__ __align__(16) char lds[];
   __shared__ int32_t s_has;
+  __shared__ float2 s_part[kBlock / kWave];
   const int64_t row = block_index() / a.splits;
   const int c = (int)(block_index() - row * a.splits);
   if (row >= a.n) return;
   const int tid = threadIdx.x;
   const int pieces = a.vocab / V, rest = a.vocab - pieces * V;
-  const int p0 = c * a.chunk, p1 = min(pieces, p0 + a.chunk);
+  const int p0 = c * a.chunk;
+  int p1 = min(pieces, p0 + a.chunk);
+  bool end = c == a.splits - 1;
   const char* zp = a.z.p + row * a.z.stride;
   char* dp = a.dz.p + row * a.dz.stride;
   const Entries en = entries_at(lds, 0, a.kp);
@@ -579,8 +604,23 @@ __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
       store_loss(a, row, a.lesson[row], empty, lse_of(st, top, a.inv_temp));
   } else {
     const float lse = a.lse_in[row];
-    empty = lse == -INFINITY;
-    top = soft_of(lse * a.temp, a.c2);
+    if (is_far(weight, lse)) {
+      // One block has the whole row, which it reads before it writes any of it.
+      if (c != 0) return;
+      p1 = pieces;
+      end = true;
+      MaxSum st = join_lanes(lane_stats<T, V>(a, zp, 0, p1, true), kWave, a.c2);
+      if (lane_id() == 0) s_part[tid / kWave] = make_float2(st.m, st.s);
+      __syncthreads();
+      st = join_waves(s_part, kBlock / kWave, a.c2);
+      empty = st.s == 0.0f;
+      top = soft_of(st.m, a.c2);
+      inv = 1.0f / st.s;
+      if (p < p1) load_batch<T, V>(zp, p, p1, raw);
+    } else {
+      empty = lse == -INFINITY;
+      top = soft_of(lse * a.temp, a.c2);
+    }
   }
   if (tid < kWave) {
     take_entries(a, row, tid, kWave, held);
@@ -603,7 +643,6 @@ __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
     p += kBlock * kSplitUnroll;
     if (p < p1) load_batch<T, V>(zp, p, p1, raw);
   }
-  const bool end = c == a.splits - 1;
   if (end && tid < rest) {
     float v[1];
     row_load<T, 1>(zp + (pieces * V + tid) * (int64_t)sizeof(T), v);

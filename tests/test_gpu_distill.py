@@ -338,3 +338,17 @@ def test_the_largest_logit_may_be_a_masks_value(mask, T, v):
     args, want, bound = huge_rows(v, mask, T)
     loss, lse, dz, st = run(*args, T, 1.0, True)
     assert within(dz, want, bound) <= 0 and st == 0
+
+
+@pytest.mark.parametrize("place", [False, True])
+@pytest.mark.parametrize("v", [5, 50, 5000, 30_000, 40_000, 140_001])
+@pytest.mark.parametrize("mask,T", HUGE + [(torch.finfo(F32).min, 1.0), (torch.finfo(F32).min, 3.0),
+                                           (torch.finfo(F32).min / 4, 0.5), (-20_000.0, 1.0)])
+def test_the_gradient_from_an_lse_that_holds_no_more_than_its_largest_logit(mask, T, v, place):
+    args, want, bound = huge_rows(v, mask, T)
+    z = args[0]
+    if mask == -20_000.0:
+        z[2] = mask
+        z[2, 2] = 0.0
+    loss, lse, dz, st = run(*args, T, 1.0, False, dz=(z, None, None) if place else None)
+    assert within(dz, want, bound) <= 0 and st == 0
