@@ -33,7 +33,8 @@ struct DistillArgs {
   int32_t splits;              // blocks of a row
   int32_t chunk;               // pieces of a split
   float2* part;                // [n][splits]: maximum of z, sum of exp((z - maximum) / T)
-  float2* lesson;              // [n]: sum p (log p - z / T); whether the row has a lesson
+  float2* lesson;              // [n]: sum p (log p - (z - pivot) / T); the pivot, -infinity
+                               // where the row has no lesson
   int32_t* status;
 };
 
@@ -112,6 +113,15 @@ constexpr float kFarLse = 4096.0f;
 
 __device__ __forceinline__ bool is_far(float weight, float lse) {
   return weight != 0.0f && !(fabsf(lse) < kFarLse);
+}
+
+// log q of a logit, from the distance to the largest one: the difference of z / T
+// and an lse loses log q where both are large.
+__device__ __forceinline__ float log_q(const DistillArgs& a, float z, const MaxSum& st,
+                                       const Soft& t) {
+  const float l2 = __builtin_amdgcn_logf(st.s);
+  return t.coarse ? (z - t.m) * a.inv_temp - kLn2 * l2
+                  : kLn2 * (__builtin_fmaf(z, t.c2, -t.b) - l2);
 }
 
 // ---------------------------------------------------------------------------
@@ -249,13 +259,14 @@ __device__ __forceinline__ void share_logits(const DistillArgs& a, int l, int la
     if (u * lanes + l < a.k) en.z[u * lanes + l] = h.id[u] < 0 ? 0.0f : (float)h.z[u];
 }
 
-// sum_k p_k (log p_k - z_k / T + lse), by the same lanes.
+// sum_k p_k (log p_k - log_qk(z_k)), by the same lanes.
+template <typename F>
 __device__ __forceinline__ float lesson_of(const DistillArgs& a, int l, int lanes,
-                                           const Entries& en, float lse) {
+                                           const Entries& en, F log_qk) {
   float v = 0.0f;
   for (int j = l; j < a.k; j += lanes) {
     const float p = en.id[j] < 0 ? 0.0f : __builtin_amdgcn_exp2f(en.lp[j]);
-    if (p != 0.0f) v += p * (kLn2 * en.lp[j] - (en.z[j] * a.inv_temp - lse));
+    if (p != 0.0f) v += p * (kLn2 * en.lp[j] - log_qk(en.z[j]));
   }
   return lanes_sum(v, lanes);
 }
@@ -358,6 +369,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
   // Softmax statistics: q_j = inv * exp_of(z_j, top).
   Soft top;
   float inv = 1.0f, lse = 0.0f;
+  MaxSum all = {};
   bool empty, fresh = true;
   if constexpr (MODE == kBackward) {
     lse = a.lse_in[row];
@@ -388,7 +400,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
         s += sum;
       }
     if constexpr (MODE != kLossOnly) keep_packed(raw);
-    MaxSum all = {top.m, lanes_sum(s, min(lanes, kWave))};
+    all = {top.m, lanes_sum(s, min(lanes, kWave))};
     if constexpr (BLK) {
       if (lane_id() == 0) s_part[threadIdx.x / kWave] = make_float2(all.m, all.s);
       __syncthreads();
@@ -408,7 +420,8 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
   has = has && !empty;
   if constexpr (MODE != kBackward) {
     if (l < el) {
-      const float v = has ? lesson_of(a, l, el, en, lse) : 0.0f;
+      const float v =
+          has ? lesson_of(a, l, el, en, [&](float z) { return log_q(a, z, all, top); }) : 0.0f;
       if (l == 0) {
         a.loss[row] = has ? weight * a.temp * a.temp * v : 0.0f;
         if (a.lse) a.lse[row] = lse;
@@ -523,8 +536,15 @@ __global__ void __launch_bounds__(kBlock) k_distill_stats(DistillArgs a) {
     take_entries(a, row, tid, kWave, held);
     const bool has = share_entries<false>(a, weight_of(a, row), tid, kWave, held, en);
     share_logits(a, tid, kWave, held, en);
-    const float v = lesson_of(a, tid, kWave, en, 0.0f);
-    if (tid == 0) a.lesson[row] = make_float2(v, has ? 1.0f : 0.0f);
+    // Relative to the largest of the entries' logits, whose log q is known later.
+    float pivot = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kPerLane; ++u)
+      if (held.id[u] >= 0) pivot = fmaxf(pivot, (float)held.z[u]);
+    pivot = lanes_maxf(pivot, kWave);
+    if (pivot == -INFINITY) pivot = 0.0f;
+    const float v = lesson_of(a, tid, kWave, en, [&](float z) { return (z - pivot) * a.inv_temp; });
+    if (tid == 0) a.lesson[row] = make_float2(v, has ? pivot : -INFINITY);
     return;
   }
   const int p0 = c * a.chunk, p1 = min(a.vocab / V, p0 + a.chunk);
@@ -550,11 +570,11 @@ __device__ __forceinline__ MaxSum row_stats(const DistillArgs& a, int64_t row) {
 }
 
 __device__ __forceinline__ void store_loss(const DistillArgs& a, int64_t row, float2 lesson,
-                                           bool empty, float lse) {
+                                           const MaxSum& st, const Soft& t) {
   const float weight = weight_of(a, row);
-  a.loss[row] =
-      lesson.y != 0.0f && !empty ? weight * a.temp * a.temp * (lesson.x + lse) : 0.0f;
-  if (a.lse) a.lse[row] = lse;
+  a.loss[row] = lesson.y != -INFINITY && st.s != 0.0f
+                    ? weight * a.temp * a.temp * (lesson.x - log_q(a, lesson.y, st, t)) : 0.0f;
+  if (a.lse) a.lse[row] = lse_of(st, t, a.inv_temp);
 }
 
 // The loss alone: a wave per row.  3 us for few rows, an empty launch's time.
@@ -564,7 +584,7 @@ __global__ void __launch_bounds__(kWave) k_distill_loss(DistillArgs a) {
   const float2 lesson = a.lesson[row];
   const MaxSum st = row_stats(a, row);
   if (threadIdx.x == 0)
-    store_loss(a, row, lesson, st.s == 0.0f, lse_of(st, soft_of(st.m, a.c2), a.inv_temp));
+    store_loss(a, row, lesson, st, soft_of(st.m, a.c2));
 }
 
 // The gradient of one split: reads it again and writes it.  64 rows of 262,144 fp32
@@ -601,7 +621,7 @@ __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
     top = soft_of(st.m, a.c2);
     inv = 1.0f / st.s;
     if (c == 0 && tid == 0)
-      store_loss(a, row, a.lesson[row], empty, lse_of(st, top, a.inv_temp));
+      store_loss(a, row, a.lesson[row], st, top);
   } else {
     const float lse = a.lse_in[row];
     if (is_far(weight, lse)) {

@@ -5,6 +5,7 @@ relative error of 3 |x| U in the term) and the exponential's own two units; a
 sum of such terms adds one rounding per addition along its longest chain,
 which is a lane's elements and the tree after it.  Logarithms of p and of the
 sum are off by a few U of their size."""
+import math
 import zlib
 
 import pytest
@@ -352,3 +353,16 @@ def test_the_gradient_from_an_lse_that_holds_no_more_than_its_largest_logit(mask
         z[2, 2] = 0.0
     loss, lse, dz, st = run(*args, T, 1.0, False, dz=(z, None, None) if place else None)
     assert within(dz, want, bound) <= 0 and st == 0
+
+
+@pytest.mark.parametrize("v", [5, 50, 5000, 30_000, 40_000])
+@pytest.mark.parametrize("mask,T", [(-1e30, 1.0), (-1e10, 0.1), (-3e5, 2.0), (torch.finfo(F32).min, 1.0)])
+def test_the_loss_of_a_row_of_one_value(mask, T, v):
+    """log p - log q = log v - log 4, whatever the value: a product and two
+    logarithms of a sum that a lane's elements and the tree after it make."""
+    (z, ids, top, w), _, _ = huge_rows(v, mask, T)
+    z[:] = mask
+    loss, lse, dz, st = run(z, ids, top, w, T, 1.0, False)
+    a = w.cpu().double() * T * T
+    want = a * (torch.log(torch.tensor(float(v)).double()) - math.log(4.0))
+    assert within(loss, want, a * (200 + v / 256) * U + 8 * U * (want.abs() + a * math.log(4.0 * v))) <= 0
