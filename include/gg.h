@@ -614,8 +614,10 @@ int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t id_bits, i
  * rstd = (mean(s^2) + eps)^-1/2, y = s * rstd * w (w_d NULL: ones), in fp32
  * from the unrounded s.  Outputs, each NULL where it is not wanted: sum (s),
  * y, q (y in 8 bits) and rstd_d [n].  q's scale is max(|y|) of its group or
- * row / 448, at least 2^-126, and its code y / scale rounded to nearest even; a
- * group that holds a NaN or an infinity has that scale.  x and y have one type
+ * row / 448, at least 2^-126, and its code y / scale, both quotients of the fp32
+ * y rounded to fp32, the code's then to nearest even; a group that holds a NaN or
+ * an infinity has that scale, and code 0 beside an infinity.  A row whose sum of
+ * squares passes fp32's range has rstd 0.  x and y have one type
  * of GG_F32, GG_F16 and GG_BF16; res and sum have that type or both GG_F32;
  * weights [dim] too (w_dtype).  sum and y may be the memory of res or x. */
 int gg_rmsnorm_forward(const gg_rows_t* x, const gg_rows_t* res, int64_t n, int32_t dim,

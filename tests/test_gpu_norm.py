@@ -267,3 +267,38 @@ def test_rows_of_8_bits_read_back():
     top = torch.cat([p.abs().amax(1, keepdim=True).expand(-1, p.shape[1]) for p in y.split(group, 1)], 1)
     assert within(out, y, y.abs() * UNIT[E4M3] * 1.01 + FLOOR[E4M3] * top / 448 * 1.01 + 4 * U * y.abs()) <= 0
     assert not buf[:, 116:].any()
+
+
+@pytest.mark.parametrize("n,dim,group", [(8192, 1030, 0), (8192, 1030, 64), (2048, 4100, 0), (2048, 4100, 256)])
+@pytest.mark.parametrize("with_w", [False, True])
+def test_codes_are_the_rounded_quotients(n, dim, group, with_w):
+    """Scales and codes are functions of the fp32 y alone, each by one division in
+    fp32 and, for the codes, one rounding more: equal to the last bit."""
+    gg, g = lib(), torch.Generator(device=DEV).manual_seed(dim + group)
+    x = torch.randn(n, dim, generator=g, device=DEV)
+    w = torch.rand(dim, generator=g, device=DEV) + 0.5 if with_w else None
+    x[5] = 0
+    x[6] *= 1e-20
+    y, q = torch.empty_like(x), torch.empty(n, dim, dtype=E4M3, device=DEV)
+    k = -(-dim // group) if group else 1
+    sc = torch.empty(n, k, device=DEV)
+    gg.gg_rmsnorm_forward(gg.make_rows(x), None, n, dim, w, 1e-30, None, gg.make_rows(y),
+                          gg.make_rows(q, scales=sc, group=group), None)
+    y, sc = y.cpu(), sc.cpu()
+    top = torch.stack([p.abs().amax(1) for p in y.split(group or dim, 1)], 1)
+    assert torch.equal(sc, (top / 448).clamp(min=TINY))
+    want = (y / sc[:, torch.arange(dim) // (group or dim)]).to(E4M3)
+    assert torch.equal(q.cpu().view(torch.uint8), want.view(torch.uint8))
+
+
+def test_an_infinite_weight_leaves_zeros_beside_its_own_code():
+    """The scale of a row with one infinity is infinite, the other codes are 0."""
+    gg = lib()
+    x = torch.randn(3, 70, generator=gen(2)).to(DEV)
+    w = torch.ones(70, device=DEV)
+    w[9] = float("inf")
+    q, sc = torch.empty(3, 70, dtype=E4M3, device=DEV), torch.empty(3, device=DEV)
+    gg.gg_rmsnorm_forward(gg.make_rows(x), None, 3, 70, w, 1e-6, None, None,
+                          gg.make_rows(q, scales=sc), None)
+    q, other = q.float().cpu(), torch.arange(70) != 9
+    assert bool(torch.isinf(sc).all()) and not q[:, other].any() and bool(torch.isnan(q[:, 9]).all())
