@@ -513,7 +513,8 @@ __device__ __forceinline__ MaxSum lane_stats(const DistillArgs& a, const char* z
   if (end && tid < rest) {
     float v[1];
     row_load<T, 1>(zp + (pieces * V + tid) * (int64_t)sizeof(T), v);
-    st = join(st, {v[0], v[0] == -INFINITY ? 0.0f : v[0] - v[0] + 1.0f}, a.c2);
+    // (2^(z c2 - b) of the largest logit itself is 1 only up to b's rounding)
+    st = join(st, {v[0], exp_of(v[0], soft_of(v[0], a.c2))}, a.c2);
   }
   return st;
 }

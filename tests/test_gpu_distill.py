@@ -366,3 +366,50 @@ def test_the_loss_of_a_row_of_one_value(mask, T, v):
     a = w.cpu().double() * T * T
     want = a * (torch.log(torch.tensor(float(v)).double()) - math.log(4.0))
     assert within(loss, want, a * (200 + v / 256) * U + 8 * U * (want.abs() + a * math.log(4.0 * v))) <= 0
+
+
+# Rows that are split, with elements behind the last whole piece, where |z| / T lies
+# below 2^31 and m / T's own rounding is far above a unit of the exponent.  Rows of
+# one value; its only largest logit at the end, at the front, and at both.
+SPLIT_TAILS = [(40_001, F32), (40_002, F32), (40_003, F32), (70_001, BF16), (70_007, F16)]
+LARGE = [(60_000.0, 6e-5), (-60_000.0, 6e-3), (60_000.0, 0.6), (-60_000.0, 0.06), (3.3, 1e-8)]
+
+
+@pytest.mark.parametrize("mode", ["loss", "fused", "two", "in place"])
+@pytest.mark.parametrize("v,t", SPLIT_TAILS)
+@pytest.mark.parametrize("mask,T", LARGE)
+def test_the_last_elements_of_split_rows_count_as_the_others(mask, T, v, t, mode):
+    """q depends on differences, which are 0 or far too large to count here; the
+    rounding of m / T, up to 64 units of the exponent, is in both of log q's terms."""
+    gg = lib()
+    z, ids, top, w = make(4, v, 4, t, seed=12)
+    low, high = sorted((mask, mask / 2))
+    z[:] = low
+    z[1, v - 1] = z[2, 2] = z[3, 1] = z[3, v - 1] = high
+    ids[:] = torch.tensor([0, 1, 2, v - 1])
+    top[:] = 0.25
+    (rl, rs, rd), (_, bs, _), _ = reference(z, ids, top, w, T, 1.0)
+    a = w.cpu().double()
+    Td = torch.tensor(T, dtype=F32).double()
+    x = z.cpu().double() / Td
+    q = torch.softmax(x, 1)
+    far = (x.amax(1, keepdim=True) - x[:, [0, 1, 2, v - 1]]).mean(1)
+    chain = (220 + v / 256) * U
+    bl = a * Td * Td * (chain + 8 * U * (far + math.log(4.0 * v) + 70))
+    at_ids = torch.zeros_like(q).scatter_(1, ids.cpu().long(), 0.25 * 40 * U)
+    bd = (a * Td)[:, None] * (q * chain + at_ids) + 1.01 * UNIT[t] * rd.abs() + FLOOR[t]
+    if mode == "loss":
+        loss, lse = (torch.full((4,), float("nan"), device=DEV) for _ in range(2))
+        st = torch.zeros(1, dtype=torch.int32, device=DEV)
+        ws = torch.full((gg.gg_ws_distill(4, v),), 0xFF, dtype=torch.uint8, device=DEV)
+        gg.gg_distill_forward(gg.make_rows(z), 4, v, ids, gg.make_rows(top), 4, T, 1.0, w, loss, lse,
+                              None, st, ws)
+        dz, st = None, int(st)
+    else:
+        loss, lse, dz, st = run(z, ids, top, w, T, 1.0, mode == "fused",
+                                dz=(z, None, None) if mode == "in place" else None)
+    assert st == 0
+    assert within(loss, rl, bl + FLOOR[F32]) <= 0
+    assert within(lse, rs, bs) <= 0
+    if dz is not None:
+        assert within(dz, rd, bd) <= 0
