@@ -658,7 +658,8 @@ size_t gg_ws_distill(int64_t n, int64_t vocab);
  * weight (a = 0) or with no logit above -infinity has loss 0 and a gradient of
  * zeros.  Ids outside -1 .. vocab - 1 are no entries and set GG_DEV_BAD_ID.  z,
  * top: GG_F32, GG_F16 or GG_BF16; dz has z's type and may be its memory.  The
- * gradient is rounded once from fp32.  ws: 8-byte aligned. */
+ * gradient is rounded once from fp32; the loss takes a T^2 times the roundings of
+ * log p and log q, a few 2^-24 of their size.  ws: 8-byte aligned. */
 int gg_distill_forward(const gg_rows_t* z, int64_t n, int64_t vocab, const void* top_ids_d,
                        int32_t id_bits, int64_t ids_stride, const gg_rows_t* top, int32_t k,
                        float temperature, float weight, const float* row_w_d, float* loss_d,

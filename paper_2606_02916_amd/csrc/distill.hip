@@ -74,6 +74,11 @@ __device__ __forceinline__ float weight_of(const DistillArgs& a, int64_t row) {
   return a.row_w ? a.weight * a.row_w[row] : a.weight;
 }
 
+// A row's loss from its divergence v.  (T^2 alone may be 0 or infinite in fp32.)
+__device__ __forceinline__ float scaled(const DistillArgs& a, float weight, float v) {
+  return weight * (a.temp * (a.temp * v));
+}
+
 struct MaxSum {
   float m, s;     // largest logit; sum of exp((z - m) / T)
 };
@@ -425,7 +430,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
       const float v =
           has ? lesson_of(a, l, el, en, [&](float z) { return log_q(a, z, all, top); }) : 0.0f;
       if (l == 0) {
-        a.loss[row] = has ? weight * a.temp * a.temp * v : 0.0f;
+        a.loss[row] = has ? scaled(a, weight, v) : 0.0f;
         if (a.lse) a.lse[row] = lse;
       }
     }
@@ -576,7 +581,7 @@ __device__ __forceinline__ void store_loss(const DistillArgs& a, int64_t row, fl
                                            const MaxSum& st, const Soft& t) {
   const float weight = weight_of(a, row);
   a.loss[row] = lesson.y != -INFINITY && st.s != 0.0f
-                    ? weight * a.temp * a.temp * (lesson.x - log_q(a, lesson.y, st, t)) : 0.0f;
+                    ? scaled(a, weight, lesson.x - log_q(a, lesson.y, st, t)) : 0.0f;
   if (a.lse) a.lse[row] = lse_of(st, t, a.inv_temp);
 }
 

@@ -413,3 +413,28 @@ def test_the_last_elements_of_split_rows_count_as_the_others(mask, T, v, t, mode
     assert within(lse, rs, bs) <= 0
     if dz is not None:
         assert within(dz, rd, bd) <= 0
+
+
+# All differences are far beyond 2^31 T, so the rows' largest logits take everything:
+# the loss is a T times distances, finite although T^2 is not a number of fp32.
+@pytest.mark.parametrize("v", [50, 5000, 40_000])
+@pytest.mark.parametrize("T", [1e-20, 1e-25, 1e-30])
+def test_the_loss_at_the_smallest_temperatures(T, v):
+    z, ids, top, w = make(4, v, 4, F32, seed=13)
+    ids[:] = torch.arange(4)
+    z[:, 4:] = 0.0
+    z[:, :4] = torch.tensor([-3.0, -1.0, 2.0, 5.0])
+    top[:] = torch.tensor([1.0, 4.0, 2.0, 3.0])          # all of p at the second
+    loss, lse, dz, st = run(z, ids, top, w, T, 1.0, True)
+    want = w.cpu().double() * torch.tensor(T, dtype=F32).double() * 6.0
+    assert st == 0 and within(loss, want, 16 * U * want + FLOOR[F32]) <= 0
+
+
+@pytest.mark.parametrize("T", [1e20, 1e30])
+def test_a_loss_of_zero_at_the_largest_temperatures(T):
+    """Entries that cover the vocabulary, all logits equal: p = q exactly."""
+    z, ids, top, w = make(3, 4, 4, F32, seed=14)
+    ids[:] = torch.arange(4)
+    z[:], top[:] = 0.5, 2.0
+    loss, lse, dz, st = run(z, ids, top, w, T, 1.0, True)
+    assert st == 0 and not loss.any() and not dz.any()
