@@ -209,8 +209,8 @@ __device__ __forceinline__ void take_entries(const DistillArgs& a, int64_t row, 
   if (bad) set_status(a.status, GG_DEV_BAD_ID);
 }
 
-// Whether the row has a lesson: an entry with a logit above -infinity, and a
-// weight.  SUM: p is summed over equal ids (for the gradient).
+// Whether the row has a lesson: an entry with a logit above -infinity, or a NaN
+// (which a maximum passes over), and a weight.  SUM: p is summed over equal ids (for the gradient).
 template <bool SUM, typename T>
 __device__ __forceinline__ bool share_entries(const DistillArgs& a, float weight, int l, int lanes,
                                               const Held<T>& h, const Entries& en) {
@@ -221,7 +221,8 @@ __device__ __forceinline__ bool share_entries(const DistillArgs& a, float weight
   float total = 0.0f;
 #pragma unroll
   for (int u = 0; u < kPerLane; ++u) total += exp_of(h.t[u], f);
-  const float log_total = __builtin_amdgcn_logf(lanes_sum(total, lanes));
+  total = lanes_sum(total, lanes);
+  const float log_total = __builtin_amdgcn_logf(total);
 #pragma unroll
   for (int u = 0; u < kPerLane; ++u) {
     const int j = u * lanes + l;
@@ -253,7 +254,7 @@ __device__ __forceinline__ bool share_entries(const DistillArgs& a, float weight
     for (int u = 0; u < kPerLane; ++u)
       if (u * lanes + l < a.k) en.p[u * lanes + l] = p[u];
   }
-  return f.m != -INFINITY && weight != 0.0f;
+  return !(total == 0.0f) && weight != 0.0f;
 }
 
 template <typename T>

@@ -438,3 +438,30 @@ def test_a_loss_of_zero_at_the_largest_temperatures(T):
     z[:], top[:] = 0.5, 2.0
     loss, lse, dz, st = run(z, ids, top, w, T, 1.0, True)
     assert st == 0 and not loss.any() and not dz.any()
+
+
+@pytest.mark.parametrize("mode", ["loss", "fused", "two"])
+@pytest.mark.parametrize("v", [50, 5000, 40_000])
+def test_a_teacher_of_nans_alone_shows(v, mode):
+    """A row whose entries' logits are all NaN has a loss of NaN, and a gradient of NaN
+    at its entries; one without entries has none, whatever lies at its -1."""
+    gg = lib()
+    z, ids, top, w = make(3, v, 4, F32, seed=15)
+    ids[:] = torch.arange(4)
+    top[0] = float("nan")
+    ids[1, 1:], top[1, 0] = -1, float("nan")
+    ids[2], top[2] = -1, float("nan")
+    if mode == "loss":
+        loss = torch.zeros(3, device=DEV)
+        st = torch.zeros(1, dtype=torch.int32, device=DEV)
+        ws = torch.empty(gg.gg_ws_distill(3, v), dtype=torch.uint8, device=DEV)
+        gg.gg_distill_forward(gg.make_rows(z), 3, v, ids, gg.make_rows(top), 4, 2.0, 1.0, w, loss,
+                              None, None, st, ws)
+    else:
+        loss, _, dz, st = run(z, ids, top, w, 2.0, 1.0, mode == "fused")
+        nan = torch.isnan(dz.cpu())
+        assert nan[0, :4].all() and not nan[0, 4:].any()
+        assert nan[1, 0] and not nan[1, 1:].any()
+        assert not dz[2].any()
+    loss = loss.cpu()
+    assert torch.isnan(loss[:2]).all() and loss[2] == 0
