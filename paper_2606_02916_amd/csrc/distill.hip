@@ -23,6 +23,7 @@ struct DistillArgs {
   int64_t n;
   float temp, inv_temp;        // T, 1 / T
   float c2;                    // log2(e) / T
+  float t_ln2;                 // T log(2)
   float weight;
   const float* row_w;          // nullptr: ones
   float* loss;
@@ -33,7 +34,7 @@ struct DistillArgs {
   int32_t splits;              // blocks of a row
   int32_t chunk;               // pieces of a split
   float2* part;                // [n][splits]: maximum of z, sum of exp((z - maximum) / T)
-  float2* lesson;              // [n]: sum p (log p - (z - pivot) / T); the pivot, -infinity
+  float2* lesson;              // [n]: sum p (T log p - (z - pivot)); the pivot, -infinity
                                // where the row has no lesson
   int32_t* status;
 };
@@ -72,11 +73,6 @@ __device__ __forceinline__ float factor(const Soft& a, const Soft& t) {
 
 __device__ __forceinline__ float weight_of(const DistillArgs& a, int64_t row) {
   return a.row_w ? a.weight * a.row_w[row] : a.weight;
-}
-
-// A row's loss from its divergence v.  (T^2 alone may be 0 or infinite in fp32.)
-__device__ __forceinline__ float scaled(const DistillArgs& a, float weight, float v) {
-  return weight * (a.temp * (a.temp * v));
 }
 
 struct MaxSum {
@@ -120,13 +116,15 @@ __device__ __forceinline__ bool is_far(float weight, float lse) {
   return weight != 0.0f && !(fabsf(lse) < kFarLse);
 }
 
-// log q of a logit, from the distance to the largest one: the difference of z / T
-// and an lse loses log q where both are large.
-__device__ __forceinline__ float log_q(const DistillArgs& a, float z, const MaxSum& st,
-                                       const Soft& t) {
-  const float l2 = __builtin_amdgcn_logf(st.s);
-  return t.coarse ? (z - t.m) * a.inv_temp - kLn2 * l2
-                  : kLn2 * (__builtin_fmaf(z, t.c2, -t.b) - l2);
+// T log q of a logit, from the distance to the largest one: the difference of z / T
+// and an lse loses log q where both are large.  Beyond 2^40 units of the exponent it
+// is the distance itself, which is a number where z / T may be none (the type's lowest
+// value, or a tiny T): losses are summed in these units and then scaled by T once
+// more, since T^2 may be 0 or infinite too.
+__device__ __forceinline__ float t_log_q(const DistillArgs& a, float z, const MaxSum& st,
+                                         const Soft& t) {
+  const float l2 = __builtin_amdgcn_logf(st.s), d = __builtin_fmaf(z, t.c2, -t.b);
+  return t.coarse || fabsf(d) > 0x1p40f ? (z - t.m) - a.t_ln2 * l2 : a.t_ln2 * (d - l2);
 }
 
 // ---------------------------------------------------------------------------
@@ -265,14 +263,14 @@ __device__ __forceinline__ void share_logits(const DistillArgs& a, int l, int la
     if (u * lanes + l < a.k) en.z[u * lanes + l] = h.id[u] < 0 ? 0.0f : (float)h.z[u];
 }
 
-// sum_k p_k (log p_k - log_qk(z_k)), by the same lanes.
+// sum_k p_k (T log p_k - t_log_qk(z_k)), by the same lanes.
 template <typename F>
 __device__ __forceinline__ float lesson_of(const DistillArgs& a, int l, int lanes,
-                                           const Entries& en, F log_qk) {
+                                           const Entries& en, F t_log_qk) {
   float v = 0.0f;
   for (int j = l; j < a.k; j += lanes) {
     const float p = en.id[j] < 0 ? 0.0f : __builtin_amdgcn_exp2f(en.lp[j]);
-    if (p != 0.0f) v += p * (kLn2 * en.lp[j] - log_qk(en.z[j]));
+    if (p != 0.0f) v += p * (a.t_ln2 * en.lp[j] - t_log_qk(en.z[j]));
   }
   return lanes_sum(v, lanes);
 }
@@ -429,9 +427,9 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_distill_rows(DistillArg
   if constexpr (MODE != kBackward) {
     if (l < el) {
       const float v =
-          has ? lesson_of(a, l, el, en, [&](float z) { return log_q(a, z, all, top); }) : 0.0f;
+          has ? lesson_of(a, l, el, en, [&](float z) { return t_log_q(a, z, all, top); }) : 0.0f;
       if (l == 0) {
-        a.loss[row] = has ? scaled(a, weight, v) : 0.0f;
+        a.loss[row] = has ? weight * (a.temp * v) : 0.0f;
         if (a.lse) a.lse[row] = lse;
       }
     }
@@ -552,7 +550,7 @@ __global__ void __launch_bounds__(kBlock) k_distill_stats(DistillArgs a) {
       if (held.id[u] >= 0) pivot = fmaxf(pivot, (float)held.z[u]);
     pivot = lanes_maxf(pivot, kWave);
     if (pivot == -INFINITY) pivot = 0.0f;
-    const float v = lesson_of(a, tid, kWave, en, [&](float z) { return (z - pivot) * a.inv_temp; });
+    const float v = lesson_of(a, tid, kWave, en, [&](float z) { return z - pivot; });
     if (tid == 0) a.lesson[row] = make_float2(v, has ? pivot : -INFINITY);
     return;
   }
@@ -582,7 +580,7 @@ __device__ __forceinline__ void store_loss(const DistillArgs& a, int64_t row, fl
                                            const MaxSum& st, const Soft& t) {
   const float weight = weight_of(a, row);
   a.loss[row] = lesson.y != -INFINITY && st.s != 0.0f
-                    ? scaled(a, weight, lesson.x - log_q(a, lesson.y, st, t)) : 0.0f;
+                    ? weight * (a.temp * (lesson.x - t_log_q(a, lesson.y, st, t))) : 0.0f;
   if (a.lse) a.lse[row] = lse_of(st, t, a.inv_temp);
 }
 
@@ -822,6 +820,7 @@ int pack_args(const gg_rows_t* z, int64_t n, int64_t vocab, const void* top_ids_
   a->temp = temperature;
   a->inv_temp = 1.0f / temperature;
   a->c2 = kLog2e / temperature;
+  a->t_ln2 = kLn2 * temperature;
   a->weight = weight;
   a->row_w = row_w_d;
   a->status = status_d;

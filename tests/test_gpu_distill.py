@@ -465,3 +465,27 @@ def test_a_teacher_of_nans_alone_shows(v, mode):
         assert not dz[2].any()
     loss = loss.cpu()
     assert torch.isnan(loss[:2]).all() and loss[2] == 0
+
+
+@pytest.mark.parametrize("mode", ["loss", "fused", "two"])
+@pytest.mark.parametrize("v", [50, 5000, 40_000])
+@pytest.mark.parametrize("T", [0.25, 1.0, 1.5])
+def test_the_loss_where_an_entry_is_masked_by_the_types_lowest_value(T, v, mode):
+    """p times the distance, a number of fp32 although z log2(e) / T is none."""
+    gg = lib()
+    z, ids, top, w = make(3, v, 4, F32, seed=16)
+    ids[:] = torch.arange(4)
+    z[:, 2] = torch.finfo(F32).min
+    top[:] = torch.tensor([8.0, 8.0, 8.0 - T, 8.0])
+    if mode == "loss":
+        loss = torch.zeros(3, device=DEV)
+        st = torch.zeros(1, dtype=torch.int32, device=DEV)
+        ws = torch.empty(gg.gg_ws_distill(3, v), dtype=torch.uint8, device=DEV)
+        gg.gg_distill_forward(gg.make_rows(z), 3, v, ids, gg.make_rows(top), 4, T, 1.0, w, loss, None,
+                              None, st, ws)
+    else:
+        loss = run(z, ids, top, w, T, 1.0, mode == "fused")[0]
+    p = math.exp(-1) / (3 + math.exp(-1))
+    want = w.cpu().double() * T * p * -torch.finfo(F32).min
+    assert bool((want < torch.finfo(F32).max).all())
+    assert within(loss, want, 40 * U * want) <= 0
