@@ -489,3 +489,14 @@ def test_the_loss_where_an_entry_is_masked_by_the_types_lowest_value(T, v, mode)
     want = w.cpu().double() * T * p * -torch.finfo(F32).min
     assert bool((want < torch.finfo(F32).max).all())
     assert within(loss, want, 40 * U * want) <= 0
+
+
+@pytest.mark.parametrize("fused", [True, False])
+@pytest.mark.parametrize("v", [50, 5000, 40_000, 140_001])
+@pytest.mark.parametrize("rest,T", [(-3e38, 0.5), (3e38, 0.5), (-3e38, 2.0), (0.0, 1.0)])
+def test_the_loss_is_infinite_where_all_entries_have_no_logit(rest, T, v, fused):
+    z, ids, top, w = make(2, v, 4, F32, seed=17)
+    ids[:] = torch.arange(4)
+    z[:], z[:, :4] = rest, -INF
+    loss, _, dz, st = run(z, ids, top, w, T, 1.0, fused)
+    assert (loss == INF).all() and torch.isfinite(dz).all() and st == 0
