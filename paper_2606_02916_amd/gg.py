@@ -114,6 +114,8 @@ class gg_sage_layer_t(C.Structure):
 class gg_rows_t(C.Structure):
     _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("dtype", C.c_int32),
                 ("group", C.c_int32), ("scales", C.c_void_p), ("scales_stride", C.c_int64)]
+    # The shape of make_rows' tensor; a description filled in by hand has no limit.
+    rows = cols = 1 << 62
 
 
 GG_F32, GG_F16, GG_BF16, GG_E4M3 = 0, 1, 2, 3
@@ -502,12 +504,18 @@ def make_rows(t, scales=None, group=0):
         r.group, r.scales, r.scales_stride = group, scales.data_ptr(), scales.stride(0) * 4
     elif scales is not None or group:
         raise GGError(f"scales for rows of {t.dtype}")
+    r.rows, r.cols = t.shape
     r.keep = (t, scales)
     return r
 
 
-def _rows(r):
-    return None if r is None else C.byref(r)
+def _rows(r, n, cols, what):
+    """Address of a description of at least n rows of cols elements."""
+    if r is None:
+        return None
+    if n > r.rows or cols > r.cols:
+        raise GGError(f"{what}: {r.rows} rows of {r.cols} elements for {n} of {cols}")
+    return C.byref(r)
 
 
 _ID_BITS = {torch.int32: 32, torch.int64: 64}
@@ -526,8 +534,9 @@ def gg_embed_forward(table, num_rows, dim, ids, n, scale, out, status, stream=No
     """table and out: make_rows of a [num_rows, dim] and an [n, dim] tensor.
     ids: int32 or int64, or None for the rows 0 .. n-1."""
     ptr, bits = _ids(ids, n, "gg_embed_forward")
-    return check(lib.gg_embed_forward(_rows(table), num_rows, dim, ptr, bits, n, scale, _rows(out),
-                                      _ptr(status), _stream(stream)), "gg_embed_forward")
+    return check(lib.gg_embed_forward(_rows(table, num_rows, dim, "table"), num_rows, dim, ptr, bits,
+                                      n, scale, _rows(out, n, dim, "out"), _ptr(status),
+                                      _stream(stream)), "gg_embed_forward")
 
 
 def gg_ws_embed(n, num_rows, dim):
@@ -537,9 +546,9 @@ def gg_ws_embed(n, num_rows, dim):
 def gg_embed_backward(dy, ids, n, num_rows, dim, scale, grad, flags, status, ws, stream=None):
     """dy and grad: make_rows of an [n, dim] and a [num_rows, dim] tensor."""
     ptr, bits = _ids(ids, n, "gg_embed_backward")
-    return check(lib.gg_embed_backward(_rows(dy), ptr, bits, n, num_rows, dim, scale, _rows(grad),
-                                       flags, _ptr(status), _ptr(ws), ws.numel(),
-                                       _stream(stream)), "gg_embed_backward")
+    return check(lib.gg_embed_backward(_rows(dy, n, dim, "dy"), ptr, bits, n, num_rows, dim, scale,
+                                       _rows(grad, num_rows, dim, "grad"), flags, _ptr(status),
+                                       _ptr(ws), ws.numel(), _stream(stream)), "gg_embed_backward")
 
 
 def _weight(w, dim, what):
@@ -563,8 +572,9 @@ def _fp32(t, n, what):
 def gg_rmsnorm_forward(x, res, n, dim, w, eps, sum, y, q, rstd, stream=None):
     """x, res, sum, y, q: make_rows, or None (all but x)."""
     ptr, wt = _weight(w, dim, "gg_rmsnorm_forward")
-    return check(lib.gg_rmsnorm_forward(_rows(x), _rows(res), n, dim, ptr, wt, eps, _rows(sum),
-                                        _rows(y), _rows(q), _fp32(rstd, n, "rstd"),
+    return check(lib.gg_rmsnorm_forward(_rows(x, n, dim, "x"), _rows(res, n, dim, "res"), n, dim, ptr,
+                                        wt, eps, _rows(sum, n, dim, "sum"), _rows(y, n, dim, "y"),
+                                        _rows(q, n, dim, "q"), _fp32(rstd, n, "rstd"),
                                         _stream(stream)), "gg_rmsnorm_forward")
 
 
@@ -575,8 +585,9 @@ def gg_ws_rmsnorm(n, dim):
 def gg_rmsnorm_backward(dy, dsum, s, rstd, n, dim, w, dx, dw, ws, stream=None):
     """dy, dsum, s, dx: make_rows (dsum may be None); dw and ws may be None."""
     ptr, wt = _weight(w, dim, "gg_rmsnorm_backward")
-    return check(lib.gg_rmsnorm_backward(_rows(dy), _rows(dsum), _rows(s), _fp32(rstd, n, "rstd"),
-                                         n, dim, ptr, wt, _rows(dx), _fp32(dw, dim, "dw"),
+    return check(lib.gg_rmsnorm_backward(_rows(dy, n, dim, "dy"), _rows(dsum, n, dim, "dsum"),
+                                         _rows(s, n, dim, "s"), _fp32(rstd, n, "rstd"), n, dim, ptr,
+                                         wt, _rows(dx, n, dim, "dx"), _fp32(dw, dim, "dw"),
                                          _ptr(ws), 0 if ws is None else ws.numel(),
                                          _stream(stream)), "gg_rmsnorm_backward")
 
@@ -598,9 +609,10 @@ def gg_distill_forward(z, n, vocab, top_ids, top, k, temperature, weight, row_w,
     """z, top and dz: make_rows (dz may be None); top_ids: an [n, k] tensor;
     row_w and lse may be None."""
     ptr, bits, stride = _top_ids(top_ids, n, k)
-    return check(lib.gg_distill_forward(_rows(z), n, vocab, ptr, bits, stride, _rows(top), k,
-                                        temperature, weight, _fp32(row_w, n, "row_w"),
-                                        _fp32(loss, n, "loss"), _fp32(lse, n, "lse"), _rows(dz),
+    return check(lib.gg_distill_forward(_rows(z, n, vocab, "z"), n, vocab, ptr, bits, stride,
+                                        _rows(top, n, k, "top"), k, temperature, weight,
+                                        _fp32(row_w, n, "row_w"), _fp32(loss, n, "loss"),
+                                        _fp32(lse, n, "lse"), _rows(dz, n, vocab, "dz"),
                                         _ptr(status), _ptr(ws), ws.numel(), _stream(stream)),
                  "gg_distill_forward")
 
@@ -609,10 +621,11 @@ def gg_distill_backward(z, n, vocab, top_ids, top, k, temperature, weight, row_w
                         stream=None):
     """The gradient alone, from the forward call's lse."""
     ptr, bits, stride = _top_ids(top_ids, n, k)
-    return check(lib.gg_distill_backward(_rows(z), n, vocab, ptr, bits, stride, _rows(top), k,
-                                         temperature, weight, _fp32(row_w, n, "row_w"),
-                                         _fp32(lse, n, "lse"), _rows(dz), _ptr(status),
-                                         _stream(stream)), "gg_distill_backward")
+    return check(lib.gg_distill_backward(_rows(z, n, vocab, "z"), n, vocab, ptr, bits, stride,
+                                         _rows(top, n, k, "top"), k, temperature, weight,
+                                         _fp32(row_w, n, "row_w"), _fp32(lse, n, "lse"),
+                                         _rows(dz, n, vocab, "dz"), _ptr(status), _stream(stream)),
+                 "gg_distill_backward")
 
 
 def gg_read_status(status, stream=None):

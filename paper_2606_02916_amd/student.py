@@ -34,6 +34,13 @@ def rows_8bit(buf, dim, group=0):
                         scales=buf[:, at:end].view(torch.float32), group=group)
 
 
+def _shaped(t, n, cols, what):
+    """t, of at least n rows of just cols elements."""
+    if t.dim() != 2 or t.shape[0] < n or t.shape[1] != cols:
+        raise gg.GGError(f"{what} of shape {tuple(t.shape)} for {n} rows of {cols}")
+    return t
+
+
 class Student:
     """table [num_nodes, dim], norm weights w [dim] (fp32) and head [dim,
     classes] on the device, with the buffers of steps of up to max_rows rows
@@ -74,11 +81,12 @@ class Student:
         added to the looked-up rows if given; into self.y, and in 8 bits into q."""
         if n > self.max_rows:
             raise gg.GGError(f"{n} rows for a student of {self.max_rows}")
+        if x is not None:
+            x = gg.make_rows(_shaped(x, n, self.dim, "x"))
         gg.gg_embed_forward(self._table, self.N, self.dim, ids, n, self.scale, self._e,
                             self.status, stream=stream)
-        gg.gg_rmsnorm_forward(self._e, None if x is None else gg.make_rows(x), n, self.dim, self.w,
-                              self.eps, self._e, self._y if y else None, q, self.rstd,
-                              stream=stream)
+        gg.gg_rmsnorm_forward(self._e, x, n, self.dim, self.w, self.eps, self._e,
+                              self._y if y else None, q, self.rstd, stream=stream)
 
     def forward(self, ids, n, x=None):
         """Logits [n, classes] of the nodes ids[:n] on the current stream."""
@@ -91,6 +99,7 @@ class Student:
         classes top_ids [n, k] and their logits top [n, k]; row_w [n]: fp32
         weights of the rows (mean loss by default).  On the current stream;
         returns the rows' weighted losses."""
+        _shaped(top_ids, n, self.k, "top_ids"), _shaped(top, n, self.k, "top")
         self.forward(ids, n, x)
         weight = 1.0 if row_w is not None else 1.0 / max(n, 1)
         gg.gg_distill_forward(self._z, n, self.classes, top_ids, gg.make_rows(top), self.k,
@@ -111,13 +120,19 @@ class Student:
     def write_rows(self, buf, ids, n, group=0, x=None):
         """The normed rows of ids[:n] in 8 bits into buf (uint8 rows, see
         rows_8bit): feature rows for a fetch pipeline."""
-        self._normed(ids, n, x, q=rows_8bit(buf, self.dim, group), y=False)
+        q = rows_8bit(buf, self.dim, group)
+        if n > buf.shape[0]:
+            raise gg.GGError(f"{n} rows for a buffer of {buf.shape[0]}")
+        self._normed(ids, n, x, q=q, y=False)
         return buf
 
 
 def read_rows(buf, n, dim, group, out, status):
     """8-bit rows buf[:n] (gathered by a fetch pipeline, say) as numbers in
     out [n, dim], on the current stream."""
-    gg.gg_embed_forward(rows_8bit(buf, dim, group), buf.shape[0], dim, None, n, 1.0,
-                        gg.make_rows(out), status)
+    rows = rows_8bit(buf, dim, group)
+    if n > buf.shape[0]:
+        raise gg.GGError(f"{n} rows of a buffer of {buf.shape[0]}")
+    gg.gg_embed_forward(rows, buf.shape[0], dim, None, n, 1.0,
+                        gg.make_rows(_shaped(out, n, dim, "out")), status)
     return out

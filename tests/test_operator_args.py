@@ -200,3 +200,71 @@ def test_bindings_check_shapes_of_lists_and_vectors():
                 lambda: gg._weight(torch.zeros(4), 5, "x"), lambda: gg._weight(ids[0], 8, "x")):
         with pytest.raises(gg.GGError):
             bad()
+
+
+def test_bindings_check_the_rows():
+    """No description of fewer rows or narrower ones than the call goes over: refused
+    before the stream is asked for, so without a GPU."""
+    st, ws = torch.zeros(1, dtype=torch.int32), torch.zeros(1 << 16, dtype=torch.uint8)
+    ids, top_ids = torch.zeros(7, dtype=torch.int64), torch.zeros(7, 3, dtype=torch.int64)
+    r = lambda *shape: gg.make_rows(torch.zeros(*shape))  # noqa: E731
+    good, vec = r(7, 20), torch.zeros(20)
+    for name in ("short", "narrow"):
+        bad = r(6, 20) if name == "short" else r(7, 19)
+        k = r(6, 3) if name == "short" else r(7, 2)
+        for call in (
+                lambda: gg.gg_embed_forward(bad, 7, 20, ids, 7, 1.0, good, st),
+                lambda: gg.gg_embed_forward(good, 7, 20, ids, 7, 1.0, bad, st),
+                lambda: gg.gg_embed_backward(bad, ids, 7, 7, 20, 1.0, good, 0, st, ws),
+                lambda: gg.gg_embed_backward(good, ids, 7, 7, 20, 1.0, bad, 0, st, ws),
+                lambda: gg.gg_rmsnorm_forward(bad, good, 7, 20, None, 1e-6, good, good, None, None),
+                lambda: gg.gg_rmsnorm_forward(good, bad, 7, 20, None, 1e-6, good, good, None, None),
+                lambda: gg.gg_rmsnorm_forward(good, good, 7, 20, None, 1e-6, bad, good, None, None),
+                lambda: gg.gg_rmsnorm_forward(good, good, 7, 20, None, 1e-6, good, bad, None, None),
+                lambda: gg.gg_rmsnorm_backward(bad, None, good, vec, 7, 20, None, good, None, None),
+                lambda: gg.gg_rmsnorm_backward(good, bad, good, vec, 7, 20, None, good, None, None),
+                lambda: gg.gg_rmsnorm_backward(good, None, bad, vec, 7, 20, None, good, None, None),
+                lambda: gg.gg_rmsnorm_backward(good, None, good, vec, 7, 20, None, bad, None, None),
+                lambda: gg.gg_distill_forward(bad, 7, 20, top_ids, r(7, 3), 3, 1.0, 1.0, None, vec, vec,
+                                              good, st, ws),
+                lambda: gg.gg_distill_forward(good, 7, 20, top_ids, k, 3, 1.0, 1.0, None, vec, vec,
+                                              good, st, ws),
+                lambda: gg.gg_distill_forward(good, 7, 20, top_ids, r(7, 3), 3, 1.0, 1.0, None, vec,
+                                              vec, bad, st, ws),
+                lambda: gg.gg_distill_backward(bad, 7, 20, top_ids, r(7, 3), 3, 1.0, 1.0, None, vec,
+                                               good, st),
+                lambda: gg.gg_distill_backward(good, 7, 20, top_ids, k, 3, 1.0, 1.0, None, vec, good,
+                                               st),
+                lambda: gg.gg_distill_backward(good, 7, 20, top_ids, r(7, 3), 3, 1.0, 1.0, None, vec,
+                                               bad, st)):
+            with pytest.raises(gg.GGError, match="rows of"):
+                call()
+    q = torch.zeros(6, 20, dtype=torch.float8_e4m3fn)
+    with pytest.raises(gg.GGError, match="rows of"):
+        gg.gg_rmsnorm_forward(good, None, 7, 20, None, 1e-6, None, None,
+                              gg.make_rows(q, scales=torch.zeros(6)), None)
+
+
+def test_the_student_checks_its_tensors():
+    from paper_2606_02916_amd import Student, student
+    s = Student(50, 20, 9, max_rows=7, k=3, device="cpu")
+    ids = torch.zeros(7, dtype=torch.int64)
+    top_ids, top = torch.zeros(7, 3, dtype=torch.int64), torch.zeros(7, 3)
+    buf = torch.zeros(6, student.row_bytes_8bit(20), dtype=torch.uint8)
+    for call, word in (
+            (lambda: s.forward(ids, 8), "student of 7"),
+            (lambda: s.forward(ids, 7, torch.zeros(6, 20)), "x of shape"),
+            (lambda: s.forward(ids, 7, torch.zeros(7, 19)), "x of shape"),
+            (lambda: s.forward(ids[:6], 7), "ids"),
+            (lambda: s.step(ids, 7, top_ids, top[:6]), "top of shape"),
+            (lambda: s.step(ids, 7, top_ids, top[:, :2]), "top of shape"),
+            (lambda: s.step(ids, 7, top_ids[:, :2], top), "top_ids of shape"),
+            (lambda: s.step(ids, 7, top_ids, top, torch.zeros(7, 21)), "x of shape"),
+            (lambda: s.write_rows(buf, ids, 7), "buffer of 6"),
+            (lambda: s.write_rows(buf[:, :20], ids, 6), "8-bit rows"),
+            (lambda: s.write_rows(buf, ids, 6, x=torch.zeros(5, 20)), "x of shape"),
+            (lambda: student.read_rows(buf, 7, 20, 0, torch.zeros(7, 20), s.status), "buffer of 6"),
+            (lambda: student.read_rows(buf, 6, 20, 0, torch.zeros(5, 20), s.status), "out of shape"),
+            (lambda: student.read_rows(buf, 6, 20, 0, torch.zeros(6, 18), s.status), "out of shape")):
+        with pytest.raises(gg.GGError, match=word):
+            call()
