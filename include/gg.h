@@ -601,7 +601,7 @@ size_t gg_ws_embed(int64_t n, int64_t num_rows, int32_t dim);
  * and ids out of range (GG_DEV_BAD_ID) add nothing.  The ids are sorted and
  * every row's terms are added in fp32 in an order that depends on the ids
  * alone, so results are reproducible bit for bit.  n and num_rows are at most
- * 2^31 - 2. */
+ * 2^31 - 2.  ws: 8-byte aligned. */
 int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t id_bits, int64_t n,
                       int64_t num_rows, int32_t dim, float scale, const gg_rows_t* grad,
                       int32_t flags, int32_t* status_d, void* ws, size_t ws_bytes,

@@ -1059,7 +1059,8 @@ extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t
   if (rc == GG_OK) rc = pack_rows(grad, "grad", num_rows, dim, kBitFloats, true, &a.grad);
   if (rc != GG_OK) return rc;
   const size_t need = embed_ws_layout(n, dim, nullptr, nullptr);
-  GG_REQUIRE(n == 0 || (ws && ws_bytes >= need), "workspace of %zu bytes < %zu", ws_bytes, need);
+  GG_REQUIRE(n == 0 || (ws && (uintptr_t)ws % 8 == 0 && ws_bytes >= need),
+             "workspace of %zu bytes < %zu, or not aligned", ws_bytes, need);
   a.add = flags & GG_EMBED_ADD;
   if (a.add ? n == 0 : num_rows == 0) return GG_OK;
   EmbedWs w = {};

@@ -268,3 +268,9 @@ def test_the_student_checks_its_tensors():
             (lambda: student.read_rows(buf, 6, 20, 0, torch.zeros(6, 18), s.status), "out of shape")):
         with pytest.raises(gg.GGError, match=word):
             call()
+
+
+@pytest.mark.parametrize("off", [1, 2, 4])
+def test_gradient_refuses_a_workspace_off_its_alignment(off):
+    """Pairs of 32-bit counters are read from it."""
+    refused(gg.lib.gg_embed_backward, GRAD, dict(ws=P + off), "workspace")
