@@ -1062,7 +1062,7 @@ extern "C" int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t
   GG_REQUIRE(n == 0 || (ws && (uintptr_t)ws % 8 == 0 && ws_bytes >= need),
              "workspace of %zu bytes < %zu, or not aligned", ws_bytes, need);
   a.add = flags & GG_EMBED_ADD;
-  if (a.add ? n == 0 : num_rows == 0) return GG_OK;
+  if (n == 0 && (a.add || num_rows == 0)) return GG_OK;      // (ids are looked at in any case)
   EmbedWs w = {};
   if (n > 0) embed_ws_layout(n, dim, (char*)ws, &w);
 

@@ -304,3 +304,19 @@ def test_rows_beyond_four_gigabytes():
     assert not bool(rest) and int(st) == 0
     twice = (out[1].cpu().float() + out[3].cpu().float()).to(BF16)
     assert torch.equal(table[v - 1].cpu(), twice) and torch.equal(table[0], out[0])
+
+
+@pytest.mark.parametrize("n", [5, 20_000, 600_000])
+@pytest.mark.parametrize("add", [False, True])
+def test_ids_for_a_gradient_of_no_rows_are_reported(n, add):
+    gg = lib()
+    grad = torch.empty(0, 8, device=DEV)
+    dy = torch.ones(n, 8, device=DEV)
+    ws = torch.empty(gg.gg_ws_embed(n, 0, 8), dtype=torch.uint8, device=DEV)
+    for first, want in ((-1, 0), (0, gg.DEV_BAD_ID)):
+        ids = torch.full((n,), -1, dtype=torch.int64, device=DEV)
+        ids[n // 2] = first
+        st = status_word()
+        gg.gg_embed_backward(gg.make_rows(dy), ids, n, 0, 8, 1.0, gg.make_rows(grad),
+                             gg.GG_EMBED_ADD if add else 0, st, ws)
+        assert int(st) == want
