@@ -42,10 +42,12 @@ def _shaped(t, n, cols, what):
 
 
 class Student:
-    """table [num_nodes, dim], norm weights w [dim] (fp32) and head [dim,
-    classes] on the device, with the buffers of steps of up to max_rows rows
-    and k teacher entries each.  dtype: fp32, fp16 or bf16, of the table, the
-    head and the activations."""
+    """table [num_nodes, dim], norm weights w [dim] and head [dim, classes] on
+    the device, with the buffers of steps of up to max_rows rows and k teacher
+    entries each.  What is trained is fp32: most of a step of a mean loss is less
+    than half a unit of a 16-bit number and would be rounded away.  dtype: fp32,
+    fp16 or bf16, of the activations, their gradients and the copy of the head
+    that they are multiplied with."""
 
     def __init__(self, num_nodes, dim, classes, max_rows, k=8, temperature=2.0, rate=0.05,
                  dtype=torch.float32, eps=1e-6, device=None, generator=None):
@@ -56,7 +58,7 @@ class Student:
         self.scale = math.sqrt(dim)
 
         def normal(*shape, std):
-            return (torch.randn(*shape, generator=generator, device=dev) * std).to(dtype)
+            return torch.randn(*shape, generator=generator, device=dev) * std
 
         self.table = normal(self.N, self.dim, std=1 / self.scale)
         self.w = torch.ones(self.dim, device=dev)
@@ -67,7 +69,8 @@ class Student:
         # e becomes the sum with x, and in a step its gradient; z its gradient
         self.e, self.y, self.dy, self.z = rows(dim), rows(dim), rows(dim), rows(classes)
         self.rstd, self.loss, self.lse = vec(), vec(), vec()
-        self.dw, self.dhead = torch.empty_like(self.w), torch.empty_like(self.head)
+        self.dw, self.dhead = torch.empty_like(self.w), torch.empty_like(self.head, dtype=dtype)
+        self._head = torch.empty_like(self.dhead) if dtype != torch.float32 else self.head
         self._table = gg.make_rows(self.table)
         self._e, self._y, self._dy, self._z = (gg.make_rows(t)
                                                for t in (self.e, self.y, self.dy, self.z))
@@ -91,7 +94,9 @@ class Student:
     def forward(self, ids, n, x=None):
         """Logits [n, classes] of the nodes ids[:n] on the current stream."""
         self._normed(ids, n, x)
-        return torch.mm(self.y[:n], self.head, out=self.z[:n])
+        if self._head is not self.head:
+            self._head.copy_(self.head)
+        return torch.mm(self.y[:n], self._head, out=self.z[:n])
 
     def step(self, ids, n, top_ids, top, x=None, row_w=None):
         """One step of gradient descent on the nodes ids[:n] (int32 or int64,
@@ -107,7 +112,7 @@ class Student:
                               self.status, self.ws)
         dz = self.z[:n]
         torch.mm(self.y[:n].t(), dz, out=self.dhead)
-        torch.mm(dz, self.head.t(), out=self.dy[:n])
+        torch.mm(dz, self._head.t(), out=self.dy[:n])
         gg.gg_rmsnorm_backward(self._dy, None, self._e, self.rstd, n, self.dim, self.w, self._e,
                                self.dw, self.ws)
         # the step on the table, in place: only rows that occur are touched

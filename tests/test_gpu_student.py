@@ -7,7 +7,7 @@ import torch
 
 import synth
 from tests.gpu_util import World
-from tests.op_util import E4M3, F32, U
+from tests.op_util import BF16, E4M3, F16, F32, U, UNIT
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -188,3 +188,35 @@ def test_operators_in_a_replayed_graph():
         for a, b in zip(outs, want):
             assert torch.equal(a, b), seed
     assert int(status) == 0
+
+
+@pytest.mark.parametrize("t", [F16, BF16])
+def test_a_step_with_16_bit_activations_lands_whole(t):
+    """The parameters move by what the step's own gradients ask for, to a rounding of
+    fp32.  Those gradients, after some 64 roundings to 16 bits that a logit's products
+    and the softmax add up at most, are the 64-bit step's."""
+    from paper_2606_02916_amd import Student
+    n, N, dim, classes, k = 1024, 2000, 100, 47, 8
+    st = Student(N, dim, classes, max_rows=n, k=k, dtype=t, device=DEV, generator=gen(7))
+    g = torch.Generator().manual_seed(8)
+    ids = torch.randint(0, N, (n,), generator=g)
+    ids[5:9] = -1
+    top_ids = torch.stack([torch.randperm(classes, generator=g)[:k] for _ in range(n)])
+    top = (torch.randn(n, k, generator=g) * 2 + 5).to(t)
+    before = [p.clone() for p in (st.table, st.w, st.head)]
+    want, grads = step64(*before, ids, top_ids, top, None, st.scale, st.temperature, st.eps, 1 / n)
+    st.step(ids.to(DEV), n, top_ids.to(DEV), top.to(DEV))
+    assert int(st.status) == 0
+    moved = [p.cpu().double() - b.cpu().double() for p, b in zip((st.table, st.w, st.head), before)]
+    # the buffer of the looked-up rows holds their gradient after a step
+    de, keep = st.e[:n].cpu().double(), ids >= 0
+    asked, size = torch.zeros(2, N, dim, dtype=torch.float64)
+    asked.index_add_(0, ids[keep], de[keep])
+    size.index_add_(0, ids[keep], de[keep].abs())
+    bound = 2 * U * before[0].cpu().double().abs() + 40 * U * st.rate * st.scale * size
+    assert bool(((moved[0] + st.rate * st.scale * asked).abs() <= bound).all())
+    bound = 2 * U * (before[2].cpu().double().abs() + st.rate * st.dhead.cpu().double().abs())
+    assert bool(((moved[2] + st.rate * st.dhead.cpu().double()).abs() <= bound).all())
+    for m, grad in zip(moved, grads):
+        assert float((m + st.rate * grad).norm()) <= 64 * UNIT[t] * st.rate * float(grad.norm())
+    assert float((st.loss[:n].cpu().double() - want).norm()) <= 64 * UNIT[t] * float(want.norm())
