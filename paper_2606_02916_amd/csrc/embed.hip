@@ -36,13 +36,9 @@ struct LookupArgs {
 template <typename TI, typename TO, int V, int U>
 __global__ void __launch_bounds__(kBlock) k_embed_rows(LookupArgs a) {
   // The block's first row and piece (the same for all lanes).
-  const uint64_t base = (uint64_t)blockIdx.x * (kBlock * U);
-  uint64_t row0;
-  if (base >> 32)
-    row0 = base / a.pieces;
-  else
-    row0 = (uint32_t)base / a.pieces;
-  const uint32_t rem = (uint32_t)(base - row0 * a.pieces);
+  // (below the number of pieces, which is 2^32 at most)
+  const uint32_t base = blockIdx.x * (uint32_t)(kBlock * U);
+  const uint32_t row0 = base / a.pieces, rem = base - row0 * a.pieces;
   // All ids, then all rows: a lane waits twice, whatever U is.
   typename Raw<TI, V>::vec raw[U];
   float mul[U], mul2[U];
@@ -56,7 +52,7 @@ __global__ void __launch_bounds__(kBlock) k_embed_rows(LookupArgs a) {
     const uint32_t r = chunk_row(o, a.pmagic);
     int32_t skip;
     e[j] = piece_start<V>((int32_t)(o - r * a.pieces), a.dim, &skip);
-    row[j] = (int64_t)(row0 + r);
+    row[j] = (int64_t)row0 + r;
     ok[j] = row[j] < a.n;
     id[j] = min(row[j], a.n - 1);
   }
