@@ -320,3 +320,21 @@ def test_ids_for_a_gradient_of_no_rows_are_reported(n, add):
         gg.gg_embed_backward(gg.make_rows(dy), ids, n, 0, 8, 1.0, gg.make_rows(grad),
                              gg.GG_EMBED_ADD if add else 0, st, ws)
         assert int(st) == want
+
+
+@pytest.mark.parametrize("tin,tout,n,dim", [(F32, F32, 9001, 1001), (BF16, F16, 17_003, 1030),
+                                            (E4M3, F16, 17_003, 1030), (F16, F32, 3_000_001, 3)])
+def test_lookup_of_more_than_the_caches_take(tin, tout, n, dim):
+    """Outputs of more than 32 MB, a product rounded once: equal to the last bit."""
+    gg, g = lib(), torch.Generator(device=DEV).manual_seed(dim)
+    v = 1500
+    x = torch.randn(v, dim, generator=g, device=DEV).to(tin)
+    sc = torch.rand(v, generator=g, device=DEV) + 0.5 if tin == E4M3 else None
+    ids = torch.randint(-1, v, (n,), generator=g, device=DEV)
+    out = torch.full((n, dim), float("nan"), dtype=tout, device=DEV)
+    assert out.numel() * out.element_size() > 32 << 20
+    st = status_word()
+    gg.gg_embed_forward(gg.make_rows(x, scales=sc), v, dim, ids, n, 0.5, gg.make_rows(out), st)
+    want = x.float() * (0.5 if sc is None else (sc * 0.5)[:, None])
+    want = torch.cat([want, torch.zeros(1, dim, device=DEV)]).to(tout)[ids]
+    assert torch.equal(out, want) and int(st) == 0

@@ -302,3 +302,39 @@ def test_an_infinite_weight_leaves_zeros_beside_its_own_code():
                           gg.make_rows(q, scales=sc), None)
     q, other = q.float().cpu(), torch.arange(70) != 9
     assert bool(torch.isinf(sc).all()) and not q[:, other].any() and bool(torch.isnan(q[:, 9]).all())
+
+
+@pytest.mark.parametrize("t,ts,n,dim,group", [(BF16, BF16, 9001, 1030, 64), (F32, F32, 1003, 8200, 0),
+                                              (F16, F32, 120_001, 70, 32)])
+def test_outputs_of_more_than_the_caches_take(t, ts, n, dim, group):
+    """Of more than 32 MB together: the rows that calls of fewer give."""
+    gg, g = lib(), torch.Generator(device=DEV).manual_seed(dim)
+    x = torch.randn(n, dim, generator=g, device=DEV).to(t)
+    res = torch.randn(n, dim, generator=g, device=DEV).to(ts)
+    w = torch.rand(dim, generator=g, device=DEV) + 0.5
+    k = -(-dim // group) if group else 1
+
+    def outputs():
+        return (torch.full((n, dim), float("nan"), dtype=ts, device=DEV),
+                torch.full((n, dim), float("nan"), dtype=t, device=DEV),
+                torch.full((n, dim), float("nan"), device=DEV).to(E4M3),
+                torch.full((n, k), float("nan"), device=DEV), torch.full((n,), float("nan"), device=DEV))
+
+    def call(o, a, b):
+        s, y, q, sc, r = (p[a:b] for p in o)
+        gg.gg_rmsnorm_forward(gg.make_rows(x[a:b]), gg.make_rows(res[a:b]), b - a, dim, w, 1e-6,
+                              gg.make_rows(s), gg.make_rows(y),
+                              gg.make_rows(q, scales=sc, group=group), r)
+
+    whole, parts = outputs(), outputs()
+    assert sum(p[0].numel() * p.element_size() for p in whole[:3]) * n > 32 << 20
+    call(whole, 0, n)
+    step = (20 << 20) // (dim * 8)
+    assert step >= 256          # (the waves of a wide row go by whether there are 256 rows)
+    cut = list(range(0, n, step))
+    if n - cut[-1] < 256:
+        cut.pop()
+    for a, b in zip(cut, cut[1:] + [n]):
+        call(parts, a, b)
+    for a, b in zip(whole, parts):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))

@@ -60,3 +60,40 @@ def test_readme_example_runs_as_written():
           "shards": shards, "windows": windows, "_check": _check}
     exec(compile(_example(), "README.md", "exec"), ns)
     assert seen == list(range(len(windows)))
+
+
+def _student_example():
+    text = open(os.path.join(helpers.ROOT, "README.md")).read()
+    start = text.index("    from paper_2606_02916_amd import Student\n")
+    end = text.index("\n", text.index("    read_rows(", start))
+    return textwrap.dedent(text[start:end])
+
+
+def test_the_students_example_runs_as_written():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    print("the README's example of teaching a student", flush=True)
+    dev = torch.device("cuda:0")
+    g = torch.Generator(device=dev).manual_seed(1)
+    num_nodes, n, m = 5000, 900, 700
+    seeds = torch.randint(0, num_nodes, (800,), generator=g, device=dev)
+    logits = torch.randn(900, 47, generator=g, device=dev)      # a consumer's buffer, seeds first
+    nodes = torch.randint(0, num_nodes, (n,), generator=g, device=dev, dtype=torch.int32)
+    out = torch.empty(m, 100, device=dev)
+    ns = {"torch": torch, "num_nodes": num_nodes, "seeds": seeds, "logits": logits, "nodes": nodes,
+          "n": n, "m": m, "out": out}
+    lines = _student_example().split("\n")
+    at = next(i for i, ln in enumerate(lines) if ln.startswith("read_rows("))
+    lines.insert(at, "gathered = rows[:m]")
+    exec(compile("\n".join(lines), "README.md", "exec"), ns)
+    s, rows = ns["s"], ns["rows"]
+    assert int(s.status) == 0
+    assert ns["loss"].shape == (800,) and bool(torch.isfinite(ns["loss"]).all())
+    assert ns["z"].shape == (n, 47)
+    # the 8-bit rows are the nodes' normed rows to within a code's rounding
+    t = s.table[nodes[:m].long()].double()
+    y = t / (t.square().mean(1, keepdim=True) + s.eps / s.scale ** 2) ** 0.5 * s.w.double()
+    off = (out.double() - y).abs()
+    top = y.abs().amax(1, keepdim=True)
+    assert bool((off <= y.abs() * 2.0 ** -4 * 1.01 + top / 448 * 2.0 ** -10 * 1.01 +
+                 1e-5 * y.abs()).all())
