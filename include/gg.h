@@ -584,7 +584,8 @@ typedef struct gg_rows {
  * in order (8-bit rows that the fetch path gathered, back to fp32).  An id of
  * -1 (the padding of neighbour lists) gives a row of zeros, any other id
  * outside [0, num_rows) too, and sets GG_DEV_BAD_ID.  table: any type; out:
- * GG_F32, GG_F16 or GG_BF16, and no memory of the table's. */
+ * GG_F32, GG_F16 or GG_BF16, and no memory of the table's.  A call takes 2^32
+ * pieces at most: of 16 bytes of the wider type, or elements of rows of less. */
 int gg_embed_forward(const gg_rows_t* table, int64_t num_rows, int32_t dim, const void* ids_d,
                      int32_t id_bits, int64_t n, float scale, const gg_rows_t* out,
                      int32_t* status_d, hipStream_t stream);
@@ -601,7 +602,9 @@ size_t gg_ws_embed(int64_t n, int64_t num_rows, int32_t dim);
  * and ids out of range (GG_DEV_BAD_ID) add nothing.  The ids are sorted and
  * every row's terms are added in fp32 in an order that depends on the ids
  * alone, so results are reproducible bit for bit.  n and num_rows are at most
- * 2^31 - 2.  ws: 8-byte aligned. */
+ * 2^31 - 2; from about 2^25 ids on the sort is bound by its counters, whose reads
+ * grow with n^2 (2^24 ids of 8 fp16 1.1 ms, 2^25 9.6, 2^26 19).  ws: 8-byte
+ * aligned. */
 int gg_embed_backward(const gg_rows_t* dy, const void* ids_d, int32_t id_bits, int64_t n,
                       int64_t num_rows, int32_t dim, float scale, const gg_rows_t* grad,
                       int32_t flags, int32_t* status_d, void* ws, size_t ws_bytes,
@@ -669,7 +672,7 @@ int gg_distill_forward(const gg_rows_t* z, int64_t n, int64_t vocab, const void*
 /* The gradient alone, from the lse_d of the forward call; row_w_d may now hold
  * the gradient that reaches each row's loss.  q takes the rounding of lse, a few
  * |lse| 2^-24 of its size; rows with an lse of 4096 or more have theirs computed
- * again, by one workgroup where rows are split. */
+ * again, by one workgroup where rows are split (one row of 2^24 bf16 4.2 ms). */
 int gg_distill_backward(const gg_rows_t* z, int64_t n, int64_t vocab, const void* top_ids_d,
                         int32_t id_bits, int64_t ids_stride, const gg_rows_t* top, int32_t k,
                         float temperature, float weight, const float* row_w_d, const float* lse_d,

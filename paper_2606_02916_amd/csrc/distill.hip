@@ -297,7 +297,7 @@ __device__ __forceinline__ void store_entries(const DistillArgs& a, int64_t row,
 // Bound by memory where rows are long: 4,096 of 128,000 bf16, loss and gradient
 // 400 us, 5.2 TB/s read and written; the loss alone 214, 4.9; of 50,000 x 1,500 fp32
 // 49 us, 6.1.  Short rows are bound by what a row costs beside its logits, its
-// entries' softmax and the reductions: 1M of 9 with 5 entries 50 us.  Rows that do
+// entries' softmax and the reductions: 1M of 9 with 5 entries 55 us.  Rows that do
 // not start at 16 bytes have single elements up to the first boundary: 4,096 of 128,001
 // bf16 404 us, 5.2 TB/s (whole pieces from the row's start 506, every access of a wave
 // touching one line more).
@@ -596,7 +596,11 @@ __global__ void __launch_bounds__(kWave) k_distill_loss(DistillArgs a) {
 
 // The gradient of one split: reads it again and writes it.  64 rows of 262,144 fp32
 // 25 us with the gradient alone, 5.3 TB/s; 12 of 64 splits 7.6 us, whose first half
-// is the wait for ids, then logits at them, beside the split's own loads.
+// is the wait for ids, then logits at them, beside the split's own loads.  A far lse's
+// row is one block's: 64 rows of 262,144 bf16 126 us instead of 18, 12 of 200,003
+// fp32 112 instead of 8, one of 2^24 bf16 4.2 ms.  (That path takes registers, 86
+// instead of 47 in 16 bits and so five waves a SIMD instead of eight, but no time:
+// 64 rows of 262,144 bf16 17.5 us with it and 17.6 without, 512 107 both.)
 template <typename T, int V, int MODE>
 __global__ void __launch_bounds__(kBlock) k_distill_finish(DistillArgs a) {
   extern __shared__ __align__(16) char lds[];

@@ -111,7 +111,10 @@ __global__ void __launch_bounds__(kBlock) k_embed_rows(LookupArgs a) {
 // Each launch waits more than it works: 200,003 ids take four of 5, 13, 5 and 13
 // us, of which reading and writing the pairs at a copy's rate would be half a
 // microsecond each.  What they cost is the way through one tile: its load, the
-// counters of all tiles, the scan, LDS and the store.
+// counters of all tiles, the scan, LDS and the store.  Every tile reads every
+// tile's counters, 1 KB each: up to 2^24 ids those stay in an XCD's cache (1M ids
+// of 8 fp16 92 us for the whole call, 4.2M 236, 16.8M 1.1 ms), beyond they are the
+// call (33.6M 9.6 ms, 67M 19).
 // ---------------------------------------------------------------------------
 // Up to this many pairs find their places by counting, in a single launch.
 constexpr int kRankBlock = 1024;
@@ -379,9 +382,10 @@ __global__ void __launch_bounds__(NT) k_sort_scatter(Keys a, const int32_t* hist
 // Few pairs: a pair's place is the number of smaller keys, and of equal ones
 // before it.  A block has 64 pairs, one per lane, and its waves compare them
 // with a share of all keys each, which they read from LDS four at a time.  That
-// is n^2 comparisons, but on the whole chip and in one launch: 14,298 ids in
-// 20 us, where two passes over a tile in one block's LDS took 29 and four
-// launches of the other kernels 27.  Comparisons bound it.
+// is n^2 comparisons, but on the whole chip and in one launch.  Comparisons bound
+// it: rows of 64 fp32 added into 233,000, the whole call with this sort and with
+// four launches of the other kernels: 4,000 ids 16 and 26 us, 8,000 22 and 28,
+// 12,000 27 and 30, 14,298 29 both, 16,384 32 and 30.
 __global__ void __launch_bounds__(kRankBlock) k_sort_rank(Keys a, int blocks, uint32_t* key_out,
                                                           uint32_t* pos_out, FillArgs f) {
   if ((int)blockIdx.x >= blocks)

@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
     // The reciprocal in two parts, so that the codes are those of the quotient
     // rounded to fp32, at one operation an element more than a product with its
     // first part, which is a unit off and now and then another code (233,000 rows of
-    // 602 fp32 in groups of 64 137 us so, 143 this way, a quarter more divided outright).
+    // 602 fp32 in groups of 64 137 us so, 144 this way, a quarter more divided outright).
     const float inv = __builtin_amdgcn_rcpf(scale);
     const float low = __builtin_fmaf(-fminf(scale, kLargest), inv, 1.0f) * inv;
     const bool first = per_row ? p == 0 : (p & ((1 << a.group_lanes_log) - 1)) == 0;

@@ -92,7 +92,8 @@ class Student:
                               self._y if y else None, q, self.rstd, stream=stream)
 
     def forward(self, ids, n, x=None):
-        """Logits [n, classes] of the nodes ids[:n] on the current stream."""
+        """Logits [n, classes] of the nodes ids[:n] on the current stream: a view of
+        self.z, which the next forward overwrites and a step turns into the gradient."""
         self._normed(ids, n, x)
         if self._head is not self.head:
             self._head.copy_(self.head)
@@ -103,7 +104,8 @@ class Student:
         nodes may recur; -1 is skipped by the table) against the teacher's top
         classes top_ids [n, k] and their logits top [n, k]; row_w [n]: fp32
         weights of the rows (mean loss by default).  On the current stream;
-        returns the rows' weighted losses."""
+        returns the rows' weighted losses, a view of self.loss, which the next step
+        overwrites."""
         _shaped(top_ids, n, self.k, "top_ids"), _shaped(top, n, self.k, "top")
         self.forward(ids, n, x)
         weight = 1.0 if row_w is not None else 1.0 / max(n, 1)
