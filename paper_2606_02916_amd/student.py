@@ -141,5 +141,5 @@ def read_rows(buf, n, dim, group, out, status):
     if n > buf.shape[0]:
         raise gg.GGError(f"{n} rows of a buffer of {buf.shape[0]}")
     gg.gg_embed_forward(rows, buf.shape[0], dim, None, n, 1.0,
-                        gg.make_rows(_shaped(out, n, dim, "out")), status)
+                        gg.make_rows(out), status)
     return out

@@ -264,8 +264,8 @@ def test_the_student_checks_its_tensors():
             (lambda: s.write_rows(buf[:, :20], ids, 6), "8-bit rows"),
             (lambda: s.write_rows(buf, ids, 6, x=torch.zeros(5, 20)), "x of shape"),
             (lambda: student.read_rows(buf, 7, 20, 0, torch.zeros(7, 20), s.status), "buffer of 6"),
-            (lambda: student.read_rows(buf, 6, 20, 0, torch.zeros(5, 20), s.status), "out of shape"),
-            (lambda: student.read_rows(buf, 6, 20, 0, torch.zeros(6, 18), s.status), "out of shape")):
+            (lambda: student.read_rows(buf, 6, 20, 0, torch.zeros(5, 20), s.status), "out: 5 rows"),
+            (lambda: student.read_rows(buf, 6, 20, 0, torch.zeros(6, 18), s.status), "out: 6 rows")):
         with pytest.raises(gg.GGError, match=word):
             call()
 
