@@ -288,8 +288,7 @@ def _keep(s):
         else:
             r[k] = gg.make_rows(t, scales=s[k + "_scales"], group=group)
     size = {"norm_grad": lambda: gg.gg_ws_layernorm(c["n"], c["dim"]),
-            "product": lambda: gg.gg_ws_product(c["n"], c["k"], c["m"]),
-            "product_grad": lambda: gg.gg_ws_product_backward(c["n"], c["k"], c["m"]),
+            "product_grad": lambda: gg.gg_ws_product(c["n"], c["k"], c["m"]),
             }.get(op, lambda: 0)()
     s["ws"] = torch.empty(max(size, 1), dtype=torch.uint8, device="cuda")
 
@@ -346,7 +345,7 @@ def _own_blocks(s):
 def _own_product(s):
     from paper_2606_02916_amd import gg
     c, r = s["c"], s["r"]
-    gg.gg_product_forward(r["a"], c["n"], c["k"], r["w"], c["m"], r["out"], s["ws"])
+    gg.gg_product_forward(r["a"], c["n"], c["k"], r["w"], c["m"], r["out"])
     return {"out": s["out"]}
 
 
