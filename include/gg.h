@@ -635,12 +635,65 @@ size_t gg_ws_rmsnorm(int64_t n, int32_t dim);
  * mean(dy w s)) is the gradient of x and of res alike; dw_d [dim] (fp32, or
  * NULL: not wanted) = sum over the rows of dy s rstd, in an order that depends
  * on n and dim alone.  dy has the type of y, and s, dsum and dx one type: that
- * one or GG_F32.  dx may be the memory of dsum, dy or s.  ws: for dw_d only,
+ * one or GG_F32; s may also be 8-bit rows (what gg_quantise_rows made of it).  dx may be
+ * the memory of dsum, dy or s (not in 8 bits).  ws: for dw_d only,
  * 16-byte aligned. */
 int gg_rmsnorm_backward(const gg_rows_t* dy, const gg_rows_t* dsum, const gg_rows_t* s,
                         const float* rstd_d, int64_t n, int32_t dim, const void* w_d,
                         int32_t w_dtype, const gg_rows_t* dx, float* dw_d, void* ws,
                         size_t ws_bytes, hipStream_t stream);
+
+/* Layer norm of n rows: s = x + res (res NULL: s = x), mean and rstd =
+ * (mean((s - mean)^2) + eps)^-1/2 over the row, y = (s - mean) * rstd * w + b (w_d NULL:
+ * ones, b_d NULL: zeros; both of w_dtype), in fp32 from the unrounded s, the variance
+ * about the mean that was just taken.  Outputs, each NULL where it is not wanted: sum
+ * (s), y, q (y in 8 bits), kept (s in 8 bits, for the gradient), mean_d and rstd_d
+ * [n].  Types, scales, codes and aliases as gg_rmsnorm_forward's, kept as q.  A row whose
+ * sum passes fp32's range has NaNs, one whose squares' sum does rstd 0; with eps 0 a row of
+ * equal elements has NaNs. */
+int gg_layernorm_forward(const gg_rows_t* x, const gg_rows_t* res, int64_t n, int32_t dim,
+                         const void* w_d, const void* b_d, int32_t w_dtype, float eps,
+                         const gg_rows_t* sum, const gg_rows_t* y, const gg_rows_t* q,
+                         const gg_rows_t* kept, float* mean_d, float* rstd_d, hipStream_t stream);
+
+size_t gg_ws_layernorm(int64_t n, int32_t dim);
+
+/* Its gradient.  With g = dy w and h = (s - mean) rstd: dx = dsum + rstd * (g -
+ * mean(g) - h mean(g h)), dw_d = sum over the rows of dy h, db_d = of dy (fp32 [dim], each
+ * NULL where it is not wanted), in an order that depends on n and dim alone.  s: as the
+ * forward call's sum or, in 8 bits, kept; then dx and dsum have the type of dy or
+ * GG_F32.  All else as gg_rmsnorm_backward. */
+int gg_layernorm_backward(const gg_rows_t* dy, const gg_rows_t* dsum, const gg_rows_t* s,
+                          const float* mean_d, const float* rstd_d, int64_t n, int32_t dim,
+                          const void* w_d, int32_t w_dtype, const gg_rows_t* dx, float* dw_d,
+                          float* db_d, void* ws, size_t ws_bytes, hipStream_t stream);
+
+#define GG_QUANTISE_MAX_DIM (1 << 24)
+#define GG_SCALE_BLOCK 128    /* rows and columns of 8-bit weights that share a scale */
+
+/* A matrix of weights in 8 bits on the device: row r's e4m3 codes lie back to back at
+ * data + r * stride (bytes; any), and the element in column c stands for code times the
+ * fp32 scale number c / 128 at scales + r / 128 * scales_stride (bytes; a multiple of
+ * 4).  The last blocks of a row or column may be smaller. */
+typedef struct gg_blocks {
+  void* data;
+  int64_t stride;
+  void* scales;
+  int64_t scales_stride;
+} gg_blocks_t;
+
+/* Rows into 8 bits: of each group of q's, or with group 0 of each row, scale =
+ * max(max|x| / 448, 2^-126) and codes x / scale, rounded as gg_rmsnorm_forward's (a
+ * zero of either sign for a zero); NaNs and infinities as there.  x: GG_F32, GG_F16 or GG_BF16; q: GG_E4M3, and no memory of
+ * x's. */
+int gg_quantise_rows(const gg_rows_t* x, int64_t n, int64_t dim, const gg_rows_t* q,
+                     hipStream_t stream);
+
+/* Weights w [rows][cols] into 8 bits, scales and codes by blocks of 128 x 128 as above:
+ * as they are (q), transposed (qt [cols][rows], for the way back), or both in one pass;
+ * either may be NULL. */
+int gg_quantise_blocks(const gg_rows_t* w, int64_t rows, int64_t cols, const gg_blocks_t* q,
+                       const gg_blocks_t* qt, hipStream_t stream);
 
 #define GG_DISTILL_MAX_ROWS (1LL << 27)
 #define GG_DISTILL_MAX_VOCAB (1 << 24)

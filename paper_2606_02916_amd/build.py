@@ -12,8 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libgg.so")
 SOURCES = ["common.hip", "sample.hip", "hotset.hip", "bucket.hip", "stage.hip", "gather.hip",
-           "sim.hip", "sage.hip", "embed.hip", "norm.hip",
-           "distill.hip"]
+           "sim.hip", "sage.hip", "embed.hip", "norm.hip", "layernorm.hip",
+           "quantise.hip", "distill.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

@@ -1,0 +1,67 @@
+// 8-bit rows: the scale of a group of elements, and their codes.
+#pragma once
+
+#include "rows.hpp"
+
+namespace gg {
+
+constexpr float kE4M3Max = 448.0f;
+constexpr float kScaleMin = 1.17549435e-38f;   // 2^-126
+constexpr float kLargest = 3.4028235e38f;
+
+// Weights in 8 bits, passed by value: row r's codes at p + r * stride, the scale of
+// its columns 128 c .. 128 c + 127 at scales + r / 128 * sstride + 4 c.
+struct KBlocks {
+  char* p;
+  int64_t stride;
+  char* scales;
+  int64_t sstride;
+};
+
+constexpr int32_t kScaleBlock = GG_SCALE_BLOCK;
+
+// Checks [rows][cols] weights in 8 bits and packs them.
+int pack_blocks(const gg_blocks_t* b, const char* name, int64_t rows, int64_t cols, bool written,
+                KBlocks* out);
+
+// Largest magnitude, as bits, of a piece's own elements: only a row's last
+// piece has others (skip > 0).
+template <int V>
+__device__ __forceinline__ uint32_t magnitude(const float (&v)[V], int32_t skip) {
+  uint32_t m = 0;
+  if (skip == 0) {
+#pragma unroll
+    for (int k = 0; k < V; ++k) m = max(m, __float_as_uint(v[k]) & 0x7fffffffu);
+  } else {
+#pragma unroll
+    for (int k = 0; k < V; ++k) m = max(m, k >= skip ? __float_as_uint(v[k]) & 0x7fffffffu : 0u);
+  }
+  return m;
+}
+
+// max / 448 rounded as a division, and the least scale; a NaN or an infinity stays.
+__device__ __forceinline__ float scale_of(float m) {
+  constexpr float kInv = 1.0f / kE4M3Max;
+  const float q = m * kInv;
+  const float scale = __builtin_fmaf(__builtin_fmaf(-fminf(q, kLargest), kE4M3Max, m), kInv, q);
+  return scale < kScaleMin ? kScaleMin : scale;
+}
+
+// The codes of a group are the quotients by its scale, by a reciprocal in two
+// parts: at one operation an element more than a product with its first part, which
+// is a unit off and now and then another code (233,000 rows of 602 fp32 in groups of 64
+// normed 137 us so, 144 this way, a quarter more divided outright).  Of all pairs of an
+// element and a group's largest one in bf16 and fp16 none has another quotient than the
+// division's, whichever way the reciprocal is rounded.  (A zero may lose its sign.)
+struct Quotient {
+  float inv, low;
+  __device__ __forceinline__ explicit Quotient(float scale) {
+    inv = __builtin_amdgcn_rcpf(scale);
+    low = __builtin_fmaf(-fminf(scale, kLargest), inv, 1.0f) * inv;
+  }
+  __device__ __forceinline__ float operator()(float v) const {
+    return __builtin_fmaf(v, inv, v * low);
+  }
+};
+
+}  // namespace gg

@@ -118,8 +118,16 @@ class gg_rows_t(C.Structure):
     rows = cols = 1 << 62
 
 
+class gg_blocks_t(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64), ("scales", C.c_void_p),
+                ("scales_stride", C.c_int64)]
+    rows = cols = 1 << 62
+
+
 GG_F32, GG_F16, GG_BF16, GG_E4M3 = 0, 1, 2, 3
 GG_EMBED_ADD = 1
+GG_PRODUCT_ADD = 1
+GG_SCALE_BLOCK = 128
 STAGE_STATS_BYTES = C.sizeof(gg_stage_stats_t)
 GATHER_STATS_BYTES = C.sizeof(gg_gather_stats_t)
 SIM_ACC_BYTES = C.sizeof(gg_sim_acc_t)
@@ -161,6 +169,13 @@ SIGNATURES = {
     "gg_rmsnorm_forward": (C.c_int, [_P, _P, _I64, _I32, _P, _I32, C.c_float, _P, _P, _P, _P, _P]),
     "gg_ws_rmsnorm": (_SZ, [_I64, _I32]),
     "gg_rmsnorm_backward": (C.c_int, [_P, _P, _P, _P, _I64, _I32, _P, _I32, _P, _P, _P, _SZ, _P]),
+    "gg_layernorm_forward": (C.c_int, [_P, _P, _I64, _I32, _P, _P, _I32, C.c_float, _P, _P, _P, _P,
+                                       _P, _P, _P]),
+    "gg_ws_layernorm": (_SZ, [_I64, _I32]),
+    "gg_layernorm_backward": (C.c_int, [_P, _P, _P, _P, _P, _I64, _I32, _P, _I32, _P, _P, _P, _P, _SZ,
+                                        _P]),
+    "gg_quantise_rows": (C.c_int, [_P, _I64, _I64, _P, _P]),
+    "gg_quantise_blocks": (C.c_int, [_P, _I64, _I64, _P, _P, _P]),
     "gg_ws_distill": (_SZ, [_I64, _I64]),
     "gg_distill_forward": (C.c_int, [_P, _I64, _I64, _P, _I32, _I64, _P, _I32, C.c_float, C.c_float,
                                      _P, _P, _P, _P, _P, _P, _SZ, _P]),
@@ -513,6 +528,8 @@ def _rows(r, n, cols, what):
     """Address of a description of at least n rows of cols elements."""
     if r is None:
         return None
+    if not isinstance(r, gg_rows_t):
+        raise GGError(f"{what}: rows come from make_rows")
     if n > r.rows or cols > r.cols:
         raise GGError(f"{what}: {r.rows} rows of {r.cols} elements for {n} of {cols}")
     return C.byref(r)
@@ -590,6 +607,87 @@ def gg_rmsnorm_backward(dy, dsum, s, rstd, n, dim, w, dx, dw, ws, stream=None):
                                          wt, _rows(dx, n, dim, "dx"), _fp32(dw, dim, "dw"),
                                          _ptr(ws), 0 if ws is None else ws.numel(),
                                          _stream(stream)), "gg_rmsnorm_backward")
+
+
+def _bias(w, b, dim, what):
+    """Addresses of dim contiguous weights and biases (either may be None), and their dtype."""
+    if w is not None and b is not None and w.dtype != b.dtype:
+        raise GGError(f"{what}: weights of {w.dtype} and biases of {b.dtype}")
+    (wp, wt), (bp, bt) = _weight(w, dim, what), _weight(b, dim, what)
+    return wp, bp, wt if w is not None else bt
+
+
+def gg_layernorm_forward(x, res, n, dim, w, b, eps, sum, y, q, kept, mean, rstd, stream=None):
+    """x, res, sum, y, q, kept: make_rows, or None (all but x); w and b: dim values of
+    one type, or None."""
+    wp, bp, wt = _bias(w, b, dim, "gg_layernorm_forward")
+    return check(lib.gg_layernorm_forward(_rows(x, n, dim, "x"), _rows(res, n, dim, "res"), n, dim, wp,
+                                          bp, wt, eps, _rows(sum, n, dim, "sum"),
+                                          _rows(y, n, dim, "y"), _rows(q, n, dim, "q"),
+                                          _rows(kept, n, dim, "kept"), _fp32(mean, n, "mean"),
+                                          _fp32(rstd, n, "rstd"), _stream(stream)),
+                 "gg_layernorm_forward")
+
+
+def gg_ws_layernorm(n, dim):
+    return int(lib.gg_ws_layernorm(n, dim))
+
+
+def gg_layernorm_backward(dy, dsum, s, mean, rstd, n, dim, w, dx, dw, db, ws, stream=None):
+    """dy, dsum, s, dx: make_rows (dsum may be None; s: the forward call's sum, or
+    kept); dw, db and ws may be None."""
+    ptr, wt = _weight(w, dim, "gg_layernorm_backward")
+    return check(lib.gg_layernorm_backward(_rows(dy, n, dim, "dy"), _rows(dsum, n, dim, "dsum"),
+                                           _rows(s, n, dim, "s"), _fp32(mean, n, "mean"),
+                                           _fp32(rstd, n, "rstd"), n, dim, ptr, wt,
+                                           _rows(dx, n, dim, "dx"), _fp32(dw, dim, "dw"),
+                                           _fp32(db, dim, "db"), _ptr(ws),
+                                           0 if ws is None else ws.numel(), _stream(stream)),
+                 "gg_layernorm_backward")
+
+
+def make_blocks(t, scales):
+    """Weights in 8 bits: a 2-d e4m3 tensor whose rows are contiguous (any stride
+    between them) and the fp32 scales [row blocks, column blocks] of its blocks of
+    128 x 128.  The description keeps its tensors alive."""
+    if t.dtype != torch.float8_e4m3fn or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise GGError("blocks must be a 2-d e4m3 tensor with contiguous rows")
+    want = tuple(-(-d // GG_SCALE_BLOCK) for d in t.shape)
+    if scales.dtype != torch.float32 or tuple(scales.shape) != want or \
+            (want[1] > 1 and scales.stride(1) != 1):
+        raise GGError(f"scales must be fp32 of shape {want} with contiguous rows")
+    b = gg_blocks_t()
+    b.data, b.stride = t.data_ptr(), t.stride(0)
+    b.scales, b.scales_stride = scales.data_ptr(), scales.stride(0) * 4
+    b.rows, b.cols = t.shape
+    b.keep = (t, scales)
+    return b
+
+
+def _blocks(b, rows, cols, what):
+    """Address of a description of just [rows, cols] weights: the scales' blocks go
+    by the shape."""
+    if b is None:
+        return None
+    if not isinstance(b, gg_blocks_t):
+        raise GGError(f"{what}: weights in 8 bits come from make_blocks")
+    if (b.rows, b.cols) != (rows, cols) and b.rows != 1 << 62:
+        raise GGError(f"{what}: weights of [{b.rows}, {b.cols}] for [{rows}, {cols}]")
+    return C.byref(b)
+
+
+def gg_quantise_rows(x, n, dim, q, stream=None):
+    """x and q: make_rows of [n, dim] tensors, q's in 8 bits."""
+    return check(lib.gg_quantise_rows(_rows(x, n, dim, "x"), n, dim, _rows(q, n, dim, "q"),
+                                      _stream(stream)), "gg_quantise_rows")
+
+
+def gg_quantise_blocks(w, rows, cols, q, qt, stream=None):
+    """w: make_rows of a [rows, cols] tensor; q and qt: make_blocks of a [rows, cols]
+    and a [cols, rows] tensor, either may be None."""
+    return check(lib.gg_quantise_blocks(_rows(w, rows, cols, "w"), rows, cols,
+                                        _blocks(q, rows, cols, "q"), _blocks(qt, cols, rows, "qt"),
+                                        _stream(stream)), "gg_quantise_blocks")
 
 
 def gg_ws_distill(n, vocab):

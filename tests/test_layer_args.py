@@ -1,0 +1,190 @@
+"""Host-side argument checks of the calls for layers in 8 bits: a bad call is refused
+with a message before anything is enqueued, so no GPU is needed.  Addresses here are
+numbers that nothing reads."""
+import ctypes as C
+import os
+import subprocess
+import tempfile
+
+import pytest
+import torch
+
+from paper_2606_02916_amd import gg
+from tests.test_operator_args import P, ROOT, refused, rows
+
+
+def blocks(data=P, stride=400, scales=P, scales_stride=64):
+    b = gg.gg_blocks_t()
+    b.data, b.stride, b.scales, b.scales_stride = data, stride, scales, scales_stride
+    return b
+
+
+def test_blocks_layout_matches_the_header():
+    src = r"""
+#include <stddef.h>
+#include <stdio.h>
+#include "gg.h"
+int main() {
+  printf("%zu %zu %zu %zu %zu %d\n", sizeof(gg_blocks_t), offsetof(gg_blocks_t, data),
+         offsetof(gg_blocks_t, stride), offsetof(gg_blocks_t, scales),
+         offsetof(gg_blocks_t, scales_stride), GG_SCALE_BLOCK);
+}
+"""
+    d = tempfile.mkdtemp(prefix="ggblocks_")
+    with open(os.path.join(d, "p.cpp"), "w") as f:
+        f.write(src)
+    subprocess.run(["g++", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
+                    "-I" + os.path.join(ROOT, "include"), os.path.join(d, "p.cpp"), "-o",
+                    os.path.join(d, "p")], check=True)
+    got = [int(x) for x in subprocess.run([os.path.join(d, "p")], capture_output=True,
+                                          text=True).stdout.split()]
+    B = gg.gg_blocks_t
+    assert got == [C.sizeof(B), B.data.offset, B.stride.offset, B.scales.offset,
+                   B.scales_stride.offset, gg.GG_SCALE_BLOCK]
+
+
+NORM = dict(x=rows(), res=None, n=7, dim=100, w=P, b=P, w_dtype=gg.GG_F32, eps=1e-6, sum=None,
+            y=rows(), q=None, kept=None, mean=P, rstd=P, stream=None)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(dim=0), "dim"), (dict(dim=16385), "dim"), (dict(n=-1), "n = -1"), (dict(n=1 << 28), "n = "),
+    (dict(eps=-1.0), "eps"), (dict(eps=float("nan")), "eps"),
+    (dict(y=None, rstd=None, mean=None), "output"), (dict(x=None), "x: "),
+    (dict(x=rows(gg.GG_E4M3)), "x: dtype"), (dict(w_dtype=gg.GG_F16), "weights"),
+    (dict(w=None, w_dtype=gg.GG_F16), "weights"), (dict(w=P + 2), "weights"), (dict(b=P + 2), "bias"),
+    (dict(rstd=P + 2), "rstd"), (dict(mean=P + 2), "mean"), (dict(y=rows(gg.GG_BF16)), "y: dtype"),
+    (dict(y=rows(stride=200)), "y: stride"), (dict(res=rows(gg.GG_F16)), "res: dtype"),
+    (dict(q=rows()), "q: dtype"), (dict(kept=rows()), "kept: dtype"),
+    (dict(kept=rows(gg.GG_E4M3, group=512)), "kept: group"),
+    (dict(kept=rows(gg.GG_E4M3, group=16, scales_stride=24)), "kept: scales"),
+    (dict(kept=rows(gg.GG_E4M3, stride=99)), "kept: stride"),
+    (dict(x=rows(gg.GG_BF16), y=rows(gg.GG_BF16), res=rows(gg.GG_BF16), sum=rows()), "differ")])
+def test_norm_refuses(change, word):
+    refused(gg.lib.gg_layernorm_forward, NORM, change, word)
+
+
+NORM_BACK = dict(dy=rows(), dsum=None, s=rows(), mean=P, rstd=P, n=7, dim=100, w=P, w_dtype=gg.GG_F32,
+                 dx=rows(), dw=P, db=P, ws=P, ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(dim=0), "dim"), (dict(n=-1), "n = -1"), (dict(dy=None), "dy"), (dict(s=None), "s: "),
+    (dict(s=rows(gg.GG_F16)), "s: dtype"), (dict(dx=rows(gg.GG_F16)), "dx: dtype"),
+    (dict(s=rows(gg.GG_E4M3), dx=rows(gg.GG_F16)), "dx: dtype"),
+    (dict(s=rows(gg.GG_E4M3), dx=rows(gg.GG_E4M3)), "dx: dtype"),
+    (dict(s=rows(gg.GG_E4M3, group=8)), "s: group"), (dict(s=rows(gg.GG_E4M3, scales=None)), "s: "),
+    (dict(dsum=rows(gg.GG_BF16)), "dsum: dtype"), (dict(rstd=None), "rstd"), (dict(mean=None), "mean"),
+    (dict(mean=P + 1), "mean"), (dict(dw=P + 1), "dw"), (dict(db=P + 1), "db"),
+    (dict(w_dtype=gg.GG_BF16), "weights"), (dict(w=P + 1), "weights"), (dict(ws=None), "workspace"),
+    (dict(ws=P + 8), "workspace"), (dict(ws_bytes=16), "workspace"),
+    (dict(dw=None, ws=None), "workspace"),
+    (dict(ws_bytes=gg.gg_ws_rmsnorm(7, 100)), "workspace"), (dict(dx=rows(stride=4)), "dx: stride")])
+def test_norm_gradient_refuses(change, word):
+    refused(gg.lib.gg_layernorm_backward, NORM_BACK, change, word)
+
+
+Q8 = rows(gg.GG_E4M3, group=16)
+ROWS = dict(x=rows(), n=7, dim=100, q=Q8, stream=None)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(dim=0), "dim"), (dict(dim=(1 << 24) + 1), "dim"), (dict(n=-1), "n = -1"),
+    (dict(n=1 << 28), "n = "), (dict(x=None), "x: "), (dict(q=None), "q: "),
+    (dict(x=rows(gg.GG_E4M3)), "x: dtype"), (dict(q=rows()), "q: dtype"),
+    (dict(x=rows(data=P + 2)), "x: not aligned"), (dict(q=rows(gg.GG_E4M3, stride=99)), "q: stride"),
+    (dict(q=rows(gg.GG_E4M3, group=24)), "q: group"), (dict(q=rows(gg.GG_E4M3, scales=None)), "q: "),
+    (dict(q=rows(gg.GG_E4M3, group=16, scales_stride=24)), "q: scales")])
+def test_rows_refuse(change, word):
+    refused(gg.lib.gg_quantise_rows, ROWS, change, word)
+
+
+BLOCKS = dict(w=rows(stride=1200), rows=200, cols=300, q=blocks(), qt=blocks(), stream=None)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(rows=0), "rows 0"), (dict(cols=0), "cols 0"), (dict(rows=(1 << 24) + 1), "rows"),
+    (dict(cols=(1 << 24) + 1), "cols"), (dict(q=None, qt=None), "output"), (dict(w=None), "w: "),
+    (dict(w=rows(gg.GG_E4M3)), "w: dtype"), (dict(q=blocks(data=None)), "q: data"),
+    (dict(q=blocks(scales=None)), "q: data or scales"), (dict(q=blocks(stride=299)), "q: stride"),
+    (dict(qt=blocks(stride=199)), "qt: stride"), (dict(q=blocks(scales=P + 2)), "q: scales"),
+    (dict(q=blocks(scales_stride=8)), "q: scales"), (dict(qt=blocks(scales_stride=4)), "qt: scales"),
+    (dict(q=blocks(scales_stride=14)), "q: scales"), (dict(q=blocks(stride=-400)), "q: stride")])
+def test_blocks_refuse(change, word):
+    refused(gg.lib.gg_quantise_blocks, BLOCKS, change, word)
+
+
+def test_make_blocks_refuses_what_it_cannot_describe():
+    q, sc = torch.zeros(130, 300, dtype=torch.float8_e4m3fn), torch.zeros(2, 3)
+    b = gg.make_blocks(q[:, 4:260], torch.zeros(2, 9)[:, 3:5])
+    assert (b.stride, b.scales_stride, b.rows, b.cols) == (300, 36, 130, 256)
+    for bad in (lambda: gg.make_blocks(q.view(torch.uint8), sc), lambda: gg.make_blocks(q[0], sc),
+                lambda: gg.make_blocks(q[:, ::2], sc), lambda: gg.make_blocks(q.t(), sc.t()),
+                lambda: gg.make_blocks(q, sc.double()), lambda: gg.make_blocks(q, torch.zeros(3, 2).t()),
+                lambda: gg.make_blocks(q, torch.zeros(2, 2)), lambda: gg.make_blocks(q, torch.zeros(130, 3))):
+        with pytest.raises(gg.GGError):
+            bad()
+
+
+def test_workspaces():
+    assert gg.gg_ws_layernorm(-1, 9) == gg.gg_ws_layernorm(9, 0) == gg.gg_ws_layernorm(9, 16_385) == 0
+    got = [gg.gg_ws_layernorm(n, 100) for n in (0, 1, 7, 700, 1023, 1024, 5000, 1 << 27)]
+    assert got == sorted(got) and got[-1] == 2 * 1024 * 400
+
+
+def test_bindings_check_shapes():
+    """No description of fewer rows or narrower ones than the call goes over, of other
+    weights, or of another kind: refused before the stream is asked for."""
+    r = lambda *shape: gg.make_rows(torch.zeros(*shape))  # noqa: E731
+    r8 = lambda n, d: gg.make_rows(torch.zeros(n, d, dtype=torch.float8_e4m3fn),  # noqa: E731
+                                   scales=torch.zeros(n))
+    b = lambda n, d: gg.make_blocks(torch.zeros(n, d, dtype=torch.float8_e4m3fn),  # noqa: E731
+                                    torch.zeros(-(-n // 128), -(-d // 128)))
+    good, vec, w = r(7, 20), torch.zeros(7), torch.zeros(20)
+    for name in ("short", "narrow"):
+        bad, bad8 = (r(6, 20), r8(6, 20)) if name == "short" else (r(7, 19), r8(7, 19))
+        for call in (
+                lambda: gg.gg_layernorm_forward(bad, good, 7, 20, None, None, 1e-6, good, good, None,
+                                                None, None, None),
+                lambda: gg.gg_layernorm_forward(good, bad, 7, 20, None, None, 1e-6, good, good, None,
+                                                None, None, None),
+                lambda: gg.gg_layernorm_forward(good, good, 7, 20, None, None, 1e-6, bad, good, None,
+                                                None, None, None),
+                lambda: gg.gg_layernorm_forward(good, good, 7, 20, None, None, 1e-6, good, bad, None,
+                                                None, None, None),
+                lambda: gg.gg_layernorm_forward(good, good, 7, 20, None, None, 1e-6, good, good, bad8,
+                                                None, None, None),
+                lambda: gg.gg_layernorm_forward(good, good, 7, 20, None, None, 1e-6, good, good, None,
+                                                bad8, None, None),
+                lambda: gg.gg_layernorm_backward(bad, None, good, vec, vec, 7, 20, None, good, None, None,
+                                                 None),
+                lambda: gg.gg_layernorm_backward(good, bad, good, vec, vec, 7, 20, None, good, None, None,
+                                                 None),
+                lambda: gg.gg_layernorm_backward(good, None, bad8, vec, vec, 7, 20, None, good, None,
+                                                 None, None),
+                lambda: gg.gg_layernorm_backward(good, None, good, vec, vec, 7, 20, None, bad, None, None,
+                                                 None),
+                lambda: gg.gg_quantise_rows(bad, 7, 20, r8(7, 20)),
+                lambda: gg.gg_quantise_rows(good, 7, 20, bad8),
+                lambda: gg.gg_quantise_blocks(bad, 7, 20, b(7, 20), None)):
+            with pytest.raises(gg.GGError, match="rows of"):
+                call()
+    for call, word in (
+            (lambda: gg.gg_layernorm_forward(good, None, 7, 20, w, w.half(), 1e-6, good, None, None, None,
+                                             None, None), "biases of"),
+            (lambda: gg.gg_layernorm_forward(good, None, 7, 20, w[:19], None, 1e-6, good, None, None,
+                                             None, None, None), "weights must"),
+            (lambda: gg.gg_layernorm_forward(good, None, 7, 20, None, w[:19], 1e-6, good, None, None,
+                                             None, None, None), "weights must"),
+            (lambda: gg.gg_layernorm_forward(good, None, 7, 20, None, None, 1e-6, good, None, None, None,
+                                             vec[:6], None), "mean"),
+            (lambda: gg.gg_layernorm_backward(good, None, good, vec[:6], vec, 7, 20, None, good, None,
+                                              None, None), "mean"),
+            (lambda: gg.gg_layernorm_backward(good, None, good, vec, vec, 7, 20, None, good, None, vec,
+                                              None), "db"),
+            (lambda: gg.gg_quantise_blocks(good, 7, 20, b(7, 21), None), "q: weights of"),
+            (lambda: gg.gg_quantise_blocks(good, 7, 20, None, b(7, 20)), "qt: weights of"),
+            (lambda: gg.gg_quantise_blocks(good, 7, 20, r8(7, 20), None), "make_blocks"),
+            (lambda: gg.gg_quantise_rows(good, 7, 20, b(7, 20)), "make_rows")):
+        with pytest.raises(gg.GGError, match=word):
+            call()
