@@ -695,6 +695,22 @@ int gg_quantise_rows(const gg_rows_t* x, int64_t n, int64_t dim, const gg_rows_t
 int gg_quantise_blocks(const gg_rows_t* w, int64_t rows, int64_t cols, const gg_blocks_t* q,
                        const gg_blocks_t* qt, hipStream_t stream);
 
+#define GG_PRODUCT_MAX_ROWS (1LL << 27)
+#define GG_PRODUCT_MAX_DIM (1 << 24)
+
+/* The product of 8-bit rows a [n][k] (group 128, or 0) with 8-bit weights b [m][k]:
+ * out[i][j] = sum over c of a[i][c] b[j][c], rounded once to out's type (GG_F32, GG_F16
+ * or GG_BF16).  Each 128 columns' codes are multiplied and added in matrix
+ * instructions, their sum scaled and added in fp32, in an order that depends on the sizes
+ * alone.  For GG_F32 the products are exact and their sums fp32.  For 16-bit outputs
+ * the 8-bit instructions add the products of columns 8 c .. 8 c + 7 at a time, each cut off
+ * below 2^-13 of the largest one's power of two (codes below 2^-6 counting as that): some
+ * 2^-16 of a result, at twice the rate.  The gradient of the rows is the same call on the output's gradient in 8
+ * bits and the transposed weights (gg_quantise_rows, gg_quantise_blocks).  out is no
+ * memory of a or b. */
+int gg_product_forward(const gg_rows_t* a, int64_t n, int64_t k, const gg_blocks_t* b, int64_t m,
+                       const gg_rows_t* out, hipStream_t stream);
+
 #define GG_DISTILL_MAX_ROWS (1LL << 27)
 #define GG_DISTILL_MAX_VOCAB (1 << 24)
 #define GG_DISTILL_MAX_K 256

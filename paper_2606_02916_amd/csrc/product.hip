@@ -1,0 +1,367 @@
+// The product of 8-bit rows with 8-bit weights:
+//   out[i][j] = sum_g sa[i][g] sb[j / 128][g] sum_{k in block g} a[i][k] b[j][k],
+// codes multiplied by matrix instructions over a block of 128, each block's sum scaled
+// and added in fp32.
+#include "codes.hpp"
+
+namespace gg {
+namespace {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef bf16 v8bf __attribute__((ext_vector_type(8)));
+
+constexpr int32_t kBlockK = kScaleBlock;   // bytes of a row in a step
+
+struct ProductArgs {
+  KRows a, out;
+  KBlocks b;
+  int64_t n;
+  int32_t k, m, kb;            // kb: blocks of k
+  int32_t per_row;             // a has one scale a row
+  int32_t tiles_i, tiles_j;
+};
+
+// 16 bytes of a row's codes from column c on, zeros behind its end.
+__device__ __forceinline__ v4i load_codes(const char* row, int32_t c, int32_t k) {
+  v4i v = {};
+  if (c + 16 <= k) {
+    typedef v4i mem __attribute__((aligned(1)));
+    v = *(const GG_GLOBAL mem*)(row + c);
+  } else {
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (c + 4 * w + i < k)
+          v[w] |= (int)((uint32_t) * (const GG_GLOBAL uint8_t*)(row + c + 4 * w + i) << 8 * i);
+  }
+  return v;
+}
+
+// A lane's 32 codes as the operand of a product of 16 rows by 16 rows over 128
+// columns.  Which columns a lane has does not matter, both operands agree on it.
+//
+// The 8-bit matrix instructions add eight products at a time (a lane's codes 8 c .. 8 c +
+// 7) and drop, towards zero, what lies below 2^-13 of the largest one's power of two:
+// 2^-16 of the result where codes are normally distributed, 2^-14 where they are spread
+// over many powers of two.  That is well below the rounding of a 16-bit output (2^-9,
+// 2^-12) and not of a 32-bit one, whose codes are multiplied as bf16: exact products,
+// added in fp32, at half the rate.
+template <bool EXACT>
+struct Codes {
+  v8i v;
+  __device__ __forceinline__ void set(v4i lo, v4i hi) {
+    v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+};
+template <>
+struct Codes<true> {
+  v8bf v[4];
+  __device__ __forceinline__ void set(v4i lo, v4i hi) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int w0 = i < 2 ? lo[2 * i] : hi[2 * i - 4], w1 = i < 2 ? lo[2 * i + 1] : hi[2 * i - 3];
+      const v2bf p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)w0, 1.0f, false),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)w0, 1.0f, true),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)w1, 1.0f, false),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)w1, 1.0f, true)};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = p[j / 2][j % 2];
+    }
+  }
+};
+
+__device__ __forceinline__ v4f multiply(const Codes<false>& a, const Codes<false>& b) {
+  // e4m3 by e4m3, without scales of the instruction's own
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.v, b.v, v4f{}, 0, 0, 0, 0, 0, 0);
+}
+__device__ __forceinline__ v4f multiply(const Codes<true>& a, const Codes<true>& b) {
+  v4f d = {};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[i], b.v[i], d, 0, 0, 0);
+  return d;
+}
+
+// Four columns of a row of the output.
+template <typename O>
+__device__ __forceinline__ void store_four(const KRows& out, int64_t i, int32_t j, int32_t m, v4f v) {
+  char* to = out.p + i * out.stride + j * (int64_t)sizeof(O);
+  const float f[4] = {v[0], v[1], v[2], v[3]};
+  if (j + 4 <= m) {
+    row_store<O, 4>(to, f);
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float one[1] = {f[r]};
+      if (j + r < m) row_store<O, 1>(to + r * sizeof(O), one);
+    }
+  }
+}
+
+// A tile's place: each of the 8 XCDs, which take blocks in turn, has a run of tiles,
+// and in it bands of kBand tiles of rows, so that the blocks on one L2 at a time share
+// rows and weights.
+constexpr int32_t kXcds = 8, kBand = 4;
+
+__device__ __forceinline__ void tile_place(const ProductArgs& a, int32_t* ti, int32_t* tj) {
+  const uint32_t total = gridDim.x, b = blockIdx.x, x = b % kXcds, q = total / kXcds,
+                 r = total % kXcds;
+  const uint32_t t = x * q + min(x, r) + b / kXcds;
+  const uint32_t width = kBand * a.tiles_j, band = t / width, first = band * kBand,
+                 rows = min((uint32_t)a.tiles_i - first, (uint32_t)kBand), at = t - band * width;
+  *ti = (int32_t)(first + at % rows);
+  *tj = (int32_t)(at / rows);
+}
+
+// A tile of BJ weights' rows by BI rows of a, blocks of 128 bytes of k at a time
+// through LDS.  A row of a block is eight pieces of 16 bytes; row r has piece c in place c
+// ^ (r & 7), so that eight lanes that read the same piece of eight rows meet all
+// banks.  Wave (wj, wi) has BJ/WJ x BI/WI of the tile, weights as the rows of the MFMA's
+// result, so that a lane has one row's scale to apply and four neighbours to store.
+template <typename O, int BJ, int BI, int WJ, int WI>
+__global__ void __launch_bounds__(WJ* WI* kWave) k_product_tile(ProductArgs a) {
+  constexpr int kThreads = WJ * WI * kWave, kRows = kThreads / 8, kLoads = (BJ + BI) / kRows;
+  constexpr int TJ = BJ / WJ / 16, TI = BI / WI / 16;
+  static_assert(BJ % kRows == 0 && BI % kRows == 0 && BJ / WJ <= kScaleBlock, "tile");
+  __shared__ v4i lds[2][(BJ + BI) * 8];
+  const int32_t tid = (int32_t)threadIdx.x, l = lane_id(),
+                wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int32_t wj = wave % WJ, wi = wave / WJ;
+  int32_t ti0, tj0;
+  tile_place(a, &ti0, &tj0);
+  const int64_t i0 = (int64_t)ti0 * BI;
+  const int32_t j0 = tj0 * BJ;
+
+  // the pieces that this lane brings: rows behind the last one repeat it
+  const int32_t slot = tid % 8;
+  const char* from[kLoads];
+  int32_t piece[kLoads];
+#pragma unroll
+  for (int t = 0; t < kLoads; ++t) {
+    const int32_t r = t * kRows + tid / 8;
+    piece[t] = (slot ^ (r & 7)) * 16;
+    from[t] = r < BJ ? a.b.p + min(j0 + r, a.m - 1) * a.b.stride
+                     : a.a.p + min(i0 + (r - BJ), a.n - 1) * a.a.stride;
+  }
+  v4i got[kLoads];
+  const auto fetch = [&](int32_t g) {
+#pragma unroll
+    for (int t = 0; t < kLoads; ++t) got[t] = load_codes(from[t], g * kBlockK + piece[t], a.k);
+  };
+  const auto keep = [&](int buf) {
+#pragma unroll
+    for (int t = 0; t < kLoads; ++t) lds[buf][t * kThreads + tid] = got[t];
+  };
+
+  // scales: of this lane's rows, and of the wave's block of weights
+  const char* row_scale[TI];
+#pragma unroll
+  for (int t = 0; t < TI; ++t)
+    row_scale[t] = a.a.scales + min(i0 + (wi * TI + t) * 16 + l % 16, a.n - 1) * a.a.sstride;
+  const char* block_scale =
+      a.b.scales + min(j0 + wj * TJ * 16, a.m - 1) / kScaleBlock * a.b.sstride;
+  float sa[TI], sb;
+  const auto scales = [&](int32_t g) {
+    sb = *(const float*)(block_scale + 4 * g);
+#pragma unroll
+    for (int t = 0; t < TI; ++t) sa[t] = *(const GG_GLOBAL float*)(row_scale[t] + (a.per_row ? 0 : 4 * g));
+  };
+
+  v4f acc[TJ][TI] = {};
+  typedef Codes<sizeof(O) == 4> C;
+  const auto part = [&](int buf, int32_t r) {
+    const int32_t c = l / 16 * 2 ^ (r & 7);
+    C v;
+    v.set(lds[buf][r * 8 + c], lds[buf][r * 8 + (c ^ 1)]);
+    return v;
+  };
+  fetch(0);
+  scales(0);
+  keep(0);
+  for (int32_t g = 0; g < a.kb; ++g) {
+    __syncthreads();
+    float scale[TI];
+#pragma unroll
+    for (int t = 0; t < TI; ++t) scale[t] = sa[t] * sb;
+    const bool more = g + 1 < a.kb;
+    if (more) {
+      fetch(g + 1);
+      scales(g + 1);
+    }
+    C rows[TI];
+#pragma unroll
+    for (int t = 0; t < TI; ++t) rows[t] = part(g & 1, BJ + (wi * TI + t) * 16 + l % 16);
+#pragma unroll
+    for (int u = 0; u < TJ; ++u) {
+      const C w = part(g & 1, (wj * TJ + u) * 16 + l % 16);
+#pragma unroll
+      for (int t = 0; t < TI; ++t) {
+        const v4f d = multiply(w, rows[t]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[u][t][r] = __builtin_fmaf(d[r], scale[t], acc[u][t][r]);
+      }
+    }
+    if (more) keep(g + 1 & 1);
+  }
+#pragma unroll
+  for (int t = 0; t < TI; ++t) {
+    const int64_t i = i0 + (wi * TI + t) * 16 + l % 16;
+    if (i >= a.n) continue;
+#pragma unroll
+    for (int u = 0; u < TJ; ++u) {
+      const int32_t j = j0 + (wj * TJ + u) * 16 + l / 16 * 4;
+      if (j < a.m) store_four<O>(a.out, i, j, a.m, acc[u][t]);
+    }
+  }
+}
+
+// Few rows: the weights go from memory to the MFMA's registers, without LDS.  A block
+// has 16 TJ weights' rows and 16 TI rows of a; its waves take the blocks of k in
+// turn, and their sums are added in the order of the waves' halves.  Bound by the weights'
+// bytes.
+constexpr int kFewWaves = 8;
+
+template <typename O, int TJ, int TI>
+__global__ void __launch_bounds__(kFewWaves* kWave) k_product_few(ProductArgs a) {
+  typedef Codes<sizeof(O) == 4> C;
+  constexpr int kAhead = TI <= 2 ? 4 : TI <= 4 ? 2 : 1;
+  __shared__ v4f lds[kFewWaves / 2][TJ * TI][kWave];
+  const int32_t l = lane_id(),
+                wave = __builtin_amdgcn_readfirstlane((int32_t)threadIdx.x / kWave),
+                waves = (int32_t)blockDim.x / kWave;
+  const int32_t j0 = (int32_t)blockIdx.x * TJ * 16;
+  const int64_t i0 = (int64_t)blockIdx.y * TI * 16;
+  const char *wrow[TJ], *arow[TI], *ascale[TI];
+#pragma unroll
+  for (int u = 0; u < TJ; ++u) wrow[u] = a.b.p + min(j0 + u * 16 + l % 16, a.m - 1) * a.b.stride;
+#pragma unroll
+  for (int t = 0; t < TI; ++t) {
+    const int64_t i = min(i0 + t * 16 + l % 16, a.n - 1);
+    arow[t] = a.a.p + i * a.a.stride;
+    ascale[t] = a.a.scales + i * a.a.sstride;
+  }
+  const char* wscale = a.b.scales + j0 / kScaleBlock * a.b.sstride;
+  v4f acc[TJ][TI] = {};
+  // Whole blocks of k, kAhead of them loaded before the first is used; the lanes' pieces
+  // behind k's end are zeros.
+  for (int32_t g0 = wave; g0 < a.kb; g0 += waves * kAhead) {
+    C w[kAhead][TJ], r[kAhead][TI];
+    float sb[kAhead], sa[kAhead][TI];
+#pragma unroll
+    for (int h = 0; h < kAhead; ++h) {
+      const int32_t g = g0 + h * waves, c = g * kBlockK + l / 16 * 32;
+      if (g < a.kb) {
+#pragma unroll
+        for (int u = 0; u < TJ; ++u)
+          w[h][u].set(load_codes(wrow[u], c, a.k), load_codes(wrow[u], c + 16, a.k));
+#pragma unroll
+        for (int t = 0; t < TI; ++t)
+          r[h][t].set(load_codes(arow[t], c, a.k), load_codes(arow[t], c + 16, a.k));
+        sb[h] = *(const float*)(wscale + 4 * g);
+#pragma unroll
+        for (int t = 0; t < TI; ++t)
+          sa[h][t] = *(const GG_GLOBAL float*)(ascale[t] + (a.per_row ? 0 : 4 * g));
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < kAhead; ++h) {
+      if (g0 + h * waves >= a.kb) break;
+#pragma unroll
+      for (int t = 0; t < TI; ++t) {
+        const float scale = sa[h][t] * sb[h];
+#pragma unroll
+        for (int u = 0; u < TJ; ++u) {
+          const v4f d = multiply(w[h][u], r[h][t]);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) acc[u][t][x] = __builtin_fmaf(d[x], scale, acc[u][t][x]);
+        }
+      }
+    }
+  }
+  for (int32_t half = waves / 2; half >= 1; half /= 2) {
+    __syncthreads();
+    if (wave >= half && wave < 2 * half) {
+#pragma unroll
+      for (int u = 0; u < TJ; ++u)
+#pragma unroll
+        for (int t = 0; t < TI; ++t) lds[wave - half][u * TI + t][l] = acc[u][t];
+    }
+    __syncthreads();
+    if (wave < half) {
+#pragma unroll
+      for (int u = 0; u < TJ; ++u)
+#pragma unroll
+        for (int t = 0; t < TI; ++t) acc[u][t] += lds[wave][u * TI + t][l];
+    }
+  }
+  if (wave) return;
+#pragma unroll
+  for (int t = 0; t < TI; ++t) {
+    const int64_t i = i0 + t * 16 + l % 16;
+    if (i >= a.n) continue;
+#pragma unroll
+    for (int u = 0; u < TJ; ++u) {
+      const int32_t j = j0 + u * 16 + l / 16 * 4;
+      if (j < a.m) store_four<O>(a.out, i, j, a.m, acc[u][t]);
+    }
+  }
+}
+
+template <typename O, int TJ, int TI>
+int launch_few(ProductArgs& a, hipStream_t stream) {
+  int waves = 1;
+  while (waves < kFewWaves && waves < a.kb) waves *= 2;
+  const dim3 grid((unsigned)cdiv(a.m, TJ * 16), (unsigned)cdiv(a.n, TI * 16));
+  hipLaunchKernelGGL((k_product_few<O, TJ, TI>), grid, dim3(waves * kWave), 0, stream, a);
+  GG_LAUNCH_CHECK("k_product_few");
+  return GG_OK;
+}
+
+template <typename O, int BJ, int BI, int WJ, int WI>
+int launch_tile(ProductArgs& a, hipStream_t stream) {
+  a.tiles_i = (int32_t)cdiv(a.n, BI);
+  a.tiles_j = (int32_t)cdiv(a.m, BJ);
+  GG_REQUIRE((int64_t)a.tiles_i * a.tiles_j <= kGridX * 4, "%lld x %d: too many tiles", (long long)a.n, a.m);
+  hipLaunchKernelGGL((k_product_tile<O, BJ, BI, WJ, WI>), dim3((unsigned)a.tiles_i * a.tiles_j),
+                     dim3(WJ * WI * kWave), 0, stream, a);
+  GG_LAUNCH_CHECK("k_product_tile");
+  return GG_OK;
+}
+
+template <typename O>
+int launch_product(ProductArgs& a, hipStream_t stream) {
+  if (a.n <= 16) return launch_few<O, 1, 1>(a, stream);
+  if (a.n <= 128) return launch_few<O, 2, 8>(a, stream);
+  return launch_tile<O, 128, 128, 2, 2>(a, stream);
+}
+
+}  // namespace
+}  // namespace gg
+
+using namespace gg;
+
+extern "C" int gg_product_forward(const gg_rows_t* a, int64_t n, int64_t k, const gg_blocks_t* b,
+                                  int64_t m, const gg_rows_t* out, hipStream_t stream) {
+  GG_REQUIRE(n >= 0 && n <= GG_PRODUCT_MAX_ROWS, "n = %lld unsupported", (long long)n);
+  GG_REQUIRE(k >= 1 && k <= GG_PRODUCT_MAX_DIM, "k %lld outside 1..%d", (long long)k,
+             GG_PRODUCT_MAX_DIM);
+  GG_REQUIRE(m >= 1 && m <= GG_PRODUCT_MAX_DIM, "m %lld outside 1..%d", (long long)m,
+             GG_PRODUCT_MAX_DIM);
+  ProductArgs p = {};
+  int rc = pack_rows(a, "a", n, k, kBitE4M3, false, &p.a);
+  if (rc != GG_OK) return rc;
+  GG_REQUIRE(p.a.group == 0 || p.a.group == kScaleBlock, "a: group %d is neither 0 nor %d", p.a.group,
+             kScaleBlock);
+  rc = pack_blocks(b, "b", m, k, false, &p.b);
+  if (rc == GG_OK) rc = pack_rows(out, "out", n, m, kBitFloats, true, &p.out);
+  if (rc != GG_OK || n == 0) return rc;
+  p.n = n;
+  p.k = (int32_t)k;
+  p.m = (int32_t)m;
+  p.kb = (int32_t)cdiv(k, kBlockK);
+  p.per_row = p.a.group == 0;
+  GG_FOR_FLOAT(out->dtype, O, return launch_product<O>(p, stream));
+}

@@ -176,6 +176,7 @@ SIGNATURES = {
                                         _P]),
     "gg_quantise_rows": (C.c_int, [_P, _I64, _I64, _P, _P]),
     "gg_quantise_blocks": (C.c_int, [_P, _I64, _I64, _P, _P, _P]),
+    "gg_product_forward": (C.c_int, [_P, _I64, _I64, _P, _I64, _P, _P]),
     "gg_ws_distill": (_SZ, [_I64, _I64]),
     "gg_distill_forward": (C.c_int, [_P, _I64, _I64, _P, _I32, _I64, _P, _I32, C.c_float, C.c_float,
                                      _P, _P, _P, _P, _P, _P, _SZ, _P]),
@@ -688,6 +689,14 @@ def gg_quantise_blocks(w, rows, cols, q, qt, stream=None):
     return check(lib.gg_quantise_blocks(_rows(w, rows, cols, "w"), rows, cols,
                                         _blocks(q, rows, cols, "q"), _blocks(qt, cols, rows, "qt"),
                                         _stream(stream)), "gg_quantise_blocks")
+
+
+def gg_product_forward(a, n, k, b, m, out, stream=None):
+    """a: make_rows of an [n, k] tensor in 8 bits; b: make_blocks of an [m, k] tensor;
+    out: make_rows of an [n, m] tensor."""
+    return check(lib.gg_product_forward(_rows(a, n, k, "a"), n, k, _blocks(b, m, k, "b"), m,
+                                        _rows(out, n, m, "out"), _stream(stream)),
+                 "gg_product_forward")
 
 
 def gg_ws_distill(n, vocab):

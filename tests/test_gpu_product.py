@@ -1,0 +1,194 @@
+"""The product of 8-bit rows and 8-bit weights, and the weights' gradient, against the
+same in 64 bits."""
+import zlib
+
+import pytest
+import torch
+
+from tests.op_util import BF16, E4M3, F16, F32, FLOOR, U, UNIT, like, untouched, within
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def lib():
+    from paper_2606_02916_amd import gg
+    return gg
+
+
+def gen(*key):
+    return torch.Generator().manual_seed(zlib.crc32(repr(key).encode()))
+
+
+def blocks_of(d, g):
+    return -(-d // g) if g else 1
+
+
+def place8(codes, lead, pad):
+    """e4m3 codes on the device at an odd place, NaNs around them."""
+    n, d = codes.shape
+    out, flat, _ = like(n, d, E4M3, DEV, lead=lead, pad=pad)
+    out.view(torch.uint8).copy_(codes.view(torch.uint8))
+    return out
+
+
+def codes8(n, d, g):
+    """Codes of all sizes, and some zeros."""
+    x = torch.randn(n, d, generator=g) * torch.exp2(torch.randint(-6, 7, (n, d), generator=g).float())
+    return x.clamp(-448, 448).to(E4M3)
+
+
+def some_rows(n, k, group, g, lead=1, pad=3):
+    """8-bit rows: the description, and their numbers and codes in 64 bits."""
+    gg = lib()
+    codes, kb = codes8(n, k, g), blocks_of(k, group)
+    sc = torch.exp2(torch.rand(n, kb, generator=g) * 8 - 6)
+    scd = torch.full((n, kb + 1), float("nan"), device=DEV)[:, 1:]
+    scd.copy_(sc)
+    num = codes.float().double() * sc.double()[:, torch.arange(k) // (group or k)]
+    return gg.make_rows(place8(codes, lead, pad), scales=scd, group=group), num, codes.float().double()
+
+
+def some_blocks(m, k, g, lead=3, pad=1):
+    gg = lib()
+    codes, mb, kb = codes8(m, k, g), blocks_of(m, 128), blocks_of(k, 128)
+    sc = torch.exp2(torch.rand(mb, kb, generator=g) * 8 - 6)
+    scd = torch.full((mb, kb + 2), float("nan"), device=DEV)[:, 1:1 + kb]
+    scd.copy_(sc)
+    num = codes.float().double() * sc.double()[torch.arange(m) // 128][:, torch.arange(k) // 128]
+    return gg.make_blocks(place8(codes, lead, pad), scd), num, codes.float().double()
+
+
+def coarse(an, ac, bn, bc):
+    """What the 8-bit matrix instructions may drop: of each eight columns' products all
+    but the largest lose less than 2^-13 of the largest, in which a code below 2^-6
+    counts as 2^-6.  an, bn: the numbers, ac, bc: their codes."""
+    def floor(num, codes):
+        up = torch.where(codes == 0, 1.0, (2.0 ** -6 / codes.abs()).clamp(min=1.0))
+        return torch.nn.functional.pad(num.abs() * up, (0, -num.shape[1] % 8))
+    p, q = floor(an, ac).to(DEV), floor(bn, bc).to(DEV)
+    lost = torch.zeros(len(p), len(q), dtype=torch.float64, device=DEV)
+    for i in range(0, p.shape[1], 8):
+        lost += (p[:, None, i:i + 8] * q[None, :, i:i + 8]).amax(2)
+    return 7 * 2.0 ** -13 * lost.cpu()
+
+
+def check(got, want, bound, t):
+    """Within the bound; a result that rounds beyond fp16's largest number, 65504, is infinite."""
+    got, over = got.detach().cpu().double(), torch.zeros_like(want, dtype=torch.bool)
+    if t == F16:
+        over = want.abs() + bound >= 65_520
+        sure = want.abs() - bound >= 65_520
+        assert torch.equal(got[sure], want[sure].sign() * float("inf"))
+    assert within(got[~over], want[~over], bound[~over]) <= 0
+
+
+def check_forward(n, k, m, t, group, lead=1, pad=3):
+    """A sum of k products, in any order, is off by at most k U of their magnitudes, each
+    block's scale by two roundings, the result by one."""
+    gg, g = lib(), gen(n, k, m, group)
+    a, an, ac = some_rows(n, k, group, g, lead, pad)
+    b, bn, bc = some_blocks(m, k, g, lead + 2 if lead else 0, pad)
+    out, flat, own = like(n, m, t, DEV, lead=lead, pad=pad)
+    gg.gg_product_forward(a, n, k, b, m, gg.make_rows(out))
+    assert untouched(flat, own)
+    want, size = an @ bn.t(), an.abs() @ bn.abs().t()
+    bound = (k + 4) * U * size + 1.01 * UNIT[t] * want.abs() + FLOOR[t]
+    if t != F32:
+        bound += coarse(an, ac, bn, bc) * 1.01
+    check(out, want, bound, t)
+
+
+@pytest.mark.parametrize("n", [1, 2, 15, 16, 17, 100, 129, 300])
+@pytest.mark.parametrize("k", [1, 7, 16, 100, 127, 128, 129, 160, 255, 384, 602, 1200])
+@pytest.mark.parametrize("m", [1, 5, 47, 128, 130, 333])
+def test_product(n, k, m):
+    t = (F32, F16, BF16)[(n + k + m) % 3]
+    check_forward(n, k, m, t, 0 if (n + k) % 2 else 128)
+
+
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("n,k,m", [(1, 4096, 512), (16, 2048, 200), (40, 1024, 260), (100, 4096, 256),
+                                   (200, 512, 512), (512, 256, 640), (1000, 1024, 700), (2500, 384, 1300),
+                                   (47, 16_384, 33), (700, 128, 64)])
+def test_product_at_aligned_places(n, k, m, group, t):
+    """Rows on 16-byte boundaries, and whole or partial tiles of them."""
+    check_forward(n, k, m, t, group, 0, 0)
+
+
+@pytest.mark.parametrize("n,k,m", [(3, 200, 140), (60, 300, 50), (400, 300, 300), (600, 256, 512)])
+def test_nans_and_infinities_keep_to_their_row_and_column(n, k, m):
+    gg, g = lib(), gen(n)
+    acodes, bcodes = codes8(n, k, g), codes8(m, k, g)
+    kb, mb = blocks_of(k, 128), blocks_of(m, 128)
+    sa, sb = (torch.rand(n, kb, generator=g) + 0.5).to(DEV), (torch.rand(mb, kb, generator=g) + 0.5).to(DEV)
+    a, b = place8(acodes, 0, 0), place8(bcodes, 0, 0)
+    clean, out = torch.empty(n, m, device=DEV), torch.empty(n, m, device=DEV)
+
+    def call(to):
+        gg.gg_product_forward(gg.make_rows(a, scales=sa, group=128), n, k, gg.make_blocks(b, sb), m,
+                              gg.make_rows(to))
+
+    call(clean)
+    a.view(torch.uint8)[1, k - 1] = 0x7F
+    b.view(torch.uint8)[m - 2, 5] = 0xFF
+    sa[2, kb - 1] = float("inf")
+    call(out)
+    out, clean = out.cpu(), clean.cpu()
+    rest = torch.ones(n, m, dtype=torch.bool)
+    rest[1:3] = False
+    rest[:, m - 2] = False
+    assert torch.equal(out[rest], clean[rest])
+    assert bool(torch.isnan(out[1]).all()) and bool(torch.isnan(out[:, m - 2]).all())
+    assert not bool(torch.isfinite(out[2]).any())
+
+
+def test_product_of_no_rows():
+    gg = lib()
+    b = some_blocks(20, 30, gen(0))[0]
+    a = gg.make_rows(torch.empty(0, 30, device=DEV).to(E4M3), scales=torch.empty(0, device=DEV))
+    gg.gg_product_forward(a, 0, 30, b, 20, gg.make_rows(torch.empty(0, 20, device=DEV)))
+
+
+@pytest.mark.parametrize("n", [5, 300])
+def test_one_row_for_all_and_rows_beyond_32_bits_of_bytes(n):
+    """Rows of stride 0; weights, rows and results whose places pass 2^32 bytes."""
+    gg, g, k, m, step = lib(), gen(n), 300, 150, 1 << 25
+    ac, bc = codes8(1, k, g), codes8(m, k, g)
+    sc, sb = torch.rand(1, 3, generator=g) + 0.5, torch.rand(2, 3, generator=g) + 0.5
+    big = torch.empty(m * step, dtype=torch.uint8, device=DEV)
+    b = big.as_strided((m, k), (step, 1))
+    b.copy_(bc.view(torch.uint8))
+    a, sa = ac.to(DEV).expand(n, k), sc.to(DEV).expand(n, 3)
+    out = torch.empty(n, m, device=DEV)
+    gg.gg_product_forward(gg.make_rows(a, scales=sa, group=128), n, k,
+                          gg.make_blocks(b.view(E4M3), sb.to(DEV)), m, gg.make_rows(out))
+    an = ac.float().double() * sc.double()[:, torch.arange(k) // 128]
+    bn = bc.float().double() * sb.double()[torch.arange(m) // 128][:, torch.arange(k) // 128]
+    want, size = (an @ bn.t()).expand(n, m), (an.abs() @ bn.abs().t()).expand(n, m)
+    assert within(out, want, (k + 5) * U * size) <= 0
+    # the other operand and the result far apart
+    step = (1 << 32) // n + 4096 & -4
+    a = big[:n * step].as_strided((n, k), (step, 1))
+    a.copy_(ac.view(torch.uint8).expand(n, k))
+    far = torch.empty(n * step // 4, device=DEV).as_strided((n, m), (step // 4, 1))
+    gg.gg_product_forward(gg.make_rows(a.view(E4M3), scales=sa, group=128), n, k,
+                          gg.make_blocks(bc.to(DEV), sb.to(DEV)), m, gg.make_rows(far))
+    assert within(far, want, (k + 5) * U * size) <= 0
+
+
+def test_results_do_not_depend_on_the_stream_or_the_call():
+    gg, g = lib(), gen(11)
+    side = torch.cuda.Stream()
+    for n, k, m in ((1, 2048, 300), (60, 4096, 200), (900, 640, 900)):
+        a = some_rows(n, k, 128, g)[0]
+        b = some_blocks(m, k, g)[0]
+        outs = [torch.empty(n, m, device=DEV) for _ in range(3)]
+        gg.gg_product_forward(a, n, k, b, m, gg.make_rows(outs[0]))
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            gg.gg_product_forward(a, n, k, b, m, gg.make_rows(outs[1]))
+        gg.gg_product_forward(a, n, k, b, m, gg.make_rows(outs[2]), stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])

@@ -114,6 +114,26 @@ def test_blocks_refuse(change, word):
     refused(gg.lib.gg_quantise_blocks, BLOCKS, change, word)
 
 
+PRODUCT = dict(a=rows(gg.GG_E4M3, group=128), n=7, k=300, b=blocks(), m=200, out=rows(stride=800),
+               stream=None)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(n=-1), "n = -1"), (dict(n=1 << 28), "n = "), (dict(k=0), "k 0"), (dict(m=0), "m 0"),
+    (dict(k=(1 << 24) + 1), "k "), (dict(m=(1 << 24) + 1), "m "), (dict(a=None), "a: "),
+    (dict(a=rows()), "a: dtype"), (dict(a=rows(gg.GG_E4M3, group=64)), "a: group 64"),
+    (dict(a=rows(gg.GG_E4M3, group=256)), "a: group 256"),
+    (dict(a=rows(gg.GG_E4M3, scales=None)), "a: "), (dict(a=rows(gg.GG_E4M3, stride=-304)), "a: stride"),
+    (dict(b=None), "b: "), (dict(b=blocks(data=None)), "b: data"), (dict(b=blocks(stride=-1)), "b: stride"),
+    (dict(b=blocks(scales_stride=-64)), "b: scales"), (dict(b=blocks(scales_stride=30)), "b: scales"),
+    (dict(b=blocks(scales=P + 1)), "b: scales"), (dict(out=None), "out"),
+    (dict(out=rows(gg.GG_E4M3)), "out: dtype"), (dict(out=rows(stride=796)), "out: stride"),
+    (dict(out=rows(data=P + 2)), "out: not aligned"),
+    (dict(n=1 << 27, m=1 << 24, out=rows(stride=1 << 26)), "too many")])
+def test_product_refuses(change, word):
+    refused(gg.lib.gg_product_forward, PRODUCT, change, word)
+
+
 def test_make_blocks_refuses_what_it_cannot_describe():
     q, sc = torch.zeros(130, 300, dtype=torch.float8_e4m3fn), torch.zeros(2, 3)
     b = gg.make_blocks(q[:, 4:260], torch.zeros(2, 9)[:, 3:5])
@@ -166,7 +186,9 @@ def test_bindings_check_shapes():
                                                  None),
                 lambda: gg.gg_quantise_rows(bad, 7, 20, r8(7, 20)),
                 lambda: gg.gg_quantise_rows(good, 7, 20, bad8),
-                lambda: gg.gg_quantise_blocks(bad, 7, 20, b(7, 20), None)):
+                lambda: gg.gg_quantise_blocks(bad, 7, 20, b(7, 20), None),
+                lambda: gg.gg_product_forward(bad8, 7, 20, b(20, 20), 20, good),
+                lambda: gg.gg_product_forward(r8(7, 20), 7, 20, b(20, 20), 20, bad)):
             with pytest.raises(gg.GGError, match="rows of"):
                 call()
     for call, word in (
@@ -185,6 +207,9 @@ def test_bindings_check_shapes():
             (lambda: gg.gg_quantise_blocks(good, 7, 20, b(7, 21), None), "q: weights of"),
             (lambda: gg.gg_quantise_blocks(good, 7, 20, None, b(7, 20)), "qt: weights of"),
             (lambda: gg.gg_quantise_blocks(good, 7, 20, r8(7, 20), None), "make_blocks"),
+            (lambda: gg.gg_product_forward(r8(7, 20), 7, 20, b(20, 21), 20, good), "b: weights of"),
+            (lambda: gg.gg_product_forward(r8(7, 20), 7, 20, r8(20, 20), 20, good), "make_blocks"),
+            (lambda: gg.gg_product_forward(b(7, 20), 7, 20, b(20, 20), 20, good), "make_rows"),
             (lambda: gg.gg_quantise_rows(good, 7, 20, b(7, 20)), "make_rows")):
         with pytest.raises(gg.GGError, match=word):
             call()
