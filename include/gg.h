@@ -711,6 +711,22 @@ int gg_quantise_blocks(const gg_rows_t* w, int64_t rows, int64_t cols, const gg_
 int gg_product_forward(const gg_rows_t* a, int64_t n, int64_t k, const gg_blocks_t* b, int64_t m,
                        const gg_rows_t* out, hipStream_t stream);
 
+#define GG_PRODUCT_ADD 1      /* gg_product_backward adds to dw instead of writing it */
+
+/* Workspace bytes; a workspace for n rows serves calls of fewer of the same k and m. */
+size_t gg_ws_product(int64_t n, int64_t k, int64_t m);
+
+/* The gradient of the weights, from the 8-bit rows a that gg_product_forward took and
+ * the gradient dz [n][m] of its output (GG_F32, GG_F16 or GG_BF16): dw[j][c] = sum over i of
+ * dz[i][j] a[i][c], [m][k], of dz's type or GG_F32; with GG_PRODUCT_ADD added to what dw
+ * holds.  Sums are fp32, in an order that depends on the sizes alone, rounded once
+ * with what is added.  The terms' dz times scale enter as fp32 numbers for a dw of
+ * GG_F32, to 2^-15 for GG_F16 and rounded to bf16 for GG_BF16.  No row (n 0): zeros.  dw
+ * is no memory of a or dz.  ws: 16-byte aligned, NULL where gg_ws_product is 0. */
+int gg_product_backward(const gg_rows_t* a, int64_t n, int64_t k, const gg_rows_t* dz, int64_t m,
+                        const gg_rows_t* dw, int32_t flags, void* ws, size_t ws_bytes,
+                        hipStream_t stream);
+
 #define GG_DISTILL_MAX_ROWS (1LL << 27)
 #define GG_DISTILL_MAX_VOCAB (1 << 24)
 #define GG_DISTILL_MAX_K 256

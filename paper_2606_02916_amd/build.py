@@ -13,7 +13,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libgg.so")
 SOURCES = ["common.hip", "sample.hip", "hotset.hip", "bucket.hip", "stage.hip", "gather.hip",
            "sim.hip", "sage.hip", "embed.hip", "norm.hip", "layernorm.hip",
-           "quantise.hip", "product.hip", "distill.hip"]
+           "quantise.hip", "product.hip", "product_grad.hip", "distill.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

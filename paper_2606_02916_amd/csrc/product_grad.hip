@@ -1,0 +1,344 @@
+// The gradient of 8-bit weights from the 8-bit rows that the forward product took:
+//   dw[j][c] = sum_i dz[i][j] a[i][c],   a[i][c] = code[i][c] * scale[i][c / 128].
+#include <type_traits>
+
+#include "codes.hpp"
+
+namespace gg {
+namespace {
+
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef bf16 v8bf __attribute__((ext_vector_type(8)));
+
+struct GradArgs {
+  KRows a, dz, dw;
+  int64_t n, chunk;            // rows, and those of a split
+  int32_t k, m;
+  int32_t per_row;             // a has one scale a row
+  int32_t add;
+  int32_t tiles_k, tiles_j, splits;
+  float* part;                 // [splits][m][k] where there are several
+};
+
+constexpr int32_t kTileK = kScaleBlock;    // columns of a tile: one scale of each row
+constexpr int32_t kTileI = 32;             // rows of a step
+
+// Scaled gradients as bf16 numbers that add up to them.  The codes are bf16 numbers
+// themselves, so products are exact and sums fp32.  One part for bf16 results (2^-8 of a
+// term at most, the rounding that the result itself gets, and less of a sum of many), two for
+// fp16 (2^-15), three for fp32, which are the fp32 number.
+// Infinities and NaNs are whole in the first part.
+template <int PARTS>
+__device__ __forceinline__ void split(float x, float y, uint32_t (&p)[PARTS]) {
+  if constexpr (PARTS == 1) {
+    const v2bf v = {(bf16)x, (bf16)y};
+    p[0] = __builtin_bit_cast(uint32_t, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+      const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
+      if (i + 1 == PARTS && PARTS == 2) {
+        const v2bf v = {(bf16)x, (bf16)y};
+        p[i] = __builtin_bit_cast(uint32_t, v);
+      } else {
+        p[i] = __builtin_amdgcn_perm(b, a, 0x07060302);   // the upper halves
+      }
+      if (i + 1 < PARTS) {
+        x = __builtin_isfinite(x) ? x - __uint_as_float(a & 0xffff0000u) : 0.0f;
+        y = __builtin_isfinite(y) ? y - __uint_as_float(b & 0xffff0000u) : 0.0f;
+      }
+    }
+  }
+}
+
+// Four columns of a row of fp32 sums into dw, added to it with `add`.
+template <typename O>
+__device__ __forceinline__ void store_sums(const GradArgs& a, int32_t j, int32_t c, const float (&f)[4]) {
+  char* to = a.dw.p + j * a.dw.stride + c * (int64_t)sizeof(O);
+  if (c + 4 <= a.k) {
+    float v[4] = {};
+    if (a.add) row_load<O, 4>(to, v);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] += f[r];
+    row_store<O, 4>(to, v);
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      if (c + r >= a.k) break;
+      float one[1] = {};
+      if (a.add) row_load<O, 1>(to + r * sizeof(O), one);
+      one[0] += f[r];
+      row_store<O, 1>(to + r * sizeof(O), one);
+    }
+  }
+}
+
+// A tile of 128 columns of a by BJ of dz, 32 rows at a time through LDS.  Both
+// operands of the MFMA run along the rows, which lie across both matrices: LDS keeps
+// them as they come, and the transposing reads hand a lane four rows' elements of its
+// column.  A row of the tile is 32 bytes longer than its elements, so that the 4 x 32
+// bytes of such a read meet different banks.  Codes are turned into bf16 and gradients
+// scaled and split once, on the way into LDS.  Wave (wk, wj) has 64 x BJ/2 of the tile.
+template <typename Z, typename O, int PARTS, int BJ>
+__global__ void __launch_bounds__(kBlock) k_product_grad(GradArgs a) {
+  constexpr int TK = 4, TJ = BJ / 32, V = kVec<Z>;
+  constexpr int kPitchA = kTileK + 16, kPitchZ = BJ + 16;
+  constexpr int kLanesZ = BJ / V, kStepZ = kBlock / kLanesZ, kLoadsZ = kTileI / kStepZ;
+  static_assert(kTileI * kTileK == kBlock * 16 && kTileI % kStepZ == 0, "a step's loads");
+  __shared__ __attribute__((aligned(16))) short la[2][kTileI * kPitchA];
+  __shared__ __attribute__((aligned(16))) short lz[2][PARTS][kTileI * kPitchZ];
+  const int32_t tid = (int32_t)threadIdx.x, l = lane_id(),
+                wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int32_t wk = wave % 2, wj = wave / 2;
+  const int32_t c0 = (int32_t)(blockIdx.x % a.tiles_k) * kTileK,
+                j0 = (int32_t)(blockIdx.x / a.tiles_k) * BJ;
+  const int64_t first = blockIdx.y * a.chunk, end = min(a.n, first + a.chunk);
+
+  // a step's loads: 16 codes a lane, and kLoadsZ pieces of gradients with their rows' scales
+  const int32_t ra = tid / 8, ca = tid % 8 * 16, rz = tid / kLanesZ, cz = tid % kLanesZ * V;
+  const int64_t scale_at = a.per_row ? 0 : c0 / kScaleBlock * 4LL;
+  v4i codes;
+  typename Raw<Z, V>::vec raw[kLoadsZ];
+  float scale[kLoadsZ];
+  const auto fetch = [&](int64_t i0) {
+    codes = {};
+    if (i0 + ra < end) {
+      const char* row = a.a.p + (i0 + ra) * a.a.stride;
+      const int32_t c = c0 + ca;
+      if (c + 16 <= a.k) {
+        typedef v4i mem __attribute__((aligned(1)));
+        codes = *(const GG_GLOBAL mem*)(row + c);
+      } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (c + 4 * w + i < a.k)
+              codes[w] |= (int)((uint32_t) * (const GG_GLOBAL uint8_t*)(row + c + 4 * w + i) << 8 * i);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < kLoadsZ; ++t) {
+      const int64_t i = i0 + t * kStepZ + rz;
+      raw[t] = {};
+      scale[t] = 0.0f;
+      if (i < end) {
+        const char* row = a.dz.p + i * a.dz.stride;
+        const int32_t j = j0 + cz;
+        scale[t] = *(const GG_GLOBAL float*)(a.a.scales + i * a.a.sstride + scale_at);
+        if (j + V <= a.m) {
+          raw[t] = raw_load<Z, V>(row + j * (int64_t)sizeof(Z));
+        } else {
+#pragma unroll
+          for (int x = 0; x < V; ++x)
+            if (j + x < a.m) raw[t][x] = raw_load<Z, 1>(row + (j + x) * (int64_t)sizeof(Z));
+        }
+      }
+    }
+  };
+  const auto keep = [&](int buf) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[2 * i] = __builtin_bit_cast(
+          uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)codes[i], 1.0f, false));
+      w[2 * i + 1] = __builtin_bit_cast(
+          uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)codes[i], 1.0f, true));
+    }
+    v4i* to = (v4i*)&la[buf][ra * kPitchA + ca];
+    to[0] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+    to[1] = v4i{(int)w[4], (int)w[5], (int)w[6], (int)w[7]};
+#pragma unroll
+    for (int t = 0; t < kLoadsZ; ++t) {
+      float v[V];
+      to_f32<Z, V>(raw[t], v);
+      uint32_t p[V / 2][PARTS];
+#pragma unroll
+      for (int x = 0; x < V / 2; ++x) split<PARTS>(v[2 * x] * scale[t], v[2 * x + 1] * scale[t], p[x]);
+#pragma unroll
+      for (int q = 0; q < PARTS; ++q) {
+        uint32_t* at = (uint32_t*)&lz[buf][q][(t * kStepZ + rz) * kPitchZ + cz];
+#pragma unroll
+        for (int x = 0; x < V / 2; ++x) at[x] = p[x][q];
+      }
+    }
+  };
+  // rows 4 q .. 4 q + 3 and 16 + them for lanes 16 q .. 16 q + 15, a column each
+  const int32_t tr = l % 16 / 4 + l / 16 * 4, tc = l % 4 * 4;
+  const auto operand = [&](const short* tile, int pitch, int32_t col) {
+    typedef __attribute__((address_space(3))) v4s* at;
+    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(tile + tr * pitch + col + tc));
+    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(tile + (16 + tr) * pitch + col + tc));
+    return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+
+  v4f acc[TK][TJ] = {};
+  if (first < end) {
+    fetch(first);
+    keep(0);
+  }
+  int buf = 0;
+  for (int64_t i0 = first; i0 < end; i0 += kTileI, buf ^= 1) {
+    __syncthreads();
+    const bool more = i0 + kTileI < end;
+    if (more) fetch(i0 + kTileI);
+    v8bf x[TK];
+#pragma unroll
+    for (int u = 0; u < TK; ++u) x[u] = operand(la[buf], kPitchA, (wk * TK + u) * 16);
+#pragma unroll
+    for (int t = 0; t < TJ; ++t)
+#pragma unroll
+      for (int q = PARTS - 1; q >= 0; --q) {
+        const v8bf z = operand(lz[buf][q], kPitchZ, (wj * TJ + t) * 16);
+#pragma unroll
+        for (int u = 0; u < TK; ++u)
+          acc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[u], z, acc[u][t], 0, 0, 0);
+      }
+    if (more) keep(buf ^ 1);
+  }
+#pragma unroll
+  for (int t = 0; t < TJ; ++t) {
+    const int32_t j = j0 + (wj * TJ + t) * 16 + l % 16;
+    if (j >= a.m) continue;
+#pragma unroll
+    for (int u = 0; u < TK; ++u) {
+      const int32_t c = c0 + (wk * TK + u) * 16 + l / 16 * 4;
+      if (c >= a.k) continue;
+      const float f[4] = {acc[u][t][0], acc[u][t][1], acc[u][t][2], acc[u][t][3]};
+      if (a.part) {
+        float* to = a.part + ((int64_t)blockIdx.y * a.m + j) * a.k + c;
+        if (c + 4 <= a.k) {
+          row_store<float, 4>((char*)to, f);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (c + r < a.k) to[r] = f[r];
+        }
+      } else {
+        store_sums<O>(a, j, c, f);
+      }
+    }
+  }
+}
+
+// The splits' sums, in their order.
+template <typename O>
+__global__ void __launch_bounds__(kBlock) k_product_join(GradArgs a) {
+  const int32_t across = (a.k + 3) / 4;
+  const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+  if (i >= (int64_t)a.m * across) return;
+  const int32_t j = (int32_t)(i / across), c = (int32_t)(i - (int64_t)j * across) * 4;
+  const float* p = a.part + (int64_t)j * a.k + c;
+  const int64_t step = (int64_t)a.m * a.k;
+  float f[4] = {};
+  if (c + 4 <= a.k) {
+#pragma unroll 8
+    for (int32_t s = 0; s < a.splits; ++s) {
+      float v[4];
+      row_load<float, 4>((const char*)(p + s * step), v);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) f[r] += v[r];
+    }
+  } else {
+    for (int32_t s = 0; s < a.splits; ++s)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (c + r < a.k) f[r] += p[s * step + r];
+  }
+  store_sums<O>(a, j, c, f);
+}
+
+// How many splits of the rows: enough that blocks fill the chip's 256 CUs twice, of 256
+// rows at least.
+constexpr int64_t kGradBlocks = 512, kGradRows = 256;
+
+template <typename F>
+void grad_shape(int64_t n, int64_t k, int64_t m, F f) {
+  const int bj = m <= 64 ? 64 : 128;
+  const int64_t tiles = cdiv(k, kTileK) * cdiv(m, bj);
+  const int64_t splits = std::max<int64_t>(1, std::min(cdiv(kGradBlocks, tiles), cdiv(n, kGradRows)));
+  f(bj, tiles, splits);
+}
+
+template <typename Z, typename O, int PARTS>
+int launch_grad(GradArgs& a, hipStream_t stream) {
+  int rc = GG_OK;
+  grad_shape(a.n, a.k, a.m, [&](int bj, int64_t tiles, int64_t splits) {
+    a.tiles_k = (int32_t)cdiv(a.k, kTileK);
+    a.tiles_j = (int32_t)cdiv(a.m, bj);
+    a.splits = (int32_t)splits;
+    a.chunk = align_up(cdiv(a.n, splits), kTileI);
+    if (splits == 1) a.part = nullptr;
+    const dim3 grid((unsigned)tiles, (unsigned)splits);
+    if (bj == 64)
+      hipLaunchKernelGGL((k_product_grad<Z, O, PARTS, 64>), grid, dim3(kBlock), 0, stream, a);
+    else
+      hipLaunchKernelGGL((k_product_grad<Z, O, PARTS, 128>), grid, dim3(kBlock), 0, stream, a);
+  });
+  GG_LAUNCH_CHECK("k_product_grad");
+  if (a.part) {
+    const int64_t lanes = a.m * cdiv(a.k, 4);
+    hipLaunchKernelGGL((k_product_join<O>), dim3((unsigned)cdiv(lanes, kBlock)), dim3(kBlock), 0,
+                       stream, a);
+    GG_LAUNCH_CHECK("k_product_join");
+  }
+  return rc;
+}
+
+}  // namespace
+}  // namespace gg
+
+using namespace gg;
+
+static bool grad_sizes(int64_t n, int64_t k, int64_t m) {
+  return n >= 0 && n <= GG_PRODUCT_MAX_ROWS && k >= 1 && k <= GG_PRODUCT_MAX_DIM && m >= 1 &&
+         m <= GG_PRODUCT_MAX_DIM;
+}
+
+extern "C" size_t gg_ws_product(int64_t n, int64_t k, int64_t m) {
+  if (!grad_sizes(n, k, m)) return 0;
+  size_t bytes = 0;
+  grad_shape(n, k, m, [&](int, int64_t, int64_t splits) {
+    if (splits > 1) bytes = align_up((size_t)splits * m * k * sizeof(float), 256);
+  });
+  return bytes;
+}
+
+extern "C" int gg_product_backward(const gg_rows_t* a, int64_t n, int64_t k, const gg_rows_t* dz,
+                                   int64_t m, const gg_rows_t* dw, int32_t flags, void* ws,
+                                   size_t ws_bytes, hipStream_t stream) {
+  GG_REQUIRE(n >= 0 && n <= GG_PRODUCT_MAX_ROWS, "n = %lld unsupported", (long long)n);
+  GG_REQUIRE(k >= 1 && k <= GG_PRODUCT_MAX_DIM, "k %lld outside 1..%d", (long long)k,
+             GG_PRODUCT_MAX_DIM);
+  GG_REQUIRE(m >= 1 && m <= GG_PRODUCT_MAX_DIM, "m %lld outside 1..%d", (long long)m,
+             GG_PRODUCT_MAX_DIM);
+  GG_REQUIRE((flags & ~GG_PRODUCT_ADD) == 0, "unknown flags %d", flags);
+  GradArgs p = {};
+  int rc = pack_rows(a, "a", n, k, kBitE4M3, false, &p.a);
+  if (rc != GG_OK) return rc;
+  GG_REQUIRE(p.a.group == 0 || p.a.group == kScaleBlock, "a: group %d is neither 0 nor %d", p.a.group,
+             kScaleBlock);
+  rc = pack_rows(dz, "dz", n, m, kBitFloats, false, &p.dz);
+  if (rc == GG_OK) rc = pack_rows(dw, "dw", m, k, (1u << dz->dtype) | kBitF32, true, &p.dw);
+  if (rc != GG_OK) return rc;
+  const size_t need = gg_ws_product(n, k, m);
+  GG_REQUIRE(need == 0 || (ws && (uintptr_t)ws % 16 == 0 && ws_bytes >= need),
+             "workspace of %zu bytes < %zu, or not aligned", ws_bytes, need);
+  GG_REQUIRE(cdiv(k, kTileK) * cdiv(m, 64) <= kGridX * 4, "%lld x %lld: too many tiles", (long long)m,
+             (long long)k);
+  p.n = n;
+  p.k = (int32_t)k;
+  p.m = (int32_t)m;
+  p.per_row = p.a.group == 0;
+  p.add = flags & GG_PRODUCT_ADD;
+  p.part = (float*)ws;
+  if (n == 0 && p.add) return GG_OK;
+  GG_FOR_FLOAT(dz->dtype, Z, {
+    if (dw->dtype == GG_F32) return launch_grad<Z, float, 3>(p, stream);
+    if constexpr (sizeof(Z) == 2) return launch_grad<Z, Z, std::is_same<Z, f16>::value ? 2 : 1>(p, stream);
+    return GG_ERR_UNSUPPORTED;
+  });
+}

@@ -177,6 +177,8 @@ SIGNATURES = {
     "gg_quantise_rows": (C.c_int, [_P, _I64, _I64, _P, _P]),
     "gg_quantise_blocks": (C.c_int, [_P, _I64, _I64, _P, _P, _P]),
     "gg_product_forward": (C.c_int, [_P, _I64, _I64, _P, _I64, _P, _P]),
+    "gg_ws_product": (_SZ, [_I64, _I64, _I64]),
+    "gg_product_backward": (C.c_int, [_P, _I64, _I64, _P, _I64, _P, _I32, _P, _SZ, _P]),
     "gg_ws_distill": (_SZ, [_I64, _I64]),
     "gg_distill_forward": (C.c_int, [_P, _I64, _I64, _P, _I32, _I64, _P, _I32, C.c_float, C.c_float,
                                      _P, _P, _P, _P, _P, _P, _SZ, _P]),
@@ -697,6 +699,19 @@ def gg_product_forward(a, n, k, b, m, out, stream=None):
     return check(lib.gg_product_forward(_rows(a, n, k, "a"), n, k, _blocks(b, m, k, "b"), m,
                                         _rows(out, n, m, "out"), _stream(stream)),
                  "gg_product_forward")
+
+
+def gg_ws_product(n, k, m):
+    return int(lib.gg_ws_product(n, k, m))
+
+
+def gg_product_backward(a, n, k, dz, m, dw, flags, ws, stream=None):
+    """a: make_rows of an [n, k] tensor in 8 bits; dz and dw: make_rows of an [n, m] and
+    an [m, k] tensor; ws may be None where gg_ws_product(n, k, m) is 0."""
+    return check(lib.gg_product_backward(_rows(a, n, k, "a"), n, k, _rows(dz, n, m, "dz"), m,
+                                         _rows(dw, m, k, "dw"), flags, _ptr(ws),
+                                         0 if ws is None else ws.numel(), _stream(stream)),
+                 "gg_product_backward")
 
 
 def gg_ws_distill(n, vocab):

@@ -192,3 +192,163 @@ def test_results_do_not_depend_on_the_stream_or_the_call():
         gg.gg_product_forward(a, n, k, b, m, gg.make_rows(outs[2]), stream=side)
         torch.cuda.current_stream().wait_stream(side)
         assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+# ---------------------------------------------------------------------------
+# The weights' gradient.
+# ---------------------------------------------------------------------------
+PARTS = {F32: 0.0, F16: 2.0 ** -15, BF16: 2.0 ** -8}    # what is left off dz * scale
+
+
+def grad_case(n, k, m, tz, t, group, add=False, lead=1, pad=3, dz=None):
+    gg, g = lib(), gen(n, k, m, str(tz), group)
+    a, an, _ = some_rows(n, k, group, g, lead, pad)
+    z = (torch.randn(n, m, generator=g) * torch.exp2(torch.randint(-8, 3, (n, 1), generator=g).float())).to(tz)
+    zd, _, _ = like(n, m, tz, DEV, lead=lead, pad=pad)
+    zd.copy_(z)
+    dw, flat, own = like(m, k, t, DEV, lead=lead, pad=pad)
+    old = torch.randn(m, k, generator=g).to(t) * 8
+    if add:
+        dw.copy_(old)
+    size = gg.gg_ws_product(n, k, m)
+    ws = torch.full((size,), 0xFF, dtype=torch.uint8, device=DEV) if size else None
+    gg.gg_product_backward(a, n, k, gg.make_rows(zd), m, gg.make_rows(dw),
+                           gg.GG_PRODUCT_ADD if add else 0, ws)
+    assert untouched(flat, own)
+    z = z.double()
+    want, size = z.t() @ an, z.abs().t() @ an.abs()
+    if add:
+        want = want + old.double()
+        size = size + old.double().abs()
+    # (splits add one rounding each, and their join)
+    bound = (n + n / 256 + 4) * U * size + 1.01 * PARTS[t] * size + 1.01 * UNIT[t] * want.abs() + FLOOR[t]
+    return dw, want, bound
+
+
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 100, 257, 1000])
+@pytest.mark.parametrize("k", [1, 7, 100, 128, 129, 200, 602])
+@pytest.mark.parametrize("m", [1, 5, 47, 64, 65, 130, 333])
+def test_weight_gradient(n, k, m):
+    tz, t = ((F32, F32), (F16, F16), (BF16, BF16), (F16, F32), (BF16, F32))[(n + k + m) % 5]
+    check(*grad_case(n, k, m, tz, t, 0 if (n + k) % 2 else 128, add=(n + m) % 3 == 0), t)
+
+
+@pytest.mark.parametrize("tz,t", [(F32, F32), (F16, F16), (BF16, BF16), (F16, F32), (BF16, F32)])
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("n,k,m", [(64, 128, 64), (128, 256, 512), (3000, 128, 40), (5000, 512, 256),
+                                   (1024, 1024, 1024), (520, 640, 2048), (40_001, 100, 47)])
+@pytest.mark.parametrize("add", [False, True])
+def test_weight_gradient_at_aligned_places(n, k, m, group, tz, t, add):
+    check(*grad_case(n, k, m, tz, t, group, add, 0, 0), t)
+
+
+def test_weight_gradient_of_no_rows():
+    gg = lib()
+    a = gg.make_rows(torch.empty(0, 30, device=DEV).to(E4M3), scales=torch.empty(0, device=DEV))
+    dz = gg.make_rows(torch.empty(0, 20, device=DEV))
+    dw = torch.full((20, 30), 3.0, device=DEV)
+    gg.gg_product_backward(a, 0, 30, dz, 20, gg.make_rows(dw), gg.GG_PRODUCT_ADD, None)
+    assert bool((dw == 3).all())
+    gg.gg_product_backward(a, 0, 30, dz, 20, gg.make_rows(dw), 0, None)
+    assert not dw.any()
+
+
+@pytest.mark.parametrize("tz,t", [(F32, F32), (F16, F16), (BF16, BF16), (BF16, F32)])
+def test_infinities_of_a_gradient(tz, t):
+    """An infinite gradient makes its weights' row infinite (NaN where the code is zero),
+    a NaN makes it NaN, a NaN code its column, and nothing else changes."""
+    gg, g, n, k, m = lib(), gen(1), 300, 140, 70
+    codes = codes8(n, k, g)
+    codes.view(torch.uint8)[7] = torch.where(torch.arange(k) % 2 == 0, 0x38, 0xB8)   # 1, -1
+    codes.view(torch.uint8)[9, 3] = 0
+    z = torch.randn(n, m, generator=g).to(tz)
+    a, zd, sc = place8(codes, 0, 0), z.to(DEV), torch.ones(n, device=DEV)
+    size = gg.gg_ws_product(n, k, m)
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+
+    def call():
+        dw = torch.empty(m, k, dtype=t, device=DEV)
+        gg.gg_product_backward(gg.make_rows(a, scales=sc), n, k, gg.make_rows(zd), m, gg.make_rows(dw), 0,
+                               ws)
+        return dw.cpu().float()
+
+    clean = call()
+    zd[7, 5] = float("inf")
+    zd[8, 6] = float("nan")
+    zd[9, 7] = -float("inf")
+    a.view(torch.uint8)[20, 100] = 0x7F
+    dw, rest = call(), torch.ones(m, k, dtype=torch.bool)
+    rest[5:8] = False
+    rest[:, 100] = False
+    assert torch.equal(dw[rest], clean[rest])
+    sign = torch.where(torch.arange(k) % 2 == 0, 1.0, -1.0) * float("inf")
+    here = torch.arange(k) != 100
+    assert torch.equal(dw[5][here], sign[here])
+    assert bool(torch.isnan(dw[6]).all()) and bool(torch.isnan(dw[:, 100]).all())
+    assert bool(torch.isnan(dw[7, 3]))
+    nonzero = (codes[9].float() != 0) & here
+    assert torch.equal(dw[7][nonzero], -codes[9].float()[nonzero].sign() * float("inf"))
+
+
+def test_weight_gradient_of_rows_beyond_32_bits_of_bytes():
+    gg, g, n, k, m, step = lib(), gen(4), 300, 200, 70, 1 << 24
+    codes, z = codes8(n, k, g), torch.randn(n, m, generator=g)
+    sc = torch.rand(n, generator=g) + 0.5
+    big = torch.empty(n * step, dtype=torch.uint8, device=DEV)
+    a = big.as_strided((n, k), (step, 1))
+    a.copy_(codes.view(torch.uint8))
+    far = big[1024:].view(F32).as_strided((n, m), (step // 4, 1))
+    far.copy_(z)
+    out = big[4096:].view(F32).as_strided((m, k), (1 << 24, 1))
+    ws = torch.empty(gg.gg_ws_product(n, k, m), dtype=torch.uint8, device=DEV)
+    gg.gg_product_backward(gg.make_rows(a.view(E4M3), scales=sc.to(DEV)), n, k, gg.make_rows(far), m,
+                           gg.make_rows(out), 0, ws)
+    an = codes.float().double() * sc.double()[:, None]
+    want, size = z.double().t() @ an, z.double().abs().t() @ an.abs()
+    assert within(out, want, (n + 6) * U * size) <= 0
+
+
+def test_gradients_against_differences():
+    """The loss sum(c * (a b^T)) along directions of a and b, numbers in 8 bits: central
+    differences of a bilinear form are exact but for their own roundings in 64 bits.  The
+    way to a is the forward call on c in 8 bits and the transposed weights, whose own
+    rounding to 8 bits the difference takes along."""
+    gg, g, n, k, m = lib(), gen(21), 150, 200, 140
+    w = torch.randn(m, k, generator=g).to(DEV)
+    b, bt = (torch.empty(s, dtype=E4M3, device=DEV) for s in ((m, k), (k, m)))
+    sb, sbt = (torch.empty(2, 2, device=DEV) for _ in range(2))
+    blocks, back = gg.make_blocks(b, sb), gg.make_blocks(bt, sbt)
+    gg.gg_quantise_blocks(gg.make_rows(w), m, k, blocks, back)
+    x, c = torch.randn(n, k, generator=g).to(DEV), torch.randn(n, m, generator=g).to(DEV)
+    a, c8 = (torch.empty(s, dtype=E4M3, device=DEV) for s in ((n, k), (n, m)))
+    sa, sc = (torch.empty(n, 2, device=DEV) for _ in range(2))
+    ar, cr = (gg.make_rows(t, scales=s, group=128) for t, s in ((a, sa), (c8, sc)))
+    gg.gg_quantise_rows(gg.make_rows(x), n, k, ar)
+    gg.gg_quantise_rows(gg.make_rows(c), n, m, cr)
+    da, db = torch.empty(n, k, device=DEV), torch.empty(m, k, device=DEV)
+    gg.gg_product_forward(cr, n, m, back, k, gg.make_rows(da))
+    ws = torch.empty(gg.gg_ws_product(n, k, m), dtype=torch.uint8, device=DEV)
+    gg.gg_product_backward(ar, n, k, gg.make_rows(c), m, gg.make_rows(db), 0, ws)
+    num = lambda q, s: q.float().cpu().double() * s.cpu().double()[:, torch.arange(q.shape[1]) // 128]  # noqa: E731
+    an, cn = num(a, sa), num(c8, sc)
+    bn = num(b, sb[(torch.arange(m) // 128).to(DEV)])
+    way_a, way_b = (torch.randn(s, generator=g).double() for s in ((n, k), (m, k)))
+    for got, way, f in ((da, way_a, lambda h: (cn * ((an + h * way_a) @ bn.t())).sum()),
+                        (db, way_b, lambda h: (c.cpu().double() * (an @ (bn + h * way_b).t())).sum())):
+        slope = float(f(0.5) - f(-0.5))
+        part = got.cpu().double() * way
+        size = float((cn.abs() @ bn.abs() * way.abs()).sum() if got is da else
+                     (c.cpu().double().abs().t() @ an.abs() * way.abs()).sum())
+        assert abs(float(part.sum()) - slope) <= size * (max(n, m) + 8) * U
+
+
+def test_gradients_are_the_same_each_time_and_on_another_stream():
+    side = torch.cuda.Stream()
+    for n, k, m in ((20_000, 200, 47), (700, 900, 1300)):
+        first = grad_case(n, k, m, F32, F32, 128)[0]
+        for _ in range(2):
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                again = grad_case(n, k, m, F32, F32, 128)[0]
+            torch.cuda.current_stream().wait_stream(side)
+            assert torch.equal(first, again)

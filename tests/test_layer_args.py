@@ -134,6 +134,26 @@ def test_product_refuses(change, word):
     refused(gg.lib.gg_product_forward, PRODUCT, change, word)
 
 
+PRODUCT_BACK = dict(a=rows(gg.GG_E4M3, group=128), n=700, k=300, dz=rows(stride=800), m=200,
+                    dw=rows(stride=1200), flags=0, ws=P, ws_bytes=1 << 30, stream=None)
+
+
+@pytest.mark.parametrize("change,word", [
+    (dict(n=-1), "n = -1"), (dict(n=1 << 28), "n = "), (dict(k=0), "k 0"), (dict(m=0), "m 0"),
+    (dict(k=(1 << 24) + 1), "k "), (dict(m=(1 << 24) + 1), "m "), (dict(a=None), "a: "),
+    (dict(a=rows()), "a: dtype"), (dict(a=rows(gg.GG_E4M3, group=64)), "a: group 64"),
+    (dict(a=rows(gg.GG_E4M3, scales=None)), "a: "), (dict(dz=None), "dz: "),
+    (dict(dz=rows(gg.GG_E4M3)), "dz: dtype"), (dict(dz=rows(data=P + 2)), "dz: not aligned"),
+    (dict(dw=None), "dw: "), (dict(dw=rows(gg.GG_BF16, stride=600)), "dw: dtype"),
+    (dict(dw=rows(stride=1196)), "dw: stride"),
+    (dict(dz=rows(gg.GG_F16), dw=rows(gg.GG_BF16, stride=600)), "dw: dtype"), (dict(flags=2), "flags"),
+    (dict(flags=-1), "flags"), (dict(ws=None), "workspace"), (dict(ws=P + 8), "workspace"),
+    (dict(ws_bytes=gg.gg_ws_product(700, 300, 200) - 1), "workspace"),
+    (dict(k=1 << 24, m=1 << 24, dw=rows(stride=1 << 26)), "too many")])
+def test_weight_gradient_refuses(change, word):
+    refused(gg.lib.gg_product_backward, PRODUCT_BACK, change, word)
+
+
 def test_make_blocks_refuses_what_it_cannot_describe():
     q, sc = torch.zeros(130, 300, dtype=torch.float8_e4m3fn), torch.zeros(2, 3)
     b = gg.make_blocks(q[:, 4:260], torch.zeros(2, 9)[:, 3:5])
@@ -150,6 +170,10 @@ def test_workspaces():
     assert gg.gg_ws_layernorm(-1, 9) == gg.gg_ws_layernorm(9, 0) == gg.gg_ws_layernorm(9, 16_385) == 0
     got = [gg.gg_ws_layernorm(n, 100) for n in (0, 1, 7, 700, 1023, 1024, 5000, 1 << 27)]
     assert got == sorted(got) and got[-1] == 2 * 1024 * 400
+    assert gg.gg_ws_product(-1, 9, 9) == gg.gg_ws_product(9, 0, 9) == gg.gg_ws_product(9, 9, 0) == 0
+    for k, m in ((1, 1), (100, 47), (602, 41), (4096, 4096), (9, 1 << 24)):
+        got = [gg.gg_ws_product(n, k, m) for n in (0, 1, 256, 257, 512, 513, 5000, 100_000, 1 << 27)]
+        assert got == sorted(got) and got[2] == 0 and all(x % (4 * k * m) < 256 for x in got)
 
 
 def test_bindings_check_shapes():
@@ -188,7 +212,10 @@ def test_bindings_check_shapes():
                 lambda: gg.gg_quantise_rows(good, 7, 20, bad8),
                 lambda: gg.gg_quantise_blocks(bad, 7, 20, b(7, 20), None),
                 lambda: gg.gg_product_forward(bad8, 7, 20, b(20, 20), 20, good),
-                lambda: gg.gg_product_forward(r8(7, 20), 7, 20, b(20, 20), 20, bad)):
+                lambda: gg.gg_product_forward(r8(7, 20), 7, 20, b(20, 20), 20, bad),
+                lambda: gg.gg_product_backward(bad8, 7, 20, good, 20, r(20, 20), 0, None),
+                lambda: gg.gg_product_backward(r8(7, 20), 7, 20, bad, 20, r(20, 20), 0, None),
+                lambda: gg.gg_product_backward(r8(7, 20), 7, 20, r(7, 7), 7, bad, 0, None)):
             with pytest.raises(gg.GGError, match="rows of"):
                 call()
     for call, word in (
