@@ -240,3 +240,17 @@ def test_bindings_check_shapes():
             (lambda: gg.gg_quantise_rows(good, 7, 20, b(7, 20)), "make_rows")):
         with pytest.raises(gg.GGError, match=word):
             call()
+
+
+def test_the_student_checks_its_norm_and_tensors():
+    from paper_2606_02916_amd import Student
+    with pytest.raises(gg.GGError, match="neither"):
+        Student(50, 20, 9, max_rows=7, device="cpu", norm="batch")
+    s = Student(50, 20, 9, max_rows=7, k=3, device="cpu", norm="layer", eight_bit=True)
+    ids, top = torch.zeros(8, dtype=torch.int64), torch.zeros(7, 3)
+    for call, word in ((lambda: s.forward(ids, 8), "student of 7"),
+                       (lambda: s.forward(ids, 7, torch.zeros(7, 19)), "x of shape"),
+                       (lambda: s.step(ids, 7, top[:, :2].long(), top), "top_ids of shape"),
+                       (lambda: s.step(ids, 8, torch.zeros(8, 3).long(), torch.zeros(8, 3)), "student of 7")):
+        with pytest.raises(gg.GGError, match=word):
+            call()
