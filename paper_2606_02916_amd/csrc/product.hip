@@ -2,13 +2,14 @@
 //   out[i][j] = sum_g sa[i][g] sb[j / 128][g] sum_{k in block g} a[i][k] b[j][k],
 // codes multiplied by matrix instructions over a block of 128, each block's sum scaled
 // and added in fp32.
+#include <type_traits>
+
 #include "codes.hpp"
 
 namespace gg {
 namespace {
 
 typedef int v8i __attribute__((ext_vector_type(8)));
-typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef bf16 v8bf __attribute__((ext_vector_type(8)));
@@ -23,23 +24,6 @@ struct ProductArgs {
   int32_t per_row;             // a has one scale a row
   int32_t tiles_i, tiles_j;
 };
-
-// 16 bytes of a row's codes from column c on, zeros behind its end.
-__device__ __forceinline__ v4i load_codes(const char* row, int32_t c, int32_t k) {
-  v4i v = {};
-  if (c + 16 <= k) {
-    typedef v4i mem __attribute__((aligned(1)));
-    v = *(const GG_GLOBAL mem*)(row + c);
-  } else {
-#pragma unroll
-    for (int w = 0; w < 4; ++w)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (c + 4 * w + i < k)
-          v[w] |= (int)((uint32_t) * (const GG_GLOBAL uint8_t*)(row + c + 4 * w + i) << 8 * i);
-  }
-  return v;
-}
 
 // A lane's 32 codes as the operand of a product of 16 rows by 16 rows over 128
 // columns.  Which columns a lane has does not matter, both operands agree on it.
@@ -118,14 +102,20 @@ __device__ __forceinline__ void tile_place(const ProductArgs& a, int32_t* ti, in
 
 // A tile of BJ weights' rows by BI rows of a, blocks of 128 bytes of k at a time
 // through LDS.  A row of a block is eight pieces of 16 bytes; row r has piece c in place c
-// ^ (r & 7), so that eight lanes that read the same piece of eight rows meet all
-// banks.  Wave (wj, wi) has BJ/WJ x BI/WI of the tile, weights as the rows of the MFMA's
+// ^ (r / 2 & 7), so that sixteen lanes that read the same piece of sixteen rows meet all
+// banks (with r & 7, eight lanes, reads take twice as long).  Wave (wj, wi) has BJ/WJ x
+// BI/WI of the tile, weights as the rows of the MFMA's
 // result, so that a lane has one row's scale to apply and four neighbours to store.
-template <typename O, int BJ, int BI, int WJ, int WI>
+// DIRECT (both matrices on 16-byte boundaries): pieces go from memory to LDS without a
+// register between, a step ahead; the block at k's end, if it is not whole, and all
+// others' without DIRECT through registers, with zeros behind the end.
+template <typename O, int BJ, int BI, int WJ, int WI, bool DIRECT>
 __global__ void __launch_bounds__(WJ* WI* kWave) k_product_tile(ProductArgs a) {
-  constexpr int kThreads = WJ * WI * kWave, kRows = kThreads / 8, kLoads = (BJ + BI) / kRows;
+  constexpr int kThreads = WJ * WI * kWave, kRows = kThreads / 8, kLoads = (BJ + BI) / kRows,
+                kLoadsJ = BJ / kRows;
   constexpr int TJ = BJ / WJ / 16, TI = BI / WI / 16;
   static_assert(BJ % kRows == 0 && BI % kRows == 0 && BJ / WJ <= kScaleBlock, "tile");
+  typedef Codes<sizeof(O) == 4> C;
   __shared__ v4i lds[2][(BJ + BI) * 8];
   const int32_t tid = (int32_t)threadIdx.x, l = lane_id(),
                 wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -136,24 +126,51 @@ __global__ void __launch_bounds__(WJ* WI* kWave) k_product_tile(ProductArgs a) {
   const int32_t j0 = tj0 * BJ;
 
   // the pieces that this lane brings: rows behind the last one repeat it
+  const char* const jbase = a.b.p + j0 * a.b.stride;
+  const char* const ibase = a.a.p + i0 * a.a.stride;
+  const int32_t jlast = min(a.m - j0, BJ) - 1, ilast = (int32_t)min(a.n - i0, (int64_t)BI) - 1;
   const int32_t slot = tid % 8;
-  const char* from[kLoads];
-  int32_t piece[kLoads];
+  typedef typename std::conditional<DIRECT, uint32_t, int64_t>::type Off;
+  Off from[kLoads];
 #pragma unroll
   for (int t = 0; t < kLoads; ++t) {
     const int32_t r = t * kRows + tid / 8;
-    piece[t] = (slot ^ (r & 7)) * 16;
-    from[t] = r < BJ ? a.b.p + min(j0 + r, a.m - 1) * a.b.stride
-                     : a.a.p + min(i0 + (r - BJ), a.n - 1) * a.a.stride;
+    from[t] = t < kLoadsJ ? (Off)min(r, jlast) * (Off)a.b.stride
+                          : (Off)min(r - BJ, ilast) * (Off)a.a.stride;
+    from[t] += (slot ^ (r >> 1 & 7)) * 16;
   }
-  v4i got[kLoads];
+  // without DIRECT: a whole block into registers, and on into LDS
+  v4i got[DIRECT ? 1 : kLoads];
   const auto fetch = [&](int32_t g) {
+    typedef v4i mem __attribute__((aligned(1)));
+    if constexpr (!DIRECT)
 #pragma unroll
-    for (int t = 0; t < kLoads; ++t) got[t] = load_codes(from[t], g * kBlockK + piece[t], a.k);
+      for (int t = 0; t < kLoads; ++t)
+        got[t] = *(const GG_GLOBAL mem*)((t < kLoadsJ ? jbase : ibase) + (int64_t)g * kBlockK + from[t]);
   };
   const auto keep = [&](int buf) {
+    if constexpr (!DIRECT)
 #pragma unroll
-    for (int t = 0; t < kLoads; ++t) lds[buf][t * kThreads + tid] = got[t];
+      for (int t = 0; t < kLoads; ++t) lds[buf][t * kThreads + tid] = got[t];
+  };
+  // the block at k's end
+  const auto last = [&](int32_t g, int buf) {
+#pragma unroll 1
+    for (int t = 0; t < kLoads; ++t) {
+      const int32_t r = t * kRows + tid / 8;
+      const char* row = t < kLoadsJ ? jbase + min(r, jlast) * a.b.stride
+                                    : ibase + min(r - BJ, ilast) * a.a.stride;
+      lds[buf][t * kThreads + tid] = load_codes(row, g * kBlockK + (slot ^ (r >> 1 & 7)) * 16, a.k);
+    }
+  };
+  const auto bring = [&](int32_t g, int buf) {
+#pragma unroll
+    for (int t = 0; t < kLoads; ++t) {
+      const char* p = (t < kLoadsJ ? jbase : ibase) + (int64_t)g * kBlockK + from[t];
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)p,
+          (__attribute__((address_space(3))) void*)&lds[buf][t * kThreads + wave * kWave], 16, 0, 0);
+    }
   };
 
   // scales: of this lane's rows, and of the wave's block of weights
@@ -171,40 +188,61 @@ __global__ void __launch_bounds__(WJ* WI* kWave) k_product_tile(ProductArgs a) {
   };
 
   v4f acc[TJ][TI] = {};
-  typedef Codes<sizeof(O) == 4> C;
   const auto part = [&](int buf, int32_t r) {
-    const int32_t c = l / 16 * 2 ^ (r & 7);
+    const int32_t c = l / 16 * 2 ^ (r >> 1 & 7);
     C v;
     v.set(lds[buf][r * 8 + c], lds[buf][r * 8 + (c ^ 1)]);
     return v;
   };
-  fetch(0);
+  const int32_t whole = a.k / kBlockK;
   scales(0);
-  keep(0);
+  if (whole == 0) {
+    last(0, 0);
+  } else if (DIRECT) {
+    bring(0, 0);
+  } else {
+    fetch(0);
+    keep(0);
+  }
   for (int32_t g = 0; g < a.kb; ++g) {
+    const int buf = g & 1;
+    if (DIRECT) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): the pieces are there
     __syncthreads();
     float scale[TI];
 #pragma unroll
     for (int t = 0; t < TI; ++t) scale[t] = sa[t] * sb;
-    const bool more = g + 1 < a.kb;
-    if (more) {
-      fetch(g + 1);
-      scales(g + 1);
+    if (g + 1 < a.kb) scales(g + 1);
+    if (g + 1 < whole) {
+      if (DIRECT)
+        bring(g + 1, buf ^ 1);
+      else
+        fetch(g + 1);
+    } else if (g + 1 < a.kb) {
+      last(g + 1, buf ^ 1);
     }
-    C rows[TI];
+    // A product's sum is scaled kLag products later, when the matrix unit has it, and the
+    // weights of the next 16 rows are read before this one's products.
+    constexpr int kLag = 3, N = TJ * TI;
+    C rows[TI], w[2];
+    v4f d[N];
+    w[0] = part(buf, wj * TJ * 16 + l % 16);
 #pragma unroll
-    for (int t = 0; t < TI; ++t) rows[t] = part(g & 1, BJ + (wi * TI + t) * 16 + l % 16);
+    for (int t = 0; t < TI; ++t) rows[t] = part(buf, BJ + (wi * TI + t) * 16 + l % 16);
 #pragma unroll
-    for (int u = 0; u < TJ; ++u) {
-      const C w = part(g & 1, (wj * TJ + u) * 16 + l % 16);
-#pragma unroll
-      for (int t = 0; t < TI; ++t) {
-        const v4f d = multiply(w, rows[t]);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) acc[u][t][r] = __builtin_fmaf(d[r], scale[t], acc[u][t][r]);
+    for (int x = 0; x < N + kLag; ++x) {
+      const int u = x / TI, t = x % TI, y = x - kLag;
+      if (x < N) {
+        if (t == 0 && u + 1 < TJ) w[u + 1 & 1] = part(buf, (wj * TJ + u + 1) * 16 + l % 16);
+        d[x] = multiply(w[u & 1], rows[t]);
       }
+      if (y >= 0) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          acc[y / TI][y % TI][r] = __builtin_fmaf(d[y][r], scale[y % TI], acc[y / TI][y % TI][r]);
+      }
+      __builtin_amdgcn_sched_barrier(0);   // in this order: otherwise sums are waited for
     }
-    if (more) keep(g + 1 & 1);
+    if (g + 1 < whole) keep(buf ^ 1);
   }
 #pragma unroll
   for (int t = 0; t < TI; ++t) {
@@ -320,12 +358,12 @@ int launch_few(ProductArgs& a, hipStream_t stream) {
   return GG_OK;
 }
 
-template <typename O, int BJ, int BI, int WJ, int WI>
+template <typename O, int BJ, int BI, int WJ, int WI, bool DIRECT>
 int launch_tile(ProductArgs& a, hipStream_t stream) {
   a.tiles_i = (int32_t)cdiv(a.n, BI);
   a.tiles_j = (int32_t)cdiv(a.m, BJ);
   GG_REQUIRE((int64_t)a.tiles_i * a.tiles_j <= kGridX * 4, "%lld x %d: too many tiles", (long long)a.n, a.m);
-  hipLaunchKernelGGL((k_product_tile<O, BJ, BI, WJ, WI>), dim3((unsigned)a.tiles_i * a.tiles_j),
+  hipLaunchKernelGGL((k_product_tile<O, BJ, BI, WJ, WI, DIRECT>), dim3((unsigned)a.tiles_i * a.tiles_j),
                      dim3(WJ * WI * kWave), 0, stream, a);
   GG_LAUNCH_CHECK("k_product_tile");
   return GG_OK;
@@ -335,7 +373,13 @@ template <typename O>
 int launch_product(ProductArgs& a, hipStream_t stream) {
   if (a.n <= 16) return launch_few<O, 1, 1>(a, stream);
   if (a.n <= 128) return launch_few<O, 2, 8>(a, stream);
-  return launch_tile<O, 128, 128, 2, 2>(a, stream);
+  const bool direct = aligned16(a.a.p) && aligned16(a.b.p) && a.a.stride % 16 == 0 &&
+                      a.b.stride % 16 == 0 && std::max(a.a.stride, a.b.stride) <= 1 << 23;
+  if (!direct) return launch_tile<O, 128, 128, 2, 2, false>(a, stream);
+  if constexpr (sizeof(O) == 2)
+    if (cdiv(a.n, 256) * cdiv(a.m, 256) >= 192)
+      return launch_tile<O, 256, 256, 2, 4, true>(a, stream);
+  return launch_tile<O, 128, 128, 2, 2, true>(a, stream);
 }
 
 }  // namespace

@@ -8,7 +8,6 @@ namespace gg {
 namespace {
 
 typedef short v4s __attribute__((ext_vector_type(4)));
-typedef int v4i __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef bf16 v2bf __attribute__((ext_vector_type(2)));
 typedef bf16 v8bf __attribute__((ext_vector_type(8)));
@@ -105,21 +104,7 @@ __global__ void __launch_bounds__(kBlock) k_product_grad(GradArgs a) {
   float scale[kLoadsZ];
   const auto fetch = [&](int64_t i0) {
     codes = {};
-    if (i0 + ra < end) {
-      const char* row = a.a.p + (i0 + ra) * a.a.stride;
-      const int32_t c = c0 + ca;
-      if (c + 16 <= a.k) {
-        typedef v4i mem __attribute__((aligned(1)));
-        codes = *(const GG_GLOBAL mem*)(row + c);
-      } else {
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (c + 4 * w + i < a.k)
-              codes[w] |= (int)((uint32_t) * (const GG_GLOBAL uint8_t*)(row + c + 4 * w + i) << 8 * i);
-      }
-    }
+    if (i0 + ra < end) codes = load_codes(a.a.p + (i0 + ra) * a.a.stride, c0 + ca, a.k);
 #pragma unroll
     for (int t = 0; t < kLoadsZ; ++t) {
       const int64_t i = i0 + t * kStepZ + rz;

@@ -111,7 +111,7 @@ def test_product(n, k, m):
 @pytest.mark.parametrize("group", [0, 128])
 @pytest.mark.parametrize("n,k,m", [(1, 4096, 512), (16, 2048, 200), (40, 1024, 260), (100, 4096, 256),
                                    (200, 512, 512), (512, 256, 640), (1000, 1024, 700), (2500, 384, 1300),
-                                   (47, 16_384, 33), (700, 128, 64)])
+                                   (47, 16_384, 33), (700, 128, 64), (3400, 400, 3700), (4097, 128, 3000)])
 def test_product_at_aligned_places(n, k, m, group, t):
     """Rows on 16-byte boundaries, and whole or partial tiles of them."""
     check_forward(n, k, m, t, group, 0, 0)
