@@ -100,17 +100,179 @@ __device__ __forceinline__ void tile_place(const ProductArgs& a, int32_t* ti, in
   *tj = (int32_t)(at / rows);
 }
 
+// The products of a wave's TJ x TI operands from LDS, added to acc with the scales of
+// its rows.  A product's sum is scaled kLag products later, when the matrix unit has it,
+// and the weights of the next 16 rows are read before this one's products; kept in
+// this order, since otherwise each sum is waited for (614 us instead of 712 for 8,191 x
+// 4,096 to 16,384).  read(r): the operand of row r of the tile, weights first.
+template <int TJ, int TI, typename C, typename R>
+__device__ __forceinline__ void multiply_step(int32_t jrow, int32_t irow, const float (&scale)[TI],
+                                              v4f (&acc)[TJ][TI], R read) {
+  constexpr int N = TJ * TI, kLag = N > 3 ? 3 : N - 1;
+  C rows[TI], w[2];
+  v4f d[N];
+  w[0] = read(jrow);
+#pragma unroll
+  for (int t = 0; t < TI; ++t) rows[t] = read(irow + t * 16);
+#pragma unroll
+  for (int x = 0; x < N + kLag; ++x) {
+    const int u = x / TI, t = x % TI, y = x - kLag;
+    if (x < N) {
+      if (t == 0 && u + 1 < TJ) w[u + 1 & 1] = read(jrow + (u + 1) * 16);
+      d[x] = multiply(w[u & 1], rows[t]);
+    }
+    if (y >= 0) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        acc[y / TI][y % TI][r] = __builtin_fmaf(d[y][r], scale[y % TI], acc[y / TI][y % TI][r]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+template <typename O, int TJ, int TI>
+__device__ __forceinline__ void store_tile(const ProductArgs& a, int64_t i0, int32_t j0, int32_t l,
+                                           const v4f (&acc)[TJ][TI]) {
+#pragma unroll
+  for (int t = 0; t < TI; ++t) {
+    const int64_t i = i0 + t * 16 + l % 16;
+    if (i >= a.n) continue;
+#pragma unroll
+    for (int u = 0; u < TJ; ++u) {
+      const int32_t j = j0 + u * 16 + l / 16 * 4;
+      if (j < a.m) store_four<O>(a.out, i, j, a.m, acc[u][t]);
+    }
+  }
+}
+
+// A wave's 64 lanes' pieces of 16 bytes, or words, from base + off to consecutive places of LDS
+// at byte `to`.  Written out, since before the next read of LDS the compiler waits for all such
+// loads that it knows of; these are waited for by their number.  They write no register.
+__device__ __forceinline__ void load_to_lds16(const char* base, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off),
+               "s"(base)
+               : "memory");
+}
+__device__ __forceinline__ void load_to_lds4(const char* p, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(p)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t lds_at(const void* p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
+}
+
 // A tile of BJ weights' rows by BI rows of a, blocks of 128 bytes of k at a time
 // through LDS.  A row of a block is eight pieces of 16 bytes; row r has piece c in place c
 // ^ (r / 2 & 7), so that sixteen lanes that read the same piece of sixteen rows meet all
 // banks (with r & 7, eight lanes, reads take twice as long).  Wave (wj, wi) has BJ/WJ x
-// BI/WI of the tile, weights as the rows of the MFMA's
-// result, so that a lane has one row's scale to apply and four neighbours to store.
-// DIRECT (both matrices on 16-byte boundaries): pieces go from memory to LDS without a
-// register between, a step ahead; the block at k's end, if it is not whole, and all
-// others' without DIRECT through registers, with zeros behind the end.
-template <typename O, int BJ, int BI, int WJ, int WI, bool DIRECT>
-__global__ void __launch_bounds__(WJ* WI* kWave) k_product_tile(ProductArgs a) {
+// BI/WI of the tile, weights as the rows of the MFMA's result, so that a lane has one
+// row's scale to apply and four neighbours to store.
+//
+// Both matrices lie on 16-byte boundaries: pieces go from memory to LDS without a register
+// between, STAGES - 1 blocks ahead, and the scales with them, so that the wait for a block
+// can count the loads behind it.  A block at k's end that is not whole comes
+// through registers, with zeros behind the end.
+template <typename O, int BJ, int BI, int WJ, int WI, int STAGES>
+__global__ void __launch_bounds__(WJ* WI* kWave, 2) k_product_pipe(ProductArgs a) {
+  constexpr int kThreads = WJ * WI * kWave, kPieces = (BJ + BI) * 8, kLoads = kPieces / kThreads,
+                kBlocksJ = (BJ + kScaleBlock - 1) / kScaleBlock;
+  constexpr int TJ = BJ / WJ / 16, TI = BI / WI / 16;
+  static_assert(kPieces % kThreads == 0 && kThreads % 8 == 0, "whole loads");
+  static_assert(BJ / WJ <= kScaleBlock && kScaleBlock % (BJ / WJ) == 0, "one block of weights a wave");
+  static_assert(BI + kBlocksJ <= kThreads, "a lane for each scale");
+  constexpr int kBehind = (kLoads + 1) * (STAGES - 2);   // loads that may be under way
+  static_assert(kBehind < 64, "the counter of loads");
+  typedef Codes<sizeof(O) == 4> C;
+  __shared__ v4i lds[STAGES][kPieces];
+  __shared__ float scales[STAGES][kThreads];
+  const int32_t tid = (int32_t)threadIdx.x, l = lane_id(),
+                wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int32_t wj = wave % WJ, wi = wave / WJ;
+  int32_t ti0, tj0;
+  tile_place(a, &ti0, &tj0);
+  const int64_t i0 = (int64_t)ti0 * BI;
+  const int32_t j0 = tj0 * BJ;
+
+  // the pieces that this lane brings: rows behind the last one repeat it
+  const char* const jbase = a.b.p + j0 * a.b.stride;
+  const char* const ibase = a.a.p + i0 * a.a.stride;
+  const int32_t jlast = min(a.m - j0, BJ) - 1, ilast = (int32_t)min(a.n - i0, (int64_t)BI) - 1;
+  const auto row_of = [&](int t, int64_t* off) {
+    const int32_t r = (t * kThreads + tid) / 8;
+    *off = r < BJ ? min(r, jlast) * a.b.stride : min(r - BJ, ilast) * a.a.stride;
+    return r;
+  };
+  uint32_t from[kLoads];
+#pragma unroll
+  for (int t = 0; t < kLoads; ++t) {
+    int64_t off;
+    const int32_t r = row_of(t, &off);
+    from[t] = (uint32_t)off + (tid % 8 ^ (r >> 1 & 7)) * 16;
+  }
+  // its scale: a row's, or behind them a block's of weights
+  const char* scale_from;
+  int32_t scale_step = a.per_row ? 0 : 4;
+  if (tid < BI) {
+    scale_from = a.a.scales + (i0 + min(tid, ilast)) * a.a.sstride;
+  } else {
+    scale_from = a.b.scales + min(j0 + min(tid - BI, kBlocksJ - 1) * kScaleBlock, a.m - 1) /
+                                  kScaleBlock * a.b.sstride;
+    scale_step = 4;
+  }
+  const int32_t whole = a.k / kBlockK;
+  const auto bring = [&](int32_t g, int slot) {
+    if (g < whole) {
+      const char *jp = jbase + (int64_t)g * kBlockK, *ip = ibase + (int64_t)g * kBlockK;
+#pragma unroll
+      for (int t = 0; t < kLoads; ++t) {
+        // (a load's 64 lanes are of one matrix: BJ is a multiple of 8)
+        const bool weights = (t * kThreads + wave * kWave) / 8 < BJ;
+        load_to_lds16(weights ? jp : ip, from[t], lds_at(&lds[slot][t * kThreads + wave * kWave]));
+      }
+    } else {
+#pragma unroll 1
+      for (int t = 0; t < kLoads; ++t) {
+        int64_t off;
+        const int32_t r = row_of(t, &off);
+        lds[slot][t * kThreads + tid] = load_codes((r < BJ ? jbase : ibase) + off,
+                                                   g * kBlockK + (tid % 8 ^ (r >> 1 & 7)) * 16, a.k);
+      }
+    }
+    load_to_lds4(scale_from + (int64_t)g * scale_step, lds_at(&scales[slot][wave * kWave]));
+  };
+
+  v4f acc[TJ][TI] = {};
+#pragma unroll
+  for (int g = 0; g < STAGES - 1; ++g)
+    if (g < a.kb) bring(g, g);
+  int slot = 0;
+  for (int32_t g = 0; g < a.kb; ++g) {
+    // block g is here, in all waves' parts, and block g - 1 has been read
+    if (g + STAGES - 2 < whole)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kBehind) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (g + STAGES - 1 < a.kb) bring(g + STAGES - 1, slot ? slot - 1 : STAGES - 1);
+    const float* sc = scales[slot];
+    const float sb = sc[BI + wj * TJ * 16 / kScaleBlock];
+    float scale[TI];
+#pragma unroll
+    for (int t = 0; t < TI; ++t) scale[t] = sc[(wi * TI + t) * 16 + l % 16] * sb;
+    multiply_step<TJ, TI, C>(wj * TJ * 16 + l % 16, BJ + wi * TI * 16 + l % 16, scale, acc,
+                             [&](int32_t r) {
+                               const int32_t c = l / 16 * 2 ^ (r >> 1 & 7);
+                               C v;
+                               v.set(lds[slot][r * 8 + c], lds[slot][r * 8 + (c ^ 1)]);
+                               return v;
+                             });
+    slot = slot + 1 < STAGES ? slot + 1 : 0;
+  }
+  store_tile<O, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc);
+}
+
+// The same for matrices off 16-byte boundaries: blocks come through registers.
+template <typename O, int BJ, int BI, int WJ, int WI>
+__global__ void __launch_bounds__(WJ* WI* kWave, sizeof(O) == 4 ? 1 : 2) k_product_tile(ProductArgs a) {
   constexpr int kThreads = WJ * WI * kWave, kRows = kThreads / 8, kLoads = (BJ + BI) / kRows,
                 kLoadsJ = BJ / kRows;
   constexpr int TJ = BJ / WJ / 16, TI = BI / WI / 16;
@@ -125,54 +287,25 @@ __global__ void __launch_bounds__(WJ* WI* kWave) k_product_tile(ProductArgs a) {
   const int64_t i0 = (int64_t)ti0 * BI;
   const int32_t j0 = tj0 * BJ;
 
-  // the pieces that this lane brings: rows behind the last one repeat it
-  const char* const jbase = a.b.p + j0 * a.b.stride;
-  const char* const ibase = a.a.p + i0 * a.a.stride;
-  const int32_t jlast = min(a.m - j0, BJ) - 1, ilast = (int32_t)min(a.n - i0, (int64_t)BI) - 1;
+  // the rows of this lane's pieces: those behind the last one repeat it
   const int32_t slot = tid % 8;
-  typedef typename std::conditional<DIRECT, uint32_t, int64_t>::type Off;
-  Off from[kLoads];
+  const char* row[kLoads];
 #pragma unroll
   for (int t = 0; t < kLoads; ++t) {
     const int32_t r = t * kRows + tid / 8;
-    from[t] = t < kLoadsJ ? (Off)min(r, jlast) * (Off)a.b.stride
-                          : (Off)min(r - BJ, ilast) * (Off)a.a.stride;
-    from[t] += (slot ^ (r >> 1 & 7)) * 16;
+    row[t] = t < kLoadsJ ? a.b.p + min(j0 + r, a.m - 1) * a.b.stride
+                         : a.a.p + min(i0 + (r - BJ), a.n - 1) * a.a.stride;
   }
-  // without DIRECT: a whole block into registers, and on into LDS
-  v4i got[DIRECT ? 1 : kLoads];
+  v4i got[kLoads];
   const auto fetch = [&](int32_t g) {
-    typedef v4i mem __attribute__((aligned(1)));
-    if constexpr (!DIRECT)
 #pragma unroll
-      for (int t = 0; t < kLoads; ++t)
-        got[t] = *(const GG_GLOBAL mem*)((t < kLoadsJ ? jbase : ibase) + (int64_t)g * kBlockK + from[t]);
+    for (int t = 0; t < kLoads; ++t)
+      got[t] = load_codes(row[t], g * kBlockK + (slot ^ ((t * kRows + tid / 8) >> 1 & 7)) * 16, a.k);
   };
   const auto keep = [&](int buf) {
-    if constexpr (!DIRECT)
 #pragma unroll
-      for (int t = 0; t < kLoads; ++t) lds[buf][t * kThreads + tid] = got[t];
+    for (int t = 0; t < kLoads; ++t) lds[buf][t * kThreads + tid] = got[t];
   };
-  // the block at k's end
-  const auto last = [&](int32_t g, int buf) {
-#pragma unroll 1
-    for (int t = 0; t < kLoads; ++t) {
-      const int32_t r = t * kRows + tid / 8;
-      const char* row = t < kLoadsJ ? jbase + min(r, jlast) * a.b.stride
-                                    : ibase + min(r - BJ, ilast) * a.a.stride;
-      lds[buf][t * kThreads + tid] = load_codes(row, g * kBlockK + (slot ^ (r >> 1 & 7)) * 16, a.k);
-    }
-  };
-  const auto bring = [&](int32_t g, int buf) {
-#pragma unroll
-    for (int t = 0; t < kLoads; ++t) {
-      const char* p = (t < kLoadsJ ? jbase : ibase) + (int64_t)g * kBlockK + from[t];
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)p,
-          (__attribute__((address_space(3))) void*)&lds[buf][t * kThreads + wave * kWave], 16, 0, 0);
-    }
-  };
-
   // scales: of this lane's rows, and of the wave's block of weights
   const char* row_scale[TI];
 #pragma unroll
@@ -188,72 +321,30 @@ __global__ void __launch_bounds__(WJ* WI* kWave) k_product_tile(ProductArgs a) {
   };
 
   v4f acc[TJ][TI] = {};
-  const auto part = [&](int buf, int32_t r) {
-    const int32_t c = l / 16 * 2 ^ (r >> 1 & 7);
-    C v;
-    v.set(lds[buf][r * 8 + c], lds[buf][r * 8 + (c ^ 1)]);
-    return v;
-  };
-  const int32_t whole = a.k / kBlockK;
+  fetch(0);
   scales(0);
-  if (whole == 0) {
-    last(0, 0);
-  } else if (DIRECT) {
-    bring(0, 0);
-  } else {
-    fetch(0);
-    keep(0);
-  }
+  keep(0);
   for (int32_t g = 0; g < a.kb; ++g) {
     const int buf = g & 1;
-    if (DIRECT) __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): the pieces are there
     __syncthreads();
     float scale[TI];
 #pragma unroll
     for (int t = 0; t < TI; ++t) scale[t] = sa[t] * sb;
-    if (g + 1 < a.kb) scales(g + 1);
-    if (g + 1 < whole) {
-      if (DIRECT)
-        bring(g + 1, buf ^ 1);
-      else
-        fetch(g + 1);
-    } else if (g + 1 < a.kb) {
-      last(g + 1, buf ^ 1);
+    const bool more = g + 1 < a.kb;
+    if (more) {
+      fetch(g + 1);
+      scales(g + 1);
     }
-    // A product's sum is scaled kLag products later, when the matrix unit has it, and the
-    // weights of the next 16 rows are read before this one's products.
-    constexpr int kLag = 3, N = TJ * TI;
-    C rows[TI], w[2];
-    v4f d[N];
-    w[0] = part(buf, wj * TJ * 16 + l % 16);
-#pragma unroll
-    for (int t = 0; t < TI; ++t) rows[t] = part(buf, BJ + (wi * TI + t) * 16 + l % 16);
-#pragma unroll
-    for (int x = 0; x < N + kLag; ++x) {
-      const int u = x / TI, t = x % TI, y = x - kLag;
-      if (x < N) {
-        if (t == 0 && u + 1 < TJ) w[u + 1 & 1] = part(buf, (wj * TJ + u + 1) * 16 + l % 16);
-        d[x] = multiply(w[u & 1], rows[t]);
-      }
-      if (y >= 0) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          acc[y / TI][y % TI][r] = __builtin_fmaf(d[y][r], scale[y % TI], acc[y / TI][y % TI][r]);
-      }
-      __builtin_amdgcn_sched_barrier(0);   // in this order: otherwise sums are waited for
-    }
-    if (g + 1 < whole) keep(buf ^ 1);
+    multiply_step<TJ, TI, C>(wj * TJ * 16 + l % 16, BJ + wi * TI * 16 + l % 16, scale, acc,
+                             [&](int32_t r) {
+                               const int32_t c = l / 16 * 2 ^ (r >> 1 & 7);
+                               C v;
+                               v.set(lds[buf][r * 8 + c], lds[buf][r * 8 + (c ^ 1)]);
+                               return v;
+                             });
+    if (more) keep(buf ^ 1);
   }
-#pragma unroll
-  for (int t = 0; t < TI; ++t) {
-    const int64_t i = i0 + (wi * TI + t) * 16 + l % 16;
-    if (i >= a.n) continue;
-#pragma unroll
-    for (int u = 0; u < TJ; ++u) {
-      const int32_t j = j0 + (wj * TJ + u) * 16 + l / 16 * 4;
-      if (j < a.m) store_four<O>(a.out, i, j, a.m, acc[u][t]);
-    }
-  }
+  store_tile<O, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc);
 }
 
 // Few rows: the weights go from memory to the MFMA's registers, without LDS.  A block
@@ -358,12 +449,28 @@ int launch_few(ProductArgs& a, hipStream_t stream) {
   return GG_OK;
 }
 
-template <typename O, int BJ, int BI, int WJ, int WI, bool DIRECT>
-int launch_tile(ProductArgs& a, hipStream_t stream) {
-  a.tiles_i = (int32_t)cdiv(a.n, BI);
-  a.tiles_j = (int32_t)cdiv(a.m, BJ);
+int tiles_of(ProductArgs& a, int bj, int bi) {
+  a.tiles_i = (int32_t)cdiv(a.n, bi);
+  a.tiles_j = (int32_t)cdiv(a.m, bj);
   GG_REQUIRE((int64_t)a.tiles_i * a.tiles_j <= kGridX * 4, "%lld x %d: too many tiles", (long long)a.n, a.m);
-  hipLaunchKernelGGL((k_product_tile<O, BJ, BI, WJ, WI, DIRECT>), dim3((unsigned)a.tiles_i * a.tiles_j),
+  return GG_OK;
+}
+
+template <typename O, int BJ, int BI, int WJ, int WI, int STAGES>
+int launch_pipe(ProductArgs& a, hipStream_t stream) {
+  const int rc = tiles_of(a, BJ, BI);
+  if (rc != GG_OK) return rc;
+  hipLaunchKernelGGL((k_product_pipe<O, BJ, BI, WJ, WI, STAGES>),
+                     dim3((unsigned)a.tiles_i * a.tiles_j), dim3(WJ * WI * kWave), 0, stream, a);
+  GG_LAUNCH_CHECK("k_product_pipe");
+  return GG_OK;
+}
+
+template <typename O, int BJ, int BI, int WJ, int WI>
+int launch_tile(ProductArgs& a, hipStream_t stream) {
+  const int rc = tiles_of(a, BJ, BI);
+  if (rc != GG_OK) return rc;
+  hipLaunchKernelGGL((k_product_tile<O, BJ, BI, WJ, WI>), dim3((unsigned)a.tiles_i * a.tiles_j),
                      dim3(WJ * WI * kWave), 0, stream, a);
   GG_LAUNCH_CHECK("k_product_tile");
   return GG_OK;
@@ -371,15 +478,18 @@ int launch_tile(ProductArgs& a, hipStream_t stream) {
 
 template <typename O>
 int launch_product(ProductArgs& a, hipStream_t stream) {
-  if (a.n <= 16) return launch_few<O, 1, 1>(a, stream);
-  if (a.n <= 128) return launch_few<O, 2, 8>(a, stream);
   const bool direct = aligned16(a.a.p) && aligned16(a.b.p) && a.a.stride % 16 == 0 &&
                       a.b.stride % 16 == 0 && std::max(a.a.stride, a.b.stride) <= 1 << 23;
-  if (!direct) return launch_tile<O, 128, 128, 2, 2, false>(a, stream);
+  if (a.n <= 16 || (a.n <= 128 && !direct)) {
+    if (a.n <= 16) return launch_few<O, 1, 1>(a, stream);
+    return launch_few<O, 2, 8>(a, stream);
+  }
+  if (!direct) return launch_tile<O, 128, 128, 2, 2>(a, stream);
+  if (a.n <= 128) return launch_pipe<O, 32, 128, 1, 4, 7>(a, stream);
   if constexpr (sizeof(O) == 2)
     if (cdiv(a.n, 256) * cdiv(a.m, 256) >= 192)
-      return launch_tile<O, 256, 256, 2, 4, true>(a, stream);
-  return launch_tile<O, 128, 128, 2, 2, true>(a, stream);
+      return launch_pipe<O, 256, 256, 2, 4, 2>(a, stream);
+  return launch_pipe<O, 128, 128, 2, 2, 2>(a, stream);
 }
 
 }  // namespace
