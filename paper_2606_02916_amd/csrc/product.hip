@@ -100,31 +100,41 @@ __device__ __forceinline__ void tile_place(const ProductArgs& a, int32_t* ti, in
   *tj = (int32_t)(at / rows);
 }
 
+// A lane's codes of a row in LDS: its pieces 2 q and 2 q + 1, q = l / 16, where rows keep
+// piece c in place c ^ (row / 2 & 7).  Rows 16 apart are alike.
+template <typename C>
+__device__ __forceinline__ C operand(const v4i* row, int32_t l) {
+  const int32_t c = l / 16 * 2 ^ (l >> 1 & 7);
+  C v;
+  v.set(row[c], row[c ^ 1]);
+  return v;
+}
+
 // The products of a wave's TJ x TI operands from LDS, added to acc with the scales of
 // its rows.  A product's sum is scaled kLag products later, when the matrix unit has it,
 // and the weights of the next 16 rows are read before this one's products; kept in
 // this order, since otherwise each sum is waited for (614 us instead of 712 for 8,191 x
-// 4,096 to 16,384).  read(r): the operand of row r of the tile, weights first.
-template <int TJ, int TI, typename C, typename R>
-__device__ __forceinline__ void multiply_step(int32_t jrow, int32_t irow, const float (&scale)[TI],
-                                              v4f (&acc)[TJ][TI], R read) {
+// 4,096 to 16,384).  weights(r) and rows(r): the operands of this lane's row r.
+template <int TJ, int TI, typename C, typename W, typename R>
+__device__ __forceinline__ void multiply_step(const float (&scale)[TI], v4f (&acc)[TJ][TI], W weights,
+                                              R rows) {
   constexpr int N = TJ * TI, kLag = N > 3 ? 3 : N - 1;
-  C rows[TI], w[2];
+  C r[TI], w[2];
   v4f d[N];
-  w[0] = read(jrow);
+  w[0] = weights(0);
 #pragma unroll
-  for (int t = 0; t < TI; ++t) rows[t] = read(irow + t * 16);
+  for (int t = 0; t < TI; ++t) r[t] = rows(t * 16);
 #pragma unroll
   for (int x = 0; x < N + kLag; ++x) {
     const int u = x / TI, t = x % TI, y = x - kLag;
     if (x < N) {
-      if (t == 0 && u + 1 < TJ) w[u + 1 & 1] = read(jrow + (u + 1) * 16);
-      d[x] = multiply(w[u & 1], rows[t]);
+      if (t == 0 && u + 1 < TJ) w[u + 1 & 1] = weights((u + 1) * 16);
+      d[x] = multiply(w[u & 1], r[t]);
     }
     if (y >= 0) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        acc[y / TI][y % TI][r] = __builtin_fmaf(d[y][r], scale[y % TI], acc[y / TI][y % TI][r]);
+      for (int i = 0; i < 4; ++i)
+        acc[y / TI][y % TI][i] = __builtin_fmaf(d[y][i], scale[y % TI], acc[y / TI][y % TI][i]);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -258,13 +268,9 @@ __global__ void __launch_bounds__(WJ* WI* kWave, 2) k_product_pipe(ProductArgs a
     float scale[TI];
 #pragma unroll
     for (int t = 0; t < TI; ++t) scale[t] = sc[(wi * TI + t) * 16 + l % 16] * sb;
-    multiply_step<TJ, TI, C>(wj * TJ * 16 + l % 16, BJ + wi * TI * 16 + l % 16, scale, acc,
-                             [&](int32_t r) {
-                               const int32_t c = l / 16 * 2 ^ (r >> 1 & 7);
-                               C v;
-                               v.set(lds[slot][r * 8 + c], lds[slot][r * 8 + (c ^ 1)]);
-                               return v;
-                             });
+    const v4i *w = lds[slot] + (wj * TJ * 16 + l % 16) * 8, *r = lds[slot] + (BJ + wi * TI * 16 + l % 16) * 8;
+    multiply_step<TJ, TI, C>(scale, acc, [&](int x) { return operand<C>(w + x * 8, l); },
+                             [&](int x) { return operand<C>(r + x * 8, l); });
     slot = slot + 1 < STAGES ? slot + 1 : 0;
   }
   store_tile<O, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc);
@@ -335,80 +341,123 @@ __global__ void __launch_bounds__(WJ* WI* kWave, sizeof(O) == 4 ? 1 : 2) k_produ
       fetch(g + 1);
       scales(g + 1);
     }
-    multiply_step<TJ, TI, C>(wj * TJ * 16 + l % 16, BJ + wi * TI * 16 + l % 16, scale, acc,
-                             [&](int32_t r) {
-                               const int32_t c = l / 16 * 2 ^ (r >> 1 & 7);
-                               C v;
-                               v.set(lds[buf][r * 8 + c], lds[buf][r * 8 + (c ^ 1)]);
-                               return v;
-                             });
+    const v4i *w = lds[buf] + (wj * TJ * 16 + l % 16) * 8, *r = lds[buf] + (BJ + wi * TI * 16 + l % 16) * 8;
+    multiply_step<TJ, TI, C>(scale, acc, [&](int x) { return operand<C>(w + x * 8, l); },
+                             [&](int x) { return operand<C>(r + x * 8, l); });
     if (more) keep(buf ^ 1);
   }
   store_tile<O, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc);
 }
 
-// Few rows: the weights go from memory to the MFMA's registers, without LDS.  A block
-// has 16 TJ weights' rows and 16 TI rows of a; its waves take the blocks of k in
-// turn, and their sums are added in the order of the waves' halves.  Bound by the weights'
-// bytes.
+// Few rows: operands go from memory to registers, without LDS.  A block has 16 TJ weights'
+// rows and 16 TI rows of a; its waves take the blocks of k in turn, with no wait for each
+// other, the next one's operands loaded before this one's products, and their sums are
+// added in the order of the waves' halves.  Bound by the weights' bytes, and for
+// more than some 32 rows by those of a, which every block reads from the caches.
 constexpr int kFewWaves = 8;
 
 template <typename O, int TJ, int TI>
-__global__ void __launch_bounds__(kFewWaves* kWave) k_product_few(ProductArgs a) {
+__global__ void __launch_bounds__(kFewWaves* kWave, 2) k_product_few(ProductArgs a) {
+  constexpr int kAhead = TI == 1 ? 2 : 1;        // blocks in a step
   typedef Codes<sizeof(O) == 4> C;
-  constexpr int kAhead = TI <= 2 ? 4 : TI <= 4 ? 2 : 1;
   __shared__ v4f lds[kFewWaves / 2][TJ * TI][kWave];
   const int32_t l = lane_id(),
                 wave = __builtin_amdgcn_readfirstlane((int32_t)threadIdx.x / kWave),
                 waves = (int32_t)blockDim.x / kWave;
-  const int32_t j0 = (int32_t)blockIdx.x * TJ * 16;
-  const int64_t i0 = (int64_t)blockIdx.y * TI * 16;
-  const char *wrow[TJ], *arow[TI], *ascale[TI];
+  int32_t ti0, tj0;
+  tile_place(a, &ti0, &tj0);
+  const int32_t j0 = tj0 * TJ * 16;
+  const int64_t i0 = (int64_t)ti0 * TI * 16;
+  // rows behind the last one repeat it
+  const char* const wbase = a.b.p + j0 * a.b.stride;
+  const char* const rbase = a.a.p + i0 * a.a.stride;
+  const char* const sbase = a.a.scales + i0 * a.a.sstride;
+  const char* const wscale = a.b.scales + j0 / kScaleBlock * a.b.sstride;
+  const int32_t jlast = a.m - j0 - 1, ilast = (int32_t)min(a.n - i0, (int64_t)TI * 16) - 1;
+  uint32_t w_off[TJ], r_off[TI], s_off[TI];
 #pragma unroll
-  for (int u = 0; u < TJ; ++u) wrow[u] = a.b.p + min(j0 + u * 16 + l % 16, a.m - 1) * a.b.stride;
+  for (int u = 0; u < TJ; ++u) w_off[u] = (uint32_t)min(u * 16 + l % 16, jlast) * (uint32_t)a.b.stride;
 #pragma unroll
   for (int t = 0; t < TI; ++t) {
-    const int64_t i = min(i0 + t * 16 + l % 16, a.n - 1);
-    arow[t] = a.a.p + i * a.a.stride;
-    ascale[t] = a.a.scales + i * a.a.sstride;
+    r_off[t] = (uint32_t)min(t * 16 + l % 16, ilast) * (uint32_t)a.a.stride;
+    s_off[t] = (uint32_t)min(t * 16 + l % 16, ilast) * (uint32_t)a.a.sstride;
   }
-  const char* wscale = a.b.scales + j0 / kScaleBlock * a.b.sstride;
-  v4f acc[TJ][TI] = {};
-  // Whole blocks of k, kAhead of them loaded before the first is used; the lanes' pieces
-  // behind k's end are zeros.
-  for (int32_t g0 = wave; g0 < a.kb; g0 += waves * kAhead) {
-    C w[kAhead][TJ], r[kAhead][TI];
+  const int32_t whole = a.k / kBlockK, lane_c = l / 16 * 32;
+  struct Step {
+    v4i w[kAhead][TJ][2], r[kAhead][TI][2];
     float sb[kAhead], sa[kAhead][TI];
+  };
+  const auto load_scales = [&](int32_t g, int h, Step& s) {
+    s.sb[h] = *(const float*)(wscale + 4LL * g);
+#pragma unroll
+    for (int t = 0; t < TI; ++t)
+      s.sa[h][t] = *(const GG_GLOBAL float*)(sbase + (a.per_row ? 0 : 4LL * g) + s_off[t]);
+  };
+  const auto load = [&](int32_t g0, Step& s) {
+    typedef v4i mem __attribute__((aligned(1)));
 #pragma unroll
     for (int h = 0; h < kAhead; ++h) {
-      const int32_t g = g0 + h * waves, c = g * kBlockK + l / 16 * 32;
-      if (g < a.kb) {
+      const int32_t g = g0 + h * waves;
+      if (g >= whole) break;
+      const char *wp = wbase + (int64_t)g * kBlockK, *rp = rbase + (int64_t)g * kBlockK;
+      load_scales(g, h, s);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
 #pragma unroll
         for (int u = 0; u < TJ; ++u)
-          w[h][u].set(load_codes(wrow[u], c, a.k), load_codes(wrow[u], c + 16, a.k));
+          s.w[h][u][x] = *(const GG_GLOBAL mem*)(wp + (w_off[u] + lane_c) + 16 * x);
 #pragma unroll
         for (int t = 0; t < TI; ++t)
-          r[h][t].set(load_codes(arow[t], c, a.k), load_codes(arow[t], c + 16, a.k));
-        sb[h] = *(const float*)(wscale + 4 * g);
-#pragma unroll
-        for (int t = 0; t < TI; ++t)
-          sa[h][t] = *(const GG_GLOBAL float*)(ascale[t] + (a.per_row ? 0 : 4 * g));
+          s.r[h][t][x] = *(const GG_GLOBAL mem*)(rp + (r_off[t] + lane_c) + 16 * x);
       }
     }
+  };
+  v4f acc[TJ][TI] = {};
+  const auto add = [&](int h, const Step& s) {
+    C w[TJ];
+#pragma unroll
+    for (int u = 0; u < TJ; ++u) w[u].set(s.w[h][u][0], s.w[h][u][1]);
+#pragma unroll
+    for (int t = 0; t < TI; ++t) {
+      const float scale = s.sa[h][t] * s.sb[h];
+      C r;
+      r.set(s.r[h][t][0], s.r[h][t][1]);
+#pragma unroll
+      for (int u = 0; u < TJ; ++u) {
+        const v4f d = multiply(w[u], r);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) acc[u][t][x] = __builtin_fmaf(d[x], scale, acc[u][t][x]);
+      }
+    }
+  };
+  const auto add_all = [&](int32_t g0, const Step& s) {
 #pragma unroll
     for (int h = 0; h < kAhead; ++h) {
-      if (g0 + h * waves >= a.kb) break;
-#pragma unroll
-      for (int t = 0; t < TI; ++t) {
-        const float scale = sa[h][t] * sb[h];
-#pragma unroll
-        for (int u = 0; u < TJ; ++u) {
-          const v4f d = multiply(w[h][u], r[h][t]);
-#pragma unroll
-          for (int x = 0; x < 4; ++x) acc[u][t][x] = __builtin_fmaf(d[x], scale, acc[u][t][x]);
-        }
-      }
+      if (g0 + h * waves >= whole) break;
+      add(h, s);
     }
+  };
+  Step s[2];
+  const int32_t step = waves * kAhead;
+  load(wave, s[0]);
+  for (int32_t g = wave; g < whole; g += 2 * step) {
+    load(g + step, s[1]);
+    add_all(g, s[0]);
+    if (g + step >= whole) break;
+    load(g + 2 * step, s[0]);
+    add_all(g + step, s[1]);
+  }
+  if (whole < a.kb && whole % waves == wave) {   // the block at k's end
+    load_scales(whole, 0, s[0]);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int32_t c = whole * kBlockK + lane_c + 16 * x;
+#pragma unroll
+      for (int u = 0; u < TJ; ++u) s[0].w[0][u][x] = load_codes(wbase + w_off[u], c, a.k);
+#pragma unroll
+      for (int t = 0; t < TI; ++t) s[0].r[0][t][x] = load_codes(rbase + r_off[t], c, a.k);
+    }
+    add(0, s[0]);
   }
   for (int32_t half = waves / 2; half >= 1; half /= 2) {
     __syncthreads();
@@ -426,33 +475,25 @@ __global__ void __launch_bounds__(kFewWaves* kWave) k_product_few(ProductArgs a)
         for (int t = 0; t < TI; ++t) acc[u][t] += lds[wave][u * TI + t][l];
     }
   }
-  if (wave) return;
-#pragma unroll
-  for (int t = 0; t < TI; ++t) {
-    const int64_t i = i0 + t * 16 + l % 16;
-    if (i >= a.n) continue;
-#pragma unroll
-    for (int u = 0; u < TJ; ++u) {
-      const int32_t j = j0 + u * 16 + l / 16 * 4;
-      if (j < a.m) store_four<O>(a.out, i, j, a.m, acc[u][t]);
-    }
-  }
-}
-
-template <typename O, int TJ, int TI>
-int launch_few(ProductArgs& a, hipStream_t stream) {
-  int waves = 1;
-  while (waves < kFewWaves && waves < a.kb) waves *= 2;
-  const dim3 grid((unsigned)cdiv(a.m, TJ * 16), (unsigned)cdiv(a.n, TI * 16));
-  hipLaunchKernelGGL((k_product_few<O, TJ, TI>), grid, dim3(waves * kWave), 0, stream, a);
-  GG_LAUNCH_CHECK("k_product_few");
-  return GG_OK;
+  if (wave == 0) store_tile<O, TJ, TI>(a, i0, j0, l, acc);
 }
 
 int tiles_of(ProductArgs& a, int bj, int bi) {
   a.tiles_i = (int32_t)cdiv(a.n, bi);
   a.tiles_j = (int32_t)cdiv(a.m, bj);
   GG_REQUIRE((int64_t)a.tiles_i * a.tiles_j <= kGridX * 4, "%lld x %d: too many tiles", (long long)a.n, a.m);
+  return GG_OK;
+}
+
+template <typename O, int TJ, int TI>
+int launch_few(ProductArgs& a, hipStream_t stream) {
+  const int rc = tiles_of(a, 16 * TJ, 16 * TI);
+  if (rc != GG_OK) return rc;
+  int waves = 1;
+  while (waves < kFewWaves && waves < a.kb) waves *= 2;
+  hipLaunchKernelGGL((k_product_few<O, TJ, TI>), dim3((unsigned)a.tiles_i * a.tiles_j),
+                     dim3(waves * kWave), 0, stream, a);
+  GG_LAUNCH_CHECK("k_product_few");
   return GG_OK;
 }
 
@@ -478,14 +519,22 @@ int launch_tile(ProductArgs& a, hipStream_t stream) {
 
 template <typename O>
 int launch_product(ProductArgs& a, hipStream_t stream) {
-  const bool direct = aligned16(a.a.p) && aligned16(a.b.p) && a.a.stride % 16 == 0 &&
-                      a.b.stride % 16 == 0 && std::max(a.a.stride, a.b.stride) <= 1 << 23;
-  if (a.n <= 16 || (a.n <= 128 && !direct)) {
+  // offsets in a tile are of 32 bits
+  const bool near = std::max({a.a.stride, a.b.stride, a.a.sstride}) <= 1 << 23;
+  const bool direct = near && aligned16(a.a.p) && aligned16(a.b.p) && a.a.stride % 16 == 0 &&
+                      a.b.stride % 16 == 0;
+  if (near && a.n <= 128) {
+    const bool many = a.m > 64 * 96;      // weights for a block on each CU all the same
     if (a.n <= 16) return launch_few<O, 1, 1>(a, stream);
-    return launch_few<O, 2, 8>(a, stream);
+    if (a.n <= 32) return launch_few<O, 2, 2>(a, stream);
+    if (a.n <= 48 || (a.n > 64 && a.n <= 96)) {
+      if (many && a.n > 64) return launch_few<O, 4, 3>(a, stream);
+      return launch_few<O, 2, 3>(a, stream);
+    }
+    if (many && a.n > 64) return launch_few<O, 4, 4>(a, stream);
+    return launch_few<O, 2, 4>(a, stream);
   }
   if (!direct) return launch_tile<O, 128, 128, 2, 2>(a, stream);
-  if (a.n <= 128) return launch_pipe<O, 32, 128, 1, 4, 7>(a, stream);
   if constexpr (sizeof(O) == 2)
     if (cdiv(a.n, 256) * cdiv(a.m, 256) >= 192)
       return launch_pipe<O, 256, 256, 2, 4, 2>(a, stream);
