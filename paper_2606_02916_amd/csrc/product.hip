@@ -2,17 +2,12 @@
 //   out[i][j] = sum_g sa[i][g] sb[j / 128][g] sum_{k in block g} a[i][k] b[j][k],
 // codes multiplied by matrix instructions over a block of 128, each block's sum scaled
 // and added in fp32.
-#include <type_traits>
-
-#include "codes.hpp"
+#include "product.hpp"
 
 namespace gg {
 namespace {
 
 typedef int v8i __attribute__((ext_vector_type(8)));
-typedef float v4f __attribute__((ext_vector_type(4)));
-typedef bf16 v2bf __attribute__((ext_vector_type(2)));
-typedef bf16 v8bf __attribute__((ext_vector_type(8)));
 
 constexpr int32_t kBlockK = kScaleBlock;   // bytes of a row in a step
 
@@ -85,21 +80,6 @@ __device__ __forceinline__ void store_four(const KRows& out, int64_t i, int32_t 
   }
 }
 
-// A tile's place: each of the 8 XCDs, which take blocks in turn, has a run of tiles,
-// and in it bands of kBand tiles of rows, so that the blocks on one L2 at a time share
-// rows and weights.
-constexpr int32_t kXcds = 8, kBand = 4;
-
-__device__ __forceinline__ void tile_place(const ProductArgs& a, int32_t* ti, int32_t* tj) {
-  const uint32_t total = gridDim.x, b = blockIdx.x, x = b % kXcds, q = total / kXcds,
-                 r = total % kXcds;
-  const uint32_t t = x * q + min(x, r) + b / kXcds;
-  const uint32_t width = kBand * a.tiles_j, band = t / width, first = band * kBand,
-                 rows = min((uint32_t)a.tiles_i - first, (uint32_t)kBand), at = t - band * width;
-  *ti = (int32_t)(first + at % rows);
-  *tj = (int32_t)(at / rows);
-}
-
 // A lane's codes of a row in LDS: its pieces 2 q and 2 q + 1, q = l / 16, where rows keep
 // piece c in place c ^ (row / 2 & 7).  Rows 16 apart are alike.
 template <typename C>
@@ -155,22 +135,6 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, int64_t i0, int
   }
 }
 
-// A wave's 64 lanes' pieces of 16 bytes, or words, from base + off to consecutive places of LDS
-// at byte `to`.  Written out, since before the next read of LDS the compiler waits for all such
-// loads that it knows of; these are waited for by their number.  They write no register.
-__device__ __forceinline__ void load_to_lds16(const char* base, uint32_t off, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off),
-               "s"(base)
-               : "memory");
-}
-__device__ __forceinline__ void load_to_lds4(const char* p, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(p)
-               : "memory");
-}
-__device__ __forceinline__ uint32_t lds_at(const void* p) {
-  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p;
-}
-
 // A tile of BJ weights' rows by BI rows of a, blocks of 128 bytes of k at a time
 // through LDS.  A row of a block is eight pieces of 16 bytes; row r has piece c in place c
 // ^ (r / 2 & 7), so that sixteen lanes that read the same piece of sixteen rows meet all
@@ -179,27 +143,31 @@ __device__ __forceinline__ uint32_t lds_at(const void* p) {
 // row's scale to apply and four neighbours to store.
 //
 // Both matrices lie on 16-byte boundaries: pieces go from memory to LDS without a register
-// between, STAGES - 1 blocks ahead, and the scales with them, so that the wait for a block
-// can count the loads behind it.  A block at k's end that is not whole comes
-// through registers, with zeros behind the end.
-template <typename O, int BJ, int BI, int WJ, int WI, int STAGES>
-__global__ void __launch_bounds__(WJ* WI* kWave, 2) k_product_pipe(ProductArgs a) {
-  constexpr int kThreads = WJ * WI * kWave, kPieces = (BJ + BI) * 8, kLoads = kPieces / kThreads,
-                kBlocksJ = (BJ + kScaleBlock - 1) / kScaleBlock;
+// between, STAGES - 1 steps ahead, and the scales with them, so that the wait for a step
+// can count the loads behind it.  A step has WK blocks of k, each for WJ x WI waves, whose
+// sums are added at the end: few rows' steps are short, and so there are half as
+// many.  A step at k's end that is not whole comes through registers, with zeros
+// behind the end.
+template <typename O, int BJ, int BI, int WJ, int WI, int WK, int STAGES>
+__global__ void __launch_bounds__(WJ* WI* WK* kWave, 2) k_product_pipe(ProductArgs a) {
+  constexpr int kThreads = WJ * WI * WK * kWave, kGroup = kThreads / WK, kPieces = (BJ + BI) * 8,
+                kLoads = kPieces * WK / kThreads, kBlocksJ = (BJ + kScaleBlock - 1) / kScaleBlock;
   constexpr int TJ = BJ / WJ / 16, TI = BI / WI / 16;
-  static_assert(kPieces % kThreads == 0 && kThreads % 8 == 0, "whole loads");
+  static_assert(kPieces % kGroup == 0, "whole loads");
   static_assert(BJ / WJ <= kScaleBlock && kScaleBlock % (BJ / WJ) == 0, "one block of weights a wave");
-  static_assert(BI + kBlocksJ <= kThreads, "a lane for each scale");
+  static_assert(BI + kBlocksJ <= kGroup, "a lane for each scale");
   constexpr int kBehind = (kLoads + 1) * (STAGES - 2);   // loads that may be under way
   static_assert(kBehind < 64, "the counter of loads");
   typedef Codes<sizeof(O) == 4> C;
-  __shared__ v4i lds[STAGES][kPieces];
+  __shared__ v4i lds[STAGES][WK][kPieces];
   __shared__ float scales[STAGES][kThreads];
-  const int32_t tid = (int32_t)threadIdx.x, l = lane_id(),
-                wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int32_t l = lane_id(),
+                wave_all = __builtin_amdgcn_readfirstlane((int32_t)threadIdx.x / kWave);
+  // a group of waves brings its own block of a step and multiplies it
+  const int32_t wk = wave_all / (WJ * WI), wave = wave_all % (WJ * WI), tid = wave * kWave + l;
   const int32_t wj = wave % WJ, wi = wave / WJ;
   int32_t ti0, tj0;
-  tile_place(a, &ti0, &tj0);
+  tile_place(a.tiles_i, a.tiles_j, &ti0, &tj0);
   const int64_t i0 = (int64_t)ti0 * BI;
   const int32_t j0 = tj0 * BJ;
 
@@ -208,7 +176,7 @@ __global__ void __launch_bounds__(WJ* WI* kWave, 2) k_product_pipe(ProductArgs a
   const char* const ibase = a.a.p + i0 * a.a.stride;
   const int32_t jlast = min(a.m - j0, BJ) - 1, ilast = (int32_t)min(a.n - i0, (int64_t)BI) - 1;
   const auto row_of = [&](int t, int64_t* off) {
-    const int32_t r = (t * kThreads + tid) / 8;
+    const int32_t r = (t * kGroup + tid) / 8;
     *off = r < BJ ? min(r, jlast) * a.b.stride : min(r - BJ, ilast) * a.a.stride;
     return r;
   };
@@ -229,49 +197,73 @@ __global__ void __launch_bounds__(WJ* WI* kWave, 2) k_product_pipe(ProductArgs a
                                   kScaleBlock * a.b.sstride;
     scale_step = 4;
   }
-  const int32_t whole = a.k / kBlockK;
-  const auto bring = [&](int32_t g, int slot) {
-    if (g < whole) {
+  const int32_t whole = a.k / (kBlockK * WK), steps = (a.kb + WK - 1) / WK;
+  const auto bring = [&](int32_t s, int slot) {
+    const int32_t g = s * WK + wk;
+    v4i* const to = lds[slot][wk];
+    if (s < whole) {
       const char *jp = jbase + (int64_t)g * kBlockK, *ip = ibase + (int64_t)g * kBlockK;
 #pragma unroll
       for (int t = 0; t < kLoads; ++t) {
         // (a load's 64 lanes are of one matrix: BJ is a multiple of 8)
-        const bool weights = (t * kThreads + wave * kWave) / 8 < BJ;
-        load_to_lds16(weights ? jp : ip, from[t], lds_at(&lds[slot][t * kThreads + wave * kWave]));
+        const bool weights = (t * kGroup + wave * kWave) / 8 < BJ;
+        load_to_lds16(weights ? jp : ip, from[t], lds_at(to + t * kGroup + wave * kWave));
       }
     } else {
 #pragma unroll 1
       for (int t = 0; t < kLoads; ++t) {
         int64_t off;
         const int32_t r = row_of(t, &off);
-        lds[slot][t * kThreads + tid] = load_codes((r < BJ ? jbase : ibase) + off,
-                                                   g * kBlockK + (tid % 8 ^ (r >> 1 & 7)) * 16, a.k);
+        to[t * kGroup + tid] = load_codes((r < BJ ? jbase : ibase) + off,
+                                          g * kBlockK + (tid % 8 ^ (r >> 1 & 7)) * 16, a.k);
       }
     }
-    load_to_lds4(scale_from + (int64_t)g * scale_step, lds_at(&scales[slot][wave * kWave]));
+    load_to_lds4(scale_from + (int64_t)min(g, a.kb - 1) * scale_step,
+                 lds_at(&scales[slot][wave_all * kWave]));
   };
 
   v4f acc[TJ][TI] = {};
 #pragma unroll
-  for (int g = 0; g < STAGES - 1; ++g)
-    if (g < a.kb) bring(g, g);
+  for (int s = 0; s < STAGES - 1; ++s)
+    if (s < steps) bring(s, s);
   int slot = 0;
-  for (int32_t g = 0; g < a.kb; ++g) {
-    // block g is here, in all waves' parts, and block g - 1 has been read
-    if (g + STAGES - 2 < whole)
+  for (int32_t s = 0; s < steps; ++s) {
+    // step s is here, in all waves' parts, and step s - 1 has been read
+    if (s + STAGES - 2 < whole)
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kBehind) : "memory");
     else
       asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (g + STAGES - 1 < a.kb) bring(g + STAGES - 1, slot ? slot - 1 : STAGES - 1);
-    const float* sc = scales[slot];
-    const float sb = sc[BI + wj * TJ * 16 / kScaleBlock];
-    float scale[TI];
+    if (s + STAGES - 1 < steps) bring(s + STAGES - 1, slot ? slot - 1 : STAGES - 1);
+    if (WK == 1 || s * WK + wk < a.kb) {
+      const float* sc = scales[slot] + wk * kGroup;
+      const float sb = sc[BI + wj * TJ * 16 / kScaleBlock];
+      float scale[TI];
 #pragma unroll
-    for (int t = 0; t < TI; ++t) scale[t] = sc[(wi * TI + t) * 16 + l % 16] * sb;
-    const v4i *w = lds[slot] + (wj * TJ * 16 + l % 16) * 8, *r = lds[slot] + (BJ + wi * TI * 16 + l % 16) * 8;
-    multiply_step<TJ, TI, C>(scale, acc, [&](int x) { return operand<C>(w + x * 8, l); },
-                             [&](int x) { return operand<C>(r + x * 8, l); });
+      for (int t = 0; t < TI; ++t) scale[t] = sc[(wi * TI + t) * 16 + l % 16] * sb;
+      const v4i *w = lds[slot][wk] + (wj * TJ * 16 + l % 16) * 8,
+                *r = lds[slot][wk] + (BJ + wi * TI * 16 + l % 16) * 8;
+      multiply_step<TJ, TI, C>(scale, acc, [&](int x) { return operand<C>(w + x * 8, l); },
+                               [&](int x) { return operand<C>(r + x * 8, l); });
+    }
     slot = slot + 1 < STAGES ? slot + 1 : 0;
+  }
+  if constexpr (WK > 1) {
+    // the groups' sums, in order
+    typedef v4f Sums[TJ * TI][kWave];
+    static_assert(sizeof(Sums) * WJ * WI <= sizeof(lds), "room for a group's sums");
+    Sums* sums = (Sums*)&lds[0][0][0] + wave;
+#pragma unroll
+    for (int x = 1; x < WK; ++x) {
+      __syncthreads();
+      if (wk == x)
+#pragma unroll
+        for (int y = 0; y < TJ * TI; ++y) (*sums)[y][l] = acc[y / TI][y % TI];
+      __syncthreads();
+      if (wk == 0)
+#pragma unroll
+        for (int y = 0; y < TJ * TI; ++y) acc[y / TI][y % TI] += (*sums)[y][l];
+    }
+    if (wk) return;
   }
   store_tile<O, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc);
 }
@@ -289,7 +281,7 @@ __global__ void __launch_bounds__(WJ* WI* kWave, sizeof(O) == 4 ? 1 : 2) k_produ
                 wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int32_t wj = wave % WJ, wi = wave / WJ;
   int32_t ti0, tj0;
-  tile_place(a, &ti0, &tj0);
+  tile_place(a.tiles_i, a.tiles_j, &ti0, &tj0);
   const int64_t i0 = (int64_t)ti0 * BI;
   const int32_t j0 = tj0 * BJ;
 
@@ -365,7 +357,7 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) k_product_few(ProductArgs
                 wave = __builtin_amdgcn_readfirstlane((int32_t)threadIdx.x / kWave),
                 waves = (int32_t)blockDim.x / kWave;
   int32_t ti0, tj0;
-  tile_place(a, &ti0, &tj0);
+  tile_place(a.tiles_i, a.tiles_j, &ti0, &tj0);
   const int32_t j0 = tj0 * TJ * 16;
   const int64_t i0 = (int64_t)ti0 * TI * 16;
   // rows behind the last one repeat it
@@ -497,12 +489,12 @@ int launch_few(ProductArgs& a, hipStream_t stream) {
   return GG_OK;
 }
 
-template <typename O, int BJ, int BI, int WJ, int WI, int STAGES>
+template <typename O, int BJ, int BI, int WJ, int WI, int WK, int STAGES>
 int launch_pipe(ProductArgs& a, hipStream_t stream) {
   const int rc = tiles_of(a, BJ, BI);
   if (rc != GG_OK) return rc;
-  hipLaunchKernelGGL((k_product_pipe<O, BJ, BI, WJ, WI, STAGES>),
-                     dim3((unsigned)a.tiles_i * a.tiles_j), dim3(WJ * WI * kWave), 0, stream, a);
+  hipLaunchKernelGGL((k_product_pipe<O, BJ, BI, WJ, WI, WK, STAGES>),
+                     dim3((unsigned)a.tiles_i * a.tiles_j), dim3(WJ * WI * WK * kWave), 0, stream, a);
   GG_LAUNCH_CHECK("k_product_pipe");
   return GG_OK;
 }
@@ -524,21 +516,18 @@ int launch_product(ProductArgs& a, hipStream_t stream) {
   const bool direct = near && aligned16(a.a.p) && aligned16(a.b.p) && a.a.stride % 16 == 0 &&
                       a.b.stride % 16 == 0;
   if (near && a.n <= 128) {
-    const bool many = a.m > 64 * 96;      // weights for a block on each CU all the same
     if (a.n <= 16) return launch_few<O, 1, 1>(a, stream);
+    if (direct && a.n > 96) return launch_pipe<O, 32, 128, 1, 4, 2, 3>(a, stream);
+    if (direct && a.n > 64) return launch_pipe<O, 32, 96, 2, 2, 2, 3>(a, stream);
+    if (direct && a.n > 32) return launch_pipe<O, 32, 64, 1, 4, 2, 5>(a, stream);
     if (a.n <= 32) return launch_few<O, 2, 2>(a, stream);
-    if (a.n <= 48 || (a.n > 64 && a.n <= 96)) {
-      if (many && a.n > 64) return launch_few<O, 4, 3>(a, stream);
-      return launch_few<O, 2, 3>(a, stream);
-    }
-    if (many && a.n > 64) return launch_few<O, 4, 4>(a, stream);
     return launch_few<O, 2, 4>(a, stream);
   }
   if (!direct) return launch_tile<O, 128, 128, 2, 2>(a, stream);
   if constexpr (sizeof(O) == 2)
     if (cdiv(a.n, 256) * cdiv(a.m, 256) >= 192)
-      return launch_pipe<O, 256, 256, 2, 4, 2>(a, stream);
-  return launch_pipe<O, 128, 128, 2, 2, 2>(a, stream);
+      return launch_pipe<O, 256, 256, 2, 4, 1, 2>(a, stream);
+  return launch_pipe<O, 128, 128, 2, 2, 1, 2>(a, stream);
 }
 
 }  // namespace

@@ -1,16 +1,11 @@
 // The gradient of 8-bit weights from the 8-bit rows that the forward product took:
 //   dw[j][c] = sum_i dz[i][j] a[i][c],   a[i][c] = code[i][c] * scale[i][c / 128].
-#include <type_traits>
-
-#include "codes.hpp"
+#include "product.hpp"
 
 namespace gg {
 namespace {
 
 typedef short v4s __attribute__((ext_vector_type(4)));
-typedef float v4f __attribute__((ext_vector_type(4)));
-typedef bf16 v2bf __attribute__((ext_vector_type(2)));
-typedef bf16 v8bf __attribute__((ext_vector_type(8)));
 
 struct GradArgs {
   KRows a, dz, dw;
@@ -73,6 +68,187 @@ __device__ __forceinline__ void store_sums(const GradArgs& a, int32_t j, int32_t
       row_store<O, 1>(to + r * sizeof(O), one);
     }
   }
+}
+
+// A wave's sums into dw, or into its split's.
+template <typename O, int TK, int TJ>
+__device__ __forceinline__ void store_tile(const GradArgs& a, int32_t c0, int32_t j0, int32_t l,
+                                           const v4f (&acc)[TK][TJ]) {
+#pragma unroll
+  for (int t = 0; t < TJ; ++t) {
+    const int32_t j = j0 + t * 16 + l % 16;
+    if (j >= a.m) continue;
+#pragma unroll
+    for (int u = 0; u < TK; ++u) {
+      const int32_t c = c0 + u * 16 + l / 16 * 4;
+      if (c >= a.k) continue;
+      const float f[4] = {acc[u][t][0], acc[u][t][1], acc[u][t][2], acc[u][t][3]};
+      if (a.part) {
+        float* to = a.part + ((int64_t)blockIdx.y * a.m + j) * a.k + c;
+        if (c + 4 <= a.k) {
+          row_store<float, 4>((char*)to, f);
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            if (c + r < a.k) to[r] = f[r];
+        }
+      } else {
+        store_sums<O>(a, j, c, f);
+      }
+    }
+  }
+}
+
+// The transposing read: 16 lanes' four elements of 8 bytes, lanes 4 r .. 4 r + 3 at row r's
+// 16 columns; lane c of them gets column c of the four rows.
+__device__ __forceinline__ v4s read_across(const void* p) {
+  typedef __attribute__((address_space(3))) v4s* at;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)p);
+}
+
+__device__ __forceinline__ v8bf both(v4s lo, v4s hi) {
+  return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// bf16 gradients into bf16 weights' gradients: tiles of 256 columns of a by 256 of dz, 64
+// rows at a time.  The gradients go to LDS as they are, without a register between; codes
+// times their scales are rounded to bf16 on the way (2^-8 of a term at most, as the
+// result itself), which is a quarter of the matrix unit's time in other operations, where
+// scaled gradients, a version for each 128 columns, are more than all of it.  LDS holds
+// rows of 512 bytes, unit u of 32 bytes in place u ^ (row & 7), so that the eight rows
+// that half a wave reads across meet all banks.  Wave (wk, wj) has 128 x 64 of the tile.
+constexpr int32_t kWideK = 256, kWideJ = 256, kWideI = 64;
+
+__global__ void __launch_bounds__(512) k_product_grad_wide(GradArgs a) {
+  constexpr int TK = 8, TJ = 4, kRowBytes = 512;
+  __shared__ __attribute__((aligned(16))) char la[2][kWideI * kRowBytes], lz[2][kWideI * kRowBytes];
+  const int32_t tid = (int32_t)threadIdx.x, l = lane_id(),
+                wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int32_t wk = wave % 2, wj = wave / 2;
+  int32_t tk0, tj0;
+  tile_place(a.tiles_k, a.tiles_j, &tk0, &tj0);
+  const int32_t c0 = tk0 * kWideK, j0 = tj0 * kWideJ;
+  const int64_t first = blockIdx.y * a.chunk, end = min(a.n, first + a.chunk);
+
+  // Codes: 16 of a row, of two rows, a lane; a unit of LDS each.
+  const int32_t ra = tid / 16, ua = tid % 16, ca = c0 + ua * 16;
+  const int32_t scale_col = a.per_row || ca >= a.k ? 0 : ca / kScaleBlock * 4;
+  const char* code_at = a.a.p + (first + ra) * a.a.stride + ca;
+  const char* scale_at = a.a.scales + (first + ra) * a.a.sstride + scale_col;
+  const int64_t code_half = 32 * a.a.stride, scale_half = 32 * a.a.sstride;
+  v4i codes[2];
+  float scale[2];
+  // Gradients: a wave's load brings two rows, 16 bytes a lane; columns behind the last ones
+  // repeat them.
+  const char* zp = a.dz.p + (first + wave * 2) * a.dz.stride;
+  const int32_t uz = l % 32 / 2, hz = l % 2;
+  uint32_t z_off[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const int32_t r = t * 16 + wave * 2 + l / 32;
+    const int32_t j = min(j0 + ((uz ^ (r & 7)) * 2 + hz) * 8, a.m - 8);
+    z_off[t] = (uint32_t)(t * 16 + l / 32) * (uint32_t)a.dz.stride + (uint32_t)j * 2;
+  }
+  const auto put = [&](v4i code, float scale, int32_t r, int buf) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(code[i], false);
+      const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(code[i], true);
+      const v2bf p = {(bf16)(lo[0] * scale), (bf16)(lo[1] * scale)},
+                 q = {(bf16)(hi[0] * scale), (bf16)(hi[1] * scale)};
+      w[2 * i] = __builtin_bit_cast(uint32_t, p);
+      w[2 * i + 1] = __builtin_bit_cast(uint32_t, q);
+    }
+    v4i* to = (v4i*)&la[buf][r * kRowBytes + (ua ^ (r & 7)) * 32];
+    to[0] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
+    to[1] = v4i{(int)w[4], (int)w[5], (int)w[6], (int)w[7]};
+  };
+  // whole steps' codes wait in registers, others go to LDS at once
+  const auto plain = [&](int64_t i0) { return c0 + kWideK <= a.k && i0 + kWideI <= end; };
+  const auto fetch = [&](int64_t i0, int buf) {
+    if (plain(i0)) {
+      typedef v4i mem __attribute__((aligned(1)));
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        codes[t] = *(const GG_GLOBAL mem*)(code_at + t * code_half);
+        scale[t] = *(const GG_GLOBAL float*)(scale_at + t * scale_half);
+      }
+    } else {
+#pragma unroll 1
+      for (int t = 0; t < 2; ++t) {
+        v4i code = {};
+        float s = 0.0f;
+        if (i0 + t * 32 + ra < end) {
+          code = load_codes(code_at + t * code_half - ca, ca, a.k);
+          s = *(const GG_GLOBAL float*)(scale_at + t * scale_half);
+        }
+        put(code, s, t * 32 + ra, buf);
+      }
+    }
+    code_at += 2 * code_half;
+    scale_at += 2 * scale_half;
+  };
+  const auto keep = [&](int64_t i0, int buf) {
+    if (plain(i0))
+#pragma unroll
+      for (int t = 0; t < 2; ++t) put(codes[t], scale[t], t * 32 + ra, buf);
+  };
+  const auto bring = [&](int64_t i0, int buf) {
+    if (i0 + kWideI <= end) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        load_to_lds16(zp, z_off[t], lds_at(&lz[buf][(t * 16 + wave * 2) * kRowBytes]));
+    } else {
+#pragma unroll 1
+      for (int t = 0; t < 4; ++t) {
+        const int32_t r = t * 16 + wave * 2 + l / 32;
+        const int32_t j = min(j0 + ((uz ^ (r & 7)) * 2 + hz) * 8, a.m - 8);
+        v4i v = {};
+        if (i0 + r < end) v = *(const GG_GLOBAL v4i*)(a.dz.p + (i0 + r) * a.dz.stride + j * 2LL);
+        *(v4i*)&lz[buf][(t * 16 + wave * 2) * kRowBytes + l * 16] = v;
+      }
+    }
+    zp += kWideI * a.dz.stride;
+  };
+  // A unit's 16 columns of rows 4 q .. 4 q + 3 for lanes 16 q .. 16 q + 15 and of the rows 16
+  // behind them.
+  const int32_t tr = l % 16 / 4 + l / 16 * 4;
+  const auto operand = [&](const char* rows, int32_t unit) {
+    const char* p = rows + tr * kRowBytes + ((unit ^ (tr & 7)) * 32 + l % 4 * 8);
+    return both(read_across(p), read_across(p + 16 * kRowBytes));
+  };
+  v4f acc[TK][TJ] = {};
+  if (first < end) {
+    fetch(first, 0);
+    bring(first, 0);
+    keep(first, 0);
+  }
+  int buf = 0;
+  for (int64_t i0 = first; i0 < end; i0 += kWideI, buf ^= 1) {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const bool more = i0 + kWideI < end;
+    if (more) {
+      fetch(i0 + kWideI, buf ^ 1);
+      bring(i0 + kWideI, buf ^ 1);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const char *pa = la[buf] + h * 32 * kRowBytes, *pz = lz[buf] + h * 32 * kRowBytes;
+      v8bf x[TK];
+#pragma unroll
+      for (int u = 0; u < TK; ++u) x[u] = operand(pa, wk * TK + u);
+#pragma unroll
+      for (int t = 0; t < TJ; ++t) {
+        const v8bf z = operand(pz, wj * TJ + t);
+#pragma unroll
+        for (int u = 0; u < TK; ++u)
+          acc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[u], z, acc[u][t], 0, 0, 0);
+      }
+    }
+    if (more) keep(i0 + kWideI, buf ^ 1);
+  }
+  store_tile<bf16, TK, TJ>(a, c0 + wk * TK * 16, j0 + wj * TJ * 16, l, acc);
 }
 
 // A tile of 128 columns of a by BJ of dz, 32 rows at a time through LDS.  Both
@@ -154,10 +330,8 @@ __global__ void __launch_bounds__(kBlock) k_product_grad(GradArgs a) {
   // rows 4 q .. 4 q + 3 and 16 + them for lanes 16 q .. 16 q + 15, a column each
   const int32_t tr = l % 16 / 4 + l / 16 * 4, tc = l % 4 * 4;
   const auto operand = [&](const short* tile, int pitch, int32_t col) {
-    typedef __attribute__((address_space(3))) v4s* at;
-    const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(tile + tr * pitch + col + tc));
-    const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((at)(tile + (16 + tr) * pitch + col + tc));
-    return __builtin_bit_cast(v8bf, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    const short* p = tile + tr * pitch + col + tc;
+    return both(read_across(p), read_across(p + 16 * pitch));
   };
 
   v4f acc[TK][TJ] = {};
@@ -184,29 +358,7 @@ __global__ void __launch_bounds__(kBlock) k_product_grad(GradArgs a) {
       }
     if (more) keep(buf ^ 1);
   }
-#pragma unroll
-  for (int t = 0; t < TJ; ++t) {
-    const int32_t j = j0 + (wj * TJ + t) * 16 + l % 16;
-    if (j >= a.m) continue;
-#pragma unroll
-    for (int u = 0; u < TK; ++u) {
-      const int32_t c = c0 + (wk * TK + u) * 16 + l / 16 * 4;
-      if (c >= a.k) continue;
-      const float f[4] = {acc[u][t][0], acc[u][t][1], acc[u][t][2], acc[u][t][3]};
-      if (a.part) {
-        float* to = a.part + ((int64_t)blockIdx.y * a.m + j) * a.k + c;
-        if (c + 4 <= a.k) {
-          row_store<float, 4>((char*)to, f);
-        } else {
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (c + r < a.k) to[r] = f[r];
-        }
-      } else {
-        store_sums<O>(a, j, c, f);
-      }
-    }
-  }
+  store_tile<O, TK, TJ>(a, c0 + wk * TK * 16, j0 + wj * TJ * 16, l, acc);
 }
 
 // The splits' sums, in their order.
@@ -236,33 +388,42 @@ __global__ void __launch_bounds__(kBlock) k_product_join(GradArgs a) {
   store_sums<O>(a, j, c, f);
 }
 
-// How many splits of the rows: enough that blocks fill the chip's 256 CUs twice, of 256
-// rows at least.
-constexpr int64_t kGradBlocks = 512, kGradRows = 256;
+// How many splits of the rows: enough that blocks fill the chip's 256 CUs, twice where
+// two fit one, of some rows at least.
+struct GradShape {
+  int bj;
+  int64_t tiles_k, tiles_j, splits;
+};
 
-template <typename F>
-void grad_shape(int64_t n, int64_t k, int64_t m, F f) {
-  const int bj = m <= 64 ? 64 : 128;
-  const int64_t tiles = cdiv(k, kTileK) * cdiv(m, bj);
-  const int64_t splits = std::max<int64_t>(1, std::min(cdiv(kGradBlocks, tiles), cdiv(n, kGradRows)));
-  f(bj, tiles, splits);
+GradShape shape_of(int64_t n, int64_t k, int64_t m, bool wide) {
+  GradShape s;
+  s.bj = wide ? kWideJ : m <= 64 ? 64 : 128;
+  s.tiles_k = cdiv(k, wide ? kWideK : kTileK);
+  s.tiles_j = cdiv(m, s.bj);
+  const int64_t blocks = wide ? 256 : 512, rows = wide ? 512 : 256;
+  s.splits = std::max<int64_t>(1, std::min(blocks / (s.tiles_k * s.tiles_j), cdiv(n, rows)));
+  return s;
 }
 
 template <typename Z, typename O, int PARTS>
 int launch_grad(GradArgs& a, hipStream_t stream) {
-  int rc = GG_OK;
-  grad_shape(a.n, a.k, a.m, [&](int bj, int64_t tiles, int64_t splits) {
-    a.tiles_k = (int32_t)cdiv(a.k, kTileK);
-    a.tiles_j = (int32_t)cdiv(a.m, bj);
-    a.splits = (int32_t)splits;
-    a.chunk = align_up(cdiv(a.n, splits), kTileI);
-    if (splits == 1) a.part = nullptr;
-    const dim3 grid((unsigned)tiles, (unsigned)splits);
-    if (bj == 64)
-      hipLaunchKernelGGL((k_product_grad<Z, O, PARTS, 64>), grid, dim3(kBlock), 0, stream, a);
-    else
-      hipLaunchKernelGGL((k_product_grad<Z, O, PARTS, 128>), grid, dim3(kBlock), 0, stream, a);
-  });
+  // (the wide kernel moves whole pieces of 16 bytes of the gradients, with offsets of 32 bits)
+  const bool wide = std::is_same<Z, bf16>::value && std::is_same<O, bf16>::value && a.m % 8 == 0 &&
+                    a.m >= 128 && a.k >= 128 && a.n >= 128 && aligned16(a.dz.p) &&
+                    a.dz.stride % 16 == 0 && a.dz.stride <= 1 << 25;
+  const GradShape s = shape_of(a.n, a.k, a.m, wide);
+  a.tiles_k = (int32_t)s.tiles_k;
+  a.tiles_j = (int32_t)s.tiles_j;
+  a.splits = (int32_t)s.splits;
+  a.chunk = align_up(cdiv(a.n, s.splits), kWideI);
+  if (s.splits == 1) a.part = nullptr;
+  const dim3 grid((unsigned)(s.tiles_k * s.tiles_j), (unsigned)s.splits);
+  if (wide)
+    hipLaunchKernelGGL(k_product_grad_wide, grid, dim3(512), 0, stream, a);
+  else if (s.bj == 64)
+    hipLaunchKernelGGL((k_product_grad<Z, O, PARTS, 64>), grid, dim3(kBlock), 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_product_grad<Z, O, PARTS, 128>), grid, dim3(kBlock), 0, stream, a);
   GG_LAUNCH_CHECK("k_product_grad");
   if (a.part) {
     const int64_t lanes = a.m * cdiv(a.k, 4);
@@ -270,7 +431,7 @@ int launch_grad(GradArgs& a, hipStream_t stream) {
                        stream, a);
     GG_LAUNCH_CHECK("k_product_join");
   }
-  return rc;
+  return GG_OK;
 }
 
 }  // namespace
@@ -285,11 +446,8 @@ static bool grad_sizes(int64_t n, int64_t k, int64_t m) {
 
 extern "C" size_t gg_ws_product(int64_t n, int64_t k, int64_t m) {
   if (!grad_sizes(n, k, m)) return 0;
-  size_t bytes = 0;
-  grad_shape(n, k, m, [&](int, int64_t, int64_t splits) {
-    if (splits > 1) bytes = align_up((size_t)splits * m * k * sizeof(float), 256);
-  });
-  return bytes;
+  const int64_t splits = std::max(shape_of(n, k, m, false).splits, shape_of(n, k, m, true).splits);
+  return splits > 1 ? align_up((size_t)splits * m * k * sizeof(float), 256) : 0;
 }
 
 extern "C" int gg_product_backward(const gg_rows_t* a, int64_t n, int64_t k, const gg_rows_t* dz,

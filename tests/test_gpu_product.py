@@ -236,7 +236,8 @@ def test_weight_gradient(n, k, m):
 @pytest.mark.parametrize("tz,t", [(F32, F32), (F16, F16), (BF16, BF16), (F16, F32), (BF16, F32)])
 @pytest.mark.parametrize("group", [0, 128])
 @pytest.mark.parametrize("n,k,m", [(64, 128, 64), (128, 256, 512), (3000, 128, 40), (5000, 512, 256),
-                                   (1024, 1024, 1024), (520, 640, 2048), (40_001, 100, 47)])
+                                   (1024, 1024, 1024), (520, 640, 2048), (40_001, 100, 47), (130, 130, 136),
+                                   (2000, 700, 1000)])
 @pytest.mark.parametrize("add", [False, True])
 def test_weight_gradient_at_aligned_places(n, k, m, group, tz, t, add):
     check(*grad_case(n, k, m, tz, t, group, add, 0, 0), t)
