@@ -64,27 +64,29 @@ struct Quotient {
   }
 };
 
-// 16 bytes of a row's codes from column c on, zeros behind its end: there the row's
-// last 16 bytes are read and moved down.
 typedef int v4i __attribute__((ext_vector_type(4)));
 
+// 16 bytes moved down by 0 to 15 of them, zeros behind.
+__device__ __forceinline__ v4i move_down(v4i v, int32_t bytes) {
+  typedef uint64_t two __attribute__((ext_vector_type(2)));
+  const two w = __builtin_bit_cast(two, v);
+  const int32_t s = 8 * min(bytes, 15);
+  const uint64_t lo = s < 64 ? w[0] >> s | w[1] << 1 << (63 - s) : w[1] >> (s - 64),
+                 hi = s < 64 ? w[1] >> s : 0;
+  return v4i{(int)lo, (int)(lo >> 32), (int)hi, (int)(hi >> 32)};
+}
+
+// 16 bytes of a row's codes from column c on, zeros behind its end: there the row's
+// last 16 bytes are read and moved down.
 __device__ __forceinline__ v4i load_codes(const char* row, int32_t c, int32_t k) {
   typedef v4i mem __attribute__((aligned(1)));
   if (c + 16 <= k) return *(const GG_GLOBAL mem*)(row + c);
+  if (c >= k) return v4i{};
+  if (k >= 16) return move_down(*(const GG_GLOBAL mem*)(row + k - 16), c + 16 - k);
   uint64_t w[2] = {};
-  if (c < k) {
-    if (k >= 16) {
-      typedef uint64_t two __attribute__((ext_vector_type(2), aligned(1)));
-      const two v = *(const GG_GLOBAL two*)(row + k - 16);
-      const int32_t s = 8 * (c + 16 - k);            // bits of it that lie before c
-      w[0] = s < 64 ? v[0] >> s | v[1] << 1 << (63 - s) : v[1] >> (s - 64);
-      w[1] = s < 64 ? v[1] >> s : 0;
-    } else {
 #pragma unroll 1
-      for (int32_t i = 0; i < k; ++i)               // c is 0
-        w[i / 8] |= (uint64_t) * (const GG_GLOBAL uint8_t*)(row + i) << 8 * (i % 8);
-    }
-  }
+  for (int32_t i = 0; i < k; ++i)               // c is 0
+    w[i / 8] |= (uint64_t) * (const GG_GLOBAL uint8_t*)(row + i) << 8 * (i % 8);
   return v4i{(int)w[0], (int)(w[0] >> 32), (int)w[1], (int)(w[1] >> 32)};
 }
 

@@ -130,10 +130,13 @@ __global__ void __launch_bounds__(512) k_product_grad_wide(GradArgs a) {
   const int32_t c0 = tk0 * kWideK, j0 = tj0 * kWideJ;
   const int64_t first = blockIdx.y * a.chunk, end = min(a.n, first + a.chunk);
 
-  // Codes: 16 of a row, of two rows, a lane; a unit of LDS each.
-  const int32_t ra = tid / 16, ua = tid % 16, ca = c0 + ua * 16;
-  const int32_t scale_col = a.per_row || ca >= a.k ? 0 : ca / kScaleBlock * 4;
-  const char* code_at = a.a.p + (first + ra) * a.a.stride + ca;
+  // Codes: 16 of a row, of two rows, a lane; a unit of LDS each.  Columns behind the last
+  // ones may hold anything, they are columns of no result; the piece that holds the last
+  // one is read from 16 before the row's end and moved down.
+  const int32_t ra = tid / 16, ua = tid % 16, ca = c0 + ua * 16, cl = min(ca, a.k - 16);
+  const bool edge = c0 + kWideK > a.k;
+  const int32_t scale_col = a.per_row ? 0 : min(ca, a.k - 1) / kScaleBlock * 4;
+  const char* code_at = a.a.p + (first + ra) * a.a.stride + cl;
   const char* scale_at = a.a.scales + (first + ra) * a.a.sstride + scale_col;
   const int64_t code_half = 32 * a.a.stride, scale_half = 32 * a.a.sstride;
   v4i codes[2];
@@ -150,6 +153,7 @@ __global__ void __launch_bounds__(512) k_product_grad_wide(GradArgs a) {
     z_off[t] = (uint32_t)(t * 16 + l / 32) * (uint32_t)a.dz.stride + (uint32_t)j * 2;
   }
   const auto put = [&](v4i code, float scale, int32_t r, int buf) {
+    if (edge) code = move_down(code, ca - cl);
     uint32_t w[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -164,52 +168,42 @@ __global__ void __launch_bounds__(512) k_product_grad_wide(GradArgs a) {
     to[0] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
     to[1] = v4i{(int)w[4], (int)w[5], (int)w[6], (int)w[7]};
   };
-  // whole steps' codes wait in registers, others go to LDS at once
-  const auto plain = [&](int64_t i0) { return c0 + kWideK <= a.k && i0 + kWideI <= end; };
-  const auto fetch = [&](int64_t i0, int buf) {
-    if (plain(i0)) {
-      typedef v4i mem __attribute__((aligned(1)));
+  typedef v4i mem __attribute__((aligned(1)));
+  // a step of 64 rows: codes wait in registers
+  const auto fetch = [&](int buf) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        codes[t] = *(const GG_GLOBAL mem*)(code_at + t * code_half);
-        scale[t] = *(const GG_GLOBAL float*)(scale_at + t * scale_half);
-      }
-    } else {
-#pragma unroll 1
-      for (int t = 0; t < 2; ++t) {
-        v4i code = {};
-        float s = 0.0f;
-        if (i0 + t * 32 + ra < end) {
-          code = load_codes(code_at + t * code_half - ca, ca, a.k);
-          s = *(const GG_GLOBAL float*)(scale_at + t * scale_half);
-        }
-        put(code, s, t * 32 + ra, buf);
-      }
+    for (int t = 0; t < 2; ++t) {
+      codes[t] = *(const GG_GLOBAL mem*)(code_at + t * code_half);
+      scale[t] = *(const GG_GLOBAL float*)(scale_at + t * scale_half);
     }
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      load_to_lds16(zp, z_off[t], lds_at(&lz[buf][(t * 16 + wave * 2) * kRowBytes]));
     code_at += 2 * code_half;
     scale_at += 2 * scale_half;
-  };
-  const auto keep = [&](int64_t i0, int buf) {
-    if (plain(i0))
-#pragma unroll
-      for (int t = 0; t < 2; ++t) put(codes[t], scale[t], t * 32 + ra, buf);
-  };
-  const auto bring = [&](int64_t i0, int buf) {
-    if (i0 + kWideI <= end) {
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-        load_to_lds16(zp, z_off[t], lds_at(&lz[buf][(t * 16 + wave * 2) * kRowBytes]));
-    } else {
-#pragma unroll 1
-      for (int t = 0; t < 4; ++t) {
-        const int32_t r = t * 16 + wave * 2 + l / 32;
-        const int32_t j = min(j0 + ((uz ^ (r & 7)) * 2 + hz) * 8, a.m - 8);
-        v4i v = {};
-        if (i0 + r < end) v = *(const GG_GLOBAL v4i*)(a.dz.p + (i0 + r) * a.dz.stride + j * 2LL);
-        *(v4i*)&lz[buf][(t * 16 + wave * 2) * kRowBytes + l * 16] = v;
-      }
-    }
     zp += kWideI * a.dz.stride;
+  };
+  const auto keep = [&](int buf) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) put(codes[t], scale[t], t * 32 + ra, buf);
+  };
+  // fewer rows, with zeros behind them
+  const auto fetch_last = [&](int32_t rows, int buf) {
+#pragma unroll 1
+    for (int t = 0; t < 2; ++t) {
+      const bool here = t * 32 + ra < rows;
+      v4i code = {};
+      if (here) code = *(const GG_GLOBAL mem*)(code_at + t * code_half);
+      put(code, here ? *(const GG_GLOBAL float*)(scale_at + t * scale_half) : 0.0f, t * 32 + ra, buf);
+    }
+#pragma unroll 1
+    for (int t = 0; t < 4; ++t) {
+      const int32_t r = t * 16 + wave * 2 + l / 32;
+      const int32_t j = min(j0 + ((uz ^ (r & 7)) * 2 + hz) * 8, a.m - 8);
+      v4i v = {};
+      if (r < rows) v = *(const GG_GLOBAL v4i*)(zp + (t * 16 + l / 32) * a.dz.stride + j * 2LL);
+      *(v4i*)&lz[buf][(t * 16 + wave * 2) * kRowBytes + l * 16] = v;
+    }
   };
   // A unit's 16 columns of rows 4 q .. 4 q + 3 for lanes 16 q .. 16 q + 15 and of the rows 16
   // behind them.
@@ -219,19 +213,7 @@ __global__ void __launch_bounds__(512) k_product_grad_wide(GradArgs a) {
     return both(read_across(p), read_across(p + 16 * kRowBytes));
   };
   v4f acc[TK][TJ] = {};
-  if (first < end) {
-    fetch(first, 0);
-    bring(first, 0);
-    keep(first, 0);
-  }
-  int buf = 0;
-  for (int64_t i0 = first; i0 < end; i0 += kWideI, buf ^= 1) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    const bool more = i0 + kWideI < end;
-    if (more) {
-      fetch(i0 + kWideI, buf ^ 1);
-      bring(i0 + kWideI, buf ^ 1);
-    }
+  const auto add = [&](int buf) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const char *pa = la[buf] + h * 32 * kRowBytes, *pz = lz[buf] + h * 32 * kRowBytes;
@@ -246,7 +228,29 @@ __global__ void __launch_bounds__(512) k_product_grad_wide(GradArgs a) {
           acc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[u], z, acc[u][t], 0, 0, 0);
       }
     }
-    if (more) keep(i0 + kWideI, buf ^ 1);
+  };
+  const auto wait = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  const int64_t rows = max(end - first, (int64_t)0);
+  const int32_t steps = (int32_t)(rows / kWideI), rest = (int32_t)(rows % kWideI);
+  int buf = 0;
+  if (steps) {
+    fetch(0);
+    keep(0);
+    for (int32_t s = 1; s < steps; ++s) {
+      wait();
+      fetch(buf ^ 1);
+      add(buf);
+      keep(buf ^ 1);
+      buf ^= 1;
+    }
+    wait();
+    add(buf);
+    buf ^= 1;
+  }
+  if (rest) {
+    fetch_last(rest, buf);
+    wait();
+    add(buf);
   }
   store_tile<bf16, TK, TJ>(a, c0 + wk * TK * 16, j0 + wj * TJ * 16, l, acc);
 }
