@@ -169,23 +169,23 @@ __global__ void __launch_bounds__(512) k_product_grad_wide(GradArgs a) {
     to[1] = v4i{(int)w[4], (int)w[5], (int)w[6], (int)w[7]};
   };
   typedef v4i mem __attribute__((aligned(1)));
-  // a step of 64 rows: codes wait in registers
-  const auto fetch = [&](int buf) {
+  // a step of 64 rows: gradients to LDS, codes to registers
+  const auto bring = [&](int buf) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      load_to_lds16(zp, z_off[t], lds_at(&lz[buf][(t * 16 + wave * 2) * kRowBytes]));
+    zp += kWideI * a.dz.stride;
+  };
+  const auto fetch = [&] {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       codes[t] = *(const GG_GLOBAL mem*)(code_at + t * code_half);
       scale[t] = *(const GG_GLOBAL float*)(scale_at + t * scale_half);
     }
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-      load_to_lds16(zp, z_off[t], lds_at(&lz[buf][(t * 16 + wave * 2) * kRowBytes]));
+  };
+  const auto next_codes = [&] {
     code_at += 2 * code_half;
     scale_at += 2 * scale_half;
-    zp += kWideI * a.dz.stride;
-  };
-  const auto keep = [&](int buf) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) put(codes[t], scale[t], t * 32 + ra, buf);
   };
   // fewer rows, with zeros behind them
   const auto fetch_last = [&](int32_t rows, int buf) {
@@ -213,44 +213,59 @@ __global__ void __launch_bounds__(512) k_product_grad_wide(GradArgs a) {
     return both(read_across(p), read_across(p + 16 * kRowBytes));
   };
   v4f acc[TK][TJ] = {};
-  const auto add = [&](int buf) {
+  // A step's products; `more`: the next step's codes, which are in registers, go to LDS
+  // meanwhile, and those after it are read.  In this order: the operand of the next products
+  // before these, and other operations between products.
+  const auto add = [&](int buf, bool more, auto then) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const char *pa = la[buf] + h * 32 * kRowBytes, *pz = lz[buf] + h * 32 * kRowBytes;
-      v8bf x[TK];
+      v8bf x[TK], z[2];
+      z[0] = operand(pz, wj * TJ);
 #pragma unroll
       for (int u = 0; u < TK; ++u) x[u] = operand(pa, wk * TK + u);
 #pragma unroll
       for (int t = 0; t < TJ; ++t) {
-        const v8bf z = operand(pz, wj * TJ + t);
+        if (t + 1 < TJ) z[t + 1 & 1] = operand(pz, wj * TJ + t + 1);
 #pragma unroll
         for (int u = 0; u < TK; ++u)
-          acc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[u], z, acc[u][t], 0, 0, 0);
+          acc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[u], z[t & 1], acc[u][t], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+        if (h == 0 && more && t < 2) put(codes[t], scale[t], t * 32 + ra, buf ^ 1);
+        if (h == 0 && more && t == 2) then();
       }
     }
   };
-  const auto wait = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  const auto nothing = [] {};
   const int64_t rows = max(end - first, (int64_t)0);
   const int32_t steps = (int32_t)(rows / kWideI), rest = (int32_t)(rows % kWideI);
   int buf = 0;
   if (steps) {
-    fetch(0);
-    keep(0);
+    bring(0);
+    fetch();
+    next_codes();
+#pragma unroll
+    for (int t = 0; t < 2; ++t) put(codes[t], scale[t], t * 32 + ra, 0);
+    if (steps > 1) fetch();
     for (int32_t s = 1; s < steps; ++s) {
-      wait();
-      fetch(buf ^ 1);
-      add(buf);
-      keep(buf ^ 1);
+      // the gradients are there; the four loads behind them, of codes, may be under way
+      asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+      add(buf, true, [&] {
+        // (behind the codes' use: the compiler's wait for them would be one for these too)
+        bring(buf ^ 1);
+        next_codes();
+        if (s + 1 < steps) fetch();
+      });
       buf ^= 1;
     }
-    wait();
-    add(buf);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    add(buf, false, nothing);
     buf ^= 1;
   }
   if (rest) {
     fetch_last(rest, buf);
-    wait();
-    add(buf);
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    add(buf, false, nothing);
   }
   store_tile<bf16, TK, TJ>(a, c0 + wk * TK * 16, j0 + wj * TJ * 16, l, acc);
 }
