@@ -27,23 +27,25 @@ constexpr int32_t kTileI = 32;             // rows of a step
 // Infinities and NaNs are whole in the first part.
 template <int PARTS>
 __device__ __forceinline__ void split(float x, float y, uint32_t (&p)[PARTS]) {
+  const auto rounded = [](float a, float b) {
+    const v2bf v = {(bf16)a, (bf16)b};
+    return __builtin_bit_cast(uint32_t, v);
+  };
+  const auto upper = [](float a, float b) {
+    return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);
+  };
+  const auto lower = [](float a) { return a - __uint_as_float(__float_as_uint(a) & 0xffff0000u); };
   if constexpr (PARTS == 1) {
-    const v2bf v = {(bf16)x, (bf16)y};
-    p[0] = __builtin_bit_cast(uint32_t, v);
+    p[0] = rounded(x, y);
   } else {
-#pragma unroll
-    for (int i = 0; i < PARTS; ++i) {
-      const uint32_t a = __float_as_uint(x), b = __float_as_uint(y);
-      if (i + 1 == PARTS && PARTS == 2) {
-        const v2bf v = {(bf16)x, (bf16)y};
-        p[i] = __builtin_bit_cast(uint32_t, v);
-      } else {
-        p[i] = __builtin_amdgcn_perm(b, a, 0x07060302);   // the upper halves
-      }
-      if (i + 1 < PARTS) {
-        x = __builtin_isfinite(x) ? x - __uint_as_float(a & 0xffff0000u) : 0.0f;
-        y = __builtin_isfinite(y) ? y - __uint_as_float(b & 0xffff0000u) : 0.0f;
-      }
+    p[0] = upper(x, y);
+    x = __builtin_isfinite(x) ? lower(x) : 0.0f;
+    y = __builtin_isfinite(y) ? lower(y) : 0.0f;
+    if constexpr (PARTS == 2) {
+      p[1] = rounded(x, y);
+    } else {
+      p[1] = upper(x, y);
+      p[2] = upper(lower(x), lower(y));
     }
   }
 }
@@ -270,14 +272,18 @@ __global__ void __launch_bounds__(512) k_product_grad_wide(GradArgs a) {
   store_tile<bf16, TK, TJ>(a, c0 + wk * TK * 16, j0 + wj * TJ * 16, l, acc);
 }
 
-// A tile of 128 columns of a by BJ of dz, 32 rows at a time through LDS.  Both
-// operands of the MFMA run along the rows, which lie across both matrices: LDS keeps
-// them as they come, and the transposing reads hand a lane four rows' elements of its
-// column.  A row of the tile is 32 bytes longer than its elements, so that the 4 x 32
+// Every other gradient: a tile of 128 columns of a by BJ of dz, 32 rows at a time through
+// LDS.  Both operands of the MFMA run along the rows, which lie across both matrices: LDS
+// keeps them as they come, and the transposing reads hand a lane four rows' elements of
+// its column.  A row of the tile is 32 bytes longer than its elements, so that the 4 x 32
 // bytes of such a read meet different banks.  Codes are turned into bf16 and gradients
-// scaled and split once, on the way into LDS.  Wave (wk, wj) has 64 x BJ/2 of the tile.
-template <typename Z, typename O, int PARTS, int BJ>
-__global__ void __launch_bounds__(kBlock) k_product_grad(GradArgs a) {
+// scaled and split once, on the way into LDS, two steps after they were asked for.
+// Wave (wk, wj) has 64 x BJ/2 of the tile.  Columns behind the last ones may hold anything,
+// they are columns of no result; the piece that holds the last one is read from its own
+// length before the row's end and moved down, but with TINY, for rows shorter than a
+// piece, which are read by elements.
+template <typename Z, typename O, int PARTS, int BJ, bool TINY>
+__global__ void __launch_bounds__(kBlock, 2) k_product_grad(GradArgs a) {
   constexpr int TK = 4, TJ = BJ / 32, V = kVec<Z>;
   constexpr int kPitchA = kTileK + 16, kPitchZ = BJ + 16;
   constexpr int kLanesZ = BJ / V, kStepZ = kBlock / kLanesZ, kLoadsZ = kTileI / kStepZ;
@@ -292,34 +298,52 @@ __global__ void __launch_bounds__(kBlock) k_product_grad(GradArgs a) {
   const int64_t first = blockIdx.y * a.chunk, end = min(a.n, first + a.chunk);
 
   // a step's loads: 16 codes a lane, and kLoadsZ pieces of gradients with their rows' scales
-  const int32_t ra = tid / 8, ca = tid % 8 * 16, rz = tid / kLanesZ, cz = tid % kLanesZ * V;
-  const int64_t scale_at = a.per_row ? 0 : c0 / kScaleBlock * 4LL;
-  v4i codes;
-  typename Raw<Z, V>::vec raw[kLoadsZ];
-  float scale[kLoadsZ];
-  const auto fetch = [&](int64_t i0) {
-    codes = {};
-    if (i0 + ra < end) codes = load_codes(a.a.p + (i0 + ra) * a.a.stride, c0 + ca, a.k);
+  typedef v4i mem __attribute__((aligned(1)));
+  const int32_t ra = tid / 8, ca = c0 + tid % 8 * 16, rz = tid / kLanesZ, cz = j0 + tid % kLanesZ * V;
+  const int32_t cl = TINY ? ca : min(ca, a.k - 16), zl = TINY ? cz : min(cz, a.m - V);
+  const bool edge_a = c0 + kTileK > a.k, edge_z = j0 + BJ > a.m;
+  const char* code_at = a.a.p + (first + ra) * a.a.stride + cl;
+  const char* z_at = a.dz.p + (first + rz) * a.dz.stride + zl * (int64_t)sizeof(Z);
+  const char* scale_at =
+      a.a.scales + (first + rz) * a.a.sstride + (a.per_row ? 0 : c0 / kScaleBlock * 4LL);
+  struct Step {
+    v4i codes, z[kLoadsZ];
+    float scale[kLoadsZ];
+  };
+  // `rows`: as many of the step's are there (all of them but for a last step); then on by
+  // `by` rows
+  const auto fetch = [&](Step& s, auto whole, int32_t rows, int32_t by) {
+    const bool here = whole || ra < rows;
+    s.codes = {};
+    if constexpr (TINY) {
+      if (here) s.codes = load_codes(code_at - cl, cl, a.k);
+    } else if (here) {
+      s.codes = *(const GG_GLOBAL mem*)code_at;
+    }
 #pragma unroll
     for (int t = 0; t < kLoadsZ; ++t) {
-      const int64_t i = i0 + t * kStepZ + rz;
-      raw[t] = {};
-      scale[t] = 0.0f;
-      if (i < end) {
-        const char* row = a.dz.p + i * a.dz.stride;
-        const int32_t j = j0 + cz;
-        scale[t] = *(const GG_GLOBAL float*)(a.a.scales + i * a.a.sstride + scale_at);
-        if (j + V <= a.m) {
-          raw[t] = raw_load<Z, V>(row + j * (int64_t)sizeof(Z));
-        } else {
+      s.z[t] = {};
+      s.scale[t] = 0.0f;
+      const char* p = z_at + t * kStepZ * a.dz.stride;
+      if (whole || t * kStepZ + rz < rows) {
+        s.scale[t] = *(const GG_GLOBAL float*)(scale_at + t * kStepZ * a.a.sstride);
+        if constexpr (TINY) {
+          typename Raw<Z, V>::vec v = {};
 #pragma unroll
           for (int x = 0; x < V; ++x)
-            if (j + x < a.m) raw[t][x] = raw_load<Z, 1>(row + (j + x) * (int64_t)sizeof(Z));
+            if (cz + x < a.m) v[x] = raw_load<Z, 1>(p + x * sizeof(Z));
+          s.z[t] = __builtin_bit_cast(v4i, v);
+        } else {
+          s.z[t] = *(const GG_GLOBAL mem*)p;
         }
       }
     }
+    code_at += by * a.a.stride;
+    z_at += by * a.dz.stride;
+    scale_at += by * a.a.sstride;
   };
-  const auto keep = [&](int buf) {
+  const auto keep = [&](const Step& s, int buf) {
+    const v4i codes = !TINY && edge_a ? move_down(s.codes, ca - cl) : s.codes;
     uint32_t w[8];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -328,19 +352,21 @@ __global__ void __launch_bounds__(kBlock) k_product_grad(GradArgs a) {
       w[2 * i + 1] = __builtin_bit_cast(
           uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)codes[i], 1.0f, true));
     }
-    v4i* to = (v4i*)&la[buf][ra * kPitchA + ca];
+    v4i* to = (v4i*)&la[buf][ra * kPitchA + (ca - c0)];
     to[0] = v4i{(int)w[0], (int)w[1], (int)w[2], (int)w[3]};
     to[1] = v4i{(int)w[4], (int)w[5], (int)w[6], (int)w[7]};
 #pragma unroll
     for (int t = 0; t < kLoadsZ; ++t) {
+      const v4i z = !TINY && edge_z ? move_down(s.z[t], (cz - zl) * (int32_t)sizeof(Z)) : s.z[t];
       float v[V];
-      to_f32<Z, V>(raw[t], v);
+      to_f32<Z, V>(__builtin_bit_cast(typename Raw<Z, V>::vec, z), v);
       uint32_t p[V / 2][PARTS];
 #pragma unroll
-      for (int x = 0; x < V / 2; ++x) split<PARTS>(v[2 * x] * scale[t], v[2 * x + 1] * scale[t], p[x]);
+      for (int x = 0; x < V / 2; ++x)
+        split<PARTS>(v[2 * x] * s.scale[t], v[2 * x + 1] * s.scale[t], p[x]);
 #pragma unroll
       for (int q = 0; q < PARTS; ++q) {
-        uint32_t* at = (uint32_t*)&lz[buf][q][(t * kStepZ + rz) * kPitchZ + cz];
+        uint32_t* at = (uint32_t*)&lz[buf][q][(t * kStepZ + rz) * kPitchZ + (cz - j0)];
 #pragma unroll
         for (int x = 0; x < V / 2; ++x) at[x] = p[x][q];
       }
@@ -352,17 +378,8 @@ __global__ void __launch_bounds__(kBlock) k_product_grad(GradArgs a) {
     const short* p = tile + tr * pitch + col + tc;
     return both(read_across(p), read_across(p + 16 * pitch));
   };
-
   v4f acc[TK][TJ] = {};
-  if (first < end) {
-    fetch(first);
-    keep(0);
-  }
-  int buf = 0;
-  for (int64_t i0 = first; i0 < end; i0 += kTileI, buf ^= 1) {
-    __syncthreads();
-    const bool more = i0 + kTileI < end;
-    if (more) fetch(i0 + kTileI);
+  const auto add = [&](int buf) {
     v8bf x[TK];
 #pragma unroll
     for (int u = 0; u < TK; ++u) x[u] = operand(la[buf], kPitchA, (wk * TK + u) * 16);
@@ -375,36 +392,84 @@ __global__ void __launch_bounds__(kBlock) k_product_grad(GradArgs a) {
         for (int u = 0; u < TK; ++u)
           acc[u][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[u], z, acc[u][t], 0, 0, 0);
       }
-    if (more) keep(buf ^ 1);
+  };
+  const int64_t rows = max(end - first, (int64_t)0);
+  const int32_t steps = (int32_t)(rows / kTileI), rest = (int32_t)(rows % kTileI);
+  const std::true_type whole;
+  Step s[2];
+  int32_t i = 0;
+  // step i's rows are in LDS and step i + 1's on their way; behind the last whole step its
+  // rows are read again
+  const auto step = [&](Step& now, const Step& next) {
+    __syncthreads();
+    fetch(now, whole, 0, i + 3 < steps ? kTileI : 0);
+    add(i & 1);
+    keep(next, ~i & 1);
+    ++i;
+  };
+  if (steps) {
+    fetch(s[0], whole, 0, steps > 1 ? kTileI : 0);
+    fetch(s[1], whole, 0, steps > 2 ? kTileI : 0);
+    keep(s[0], 0);
+    while (i + 2 < steps) {
+      step(s[0], s[1]);
+      step(s[1], s[0]);
+    }
+    if (i + 1 < steps) step(s[0], s[1]);
+    __syncthreads();
+    add(i & 1);
+    ++i;
+  }
+  if (rest) {
+    // (the pointers are at the last whole step's rows)
+    if (steps) {
+      code_at += kTileI * a.a.stride;
+      z_at += kTileI * a.dz.stride;
+      scale_at += kTileI * a.a.sstride;
+    }
+    fetch(s[0], std::false_type(), rest, 0);
+    keep(s[0], i & 1);
+    __syncthreads();
+    add(i & 1);
   }
   store_tile<O, TK, TJ>(a, c0 + wk * TK * 16, j0 + wj * TJ * 16, l, acc);
 }
 
-// The splits' sums, in their order.
+// The splits' sums, in an order that depends on their number: a block's waves take them in
+// turn and are added up in theirs.  64 x 4 columns a block.
+constexpr int kJoinWaves = 16;
+
 template <typename O>
-__global__ void __launch_bounds__(kBlock) k_product_join(GradArgs a) {
-  const int32_t across = (a.k + 3) / 4;
-  const int64_t i = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-  if (i >= (int64_t)a.m * across) return;
-  const int32_t j = (int32_t)(i / across), c = (int32_t)(i - (int64_t)j * across) * 4;
+__global__ void __launch_bounds__(kJoinWaves* kWave) k_product_join(GradArgs a) {
+  __shared__ v4f lds[kJoinWaves][kWave];
+  const int32_t across = (a.k + 3) / 4, l = lane_id(), wave = (int32_t)threadIdx.x / kWave,
+                waves = (int32_t)blockDim.x / kWave;
+  const int64_t i = (int64_t)blockIdx.x * kWave + l;
+  const bool here = i < (int64_t)a.m * across;
+  const int32_t j = here ? (int32_t)(i / across) : 0, c = here ? (int32_t)(i - (int64_t)j * across) * 4 : 0;
   const float* p = a.part + (int64_t)j * a.k + c;
   const int64_t step = (int64_t)a.m * a.k;
-  float f[4] = {};
-  if (c + 4 <= a.k) {
-#pragma unroll 8
-    for (int32_t s = 0; s < a.splits; ++s) {
+  v4f f = {};
+  if (here && c + 4 <= a.k) {
+#pragma unroll 4
+    for (int32_t s = wave; s < a.splits; s += waves) {
       float v[4];
       row_load<float, 4>((const char*)(p + s * step), v);
 #pragma unroll
       for (int r = 0; r < 4; ++r) f[r] += v[r];
     }
-  } else {
-    for (int32_t s = 0; s < a.splits; ++s)
+  } else if (here) {
+    for (int32_t s = wave; s < a.splits; s += waves)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         if (c + r < a.k) f[r] += p[s * step + r];
   }
-  store_sums<O>(a, j, c, f);
+  lds[wave][l] = f;
+  __syncthreads();
+  if (wave || !here) return;
+  for (int32_t w = 1; w < waves; ++w) f += lds[w][l];
+  const float sums[4] = {f[0], f[1], f[2], f[3]};
+  store_sums<O>(a, j, c, sums);
 }
 
 // How many splits of the rows: enough that blocks fill the chip's 256 CUs, twice where
@@ -416,7 +481,7 @@ struct GradShape {
 
 GradShape shape_of(int64_t n, int64_t k, int64_t m, bool wide) {
   GradShape s;
-  s.bj = wide ? kWideJ : m <= 64 ? 64 : 128;
+  s.bj = wide ? kWideJ : m <= 64 || k < 16 ? 64 : 128;
   s.tiles_k = cdiv(k, wide ? kWideK : kTileK);
   s.tiles_j = cdiv(m, s.bj);
   const int64_t blocks = wide ? 256 : 512, rows = wide ? 512 : 256;
@@ -439,15 +504,18 @@ int launch_grad(GradArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)(s.tiles_k * s.tiles_j), (unsigned)s.splits);
   if (wide)
     hipLaunchKernelGGL(k_product_grad_wide, grid, dim3(512), 0, stream, a);
+  else if (a.m < kVec<Z> || a.k < 16)
+    hipLaunchKernelGGL((k_product_grad<Z, O, PARTS, 64, true>), grid, dim3(kBlock), 0, stream, a);
   else if (s.bj == 64)
-    hipLaunchKernelGGL((k_product_grad<Z, O, PARTS, 64>), grid, dim3(kBlock), 0, stream, a);
+    hipLaunchKernelGGL((k_product_grad<Z, O, PARTS, 64, false>), grid, dim3(kBlock), 0, stream, a);
   else
-    hipLaunchKernelGGL((k_product_grad<Z, O, PARTS, 128>), grid, dim3(kBlock), 0, stream, a);
+    hipLaunchKernelGGL((k_product_grad<Z, O, PARTS, 128, false>), grid, dim3(kBlock), 0, stream, a);
   GG_LAUNCH_CHECK("k_product_grad");
   if (a.part) {
-    const int64_t lanes = a.m * cdiv(a.k, 4);
-    hipLaunchKernelGGL((k_product_join<O>), dim3((unsigned)cdiv(lanes, kBlock)), dim3(kBlock), 0,
-                       stream, a);
+    int waves = 1;
+    while (waves < kJoinWaves && waves < a.splits) waves *= 2;
+    hipLaunchKernelGGL((k_product_join<O>), dim3((unsigned)cdiv(a.m * cdiv(a.k, 4), kWave)),
+                       dim3(waves * kWave), 0, stream, a);
     GG_LAUNCH_CHECK("k_product_join");
   }
   return GG_OK;
