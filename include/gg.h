@@ -702,7 +702,7 @@ int gg_quantise_blocks(const gg_rows_t* w, int64_t rows, int64_t cols, const gg_
  * out[i][j] = sum over c of a[i][c] b[j][c], rounded once to out's type (GG_F32, GG_F16
  * or GG_BF16).  Each 128 columns' codes are multiplied and added in matrix
  * instructions, their sum scaled and added in fp32, in an order that depends on the sizes
- * alone.  For GG_F32 the products are exact and their sums fp32.  For 16-bit outputs
+ * and on the element's place alone.  For GG_F32 the products are exact and their sums fp32.  For 16-bit outputs
  * the 8-bit instructions add the products of columns 8 c .. 8 c + 7 at a time, each cut off
  * below 2^-13 of the largest one's power of two (codes below 2^-6 counting as that): some
  * 2^-16 of a result, at twice the rate.  The gradient of the rows is the same call on the output's gradient in 8

@@ -17,6 +17,7 @@ struct ProductArgs {
   int64_t n;
   int32_t k, m, kb;            // kb: blocks of k
   int32_t per_row;             // a has one scale a row
+  int32_t scales16;            // four blocks' scales of a row, and of weights, are aligned
   int32_t tiles_i, tiles_j;
 };
 
@@ -80,13 +81,16 @@ __device__ __forceinline__ void store_four(const KRows& out, int64_t i, int32_t 
   }
 }
 
-// A lane's codes of a row in LDS: its pieces 2 q and 2 q + 1, q = l / 16, where rows keep
-// piece c in place c ^ (row / 2 & 7).  Rows 16 apart are alike.
+// A lane's codes of a row in LDS: its pieces q and q + 4, q = l / 16, where rows keep piece
+// c in place c ^ (row / 2 & 7).  Rows 16 apart are alike.  The sixteen lanes that LDS
+// serves at a time are 0-3, 12-15, 20-23 and 24-27, and their like: eight rows' piece q and the
+// other eight's piece q ^ 1, all in different banks.  (With pieces 2 q and 2 q + 1 the
+// same reads take twice as long.)
 template <typename C>
 __device__ __forceinline__ C operand(const v4i* row, int32_t l) {
-  const int32_t c = l / 16 * 2 ^ (l >> 1 & 7);
+  const int32_t c = l / 16 ^ (l >> 1 & 7);
   C v;
-  v.set(row[c], row[c ^ 1]);
+  v.set(row[c], row[c ^ 4]);
   return v;
 }
 
@@ -122,11 +126,11 @@ __device__ __forceinline__ void multiply_step(const float (&scale)[TI], v4f (&ac
 
 template <typename O, int TJ, int TI>
 __device__ __forceinline__ void store_tile(const ProductArgs& a, int64_t i0, int32_t j0, int32_t l,
-                                           const v4f (&acc)[TJ][TI]) {
+                                           const v4f (&acc)[TJ][TI], int64_t first = 0) {
 #pragma unroll
   for (int t = 0; t < TI; ++t) {
     const int64_t i = i0 + t * 16 + l % 16;
-    if (i >= a.n) continue;
+    if (i < first || i >= a.n) continue;
 #pragma unroll
     for (int u = 0; u < TJ; ++u) {
       const int32_t j = j0 + u * 16 + l / 16 * 4;
@@ -137,10 +141,9 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, int64_t i0, int
 
 // A tile of BJ weights' rows by BI rows of a, blocks of 128 bytes of k at a time
 // through LDS.  A row of a block is eight pieces of 16 bytes; row r has piece c in place c
-// ^ (r / 2 & 7), so that sixteen lanes that read the same piece of sixteen rows meet all
-// banks (with r & 7, eight lanes, reads take twice as long).  Wave (wj, wi) has BJ/WJ x
-// BI/WI of the tile, weights as the rows of the MFMA's result, so that a lane has one
-// row's scale to apply and four neighbours to store.
+// ^ (r / 2 & 7).  Wave (wj, wi) has BJ/WJ x BI/WI of the tile, weights as the rows of the
+// MFMA's result, so that a lane has one row's scale to apply and four neighbours to
+// store.
 //
 // Both matrices lie on 16-byte boundaries: pieces go from memory to LDS without a register
 // between, STAGES - 1 steps ahead, and the scales with them, so that the wait for a step
@@ -266,6 +269,183 @@ __global__ void __launch_bounds__(WJ* WI* WK* kWave, 2) k_product_pipe(ProductAr
     if (wk) return;
   }
   store_tile<O, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc);
+}
+
+// Tiles of 256 x 256, two blocks of k in LDS.  One wait a block, before its last quarter of
+// products: the next block has been on its way since the same place in the block before,
+// and its first operands are read into the registers that the last products leave.
+// 8,191 x 4,096 to 16,384 bf16 take 542 us, 2,030 TFLOP/s.  Without the loads 446, without
+// the scaling too 405: products, their scaling and LDS's reads do not quite overlap (a
+// wave's products alone would be 240), and the loads' requests come on top.
+template <typename O>
+__global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
+  constexpr int BJ = 256, BI = 256, WJ = 2, WI = 4, TJ = BJ / WJ / 16, TI = BI / WI / 16, kThreads = 512;
+  typedef Codes<false> C;
+  __shared__ v4i lds[2][(BJ + BI) * 8];
+  __shared__ v4f scales[2][kThreads];
+  const int32_t tid = (int32_t)threadIdx.x, l = lane_id(),
+                wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int32_t wj = wave % WJ, wi = wave / WJ;
+  int32_t ti0, tj0;
+  tile_place(a.tiles_i, a.tiles_j, &ti0, &tj0);
+  // the last tile of rows reaches back instead of over their end
+  const int64_t i0 = min((int64_t)ti0 * BI, a.n - BI);
+  const int32_t skip = (int32_t)((int64_t)ti0 * BI - i0);
+  const int32_t j0 = tj0 * BJ;
+
+  // The pieces that this lane brings: of row tid / 8 and those 64, 128 and 192 behind it, of
+  // weights and of a; weights' rows behind the last one repeat it.
+  const char* const jbase = a.b.p + j0 * a.b.stride;
+  const char* const ibase = a.a.p + i0 * a.a.stride;
+  const int32_t jlast = min(a.m - j0, BJ) - 1;
+  const int32_t piece = (tid % 8 ^ (tid >> 4 & 7)) * 16;
+  uint32_t jfrom[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+    jfrom[t] = (uint32_t)min(t * 64 + tid / 8, jlast) * (uint32_t)a.b.stride + piece;
+  const uint32_t ifrom = (uint32_t)(tid / 8) * (uint32_t)a.a.stride + piece;
+  // its scale: a row's, or behind them a block's of weights
+  const bool of_row = tid < BI;
+  const char* const scale_from =
+      of_row ? a.a.scales + (i0 + tid) * a.a.sstride
+             : a.b.scales + min(j0 + min(tid - BI, 1) * kScaleBlock, a.m - 1) / kScaleBlock * a.b.sstride;
+  const int32_t scale_step = of_row && a.per_row ? 0 : 4;
+  // Scales come for four blocks at a time where they lie on 16-byte boundaries (each
+  // lane's is in a line of its own: a load for each block costs 30 us of 577, 8,191 x 4,096
+  // to 16,384), for one at a time elsewhere.
+  const bool fours = a.scales16;
+  const int32_t whole = a.k / kBlockK;
+  // Each XCD's blocks begin at another block of k, so that rows a power of two apart do
+  // not all ask the same part of memory (542 us instead of 556).
+  const int32_t turn = (int32_t)(blockIdx.x % kXcds) * whole / kXcds / 4 * 4;
+  const auto at = [&](int32_t g) {
+    const int32_t x = g + turn;
+    return x >= whole ? x - whole : x;
+  };
+  const auto bring_scale = [&](int32_t g, int slot) {
+    load_to_lds4(scale_from + g * scale_step, lds_at((float*)scales[slot] + wave * kWave));
+  };
+  const auto bring_scales = [&](int32_t g) {
+    if (!fours)
+      bring_scale(at(g), g & 1);
+    else if (g % 4 == 0)
+      load_to_lds16_at(scale_from + at(g) * 4, lds_at(scales[g / 4 & 1] + wave * kWave));
+  };
+  const auto bring = [&](int32_t g, int slot) {
+    const char *jp = jbase + (int64_t)at(g) * kBlockK, *ip = ibase + (int64_t)at(g) * kBlockK;
+    const uint32_t to = lds_at(lds[slot] + wave * kWave);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      load_to_lds16(jp, jfrom[t], to + t * kThreads * 16);
+      load_to_lds16(ip + t * 64 * a.a.stride, ifrom, to + (t + 4) * kThreads * 16);
+    }
+    bring_scales(g);
+  };
+
+  const auto wait = [] { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  constexpr int kEarly = TJ - 2;      // 16-row pieces of weights before the wait
+  v4f acc[TJ][TI] = {};
+  C rows[TI], w[4];
+  float scale[TI], held[2] = {};
+  v4f d[3] = {};                      // products whose sums are not scaled yet
+  const auto weights = [&](int buf, int u) {
+    return operand<C>(lds[buf] + (wj * TJ * 16 + l % 16) * 8 + u * 128, l);
+  };
+  const auto row = [&](int buf, int t) {
+    return operand<C>(lds[buf] + (BJ + wi * TI * 16 + l % 16) * 8 + t * 128, l);
+  };
+  const auto add = [&](int u, int t, const v4f& x, float s) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[u][t][i] = __builtin_fmaf(x[i], s, acc[u][t][i]);
+    // (here, not behind the wait, where all of them would have to be held for)
+    asm volatile("" : "+v"(acc[u][t]));
+  };
+  const auto read_scales = [&](const float* sc, int step) {
+    const float sb = sc[(BI + wj) * step];
+#pragma unroll
+    for (int t = 0; t < TI; ++t) scale[t] = sc[((wi * TI + t) * 16 + l % 16) * step] * sb;
+  };
+  const auto scales_of = [&](int32_t g) {
+    if (fours)
+      read_scales((const float*)scales[g / 4 & 1] + g % 4, 4);
+    else
+      read_scales((const float*)scales[g & 1], 1);
+  };
+  if (whole) {
+    bring(0, 0);
+    wait();
+    if (whole > 1) bring(1, 1);
+    scales_of(0);
+    w[0] = weights(0, 0);
+    w[1] = weights(0, 1);
+#pragma unroll
+    for (int t = 0; t < TI; ++t) rows[t] = row(0, t);
+  }
+  for (int32_t g = 0; g < whole; ++g) {
+    const int buf = g & 1;
+#pragma unroll
+    for (int x = 0; x < kEarly * TI; ++x) {
+      const int u = x / TI, t = x % TI;
+      if (t == 0) w[(u + 2) % 4] = weights(buf, u + 2);
+      const v4f z = multiply(w[u % 4], rows[t]);
+      if (x == 0) add(TJ - 1, 2, d[0], held[0]);
+      if (x == 1) add(TJ - 2, 3, d[1], held[1]);
+      if (x == 2) add(TJ - 1, 3, d[2], held[1]);
+      if (x >= 3) add((x - 3) / TI, (x - 3) % TI, d[x % 3], scale[(x - 3) % TI]);
+      d[x % 3] = z;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    // the next block is here, and this one has been read; what is read of the next one
+    // meets the rest of this one's products
+    wait();
+    if (g + 2 < whole) bring(g + 2, buf);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int y = 0; y < 2 * TI; ++y) {
+      const int x = kEarly * TI + y, u = kEarly + y % 2, t = y / 2;
+      const v4f z = multiply(w[u % 4], rows[t]);
+      // (the tile three products before)
+      const int v = y - 3;
+      if (v < 0)
+        add((x - 3) / TI, (x - 3) % TI, d[x % 3], scale[(x - 3) % TI]);
+      else
+        add(kEarly + v % 2, v / 2, d[x % 3], scale[v / 2]);
+      d[x % 3] = z;
+      if (y % 2) rows[t] = row(buf ^ 1, t);
+      if (y < 2) w[y] = weights(buf ^ 1, y);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    held[0] = scale[2];
+    held[1] = scale[3];
+    scales_of(g + 1);
+    static_assert(TI == 4 && (kEarly * TI + 2 * TI) % 3 == 2 && TJ % 4 == 0, "the order of d and w");
+    const v4f z = d[2];
+    d[2] = d[1];
+    d[1] = d[0];
+    d[0] = z;
+  }
+  add(TJ - 1, 2, d[0], held[0]);
+  add(TJ - 2, 3, d[1], held[1]);
+  add(TJ - 1, 3, d[2], held[1]);
+  if (whole < a.kb) {
+    // the block at k's end, zeros behind it (the empty statement keeps what is needed here
+    // only from being computed before the loop, whose registers are all taken)
+    int32_t lane = tid;
+    asm volatile("" : "+v"(lane));
+    __syncthreads();
+    bring_scale(whole, 0);
+#pragma unroll 1
+    for (int t = 0; t < 8; ++t) {
+      const int32_t r = t % 4 * 64 + lane / 8;
+      const char* from = t < 4 ? jbase + min(r, jlast) * a.b.stride : ibase + r * a.a.stride;
+      lds[0][t * kThreads + lane] = load_codes(from, whole * kBlockK + (lane % 8 ^ (lane >> 4 & 7)) * 16, a.k);
+    }
+    wait();
+    read_scales((const float*)scales[0], 1);
+    multiply_step<TJ, TI, C>(scale, acc, [&](int x) { return weights(0, x / 16); },
+                             [&](int x) { return row(0, x / 16); });
+  }
+  store_tile<O, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc, i0 + skip);
 }
 
 // The same for matrices off 16-byte boundaries: blocks come through registers.
@@ -499,6 +679,15 @@ int launch_pipe(ProductArgs& a, hipStream_t stream) {
   return GG_OK;
 }
 
+template <typename O>
+int launch_wide(ProductArgs& a, hipStream_t stream) {
+  const int rc = tiles_of(a, 256, 256);
+  if (rc != GG_OK) return rc;
+  hipLaunchKernelGGL((k_product_wide<O>), dim3((unsigned)a.tiles_i * a.tiles_j), dim3(512), 0, stream, a);
+  GG_LAUNCH_CHECK("k_product_wide");
+  return GG_OK;
+}
+
 template <typename O, int BJ, int BI, int WJ, int WI>
 int launch_tile(ProductArgs& a, hipStream_t stream) {
   const int rc = tiles_of(a, BJ, BI);
@@ -525,8 +714,8 @@ int launch_product(ProductArgs& a, hipStream_t stream) {
   }
   if (!direct) return launch_tile<O, 128, 128, 2, 2>(a, stream);
   if constexpr (sizeof(O) == 2)
-    if (cdiv(a.n, 256) * cdiv(a.m, 256) >= 192)
-      return launch_pipe<O, 256, 256, 2, 4, 1, 2>(a, stream);
+    if (a.n >= 256 && cdiv(a.n, 256) * cdiv(a.m, 256) >= 192)
+      return launch_wide<O>(a, stream);
   return launch_pipe<O, 128, 128, 2, 2, 1, 2>(a, stream);
 }
 
@@ -555,5 +744,7 @@ extern "C" int gg_product_forward(const gg_rows_t* a, int64_t n, int64_t k, cons
   p.m = (int32_t)m;
   p.kb = (int32_t)cdiv(k, kBlockK);
   p.per_row = p.a.group == 0;
+  p.scales16 = !p.per_row && p.kb % 4 == 0 && aligned16(p.a.scales) && aligned16(p.b.scales) &&
+               p.a.sstride % 16 == 0 && p.b.sstride % 16 == 0;
   GG_FOR_FLOAT(out->dtype, O, return launch_product<O>(p, stream));
 }

@@ -17,10 +17,13 @@ typedef bf16 v8bf __attribute__((ext_vector_type(8)));
 // rows and weights.
 constexpr int32_t kXcds = 8, kBand = 4;
 
+__device__ __forceinline__ uint32_t xcd_turn(uint32_t b, uint32_t total) {
+  const uint32_t x = b % kXcds, q = total / kXcds, r = total % kXcds;
+  return x * q + min(x, r) + b / kXcds;
+}
+
 __device__ __forceinline__ void tile_place(int32_t tiles_i, int32_t tiles_j, int32_t* ti, int32_t* tj) {
-  const uint32_t total = gridDim.x, b = blockIdx.x, x = b % kXcds, q = total / kXcds,
-                 r = total % kXcds;
-  const uint32_t t = x * q + min(x, r) + b / kXcds;
+  const uint32_t t = xcd_turn(blockIdx.x, gridDim.x);
   const uint32_t width = kBand * tiles_j, band = t / width, first = band * kBand,
                  rows = min((uint32_t)tiles_i - first, (uint32_t)kBand), at = t - band * width;
   *ti = (int32_t)(first + at % rows);
@@ -33,6 +36,10 @@ __device__ __forceinline__ void tile_place(int32_t tiles_i, int32_t tiles_j, int
 __device__ __forceinline__ void load_to_lds16(const char* base, uint32_t off, uint32_t to) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off),
                "s"(base)
+               : "memory");
+}
+__device__ __forceinline__ void load_to_lds16_at(const char* p, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(p)
                : "memory");
 }
 __device__ __forceinline__ void load_to_lds4(const char* p, uint32_t to) {

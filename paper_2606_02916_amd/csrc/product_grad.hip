@@ -74,8 +74,8 @@ __device__ __forceinline__ void store_sums(const GradArgs& a, int32_t j, int32_t
 
 // A wave's sums into dw, or into its split's.
 template <typename O, int TK, int TJ>
-__device__ __forceinline__ void store_tile(const GradArgs& a, int32_t c0, int32_t j0, int32_t l,
-                                           const v4f (&acc)[TK][TJ]) {
+__device__ __forceinline__ void store_tile(const GradArgs& a, int32_t part, int32_t c0, int32_t j0,
+                                           int32_t l, const v4f (&acc)[TK][TJ]) {
 #pragma unroll
   for (int t = 0; t < TJ; ++t) {
     const int32_t j = j0 + t * 16 + l % 16;
@@ -86,7 +86,7 @@ __device__ __forceinline__ void store_tile(const GradArgs& a, int32_t c0, int32_
       if (c >= a.k) continue;
       const float f[4] = {acc[u][t][0], acc[u][t][1], acc[u][t][2], acc[u][t][3]};
       if (a.part) {
-        float* to = a.part + ((int64_t)blockIdx.y * a.m + j) * a.k + c;
+        float* to = a.part + ((int64_t)part * a.m + j) * a.k + c;
         if (c + 4 <= a.k) {
           row_store<float, 4>((char*)to, f);
         } else {
@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(512) k_product_grad_wide(GradArgs a) {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
     add(buf, false, nothing);
   }
-  store_tile<bf16, TK, TJ>(a, c0 + wk * TK * 16, j0 + wj * TJ * 16, l, acc);
+  store_tile<bf16, TK, TJ>(a, blockIdx.y, c0 + wk * TK * 16, j0 + wj * TJ * 16, l, acc);
 }
 
 // Every other gradient: a tile of 128 columns of a by BJ of dz, 32 rows at a time through
@@ -293,9 +293,11 @@ __global__ void __launch_bounds__(kBlock, 2) k_product_grad(GradArgs a) {
   const int32_t tid = (int32_t)threadIdx.x, l = lane_id(),
                 wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int32_t wk = wave % 2, wj = wave / 2;
-  const int32_t c0 = (int32_t)(blockIdx.x % a.tiles_k) * kTileK,
-                j0 = (int32_t)(blockIdx.x / a.tiles_k) * BJ;
-  const int64_t first = blockIdx.y * a.chunk, end = min(a.n, first + a.chunk);
+  // the tiles of a split, which read the same rows, next to each other on one XCD
+  const uint32_t place = xcd_turn(blockIdx.y * gridDim.x + blockIdx.x, gridDim.x * gridDim.y);
+  const int32_t part = (int32_t)(place / gridDim.x), tile = (int32_t)(place % gridDim.x);
+  const int32_t c0 = tile % a.tiles_k * kTileK, j0 = tile / a.tiles_k * BJ;
+  const int64_t first = part * a.chunk, end = min(a.n, first + a.chunk);
 
   // a step's loads: 16 codes a lane, and kLoadsZ pieces of gradients with their rows' scales
   typedef v4i mem __attribute__((aligned(1)));
@@ -432,7 +434,7 @@ __global__ void __launch_bounds__(kBlock, 2) k_product_grad(GradArgs a) {
     __syncthreads();
     add(i & 1);
   }
-  store_tile<O, TK, TJ>(a, c0 + wk * TK * 16, j0 + wj * TJ * 16, l, acc);
+  store_tile<O, TK, TJ>(a, part, c0 + wk * TK * 16, j0 + wj * TJ * 16, l, acc);
 }
 
 // The splits' sums, in an order that depends on their number: a block's waves take them in
@@ -472,8 +474,9 @@ __global__ void __launch_bounds__(kJoinWaves* kWave) k_product_join(GradArgs a) 
   store_sums<O>(a, j, c, sums);
 }
 
-// How many splits of the rows: enough that blocks fill the chip's 256 CUs, twice where
-// two fit one, of some rows at least.
+// How many splits of the rows: enough that blocks fill the chip's 256 CUs, which hold one
+// of the wide kernel's, two of 128 columns and three of 64 (233,000 rows of 602 x 41 fp32
+// 78 us with 768 blocks, 81 with 512, 83 with 1,024), of some rows at least.
 struct GradShape {
   int bj;
   int64_t tiles_k, tiles_j, splits;
@@ -484,7 +487,7 @@ GradShape shape_of(int64_t n, int64_t k, int64_t m, bool wide) {
   s.bj = wide ? kWideJ : m <= 64 || k < 16 ? 64 : 128;
   s.tiles_k = cdiv(k, wide ? kWideK : kTileK);
   s.tiles_j = cdiv(m, s.bj);
-  const int64_t blocks = wide ? 256 : 512, rows = wide ? 512 : 256;
+  const int64_t blocks = wide ? 256 : s.bj == 64 ? 768 : 512, rows = wide ? 512 : 256;
   s.splits = std::max<int64_t>(1, std::min(blocks / (s.tiles_k * s.tiles_j), cdiv(n, rows)));
   return s;
 }

@@ -144,6 +144,27 @@ def test_nans_and_infinities_keep_to_their_row_and_column(n, k, m):
     assert not bool(torch.isfinite(out[2]).any())
 
 
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("k", [512, 640, 1536])
+def test_scales_by_fours(k, offset):
+    """Many tiles of rows whose scales lie on 16-byte boundaries, and beside them."""
+    gg, g, n, m = lib(), gen(k), 3333, 4000
+    ac, bc, kb = codes8(n, k, g), codes8(m, k, g), k // 128
+    sa, sb = torch.exp2(torch.rand(n, kb, generator=g) * 8 - 6), torch.rand(32, kb, generator=g) + 0.5
+    wide = -(-(kb + 1) // 4) * 4
+    far = [torch.full((r, wide), float("nan"), device=DEV) for r in (n, 32)]
+    sad, sbd = (f[:, offset:offset + kb] for f in far)
+    sad.copy_(sa), sbd.copy_(sb)
+    a, b, out = ac.to(DEV), bc.to(DEV), torch.empty(n, m, dtype=BF16, device=DEV)
+    gg.gg_product_forward(gg.make_rows(a, scales=sad, group=128), n, k, gg.make_blocks(b, sbd), m,
+                          gg.make_rows(out))
+    col = torch.arange(k) // 128
+    ac, bc = ac.float().double(), bc.float().double()
+    an, bn = ac * sa.double()[:, col], bc * sb.double()[torch.arange(m) // 128][:, col]
+    want, size = ((x.to(DEV) @ y.to(DEV).t()).cpu() for x, y in ((an, bn), (an.abs(), bn.abs())))
+    check(out, want, (k + 4) * U * size + 1.01 * UNIT[BF16] * want.abs() + 1.01 * coarse(an, ac, bn, bc), BF16)
+
+
 def test_product_of_no_rows():
     gg = lib()
     b = some_blocks(20, 30, gen(0))[0]
