@@ -152,7 +152,7 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, int64_t i0, int
 // many.  A step at k's end that is not whole comes through registers, with zeros
 // behind the end.
 template <typename O, int BJ, int BI, int WJ, int WI, int WK, int STAGES>
-__global__ void __launch_bounds__(WJ* WI* WK* kWave, 2) k_product_pipe(ProductArgs a) {
+__global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_pipe(ProductArgs a) {
   constexpr int kThreads = WJ * WI * WK * kWave, kGroup = kThreads / WK, kPieces = (BJ + BI) * 8,
                 kLoads = kPieces * WK / kThreads, kBlocksJ = (BJ + kScaleBlock - 1) / kScaleBlock;
   constexpr int TJ = BJ / WJ / 16, TI = BI / WI / 16;
@@ -698,23 +698,35 @@ int launch_tile(ProductArgs& a, hipStream_t stream) {
   return GG_OK;
 }
 
+// Which kernel: microseconds measured beside the next best, bf16 results.
 template <typename O>
 int launch_product(ProductArgs& a, hipStream_t stream) {
   // offsets in a tile are of 32 bits
   const bool near = std::max({a.a.stride, a.b.stride, a.a.sstride}) <= 1 << 23;
   const bool direct = near && aligned16(a.a.p) && aligned16(a.b.p) && a.a.stride % 16 == 0 &&
                       a.b.stride % 16 == 0;
-  if (near && a.n <= 128) {
-    if (a.n <= 16) return launch_few<O, 1, 1>(a, stream);
-    if (direct && a.n > 96) return launch_pipe<O, 32, 128, 1, 4, 2, 3>(a, stream);
-    if (direct && a.n > 64) return launch_pipe<O, 32, 96, 2, 2, 2, 3>(a, stream);
-    if (direct && a.n > 32) return launch_pipe<O, 32, 64, 1, 4, 2, 5>(a, stream);
-    if (a.n <= 32) return launch_few<O, 2, 2>(a, stream);
-    return launch_few<O, 2, 4>(a, stream);
+  const auto tiles = [&](int bj, int bi) { return cdiv(a.n, bi) * cdiv(a.m, bj); };
+  // Few rows: without LDS, which gathers a's rows badly; more of them while the weights are
+  // few too (16 rows of 4,096 to 4,096 7.6, through LDS 8.5; of 8,192 to 8,192 20.2 and 14.9).
+  if (near && (a.n <= 4 || (a.n <= 16 && (!direct || (int64_t)a.m * a.k <= 1 << 24))))
+    return launch_few<O, 1, 1>(a, stream);
+  if (!direct) {
+    if (near && a.n <= 32) return launch_few<O, 2, 2>(a, stream);
+    if (near && a.n <= 128) return launch_few<O, 2, 4>(a, stream);
+    return launch_tile<O, 128, 128, 2, 2>(a, stream);
   }
-  if (!direct) return launch_tile<O, 128, 128, 2, 2>(a, stream);
+  if (a.n <= 32) return launch_pipe<O, 32, 32, 1, 2, 2, 5>(a, stream);
+  if (a.n <= 64) return launch_pipe<O, 32, 64, 1, 4, 2, 5>(a, stream);
+  if (a.n <= 96) return launch_pipe<O, 32, 96, 2, 2, 2, 3>(a, stream);
+  // The largest tiles that still leave one for each CU (256 rows of 4,096 to 4,096 15.1 in tiles
+  // of 32 x 128, 26.1 in 128 x 128; 1,024 rows 26.4 and 29.2).
+  if (tiles(32, 128) <= 256) return launch_pipe<O, 32, 128, 1, 4, 2, 3>(a, stream);
+  if (tiles(64, 128) <= 256) return launch_pipe<O, 64, 128, 2, 2, 2, 3>(a, stream);
+  if (tiles(128, 128) <= 256) return launch_pipe<O, 128, 128, 2, 2, 2, 2>(a, stream);
+  // A round of 256 of 256 x 256 takes 1.4 to 1.85 times one of 512 of 128 x 128 (8,192 and 2,048
+  // columns), and does twice as much.
   if constexpr (sizeof(O) == 2)
-    if (a.n >= 256 && cdiv(a.n, 256) * cdiv(a.m, 256) >= 192)
+    if (a.n >= 256 && cdiv(tiles(256, 256), 256) * 8 <= cdiv(tiles(128, 128), 512) * 5)
       return launch_wide<O>(a, stream);
   return launch_pipe<O, 128, 128, 2, 2, 1, 2>(a, stream);
 }

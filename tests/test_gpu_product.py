@@ -111,7 +111,9 @@ def test_product(n, k, m):
 @pytest.mark.parametrize("group", [0, 128])
 @pytest.mark.parametrize("n,k,m", [(1, 4096, 512), (16, 2048, 200), (40, 1024, 260), (100, 4096, 256),
                                    (200, 512, 512), (512, 256, 640), (1000, 1024, 700), (2500, 384, 1300),
-                                   (47, 16_384, 33), (700, 128, 64), (3400, 400, 3700), (4097, 128, 3000)])
+                                   (47, 16_384, 33), (700, 128, 64), (3400, 400, 3700), (4097, 128, 3000), (20, 640, 700),
+                                   (70, 900, 400), (600, 384, 900), (1400, 256, 2000), (2700, 272, 2500), (1500, 272, 1200),
+                                   (6000, 144, 2900)])
 def test_product_at_aligned_places(n, k, m, group, t):
     """Rows on 16-byte boundaries, and whole or partial tiles of them."""
     check_forward(n, k, m, t, group, 0, 0)
