@@ -711,8 +711,12 @@ int launch_product(ProductArgs& a, hipStream_t stream) {
   if (near && (a.n <= 4 || (a.n <= 16 && (!direct || (int64_t)a.m * a.k <= 1 << 24))))
     return launch_few<O, 1, 1>(a, stream);
   if (!direct) {
-    if (near && a.n <= 32) return launch_few<O, 2, 2>(a, stream);
-    if (near && a.n <= 128) return launch_few<O, 2, 4>(a, stream);
+    // through registers: small tiles while two blocks' waves of them fit a CU (602 columns to
+    // 41, 1,024 rows 4.5 in 16 x 16, 14 in 128 x 128; to 512 9.1 in 32 x 32 and 12)
+    const int64_t waves = std::min(a.kb, kFewWaves);
+    if (near && tiles(16, 16) * waves <= 4096) return launch_few<O, 1, 1>(a, stream);
+    if (near && tiles(32, 32) * waves <= 4096) return launch_few<O, 2, 2>(a, stream);
+    if (near && a.n <= 64) return launch_few<O, 2, 4>(a, stream);
     return launch_tile<O, 128, 128, 2, 2>(a, stream);
   }
   if (a.n <= 32) return launch_pipe<O, 32, 32, 1, 2, 2, 5>(a, stream);
