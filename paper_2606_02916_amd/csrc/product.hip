@@ -17,7 +17,8 @@ struct ProductArgs {
   int64_t n;
   int32_t k, m, kb;            // kb: blocks of k
   int32_t per_row;             // a has one scale a row
-  int32_t scales16;            // four blocks' scales of a row, and of weights, are aligned
+  int32_t scales16;            // four blocks' scales of a row, and of weights, are aligned, and
+                               // k is whole fours of blocks
   int32_t tiles_i, tiles_j;
 };
 
@@ -760,7 +761,7 @@ extern "C" int gg_product_forward(const gg_rows_t* a, int64_t n, int64_t k, cons
   p.m = (int32_t)m;
   p.kb = (int32_t)cdiv(k, kBlockK);
   p.per_row = p.a.group == 0;
-  p.scales16 = !p.per_row && p.kb % 4 == 0 && aligned16(p.a.scales) && aligned16(p.b.scales) &&
+  p.scales16 = !p.per_row && k % (4 * kBlockK) == 0 && aligned16(p.a.scales) && aligned16(p.b.scales) &&
                p.a.sstride % 16 == 0 && p.b.sstride % 16 == 0;
   GG_FOR_FLOAT(out->dtype, O, return launch_product<O>(p, stream));
 }

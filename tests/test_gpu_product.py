@@ -167,6 +167,25 @@ def test_scales_by_fours(k, offset):
     check(out, want, (k + 4) * U * size + 1.01 * UNIT[BF16] * want.abs() + 1.01 * coarse(an, ac, bn, bc), BF16)
 
 
+@pytest.mark.parametrize("k", [400, 1000, 1010, 4000])
+def test_the_last_of_four_blocks_is_cut(k):
+    """As many scales as whole fours of blocks have, aligned, and codes that end inside a block."""
+    gg, g, n, m = lib(), gen(k), 2200, 4000
+    ac, bc, kb = codes8(n, k, g), codes8(m, k, g), blocks_of(k, 128)
+    assert kb % 4 == 0
+    sa, sb = torch.exp2(torch.rand(n, kb, generator=g) * 8 - 6), torch.rand(32, kb, generator=g) + 0.5
+    a, b = (torch.zeros(x, kb * 128, device=DEV).to(E4M3)[:, :k] for x in (n, m))
+    a.view(torch.uint8).copy_(ac.view(torch.uint8)), b.view(torch.uint8).copy_(bc.view(torch.uint8))
+    out = torch.empty(n, m, dtype=BF16, device=DEV)
+    gg.gg_product_forward(gg.make_rows(a, scales=sa.to(DEV), group=128), n, k,
+                          gg.make_blocks(b, sb.to(DEV)), m, gg.make_rows(out))
+    col = torch.arange(k) // 128
+    ac, bc = ac.float().double(), bc.float().double()
+    an, bn = ac * sa.double()[:, col], bc * sb.double()[torch.arange(m) // 128][:, col]
+    want, size = ((x.to(DEV) @ y.to(DEV).t()).cpu() for x, y in ((an, bn), (an.abs(), bn.abs())))
+    check(out, want, (k + 4) * U * size + 1.01 * UNIT[BF16] * want.abs() + 1.01 * coarse(an, ac, bn, bc), BF16)
+
+
 def test_product_of_no_rows():
     gg = lib()
     b = some_blocks(20, 30, gen(0))[0]
