@@ -285,6 +285,31 @@ def test_weight_gradient_at_aligned_places(n, k, m, group, tz, t, add):
     check(*grad_case(n, k, m, tz, t, group, add, 0, 0), t)
 
 
+@pytest.mark.parametrize("n,k,m", [(1100, 4090, 4088), (1088, 4096, 4096), (50_001, 1030, 1000),
+                                   (33_000, 1024, 1032), (70_000, 130, 2000)])
+@pytest.mark.parametrize("group,add", [(0, False), (128, True)])
+def test_weight_gradient_with_work_for_every_cu(n, k, m, group, add):
+    """bf16 gradients whose rows lie on 16-byte boundaries, and products enough for large
+    tiles; codes and results at odd places."""
+    gg, g = lib(), gen(n, k, m)
+    a, an, _ = some_rows(n, k, group, g)
+    z = torch.randn(n, m, generator=g).to(BF16)
+    zd = like(n, m, BF16, DEV, lead=8, pad=8)[0]
+    zd.copy_(z)
+    dw, flat, own = like(m, k, BF16, DEV, lead=1, pad=3)
+    old = (torch.randn(m, k, generator=g) * 8).to(BF16)
+    if add:
+        dw.copy_(old)
+    ws = torch.full((max(gg.gg_ws_product(n, k, m), 16),), 0xFF, dtype=torch.uint8, device=DEV)
+    gg.gg_product_backward(a, n, k, gg.make_rows(zd), m, gg.make_rows(dw),
+                           gg.GG_PRODUCT_ADD if add else 0, ws)
+    assert untouched(flat, own)
+    z, an, old = z.to(DEV).double(), an.to(DEV), (old.to(DEV).double() if add else 0)
+    want, size = z.t().contiguous() @ an + old, z.abs().t().contiguous() @ an.abs() + abs(old)
+    bound = (n + 4) * U * size + 1.01 * PARTS[BF16] * size + 1.01 * UNIT[BF16] * want.abs() + FLOOR[BF16]
+    check(dw, want.cpu(), bound.cpu(), BF16)
+
+
 def test_weight_gradient_of_no_rows():
     gg = lib()
     a = gg.make_rows(torch.empty(0, 30, device=DEV).to(E4M3), scales=torch.empty(0, device=DEV))
