@@ -95,6 +95,28 @@ __device__ __forceinline__ C operand(const v4i* row, int32_t l) {
   return v;
 }
 
+// Codes at any byte.  The memory reads 16 bytes that begin inside a word in 2.8 times
+// the time of 16 that begin with one (1 row of 4,096 to 16,384 37 us and 13.5), and so
+// the whole words that hold a piece's bytes are read, and moved down to its place p.
+__device__ __forceinline__ v4i words_from(const v4i& w, int32_t next, uint32_t p) {
+  const uint32_t skip = p & 3;
+  return v4i{(int)__builtin_amdgcn_alignbyte(w[1], w[0], skip), (int)__builtin_amdgcn_alignbyte(w[2], w[1], skip),
+             (int)__builtin_amdgcn_alignbyte(w[3], w[2], skip), (int)__builtin_amdgcn_alignbyte(next, w[3], skip)};
+}
+typedef v4i words4 __attribute__((aligned(4)));
+
+// A lane's codes of a row in LDS whose words begin `skip` bytes before the row: the words
+// behind pieces q and q + 4 are the next pieces' first ones, and behind the last one, `end`.
+template <typename C>
+__device__ __forceinline__ C operand_of_words(const v4i* row, const int32_t* end, uint32_t skip, int32_t l) {
+  const int32_t q = l / 16, turn = l >> 1 & 7, c = q ^ turn;
+  const int32_t next = row[q + 1 ^ turn][0];
+  const int32_t* far = q == 3 ? end : (const int32_t*)(row + (q + 5 ^ turn));
+  C v;
+  v.set(words_from(row[c], next, skip), words_from(row[c ^ 4], *far, skip));
+  return v;
+}
+
 // The products of a wave's TJ x TI operands from LDS, added to acc with the scales of
 // its rows.  A product's sum is scaled kLag products later, when the matrix unit has it,
 // and the weights of the next 16 rows are read before this one's products; kept in
@@ -146,13 +168,13 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, int64_t i0, int
 // MFMA's result, so that a lane has one row's scale to apply and four neighbours to
 // store.
 //
-// Both matrices lie on 16-byte boundaries: pieces go from memory to LDS without a register
+// Pieces of whole words go from memory to LDS without a register
 // between, STAGES - 1 steps ahead, and the scales with them, so that the wait for a step
 // can count the loads behind it.  A step has WK blocks of k, each for WJ x WI waves, whose
 // sums are added at the end: few rows' steps are short, and so there are half as
 // many.  A step at k's end that is not whole comes through registers, with zeros
 // behind the end.
-template <typename O, int BJ, int BI, int WJ, int WI, int WK, int STAGES>
+template <typename O, int BJ, int BI, int WJ, int WI, int WK, int STAGES, bool BYTES>
 __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_pipe(ProductArgs a) {
   constexpr int kThreads = WJ * WI * WK * kWave, kGroup = kThreads / WK, kPieces = (BJ + BI) * 8,
                 kLoads = kPieces * WK / kThreads, kBlocksJ = (BJ + kScaleBlock - 1) / kScaleBlock;
@@ -160,11 +182,13 @@ __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_
   static_assert(kPieces % kGroup == 0, "whole loads");
   static_assert(BJ / WJ <= kScaleBlock && kScaleBlock % (BJ / WJ) == 0, "one block of weights a wave");
   static_assert(BI + kBlocksJ <= kGroup, "a lane for each scale");
-  constexpr int kBehind = (kLoads + 1) * (STAGES - 2);   // loads that may be under way
+  static_assert(!BYTES || BJ + BI <= kGroup, "a lane for each row");
+  constexpr int kBehind = (kLoads + 1 + BYTES) * (STAGES - 2);   // loads that may be under way
   static_assert(kBehind < 64, "the counter of loads");
   typedef Codes<sizeof(O) == 4> C;
   __shared__ v4i lds[STAGES][WK][kPieces];
   __shared__ float scales[STAGES][kThreads];
+  __shared__ int32_t ends[BYTES ? STAGES : 1][BYTES ? kThreads : 1];
   const int32_t l = lane_id(),
                 wave_all = __builtin_amdgcn_readfirstlane((int32_t)threadIdx.x / kWave);
   // a group of waves brings its own block of a step and multiplies it
@@ -184,12 +208,20 @@ __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_
     *off = r < BJ ? min(r, jlast) * a.b.stride : min(r - BJ, ilast) * a.a.stride;
     return r;
   };
+  // (BYTES: whole words, from the one with a row's first byte on)
+  const uint32_t jskip = BYTES ? (uintptr_t)jbase & 3 : 0, iskip = BYTES ? (uintptr_t)ibase & 3 : 0;
   uint32_t from[kLoads];
 #pragma unroll
   for (int t = 0; t < kLoads; ++t) {
     int64_t off;
     const int32_t r = row_of(t, &off);
-    from[t] = (uint32_t)off + (tid % 8 ^ (r >> 1 & 7)) * 16;
+    from[t] = ((uint32_t)off + (r < BJ ? jskip : iskip) & (BYTES ? ~3u : ~0u)) + (tid % 8 ^ (r >> 1 & 7)) * 16;
+  }
+  // and of row tid the word with the last byte of a block
+  const char* end_from = nullptr;
+  if constexpr (BYTES) {
+    const char* p = tid < BJ ? jbase + min(tid, jlast) * a.b.stride : ibase + min(tid - BJ, ilast) * a.a.stride;
+    end_from = (const char*)((uintptr_t)(p + kBlockK - 1) & ~(uintptr_t)3);
   }
   // its scale: a row's, or behind them a block's of weights
   const char* scale_from;
@@ -206,13 +238,15 @@ __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_
     const int32_t g = s * WK + wk;
     v4i* const to = lds[slot][wk];
     if (s < whole) {
-      const char *jp = jbase + (int64_t)g * kBlockK, *ip = ibase + (int64_t)g * kBlockK;
+      const char *jp = jbase - jskip + (int64_t)g * kBlockK, *ip = ibase - iskip + (int64_t)g * kBlockK;
 #pragma unroll
       for (int t = 0; t < kLoads; ++t) {
         // (a load's 64 lanes are of one matrix: BJ is a multiple of 8)
         const bool weights = (t * kGroup + wave * kWave) / 8 < BJ;
         load_to_lds16(weights ? jp : ip, from[t], lds_at(to + t * kGroup + wave * kWave));
       }
+      if constexpr (BYTES)
+        load_to_lds4(end_from + (int64_t)g * kBlockK, lds_at(&ends[slot][wave_all * kWave]));
     } else {
 #pragma unroll 1
       for (int t = 0; t < kLoads; ++t) {
@@ -226,6 +260,10 @@ __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_
                  lds_at(&scales[slot][wave_all * kWave]));
   };
 
+  // bytes before this lane's rows, the same for rows 16 apart
+  const int32_t wrow = wj * TJ * 16 + l % 16, rrow = wi * TI * 16 + l % 16;
+  const uint32_t wskip = jskip + (uint32_t)wrow * (uint32_t)a.b.stride,
+                 rskip = iskip + (uint32_t)rrow * (uint32_t)a.a.stride;
   v4f acc[TJ][TI] = {};
 #pragma unroll
   for (int s = 0; s < STAGES - 1; ++s)
@@ -244,10 +282,18 @@ __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_
       float scale[TI];
 #pragma unroll
       for (int t = 0; t < TI; ++t) scale[t] = sc[(wi * TI + t) * 16 + l % 16] * sb;
-      const v4i *w = lds[slot][wk] + (wj * TJ * 16 + l % 16) * 8,
-                *r = lds[slot][wk] + (BJ + wi * TI * 16 + l % 16) * 8;
-      multiply_step<TJ, TI, C>(scale, acc, [&](int x) { return operand<C>(w + x * 8, l); },
-                               [&](int x) { return operand<C>(r + x * 8, l); });
+      const v4i *w = lds[slot][wk] + wrow * 8, *r = lds[slot][wk] + (BJ + rrow) * 8;
+      if constexpr (BYTES) {
+        const int32_t *we = ends[slot] + wk * kGroup + wrow, *re = ends[slot] + wk * kGroup + BJ + rrow;
+        // (a step at k's end has its codes in place)
+        const uint32_t ws = s < whole ? wskip : 0, rs = s < whole ? rskip : 0;
+        multiply_step<TJ, TI, C>(scale, acc,
+                                 [&](int x) { return operand_of_words<C>(w + x * 8, we + x, ws, l); },
+                                 [&](int x) { return operand_of_words<C>(r + x * 8, re + x, rs, l); });
+      } else {
+        multiply_step<TJ, TI, C>(scale, acc, [&](int x) { return operand<C>(w + x * 8, l); },
+                                 [&](int x) { return operand<C>(r + x * 8, l); });
+      }
     }
     slot = slot + 1 < STAGES ? slot + 1 : 0;
   }
@@ -449,7 +495,8 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
   store_tile<O, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc, i0 + skip);
 }
 
-// The same for matrices off 16-byte boundaries: blocks come through registers.
+// Tiles of matrices with more than 2^23 bytes from a row to the next: blocks come through
+// registers.
 template <typename O, int BJ, int BI, int WJ, int WI>
 __global__ void __launch_bounds__(WJ* WI* kWave, sizeof(O) == 4 ? 1 : 2) k_product_tile(ProductArgs a) {
   constexpr int kThreads = WJ * WI * kWave, kRows = kThreads / 8, kLoads = (BJ + BI) / kRows,
@@ -522,92 +569,86 @@ __global__ void __launch_bounds__(WJ* WI* kWave, sizeof(O) == 4 ? 1 : 2) k_produ
   store_tile<O, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc);
 }
 
-// Few rows: operands go from memory to registers, without LDS.  A block has 16 TJ weights'
-// rows and 16 TI rows of a; its waves take the blocks of k in turn, with no wait for each
-// other, the next one's operands loaded before this one's products, and their sums are
-// added in the order of the waves' halves.  Bound by the weights' bytes, and for
-// more than some 32 rows by those of a, which every block reads from the caches.
+// Few rows: operands go from memory to registers, without LDS.  A block has 16 weights' rows
+// and 16 rows of a; its waves take the blocks of k in turn, with no wait for each
+// other, the next two's operands loaded before these two's products, and their sums are
+// added in the order of the waves' halves.  Bound by the weights' bytes (1 row of
+// 4,096 to 16,384 bf16 12.9 us, 5.2 TB/s), and for more rows by those of a, which every block
+// reads from the caches.  BYTES: rows may begin inside a word.
 constexpr int kFewWaves = 8;
 
-template <typename O, int TJ, int TI>
+template <typename O, bool BYTES>
 __global__ void __launch_bounds__(kFewWaves* kWave, 2) k_product_few(ProductArgs a) {
-  constexpr int kAhead = TI == 1 ? 2 : 1;        // blocks in a step
+  constexpr int kAhead = 2;                      // blocks of k in a step
   typedef Codes<sizeof(O) == 4> C;
-  __shared__ v4f lds[kFewWaves / 2][TJ * TI][kWave];
+  __shared__ v4f lds[kFewWaves / 2][kWave];
   const int32_t l = lane_id(),
                 wave = __builtin_amdgcn_readfirstlane((int32_t)threadIdx.x / kWave),
                 waves = (int32_t)blockDim.x / kWave;
   int32_t ti0, tj0;
   tile_place(a.tiles_i, a.tiles_j, &ti0, &tj0);
-  const int32_t j0 = tj0 * TJ * 16;
-  const int64_t i0 = (int64_t)ti0 * TI * 16;
+  const int32_t j0 = tj0 * 16;
+  const int64_t i0 = (int64_t)ti0 * 16;
   // rows behind the last one repeat it
   const char* const wbase = a.b.p + j0 * a.b.stride;
   const char* const rbase = a.a.p + i0 * a.a.stride;
   const char* const sbase = a.a.scales + i0 * a.a.sstride;
   const char* const wscale = a.b.scales + j0 / kScaleBlock * a.b.sstride;
-  const int32_t jlast = a.m - j0 - 1, ilast = (int32_t)min(a.n - i0, (int64_t)TI * 16) - 1;
-  uint32_t w_off[TJ], r_off[TI], s_off[TI];
-#pragma unroll
-  for (int u = 0; u < TJ; ++u) w_off[u] = (uint32_t)min(u * 16 + l % 16, jlast) * (uint32_t)a.b.stride;
-#pragma unroll
-  for (int t = 0; t < TI; ++t) {
-    r_off[t] = (uint32_t)min(t * 16 + l % 16, ilast) * (uint32_t)a.a.stride;
-    s_off[t] = (uint32_t)min(t * 16 + l % 16, ilast) * (uint32_t)a.a.sstride;
-  }
+  const int32_t r = (int32_t)min(a.n - i0 - 1, (int64_t)(l % 16));
+  const uint32_t w_off = (uint32_t)min(l % 16, a.m - j0 - 1) * (uint32_t)a.b.stride,
+                 r_off = (uint32_t)r * (uint32_t)a.a.stride, s_off = (uint32_t)r * (uint32_t)a.a.sstride;
   const int32_t whole = a.k / kBlockK, lane_c = l / 16 * 32;
+  // 32 codes of a row, and with BYTES the word with the last one
+  struct Piece {
+    v4i w[2];
+    int32_t last;
+    __device__ __forceinline__ void load(const char* base, uint32_t off) {
+      const uint32_t skip = BYTES ? (uint32_t)(uintptr_t)base + off & 3 : 0;
+      const uintptr_t p = (uintptr_t)base + off - skip;
+#pragma unroll
+      for (int x = 0; x < 2; ++x) w[x] = *(const GG_GLOBAL words4*)(p + 16 * x);
+      if (BYTES) last = *(const GG_GLOBAL int32_t*)(p + (skip ? 32 : 28));
+    }
+    __device__ __forceinline__ C codes(const char* base, uint32_t off) const {
+      C c;
+      if constexpr (BYTES) {
+        const uint32_t p = (uint32_t)(uintptr_t)base + off;
+        c.set(words_from(w[0], w[1][0], p), words_from(w[1], last, p));
+      } else {
+        c.set(w[0], w[1]);
+      }
+      return c;
+    }
+  };
   struct Step {
-    v4i w[kAhead][TJ][2], r[kAhead][TI][2];
-    float sb[kAhead], sa[kAhead][TI];
+    Piece w[kAhead], r[kAhead];
+    float sb[kAhead], sa[kAhead];
   };
   const auto load_scales = [&](int32_t g, int h, Step& s) {
     s.sb[h] = *(const float*)(wscale + 4LL * g);
-#pragma unroll
-    for (int t = 0; t < TI; ++t)
-      s.sa[h][t] = *(const GG_GLOBAL float*)(sbase + (a.per_row ? 0 : 4LL * g) + s_off[t]);
+    s.sa[h] = *(const GG_GLOBAL float*)(sbase + (a.per_row ? 0 : 4LL * g) + s_off);
   };
   const auto load = [&](int32_t g0, Step& s) {
-    typedef v4i mem __attribute__((aligned(1)));
 #pragma unroll
     for (int h = 0; h < kAhead; ++h) {
       const int32_t g = g0 + h * waves;
       if (g >= whole) break;
-      const char *wp = wbase + (int64_t)g * kBlockK, *rp = rbase + (int64_t)g * kBlockK;
       load_scales(g, h, s);
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-#pragma unroll
-        for (int u = 0; u < TJ; ++u)
-          s.w[h][u][x] = *(const GG_GLOBAL mem*)(wp + (w_off[u] + lane_c) + 16 * x);
-#pragma unroll
-        for (int t = 0; t < TI; ++t)
-          s.r[h][t][x] = *(const GG_GLOBAL mem*)(rp + (r_off[t] + lane_c) + 16 * x);
-      }
+      s.w[h].load(wbase + (int64_t)g * kBlockK, w_off + lane_c);
+      s.r[h].load(rbase + (int64_t)g * kBlockK, r_off + lane_c);
     }
   };
-  v4f acc[TJ][TI] = {};
-  const auto add = [&](int h, const Step& s) {
-    C w[TJ];
+  v4f acc[1][1] = {};
+  const auto add = [&](const C& w, const C& r, float scale) {
+    const v4f d = multiply(w, r);
 #pragma unroll
-    for (int u = 0; u < TJ; ++u) w[u].set(s.w[h][u][0], s.w[h][u][1]);
-#pragma unroll
-    for (int t = 0; t < TI; ++t) {
-      const float scale = s.sa[h][t] * s.sb[h];
-      C r;
-      r.set(s.r[h][t][0], s.r[h][t][1]);
-#pragma unroll
-      for (int u = 0; u < TJ; ++u) {
-        const v4f d = multiply(w[u], r);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) acc[u][t][x] = __builtin_fmaf(d[x], scale, acc[u][t][x]);
-      }
-    }
+    for (int x = 0; x < 4; ++x) acc[0][0][x] = __builtin_fmaf(d[x], scale, acc[0][0][x]);
   };
   const auto add_all = [&](int32_t g0, const Step& s) {
 #pragma unroll
     for (int h = 0; h < kAhead; ++h) {
       if (g0 + h * waves >= whole) break;
-      add(h, s);
+      add(s.w[h].codes(wbase, w_off), s.r[h].codes(rbase, r_off), s.sa[h] * s.sb[h]);
     }
   };
   Step s[2];
@@ -622,33 +663,21 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) k_product_few(ProductArgs
   }
   if (whole < a.kb && whole % waves == wave) {   // the block at k's end
     load_scales(whole, 0, s[0]);
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int32_t c = whole * kBlockK + lane_c + 16 * x;
-#pragma unroll
-      for (int u = 0; u < TJ; ++u) s[0].w[0][u][x] = load_codes(wbase + w_off[u], c, a.k);
-#pragma unroll
-      for (int t = 0; t < TI; ++t) s[0].r[0][t][x] = load_codes(rbase + r_off[t], c, a.k);
-    }
-    add(0, s[0]);
+    const auto end_of = [&](const char* row) {
+      const int32_t c = whole * kBlockK + lane_c;
+      C codes;
+      codes.set(load_codes(row, c, a.k), load_codes(row, c + 16, a.k));
+      return codes;
+    };
+    add(end_of(wbase + w_off), end_of(rbase + r_off), s[0].sa[0] * s[0].sb[0]);
   }
   for (int32_t half = waves / 2; half >= 1; half /= 2) {
     __syncthreads();
-    if (wave >= half && wave < 2 * half) {
-#pragma unroll
-      for (int u = 0; u < TJ; ++u)
-#pragma unroll
-        for (int t = 0; t < TI; ++t) lds[wave - half][u * TI + t][l] = acc[u][t];
-    }
+    if (wave >= half && wave < 2 * half) lds[wave - half][l] = acc[0][0];
     __syncthreads();
-    if (wave < half) {
-#pragma unroll
-      for (int u = 0; u < TJ; ++u)
-#pragma unroll
-        for (int t = 0; t < TI; ++t) acc[u][t] += lds[wave][u * TI + t][l];
-    }
+    if (wave < half) acc[0][0] += lds[wave][l];
   }
-  if (wave == 0) store_tile<O, TJ, TI>(a, i0, j0, l, acc);
+  if (wave == 0) store_tile<O, 1, 1>(a, i0, j0, l, acc);
 }
 
 int tiles_of(ProductArgs& a, int bj, int bi) {
@@ -658,14 +687,22 @@ int tiles_of(ProductArgs& a, int bj, int bi) {
   return GG_OK;
 }
 
-template <typename O, int TJ, int TI>
+// Both matrices' rows begin with a word.
+bool in_words(const ProductArgs& a) {
+  return ((uintptr_t)a.a.p | (uintptr_t)a.b.p | (uintptr_t)a.a.stride | (uintptr_t)a.b.stride) % 4 == 0;
+}
+
+template <typename O>
 int launch_few(ProductArgs& a, hipStream_t stream) {
-  const int rc = tiles_of(a, 16 * TJ, 16 * TI);
+  const int rc = tiles_of(a, 16, 16);
   if (rc != GG_OK) return rc;
   int waves = 1;
   while (waves < kFewWaves && waves < a.kb) waves *= 2;
-  hipLaunchKernelGGL((k_product_few<O, TJ, TI>), dim3((unsigned)a.tiles_i * a.tiles_j),
-                     dim3(waves * kWave), 0, stream, a);
+  const dim3 grid((unsigned)a.tiles_i * a.tiles_j), block(waves * kWave);
+  if (in_words(a))
+    hipLaunchKernelGGL((k_product_few<O, false>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_product_few<O, true>), grid, block, 0, stream, a);
   GG_LAUNCH_CHECK("k_product_few");
   return GG_OK;
 }
@@ -674,8 +711,11 @@ template <typename O, int BJ, int BI, int WJ, int WI, int WK, int STAGES>
 int launch_pipe(ProductArgs& a, hipStream_t stream) {
   const int rc = tiles_of(a, BJ, BI);
   if (rc != GG_OK) return rc;
-  hipLaunchKernelGGL((k_product_pipe<O, BJ, BI, WJ, WI, WK, STAGES>),
-                     dim3((unsigned)a.tiles_i * a.tiles_j), dim3(WJ * WI * WK * kWave), 0, stream, a);
+  const dim3 grid((unsigned)a.tiles_i * a.tiles_j), block(WJ * WI * WK * kWave);
+  if (in_words(a))
+    hipLaunchKernelGGL((k_product_pipe<O, BJ, BI, WJ, WI, WK, STAGES, false>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((k_product_pipe<O, BJ, BI, WJ, WI, WK, STAGES, true>), grid, block, 0, stream, a);
   GG_LAUNCH_CHECK("k_product_pipe");
   return GG_OK;
 }
@@ -704,22 +744,13 @@ template <typename O>
 int launch_product(ProductArgs& a, hipStream_t stream) {
   // offsets in a tile are of 32 bits
   const bool near = std::max({a.a.stride, a.b.stride, a.a.sstride}) <= 1 << 23;
-  const bool direct = near && aligned16(a.a.p) && aligned16(a.b.p) && a.a.stride % 16 == 0 &&
-                      a.b.stride % 16 == 0;
+  const bool words = in_words(a);
   const auto tiles = [&](int bj, int bi) { return cdiv(a.n, bi) * cdiv(a.m, bj); };
-  // Few rows: without LDS, which gathers a's rows badly; more of them while the weights are
-  // few too (16 rows of 4,096 to 4,096 7.6, through LDS 8.5; of 8,192 to 8,192 20.2 and 14.9).
-  if (near && (a.n <= 4 || (a.n <= 16 && (!direct || (int64_t)a.m * a.k <= 1 << 24))))
-    return launch_few<O, 1, 1>(a, stream);
-  if (!direct) {
-    // through registers: small tiles while two blocks' waves of them fit a CU (602 columns to
-    // 41, 1,024 rows 4.5 in 16 x 16, 14 in 128 x 128; to 512 9.1 in 32 x 32 and 12)
-    const int64_t waves = std::min(a.kb, kFewWaves);
-    if (near && tiles(16, 16) * waves <= 4096) return launch_few<O, 1, 1>(a, stream);
-    if (near && tiles(32, 32) * waves <= 4096) return launch_few<O, 2, 2>(a, stream);
-    if (near && a.n <= 64) return launch_few<O, 2, 4>(a, stream);
-    return launch_tile<O, 128, 128, 2, 2>(a, stream);
-  }
+  if (!near) return launch_tile<O, 128, 128, 2, 2>(a, stream);
+  // Few rows, or rows and weights that are few together: without LDS, which gathers rows
+  // badly (16 rows of 4,096 to 4,096 7.4 us, through LDS 8.5; of 8,192 to 8,192 20.1 and 14.8;
+  // 64 rows of 4,096 to 1,024 7.3 and 9.6, to 4,096 12.2 and 10.1).
+  if (a.n <= 4 || tiles(16, 16) * a.kb <= 8192) return launch_few<O>(a, stream);
   if (a.n <= 32) return launch_pipe<O, 32, 32, 1, 2, 2, 5>(a, stream);
   if (a.n <= 64) return launch_pipe<O, 32, 64, 1, 4, 2, 5>(a, stream);
   if (a.n <= 96) return launch_pipe<O, 32, 96, 2, 2, 2, 3>(a, stream);
@@ -731,7 +762,7 @@ int launch_product(ProductArgs& a, hipStream_t stream) {
   // A round of 256 of 256 x 256 takes 1.4 to 1.85 times one of 512 of 128 x 128 (8,192 and 2,048
   // columns), and does twice as much.
   if constexpr (sizeof(O) == 2)
-    if (a.n >= 256 && cdiv(tiles(256, 256), 256) * 8 <= cdiv(tiles(128, 128), 512) * 5)
+    if (words && a.n >= 256 && cdiv(tiles(256, 256), 256) * 8 <= cdiv(tiles(128, 128), 512) * 5)
       return launch_wide<O>(a, stream);
   return launch_pipe<O, 128, 128, 2, 2, 1, 2>(a, stream);
 }

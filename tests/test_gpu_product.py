@@ -119,6 +119,28 @@ def test_product_at_aligned_places(n, k, m, group, t):
     check_forward(n, k, m, t, group, 0, 0)
 
 
+@pytest.mark.parametrize("n,k,m", [(10, 4104, 4100), (20, 4100, 2050), (50, 2104, 2100), (64, 2048, 2048),
+                                   (90, 2000, 1500), (200, 1304, 1000), (700, 300, 1700), (700, 256, 1700),
+                                   (2000, 300, 1900), (2000, 388, 1901), (2100, 260, 2200), (2100, 256, 2201)])
+@pytest.mark.parametrize("a_at,b_at", [((1, 3), (2, 5)), ((4, 4), (8, 8)), ((0, 0), (1, 1)), ((3, 2), (0, 0)),
+                                       ((4, 12), (0, 0))])
+def test_product_wherever_rows_begin(n, k, m, a_at, b_at):
+    """Tiles of every size, with rows that begin with a word, on a boundary of 16 bytes or at
+    any byte, both matrices alike or not."""
+    gg, g, t = lib(), gen(n, k, m), (F32, F16, BF16)[(n + k + m + a_at[0]) % 3]
+    a, an, ac = some_rows(n, k, 128 if n % 4 else 0, g, *a_at)
+    b, bn, bc = some_blocks(m, k, g, *b_at)
+    out, flat, own = like(n, m, t, DEV, lead=1, pad=0)
+    gg.gg_product_forward(a, n, k, b, m, gg.make_rows(out))
+    assert untouched(flat, own)
+    x, y = an.to(DEV), bn.to(DEV)
+    want, size = (x @ y.t()).cpu(), (x.abs() @ y.abs().t()).cpu()
+    bound = (k + 4) * U * size + 1.01 * UNIT[t] * want.abs() + FLOOR[t]
+    if t != F32:
+        bound += coarse(an, ac, bn, bc) * 1.01
+    check(out, want, bound, t)
+
+
 @pytest.mark.parametrize("n,k,m", [(3, 200, 140), (60, 300, 50), (400, 300, 300), (600, 256, 512)])
 def test_nans_and_infinities_keep_to_their_row_and_column(n, k, m):
     gg, g = lib(), gen(n)
