@@ -684,8 +684,8 @@ typedef struct gg_blocks {
 
 /* Rows into 8 bits: of each group of q's, or with group 0 of each row, scale =
  * max(max|x| / 448, 2^-126) and codes x / scale, rounded as gg_rmsnorm_forward's (a
- * zero of either sign for a zero); NaNs and infinities as there.  x: GG_F32, GG_F16 or GG_BF16; q: GG_E4M3, and no memory of
- * x's. */
+ * zero of either sign for a zero); NaNs and infinities as there.  x: GG_F32, GG_F16 or
+ * GG_BF16; q: GG_E4M3, and no memory of x's. */
 int gg_quantise_rows(const gg_rows_t* x, int64_t n, int64_t dim, const gg_rows_t* q,
                      hipStream_t stream);
 
@@ -701,13 +701,15 @@ int gg_quantise_blocks(const gg_rows_t* w, int64_t rows, int64_t cols, const gg_
 /* The product of 8-bit rows a [n][k] (group 128, or 0) with 8-bit weights b [m][k]:
  * out[i][j] = sum over c of a[i][c] b[j][c], rounded once to out's type (GG_F32, GG_F16
  * or GG_BF16).  Each 128 columns' codes are multiplied and added in matrix
- * instructions, their sum scaled and added in fp32, in an order that depends on the sizes
- * and on the element's place alone.  For GG_F32 the products are exact and their sums fp32.  For 16-bit outputs
- * the 8-bit instructions add the products of columns 8 c .. 8 c + 7 at a time, each cut off
- * below 2^-13 of the largest one's power of two (codes below 2^-6 counting as that): some
- * 2^-16 of a result, at twice the rate.  The gradient of the rows is the same call on the output's gradient in 8
- * bits and the transposed weights (gg_quantise_rows, gg_quantise_blocks).  out is no
- * memory of a or b. */
+ * instructions, their sum scaled and added in fp32, in an order that depends on the sizes, on
+ * the element's place and on how a and b are aligned.  For GG_F32 the products are exact and
+ * their sums fp32.  For 16-bit outputs the 8-bit instructions add the products of columns
+ * 8 c .. 8 c + 7 at a time, each cut off below 2^-13 of the largest one's power of two
+ * (codes below 2^-6 counting as that): some 2^-16 of a result, at twice the rate.  The
+ * gradient of the rows is the same call on the output's gradient in 8 bits and the
+ * transposed weights (gg_quantise_rows, gg_quantise_blocks).  out is no memory of a or b.
+ * Rows may begin at any byte; those that begin with a word take two thirds of the time,
+ * and of rows that begin at multiples of 16 bytes the fewest cache lines are read. */
 int gg_product_forward(const gg_rows_t* a, int64_t n, int64_t k, const gg_blocks_t* b, int64_t m,
                        const gg_rows_t* out, hipStream_t stream);
 
@@ -719,10 +721,11 @@ size_t gg_ws_product(int64_t n, int64_t k, int64_t m);
 /* The gradient of the weights, from the 8-bit rows a that gg_product_forward took and
  * the gradient dz [n][m] of its output (GG_F32, GG_F16 or GG_BF16): dw[j][c] = sum over i of
  * dz[i][j] a[i][c], [m][k], of dz's type or GG_F32; with GG_PRODUCT_ADD added to what dw
- * holds.  Sums are fp32, in an order that depends on the sizes alone, rounded once
- * with what is added.  The terms' dz times scale enter as fp32 numbers for a dw of
- * GG_F32, to 2^-15 for GG_F16 and rounded to bf16 for GG_BF16.  No row (n 0): zeros.  dw
- * is no memory of a or dz.  ws: 16-byte aligned, NULL where gg_ws_product is 0. */
+ * holds.  Sums are fp32, in an order that depends on the sizes, the types and dz's
+ * alignment, rounded once with what is added.  Of a term's three factors two are
+ * multiplied first, dz and scale as fp32 numbers (in steps of 2^-133) for a dw of GG_F32 and
+ * to 2^-15 for GG_F16, dz or the code and scale rounded to bf16 for GG_BF16.  No row (n 0):
+ * zeros.  dw is no memory of a or dz.  ws: 16-byte aligned, NULL where gg_ws_product is 0. */
 int gg_product_backward(const gg_rows_t* a, int64_t n, int64_t k, const gg_rows_t* dz, int64_t m,
                         const gg_rows_t* dw, int32_t flags, void* ws, size_t ws_bytes,
                         hipStream_t stream);

@@ -23,7 +23,8 @@ constexpr int kRowSteps = 4;   // pieces of a lane
 // Lanes of all rows lie in one line, a row's groups side by side, so that rows of
 // any width fill the waves; a lane takes a piece at each of four places a block apart.
 // Bound by memory: each element is read once and stays in registers between the
-// largest magnitude and the codes.
+// largest magnitude and the codes.  8,191 rows of 16,384 bf16 by 128 70 us, 5.8 TB/s; at
+// odd bytes, 16,384 of 4,095 37 us, beside 4,096 34.
 template <typename T, int V>
 __global__ void __launch_bounds__(kBlock) k_rows_codes(RowsArgs a) {
   const int64_t base = block_index() * (kBlock * kRowSteps);
@@ -180,7 +181,9 @@ struct BlocksArgs {
 
 // A workgroup per 128 x 128 elements, which stay in registers between the largest
 // magnitude and the codes; the transposed codes go through LDS, four by four bytes
-// at a time.  Bound by memory.
+// at a time.  Bound by memory: 16,384 x 4,096 fp32, both ways, 83 us, 4.9 TB/s; rows and
+// columns at odd bytes, whose 4-byte stores are split, take twice as long (8,191 x
+// 4,095 bf16 61 us, 8,192 x 4,096 25).
 template <typename T>
 __global__ void __launch_bounds__(kBlock) k_blocks_codes(BlocksArgs a) {
   constexpr int V = kVec<T>, kLanes = kScaleBlock / V, kStep = kBlock / kLanes,

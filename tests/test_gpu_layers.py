@@ -1,9 +1,13 @@
 """The calls for layers in 8 bits together: a student with a layer norm, students whose
 head runs on 8-bit rows, stage by stage against 64 bits; a captured layer replayed."""
+import os
+import textwrap
+
 import pytest
 import torch
 
-from tests.op_util import BF16, E4M3, F16, F32, FLOOR, U, UNIT
+from tests import helpers
+from tests.op_util import BF16, E4M3, F16, F32, FLOOR, U, UNIT, within
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -216,3 +220,27 @@ def test_a_layer_in_a_replayed_graph(t):
         torch.cuda.synchronize()
         for i, (a, e) in enumerate(zip(outs, want)):
             assert torch.equal(a.view(torch.uint8), e.view(torch.uint8)), (seed, i)
+
+
+def test_readme_example_of_a_product():
+    """The README's lines on a layer's product, as they are written."""
+    from paper_2606_02916_amd import gg
+    text = open(os.path.join(helpers.ROOT, "README.md")).read()
+    start = text.index("    a = gg.make_rows(codes, scales=scales, group=128)")
+    code = textwrap.dedent(text[start:text.index("\n\n", start)])
+    n, k, m, g = 200, 300, 140, torch.Generator().manual_seed(3)
+    x, w, dout = (torch.randn(*s, generator=g).to(DEV) for s in ((n, k), (m, k), (n, m)))
+    ns = {"gg": gg, "torch": torch, "n": n, "k": k, "m": m, "x": x, "w": w, "dout": dout,
+          "codes": torch.empty(n, k, dtype=E4M3, device=DEV), "scales": torch.empty(n, 3, device=DEV),
+          "w8": torch.empty(m, k, dtype=E4M3, device=DEV), "w_scales": torch.empty(2, 3, device=DEV),
+          "w8t": torch.empty(k, m, dtype=E4M3, device=DEV), "wt_scales": torch.empty(3, 2, device=DEV),
+          "out": torch.empty(n, m, device=DEV), "dw": torch.empty(m, k, device=DEV)}
+    exec(code, ns)
+    # a code is off by 2^-4 of its number at most, or by half the least code, 2^-10 of a scale
+    # of at most max|x| / 448
+    def off(v):
+        return v.abs() / 16 + v.abs().max() / 448 / 1024
+    x, w, dout = x.cpu().double(), w.cpu().double(), dout.cpu().double()
+    bound = off(x) @ w.abs().t() + x.abs() @ off(w).t() + off(x) @ off(w).t()
+    assert within(ns["out"], x @ w.t(), bound * 1.001) <= 0
+    assert within(ns["dw"], dout.t() @ x, dout.abs().t() @ off(x) * 1.001) <= 0

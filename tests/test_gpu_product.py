@@ -332,6 +332,25 @@ def test_weight_gradient_with_work_for_every_cu(n, k, m, group, add):
     check(dw, want.cpu(), bound.cpu(), BF16)
 
 
+@pytest.mark.parametrize("tz,t", [(F32, F32), (F16, F16), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("n,k,m", [(40, 70, 50), (300, 260, 136)])
+def test_weight_gradient_of_small_scales(n, k, m, tz, t):
+    """Scales near the least one, whose products with gradients, and what those leave behind
+    their upper bits, lie below the least normal number."""
+    gg, g = lib(), gen(n)
+    codes, z = codes8(n, k, g), torch.randn(n, m, generator=g).to(tz)
+    sc = torch.exp2(-110 - 12 * torch.rand(n, generator=g))
+    out = torch.empty(m, k, dtype=t, device=DEV)
+    ws = torch.empty(max(gg.gg_ws_product(n, k, m), 16), dtype=torch.uint8, device=DEV)
+    gg.gg_product_backward(gg.make_rows(codes.to(DEV), scales=sc.to(DEV)), n, k, gg.make_rows(z.to(DEV)), m,
+                           gg.make_rows(out), 0, ws)
+    an, z = codes.float().double() * sc.double()[:, None], z.double()
+    want, size = z.t() @ an, z.abs().t() @ an.abs()
+    # (bf16's least number, of which a term's other factor is a multiple, is 2^-133)
+    least = (n + 4) * 2.0 ** -133 * 448 + FLOOR[t]
+    check(out, want, (n + 4) * U * size + 1.01 * PARTS[t] * size + 1.01 * UNIT[t] * want.abs() + least, t)
+
+
 def test_weight_gradient_of_no_rows():
     gg = lib()
     a = gg.make_rows(torch.empty(0, 30, device=DEV).to(E4M3), scales=torch.empty(0, device=DEV))
