@@ -172,7 +172,8 @@ def test_workspaces():
     assert got == sorted(got) and got[-1] == 2 * 1024 * 400
     assert gg.gg_ws_product(-1, 9, 9) == gg.gg_ws_product(9, 0, 9) == gg.gg_ws_product(9, 9, 0) == 0
     for k, m in ((1, 1), (100, 47), (602, 41), (4096, 4096), (9, 1 << 24)):
-        got = [gg.gg_ws_product(n, k, m) for n in (0, 1, 256, 257, 512, 513, 5000, 100_000, 1 << 27)]
+        got = [gg.gg_ws_product(n, k, m) for n in (0, 1, 64, 65, 256, 257, 512, 513, 5000, 100_000, 1 << 27)]
+        # (rows are split 64 at least to a part)
         assert got == sorted(got) and got[2] == 0 and all(x % (4 * k * m) < 256 for x in got)
 
 
