@@ -77,17 +77,22 @@ __device__ __forceinline__ v4i move_down(v4i v, int32_t bytes) {
 }
 
 // 16 bytes of a row's codes from column c on, zeros behind its end: there the row's
-// last 16 bytes are read and moved down.
-__device__ __forceinline__ v4i load_codes(const char* row, int32_t c, int32_t k) {
+// last 16 bytes are read and moved down, with no branch, so that several such loads can
+// be under way before the first is used.  (Of fewer than 16 columns c is 0 or behind them.)
+__device__ __forceinline__ v4i codes_read(const char* row, int32_t c, int32_t k) {
   typedef v4i mem __attribute__((aligned(1)));
-  if (c + 16 <= k) return *(const GG_GLOBAL mem*)(row + c);
-  if (c >= k) return v4i{};
-  if (k >= 16) return move_down(*(const GG_GLOBAL mem*)(row + k - 16), c + 16 - k);
+  if (k >= 16) return *(const GG_GLOBAL mem*)(row + min(c, k - 16));
   uint64_t w[2] = {};
 #pragma unroll 1
-  for (int32_t i = 0; i < k; ++i)               // c is 0
+  for (int32_t i = 0; i < k; ++i)
     w[i / 8] |= (uint64_t) * (const GG_GLOBAL uint8_t*)(row + i) << 8 * (i % 8);
   return v4i{(int)w[0], (int)(w[0] >> 32), (int)w[1], (int)(w[1] >> 32)};
+}
+__device__ __forceinline__ v4i codes_moved(const v4i& v, int32_t c, int32_t k) {
+  return c >= k ? v4i{} : c + 16 <= k || k < 16 ? v : move_down(v, c + 16 - k);
+}
+__device__ __forceinline__ v4i load_codes(const char* row, int32_t c, int32_t k) {
+  return codes_moved(codes_read(row, c, k), c, k);
 }
 
 }  // namespace gg

@@ -250,12 +250,17 @@ __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_
       if constexpr (BYTES)
         load_to_lds4(end_from + (int64_t)g * kBlockK, lds_at(&ends[slot][wave_all * kWave]));
     } else {
-#pragma unroll 1
+      v4i got[kLoads];
+#pragma unroll
       for (int t = 0; t < kLoads; ++t) {
         int64_t off;
         const int32_t r = row_of(t, &off);
-        to[t * kGroup + tid] = load_codes((r < BJ ? jbase : ibase) + off,
-                                          g * kBlockK + (tid % 8 ^ (r >> 1 & 7)) * 16, a.k);
+        got[t] = codes_read((r < BJ ? jbase : ibase) + off, g * kBlockK + (tid % 8 ^ (r >> 1 & 7)) * 16, a.k);
+      }
+#pragma unroll
+      for (int t = 0; t < kLoads; ++t) {
+        const int32_t r = (t * kGroup + tid) / 8;
+        to[t * kGroup + tid] = codes_moved(got[t], g * kBlockK + (tid % 8 ^ (r >> 1 & 7)) * 16, a.k);
       }
     }
     load_to_lds4(scale_from + (int64_t)min(g, a.kb - 1) * scale_step,
@@ -483,12 +488,15 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
     asm volatile("" : "+v"(lane));
     __syncthreads();
     bring_scale(whole, 0);
-#pragma unroll 1
+    const int32_t c = whole * kBlockK + (lane % 8 ^ (lane >> 4 & 7)) * 16;
+    v4i got[8];
+#pragma unroll
     for (int t = 0; t < 8; ++t) {
       const int32_t r = t % 4 * 64 + lane / 8;
-      const char* from = t < 4 ? jbase + min(r, jlast) * a.b.stride : ibase + r * a.a.stride;
-      lds[0][t * kThreads + lane] = load_codes(from, whole * kBlockK + (lane % 8 ^ (lane >> 4 & 7)) * 16, a.k);
+      got[t] = codes_read(t < 4 ? jbase + min(r, jlast) * a.b.stride : ibase + r * a.a.stride, c, a.k);
     }
+#pragma unroll
+    for (int t = 0; t < 8; ++t) lds[0][t * kThreads + lane] = codes_moved(got[t], c, a.k);
     wait();
     read_scales((const float*)scales[0], 1);
     multiply_step<TJ, TI, C>(scale, acc, [&](int x) { return weights(0, x / 16); },
@@ -753,11 +761,13 @@ int launch_product(ProductArgs& a, hipStream_t stream) {
   // badly (16 rows of 4,096 to 4,096 7.4 us, through LDS 8.5; of 8,192 to 8,192 20.1 and 14.8;
   // 64 rows of 4,096 to 1,024 7.3 and 9.6, to 4,096 12.2 and 10.1).
   if (a.n <= 4 || tiles(16, 16) * a.kb <= 8192) return launch_few<O>(a, stream);
-  if (a.n <= 32) return launch_pipe<O, 32, 32, 1, 2, 2, 5>(a, stream);
-  if (a.n <= 64) return launch_pipe<O, 32, 64, 1, 4, 2, 5>(a, stream);
-  if (a.n <= 96) return launch_pipe<O, 32, 96, 2, 2, 2, 3>(a, stream);
-  // The largest tiles that still leave one for each CU (256 rows of 4,096 to 4,096 15.1 in tiles
-  // of 32 x 128, 26.1 in 128 x 128; 1,024 rows 26.4 and 29.2).
+  // The smallest tiles of which there is one for each CU, or that hold all rows (steps of 32 x 32
+  // take 0.33 us, of 32 x 64 0.4, of 32 x 96 and beyond 0.6; 1,076 rows of 7,808 to 384 @ us in
+  // 32 x 64, 22.9 in 32 x 128; 256 rows of 4,096 to 4,096 15.1 in 32 x 128, 26.1 in 128 x 128).
+  const auto fits = [&](int bj, int bi) { return a.n <= bi || tiles(bj, bi) <= 256; };
+  if (fits(32, 32)) return launch_pipe<O, 32, 32, 1, 2, 2, 5>(a, stream);
+  if (fits(32, 64)) return launch_pipe<O, 32, 64, 1, 4, 2, 5>(a, stream);
+  if (fits(32, 96)) return launch_pipe<O, 32, 96, 2, 2, 2, 3>(a, stream);
   if (tiles(32, 128) <= 256) return launch_pipe<O, 32, 128, 1, 4, 2, 3>(a, stream);
   if (tiles(64, 128) <= 256) return launch_pipe<O, 64, 128, 2, 2, 2, 3>(a, stream);
   if (tiles(128, 128) <= 256) return launch_pipe<O, 128, 128, 2, 2, 2, 2>(a, stream);

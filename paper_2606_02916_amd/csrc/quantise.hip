@@ -199,13 +199,17 @@ __global__ void __launch_bounds__(kBlock) k_blocks_codes(BlocksArgs a) {
   const char* x = a.x.p + r0 * a.x.stride + (c0 + c) * (int64_t)sizeof(T);
   float v[kSteps][V];
   uint32_t top = 0;
-  if (nr == kScaleBlock && nc == kScaleBlock) {
-    typename Raw<T, V>::vec raw[kSteps];
+  // (the lanes whose piece the last column cuts read it by elements)
+  typename Raw<T, V>::vec raw[kSteps] = {};
+  const bool cut = c < nc && c + V > nc;
+  if (c + V <= nc) {
 #pragma unroll
-    for (int t = 0; t < kSteps; ++t) raw[t] = raw_load<T, V>(x + (t * kStep + r) * a.x.stride);
+    for (int t = 0; t < kSteps; ++t)
+      if (t * kStep + r < nr) raw[t] = raw_load<T, V>(x + (t * kStep + r) * a.x.stride);
+  }
 #pragma unroll
-    for (int t = 0; t < kSteps; ++t) to_f32<T, V>(raw[t], v[t]);
-  } else {
+  for (int t = 0; t < kSteps; ++t) to_f32<T, V>(raw[t], v[t]);
+  if (cut) {
 #pragma unroll
     for (int t = 0; t < kSteps; ++t)
 #pragma unroll

@@ -120,7 +120,8 @@ def test_product_at_aligned_places(n, k, m, group, t):
 
 
 @pytest.mark.parametrize("n,k,m", [(10, 4104, 4100), (20, 4100, 2050), (50, 2104, 2100), (64, 2048, 2048),
-                                   (90, 2000, 1500), (200, 1304, 1000), (700, 300, 1700), (700, 256, 1700),
+                                   (90, 2000, 1500), (90, 1100, 9000), (200, 1304, 1000),
+                                   (500, 520, 1000), (700, 520, 1000), (1000, 520, 1000), (700, 300, 1700), (700, 256, 1700),
                                    (2000, 300, 1900), (2000, 388, 1901), (2100, 260, 2200), (2100, 256, 2201)])
 @pytest.mark.parametrize("a_at,b_at", [((1, 3), (2, 5)), ((4, 4), (8, 8)), ((0, 0), (1, 1)), ((3, 2), (0, 0)),
                                        ((4, 12), (0, 0))])
