@@ -66,24 +66,30 @@ __device__ __forceinline__ v4f multiply(const Codes<true>& a, const Codes<true>&
   return d;
 }
 
-// Four columns of a row of the output.
-template <typename O>
-__device__ __forceinline__ void store_four(const KRows& out, int64_t i, int32_t j, int32_t m, v4f v) {
-  char* to = out.p + i * out.stride + j * (int64_t)sizeof(O);
-  const float f[4] = {v[0], v[1], v[2], v[3]};
-  if (j + 4 <= m) {
-    row_store<O, 4>(to, f);
-  } else {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const float one[1] = {f[r]};
-      if (j + r < m) row_store<O, 1>(to + r * sizeof(O), one);
-    }
-  }
+// Which of a wave's weights' rows a lane multiplies: of each 16 G rows, G products take four of
+// every 4 G, so that a lane ends with 4 G columns side by side of a row of the output, and a
+// row's four lanes with 16 G: whole cache lines in 16 bits with G = 4 (8,191 x 4,096 to 16,384
+// 521 us, with G = 1 540; 10,610 of 128 to 36,776 200 and 254).
+template <typename O, int TJ>
+constexpr int kSide = sizeof(O) == 4 ? 1 : TJ < 4 ? TJ : 4;
+
+template <int G>
+__device__ __forceinline__ int32_t lane_row(int32_t l) {
+  return l % 16 / 4 * (4 * G) + l % 4;
+}
+template <int G>
+__device__ __forceinline__ constexpr int32_t product_row(int u) {
+  return u / G * (16 * G) + u % G * 4;
+}
+// Where a row's pieces are in LDS: piece c in place c ^ key.  The sixteen rows of a product have
+// each key twice, in rows of 128 bytes of either half of the banks.
+template <int G>
+__device__ __forceinline__ int32_t row_key(int32_t r) {
+  return (r >> 1 & 1) | (r / (4 * G) & 3) << 1;
 }
 
-// A lane's codes of a row in LDS: its pieces q and q + 4, q = l / 16, where rows keep piece
-// c in place c ^ (row / 2 & 7).  Rows 16 apart are alike.  The sixteen lanes that LDS
+// A lane's codes of a row in LDS: its pieces q and q + 4, q = l / 16.  Its rows have one key,
+// l / 2 & 7.  The sixteen lanes that LDS
 // serves at a time are 0-3, 12-15, 20-23 and 24-27, and their like: eight rows' piece q and the
 // other eight's piece q ^ 1, all in different banks.  (With pieces 2 q and 2 q + 1 the
 // same reads take twice as long.)
@@ -147,17 +153,59 @@ __device__ __forceinline__ void multiply_step(const float (&scale)[TI], v4f (&ac
   }
 }
 
-template <typename O, int TJ, int TI>
+// Sixteen numbers of two bytes to any multiple of two: stores of 16 bytes that begin inside a
+// word are split by the memory, and so between a first and a last number go words
+// (10,239 rows of 114 to 53,277 fp16 450 us, 531 without).
+template <typename O>
+__device__ __forceinline__ void store_run(char* to, const float (&f)[16]) {
+  typedef uint32_t w4 __attribute__((ext_vector_type(4), aligned(4)));
+  typedef uint32_t w3 __attribute__((ext_vector_type(3), aligned(4)));
+  typedef O two __attribute__((ext_vector_type(2)));
+  uint32_t w[8];
+#pragma unroll
+  for (int x = 0; x < 8; ++x) w[x] = __builtin_bit_cast(uint32_t, two{(O)f[2 * x], (O)f[2 * x + 1]});
+  if ((uintptr_t)to & 2) {
+    uint32_t v[7];
+#pragma unroll
+    for (int x = 0; x < 7; ++x) v[x] = __builtin_amdgcn_alignbyte(w[x + 1], w[x], 2);
+    *(GG_GLOBAL uint16_t*)to = (uint16_t)w[0];
+    *(GG_GLOBAL w4*)(to + 2) = w4{v[0], v[1], v[2], v[3]};
+    *(GG_GLOBAL w3*)(to + 18) = w3{v[4], v[5], v[6]};
+    *(GG_GLOBAL uint16_t*)(to + 30) = (uint16_t)(w[7] >> 16);
+  } else {
+    *(GG_GLOBAL w4*)to = w4{w[0], w[1], w[2], w[3]};
+    *(GG_GLOBAL w4*)(to + 16) = w4{w[4], w[5], w[6], w[7]};
+  }
+}
+
+// A wave's sums, G products' columns side by side.
+template <typename O, int G, int TJ, int TI>
 __device__ __forceinline__ void store_tile(const ProductArgs& a, int64_t i0, int32_t j0, int32_t l,
                                            const v4f (&acc)[TJ][TI], int64_t first = 0) {
+  constexpr int kRun = 4 * G;                    // columns of a lane
 #pragma unroll
   for (int t = 0; t < TI; ++t) {
     const int64_t i = i0 + t * 16 + l % 16;
     if (i < first || i >= a.n) continue;
+    char* const row = a.out.p + i * a.out.stride;
 #pragma unroll
-    for (int u = 0; u < TJ; ++u) {
-      const int32_t j = j0 + u * 16 + l / 16 * 4;
-      if (j < a.m) store_four<O>(a.out, i, j, a.m, acc[u][t]);
+    for (int u = 0; u < TJ; u += G) {
+      const int32_t j = j0 + product_row<G>(u) + l / 16 * kRun;
+      float f[kRun];
+#pragma unroll
+      for (int x = 0; x < kRun; ++x) f[x] = acc[u + x / 4][t][x % 4];
+      if (j + kRun <= a.m) {
+        if constexpr (kRun == 16)
+          store_run<O>(row + j * (int64_t)sizeof(O), f);
+        else
+          row_store<O, kRun>(row + j * (int64_t)sizeof(O), f);
+      } else {
+#pragma unroll
+        for (int x = 0; x < kRun; ++x) {
+          const float one[1] = {f[x]};
+          if (j + x < a.m) row_store<O, 1>(row + (j + x) * (int64_t)sizeof(O), one);
+        }
+      }
     }
   }
 }
@@ -180,7 +228,7 @@ template <typename O, int BJ, int BI, int WJ, int WI, int WK, int STAGES, bool B
 __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_pipe(ProductArgs a) {
   constexpr int kThreads = WJ * WI * WK * kWave, kGroup = kThreads / WK, kPieces = (BJ + BI) * 8,
                 kLoads = kPieces * WK / kThreads, kBlocksJ = (BJ + kScaleBlock - 1) / kScaleBlock;
-  constexpr int TJ = BJ / WJ / 16, TI = BI / WI / 16;
+  constexpr int TJ = BJ / WJ / 16, TI = BI / WI / 16, G = kSide<O, TJ>;
   static_assert(kPieces % kGroup == 0, "whole loads");
   static_assert(BJ / WJ <= kScaleBlock && kScaleBlock % (BJ / WJ) == 0, "one block of weights a wave");
   static_assert(BI + kBlocksJ <= kGroup, "a lane for each scale");
@@ -205,6 +253,7 @@ __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_
   const char* const jbase = a.b.p + j0 * a.b.stride;
   const char* const ibase = a.a.p + i0 * a.a.stride;
   const int32_t jlast = min(a.m - j0, BJ) - 1, ilast = (int32_t)min(a.n - i0, (int64_t)BI) - 1;
+  const auto piece_of = [&](int32_t r) { return (tid % 8 ^ (r < BJ ? row_key<G>(r) : row_key<1>(r))) * 16; };
   const auto row_of = [&](int t, int64_t* off) {
     const int32_t r = (t * kGroup + tid) / 8;
     *off = r < BJ ? min(r, jlast) * a.b.stride : min(r - BJ, ilast) * a.a.stride;
@@ -217,7 +266,7 @@ __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_
   for (int t = 0; t < kLoads; ++t) {
     int64_t off;
     const int32_t r = row_of(t, &off);
-    from[t] = ((uint32_t)off + (r < BJ ? jskip : iskip) & (BYTES ? ~3u : ~0u)) + (tid % 8 ^ (r >> 1 & 7)) * 16;
+    from[t] = ((uint32_t)off + (r < BJ ? jskip : iskip) & (BYTES ? ~3u : ~0u)) + piece_of(r);
   }
   // and of row tid the word with the last byte of a block
   const char* end_from = nullptr;
@@ -255,20 +304,20 @@ __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_
       for (int t = 0; t < kLoads; ++t) {
         int64_t off;
         const int32_t r = row_of(t, &off);
-        got[t] = codes_read((r < BJ ? jbase : ibase) + off, g * kBlockK + (tid % 8 ^ (r >> 1 & 7)) * 16, a.k);
+        got[t] = codes_read((r < BJ ? jbase : ibase) + off, g * kBlockK + piece_of(r), a.k);
       }
 #pragma unroll
       for (int t = 0; t < kLoads; ++t) {
         const int32_t r = (t * kGroup + tid) / 8;
-        to[t * kGroup + tid] = codes_moved(got[t], g * kBlockK + (tid % 8 ^ (r >> 1 & 7)) * 16, a.k);
+        to[t * kGroup + tid] = codes_moved(got[t], g * kBlockK + piece_of(r), a.k);
       }
     }
     load_to_lds4(scale_from + (int64_t)min(g, a.kb - 1) * scale_step,
                  lds_at(&scales[slot][wave_all * kWave]));
   };
 
-  // bytes before this lane's rows, the same for rows 16 apart
-  const int32_t wrow = wj * TJ * 16 + l % 16, rrow = wi * TI * 16 + l % 16;
+  // bytes before this lane's rows, the same for all of them, which are fours apart
+  const int32_t wrow = wj * TJ * 16 + lane_row<G>(l), rrow = wi * TI * 16 + l % 16;
   const uint32_t wskip = jskip + (uint32_t)wrow * (uint32_t)a.b.stride,
                  rskip = iskip + (uint32_t)rrow * (uint32_t)a.a.stride;
   v4f acc[TJ][TI] = {};
@@ -295,10 +344,10 @@ __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_
         // (a step at k's end has its codes in place)
         const uint32_t ws = s < whole ? wskip : 0, rs = s < whole ? rskip : 0;
         multiply_step<TJ, TI, C>(scale, acc,
-                                 [&](int x) { return operand_of_words<C>(w + x * 8, we + x, ws, l); },
+                                 [&](int x) { return operand_of_words<C>(w + product_row<G>(x / 16) * 8, we + product_row<G>(x / 16), ws, l); },
                                  [&](int x) { return operand_of_words<C>(r + x * 8, re + x, rs, l); });
       } else {
-        multiply_step<TJ, TI, C>(scale, acc, [&](int x) { return operand<C>(w + x * 8, l); },
+        multiply_step<TJ, TI, C>(scale, acc, [&](int x) { return operand<C>(w + product_row<G>(x / 16) * 8, l); },
                                  [&](int x) { return operand<C>(r + x * 8, l); });
       }
     }
@@ -322,18 +371,18 @@ __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_
     }
     if (wk) return;
   }
-  store_tile<O, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc);
+  store_tile<O, G, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc);
 }
 
 // Tiles of 256 x 256 of rows that begin with words, two blocks of k in LDS.  One wait a block, before its last quarter of
 // products: the next block has been on its way since the same place in the block before,
 // and its first operands are read into the registers that the last products leave.
-// 8,191 x 4,096 to 16,384 bf16 take 537 us, 2,050 TFLOP/s.  Without the loads 446, without
+// 8,191 x 4,096 to 16,384 bf16 take 521 us, 2,110 TFLOP/s.  Without the loads 446, without
 // the scaling too 405: products, their scaling and LDS's reads do not quite overlap (a
 // wave's products alone would be 240), and the loads' requests come on top.
 template <typename O>
 __global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
-  constexpr int BJ = 256, BI = 256, WJ = 2, WI = 4, TJ = BJ / WJ / 16, TI = BI / WI / 16, kThreads = 512;
+  constexpr int BJ = 256, BI = 256, WJ = 2, WI = 4, TJ = BJ / WJ / 16, TI = BI / WI / 16, G = kSide<O, TJ>, kThreads = 512;
   typedef Codes<false> C;
   __shared__ v4i lds[2][(BJ + BI) * 8];
   __shared__ v4f scales[2][kThreads];
@@ -352,12 +401,13 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
   const char* const jbase = a.b.p + j0 * a.b.stride;
   const char* const ibase = a.a.p + i0 * a.a.stride;
   const int32_t jlast = min(a.m - j0, BJ) - 1;
-  const int32_t piece = (tid % 8 ^ (tid >> 4 & 7)) * 16;
+  // (rows 64 apart have one key)
+  const int32_t jpiece = (tid % 8 ^ row_key<G>(tid / 8)) * 16, ipiece = (tid % 8 ^ row_key<1>(tid / 8)) * 16;
   uint32_t jfrom[4];
 #pragma unroll
   for (int t = 0; t < 4; ++t)
-    jfrom[t] = (uint32_t)min(t * 64 + tid / 8, jlast) * (uint32_t)a.b.stride + piece;
-  const uint32_t ifrom = (uint32_t)(tid / 8) * (uint32_t)a.a.stride + piece;
+    jfrom[t] = (uint32_t)min(t * 64 + tid / 8, jlast) * (uint32_t)a.b.stride + jpiece;
+  const uint32_t ifrom = (uint32_t)(tid / 8) * (uint32_t)a.a.stride + ipiece;
   // its scale: a row's, or behind them a block's of weights
   const bool of_row = tid < BI;
   const char* const scale_from =
@@ -403,7 +453,7 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
   float scale[TI], held[2] = {};
   v4f d[3] = {};                      // products whose sums are not scaled yet
   const auto weights = [&](int buf, int u) {
-    return operand<C>(lds[buf] + (wj * TJ * 16 + l % 16) * 8 + u * 128, l);
+    return operand<C>(lds[buf] + (wj * TJ * 16 + lane_row<G>(l) + product_row<G>(u)) * 8, l);
   };
   const auto row = [&](int buf, int t) {
     return operand<C>(lds[buf] + (BJ + wi * TI * 16 + l % 16) * 8 + t * 128, l);
@@ -488,21 +538,23 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
     asm volatile("" : "+v"(lane));
     __syncthreads();
     bring_scale(whole, 0);
-    const int32_t c = whole * kBlockK + (lane % 8 ^ (lane >> 4 & 7)) * 16;
+    const auto column_of = [&](int t) {
+      return whole * kBlockK + (lane % 8 ^ (t < 4 ? row_key<G>(lane / 8) : row_key<1>(lane / 8))) * 16;
+    };
     v4i got[8];
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
       const int32_t r = t % 4 * 64 + lane / 8;
-      got[t] = codes_read(t < 4 ? jbase + min(r, jlast) * a.b.stride : ibase + r * a.a.stride, c, a.k);
+      got[t] = codes_read(t < 4 ? jbase + min(r, jlast) * a.b.stride : ibase + r * a.a.stride, column_of(t), a.k);
     }
 #pragma unroll
-    for (int t = 0; t < 8; ++t) lds[0][t * kThreads + lane] = codes_moved(got[t], c, a.k);
+    for (int t = 0; t < 8; ++t) lds[0][t * kThreads + lane] = codes_moved(got[t], column_of(t), a.k);
     wait();
     read_scales((const float*)scales[0], 1);
     multiply_step<TJ, TI, C>(scale, acc, [&](int x) { return weights(0, x / 16); },
                              [&](int x) { return row(0, x / 16); });
   }
-  store_tile<O, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc, i0 + skip);
+  store_tile<O, G, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc, i0 + skip);
 }
 
 // Tiles of matrices with more than 2^23 bytes from a row to the next: blocks come through
@@ -576,7 +628,7 @@ __global__ void __launch_bounds__(WJ* WI* kWave, sizeof(O) == 4 ? 1 : 2) k_produ
                              [&](int x) { return operand<C>(r + x * 8, l); });
     if (more) keep(buf ^ 1);
   }
-  store_tile<O, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc);
+  store_tile<O, 1, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc);
 }
 
 // Few rows: operands go from memory to registers, without LDS.  A block has 16 weights' rows
@@ -687,7 +739,7 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) k_product_few(ProductArgs
     __syncthreads();
     if (wave < half) acc[0][0] += lds[wave][l];
   }
-  if (wave == 0) store_tile<O, 1, 1>(a, i0, j0, l, acc);
+  if (wave == 0) store_tile<O, 1, 1, 1>(a, i0, j0, l, acc);
 }
 
 int tiles_of(ProductArgs& a, int bj, int bi) {
@@ -762,7 +814,7 @@ int launch_product(ProductArgs& a, hipStream_t stream) {
   // 64 rows of 4,096 to 1,024 7.3 and 9.6, to 4,096 12.2 and 10.1).
   if (a.n <= 4 || tiles(16, 16) * a.kb <= 8192) return launch_few<O>(a, stream);
   // The smallest tiles of which there is one for each CU, or that hold all rows (steps of 32 x 32
-  // take 0.33 us, of 32 x 64 0.4, of 32 x 96 and beyond 0.6; 1,076 rows of 7,808 to 384 @ us in
+  // take 0.33 us, of 32 x 64 0.4, of 32 x 96 and beyond 0.6; 1,076 rows of 7,808 to 384 17.0 us in
   // 32 x 64, 22.9 in 32 x 128; 256 rows of 4,096 to 4,096 15.1 in 32 x 128, 26.1 in 128 x 128).
   const auto fits = [&](int bj, int bi) { return a.n <= bi || tiles(bj, bi) <= 256; };
   if (fits(32, 32)) return launch_pipe<O, 32, 32, 1, 2, 2, 5>(a, stream);
@@ -772,9 +824,10 @@ int launch_product(ProductArgs& a, hipStream_t stream) {
   if (tiles(64, 128) <= 256) return launch_pipe<O, 64, 128, 2, 2, 2, 3>(a, stream);
   if (tiles(128, 128) <= 256) return launch_pipe<O, 128, 128, 2, 2, 2, 2>(a, stream);
   // A round of 256 of 256 x 256 takes 1.4 to 1.85 times one of 512 of 128 x 128 (8,192 and 2,048
-  // columns), and does twice as much.
+  // columns), and does twice as much.  Of few blocks of k its stores, with no other block on
+  // the CU, are waited for (10,239 rows to 53,277, k 512: 663 and 642, 1,024: 912 and 928).
   if constexpr (sizeof(O) == 2)
-    if (words && a.n >= 256 && cdiv(tiles(256, 256), 256) * 8 <= cdiv(tiles(128, 128), 512) * 5)
+    if (words && a.kb > 4 && a.n >= 256 && cdiv(tiles(256, 256), 256) * 8 <= cdiv(tiles(128, 128), 512) * 5)
       return launch_wide<O>(a, stream);
   return launch_pipe<O, 128, 128, 2, 2, 1, 2>(a, stream);
 }
