@@ -708,8 +708,8 @@ int gg_quantise_blocks(const gg_rows_t* w, int64_t rows, int64_t cols, const gg_
  * (codes below 2^-6 counting as that): some 2^-16 of a result, at twice the rate.  The
  * gradient of the rows is the same call on the output's gradient in 8 bits and the
  * transposed weights (gg_quantise_rows, gg_quantise_blocks).  out is no memory of a or b.
- * Rows may begin at any byte; those that begin with a word take two thirds of the time,
- * and of rows that begin at multiples of 16 bytes the fewest cache lines are read. */
+ * Rows may begin at any byte (the words that hold a row's bytes are read whole); those that
+ * begin with a word take two thirds of the time. */
 int gg_product_forward(const gg_rows_t* a, int64_t n, int64_t k, const gg_blocks_t* b, int64_t m,
                        const gg_rows_t* out, hipStream_t stream);
 
