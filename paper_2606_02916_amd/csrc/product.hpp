@@ -1,5 +1,5 @@
-// What the product of 8-bit rows and its gradient share: tiles' places, and loads from
-// memory to LDS.
+// What the product of 8-bit rows, its gradient and the weights' quantiser share: tiles'
+// places, and loads from memory to LDS.
 #pragma once
 
 #include <type_traits>

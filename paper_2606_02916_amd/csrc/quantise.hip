@@ -1,6 +1,6 @@
 // Rows and weights into 8 bits: a scale for each group of a row's elements, or
 // for each 128 x 128 elements of the weights, which may leave transposed too.
-#include "codes.hpp"
+#include "product.hpp"
 
 namespace gg {
 namespace {
@@ -176,23 +176,27 @@ struct BlocksArgs {
   KRows x;
   KBlocks q, qt;               // p == nullptr: absent
   int64_t rows, cols;
-  int32_t across;              // blocks in a row of them
+  int32_t down, across;        // blocks
+  bool shared;                 // a cache line holds codes or numbers of two blocks
 };
 
 // A workgroup per 128 x 128 elements, which stay in registers between the largest
 // magnitude and the codes; the transposed codes go through LDS, four by four bytes
-// at a time.  Bound by memory: 16,384 x 4,096 fp32, both ways, 83 us, 4.9 TB/s; rows and
-// columns at odd bytes, whose 4-byte stores are split, take twice as long (8,191 x
-// 4,095 bf16 61 us, 8,192 x 4,096 25).
+// at a time.  Bound by memory: 16,384 x 4,096 fp32, both ways, 83 us, 4.9 TB/s.  Blocks
+// whose edges lie inside cache lines are dealt in bands of rows to the XCDs, or else
+// lines go to memory in parts (8,191 x 4,095 bf16 36 us, in the order of rows 57; 8,192 x
+// 4,096 24 in that order, 26 in bands).
 template <typename T>
 __global__ void __launch_bounds__(kBlock) k_blocks_codes(BlocksArgs a) {
   constexpr int V = kVec<T>, kLanes = kScaleBlock / V, kStep = kBlock / kLanes,
                 kSteps = kScaleBlock / kStep, kPitch = kScaleBlock + 4;
   __shared__ uint32_t tile[kScaleBlock * kPitch / 4];
   __shared__ uint32_t tops[kBlock / kWave];
+  // Neighbours that share lines run on one XCD, at about one time.
   const int64_t b = block_index();
-  const int64_t rb = b / a.across, cb = b - rb * a.across;
-  const int64_t r0 = rb * kScaleBlock, c0 = cb * kScaleBlock;
+  int32_t rb = (int32_t)(b / a.across), cb = (int32_t)(b - (int64_t)rb * a.across);
+  if (a.shared) tile_place(a.down, a.across, &rb, &cb);
+  const int64_t r0 = (int64_t)rb * kScaleBlock, c0 = (int64_t)cb * kScaleBlock;
   const int32_t nr = (int32_t)min((int64_t)kScaleBlock, a.rows - r0),
                 nc = (int32_t)min((int64_t)kScaleBlock, a.cols - c0);
   const int32_t c = (int32_t)threadIdx.x % kLanes * V, r = (int32_t)threadIdx.x / kLanes;
@@ -342,7 +346,10 @@ extern "C" int gg_quantise_blocks(const gg_rows_t* w, int64_t rows, int64_t cols
   a.rows = rows;
   a.cols = cols;
   a.across = (int32_t)cdiv(cols, kScaleBlock);
-  const dim3 grid = grid_of(cdiv(rows, kScaleBlock) * a.across);
+  a.down = (int32_t)cdiv(rows, kScaleBlock);
+  const dim3 grid = grid_of((int64_t)a.down * a.across);
+  a.shared = grid.y == 1 && ((uintptr_t)a.x.p | (uintptr_t)a.x.stride | (uintptr_t)a.q.p | (uintptr_t)a.q.stride |
+                             (uintptr_t)a.qt.p | (uintptr_t)a.qt.stride) % kScaleBlock != 0;
   GG_FOR_FLOAT(w->dtype, T, {
     hipLaunchKernelGGL((k_blocks_codes<T>), grid, dim3(kBlock), 0, stream, a);
   });
