@@ -476,49 +476,47 @@ __global__ void __launch_bounds__(kJoinWaves* kWave) k_product_join(GradArgs a) 
 
 // Which kernel and how many splits of the rows: the least of a sum of measured
 // microseconds, with as many splits as fill the chip or a power of two, whose blocks
-// go evenly to its parts.  A step of 32 rows takes a block of 128 x 128 alone on its CU 0.5, 0.8 and
-// 1.15 with one, two and three parts, a block of 64 columns of dz 0.38, 0.55 and 0.73; two on a
-// CU take 1.35 and three 1.85 times as long for each.  The wide kernel, one block on a CU,
-// takes 1.4 for 64 rows while half the chip has none and 1.75 behind that, and 8 more to
-// begin and end.  Splits cost a second launch, 4, and their sums' way to memory and back at 6.5
-// MB/us.  (bf16, 1,024 rows: 4,096 x 4,096 45 us wide, 50 in tiles of 128; 2,048 x 2,048 22
-// in tiles of 128 of all rows, 34 in two splits or wide; 512 rows, 1,024 x 1,024 12 and 21.
-// 233,000 rows of 602 x 41 fp32 78 with 768 blocks, 81 with 512.)
+// go evenly to its parts.  A step of 32 rows takes a block of 128 x 128 alone on its CU 0.5,
+// 0.8 and 1.15 with one, two and three parts, a block of 64 columns of dz 0.38, 0.55 and 0.73;
+// two on a CU take 1.35 and three 1.85 times as long for each.  The wide kernel, one block
+// on a CU, takes 1.4 for 64 rows while half the chip has none and 1.75 behind that, and 8 more
+// to begin and end.  Splits cost a second launch, 4, and their sums' way to memory and
+// back at 6.5 MB/us.  (bf16, 1,024 rows: 4,096 x 4,096 45 us wide, 50 in tiles of 128; 2,048
+// x 2,048 22 in tiles of 128 of all rows, 34 in two splits or wide; 512 rows of
+// 1,024 x 1,024 9 in tiles of 64, 12 of 128, 21 wide.  233,000 rows of 602 x 41 fp32 78 with 768 blocks, 81 with 512.)
 struct GradShape {
-  int bj;
+  int bj;                      // kWideJ: the wide kernel
   int64_t tiles_k, tiles_j, splits;
   float cost;
 };
 
-GradShape tiles_of(int64_t k, int64_t m, bool wide) {
-  GradShape s = {};
-  s.bj = wide ? kWideJ : m <= 64 || k < 16 ? 64 : 128;
-  s.tiles_k = cdiv(k, wide ? kWideK : kTileK);
-  s.tiles_j = cdiv(m, s.bj);
-  return s;
+GradShape tiles_of(int64_t k, int64_t m, int bj) {
+  return {bj, cdiv(k, bj == kWideJ ? kWideK : kTileK), cdiv(m, bj), 0, 0.0f};
 }
+
+int blocks_on_a_cu(int bj) { return bj == kWideJ ? 1 : bj == 128 ? 2 : 3; }
 
 // as many as fill the chip's 256 CUs, of 64 rows at least
 int64_t most_splits(const GradShape& s, int64_t n) {
-  const int64_t blocks = s.bj == kWideJ ? 256 : s.bj == 64 ? 768 : 512;
+  const int64_t blocks = 256 * blocks_on_a_cu(s.bj);
   return std::max<int64_t>(1, std::min(blocks / (s.tiles_k * s.tiles_j), cdiv(n, kWideI)));
 }
 
-GradShape shape_of(int64_t n, int64_t k, int64_t m, int parts, bool wide) {
+GradShape shape_of(int64_t n, int64_t k, int64_t m, int parts, int bj) {
   static constexpr float kStep[2][3] = {{0.38f, 0.55f, 0.73f}, {0.5f, 0.8f, 1.15f}},
-                         kShared[3] = {1.0f, 1.35f, 1.85f};
-  GradShape best = tiles_of(k, m, wide);
-  const int64_t tiles = best.tiles_k * best.tiles_j, held = wide ? 1 : best.bj == 64 ? 3 : 2;
-  for (int64_t most = most_splits(best, n), s = most, next = 1; s; s = next / 2) {
+                         kShared[4] = {0.0f, 1.0f, 1.35f, 1.85f};
+  GradShape best = tiles_of(k, m, bj);
+  const int64_t tiles = best.tiles_k * best.tiles_j, held = blocks_on_a_cu(bj);
+  for (int64_t s = most_splits(best, n), next = 1; s; s = next / 2) {
     for (next = 1; next < s;) next *= 2;
-    const int64_t blocks = tiles * s, chunk = cdiv(n, s);
-    const float rounds = (float)cdiv(blocks, 256 * held);
+    const int64_t blocks = tiles * s, chunk = cdiv(n, s), rounds = blocks / (256 * held),
+                  rest = blocks % (256 * held);
     float cost;
-    if (wide)
-      cost = 8 + rounds * cdiv(chunk, kWideI) * (blocks <= 128 ? 1.4f : 1.75f);
+    if (bj == kWideJ)
+      cost = 8 + (rounds + (rest > 0)) * cdiv(chunk, kWideI) * (blocks <= 128 ? 1.4f : 1.75f);
     else
-      cost = rounds * cdiv(chunk, kTileI) * kStep[best.bj == 128][parts - 1] *
-             kShared[std::min(cdiv(blocks, 256), held) - 1];
+      cost = (rounds * kShared[held] + kShared[cdiv(rest, 256)]) * cdiv(chunk, kTileI) *
+             kStep[bj == 128][parts - 1];
     if (s > 1) cost += 4 + (float)s * m * k * (8 / 6.5e6f);
     if (best.splits && cost >= best.cost) continue;
     best.splits = s;
@@ -529,23 +527,23 @@ GradShape shape_of(int64_t n, int64_t k, int64_t m, int parts, bool wide) {
 
 template <typename Z, typename O, int PARTS>
 int launch_grad(GradArgs& a, hipStream_t stream) {
-  GradShape s = shape_of(a.n, a.k, a.m, PARTS, false);
+  GradShape s = shape_of(a.n, a.k, a.m, PARTS, 64);
+  const auto or_else = [&](int bj) {
+    const GradShape t = shape_of(a.n, a.k, a.m, PARTS, bj);
+    if (t.cost < s.cost) s = t;
+  };
+  if (a.m > 64 && a.k >= 16) or_else(128);
   // (the wide kernel moves whole pieces of 16 bytes of the gradients, with offsets of 32 bits)
-  bool wide = std::is_same<Z, bf16>::value && std::is_same<O, bf16>::value && a.m % 8 == 0 &&
-              a.m >= 128 && a.k >= 128 && a.n >= 128 && aligned16(a.dz.p) &&
-              a.dz.stride % 16 == 0 && a.dz.stride <= 1 << 25;
-  if (wide) {
-    const GradShape w = shape_of(a.n, a.k, a.m, PARTS, true);
-    wide = w.cost < s.cost;
-    if (wide) s = w;
-  }
+  if (std::is_same<Z, bf16>::value && std::is_same<O, bf16>::value && a.m % 8 == 0 && a.m >= 128 &&
+      a.k >= 128 && a.n >= 128 && aligned16(a.dz.p) && a.dz.stride % 16 == 0 && a.dz.stride <= 1 << 25)
+    or_else(kWideJ);
   a.tiles_k = (int32_t)s.tiles_k;
   a.tiles_j = (int32_t)s.tiles_j;
   a.splits = (int32_t)s.splits;
   a.chunk = align_up(cdiv(a.n, s.splits), kWideI);
   if (s.splits == 1) a.part = nullptr;
   const dim3 grid((unsigned)(s.tiles_k * s.tiles_j), (unsigned)s.splits);
-  if (wide)
+  if (s.bj == kWideJ)
     hipLaunchKernelGGL(k_product_grad_wide, grid, dim3(512), 0, stream, a);
   else if (a.m < kVec<Z> || a.k < 16)
     hipLaunchKernelGGL((k_product_grad<Z, O, PARTS, 64, true>), grid, dim3(kBlock), 0, stream, a);
@@ -576,7 +574,9 @@ static bool grad_sizes(int64_t n, int64_t k, int64_t m) {
 
 extern "C" size_t gg_ws_product(int64_t n, int64_t k, int64_t m) {
   if (!grad_sizes(n, k, m)) return 0;
-  const int64_t splits = std::max(most_splits(tiles_of(k, m, false), n), most_splits(tiles_of(k, m, true), n));
+  // (whichever tiles are taken)
+  int64_t splits = 1;
+  for (const int bj : {64, 128, kWideJ}) splits = std::max(splits, most_splits(tiles_of(k, m, bj), n));
   return splits > 1 ? align_up((size_t)splits * m * k * sizeof(float), 256) : 0;
 }
 

@@ -122,7 +122,8 @@ def test_product_at_aligned_places(n, k, m, group, t):
 @pytest.mark.parametrize("n,k,m", [(10, 4104, 4100), (20, 4100, 2050), (50, 2104, 2100), (64, 2048, 2048),
                                    (90, 2000, 1500), (90, 1100, 9000), (200, 1304, 1000),
                                    (500, 520, 1000), (700, 520, 1000), (1000, 520, 1000), (700, 300, 1700), (700, 256, 1700),
-                                   (2000, 300, 1900), (2000, 388, 1901), (2100, 260, 2200), (2100, 256, 2201)])
+                                   (2000, 300, 1900), (2000, 388, 1901), (2100, 260, 2200), (2100, 256, 2201), (2200, 700, 4000),
+                                   (2200, 768, 4001)])
 @pytest.mark.parametrize("a_at,b_at", [((1, 3), (2, 5)), ((4, 4), (8, 8)), ((0, 0), (1, 1)), ((3, 2), (0, 0)),
                                        ((4, 12), (0, 0))])
 def test_product_wherever_rows_begin(n, k, m, a_at, b_at):
@@ -290,6 +291,27 @@ def grad_case(n, k, m, tz, t, group, add=False, lead=1, pad=3, dz=None):
     return dw, want, bound
 
 
+def grad_on_device(n, k, m, tz, t, group, add, z_at):
+    """The same of larger sizes, the 64-bit products on the device."""
+    gg, g = lib(), gen(n, k, m)
+    a, an, _ = some_rows(n, k, group, g)
+    z = torch.randn(n, m, generator=g).to(tz)
+    zd = like(n, m, tz, DEV, lead=z_at[0], pad=z_at[1])[0]
+    zd.copy_(z)
+    dw, flat, own = like(m, k, t, DEV, lead=1, pad=3)
+    old = (torch.randn(m, k, generator=g) * 8).to(t)
+    if add:
+        dw.copy_(old)
+    ws = torch.full((max(gg.gg_ws_product(n, k, m), 16),), 0xFF, dtype=torch.uint8, device=DEV)
+    gg.gg_product_backward(a, n, k, gg.make_rows(zd), m, gg.make_rows(dw),
+                           gg.GG_PRODUCT_ADD if add else 0, ws)
+    assert untouched(flat, own)
+    z, an, old = z.to(DEV).double(), an.to(DEV), (old.to(DEV).double() if add else 0)
+    want, size = z.t().contiguous() @ an + old, z.abs().t().contiguous() @ an.abs() + abs(old)
+    bound = (n + 4) * U * size + 1.01 * PARTS[t] * size + 1.01 * UNIT[t] * want.abs() + FLOOR[t]
+    check(dw, want.cpu(), bound.cpu(), t)
+
+
 @pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 100, 257, 1000])
 @pytest.mark.parametrize("k", [1, 7, 100, 128, 129, 200, 602])
 @pytest.mark.parametrize("m", [1, 5, 47, 64, 65, 130, 333])
@@ -314,23 +336,14 @@ def test_weight_gradient_at_aligned_places(n, k, m, group, tz, t, add):
 def test_weight_gradient_with_work_for_every_cu(n, k, m, group, add):
     """bf16 gradients whose rows lie on 16-byte boundaries, and products enough for large
     tiles; codes and results at odd places."""
-    gg, g = lib(), gen(n, k, m)
-    a, an, _ = some_rows(n, k, group, g)
-    z = torch.randn(n, m, generator=g).to(BF16)
-    zd = like(n, m, BF16, DEV, lead=8, pad=8)[0]
-    zd.copy_(z)
-    dw, flat, own = like(m, k, BF16, DEV, lead=1, pad=3)
-    old = (torch.randn(m, k, generator=g) * 8).to(BF16)
-    if add:
-        dw.copy_(old)
-    ws = torch.full((max(gg.gg_ws_product(n, k, m), 16),), 0xFF, dtype=torch.uint8, device=DEV)
-    gg.gg_product_backward(a, n, k, gg.make_rows(zd), m, gg.make_rows(dw),
-                           gg.GG_PRODUCT_ADD if add else 0, ws)
-    assert untouched(flat, own)
-    z, an, old = z.to(DEV).double(), an.to(DEV), (old.to(DEV).double() if add else 0)
-    want, size = z.t().contiguous() @ an + old, z.abs().t().contiguous() @ an.abs() + abs(old)
-    bound = (n + 4) * U * size + 1.01 * PARTS[BF16] * size + 1.01 * UNIT[BF16] * want.abs() + FLOOR[BF16]
-    check(dw, want.cpu(), bound.cpu(), BF16)
+    grad_on_device(n, k, m, BF16, BF16, group, add, (8, 8))
+
+
+@pytest.mark.parametrize("tz,t", [(F32, F32), (F16, F16), (BF16, BF16), (F16, F32), (BF16, F32)])
+@pytest.mark.parametrize("n,k,m", [(9001, 1301, 1299), (20_001, 300, 1004), (1000, 2503, 2499), (257, 3001, 2999)])
+@pytest.mark.parametrize("group,add", [(128, False), (0, True)])
+def test_weight_gradient_with_work_for_tiles_of_128(n, k, m, tz, t, group, add):
+    grad_on_device(n, k, m, tz, t, group, add, (1, 3))
 
 
 @pytest.mark.parametrize("tz,t", [(F32, F32), (F16, F16), (BF16, BF16), (BF16, F32)])
