@@ -89,10 +89,9 @@ __device__ __forceinline__ int32_t row_key(int32_t r) {
 }
 
 // A lane's codes of a row in LDS: its pieces q and q + 4, q = l / 16.  Its rows have one key,
-// l / 2 & 7.  The sixteen lanes that LDS
-// serves at a time are 0-3, 12-15, 20-23 and 24-27, and their like: eight rows' piece q and the
-// other eight's piece q ^ 1, all in different banks.  (With pieces 2 q and 2 q + 1 the
-// same reads take twice as long.)
+// l / 2 & 7.  The sixteen lanes that LDS serves at a time are 0-3, 12-15, 20-23 and 24-27,
+// and their like: eight rows' piece q and the other eight's piece q ^ 1, all in different
+// banks.  (With pieces 2 q and 2 q + 1 the same reads take twice as long.)
 template <typename C>
 __device__ __forceinline__ C operand(const v4i* row, int32_t l) {
   const int32_t c = l / 16 ^ (l >> 1 & 7);
@@ -211,14 +210,12 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, int64_t i0, int
 }
 
 // A tile of BJ weights' rows by BI rows of a, blocks of 128 bytes of k at a time
-// through LDS.  A row of a block is eight pieces of 16 bytes; row r has piece c in place c
-// ^ (r / 2 & 7).  Wave (wj, wi) has BJ/WJ x BI/WI of the tile, weights as the rows of the
-// MFMA's result, so that a lane has one row's scale to apply and four neighbours to
-// store.
+// through LDS.  A row of a block is eight pieces of 16 bytes, placed by its key.  Wave (wj,
+// wi) has BJ/WJ x BI/WI of the tile, weights as the rows of the MFMA's result, so that a
+// lane has one row's scale to apply and neighbours to store.
 //
-// Pieces of whole words go from memory to LDS without a register
-// between, STAGES - 1 steps ahead, and the scales with them, so that the wait for a step
-// can count the loads behind it.  A step has WK blocks of k, each for WJ x WI waves, whose
+// Pieces of whole words go from memory to LDS without a register between, STAGES - 1 steps
+// ahead, and the scales with them, so that the wait for a step can count the loads behind it.  A step has WK blocks of k, each for WJ x WI waves, whose
 // sums are added at the end: few rows' steps are short, and so there are half as
 // many.  A step at k's end that is not whole comes through registers, with zeros
 // behind the end.  BYTES: rows may begin inside a word; the words that hold a row's block
