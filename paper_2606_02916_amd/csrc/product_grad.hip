@@ -24,7 +24,8 @@ constexpr int32_t kTileI = 32;             // rows of a step
 // themselves, so products are exact and sums fp32.  One part for bf16 results (2^-8 of a
 // term at most, the rounding that the result itself gets, and less of a sum of many), two for
 // fp16 (2^-15), three for fp32, which are the fp32 number.
-// Infinities and NaNs are whole in the first part.
+// An infinity or a NaN is whole in the first part, and the parts behind an infinity are those
+// of the largest number of its sign, which cannot cancel it.
 template <int PARTS>
 __device__ __forceinline__ void split(float x, float y, uint32_t (&p)[PARTS]) {
   const auto rounded = [](float a, float b) {
@@ -39,8 +40,8 @@ __device__ __forceinline__ void split(float x, float y, uint32_t (&p)[PARTS]) {
     p[0] = rounded(x, y);
   } else {
     p[0] = upper(x, y);
-    x = __builtin_isfinite(x) ? lower(x) : 0.0f;
-    y = __builtin_isfinite(y) ? lower(y) : 0.0f;
+    x = lower(__builtin_amdgcn_fmed3f(x, -kLargest, kLargest));
+    y = lower(__builtin_amdgcn_fmed3f(y, -kLargest, kLargest));
     if constexpr (PARTS == 2) {
       p[1] = rounded(x, y);
     } else {
