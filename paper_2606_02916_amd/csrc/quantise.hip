@@ -10,6 +10,7 @@ namespace {
 // ---------------------------------------------------------------------------
 struct RowsArgs {
   KRows x, q;
+  int64_t n;
   int64_t lanes;               // of all rows together
   int32_t dim, pieces;
   int32_t group_lanes_log;     // lanes that share a scale
@@ -80,6 +81,7 @@ template <typename T, int V>
 __global__ void __launch_bounds__(1024) k_wide_codes(RowsArgs a) {
   __shared__ uint32_t lds[1024 / kWave];
   const int64_t row = block_index();
+  if (row >= a.n) return;      // (a grid of two dimensions is rounded up)
   const char* x = a.x.p + row * a.x.stride;
   const int32_t lanes = (int32_t)blockDim.x, l = (int32_t)threadIdx.x;
   typename Raw<T, V>::vec raw[kKeep];
@@ -136,17 +138,17 @@ __global__ void __launch_bounds__(1024) k_wide_codes(RowsArgs a) {
 }
 
 template <typename T>
-int launch_rows(RowsArgs& a, int64_t n, hipStream_t stream) {
+int launch_rows(RowsArgs& a, hipStream_t stream) {
   constexpr int V = kVec<T>;
   const bool wide = a.dim >= V;
   const int vec = wide ? V : 1;
   const int32_t group = a.q.group && a.q.group < a.dim ? a.q.group : 0;
   a.pieces = (int32_t)cdiv(a.dim, vec);
-  a.stream = n * a.dim > kStreamBytes;
+  a.stream = a.n * a.dim > kStreamBytes;
   if (!group && a.pieces > kWave) {
     int threads = 128;
     while (threads < 1024 && threads * kKeep < a.pieces) threads *= 2;
-    hipLaunchKernelGGL((k_wide_codes<T, V>), grid_of(n), dim3(threads), 0, stream, a);
+    hipLaunchKernelGGL((k_wide_codes<T, V>), grid_of(a.n), dim3(threads), 0, stream, a);
     GG_LAUNCH_CHECK("k_wide_codes");
     return GG_OK;
   }
@@ -159,7 +161,7 @@ int launch_rows(RowsArgs& a, int64_t n, hipStream_t stream) {
     while ((1 << a.group_lanes_log) < a.pieces) ++a.group_lanes_log;
   }
   a.row_lanes = (int32_t)cdiv(a.pieces, 1 << a.group_lanes_log) << a.group_lanes_log;
-  a.lanes = n * a.row_lanes;
+  a.lanes = a.n * a.row_lanes;
   const dim3 grid = grid_of(cdiv(a.lanes, kBlock * kRowSteps));
   if (wide)
     hipLaunchKernelGGL((k_rows_codes<T, V>), grid, dim3(kBlock), 0, stream, a);
@@ -327,8 +329,9 @@ extern "C" int gg_quantise_rows(const gg_rows_t* x, int64_t n, int64_t dim, cons
   int rc = pack_rows(x, "x", n, dim, kBitFloats, false, &a.x);
   if (rc == GG_OK) rc = pack_rows(q, "q", n, dim, kBitE4M3, true, &a.q);
   if (rc != GG_OK || n == 0) return rc;
+  a.n = n;
   a.dim = (int32_t)dim;
-  GG_FOR_FLOAT(x->dtype, T, return launch_rows<T>(a, n, stream));
+  GG_FOR_FLOAT(x->dtype, T, return launch_rows<T>(a, stream));
 }
 
 extern "C" int gg_quantise_blocks(const gg_rows_t* w, int64_t rows, int64_t cols,

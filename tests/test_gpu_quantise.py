@@ -181,3 +181,18 @@ def test_blocks_with_nan_and_infinity_keep_to_their_block():
     assert bool(torch.isnan(q[5, 200])) and bool(torch.isnan(q[290, 3]))
     q[290, 3] = 0
     assert not q[256:, :128].any()
+
+
+def test_more_rows_than_one_dimension_of_a_grid():
+    """One scale to a wide row, a block each: 2^21 + 3 of them, and what lies behind left alone."""
+    gg, n, dim, over = lib(), (1 << 21) + 3, 260, 4096
+    x = torch.empty(n, dim, device=DEV)
+    x.normal_(generator=torch.Generator(device=DEV).manual_seed(2))
+    q = torch.full((n + over, dim), 0x7F, dtype=torch.uint8, device=DEV)
+    sc = torch.full((n + over,), float("nan"), device=DEV)
+    gg.gg_quantise_rows(gg.make_rows(x), n, dim, gg.make_rows(q[:n].view(E4M3), scales=sc[:n]))
+    assert bool((q[n:] == 0x7F).all()) and bool(torch.isnan(sc[n:]).all())
+    assert not bool(torch.isnan(sc[:n]).any())
+    for at in (0, 1 << 20, (1 << 21) - 40, n - 40):
+        wq, wsc = want_rows(x[at:at + 40], 0)
+        assert torch.equal(sc[at:at + 40].cpu()[:, None], wsc) and same(q[at:at + 40].view(E4M3), wq)
