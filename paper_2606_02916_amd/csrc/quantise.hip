@@ -197,6 +197,7 @@ __global__ void __launch_bounds__(kBlock) k_blocks_codes(BlocksArgs a) {
   // Neighbours that share lines run on one XCD, at about one time.
   const int64_t b = block_index();
   int32_t rb = (int32_t)(b / a.across), cb = (int32_t)(b - (int64_t)rb * a.across);
+  if (rb >= a.down) return;    // (a grid of two dimensions is rounded up)
   if (a.shared) tile_place(a.down, a.across, &rb, &cb);
   const int64_t r0 = (int64_t)rb * kScaleBlock, c0 = (int64_t)cb * kScaleBlock;
   const int32_t nr = (int32_t)min((int64_t)kScaleBlock, a.rows - r0),

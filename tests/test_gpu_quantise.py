@@ -196,3 +196,21 @@ def test_more_rows_than_one_dimension_of_a_grid():
     for at in (0, 1 << 20, (1 << 21) - 40, n - 40):
         wq, wsc = want_rows(x[at:at + 40], 0)
         assert torch.equal(sc[at:at + 40].cpu()[:, None], wsc) and same(q[at:at + 40].view(E4M3), wq)
+
+
+def test_more_blocks_of_weights_than_one_dimension_of_a_grid():
+    """2^24 rows (one, at a stride of 0) of 17 blocks: 2^21 + 131,072 blocks, and what lies behind
+    codes and scales left alone."""
+    gg, r, c, over = lib(), 1 << 24, 16 * 128 + 3, 4096
+    one = torch.randn(1, c, generator=gen(c)).to(BF16)
+    q = torch.full((r + over, c), 0x7F, dtype=torch.uint8, device=DEV)
+    sc = torch.full((r // 128 + over, 17), float("nan"), device=DEV)
+    gg.gg_quantise_blocks(gg.make_rows(one.to(DEV).expand(r, c)), r, c,
+                          gg.make_blocks(q[:r].view(E4M3), sc[:r // 128]), None)
+    wq, wsc = want_blocks(one)
+    assert bool((q[r:] == 0x7F).all()) and bool(torch.isnan(sc[r // 128:]).all())
+    assert bool((sc[:r // 128] == wsc.to(DEV)).all())
+    for at in (0, 1 << 23, (1 << 21) // 17 * 128 - 64, r - 128):
+        assert same(q[at:at + 128].view(E4M3), wq.expand(128, c))
+    del q
+    torch.cuda.empty_cache()

@@ -11,7 +11,7 @@ CSRC = os.path.join(helpers.ROOT, "paper_2606_02916_amd", "csrc")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 
 
-@pytest.mark.parametrize("what", ["rows"])
+@pytest.mark.parametrize("what", ["rows", "weights"])
 def test_blocks_behind_the_end_touch_nothing(what):
     """Of rows and weights put into 8 bits, with fewer and more blocks than one dimension of a
     grid holds."""
