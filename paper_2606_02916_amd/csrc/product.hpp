@@ -32,18 +32,27 @@ __device__ __forceinline__ void tile_place(int32_t tiles_i, int32_t tiles_j, int
 
 // A wave's 64 lanes' pieces of 16 bytes, or words, from base + off to consecutive places of LDS
 // at byte `to`.  Written out, since before the next read of LDS the compiler waits for all such
-// loads that it knows of; these are waited for by their number.  They write no register.
+// loads that it knows of; these are waited for by their number.  They write no register but m0,
+// which is an output so that the compiler knows (as a clobber it is warned of).
 __device__ __forceinline__ void load_to_lds16(const char* base, uint32_t off, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off),
-               "s"(base)
+  uint32_t m0;
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3"
+               : "=&{m0}"(m0)
+               : "s"(to), "v"(off), "s"(base)
                : "memory");
 }
 __device__ __forceinline__ void load_to_lds16_at(const char* p, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(p)
+  uint32_t m0;
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off"
+               : "=&{m0}"(m0)
+               : "s"(to), "v"(p)
                : "memory");
 }
 __device__ __forceinline__ void load_to_lds4(const char* p, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(p)
+  uint32_t m0;
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %2, off"
+               : "=&{m0}"(m0)
+               : "s"(to), "v"(p)
                : "memory");
 }
 __device__ __forceinline__ uint32_t lds_at(const void* p) {

@@ -1,0 +1,39 @@
+"""The loads to LDS that are written out, as compiled: their waits do not rest on where the
+compiler happens to place them.  Assembly only, no GPU."""
+import os
+import re
+import subprocess
+import tempfile
+
+import pytest
+
+from paper_2606_02916_amd import build
+from tests import helpers
+
+
+def compiled(src):
+    """The gfx950 instructions of each kernel of a source, built as the library is."""
+    out = os.path.join(tempfile.mkdtemp(prefix="gglds_"), "k.s")
+    subprocess.run([build.HIPCC, *build.FLAGS, "-Wno-align-mismatch", "--cuda-device-only", "-S", src, "-o", out],
+                   check=True)
+    text, kernels = open(out).read(), {}
+    for m in re.finditer(r"^(\w+):\s*; @\w+$(.*?)^\.Lfunc_end", text, re.S | re.M):
+        lines = (line.split(";")[0].split("//")[0].strip() for line in m[2].splitlines())
+        kernels[m[1]] = [x for x in lines if x and not x.endswith(":") and not x.startswith(".")]
+    return kernels
+
+
+@pytest.fixture(scope="module")
+def loads():
+    return compiled(os.path.join(helpers.ROOT, "tests", "device", "lds_loads.hip"))
+
+
+@pytest.mark.parametrize("kernel", ["m0_16", "m0_16_at", "m0_4"])
+def test_the_compiler_sets_its_own_place_again(loads, kernel):
+    """m0 has the place in LDS: between a load that is written out and the compiler's next one
+    it is written again."""
+    code = loads[kernel]
+    at = [i for i, x in enumerate(code) if x.startswith("global_load_lds")]
+    assert len(at) == 3
+    for a, b in zip(at, at[1:]):
+        assert any(re.search(r"\bm0,", x) for x in code[a + 1:b]), code[a:b + 1]
