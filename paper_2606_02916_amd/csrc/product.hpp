@@ -33,10 +33,12 @@ __device__ __forceinline__ void tile_place(int32_t tiles_i, int32_t tiles_j, int
 // A wave's 64 lanes' pieces of 16 bytes, or words, from base + off to consecutive places of LDS
 // at byte `to`.  Written out, since before the next read of LDS the compiler waits for all such
 // loads that it knows of; these are waited for by their number.  They write no register but m0,
-// which is an output so that the compiler knows (as a clobber it is warned of).
+// which is an output so that the compiler knows (as a clobber it is warned of).  A base that a
+// vector instruction wrote may be read five wait states later, which the compiler does not see
+// to in here: s_mov and s_nop 3 are five.  (They cost nothing that can be measured.)
 __device__ __forceinline__ void load_to_lds16(const char* base, uint32_t off, uint32_t to) {
   uint32_t m0;
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3"
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %2, %3"
                : "=&{m0}"(m0)
                : "s"(to), "v"(off), "s"(base)
                : "memory");

@@ -37,3 +37,19 @@ def test_the_compiler_sets_its_own_place_again(loads, kernel):
     assert len(at) == 3
     for a, b in zip(at, at[1:]):
         assert any(re.search(r"\bm0,", x) for x in code[a + 1:b]), code[a:b + 1]
+
+
+def test_a_base_from_lanes_is_waited_for(loads):
+    """A scalar register that a vector instruction wrote is read by a vector load five wait
+    states later at the earliest; no hardware waits for that."""
+    code = loads["base_from_lanes"]
+    load = next(i for i, x in enumerate(code) if x.startswith("global_load_lds"))
+    m = re.search(r"s\[(\d+):(\d+)\]", code[load])
+    base, wrote = {f"s{m[1]}", f"s{m[2]}"}, 0
+    states = 0
+    for x in reversed(code[:load]):
+        if x.startswith("v_readfirstlane_b32") and x.split()[1].rstrip(",") in base:
+            wrote += 1
+            assert states >= 5, code[:load + 1]
+        states += int(x.split()[1]) + 1 if x.startswith("s_nop") else 1
+    assert wrote == 2
