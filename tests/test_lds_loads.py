@@ -53,3 +53,14 @@ def test_a_base_from_lanes_is_waited_for(loads):
             assert states >= 5, code[:load + 1]
         states += int(x.split()[1]) + 1 if x.startswith("s_nop") else 1
     assert wrote == 2
+
+
+def test_waits_count_no_loads_of_the_compilers():
+    """In the weights' gradient loads to LDS are followed by loads that the compiler makes, as
+    many as it likes: a wait before a barrier that leaves some under way might leave those to LDS."""
+    kernels = compiled(os.path.join(build.CSRC, "product_grad.hip"))
+    waits = {name: [re.search(r"vmcnt\((\d+)\)", x)[1] for x, y in zip(code, code[1:])
+                    if y == "s_barrier" and x.startswith("s_waitcnt") and "vmcnt" in x]
+             for name, code in kernels.items() if any(x.startswith("global_load_lds") for x in code)}
+    assert len(waits) == 1 and len(*waits.values()) >= 3
+    assert set(*waits.values()) == {"0"}, waits
