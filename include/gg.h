@@ -703,7 +703,9 @@ int gg_quantise_blocks(const gg_rows_t* w, int64_t rows, int64_t cols, const gg_
  * or GG_BF16).  Each 128 columns' codes are multiplied and added in matrix
  * instructions, their sum scaled and added in fp32, in an order that depends on the sizes, on
  * the element's place and on how a and b are aligned.  For GG_F32 the products are exact and
- * their sums fp32.  For 16-bit outputs the 8-bit instructions add the products of columns
+ * their sums fp32, also where the product of two scales is no normal fp32 number (with scales of
+ * rows from 2^-126 on, as gg_quantise_rows makes them; two scales of 2^230 together are
+ * infinite, with a zero block's sum NaN).  For 16-bit outputs the 8-bit instructions add the products of columns
  * 8 c .. 8 c + 7 at a time, each cut off below 2^-13 of the largest one's power of two
  * (codes below 2^-6 counting as that): some 2^-16 of a result, at twice the rate.  The
  * gradient of the rows is the same call on the output's gradient in 8 bits and the

@@ -31,40 +31,63 @@ struct ProductArgs {
 // over many powers of two.  That is well below the rounding of a 16-bit output (2^-9,
 // 2^-12) and not of a 32-bit one, whose codes are multiplied as bf16: exact products,
 // added in fp32, at half the rate.
+//
+// Weights are multiplied with the power of two of their scale on the way (`power`, its
+// exponent with fp32's bias): the 8-bit instructions take one, and so does the conversion to
+// bf16, exactly.  (8,191 x 4,096 to 16,384 523 us, without 515: the instruction is longer.)
+constexpr int32_t kNoPower = 127;
+
 template <bool EXACT>
 struct Codes {
   v8i v;
-  __device__ __forceinline__ void set(v4i lo, v4i hi) {
+  __device__ __forceinline__ void set(v4i lo, v4i hi, int32_t power = kNoPower) {
     v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
   }
 };
 template <>
 struct Codes<true> {
   v8bf v[4];
-  __device__ __forceinline__ void set(v4i lo, v4i hi) {
+  __device__ __forceinline__ void set(v4i lo, v4i hi, int32_t power = kNoPower) {
+    const float two = __uint_as_float((uint32_t)power << 23);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int w0 = i < 2 ? lo[2 * i] : hi[2 * i - 4], w1 = i < 2 ? lo[2 * i + 1] : hi[2 * i - 3];
-      const v2bf p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)w0, 1.0f, false),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)w0, 1.0f, true),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)w1, 1.0f, false),
-                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)w1, 1.0f, true)};
+      const v2bf p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)w0, two, false),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)w0, two, true),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)w1, two, false),
+                         __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)w1, two, true)};
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] = p[j / 2][j % 2];
     }
   }
 };
 
-__device__ __forceinline__ v4f multiply(const Codes<false>& a, const Codes<false>& b) {
-  // e4m3 by e4m3, without scales of the instruction's own
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a.v, b.v, v4f{}, 0, 0, 0, 0, 0, 0);
+__device__ __forceinline__ v4f multiply(const Codes<false>& weights, const Codes<false>& rows, int32_t power) {
+  // e4m3 by e4m3
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(weights.v, rows.v, v4f{}, 0, 0, 0, power, 0,
+                                                          kNoPower);
 }
-__device__ __forceinline__ v4f multiply(const Codes<true>& a, const Codes<true>& b) {
+__device__ __forceinline__ v4f multiply(const Codes<true>& a, const Codes<true>& b, int32_t) {
   v4f d = {};
 #pragma unroll
   for (int i = 0; i < 4; ++i) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[i], b.v[i], d, 0, 0, 0);
   return d;
 }
+
+// A scale of weights in two factors, 2^(power - 127) and the rest.  The product of two scales
+// may pass fp32's range where the result, a block's sum of up to 2^25 and down to 2^-18 times
+// it, does not (rows of gradients of 1e-35): the power goes to the codes, and a row's scale times
+// the rest is as far from the range's ends as the row's scale.  The power itself is kept from
+// taking a block's sum out of the range; then one of both scales is so small or large that the
+// result is out of it too.
+struct Scale {
+  int32_t power;
+  float rest;
+  __device__ __forceinline__ explicit Scale(float s) {
+    power = min(max((int32_t)(__float_as_uint(s) >> 23 & 255), kNoPower - 108), kNoPower + 102);
+    rest = __builtin_amdgcn_ldexpf(s, kNoPower - power);
+  }
+};
 
 // Which of a wave's weights' rows a lane multiplies: of each 16 G rows, G products take four of
 // every 4 G, so that a lane ends with 4 G columns side by side of a row of the output, and a
@@ -93,10 +116,10 @@ __device__ __forceinline__ int32_t row_key(int32_t r) {
 // and their like: eight rows' piece q and the other eight's piece q ^ 1, all in different
 // banks.  (With pieces 2 q and 2 q + 1 the same reads take twice as long.)
 template <typename C>
-__device__ __forceinline__ C operand(const v4i* row, int32_t l) {
+__device__ __forceinline__ C operand(const v4i* row, int32_t l, int32_t power = kNoPower) {
   const int32_t c = l / 16 ^ (l >> 1 & 7);
   C v;
-  v.set(row[c], row[c ^ 4]);
+  v.set(row[c], row[c ^ 4], power);
   return v;
 }
 
@@ -113,12 +136,13 @@ typedef v4i words4 __attribute__((aligned(4)));
 // A lane's codes of a row in LDS whose words begin `skip` bytes before the row: the words
 // behind pieces q and q + 4 are the next pieces' first ones, and behind the last one, `end`.
 template <typename C>
-__device__ __forceinline__ C operand_of_words(const v4i* row, const int32_t* end, uint32_t skip, int32_t l) {
+__device__ __forceinline__ C operand_of_words(const v4i* row, const int32_t* end, uint32_t skip, int32_t l,
+                                              int32_t power = kNoPower) {
   const int32_t q = l / 16, turn = l >> 1 & 7, c = q ^ turn;
   const int32_t next = row[q + 1 ^ turn][0];
   const int32_t* far = q == 3 ? end : (const int32_t*)(row + (q + 5 ^ turn));
   C v;
-  v.set(words_from(row[c], next, skip), words_from(row[c ^ 4], *far, skip));
+  v.set(words_from(row[c], next, skip), words_from(row[c ^ 4], *far, skip), power);
   return v;
 }
 
@@ -126,10 +150,11 @@ __device__ __forceinline__ C operand_of_words(const v4i* row, const int32_t* end
 // its rows.  A product's sum is scaled kLag products later, when the matrix unit has it,
 // and the weights of the next 16 rows are read before this one's products; kept in
 // this order, since otherwise each sum is waited for (614 us instead of 712 for 8,191 x
-// 4,096 to 16,384).  weights(r) and rows(r): the operands of this lane's row r.
+// 4,096 to 16,384).  weights(r) and rows(r): the operands of this lane's row r; `power`: the
+// weights'.
 template <int TJ, int TI, typename C, typename W, typename R>
-__device__ __forceinline__ void multiply_step(const float (&scale)[TI], v4f (&acc)[TJ][TI], W weights,
-                                              R rows) {
+__device__ __forceinline__ void multiply_step(const float (&scale)[TI], int32_t power, v4f (&acc)[TJ][TI],
+                                              W weights, R rows) {
   constexpr int N = TJ * TI, kLag = N > 3 ? 3 : N - 1;
   C r[TI], w[2];
   v4f d[N];
@@ -141,7 +166,7 @@ __device__ __forceinline__ void multiply_step(const float (&scale)[TI], v4f (&ac
     const int u = x / TI, t = x % TI, y = x - kLag;
     if (x < N) {
       if (t == 0 && u + 1 < TJ) w[u + 1 & 1] = weights((u + 1) * 16);
-      d[x] = multiply(w[u & 1], r[t]);
+      d[x] = multiply(w[u & 1], r[t], power);
     }
     if (y >= 0) {
 #pragma unroll
@@ -331,20 +356,21 @@ __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_
     if (s + STAGES - 1 < steps) bring(s + STAGES - 1, slot ? slot - 1 : STAGES - 1);
     if (WK == 1 || s * WK + wk < a.kb) {
       const float* sc = scales[slot] + wk * kGroup;
-      const float sb = sc[BI + wj * TJ * 16 / kScaleBlock];
+      const Scale sb(sc[BI + wj * TJ * 16 / kScaleBlock]);
       float scale[TI];
 #pragma unroll
-      for (int t = 0; t < TI; ++t) scale[t] = sc[(wi * TI + t) * 16 + l % 16] * sb;
+      for (int t = 0; t < TI; ++t) scale[t] = sc[(wi * TI + t) * 16 + l % 16] * sb.rest;
       const v4i *w = lds[slot][wk] + wrow * 8, *r = lds[slot][wk] + (BJ + rrow) * 8;
       if constexpr (BYTES) {
         const int32_t *we = ends[slot] + wk * kGroup + wrow, *re = ends[slot] + wk * kGroup + BJ + rrow;
         // (a step at k's end has its codes in place)
         const uint32_t ws = s < whole ? wskip : 0, rs = s < whole ? rskip : 0;
-        multiply_step<TJ, TI, C>(scale, acc,
-                                 [&](int x) { return operand_of_words<C>(w + product_row<G>(x / 16) * 8, we + product_row<G>(x / 16), ws, l); },
+        multiply_step<TJ, TI, C>(scale, sb.power, acc,
+                                 [&](int x) { return operand_of_words<C>(w + product_row<G>(x / 16) * 8, we + product_row<G>(x / 16), ws, l, sb.power); },
                                  [&](int x) { return operand_of_words<C>(r + x * 8, re + x, rs, l); });
       } else {
-        multiply_step<TJ, TI, C>(scale, acc, [&](int x) { return operand<C>(w + product_row<G>(x / 16) * 8, l); },
+        multiply_step<TJ, TI, C>(scale, sb.power, acc,
+                                 [&](int x) { return operand<C>(w + product_row<G>(x / 16) * 8, l, sb.power); },
                                  [&](int x) { return operand<C>(r + x * 8, l); });
       }
     }
@@ -448,6 +474,7 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
   v4f acc[TJ][TI] = {};
   C rows[TI], w[4];
   float scale[TI], held[2] = {};
+  int32_t power = kNoPower;           // of this block's weights
   v4f d[3] = {};                      // products whose sums are not scaled yet
   const auto weights = [&](int buf, int u) {
     return operand<C>(lds[buf] + (wj * TJ * 16 + lane_row<G>(l) + product_row<G>(u)) * 8, l);
@@ -461,22 +488,27 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
     // (here, not behind the wait, where all of them would have to be held for)
     asm volatile("" : "+v"(acc[u][t]));
   };
-  const auto read_scales = [&](const float* sc, int step) {
-    const float sb = sc[(BI + wj) * step];
-#pragma unroll
-    for (int t = 0; t < TI; ++t) scale[t] = sc[((wi * TI + t) * 16 + l % 16) * step] * sb;
+  const auto product = [&](const C& x, const C& y) {
+    v4f z = multiply(x, y, power);
+    // (here, not where its sum is scaled, which may be behind the wait or the next block's scales)
+    asm volatile("" : "+v"(z));
+    return z;
   };
-  const auto scales_of = [&](int32_t g) {
-    if (fours)
-      read_scales((const float*)scales[g / 4 & 1] + g % 4, 4);
-    else
-      read_scales((const float*)scales[g & 1], 1);
+  const int32_t held_log = fours ? 2 : 0;
+  const auto scale_at = [&](int32_t g) {
+    return (const float*)scales[g >> held_log & 1] + (g & (1 << held_log) - 1);
+  };
+  const int32_t apart = fours ? 4 : 1, of_weights = (BI + wj) * apart, of_rows = (wi * TI * 16 + l % 16) * apart;
+  const auto read_scales = [&](const float* sc, const Scale& sb) {
+    power = sb.power;
+#pragma unroll
+    for (int t = 0; t < TI; ++t) scale[t] = sc[of_rows + t * 16 * apart] * sb.rest;
   };
   if (whole) {
     bring(0, 0);
     wait();
     if (whole > 1) bring(1, 1);
-    scales_of(0);
+    read_scales(scale_at(0), Scale(scale_at(0)[of_weights]));
     w[0] = weights(0, 0);
     w[1] = weights(0, 1);
 #pragma unroll
@@ -488,7 +520,7 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
     for (int x = 0; x < kEarly * TI; ++x) {
       const int u = x / TI, t = x % TI;
       if (t == 0) w[(u + 2) % 4] = weights(buf, u + 2);
-      const v4f z = multiply(w[u % 4], rows[t]);
+      const v4f z = product(w[u % 4], rows[t]);
       if (x == 0) add(TJ - 1, 2, d[0], held[0]);
       if (x == 1) add(TJ - 2, 3, d[1], held[1]);
       if (x == 2) add(TJ - 1, 3, d[2], held[1]);
@@ -500,11 +532,13 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
     // meets the rest of this one's products
     wait();
     if (g + 2 < whole) bring(g + 2, buf);
+    // (its products wait for this one)
+    const float next = scale_at(g + 1)[of_weights];
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int y = 0; y < 2 * TI; ++y) {
       const int x = kEarly * TI + y, u = kEarly + y % 2, t = y / 2;
-      const v4f z = multiply(w[u % 4], rows[t]);
+      const v4f z = product(w[u % 4], rows[t]);
       // (the tile three products before)
       const int v = y - 3;
       if (v < 0)
@@ -518,7 +552,7 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
     }
     held[0] = scale[2];
     held[1] = scale[3];
-    scales_of(g + 1);
+    read_scales(scale_at(g + 1), Scale(next));
     static_assert(TI == 4 && (kEarly * TI + 2 * TI) % 3 == 2 && TJ % 4 == 0, "the order of d and w");
     const v4f z = d[2];
     d[2] = d[1];
@@ -547,8 +581,12 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
 #pragma unroll
     for (int t = 0; t < 8; ++t) lds[0][t * kThreads + lane] = codes_moved(got[t], column_of(t), a.k);
     wait();
-    read_scales((const float*)scales[0], 1);
-    multiply_step<TJ, TI, C>(scale, acc, [&](int x) { return weights(0, x / 16); },
+    const float* sc = (const float*)scales[0];
+    const Scale end(sc[BI + wj]);
+    power = end.power;
+#pragma unroll
+    for (int t = 0; t < TI; ++t) scale[t] = sc[(wi * TI + t) * 16 + l % 16] * end.rest;
+    multiply_step<TJ, TI, C>(scale, power, acc, [&](int x) { return weights(0, x / 16); },
                              [&](int x) { return row(0, x / 16); });
   }
   store_tile<O, G, TJ, TI>(a, i0 + wi * TI * 16, j0 + wj * TJ * 16, l, acc, i0 + skip);
@@ -612,16 +650,18 @@ __global__ void __launch_bounds__(WJ* WI* kWave, sizeof(O) == 4 ? 1 : 2) k_produ
   for (int32_t g = 0; g < a.kb; ++g) {
     const int buf = g & 1;
     __syncthreads();
+    const Scale of_weights(sb);
     float scale[TI];
 #pragma unroll
-    for (int t = 0; t < TI; ++t) scale[t] = sa[t] * sb;
+    for (int t = 0; t < TI; ++t) scale[t] = sa[t] * of_weights.rest;
     const bool more = g + 1 < a.kb;
     if (more) {
       fetch(g + 1);
       scales(g + 1);
     }
     const v4i *w = lds[buf] + (wj * TJ * 16 + l % 16) * 8, *r = lds[buf] + (BJ + wi * TI * 16 + l % 16) * 8;
-    multiply_step<TJ, TI, C>(scale, acc, [&](int x) { return operand<C>(w + x * 8, l); },
+    multiply_step<TJ, TI, C>(scale, of_weights.power, acc,
+                             [&](int x) { return operand<C>(w + x * 8, l, of_weights.power); },
                              [&](int x) { return operand<C>(r + x * 8, l); });
     if (more) keep(buf ^ 1);
   }
@@ -668,13 +708,13 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) k_product_few(ProductArgs
       for (int x = 0; x < 2; ++x) w[x] = *(const GG_GLOBAL words4*)(p + 16 * x);
       if (BYTES) last = *(const GG_GLOBAL int32_t*)(p + (skip ? 32 : 28));
     }
-    __device__ __forceinline__ C codes(const char* base, uint32_t off) const {
+    __device__ __forceinline__ C codes(const char* base, uint32_t off, int32_t power = kNoPower) const {
       C c;
       if constexpr (BYTES) {
         const uint32_t p = (uint32_t)(uintptr_t)base + off;
-        c.set(words_from(w[0], w[1][0], p), words_from(w[1], last, p));
+        c.set(words_from(w[0], w[1][0], p), words_from(w[1], last, p), power);
       } else {
-        c.set(w[0], w[1]);
+        c.set(w[0], w[1], power);
       }
       return c;
     }
@@ -698,8 +738,8 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) k_product_few(ProductArgs
     }
   };
   v4f acc[1][1] = {};
-  const auto add = [&](const C& w, const C& r, float scale) {
-    const v4f d = multiply(w, r);
+  const auto add = [&](const C& w, const C& r, int32_t power, float scale) {
+    const v4f d = multiply(w, r, power);
 #pragma unroll
     for (int x = 0; x < 4; ++x) acc[0][0][x] = __builtin_fmaf(d[x], scale, acc[0][0][x]);
   };
@@ -707,7 +747,8 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) k_product_few(ProductArgs
 #pragma unroll
     for (int h = 0; h < kAhead; ++h) {
       if (g0 + h * waves >= whole) break;
-      add(s.w[h].codes(wbase, w_off), s.r[h].codes(rbase, r_off), s.sa[h] * s.sb[h]);
+      const Scale sb(s.sb[h]);
+      add(s.w[h].codes(wbase, w_off, sb.power), s.r[h].codes(rbase, r_off), sb.power, s.sa[h] * sb.rest);
     }
   };
   Step s[2];
@@ -722,13 +763,14 @@ __global__ void __launch_bounds__(kFewWaves* kWave, 2) k_product_few(ProductArgs
   }
   if (whole < a.kb && whole % waves == wave) {   // the block at k's end
     load_scales(whole, 0, s[0]);
-    const auto end_of = [&](const char* row) {
+    const auto end_of = [&](const char* row, int32_t power = kNoPower) {
       const int32_t c = whole * kBlockK + lane_c;
       C codes;
-      codes.set(load_codes(row, c, a.k), load_codes(row, c + 16, a.k));
+      codes.set(load_codes(row, c, a.k), load_codes(row, c + 16, a.k), power);
       return codes;
     };
-    add(end_of(wbase + w_off), end_of(rbase + r_off), s[0].sa[0] * s[0].sb[0]);
+    const Scale sb(s[0].sb[0]);
+    add(end_of(wbase + w_off, sb.power), end_of(rbase + r_off), sb.power, s[0].sa[0] * sb.rest);
   }
   for (int32_t half = waves / 2; half >= 1; half /= 2) {
     __syncthreads();

@@ -475,3 +475,99 @@ def test_gradients_are_the_same_each_time_and_on_another_stream():
                 again = grad_case(n, k, m, F32, F32, 128)[0]
             torch.cuda.current_stream().wait_stream(side)
             assert torch.equal(first, again)
+
+
+# ---------------------------------------------------------------------------
+# Scales at the ends of fp32's range: the product of two may lie beyond them.
+# ---------------------------------------------------------------------------
+def scaled(n, k, m, t, sa, sb, group, ac, bc, a_at=(0, 0), step=None):
+    """The product of given codes and scales, and its value, its terms' magnitudes and what the
+    8-bit instructions may drop, in 64 bits.  step: weights' rows so many bytes apart."""
+    gg = lib()
+    col, row = torch.arange(k) // 128, torch.arange(m) // 128
+    if step:
+        b = torch.empty(m * step, dtype=torch.uint8, device=DEV).as_strided((m, k), (step, 1))
+        b.copy_(bc.view(torch.uint8))
+        b = b.view(E4M3)
+    else:
+        b = bc.to(DEV)
+    out = torch.full((n, m), float("nan"), device=DEV).to(t)
+    sad = sa.to(DEV)
+    gg.gg_product_forward(gg.make_rows(place8(ac, *a_at), scales=sad, group=group), n, k,
+                          gg.make_blocks(b, sb.to(DEV)), m, gg.make_rows(out))
+    ac, bc = ac.float().double(), bc.float().double()
+    an = ac * (sa.double()[:, col] if group else sa.double()[:, :1])
+    bn = bc * sb.double()[row][:, col]
+    x, y = an.to(DEV), bn.to(DEV)
+    want, size = (x @ y.t()).cpu(), (x.abs() @ y.abs().t()).cpu()
+    return out, want, size, 0.0 if t == F32 else 1.01 * coarse(an, ac, bn, bc)
+
+
+# few rows, of words and of bytes; tiles of 32, 128 and 256 rows; rows far apart
+ENDS = [(3, 700, 140, (0, 0), None), (60, 300, 50, (1, 0), None), (64, 2048, 2048, (0, 0), None),
+        (70, 2100, 1500, (1, 2), None), (2100, 260, 2200, (0, 0), None), (2200, 768, 4001, (0, 0), None),
+        (2200, 700, 4001, (4, 0), None), (40, 300, 150, (0, 0), 1 << 24)]
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("n,k,m,a_at,step", ENDS)
+def test_scales_whose_product_is_no_normal_number(n, k, m, a_at, step, group, t):
+    """Rows of tiny gradients with ordinary weights, and tiny weights with tiny rows: the
+    product of scales lies below 2^-126, results do not."""
+    g = gen(n, k, m, group)
+    kb, mb = blocks_of(k, 128), blocks_of(m, 128)
+    # codes from 32 to 448 of either sign, more of them positive, so that sums are large
+    ac, bc = ((torch.rand(r, k, generator=g) * 416 + 32) * torch.where(torch.rand(r, k, generator=g) < 0.8, 1, -1)
+              for r in (n, m))
+    ac, bc = ac.to(E4M3), bc.to(E4M3)
+    for ea, eb in ((-126, -14), (-70, -72), (-14, -126), (-20, -110)):
+        sa = torch.exp2(ea + 4 * torch.rand(n, kb if group else 1, generator=g))
+        sb = torch.exp2(eb + 2 * torch.rand(mb, kb, generator=g))
+        out, want, size, cut = scaled(n, k, m, t, sa, sb, group, ac, bc, a_at, step)
+        assert float(size.max()) > 2.0 ** -126
+        # (below 2^-126 each block's sum is rounded to a multiple of 2^-149, bf16's results of 2^-133)
+        least = (kb + 1) * 2.0 ** -150 + (2.0 ** -134 if t == BF16 else 0)
+        check(out, want, (k + 4) * U * size + 1.01 * UNIT[t] * want.abs() + least + cut, t)
+
+
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("n,k,m,a_at,step", ENDS)
+def test_scales_whose_product_is_beyond_the_largest_number(n, k, m, a_at, step, group, t):
+    """Zeros stay zeros, and the least codes' products are finite, where the product of scales
+    passes 2^128."""
+    g = gen(n, k, m, group)
+    kb, mb = blocks_of(k, 128), blocks_of(m, 128)
+    ac, bc = (torch.where(torch.rand(r, k, generator=g) < 0.5, 2.0 ** -9, 0.0).to(E4M3) for r in (n, m))
+    ac[n // 2], bc[m // 2] = torch.zeros(k).to(E4M3), torch.zeros(k).to(E4M3)
+    for ea, eb in ((90, 40), (118, 11), (20, 110), (12, 118)):
+        sa = torch.exp2(ea + torch.rand(n, kb if group else 1, generator=g))
+        sb = torch.exp2(eb + torch.rand(mb, kb, generator=g))
+        out, want, size, cut = scaled(n, k, m, t, sa, sb, group, ac, bc, a_at, step)
+        assert float(size.max()) < 2.0 ** 127
+        if t == F16:
+            big = want >= 65_520
+            assert torch.equal(out.cpu().double(), torch.where(big, float("inf"), 0.0).double())
+        else:
+            check(out, want, (k + 4) * U * size + 1.01 * UNIT[t] * want.abs() + cut, t)
+
+
+@pytest.mark.parametrize("t", [F32, BF16])
+@pytest.mark.parametrize("n,k,m,a_at,step", ENDS)
+def test_scales_of_every_size(n, k, m, a_at, step, t):
+    """Scales from 2^-126 to 2^119, each row's and block's of its own size."""
+    g = gen(n, k, m)
+    kb, mb = blocks_of(k, 128), blocks_of(m, 128)
+    ac, bc = codes8(n, k, g), codes8(m, k, g)
+    sa = torch.exp2(torch.randint(-126, 119, (n, 1), generator=g) + torch.rand(n, kb, generator=g))
+    sb = torch.exp2(torch.randint(-126, 111, (mb, 1), generator=g) + torch.rand(mb, kb, generator=g))
+    out, want, size, cut = scaled(n, k, m, t, sa, sb, 128, ac, bc, a_at, step)
+    least = (kb + 1) * 2.0 ** -150 + (2.0 ** -134 if t == BF16 else 0)
+    bound = (k + 4) * U * size + 1.01 * UNIT[t] * want.abs() + least + cut
+    here = size < 2.0 ** 127
+    assert 0.3 < float(here.double().mean()) and float((size[here] > 2.0 ** -126).double().mean()) > 0.3
+    assert within(out.cpu()[here], want[here], bound[here]) <= 0
+    # far beyond the range no result is finite (blocks' sums that overflow in both directions add
+    # up to a NaN)
+    assert not bool(torch.isfinite(out.cpu()[want.abs() - bound > 2.0 ** 129]).any())
