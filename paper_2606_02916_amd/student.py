@@ -64,9 +64,11 @@ class Student:
     fp16 or bf16, of the activations, their gradients and the copy of the head
     that they are multiplied with.  norm: "rms", or "layer" with a bias b [dim] that is
     trained too.  eight_bit: the head multiplies 8-bit rows (scales by 128 elements; the
-    head's by 128 x 128), and what a step keeps for the way back is in 8 bits: the sums
-    before the norm and the normed rows; the gradient of the logits goes back through
-    the head in 8 bits, and as it is into the head's own gradient."""
+    head's by 128 x 128), and what a step keeps for the way back is in 8 bits: the normed
+    rows, of which there is no other copy then, and the sums before the norm, beside the
+    full rows that the looked-up ones come in and their gradient leaves in; the gradient
+    of the logits goes back through the head in 8 bits, and as it is into the head's own
+    gradient."""
 
     def __init__(self, num_nodes, dim, classes, max_rows, k=8, temperature=2.0, rate=0.05,
                  dtype=torch.float32, eps=1e-6, device=None, generator=None, norm="rms",
@@ -119,7 +121,7 @@ class Student:
     def _normed(self, ids, n, x, q=None, y=True, kept=None, stream=None):
         """The normed rows of ids[:n] (None: the nodes 0 .. n-1), with x [n, dim]
         added to the looked-up rows if given; into self.y, and in 8 bits into q; the
-        sums in 8 bits into kept."""
+        sums into self.e, or of a layer norm in 8 bits into kept instead."""
         if n > self.max_rows:
             raise gg.GGError(f"{n} rows for a student of {self.max_rows}")
         if x is not None:
@@ -128,8 +130,10 @@ class Student:
                             self.status, stream=stream)
         y = self._y if y else None
         if self.layer:
-            gg.gg_layernorm_forward(self._e, x, n, self.dim, self.w, self.b, self.eps, self._e, y, q,
-                                    kept, self.mean, self.rstd, stream=stream)
+            # (sums kept in 8 bits are all that the way back reads)
+            gg.gg_layernorm_forward(self._e, x, n, self.dim, self.w, self.b, self.eps,
+                                    self._e if kept is None else None, y, q, kept, self.mean,
+                                    self.rstd, stream=stream)
             return
         gg.gg_rmsnorm_forward(self._e, x, n, self.dim, self.w, self.eps, self._e, y, q, self.rstd,
                               stream=stream)

@@ -255,3 +255,29 @@ def test_the_student_checks_its_norm_and_tensors():
                        (lambda: s.step(ids, 8, torch.zeros(8, 3).long(), torch.zeros(8, 3)), "student of 7")):
         with pytest.raises(gg.GGError, match=word):
             call()
+
+
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+@pytest.mark.parametrize("eight_bit", [False, True])
+def test_a_step_stores_the_sums_that_its_way_back_reads(norm, eight_bit, monkeypatch):
+    """The forward norm's outputs are what the norm's gradient (or the call that puts sums into 8
+    bits) reads, no sums are stored beside them."""
+    from paper_2606_02916_amd import Student, student
+    s = Student(50, 20, 9, max_rows=7, k=3, device="cpu", norm=norm, eight_bit=eight_bit)
+    seen = []
+    for name in [x for x in dir(gg) if x.startswith("gg_") and not x.startswith("gg_ws")]:
+        if callable(getattr(gg, name)) and not isinstance(getattr(gg, name), type):
+            monkeypatch.setattr(student.gg, name, lambda *a, call=name, **k: seen.append((call, a)))
+    s.step(torch.zeros(7, dtype=torch.int64), 7, torch.zeros(7, 3).long(), torch.zeros(7, 3))
+    calls = dict(reversed(seen))
+    if norm == "layer":
+        forward, back = calls["gg_layernorm_forward"], calls["gg_layernorm_backward"]
+        stored, kept = forward[7], forward[10]
+    else:
+        forward, back = calls["gg_rmsnorm_forward"], calls["gg_rmsnorm_backward"]
+        stored, kept = forward[6], None
+        if eight_bit:
+            read, kept = [(a[0], a[3]) for c, a in seen if c == "gg_quantise_rows"][0]
+            assert read is stored
+    assert back[2] is (kept if eight_bit else stored)
+    assert (stored is None) == (norm == "layer" and eight_bit)
