@@ -571,3 +571,58 @@ def test_scales_of_every_size(n, k, m, a_at, step, t):
     # far beyond the range no result is finite (blocks' sums that overflow in both directions add
     # up to a NaN)
     assert not bool(torch.isfinite(out.cpu()[want.abs() - bound > 2.0 ** 129]).any())
+
+
+# ---------------------------------------------------------------------------
+# Kernels in every type and with both kinds of scales.
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("t", [F32, F16, BF16])
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("n,k,m", [(5, 300, 150), (140, 260, 131), (130, 128, 40)])
+def test_rows_far_apart(n, k, m, group, t):
+    """Rows of both matrices, their scales and the results more than 2^23 bytes apart."""
+    gg, g, step = lib(), gen(n, k, m, group), (1 << 23) + 4096
+    ac, bc = codes8(n, k, g), codes8(m, k, g)
+    ka, kb, mb = blocks_of(k, group), blocks_of(k, 128), blocks_of(m, 128)
+    sa, sb = (torch.exp2(torch.rand(r, c, generator=g) * 8 - 6) for r, c in ((n, ka), (mb, kb)))
+    size = torch.finfo(t).bits // 8
+    big = torch.full((max(n, m) * step,), 0xFF, dtype=torch.uint8, device=DEV)
+
+    def far(rows, cols, dtype, at):
+        e = torch.finfo(dtype).bits // 8
+        return big[at:].view(dtype).as_strided((rows, cols), (step // e, 1))
+
+    a, b, out = far(n, k, E4M3, 0), far(m, k, E4M3, 4096), far(n, m, t, 8192)
+    sad, sbd = far(n, ka, F32, 16_384), far(mb, kb, F32, 20_480)
+    a.view(torch.uint8).copy_(ac.view(torch.uint8)), b.view(torch.uint8).copy_(bc.view(torch.uint8))
+    sad.copy_(sa), sbd.copy_(sb)
+    gg.gg_product_forward(gg.make_rows(a, scales=sad, group=group), n, k, gg.make_blocks(b, sbd), m,
+                          gg.make_rows(out))
+    # what lies before and behind a result's row is left alone
+    around = torch.stack([big[i * step + 8192 - 64:i * step + 8192 + m * size + 64] for i in range(n)]).cpu()
+    assert bool((around[:, :64] == 0xFF).all()) and bool((around[:, -64:] == 0xFF).all())
+    col = torch.arange(k)
+    ac, bc = ac.float().double(), bc.float().double()
+    an = ac * sa.double()[:, col // (group or k)]
+    bn = bc * sb.double()[torch.arange(m) // 128][:, col // 128]
+    want, mag = an @ bn.t(), an.abs() @ bn.abs().t()
+    bound = (k + 4) * U * mag + 1.01 * UNIT[t] * want.abs() + FLOOR[t]
+    if t != F32:
+        bound += 1.01 * coarse(an, ac, bn, bc)
+    check(out, want, bound, t)
+
+
+@pytest.mark.parametrize("t", [F16, BF16])
+@pytest.mark.parametrize("group", [0, 128])
+@pytest.mark.parametrize("n,k,m", [(2200, 1024, 4000), (2304, 1536, 4096), (2200, 644, 4001)])
+def test_large_tiles_of_every_kind(n, k, m, group, t):
+    """More than four blocks of k and a round of large tiles, rows on word or 16-byte boundaries:
+    scales one by one, and one a row."""
+    check_forward(n, k, m, t, group, 0, 0)
+
+
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("k", [1024, 2048])
+def test_scales_by_fours_of_more_blocks(k, offset):
+    """Fours of blocks, in the tiles that load scales so, on 16-byte boundaries and beside them."""
+    test_scales_by_fours(k, offset)
