@@ -149,13 +149,15 @@ __device__ __forceinline__ C operand_of_words(const v4i* row, const int32_t* end
 // The products of a wave's TJ x TI operands from LDS, added to acc with the scales of
 // its rows.  A product's sum is scaled kLag products later, when the matrix unit has it,
 // and the weights of the next 16 rows are read before this one's products; kept in
-// this order, since otherwise each sum is waited for (614 us instead of 712 for 8,191 x
-// 4,096 to 16,384).  weights(r) and rows(r): the operands of this lane's row r; `power`: the
-// weights'.
+// this order for many products and for fp32 results (10,610 rows of 128 to 36,776 bf16 204 us, 207
+// otherwise; 8,191 of 4,096 to 16,384 fp32 1,028 and 1,053).  Of few the compiler's order hides more
+// of what comes before the first, the weights' power (300 rows of 8,192 to 1,024 bf16 16.6 us, in
+// this one 17.6).  weights(r) and rows(r): the operands of this lane's row r; `power`: the weights'.
 template <int TJ, int TI, typename C, typename W, typename R>
 __device__ __forceinline__ void multiply_step(const float (&scale)[TI], int32_t power, v4f (&acc)[TJ][TI],
                                               W weights, R rows) {
   constexpr int N = TJ * TI, kLag = N > 3 ? 3 : N - 1;
+  constexpr bool kOrdered = N >= 16 || std::is_same<C, Codes<true>>::value;
   C r[TI], w[2];
   v4f d[N];
   w[0] = weights(0);
@@ -173,7 +175,7 @@ __device__ __forceinline__ void multiply_step(const float (&scale)[TI], int32_t 
       for (int i = 0; i < 4; ++i)
         acc[y / TI][y % TI][i] = __builtin_fmaf(d[y][i], scale[y % TI], acc[y / TI][y % TI][i]);
     }
-    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (kOrdered) __builtin_amdgcn_sched_barrier(0);
   }
 }
 
