@@ -626,3 +626,37 @@ def test_large_tiles_of_every_kind(n, k, m, group, t):
 def test_scales_by_fours_of_more_blocks(k, offset):
     """Fours of blocks, in the tiles that load scales so, on 16-byte boundaries and beside them."""
     test_scales_by_fours(k, offset)
+
+
+@pytest.mark.parametrize("t", [F16, BF16])
+@pytest.mark.parametrize("n,k,m", [(3, 200, 140), (60, 300, 50), (600, 256, 512), (2200, 900, 4000)])
+def test_nans_of_8_bit_instructions_keep_to_their_row_and_column(n, k, m, t):
+    """A NaN code and infinite and NaN scales, of a row and of a block of weights."""
+    gg, g = lib(), gen(n)
+    acodes, bcodes = codes8(n, k, g), codes8(m, k, g)
+    kb, mb = blocks_of(k, 128), blocks_of(m, 128)
+    sa, sb = (torch.rand(n, kb, generator=g) + 0.5).to(DEV), (torch.rand(mb, kb, generator=g) + 0.5).to(DEV)
+    a, b = place8(acodes, 0, 0), place8(bcodes, 0, 0)
+    clean, out = (torch.empty(n, m, dtype=t, device=DEV) for _ in range(2))
+
+    def call(to):
+        gg.gg_product_forward(gg.make_rows(a, scales=sa, group=128), n, k, gg.make_blocks(b, sb), m,
+                              gg.make_rows(to))
+
+    call(clean)
+    a.view(torch.uint8)[1, k - 1] = 0x7F
+    b.view(torch.uint8)[m - 2, 5] = 0xFF
+    sa[2, kb - 1] = float("inf")
+    last = (mb - 1) * 128 if mb > 1 else m
+    if mb > 1:
+        sb[mb - 1, 0] = float("nan")
+    call(out)
+    out, clean = out.cpu(), clean.cpu()
+    rest = torch.ones(n, m, dtype=torch.bool)
+    rest[1:3] = False
+    rest[:, m - 2] = False
+    rest[:, last:] = False
+    assert torch.equal(out[rest], clean[rest])
+    assert bool(torch.isnan(out[1]).all()) and bool(torch.isnan(out[:, m - 2]).all())
+    assert bool(torch.isnan(out[:, last:]).all())
+    assert not bool(torch.isfinite(out[2]).any())
