@@ -1,6 +1,7 @@
 // Rows and weights into 8 bits: a scale for each group of a row's elements, or
 // for each 128 x 128 elements of the weights, which may leave transposed too.
-#include "product.hpp"
+#include "codes.hpp"
+#include "tiles.hpp"
 
 namespace gg {
 namespace {
