@@ -705,9 +705,9 @@ int gg_quantise_blocks(const gg_rows_t* w, int64_t rows, int64_t cols, const gg_
  * the element's place and on how a and b are aligned.  For GG_F32 the products are exact and
  * their sums fp32, also where the product of two scales is no normal fp32 number (with scales of
  * rows from 2^-126 on, as gg_quantise_rows makes them; two scales of 2^230 together are
- * infinite, with a zero block's sum NaN).  For 16-bit outputs the 8-bit instructions add the products of columns
- * 8 c .. 8 c + 7 at a time, each cut off below 2^-13 of the largest one's power of two
- * (codes below 2^-6 counting as that): some 2^-16 of a result, at twice the rate.  The
+ * infinite, with a zero block's sum NaN).  For 16-bit outputs the 8-bit instructions add the
+ * products of columns 8 c .. 8 c + 7 at a time, each cut off below 2^-13 of the largest one's
+ * power of two (codes below 2^-6 counting as that): some 2^-16 of a result, at twice the rate.  The
  * gradient of the rows is the same call on the output's gradient in 8 bits and the
  * transposed weights (gg_quantise_rows, gg_quantise_blocks).  out is no memory of a or b.
  * Rows may begin at any byte (the words that hold a row's bytes are read whole); those that
@@ -725,8 +725,9 @@ size_t gg_ws_product(int64_t n, int64_t k, int64_t m);
  * dz[i][j] a[i][c], [m][k], of dz's type or GG_F32; with GG_PRODUCT_ADD added to what dw
  * holds.  Sums are fp32, in an order that depends on the sizes, the types and dz's
  * alignment, rounded once with what is added.  Of a term's three factors two are
- * multiplied first, dz and scale as fp32 numbers (in steps of 2^-133) for a dw of GG_F32 and
- * to 2^-15 for GG_F16, dz or the code and scale rounded to bf16 for GG_BF16.  No row (n 0):
+ * multiplied first, dz and scale as fp32 numbers (in steps of 2^-133, infinite beyond their
+ * range) for a dw of GG_F32 and to 2^-15 for GG_F16, dz or the code and scale rounded to bf16
+ * for GG_BF16, which makes a sum 1.4 to 1.5 times as far off as its own rounding does.  No row (n 0):
  * zeros.  dw is no memory of a or dz.  ws: 16-byte aligned, NULL where gg_ws_product is 0. */
 int gg_product_backward(const gg_rows_t* a, int64_t n, int64_t k, const gg_rows_t* dz, int64_t m,
                         const gg_rows_t* dw, int32_t flags, void* ws, size_t ws_bytes,

@@ -148,7 +148,8 @@ __device__ __forceinline__ void store_codes(const CodeRows& q, int64_t row, int 
 // barrier.  32,768 rows of 4,096 bf16 with residual and sum take 182 us, 5.9
 // TB/s; 200,000 of 602 fp32 364 us, 5.3; 2M of 33 fp32 177 us, 6.0; without a
 // residual, 65,536 of 1,000 bf16 39 us, 6.7 (a 1 GiB copy: 5.0).  With LAYER 32,768
-// of 4,096 bf16 with residual, sum and both 8-bit rows 187 us, 5.8 TB/s.
+// of 4,096 bf16 with residual, sum and both 8-bit rows 187 us, 5.8 TB/s, call behind call; a
+// kernel trace has each at 197.
 template <typename T, typename R, bool LAYER, int V, int STEPS, bool BLK>
 __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
   __shared__ float lds[BLK ? 1024 / kWave : 1];
@@ -247,7 +248,7 @@ __global__ void __launch_bounds__(BLK ? 1024 : kBlock) k_norm(NormArgs a) {
 // shares of all blocks are added in a second launch, in the order of the
 // blocks.  Bound by memory: 32,768 rows of 4,096 bf16 209 us, 5.1 TB/s; 200,000 of
 // 602 fp32 376 us, 5.1.  With LAYER 233,000 of 602 fp32 336 us, 5.0; 16,383 of 4,096
-// bf16 from 8-bit rows 100 us, 4.7.
+// bf16 from 8-bit rows 100 us, 4.7, both launches (98 and 6 by a trace).
 // ---------------------------------------------------------------------------
 struct NormBackArgs {
   KRows dy, dsum, s, dx;

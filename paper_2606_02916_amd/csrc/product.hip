@@ -92,7 +92,7 @@ struct Scale {
 // Which of a wave's weights' rows a lane multiplies: of each 16 G rows, G products take four of
 // every 4 G, so that a lane ends with 4 G columns side by side of a row of the output, and a
 // row's four lanes with 16 G: whole cache lines in 16 bits with G = 4 (8,191 x 4,096 to 16,384
-// 521 us, with G = 1 540; 10,610 of 128 to 36,776 200 and 254).
+// 527 us, with G = 1 553; 10,610 of 128 to 36,776 204 and 232).
 template <typename O, int TJ>
 constexpr int kSide = sizeof(O) == 4 ? 1 : TJ < 4 ? TJ : 4;
 
@@ -247,7 +247,8 @@ __device__ __forceinline__ void store_tile(const ProductArgs& a, int64_t i0, int
 // many.  A step at k's end that is not whole comes through registers, with zeros
 // behind the end.  BYTES: rows may begin inside a word; the words that hold a row's block
 // are brought, with one more for each row, and moved down as operands are read (8,191 x
-// 4,096 to 16,384 bf16 840 us, 1,470 with 16 bytes from any place through registers).
+// 4,096 to 16,384 bf16 with weights one byte off 870 us, through registers with 16 bytes from any
+// place 1,470; rows 4,097 apart 990).
 template <typename O, int BJ, int BI, int WJ, int WI, int WK, int STAGES, bool BYTES>
 __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_pipe(ProductArgs a) {
   constexpr int kThreads = WJ * WI * WK * kWave, kGroup = kThreads / WK, kPieces = (BJ + BI) * 8,
@@ -402,9 +403,10 @@ __global__ void __launch_bounds__(WJ* WI* WK* kWave, BI > 32 ? 2 : 1) k_product_
 // Tiles of 256 x 256 of rows that begin with words, two blocks of k in LDS.  One wait a block, before its last quarter of
 // products: the next block has been on its way since the same place in the block before,
 // and its first operands are read into the registers that the last products leave.
-// 8,191 x 4,096 to 16,384 bf16 take 521 us, 2,110 TFLOP/s.  Without the loads 446, without
-// the scaling too 405: products, their scaling and LDS's reads do not quite overlap (a
-// wave's products alone would be 240), and the loads' requests come on top.
+// 8,191 x 4,096 to 16,384 bf16 take 524 us, 2,100 TFLOP/s (515 to 545 on different cards).
+// Of 535 432 are left without the loads, 370 without the scaling too: products, their scaling
+// and LDS's reads do not quite overlap (a wave's products alone would be 240), and the loads'
+// requests come on top.
 template <typename O>
 __global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
   constexpr int BJ = 256, BI = 256, WJ = 2, WI = 4, TJ = BJ / WJ / 16, TI = BI / WI / 16, G = kSide<O, TJ>, kThreads = 512;
@@ -440,12 +442,12 @@ __global__ void __launch_bounds__(512, 2) k_product_wide(ProductArgs a) {
              : a.b.scales + min(j0 + min(tid - BI, 1) * kScaleBlock, a.m - 1) / kScaleBlock * a.b.sstride;
   const int32_t scale_step = of_row && a.per_row ? 0 : 4;
   // Scales come for four blocks at a time where they lie on 16-byte boundaries (each
-  // lane's is in a line of its own: a load for each block costs 30 us of 577, 8,191 x 4,096
-  // to 16,384), for one at a time elsewhere.
+  // lane's is in a line of its own: one for each block takes 547 us instead of 529, 8,191 x
+  // 4,096 to 16,384), for one at a time elsewhere.
   const bool fours = a.scales16;
   const int32_t whole = a.k / kBlockK;
   // Each XCD's blocks begin at another block of k, so that rows a power of two apart do
-  // not all ask the same part of memory (542 us instead of 556).
+  // not all ask the same part of memory (529 us instead of 550).
   const int32_t turn = (int32_t)(blockIdx.x % kXcds) * whole / kXcds / 4 * 4;
   const auto at = [&](int32_t g) {
     const int32_t x = g + turn;
@@ -842,7 +844,8 @@ int launch_tile(ProductArgs& a, hipStream_t stream) {
   return GG_OK;
 }
 
-// Which kernel: microseconds measured beside the next best, bf16 results.
+// Which kernel: microseconds measured beside the next best, bf16 results.  (fp32 results, whose
+// products take twice as long, go by the same rule, without the largest tiles.)
 template <typename O>
 int launch_product(ProductArgs& a, hipStream_t stream) {
   // offsets in a tile are of 32 bits
@@ -851,11 +854,11 @@ int launch_product(ProductArgs& a, hipStream_t stream) {
   const auto tiles = [&](int bj, int bi) { return cdiv(a.n, bi) * cdiv(a.m, bj); };
   if (!near) return launch_tile<O, 128, 128, 2, 2>(a, stream);
   // Few rows, or rows and weights that are few together: without LDS, which gathers rows
-  // badly (16 rows of 4,096 to 4,096 7.4 us, through LDS 8.5; of 8,192 to 8,192 20.1 and 14.8;
-  // 64 rows of 4,096 to 1,024 7.3 and 9.6, to 4,096 12.2 and 10.1).
+  // badly (16 rows of 4,096 to 4,096 7.6 us, through LDS 8.7; of 8,192 to 8,192 20.5 and 15.1;
+  // 64 rows of 4,096 to 1,024 7.3 and 8.6, to 4,096 20.5 and 9.0).
   if (a.n <= 4 || tiles(16, 16) * a.kb <= 8192) return launch_few<O>(a, stream);
   // The smallest tiles of which there is one for each CU, or that hold all rows (steps of 32 x 32
-  // take 0.33 us, of 32 x 64 0.4, of 32 x 96 and beyond 0.6; 1,076 rows of 7,808 to 384 17.0 us in
+  // take 0.33 us, of 32 x 64 0.4, of 32 x 96 and beyond 0.6; 1,076 rows of 7,808 to 384 16.8 us in
   // 32 x 64, 22.9 in 32 x 128; 256 rows of 4,096 to 4,096 15.1 in 32 x 128, 26.1 in 128 x 128).
   const auto fits = [&](int bj, int bi) { return a.n <= bi || tiles(bj, bi) <= 256; };
   if (fits(32, 32)) return launch_pipe<O, 32, 32, 1, 2, 2, 5>(a, stream);
@@ -866,7 +869,7 @@ int launch_product(ProductArgs& a, hipStream_t stream) {
   if (tiles(128, 128) <= 256) return launch_pipe<O, 128, 128, 2, 2, 2, 2>(a, stream);
   // A round of 256 of 256 x 256 takes 1.4 to 1.85 times one of 512 of 128 x 128 (8,192 and 2,048
   // columns), and does twice as much.  Of few blocks of k its stores, with no other block on
-  // the CU, are waited for (10,239 rows to 53,277, k 512: 663 and 642, 1,024: 912 and 928).
+  // the CU, are waited for (10,239 rows to 53,277, k 512: 621 and 567, 1,024: 858 and 855).
   if constexpr (sizeof(O) == 2)
     if (words && a.kb > 4 && a.n >= 256 && cdiv(tiles(256, 256), 256) * 8 <= cdiv(tiles(128, 128), 512) * 5)
       return launch_wide<O>(a, stream);

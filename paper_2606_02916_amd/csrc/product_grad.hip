@@ -141,7 +141,8 @@ __device__ __forceinline__ v8bf both(v4s lo, v4s hi) {
 // bf16 gradients into bf16 weights' gradients: tiles of 256 columns of a by 256 of dz, 64
 // rows at a time.  The gradients go to LDS as they are, without a register between; codes
 // times their scales are rounded to bf16 on the way (2^-8 of a term at most, as the
-// result itself), which is a quarter of the matrix unit's time in other operations, where
+// result itself, of which the sum over 16,384 rows is 2.3e-3 off instead of 1.7e-3, root mean
+// squares), which is a quarter of the matrix unit's time in other operations, where
 // scaled gradients, a version for each 128 columns, are more than all of it.  LDS holds
 // rows of 512 bytes, unit u of 32 bytes in place u ^ (row & 7), so that the eight rows
 // that half a wave reads across meet all banks.  Wave (wk, wj) has 128 x 64 of the tile.
